@@ -21,7 +21,7 @@ STATUS = {
     0: "CODECOMP_OK", -1: "CODECOMP_EINVAL_NULL", -2: "CODECOMP_EINVAL_SHAPE", -3: "CODECOMP_EINVAL_WINDOW",
     -4: "CODECOMP_EINVAL_BUDGET", -5: "CODECOMP_EINVAL_POOL", -6: "CODECOMP_EINVAL_HEADS",
     -7: "CODECOMP_EINVAL_HEADDIM", -8: "CODECOMP_EINVAL_SEQLENS", -9: "CODECOMP_EINVAL_WORKSPACE",
-    -10: "CODECOMP_EINVAL_PRIOR", -11: "CODECOMP_EINVAL_MODE",
+    -10: "CODECOMP_EINVAL_PRIOR", -11: "CODECOMP_EINVAL_MODE", -12: "CODECOMP_EINVAL_PAGES",
 }
 
 
@@ -40,6 +40,28 @@ class codecomp_params(C.Structure):
         ("score_variant", C.c_int32), ("kv_dtype", C.c_int32),
         ("score_workgroups", C.c_int32), ("score_lead_tiles", C.c_int32),
     ]
+
+
+class codecomp_pages(C.Structure):
+    _fields_ = [
+        ("k", C.c_void_p), ("v", C.c_void_p), ("n_layers", C.c_int32), ("n_pages", C.c_int32), ("page_size", C.c_int32),
+        ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("kv_dtype", C.c_int32),
+        ("stride_layer", C.c_int64), ("stride_page", C.c_int64), ("stride_head", C.c_int64), ("stride_tok", C.c_int64),
+        ("k_scale", C.c_float), ("v_scale", C.c_float),
+    ]
+
+
+class codecomp_batch(C.Structure):
+    _fields_ = [
+        ("n_seqs", C.c_int32), ("n_q_heads", C.c_int32), ("table_width", C.c_int32), ("max_kv_len", C.c_int32), ("causal", C.c_int32),
+        ("softmax_scale", C.c_float), ("cu_q_host", C.c_void_p), ("cu_q_dev", C.c_void_p), ("kv_lens_dev", C.c_void_p), ("table_dev", C.c_void_p),
+        ("q_stride_tok", C.c_int64), ("q_stride_head", C.c_int64), ("new_stride_tok", C.c_int64), ("new_stride_head", C.c_int64),
+        ("out_stride_tok", C.c_int64), ("out_stride_head", C.c_int64),
+    ]
+
+
+class codecomp_rotary(C.Structure):
+    _fields_ = [("dim", C.c_int32), ("interleaved", C.c_int32), ("inverse", C.c_int32), ("magnitude", C.c_float), ("freq", C.c_double * 64)]
 
 
 class CodecompError(RuntimeError):
@@ -102,6 +124,22 @@ def lib() -> C.CDLL:
         l.codecomp_chunk_budgets.restype = C.c_int
         l.codecomp_chunk_budgets.argtypes = [DP, IP, C.c_int32, C.c_double, C.c_double, C.c_double, C.c_double,
                                              C.c_double, C.c_int32, IP]
+        PP, BP, RP, V = C.POINTER(codecomp_pages), C.POINTER(codecomp_batch), C.POINTER(codecomp_rotary), C.c_void_p
+        for name, args in {
+            "rotary_init": [RP, C.c_int32, C.c_int32, C.c_double, C.c_int32] + [C.c_double] * 4,
+            "rotate": [V, V, RP, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_int64, V, C.c_int64, C.c_int64, V],
+            "append": [V, V, V, V, RP, BP, PP, C.c_int32, V, V],
+            "pages_store": [V, V, V, P, PP, V, C.c_int32, V, V],
+            "pages_load": [PP, V, C.c_int32, V, V, P, V, V, V],
+            "pages_compact": [PP, V, C.c_int32, V, V, P, PP, V, C.c_int32, V, V],
+            "pages_copy": [PP, V, C.c_int32, V],
+            "attend_validate": [BP, PP],
+            "attend": [V, BP, PP, C.c_int32, V, V, V, C.c_size_t, V],
+        }.items():
+            f = getattr(l, "codecomp_" + name)
+            f.restype, f.argtypes = C.c_int, args
+        l.codecomp_attend_workspace_bytes.restype = C.c_size_t
+        l.codecomp_attend_workspace_bytes.argtypes = [BP, PP]
         l.codecomp_status_string.restype = C.c_char_p
         l.codecomp_status_string.argtypes = [C.c_int]
         l.codecomp_version.restype = C.c_int
@@ -260,6 +298,200 @@ def codecomp_chunk_budgets(sigma, chunk_len, *, ratio, m_min, m_max, r_max, eps,
     _check(lib().codecomp_chunk_budgets(_dp(s), ln.ctypes.data_as(ip), len(s), ratio, m_min, m_max, r_max, eps, window,
                                         out.ctypes.data_as(ip)), "codecomp_chunk_budgets")
     return out
+
+
+# ---- serving from a compressed cache (codecomp_cache.h).  Sizes and strides come from the tensors' shapes, so that a call cannot
+# reach outside of them; tensors of another type, shape or device than the call needs are refused with ValueError.
+
+ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_WAVELENGTH, ROTARY_RAMP = 0, 1, 2, 3, 4
+ROTARY_SCALINGS = {"plain": ROTARY_PLAIN, "linear": ROTARY_LINEAR, "base": ROTARY_BASE, "wavelength": ROTARY_WAVELENGTH, "ramp": ROTARY_RAMP}
+
+
+def make_rotary(dim: int, *, base: float = 10000.0, interleaved: bool = False, inverse: bool = False, scaling: int = ROTARY_PLAIN,
+                factor: float = 1.0, context: float = 0.0, low: float = 1.0, high: float = 4.0, magnitude: float = 1.0) -> codecomp_rotary:
+    """Frequencies by codecomp_rotary_init (the meaning of factor, context, low and high per scaling stands there); `freq` may be overwritten."""
+    r = codecomp_rotary()
+    _check(lib().codecomp_rotary_init(C.byref(r), dim, int(interleaved), base, scaling, factor, context, low, high), "codecomp_rotary_init")
+    r.inverse, r.magnitude = int(inverse), magnitude
+    return r
+
+
+def make_pages(k, v, *, k_scale: float = 1.0, v_scale: float = 1.0) -> codecomp_pages:
+    """A pool over two tensors [layers, pages, KV heads, page size, head_dim] with the same strides, bf16 or 8-bit (float8_e4m3fn, or codes as uint8)."""
+    import torch
+    if k.dim() != 5 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.device != v.device:
+        raise ValueError("k and v must be tensors [layers, pages, KV heads, page size, head_dim] of the same shape, strides, type and device")
+    if k.dtype not in (torch.bfloat16, torch.uint8, torch.float8_e4m3fn):
+        raise ValueError(f"a cache holds bfloat16 or 8-bit (float8_e4m3fn, uint8) elements, not {k.dtype}")
+    if k.stride(4) != 1:
+        raise ValueError("the elements of a row must be contiguous")
+    p = codecomp_pages()
+    p.k, p.v = k.data_ptr(), v.data_ptr()
+    p.n_layers, p.n_pages, p.n_kv_heads, p.page_size, p.head_dim = k.shape
+    p.kv_dtype = KV_BF16 if k.dtype == torch.bfloat16 else KV_FP8_E4M3
+    p.stride_layer, p.stride_page, p.stride_head, p.stride_tok = k.stride()[:4]
+    p.k_scale, p.v_scale = k_scale, v_scale
+    p._keep, p._device = (k, v), k.device
+    return p
+
+
+def _int32(t, shape, what: str):
+    import torch
+    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous int32 tensor of shape {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
+
+
+def make_batch(*, n_q_heads: int, cu_q_host: np.ndarray, cu_q, kv_lens, table, max_kv_len: int, causal: bool = True, softmax_scale: float = 0.0,
+               **strides) -> codecomp_batch:
+    """New tokens of n_seqs requests over their caches.  cu_q, kv_lens, table: device int32 tensors [n_seqs + 1], [n_seqs], [n_seqs, width]; the host
+    array cu_q_host (same values as cu_q) sizes the launches.  Strides of q, of new k and v, and of what comes out: 0 or left out = dense."""
+    host = np.ascontiguousarray(cu_q_host, dtype=np.int32)
+    n = len(host) - 1
+    _int32(cu_q, (n + 1,), "cu_q")
+    _int32(kv_lens, (n,), "kv_lens")
+    _int32(table, (n, table.shape[-1]), "table")
+    b = codecomp_batch()
+    b.n_seqs, b.n_q_heads, b.table_width, b.max_kv_len, b.causal, b.softmax_scale = n, n_q_heads, table.shape[1], max_kv_len, int(causal), softmax_scale
+    b.cu_q_host, b.cu_q_dev, b.kv_lens_dev, b.table_dev = host.ctypes.data, cu_q.data_ptr(), kv_lens.data_ptr(), table.data_ptr()
+    for name, val in strides.items():
+        setattr(b, name, val)
+    b._keep, b._tokens, b._device = (host, cu_q, kv_lens, table), int(host[-1]), cu_q.device
+    return b
+
+
+def _on_current(*things) -> None:
+    """All on the device that the stream is of: the library launches on the current device."""
+    import torch
+    at = torch.cuda.current_device()
+    for x in things:
+        dev = getattr(x, "_device", None) or x.device
+        if dev.type != "cuda" or dev.index != at:
+            raise ValueError(f"a tensor is on {dev}, the current device is cuda:{at}")
+
+
+def _vectors(t, what: str, shape, stride_tok: int, stride_head: int) -> int:
+    """bf16 [tokens, heads, head_dim] with the strides that the call will use (0 = dense)."""
+    import torch
+    if t.dtype != torch.bfloat16 or tuple(t.shape) != shape:
+        raise ValueError(f"{what} must be bfloat16 {shape}, not {t.dtype} {tuple(t.shape)}")
+    want = (stride_tok or shape[1] * shape[2], stride_head or shape[2], 1)
+    if any(n > 1 and s != w for n, s, w in zip(t.shape, t.stride(), want)):
+        raise ValueError(f"{what} has strides {t.stride()}, the call goes by {want}")
+    return t.data_ptr()
+
+
+def codecomp_rotate(x, positions, rotary: codecomp_rotary, out) -> None:
+    """x, out: bf16 [tokens, heads, head_dim], any strides of tokens and heads."""
+    import torch
+    if x.dim() != 3 or x.shape != out.shape or x.dtype != torch.bfloat16 or out.dtype != torch.bfloat16 or x.stride(2) != 1 or out.stride(2) != 1:
+        raise ValueError("x and out must be bfloat16 [tokens, heads, head_dim] with contiguous heads")
+    T, H, d = x.shape
+    _int32(positions, (T,), "positions")
+    _on_current(x, positions, out)
+    xs, os_ = x.stride(), out.stride()
+    _check(lib().codecomp_rotate(x.data_ptr(), positions.data_ptr(), C.byref(rotary), T, H, d, xs[0], xs[1], out.data_ptr(), os_[0], os_[1], _stream()),
+           "codecomp_rotate")
+
+
+def codecomp_append(q, k, v, positions, rotary: Optional[codecomp_rotary], batch: codecomp_batch, pages: codecomp_pages, layer: int, q_out) -> None:
+    T, d = batch._tokens, pages.head_dim
+    kv = (T, pages.n_kv_heads, d)
+    kp, vp = _vectors(k, "k", kv, batch.new_stride_tok, batch.new_stride_head), _vectors(v, "v", kv, batch.new_stride_tok, batch.new_stride_head)
+    qp = op = 0
+    if q is not None:
+        qp = _vectors(q, "q", (T, batch.n_q_heads, d), batch.q_stride_tok, batch.q_stride_head)
+    if q_out is not None:
+        op = _vectors(q_out, "q_out", (T, batch.n_q_heads, d), batch.out_stride_tok, batch.out_stride_head)
+    if positions is not None:
+        _int32(positions, (T,), "positions")
+    _on_current(batch, pages, k, v, *(t for t in (q, q_out, positions) if t is not None))
+    _check(lib().codecomp_append(qp, kp, vp, _ptr(positions), None if rotary is None else C.byref(rotary), C.byref(batch), C.byref(pages), layer, op,
+                                 _stream()), "codecomp_append")
+
+
+def _rows(t, params, what: str, total: int, strides) -> int:
+    """Dense rows [layers, KV heads, total, head_dim] in the cache's type with the strides that `params` says."""
+    import torch
+    fp8 = params.kv_dtype == KV_FP8_E4M3
+    shape = (params.n_layers, params.n_kv_heads, total, params.head_dim)
+    if (t.dtype not in (torch.uint8, torch.float8_e4m3fn) if fp8 else t.dtype != torch.bfloat16) or tuple(t.shape) != shape:
+        raise ValueError(f"{what} must be {'8-bit' if fp8 else 'bfloat16'} {shape}, not {t.dtype} {tuple(t.shape)}")
+    want = (strides[0] or shape[1] * shape[2] * shape[3], strides[1] or shape[2] * shape[3], strides[2] or shape[3], 1)
+    if any(n > 1 and s != w for n, s, w in zip(t.shape, t.stride(), want)):
+        raise ValueError(f"{what} has strides {t.stride()}, the call goes by {want}")
+    return t.data_ptr()
+
+
+def _side(params, compact: bool):
+    if compact:
+        return int(params._keep[1][-1]), (params.out_stride_layer, params.out_stride_head, params.out_stride_tok)
+    return int(params._keep[0][-1]), (params.kv_stride_layer, params.kv_stride_head, params.kv_stride_tok)
+
+
+def _table(table, first, params):
+    _int32(table, (params.n_seqs, table.shape[-1]), "table")
+    if first is not None:
+        _int32(first, (params.n_seqs,), "first")
+
+
+def _idx(idx, params):
+    _int32(idx, (params.n_layers, params.n_kv_heads, int(params._keep[1][-1])), "idx")
+
+
+def codecomp_pages_store(k, v, idx, params, pages, table, first=None) -> None:
+    """idx None: the compact k, v [L, H_kv, TB, d] into pages; else rows idx [L, H_kv, TB] of the cache k, v [L, H_kv, T, d]."""
+    total, strides = _side(params, idx is None)
+    _table(table, first, params)
+    if idx is not None:
+        _idx(idx, params)
+    kp, vp = _rows(k, params, "k", total, strides), _rows(v, params, "v", total, strides)
+    _on_current(pages, k, v, table, *(t for t in (idx, first) if t is not None))
+    _check(lib().codecomp_pages_store(kp, vp, _ptr(idx), C.byref(params), C.byref(pages), table.data_ptr(), table.shape[1], _ptr(first), _stream()),
+           "codecomp_pages_store")
+
+
+def codecomp_pages_load(pages, table, first, idx, params, k, v) -> None:
+    """idx None: all rows of the requests into k, v [L, H_kv, T, d]; else rows idx into k, v [L, H_kv, TB, d]."""
+    total, strides = _side(params, idx is not None)
+    _table(table, first, params)
+    if idx is not None:
+        _idx(idx, params)
+    kp, vp = _rows(k, params, "k", total, strides), _rows(v, params, "v", total, strides)
+    _on_current(pages, k, v, table, *(t for t in (idx, first) if t is not None))
+    _check(lib().codecomp_pages_load(C.byref(pages), table.data_ptr(), table.shape[1], _ptr(first), _ptr(idx), C.byref(params), kp, vp, _stream()),
+           "codecomp_pages_load")
+
+
+def codecomp_pages_compact(pages, table, first, idx, params, to, to_table, to_first=None) -> None:
+    _table(table, first, params)
+    _table(to_table, to_first, params)
+    _idx(idx, params)
+    _on_current(pages, to, table, to_table, idx, *(t for t in (first, to_first) if t is not None))
+    _check(lib().codecomp_pages_compact(C.byref(pages), table.data_ptr(), table.shape[1], _ptr(first), idx.data_ptr(), C.byref(params), C.byref(to),
+                                        to_table.data_ptr(), to_table.shape[1], _ptr(to_first), _stream()), "codecomp_pages_compact")
+
+
+def codecomp_pages_copy(pages, pairs) -> None:
+    """pairs: device int32 [n, 2], (source page, target page)."""
+    _int32(pairs, (pairs.shape[0], 2), "pairs")
+    _on_current(pages, pairs)
+    _check(lib().codecomp_pages_copy(C.byref(pages), pairs.data_ptr(), pairs.shape[0], _stream()), "codecomp_pages_copy")
+
+
+def codecomp_attend_workspace_bytes(batch, pages) -> int:
+    _check(lib().codecomp_attend_validate(C.byref(batch), C.byref(pages)), "codecomp_attend_validate")
+    return lib().codecomp_attend_workspace_bytes(C.byref(batch), C.byref(pages))
+
+
+def codecomp_attend(q, batch: codecomp_batch, pages: codecomp_pages, layer: int, out, workspace, lse=None) -> None:
+    import torch
+    shape = (batch._tokens, batch.n_q_heads, pages.head_dim)
+    qp, op = _vectors(q, "q", shape, batch.q_stride_tok, batch.q_stride_head), _vectors(out, "out", shape, batch.out_stride_tok, batch.out_stride_head)
+    if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != shape[:2] or not lse.is_contiguous()):
+        raise ValueError(f"lse must be a contiguous float32 tensor {shape[:2]}, not {lse.dtype} {tuple(lse.shape)}")
+    _on_current(batch, pages, q, out, *(t for t in (lse, workspace) if t is not None))
+    size = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib().codecomp_attend(qp, C.byref(batch), C.byref(pages), layer, op, _ptr(lse), _ptr(workspace), size, _stream()), "codecomp_attend")
 
 
 class DeviceProblem:

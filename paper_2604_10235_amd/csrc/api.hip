@@ -3,6 +3,7 @@
 // the first HIP call so that rejected arguments never reach a GPU.
 #include <math.h>
 
+#include "codecomp_cache.h"
 #include "plan.h"
 
 namespace codecomp {
@@ -510,6 +511,7 @@ const char* codecomp_status_string(int status) {
     case CODECOMP_EINVAL_WORKSPACE: return "workspace is NULL, not 256-byte aligned or too small";
     case CODECOMP_EINVAL_PRIOR: return "prior_weight / softmax_scale must be finite and >= 0";
     case CODECOMP_EINVAL_MODE: return "select_mode unknown or wrong for this call, or span budget out of range";
+    case CODECOMP_EINVAL_PAGES: return "page pool, page table, layer or max_kv_len out of order";
     default: return status > 0 ? "HIP runtime error (hipError_t value)" : "unknown status";
   }
 }
