@@ -1,0 +1,85 @@
+// Internal header: what the kernels of codecomp_attend share.
+#pragma once
+#include "cache.h"
+
+namespace codecomp {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+// A row's reference (what is subtracted from its logits before exp2) only moves when a logit is this far above it: weights up to 2^8
+// lose nothing in fp32 or in bf16, and most tiles then leave the sums and the outputs as they are.
+constexpr float kSlack = 8.0f;
+
+struct AttendArgs {
+  PagePool pool;
+  PagedBatch b;
+  const uint16_t* q;
+  uint16_t* out;
+  float* lse;
+  float* part_o;               // [part][rows of a part][D], not yet divided by the sum of weights
+  float* part_ml;              // [part][rows of a part][2]: reference, sum of weights
+  int64_t layer;               // byte offset of the layer in the pool
+  float c;                     // softmax_scale * k_scale * log2(e): logits in powers of two
+  int chunk, splits;           // few rows
+};
+
+__device__ __forceinline__ bf16x8 frag(u32x4 v) { return __builtin_bit_cast(bf16x8, v); }
+__device__ __forceinline__ unsigned pack2(float a, float b) { return __builtin_bit_cast(unsigned, bf16x2{(__bf16)a, (__bf16)b}); }
+
+// 8 E4M3 codes as 8 bf16: every E4M3 number is a bf16 number.
+__device__ __forceinline__ u32x4 widen8(unsigned a, unsigned b) {
+  u32x4 r;
+  r.x = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, false));
+  r.y = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, true));
+  r.z = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, false));
+  r.w = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true));
+  return r;
+}
+
+// Whether a 16-byte piece holds an infinity or NaN (E4M3 has no infinity).
+template <bool FP8>
+__device__ __forceinline__ bool not_finite(u32x4 v) {
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (FP8) {
+      const unsigned x = (v[i] & 0x7F7F7F7Fu) ^ 0x7F7F7F7Fu;       // a zero byte is a NaN
+      bad |= ((x - 0x01010101u) & ~x & 0x80808080u) != 0;
+    } else {
+      bad |= (v[i] & 0x7F80u) == 0x7F80u || (v[i] & 0x7F800000u) == 0x7F800000u;
+    }
+  }
+  return bad;
+}
+
+// 4 elements of a stored row as floats.
+template <bool FP8>
+__device__ __forceinline__ f32x4 row4(const unsigned char* p) {
+  f32x4 r;
+  if constexpr (FP8) {
+    const unsigned x = *reinterpret_cast<const unsigned*>(p);
+    const unsigned lo = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, false));
+    const unsigned hi = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, 1.0f, true));
+    r = f32x4{__uint_as_float(lo << 16), __uint_as_float(lo & 0xFFFF0000u), __uint_as_float(hi << 16), __uint_as_float(hi & 0xFFFF0000u)};
+  } else {
+    const u32x2 x = *reinterpret_cast<const u32x2*>(p);
+    r = f32x4{__uint_as_float(x.x << 16), __uint_as_float(x.x & 0xFFFF0000u), __uint_as_float(x.y << 16), __uint_as_float(x.y & 0xFFFF0000u)};
+  }
+  return r;
+}
+
+// The transposing read: a group of 16 lanes addresses four rows of 16 elements in LDS, four lanes a row, and lane i gets column i.
+__device__ __forceinline__ s16x4 read_columns(const unsigned char* lds) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)lds);
+}
+
+int launch_few(const AttendPlan& pl, AttendArgs a, hipStream_t stream);
+
+}  // namespace codecomp

@@ -1,89 +1,121 @@
-// Attention of new tokens over a paged cache.
+// codecomp_attend: which kernels a batch takes, and the workspace they share.
 #include <math.h>
 
-#include "cache.h"
+#include "attend_many.h"
 
 namespace codecomp {
 
-struct AttendArgs {
-  PagePool pool;
-  PagedBatch b;
-  const uint16_t* q;
-  uint16_t* out;
-  float* lse;
-  int64_t layer;
-  float scale;
-  int d;
-};
+extern template int launch_many_of<64, false>(const ManyArgs&, hipStream_t);
+extern template int launch_many_of<64, true>(const ManyArgs&, hipStream_t);
+extern template int launch_many_of<128, false>(const ManyArgs&, hipStream_t);
+extern template int launch_many_of<128, true>(const ManyArgs&, hipStream_t);
 
-__device__ __forceinline__ float element(const unsigned char* p, int i, bool fp8) {
-  if (!fp8) return __uint_as_float((unsigned)reinterpret_cast<const uint16_t*>(p)[i] << 16);
-  return __builtin_amdgcn_cvt_f32_fp8((int)p[i], 0);
-}
+constexpr int kFewRowsMost = 64;          // rows of a request up to which it takes attend_few_kernel
 
-// One wave per (token, query head): logits of 64 keys, a lane each, then the weighted rows, two elements a lane.
-__global__ __launch_bounds__(64) void attend_plain_kernel(const AttendArgs a) {
-  const int t = blockIdx.x, h = blockIdx.y, lane = threadIdx.x, kvh = h / a.b.G;
-  const int r = request_of(a.b.cu_q, a.b.n_seqs, t);
-  const int len = kv_len_of(a.b, r), at = len - a.b.cu_q[r + 1] + t;
-  const int seen = a.b.causal ? max(min(len, at + 1), 0) : len;
-  __shared__ float q[128];
-  for (int i = lane; i < a.d; i += 64) q[i] = element(reinterpret_cast<const unsigned char*>(a.q + t * a.b.q_st + h * a.b.q_sh), i, false);
-  __syncthreads();
-  float top = -INFINITY, sum = 0.0f, o0 = 0.0f, o1 = 0.0f;
-  for (int key0 = 0; key0 < seen; key0 += 64) {
-    const int key = key0 + lane;
-    int64_t row = -1;
-    float x = -INFINITY;
-    if (key < seen) {
-      const int page = a.b.table[(int64_t)r * a.b.table_width + (key >> a.pool.page_log2)];
-      if (page >= 0 && page < a.pool.n_pages)
-        row = a.layer + page * a.pool.s_page + kvh * a.pool.s_head + (key & ((1 << a.pool.page_log2) - 1)) * a.pool.s_tok;
-    }
-    if (row >= 0) {
-      x = 0.0f;
-      for (int i = 0; i < a.d; ++i) x = fmaf(q[i], element(a.pool.k + row, i, a.pool.fp8), x);
-      x *= a.scale * a.pool.k_scale;
-    }
-    float m = x;
-    for (int off = 1; off < 64; off <<= 1) m = fmaxf(m, __shfl_xor(m, off));
-    if (m == -INFINITY) continue;
-    const float to = fmaxf(top, m), old = expf(top - to);
-    const float p = row >= 0 ? expf(x - to) : 0.0f;
-    top = to; sum = sum * old + p; o0 *= old; o1 *= old;
-    for (int j = 0; j < min(64, seen - key0); ++j) {
-      const int64_t vrow = __shfl(row, j);
-      const float w = __shfl(p, j);
-      if (vrow < 0) continue;
-      const int e = lane * (a.d / 64);
-      o0 = fmaf(w, element(a.pool.v + vrow, e, a.pool.fp8), o0);
-      if (a.d == 128) o1 = fmaf(w, element(a.pool.v + vrow, e + 1, a.pool.fp8), o1);
-    }
-  }
-  for (int off = 1; off < 64; off <<= 1) sum += __shfl_xor(sum, off);
-  const float inv = sum > 0.0f ? a.pool.v_scale / sum : sum;
-  __bf16* o = reinterpret_cast<__bf16*>(a.out + t * a.b.o_st + h * a.b.o_sh) + lane * (a.d / 64);
-  o[0] = (__bf16)(o0 * inv);
-  if (a.d == 128) o[1] = (__bf16)(o1 * inv);
-  if (a.lse && lane == 0) a.lse[(int64_t)t * a.b.Hq + h] = top == -INFINITY ? -INFINITY : top + logf(sum);
-}
+static size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 int make_attend_plan(const codecomp_batch* b, const codecomp_pages* p, AttendPlan* pl) {
   if (int rc = make_pool(p, &pl->pool)) return rc;
   if (int rc = make_batch(b, p, &pl->batch)) return rc;
-  if (pl->batch.Hq > 65535) return CODECOMP_EINVAL_HEADS;
+  const PagedBatch& x = pl->batch;
   pl->d = p->head_dim;
   pl->scale = b->softmax_scale > 0.0f ? b->softmax_scale : 1.0f / sqrtf((float)p->head_dim);
-  pl->ws_bytes = 0;
+  int few_most = 0;
+  pl->few_rows = pl->many_rows = 0;
+  for (int r = 0; r < x.n_seqs; ++r) {
+    const int64_t rows = (int64_t)(b->cu_q_host[r + 1] - b->cu_q_host[r]) * x.G;
+    if (rows == 0) continue;
+    if (rows > kFewRowsMost) { ++pl->many_rows; continue; }
+    ++pl->few_rows;
+    if (rows > few_most) few_most = (int)rows;
+  }
+  pl->row_blocks = few_most <= 16 ? 1 : few_most <= 32 ? 2 : 4;
+  const int64_t items = (int64_t)x.n_seqs * x.Hkv;
+  // chunks of keys: about four workgroups per compute unit if all requests are of the largest length, of at least 128 keys each
+  int64_t chunk = (items * x.max_kv / 1024 + 127) / 128 * 128;
+  if (chunk < 128) chunk = 128;
+  if (chunk > 2048) chunk = 2048;
+  while ((x.max_kv + chunk - 1) / chunk > kFewMostSplits) chunk *= 2;
+  pl->chunk = (int)chunk;
+  pl->splits = x.max_kv > chunk ? (int)((x.max_kv + chunk - 1) / chunk) : 1;
+  if (items * pl->splits * 64 > INT32_MAX) return CODECOMP_EINVAL_SHAPE;
+  size_t off = 0;
+  pl->off_few = off;
+  if (pl->few_rows > 0 && pl->splits > 1) off = align256(off + (size_t)(items * pl->splits * 16 * pl->row_blocks) * (p->head_dim + 2) * sizeof(float));
+  pl->off_many = off;
+  pl->workgroups = p->head_dim == 128 ? 256 : 512;
+  if (pl->many_rows > 0)
+    off = align256(off + (size_t)pl->workgroups * 2 * kManyRows * (p->head_dim + 2) * sizeof(float) + pl->workgroups * sizeof(CutBlock));
+  pl->ws_bytes = off;
   return CODECOMP_OK;
 }
 
-int launch_attend(const AttendPlan& pl, const void* q, int layer, void* out, float* lse, void* workspace, hipStream_t stream) {
-  AttendArgs a;
-  a.pool = pl.pool; a.b = pl.batch; a.q = static_cast<const uint16_t*>(q); a.out = static_cast<uint16_t*>(out); a.lse = lse;
-  a.layer = layer * pl.pool.s_layer; a.scale = pl.scale; a.d = pl.d;
-  attend_plain_kernel<<<dim3(pl.batch.T, pl.batch.Hq), dim3(64), 0, stream>>>(a);
+// Blocks of rows whose keys several workgroups shared: blockIdx.x the workgroup that has a block's first part, blockIdx.y 16 of its rows.
+template <int D>
+__global__ __launch_bounds__(256) void join_many_kernel(const ManyArgs ma) {
+  const AttendArgs& a = ma.a;
+  const CutBlock cut = ma.cuts[blockIdx.x];
+  if (cut.r < 0) return;
+  constexpr int E = D / 16;
+  const int tid = threadIdx.x, in_block = blockIdx.y * 16 + (tid >> 4), e = (tid & 15) * E;
+  const int q0 = a.b.cu_q[cut.r], rows = (a.b.cu_q[cut.r + 1] - q0) * a.b.G, row = cut.block * kManyRows + in_block;
+  if (row >= rows) return;
+  float top = -1.0e30f, all = 0.0f, x[E];
+#pragma unroll
+  for (int i = 0; i < E; ++i) x[i] = 0.0f;
+  for (int g = blockIdx.x; g <= cut.last; ++g) {
+    const int64_t part = (int64_t)(g == (int)blockIdx.x ? cut.first_slot : 2 * g) * kManyRows + in_block;
+    const float m = a.part_ml[2 * part], l = a.part_ml[2 * part + 1];
+    const float to = fmaxf(top, m), old = top == to ? 1.0f : __builtin_amdgcn_exp2f(top - to), f = m == to ? 1.0f : __builtin_amdgcn_exp2f(m - to);
+    top = to;
+    all = all * old + l * f;
+#pragma unroll
+    for (int i = 0; i < E; i += 4) {
+      const f32x4 v = *reinterpret_cast<const f32x4*>(a.part_o + part * D + e + i);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[i + j] = x[i + j] * old + v[j] * f;
+    }
+  }
+  const int t = row / a.b.G, h = cut.head * a.b.G + row - t * a.b.G;
+  const float inv = all == 0.0f ? 0.0f : a.pool.v_scale / all;
+  uint16_t* out = a.out + (q0 + t) * a.b.o_st + h * a.b.o_sh + e;
+#pragma unroll
+  for (int i = 0; i < E; i += 2) *reinterpret_cast<unsigned*>(out + i) = pack2(x[i] * inv, x[i + 1] * inv);
+  if (a.lse && (tid & 15) == 0) a.lse[(int64_t)(q0 + t) * a.b.Hq + h] = all == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(all)) * kLn2;
+}
+
+static int launch_many(const AttendPlan& pl, const AttendArgs& a, char* workspace, hipStream_t stream) {
+  ManyArgs m;
+  m.a = a;
+  m.workgroups = pl.workgroups;
+  m.few_rows_most = kFewRowsMost;
+  m.a.part_o = reinterpret_cast<float*>(workspace);
+  m.a.part_ml = m.a.part_o + (size_t)pl.workgroups * 2 * kManyRows * pl.d;
+  m.cuts = reinterpret_cast<CutBlock*>(m.a.part_ml + (size_t)pl.workgroups * 2 * kManyRows * 2);
+  int rc;
+  if (pl.d == 128) rc = pl.pool.fp8 ? launch_many_of<128, true>(m, stream) : launch_many_of<128, false>(m, stream);
+  else rc = pl.pool.fp8 ? launch_many_of<64, true>(m, stream) : launch_many_of<64, false>(m, stream);
+  if (rc) return rc;
+  const dim3 grid(pl.workgroups, kManyRows / 16), block(256);
+  if (pl.d == 128) join_many_kernel<128><<<grid, block, 0, stream>>>(m);
+  else join_many_kernel<64><<<grid, block, 0, stream>>>(m);
   return (int)hipGetLastError();
+}
+
+int launch_attend(const AttendPlan& pl, const void* q, int layer, void* out, float* lse, void* workspace, hipStream_t stream) {
+  AttendArgs a = {};
+  a.pool = pl.pool; a.b = pl.batch; a.q = static_cast<const uint16_t*>(q); a.out = static_cast<uint16_t*>(out); a.lse = lse;
+  a.layer = layer * pl.pool.s_layer;
+  a.c = pl.scale * pl.pool.k_scale * kLog2e;
+  a.chunk = pl.chunk; a.splits = pl.splits;
+  if (pl.few_rows > 0) {
+    a.part_o = reinterpret_cast<float*>(static_cast<char*>(workspace) + pl.off_few);
+    a.part_ml = a.part_o + (size_t)pl.batch.n_seqs * pl.batch.Hkv * pl.splits * 16 * pl.row_blocks * pl.d;
+    if (int rc = launch_few(pl, a, stream)) return rc;
+  }
+  if (pl.many_rows > 0)
+    if (int rc = launch_many(pl, a, static_cast<char*>(workspace) + pl.off_many, stream)) return rc;
+  return 0;
 }
 
 }  // namespace codecomp

@@ -1,0 +1,367 @@
+// Attention of requests with few rows (new tokens x query heads per KV head, up to 64): the step of one token, and short chunks.
+//
+// Every key and value is read once for a handful of products: bound by memory.  So the cache is cut into chunks of keys, one workgroup of four
+// waves per (request, KV head, chunk), each wave with tiles of 32 keys of its own: a tile is on its way into registers while the one
+// before it is multiplied, and no wave waits for another until the chunk is done.  Chunks are joined by a second kernel (a row's
+// reference, sum of weights and unscaled output each), in order.
+//
+// Per tile, S^T = K Q^T (lane = row; 16 keys x 16 rows per MFMA), weights exp2(c s - reference) in place, O^T += V^T P^T.  The
+// order of keys inside an MFMA's contraction is free, and chosen so that a lane's weights are the right operand as they stand (keys 4 q + i
+// and 16 + 4 q + i of lane group q); V^T is read from LDS by the transposing read.  A weight enters the product as two bf16, its
+// rounded value and the rest: 16 bits of it, for MFMA time that memory hides.
+#include "attend.h"
+
+namespace codecomp {
+
+constexpr int kFewWaves = 4, kFewKeys = 32;
+
+template <int D, bool FP8>
+struct FewTile {
+  static constexpr int PIECES = D * (FP8 ? 1 : 2) / 16;      // 16-byte pieces of a stored row
+  static constexpr int ROWS = 64 / PIECES;                    // rows that a load instruction of the wave takes
+  static constexpr int LOADS = kFewKeys / ROWS;
+  // Bytes between rows in LDS: 16 rows of K fragments, and two groups of four V rows, hit all banks once.
+  static constexpr int K_ROW = 2 * D + 16, V_ROW = 2 * D + 32;
+  static constexpr int BYTES = kFewKeys * (K_ROW + V_ROW);
+};
+
+template <int D, bool FP8, int RB>
+__global__ __launch_bounds__(64 * kFewWaves, RB == 4 ? 1 : 2) void attend_few_kernel(const AttendArgs a) {
+  using T = FewTile<D, FP8>;
+  constexpr int KS = D / 32, DB = D / 16;
+  __shared__ __attribute__((aligned(16))) unsigned char lds[kFewWaves * T::BYTES];
+  __shared__ float row_m[kFewWaves][16], row_l[kFewWaves][16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, quarter = lane >> 4;
+  const int split = blockIdx.x % a.splits, item = blockIdx.x / a.splits;
+  const int r = item / a.b.Hkv, head = item - r * a.b.Hkv;
+  const int q0 = a.b.cu_q[r], nq = a.b.cu_q[r + 1] - q0, rows = nq * a.b.G;
+  if (rows == 0 || rows > 16 * RB) return;
+  const int len = kv_len_of(a.b, r);
+  const int key0 = split * a.chunk, key1 = min(len, key0 + a.chunk);
+  if (split > 0 && key0 >= len) return;
+  const bool whole = len <= a.chunk;                            // the only chunk
+
+  // query rows as right operands: row r16 of block rb, elements 32 ks + 8 quarter ..
+  u32x4 qf[RB][KS];
+  int limit[RB];                                                // keys that the lane's row sees
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    const int row = rb * 16 + l16, t = min(row, rows - 1) / a.b.G, g = min(row, rows - 1) - t * a.b.G;
+    const uint16_t* p = a.q + (q0 + t) * a.b.q_st + (head * a.b.G + g) * a.b.q_sh + quarter * 8;
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      qf[rb][ks] = *reinterpret_cast<const u32x4*>(p + ks * 32);
+      if (row >= rows) qf[rb][ks] = u32x4{0, 0, 0, 0};
+    }
+    limit[rb] = a.b.causal ? min(len, len - nq + t + 1) : len;
+  }
+  const int seen_by_all = a.b.causal ? len - nq + 1 : len;
+
+  const unsigned char* kb = a.pool.k + a.layer + head * a.pool.s_head + (lane % T::PIECES) * 16;
+  const unsigned char* vb = a.pool.v + a.layer + head * a.pool.s_head + (lane % T::PIECES) * 16;
+  const int32_t* table = a.b.table + (int64_t)r * a.b.table_width;
+  const int in_page = (1 << a.pool.page_log2) - 1;
+  unsigned char* ks_lds = lds + wave * T::BYTES;
+  unsigned char* vs_lds = ks_lds + kFewKeys * T::K_ROW;
+
+  // page of key tile + lane % 32; -1: no such key
+  auto look_up = [&](int tile) {
+    const int key = tile + (lane & 31);
+    int page = -1;
+    if (key < key1) {
+      page = table[key >> a.pool.page_log2];
+      if (page >= a.pool.n_pages) page = -1;
+    }
+    return page;
+  };
+  u32x4 kr[T::LOADS], vr[T::LOADS];
+  auto send_for = [&](int tile, int page) {
+#pragma unroll
+    for (int i = 0; i < T::LOADS; ++i) {
+      const int row = i * T::ROWS + lane / T::PIECES;
+      const int at = max(__shfl(page, row), 0);                  // rows that are not there: page 0, zeroed below
+      const int64_t off = at * a.pool.s_page + ((tile + row) & in_page) * a.pool.s_tok;
+      kr[i] = *reinterpret_cast<const u32x4*>(kb + off);
+      vr[i] = *reinterpret_cast<const u32x4*>(vb + off);
+    }
+  };
+
+  f32x4 o[RB][DB];
+  float m[RB], l[RB];
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    m[rb] = -INFINITY; l[rb] = 0.0f;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) o[rb][db] = f32x4{0, 0, 0, 0};
+  }
+
+  int tile = key0 + wave * kFewKeys;
+  int page = look_up(tile), next_page = 0;
+  if (tile < key1) {
+    send_for(tile, page);
+    next_page = look_up(tile + kFewWaves * kFewKeys);
+  }
+  for (; tile < key1; tile += kFewWaves * kFewKeys) {
+    const unsigned valid = (unsigned)__ballot(page >= 0);        // lanes 0 .. 31: the keys of the tile
+    const bool plain = valid == 0xFFFFFFFFu && tile + kFewKeys <= seen_by_all;
+    unsigned apart = 0;                                          // keys whose values are added by themselves, below
+    if (__builtin_expect(!plain, 0)) {
+      // Values that some row does not see must not meet its weight of zero in a product if they are infinite or NaN.
+      if (tile + kFewKeys > seen_by_all && seen_by_all < len) {
+#pragma unroll
+        for (int i = 0; i < T::LOADS; ++i) {
+          const uint64_t bad = __ballot(not_finite<FP8>(vr[i]));
+#pragma unroll
+          for (int j = 0; j < T::ROWS; ++j)
+            if ((bad >> (j * T::PIECES)) & ((1ull << T::PIECES) - 1)) apart |= 1u << (i * T::ROWS + j);
+        }
+        apart &= valid;
+      }
+#pragma unroll
+      for (int i = 0; i < T::LOADS; ++i) {
+        const int row = i * T::ROWS + lane / T::PIECES;
+        if (!((valid >> row) & 1)) kr[i] = vr[i] = u32x4{0, 0, 0, 0};
+        if ((apart >> row) & 1) vr[i] = u32x4{0, 0, 0, 0};
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < T::LOADS; ++i) {
+      const int row = i * T::ROWS + lane / T::PIECES, col = lane % T::PIECES;
+      if constexpr (FP8) {
+        *reinterpret_cast<u32x4*>(ks_lds + row * T::K_ROW + col * 32) = widen8(kr[i].x, kr[i].y);
+        *reinterpret_cast<u32x4*>(ks_lds + row * T::K_ROW + col * 32 + 16) = widen8(kr[i].z, kr[i].w);
+        *reinterpret_cast<u32x4*>(vs_lds + row * T::V_ROW + col * 32) = widen8(vr[i].x, vr[i].y);
+        *reinterpret_cast<u32x4*>(vs_lds + row * T::V_ROW + col * 32 + 16) = widen8(vr[i].z, vr[i].w);
+      } else {
+        *reinterpret_cast<u32x4*>(ks_lds + row * T::K_ROW + col * 16) = kr[i];
+        *reinterpret_cast<u32x4*>(vs_lds + row * T::V_ROW + col * 16) = vr[i];
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+    const int this_page = page;
+    page = next_page;
+    if (tile + kFewWaves * kFewKeys < key1) {
+      send_for(tile + kFewWaves * kFewKeys, page);
+      next_page = look_up(tile + 2 * kFewWaves * kFewKeys);
+    }
+
+    f32x4 s[RB][2];
+#pragma unroll
+    for (int kb2 = 0; kb2 < 2; ++kb2) {
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) s[rb][kb2] = f32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const u32x4 kf = *reinterpret_cast<const u32x4*>(ks_lds + (kb2 * 16 + l16) * T::K_ROW + ks * 64 + quarter * 16);
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) s[rb][kb2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(kf), frag(qf[rb][ks]), s[rb][kb2], 0, 0, 0);
+      }
+    }
+    float p[RB][8];
+    bool grows = false;
+    float top[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) p[rb][i] = s[rb][i >> 2][i & 3] * a.c;
+      if (__builtin_expect(!plain, 0)) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int j = (i >> 2) * 16 + quarter * 4 + (i & 3);
+          if (!((valid >> j) & 1) || tile + j >= limit[rb]) p[rb][i] = -INFINITY;
+        }
+      }
+      float x = fmaxf(fmaxf(fmaxf(p[rb][0], p[rb][1]), fmaxf(p[rb][2], p[rb][3])), fmaxf(fmaxf(p[rb][4], p[rb][5]), fmaxf(p[rb][6], p[rb][7])));
+      x = fmaxf(x, __shfl_xor(x, 16));
+      x = fmaxf(x, __shfl_xor(x, 32));
+      top[rb] = x;
+      grows |= x > m[rb] + kSlack;
+    }
+    if (__builtin_expect(__ballot(grows) != 0, 0)) {
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        const float to = fmaxf(m[rb], top[rb]);
+        const float old = to == m[rb] ? 1.0f : __builtin_amdgcn_exp2f(m[rb] - to);
+        m[rb] = to;
+        l[rb] *= old;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) o[rb][db] *= old;
+      }
+    }
+    bf16x8 hi[RB], lo[RB];
+#pragma unroll
+    for (int rb = 0; rb < RB; ++rb) {
+      const float ref = m[rb] == -INFINITY ? 0.0f : m[rb];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        p[rb][i] = __builtin_amdgcn_exp2f(p[rb][i] - ref);
+        l[rb] += p[rb][i];
+      }
+      u32x4 h, w;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        h[i] = pack2(p[rb][2 * i], p[rb][2 * i + 1]);
+        w[i] = pack2(p[rb][2 * i] - __uint_as_float(h[i] << 16), p[rb][2 * i + 1] - __uint_as_float(h[i] & 0xFFFF0000u));
+      }
+      hi[rb] = frag(h); lo[rb] = frag(w);
+    }
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+      const unsigned char* at = vs_lds + (quarter * 4 + (l16 >> 2)) * T::V_ROW + db * 32 + (l16 & 3) * 8;
+      const s16x4 v0 = read_columns(at), v1 = read_columns(at + 16 * T::V_ROW);
+      const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        o[rb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, hi[rb], o[rb][db], 0, 0, 0);
+        o[rb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, lo[rb], o[rb][db], 0, 0, 0);
+      }
+    }
+    while (__builtin_expect(apart != 0, 0)) {
+      const int j = __ffs(apart) - 1;
+      apart &= apart - 1;
+      const unsigned char* row = a.pool.v + a.layer + head * a.pool.s_head + __shfl(this_page, j) * a.pool.s_page + ((tile + j) & in_page) * a.pool.s_tok;
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) {
+        float w = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if ((i >> 2) == (j >> 4) && (i & 3) == (j & 3)) w = p[rb][i];
+        w = __shfl(w, ((j & 15) >> 2) * 16 + l16);
+        const bool sees = tile + j < limit[rb];
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          const f32x4 v = row4<FP8>(row + (db * 16 + quarter * 4) * (FP8 ? 1 : 2));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[rb][db][i] = sees ? fmaf(w, v[i], o[rb][db][i]) : o[rb][db][i];
+        }
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+
+  // the four waves' shares of every row, 16 rows at a time
+  constexpr int O_ROW = D + 4;
+  float* o_lds = reinterpret_cast<float*>(lds);
+  static_assert(kFewWaves * 16 * O_ROW * 4 <= kFewWaves * T::BYTES, "rows of a block fit the tiles");
+#pragma unroll
+  for (int rb = 0; rb < RB; ++rb) {
+    if (rb * 16 >= rows) break;
+    float sum = l[rb];
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    __syncthreads();
+    if (quarter == 0) { row_m[wave][l16] = m[rb]; row_l[wave][l16] = sum; }
+#pragma unroll
+    for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4*>(o_lds + (wave * 16 + l16) * O_ROW + db * 16 + quarter * 4) = o[rb][db];
+    __syncthreads();
+    constexpr int E = D / 16;                                   // elements of a row per thread
+    const int n = tid >> 4, row = rb * 16 + n, e = (tid & 15) * E;
+    if (row < rows) {
+      float to = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < kFewWaves; ++w) to = fmaxf(to, row_m[w][n]);
+      float all = 0.0f, x[E];
+#pragma unroll
+      for (int i = 0; i < E; ++i) x[i] = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kFewWaves; ++w) {
+        const float f = row_m[w][n] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(row_m[w][n] - to);
+        if (row_m[w][n] == -INFINITY && !(row_l[w][n] != row_l[w][n])) continue;          // saw nothing
+        all += f * row_l[w][n];
+#pragma unroll
+        for (int i = 0; i < E; ++i) x[i] += f * o_lds[(w * 16 + n) * O_ROW + e + i];
+      }
+      if (whole) {
+        const int t = row / a.b.G, h = head * a.b.G + row - t * a.b.G;
+        const float inv = all == 0.0f ? 0.0f : a.pool.v_scale / all;
+        uint16_t* out = a.out + (q0 + t) * a.b.o_st + h * a.b.o_sh + e;
+#pragma unroll
+        for (int i = 0; i < E; i += 2) *reinterpret_cast<unsigned*>(out + i) = pack2(x[i] * inv, x[i + 1] * inv);
+        if (a.lse && (tid & 15) == 0) a.lse[(int64_t)(q0 + t) * a.b.Hq + h] = all == 0.0f ? -INFINITY : (to + __builtin_amdgcn_logf(all)) * kLn2;
+      } else {
+        const int64_t part = (int64_t)blockIdx.x * (16 * RB) + row;
+#pragma unroll
+        for (int i = 0; i < E; i += 4) *reinterpret_cast<f32x4*>(a.part_o + part * D + e + i) = f32x4{x[i], x[i + 1], x[i + 2], x[i + 3]};
+        if ((tid & 15) == 0) { a.part_ml[2 * part] = to; a.part_ml[2 * part + 1] = all; }
+      }
+    }
+  }
+}
+
+// Chunks joined: a workgroup per row.  Weights of all chunks first, then the outputs, four elements a thread, the chunks shared out over
+// the workgroup's groups of D / 4 threads and these added up in order.
+template <int D>
+__global__ __launch_bounds__(256) void join_few_kernel(const AttendArgs a, int row_slots) {
+  constexpr int GROUPS = 256 / (D / 4);
+  __shared__ float weight[kFewMostSplits];
+  __shared__ float red[4];
+  __shared__ f32x4 sums[GROUPS][D / 4];
+  const int row = blockIdx.x % row_slots, item = blockIdx.x / row_slots, tid = threadIdx.x;
+  const int r = item / a.b.Hkv, head = item - r * a.b.Hkv;
+  const int q0 = a.b.cu_q[r], rows = (a.b.cu_q[r + 1] - q0) * a.b.G;
+  if (rows > row_slots || row >= rows) return;
+  const int len = kv_len_of(a.b, r);
+  if (len <= a.chunk) return;                                  // written by its only chunk
+  const int n = (len + a.chunk - 1) / a.chunk;
+  const int64_t part0 = (int64_t)item * a.splits * row_slots + row;       // of chunk s: + s * row_slots
+  float top = -INFINITY;
+  for (int s = tid; s < n; s += 256) {
+    const float m = a.part_ml[2 * (part0 + (int64_t)s * row_slots)];
+    weight[s] = m;
+    top = fmaxf(top, m);
+  }
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) top = fmaxf(top, __shfl_xor(top, off));
+  if ((tid & 63) == 0) red[tid >> 6] = top;
+  __syncthreads();
+  top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  __syncthreads();
+  float all = 0.0f;
+  for (int s = tid; s < n; s += 256) {
+    const float f = weight[s] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(weight[s] - top);
+    const float l = a.part_ml[2 * (part0 + (int64_t)s * row_slots) + 1];
+    weight[s] = f;
+    all += l != l ? l : f * l;
+  }
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) all += __shfl_xor(all, off);
+  if ((tid & 63) == 0) red[tid >> 6] = all;
+  __syncthreads();
+  all = red[0] + red[1] + red[2] + red[3];
+  const int group = tid / (D / 4), e = tid % (D / 4);
+  f32x4 x = {0, 0, 0, 0};
+#pragma unroll 8
+  for (int s = group; s < n; s += GROUPS) {
+    const f32x4 v = *reinterpret_cast<const f32x4*>(a.part_o + (part0 + (int64_t)s * row_slots) * D + e * 4);
+    x += v * weight[s];
+  }
+  sums[group][e] = x;
+  __syncthreads();
+  if (group == 0) {
+#pragma unroll
+    for (int g = 1; g < GROUPS; ++g) x += sums[g][e];
+    const float inv = all == 0.0f ? 0.0f : a.pool.v_scale / all;
+    const int t = row / a.b.G, h = head * a.b.G + row - t * a.b.G;
+    *reinterpret_cast<u32x2*>(a.out + (q0 + t) * a.b.o_st + h * a.b.o_sh + e * 4) = u32x2{pack2(x.x * inv, x.y * inv), pack2(x.z * inv, x.w * inv)};
+    if (a.lse && e == 0) a.lse[(int64_t)(q0 + t) * a.b.Hq + h] = all == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(all)) * kLn2;
+  }
+}
+
+template <int D, bool FP8>
+static int launch_few_of(const AttendPlan& pl, const AttendArgs& a, hipStream_t stream) {
+  const int64_t items = (int64_t)a.b.n_seqs * a.b.Hkv;
+  const dim3 grid((unsigned)(items * a.splits)), block(64 * kFewWaves);
+  if (pl.row_blocks == 1) attend_few_kernel<D, FP8, 1><<<grid, block, 0, stream>>>(a);
+  else if (pl.row_blocks == 2) attend_few_kernel<D, FP8, 2><<<grid, block, 0, stream>>>(a);
+  else attend_few_kernel<D, FP8, 4><<<grid, block, 0, stream>>>(a);
+  if (hipError_t e = hipGetLastError()) return (int)e;
+  if (a.splits > 1) join_few_kernel<D><<<dim3((unsigned)(items * 16 * pl.row_blocks)), dim3(256), 0, stream>>>(a, 16 * pl.row_blocks);
+  return (int)hipGetLastError();
+}
+
+int launch_few(const AttendPlan& pl, AttendArgs a, hipStream_t stream) {
+  if (pl.d == 128) return pl.pool.fp8 ? launch_few_of<128, true>(pl, a, stream) : launch_few_of<128, false>(pl, a, stream);
+  return pl.pool.fp8 ? launch_few_of<64, true>(pl, a, stream) : launch_few_of<64, false>(pl, a, stream);
+}
+
+}  // namespace codecomp

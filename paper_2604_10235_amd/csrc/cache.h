@@ -54,6 +54,8 @@ struct RotaryArgs {
 };
 int make_rotary(const codecomp_rotary* r, int head_dim, RotaryArgs* a);
 
+constexpr int kFewMostSplits = 2048;      // most chunks that a request's keys are cut into
+
 // codecomp_attend as laid out on the host.
 struct AttendPlan {
   PagePool pool;
@@ -63,7 +65,7 @@ struct AttendPlan {
   int few_rows, many_rows;     // requests of each kind (attend.hip)
   int row_blocks;              // few rows: blocks of 16 rows of the largest
   int chunk, splits;           // few rows: keys of a workgroup, and workgroups per request and head
-  int few_tokens_max;
+  int workgroups;              // many rows
   size_t off_few, off_many, ws_bytes;
 };
 int make_attend_plan(const codecomp_batch* b, const codecomp_pages* p, AttendPlan* plan);
