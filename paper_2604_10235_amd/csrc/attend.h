@@ -30,6 +30,12 @@ struct AttendArgs {
   int chunk, splits;           // few rows
 };
 
+// The same in all lanes, and known to be: in scalar registers.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  return (int64_t)((uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (unsigned)__builtin_amdgcn_readfirstlane((int)x));
+}
+
 __device__ __forceinline__ bf16x8 frag(u32x4 v) { return __builtin_bit_cast(bf16x8, v); }
 __device__ __forceinline__ unsigned pack2(float a, float b) { return __builtin_bit_cast(unsigned, bf16x2{(__bf16)a, (__bf16)b}); }
 
@@ -43,20 +49,22 @@ __device__ __forceinline__ u32x4 widen8(unsigned a, unsigned b) {
   return r;
 }
 
-// Whether a 16-byte piece holds an infinity or NaN (E4M3 has no infinity).
+// A 16-byte piece with zeros for its infinities and NaN (E4M3 has no infinity); `any`: whether there were some.
 template <bool FP8>
-__device__ __forceinline__ bool not_finite(u32x4 v) {
-  bool bad = false;
+__device__ __forceinline__ u32x4 finite_part(u32x4 v, bool& any) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
+    unsigned mask = 0;
     if constexpr (FP8) {
-      const unsigned x = (v[i] & 0x7F7F7F7Fu) ^ 0x7F7F7F7Fu;       // a zero byte is a NaN
-      bad |= ((x - 0x01010101u) & ~x & 0x80808080u) != 0;
+#pragma unroll
+      for (int j = 0; j < 32; j += 8) mask |= ((v[i] >> j) & 0x7Fu) == 0x7Fu ? 0xFFu << j : 0u;
     } else {
-      bad |= (v[i] & 0x7F80u) == 0x7F80u || (v[i] & 0x7F800000u) == 0x7F800000u;
+      mask = ((v[i] & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((v[i] & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
     }
+    any |= mask != 0;
+    v[i] &= ~mask;
   }
-  return bad;
+  return v;
 }
 
 // 4 elements of a stored row as floats.
@@ -74,6 +82,10 @@ __device__ __forceinline__ f32x4 row4(const unsigned char* p) {
   }
   return r;
 }
+
+// What finite_part left out, for a row that sees the value: weights are positive, so an infinity or NaN is what the sum becomes, whatever
+// the weight.
+__device__ __forceinline__ float with_the_rest(float sum, float v) { return __builtin_isfinite(v) ? sum : sum + v; }
 
 // The transposing read: a group of 16 lanes addresses four rows of 16 elements in LDS, four lanes a row, and lane i gets column i.
 __device__ __forceinline__ s16x4 read_columns(const unsigned char* lds) {

@@ -95,6 +95,7 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 4 ? 1 : 2) void attend_few_ke
     for (int db = 0; db < DB; ++db) o[rb][db] = f32x4{0, 0, 0, 0};
   }
 
+  bool left_out = false;
   int tile = key0 + wave * kFewKeys;
   int page = look_up(tile), next_page = 0;
   if (tile < key1) {
@@ -104,24 +105,14 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 4 ? 1 : 2) void attend_few_ke
   for (; tile < key1; tile += kFewWaves * kFewKeys) {
     const unsigned valid = (unsigned)__ballot(page >= 0);        // lanes 0 .. 31: the keys of the tile
     const bool plain = valid == 0xFFFFFFFFu && tile + kFewKeys <= seen_by_all;
-    unsigned apart = 0;                                          // keys whose values are added by themselves, below
     if (__builtin_expect(!plain, 0)) {
-      // Values that some row does not see must not meet its weight of zero in a product if they are infinite or NaN.
+#pragma unroll
+      for (int i = 0; i < T::LOADS; ++i)
+        if (!((valid >> (i * T::ROWS + lane / T::PIECES)) & 1)) kr[i] = vr[i] = u32x4{0, 0, 0, 0};
+      // a weight of zero must not meet an infinite or NaN value: such values are added at the end, to the rows that see them
       if (tile + kFewKeys > seen_by_all && seen_by_all < len) {
 #pragma unroll
-        for (int i = 0; i < T::LOADS; ++i) {
-          const uint64_t bad = __ballot(not_finite<FP8>(vr[i]));
-#pragma unroll
-          for (int j = 0; j < T::ROWS; ++j)
-            if ((bad >> (j * T::PIECES)) & ((1ull << T::PIECES) - 1)) apart |= 1u << (i * T::ROWS + j);
-        }
-        apart &= valid;
-      }
-#pragma unroll
-      for (int i = 0; i < T::LOADS; ++i) {
-        const int row = i * T::ROWS + lane / T::PIECES;
-        if (!((valid >> row) & 1)) kr[i] = vr[i] = u32x4{0, 0, 0, 0};
-        if ((apart >> row) & 1) vr[i] = u32x4{0, 0, 0, 0};
+        for (int i = 0; i < T::LOADS; ++i) vr[i] = finite_part<FP8>(vr[i], left_out);
       }
     }
 #pragma unroll
@@ -138,7 +129,6 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 4 ? 1 : 2) void attend_few_ke
       }
     }
     __builtin_amdgcn_wave_barrier();
-    const int this_page = page;
     page = next_page;
     if (tile + kFewWaves * kFewKeys < key1) {
       send_for(tile + kFewWaves * kFewKeys, page);
@@ -216,27 +206,25 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 4 ? 1 : 2) void attend_few_ke
         o[rb][db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, lo[rb], o[rb][db], 0, 0, 0);
       }
     }
-    while (__builtin_expect(apart != 0, 0)) {
-      const int j = __ffs(apart) - 1;
-      apart &= apart - 1;
-      const unsigned char* row = a.pool.v + a.layer + head * a.pool.s_head + __shfl(this_page, j) * a.pool.s_page + ((tile + j) & in_page) * a.pool.s_tok;
+    __builtin_amdgcn_wave_barrier();
+  }
+
+  if (__builtin_expect(__ballot(left_out) != 0, 0)) {
+    for (int key = max(seen_by_all, key0); key < key1; ++key) {
+      const int at = table[key >> a.pool.page_log2];
+      if ((key - key0) / kFewKeys % kFewWaves != wave || at < 0 || at >= a.pool.n_pages) continue;          // another wave's
+      const unsigned char* row = a.pool.v + a.layer + head * a.pool.s_head + at * a.pool.s_page + (key & in_page) * a.pool.s_tok;
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        float w = 0.0f;
+      for (int db = 0; db < DB; ++db) {
+        const f32x4 v = row4<FP8>(row + (db * 16 + quarter * 4) * (FP8 ? 1 : 2));
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if ((i >> 2) == (j >> 4) && (i & 3) == (j & 3)) w = p[rb][i];
-        w = __shfl(w, ((j & 15) >> 2) * 16 + l16);
-        const bool sees = tile + j < limit[rb];
+        for (int rb = 0; rb < RB; ++rb)
+          if (key < limit[rb]) {
 #pragma unroll
-        for (int db = 0; db < DB; ++db) {
-          const f32x4 v = row4<FP8>(row + (db * 16 + quarter * 4) * (FP8 ? 1 : 2));
-#pragma unroll
-          for (int i = 0; i < 4; ++i) o[rb][db][i] = sees ? fmaf(w, v[i], o[rb][db][i]) : o[rb][db][i];
-        }
+            for (int i = 0; i < 4; ++i) o[rb][db][i] = with_the_rest(o[rb][db][i], v[i]);
+          }
       }
     }
-    __builtin_amdgcn_wave_barrier();
   }
 
   // the four waves' shares of every row, 16 rows at a time

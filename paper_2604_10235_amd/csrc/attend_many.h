@@ -1,8 +1,8 @@
 // Internal header: attention of requests with many rows (new tokens x query heads per KV head, more than 64): prefill chunks and prompts.
 // Instantiated per head_dim and cache type in attend_many_*.hip, so that they compile side by side.
 //
-// The rows of a KV head, token by token and its query heads within, are cut into blocks of 256: four waves of 64 rows, two MFMA tiles of 32
-// each, which share the keys and values that go through LDS in tiles of 64.  S^T = K Q^T leaves a row's logits in one lane of each half of the wave;
+// The rows of a KV head, token by token and its query heads within, are cut into blocks of 256: eight waves of 32 rows,
+// which share the keys and values that go through LDS in tiles of 64.  S^T = K Q^T leaves a row's logits in one lane of each half of the wave;
 // O^T += V^T P^T takes them from there: the order of keys in a contraction is free, and chosen so that a lane's weights are its right operand as
 // they stand.  V^T comes from LDS by the transposing read.
 #pragma once
@@ -10,7 +10,7 @@
 
 namespace codecomp {
 
-constexpr int kManyRows = 256, kManyKeys = 64;
+constexpr int kManyRows = 256, kManyKeys = 64, kManyWaves = 8, kManyThreads = 64 * kManyWaves;
 
 // What a workgroup leaves for the kernel that joins blocks of rows whose keys several workgroups share.
 struct CutBlock {
@@ -44,22 +44,28 @@ __device__ __forceinline__ Blocks blocks_of(const ManyArgs& m, int r) {
   return x;
 }
 
+__device__ __forceinline__ Blocks uniform(Blocks x) {
+  x.len = uniform(x.len); x.nq = uniform(x.nq); x.rows = uniform(x.rows); x.count = uniform(x.count);
+  return x;
+}
+
 template <int D, bool FP8>
-__global__ __launch_bounds__(256, D == 128 ? 1 : 2) void attend_many_kernel(const ManyArgs ma) {
+__global__ __launch_bounds__(kManyThreads, D == 128 ? 2 : 4) void attend_many_kernel(const ManyArgs ma) {
   const AttendArgs& a = ma.a;
   constexpr int PIECES = D * (FP8 ? 1 : 2) / 16;               // 16-byte pieces of a stored row
-  constexpr int ROWS = 256 / PIECES, LOADS = kManyKeys / ROWS;  // rows per load of the workgroup, loads per tile
+  constexpr int ROWS = kManyThreads / PIECES, LOADS = ROWS > kManyKeys ? 1 : kManyKeys / ROWS;      // rows per load of the workgroup, loads per tile
   constexpr int K_ROW = 2 * D + 16, V_ROW = 2 * D + 64;          // bytes between rows in LDS: no bank conflicts in either read
   constexpr int KS = D / 16, DB = D / 32;
+  static_assert(kManyRows == 32 * kManyWaves, "a block of 32 rows per wave");
   __shared__ __attribute__((aligned(16))) unsigned char k_lds[2][kManyKeys * K_ROW];
   __shared__ __attribute__((aligned(16))) unsigned char v_lds[2][kManyKeys * V_ROW];
-  __shared__ uint64_t apart_lds[2][4];
-  __shared__ int64_t wave_sum[4];
+  __shared__ int not_finite;
+  __shared__ int64_t wave_sum[kManyWaves];
   __shared__ int found[4];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, half = lane >> 5;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), l32 = lane & 31, half = lane >> 5;
 
   // ---- this workgroup's share: the tiles of all blocks of all heads form one sequence, cut into equal parts
-  const int n = a.b.n_seqs, per = (n + 255) / 256;
+  const int n = a.b.n_seqs, per = (n + kManyThreads - 1) / kManyThreads;
   int64_t mine = 0;
   for (int r = min(tid * per, n); r < min(tid * per + per, n); ++r) {
     const Blocks x = blocks_of(ma, r);
@@ -75,10 +81,11 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void attend_many_kernel(cons
   __syncthreads();
   int64_t before = 0, per_head = 0;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
+  for (int w = 0; w < kManyWaves; ++w) {
     if (w < wave) before += wave_sum[w];
     per_head += wave_sum[w];
   }
+  per_head = uniform(per_head);
   const int64_t total = per_head * a.b.Hkv;
   const int64_t workgroups = min((int64_t)ma.workgroups, total);
   const int g = blockIdx.x;
@@ -108,8 +115,8 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void attend_many_kernel(cons
     }
   }
   __syncthreads();
-  int r = __builtin_amdgcn_readfirstlane(found[0]), block = __builtin_amdgcn_readfirstlane(found[1]), tile0 = __builtin_amdgcn_readfirstlane(found[2]);
-  Blocks of = blocks_of(ma, r);
+  int r = uniform(found[0]), block = uniform(found[1]), tile0 = uniform(found[2]);
+  Blocks of = uniform(blocks_of(ma, r));
   bool first_segment = true;
   CutBlock cut = {-1, 0, 0, 0, 0};
 
@@ -117,7 +124,7 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void attend_many_kernel(cons
     if (block >= of.count) {                                     // the next request that has blocks, or the next head
       do {
         if (++r == n) { r = 0; ++head; }
-        of = blocks_of(ma, r);
+        of = uniform(blocks_of(ma, r));
       } while (of.count == 0);
       block = 0;
     }
@@ -129,22 +136,21 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void attend_many_kernel(cons
       const int64_t end = x + tiles;                             // position behind the block
       cut = {r, block, head, slot, (int)((end * workgroups - 1) / total)};
     }
-    const int q0 = a.b.cu_q[r], row0 = block * kManyRows + wave * 64;
+    const int q0 = uniform(a.b.cu_q[r]), row0 = block * kManyRows + wave * 32, row = row0 + l32;
     const bool active = row0 < of.rows;
 
     // query rows as right operands, and the keys that the lane's rows see
-    u32x4 qf[2][KS];
-    int limit[2];
-#pragma unroll
-    for (int rb = 0; rb < 2; ++rb) {
-      const int row = row0 + rb * 32 + l32, rr = min(row, of.rows - 1), t = rr / of.G;
+    u32x4 qf[KS];
+    int limit;
+    {
+      const int rr = min(row, of.rows - 1), t = rr / of.G;
       const uint16_t* p = a.q + (q0 + t) * a.b.q_st + (head * of.G + rr - t * of.G) * a.b.q_sh + half * 8;
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        qf[rb][ks] = *reinterpret_cast<const u32x4*>(p + ks * 16);
-        if (row >= of.rows) qf[rb][ks] = u32x4{0, 0, 0, 0};
+        qf[ks] = *reinterpret_cast<const u32x4*>(p + ks * 16);
+        if (row >= of.rows) qf[ks] = u32x4{0, 0, 0, 0};
       }
-      limit[rb] = of.causal ? min(of.len, of.len - of.nq + t + 1) : of.len;
+      limit = of.causal ? min(of.len, of.len - of.nq + t + 1) : of.len;
     }
     const int seen_by_all = of.causal ? min(of.len, of.len - of.nq + block * kManyRows / of.G + 1) : of.len;
 
@@ -152,265 +158,233 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void attend_many_kernel(cons
     const unsigned char* vb = a.pool.v + a.layer + head * a.pool.s_head + (tid % PIECES) * 16;
     const int32_t* table = a.b.table + (int64_t)r * a.b.table_width;
     const int in_page = (1 << a.pool.page_log2) - 1;
-    auto look_up = [&](int tile) {                               // page of key 64 tile + lane; -1: no such key
-      const int key = tile * kManyKeys + lane;
-      int page = -1;
-      if (tile < tile1 && key < of.len) {
-        page = table[key >> a.pool.page_log2];
-        if (page >= a.pool.n_pages) page = -1;
-      }
-      return page;
+    // Entry of the page table for key 64 tile + lane (for the last key where there is none), not looked at before it is needed.
+    auto look_up = [&](int tile) __attribute__((always_inline)) { return table[max(min(tile * kManyKeys + lane, of.len - 1), 0) >> a.pool.page_log2]; };
+    auto is_there = [&](int tile, int page) __attribute__((always_inline)) {
+      return __ballot(tile < tile1 && tile * kManyKeys + lane < of.len && page >= 0 && page < a.pool.n_pages);
     };
-    auto send_for = [&](const unsigned char* base, u32x4* into, int tile, int page) {
+    // where this thread's rows of a tile are; rows that are not there: in page 0, zeroed before they are parked
+    auto places = [&](int64_t (&off)[LOADS], int tile, int page) __attribute__((always_inline)) {
+      if (page >= a.pool.n_pages) page = 0;
 #pragma unroll
       for (int i = 0; i < LOADS; ++i) {
-        const int row = i * ROWS + tid / PIECES;
-        const int at = max(__shfl(page, row), 0);                // rows that are not there: page 0, zeroed below
-        into[i] = *reinterpret_cast<const u32x4*>(base + at * a.pool.s_page + ((tile * kManyKeys + row) & in_page) * a.pool.s_tok);
+        const int at = (i * ROWS + tid / PIECES) & (kManyKeys - 1);
+        off[i] = max(__shfl(page, at), 0) * a.pool.s_page + ((tile * kManyKeys + at) & in_page) * (int)a.pool.s_tok;
       }
     };
-    auto park = [&](unsigned char* lds, int row_bytes, const u32x4* from) {
+    auto park = [&](unsigned char* lds, int row_bytes, u32x4 from, int i) __attribute__((always_inline)) {
+      if (ROWS > kManyKeys && tid / PIECES >= kManyKeys) return;           // half of the threads have a row (head_dim 64, 8 bits)
+      unsigned char* at = lds + (i * ROWS + tid / PIECES) * row_bytes + (tid % PIECES) * (FP8 ? 32 : 16);
+      if constexpr (FP8) {
+        *reinterpret_cast<u32x4*>(at) = widen8(from.x, from.y);
+        *reinterpret_cast<u32x4*>(at + 16) = widen8(from.z, from.w);
+      } else {
+        *reinterpret_cast<u32x4*>(at) = from;
+      }
+    };
+    u32x4 kr[LOADS], vr[LOADS];                                  // keys of the tile after the next, values of the next one, on their way
+    int64_t k_off[LOADS], v_off[LOADS];
+
+    f32x16 o[DB];
+    float m = -1.0e30f, l = 0.0f;                                // a row's reference, this half's sum of weights
 #pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        unsigned char* at = lds + (i * ROWS + tid / PIECES) * row_bytes + (tid % PIECES) * (FP8 ? 32 : 16);
-        if constexpr (FP8) {
-          *reinterpret_cast<u32x4*>(at) = widen8(from[i].x, from[i].y);
-          *reinterpret_cast<u32x4*>(at + 16) = widen8(from[i].z, from[i].w);
-        } else {
-          *reinterpret_cast<u32x4*>(at) = from[i];
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[db][i] = 0.0f;
+    f32x16 za, zb;                                               // logits of the first and of the second 32 keys of a tile
+    u32x4 pa[2], pb[2] = {u32x4{0, 0, 0, 0}, u32x4{0, 0, 0, 0}}; // their weights, 16 keys each
+
+    // Key fragment f (16 of a row's elements of 32 keys), value fragment f (32 columns of 16 keys).
+    auto key_frag = [&](const unsigned char* kt, int f) __attribute__((always_inline)) {
+      return *reinterpret_cast<const u32x4*>(kt + l32 * K_ROW + f * 32 + half * 16);
+    };
+    auto value_frag = [&](const unsigned char* vt, int f) __attribute__((always_inline)) {
+      const unsigned char* at = vt + ((f / DB) * 16 + half * 4 + ((lane >> 2) & 3)) * V_ROW + (f % DB) * 64 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+      const s16x4 v0 = read_columns(at), v1 = read_columns(at + 8 * V_ROW);
+      return __builtin_bit_cast(u32x4, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    auto logits = [&](f32x16& z, const unsigned char* kt) __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) z[i] = 0.0f;
+#pragma unroll
+      for (int f = 0; f < KS; ++f) z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(key_frag(kt, f)), frag(qf[f]), z, 0, 0, 0);
+    };
+    auto weigh_values = [&](const unsigned char* vt, const u32x4 (&p)[2]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int f = 0; f < KS; ++f) o[f % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(value_frag(vt, f)), frag(p[f / DB]), o[f % DB], 0, 0, 0);
+    };
+    // One step: the weights p of the 32 keys from key0 on, whose logits are z (`valid`: which of them there are); beside them, on the matrix cores,
+    // the logits zn of the next 32 keys and the outputs of the 32 before, whose weights are pp.  The order is the source's: an MFMA, the LDS read that
+    // one three further on needs, the vector work of a logit (two at head_dim 64), and what `beside` has for this place.
+    auto step = [&](f32x16& z, u32x4 (&p)[2], f32x16& zn, const unsigned char* kt, const u32x4 (&pp)[2], const unsigned char* vt, int key0, unsigned valid,
+                    auto&& beside) __attribute__((always_inline)) {
+      if (__builtin_expect(valid != 0xFFFFFFFFu || key0 + 32 > seen_by_all, 0)) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int j = 8 * (i >> 2) + 4 * half + (i & 3);
+          if (!((valid >> j) & 1) || key0 + j >= limit) z[i] = -INFINITY;
         }
       }
-    };
-    u32x4 kr[LOADS], vr[LOADS];
-
-    f32x16 o[2][DB];
-    float m[2] = {-1.0e30f, -1.0e30f}, l[2] = {0.0f, 0.0f};
+      constexpr int F = 2 * KS, RING = 4, PER = 16 / F;
+      u32x4 ring[RING];
+      float sum = 0.0f, top = 0.0f, w[16];
+      auto fetch = [&](int f) __attribute__((always_inline)) { ring[f % RING] = f & 1 ? value_frag(vt, f / 2) : key_frag(kt, f / 2); };
 #pragma unroll
-    for (int rb = 0; rb < 2; ++rb)
+      for (int i = 0; i < 16; ++i) zn[i] = 0.0f;
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int db = 0; db < DB; ++db)
+      for (int f = 0; f < RING - 1; ++f) fetch(f);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) o[rb][db][i] = 0.0f;
-
-    f32x16 s[2], s_next[2];
-    bf16x8 p_prev[2][2];                                         // weights of the 32 keys before, [rows][16 keys]
+      for (int f = 0; f < F; ++f) {
+        if (f + RING - 1 < F) fetch(f + RING - 1);
+        const int i = f / 2;
+        if (f & 1) o[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(ring[f % RING]), frag(pp[i / DB]), o[i % DB], 0, 0, 0);
+        else zn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(ring[f % RING]), frag(qf[i]), zn, 0, 0, 0);
 #pragma unroll
-    for (int rb = 0; rb < 2; ++rb)
-#pragma unroll
-      for (int k2 = 0; k2 < 2; ++k2) p_prev[rb][k2] = frag(u32x4{0, 0, 0, 0});
-
-    auto logits = [&](f32x16 (&z)[2], const unsigned char* kt) {
-#pragma unroll
-      for (int rb = 0; rb < 2; ++rb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) z[rb][i] = 0.0f;
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const u32x4 kf = *reinterpret_cast<const u32x4*>(kt + l32 * K_ROW + ks * 32 + half * 16);
-#pragma unroll
-        for (int rb = 0; rb < 2; ++rb) z[rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(kf), frag(qf[rb][ks]), z[rb], 0, 0, 0);
-      }
-    };
-    auto weigh_values = [&](const unsigned char* vt) {
-#pragma unroll
-      for (int k2 = 0; k2 < 2; ++k2)
-#pragma unroll
-        for (int db = 0; db < DB; ++db) {
-          const unsigned char* at = vt + (k2 * 16 + half * 4 + ((lane >> 2) & 3)) * V_ROW + db * 64 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
-          const s16x4 v0 = read_columns(at), v1 = read_columns(at + 8 * V_ROW);
-          const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-          for (int rb = 0; rb < 2; ++rb) o[rb][db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p_prev[rb][k2], o[rb][db], 0, 0, 0);
+        for (int e = f * PER; e < (f + 1) * PER; ++e) {
+          w[e] = __builtin_amdgcn_exp2f(fmaf(z[e], a.c, -m));
+          if (e > 0) sum += w[e - 1];
+          if (e > 1 && (e & 1) == 0) {
+            top = fmaxf(fmaxf(top, w[e - 2]), w[e - 1]);
+            p[(e - 2) >> 3][((e - 2) & 7) >> 1] = pack2(w[e - 2], w[e - 1]);
+          }
         }
+        beside(f);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      sum += w[15];
+      top = fmaxf(fmaxf(top, w[14]), w[15]);
+      p[1][3] = pack2(w[14], w[15]);
+      if (__builtin_expect(__ballot(top > 256.0f) != 0, 0)) {    // a logit far above its row's reference: move the references
+        float t = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) t = fmaxf(t, z[i]);
+        t *= a.c;
+        t = fmaxf(t, __shfl_xor(t, 32));
+        const float to = fmaxf(m, t), old = to == m ? 1.0f : __builtin_amdgcn_exp2f(m - to);
+        m = to;
+        l *= old;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[db][i] *= old;
+        sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) {
+          const float x = __builtin_amdgcn_exp2f(fmaf(z[i], a.c, -m)), y = __builtin_amdgcn_exp2f(fmaf(z[i + 1], a.c, -m));
+          sum += x + y;
+          p[i >> 3][(i & 7) >> 1] = pack2(x, y);
+        }
+      }
+      l += sum;
     };
-    // Values that some rows of the block do not see and that are infinite or NaN: zeros in LDS, added here to the rows that see them.
-    auto add_apart = [&](unsigned bits, int key0, int page) {
-      while (bits) {
-        const int j = __ffs(bits) - 1;
-        bits &= bits - 1;
-        const int key = key0 + j;
-        const unsigned char* row = a.pool.v + a.layer + head * a.pool.s_head + __shfl(page, key & 63) * a.pool.s_page + (key & in_page) * a.pool.s_tok;
+    auto zero_rows = [&](u32x4* into, uint64_t valid) {
 #pragma unroll
-        for (int rb = 0; rb < 2; ++rb) {
-          unsigned w = 0;
+      for (int i = 0; i < LOADS; ++i)
+        if (!((valid >> ((i * ROWS + tid / PIECES) & (kManyKeys - 1))) & 1)) into[i] = u32x4{0, 0, 0, 0};
+    };
+    auto partly = [&](int tile) { return (tile + 1) * kManyKeys > seen_by_all && seen_by_all < of.len; };       // some rows do not see all of it
+    auto lds_barrier = [&]() __attribute__((always_inline)) { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+
+    // ---- tiles.  A tile's keys are in LDS a step before its values.
+    lds_barrier();                                               // the segment before is through with LDS
+    if (tid == 0) not_finite = 0;
+    int page = look_up(tile0), page_next = look_up(tile0 + 1);
+    places(k_off, tile0, page);
 #pragma unroll
-          for (int k2 = 0; k2 < 2; ++k2)
+    for (int i = 0; i < LOADS; ++i) kr[i] = *reinterpret_cast<const u32x4*>(kb + k_off[i]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (k2 == (j >> 4) && i == ((j & 3) >> 1) + 2 * ((j & 15) >> 3)) w = __builtin_bit_cast(u32x4, p_prev[rb][k2])[i];
-          w = __shfl(w, ((j >> 2) & 1) * 32 + l32);
-          const float f = __uint_as_float((j & 1) ? w & 0xFFFF0000u : w << 16);
-          const bool sees = key < limit[rb];
+    for (int i = 0; i < LOADS; ++i) vr[i] = *reinterpret_cast<const u32x4*>(vb + k_off[i]);
+    // in front of the first tile: values of zero
+    for (int i = tid; i < 32 * V_ROW / 16; i += kManyThreads) *reinterpret_cast<u32x4*>(v_lds[(tile0 + 1) & 1] + 32 * V_ROW + i * 16) = u32x4{0, 0, 0, 0};
+    zero_rows(kr, is_there(tile0, page));
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) park(k_lds[tile0 & 1], K_ROW, kr[i], i);
+    places(v_off, tile0 + 1, page_next);
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) kr[i] = *reinterpret_cast<const u32x4*>(kb + v_off[i]);
+    lds_barrier();
+    if (active) logits(za, k_lds[tile0 & 1]);
+    for (int tile = tile0; tile < tile1; ++tile) {
+      const uint64_t valid = is_there(tile, page), valid_next = is_there(tile + 1, page_next);
+      // to be parked during the first step: the next tile's keys and this one's values
+      if (__builtin_expect(valid_next != ~0ull, 0)) zero_rows(kr, valid_next);
+      if (__builtin_expect(valid != ~0ull || partly(tile), 0)) {
+        zero_rows(vr, valid);
+        // a weight of zero must not meet an infinite or NaN value: such values are added at the end, to the rows that see them
+        if (partly(tile)) {
+          bool any = false;
+#pragma unroll
+          for (int i = 0; i < LOADS; ++i) vr[i] = finite_part<FP8>(vr[i], any);
+          if (any) not_finite = 1;
+        }
+      }
+      const int page_after = look_up(tile + 2);
+      unsigned char* next_keys = k_lds[(tile + 1) & 1];
+      unsigned char* these_values = v_lds[tile & 1];
+      auto park_some = [&](int f) __attribute__((always_inline)) {
+        constexpr int AT = 2 * KS - 2 * LOADS;                   // the last places of the step
+        if (f >= AT && f < AT + LOADS) park(next_keys, K_ROW, kr[f - AT], f - AT);
+        if (f >= AT + LOADS) park(these_values, V_ROW, vr[f - AT - LOADS], f - AT - LOADS);
+      };
+      auto send_some = [&](int f) __attribute__((always_inline)) {
+        if (f == 0) places(k_off, tile + 2, page_after);
+        if (f >= 1 && f <= LOADS) kr[f - 1] = *reinterpret_cast<const u32x4*>(kb + k_off[f - 1]);
+        if (f >= 1 + LOADS && f <= 2 * LOADS) vr[f - 1 - LOADS] = *reinterpret_cast<const u32x4*>(vb + v_off[f - 1 - LOADS]);
+        if (f == 2 * LOADS) {
+#pragma unroll
+          for (int i = 0; i < LOADS; ++i) v_off[i] = k_off[i];
+        }
+      };
+      if (active)
+        step(za, pa, zb, k_lds[tile & 1] + 32 * K_ROW, pb, v_lds[(tile + 1) & 1] + 32 * V_ROW, tile * kManyKeys, (unsigned)valid, park_some);
+      else
+        for (int f = 0; f < 2 * KS; ++f) park_some(f);
+      lds_barrier();
+      if (active)
+        step(zb, pb, za, next_keys, pa, these_values, tile * kManyKeys + 32, (unsigned)(valid >> 32), send_some);
+      else
+        for (int f = 0; f < 2 * KS; ++f) send_some(f);
+      page = page_next; page_next = page_after;
+    }
+    if (active) {
+      weigh_values(v_lds[(tile1 + 1) & 1] + 32 * V_ROW, pb);
+      if (__builtin_expect(partly(tile1 - 1) && not_finite != 0, 0)) {
+        for (int key = max(seen_by_all, tile0 * kManyKeys); key < min(of.len, tile1 * kManyKeys); ++key) {
+          const int at = table[key >> a.pool.page_log2];
+          if (at < 0 || at >= a.pool.n_pages || key >= limit) continue;
+          const unsigned char* from = a.pool.v + a.layer + head * a.pool.s_head + at * a.pool.s_page + (key & in_page) * a.pool.s_tok;
 #pragma unroll
           for (int db = 0; db < DB; ++db)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-              const f32x4 v = row4<FP8>(row + (db * 32 + i * 8 + half * 4) * (FP8 ? 1 : 2));
+              const f32x4 v = row4<FP8>(from + (db * 32 + i * 8 + half * 4) * (FP8 ? 1 : 2));
 #pragma unroll
-              for (int e = 0; e < 4; ++e) o[rb][db][4 * i + e] = sees ? fmaf(f, v[e], o[rb][db][4 * i + e]) : o[rb][db][4 * i + e];
+              for (int e = 0; e < 4; ++e) o[db][4 * i + e] = with_the_rest(o[db][4 * i + e], v[e]);
             }
         }
       }
-    };
-    // Weights of the 32 keys from key0 on; `valid`: which of them there are.
-    auto weights = [&](f32x16 (&z)[2], int key0, unsigned valid) {
-      if (__builtin_expect(valid != 0xFFFFFFFFu || key0 + 32 > seen_by_all, 0)) {
+      const float sum = l + __shfl_xor(l, 32);
+      if (row < of.rows && whole) {
+        const int t = row / of.G, h = head * of.G + row - t * of.G;
+        const float inv = sum == 0.0f ? 0.0f : a.pool.v_scale / sum;
+        uint16_t* out = a.out + (q0 + t) * a.b.o_st + h * a.b.o_sh + half * 4;
 #pragma unroll
-        for (int rb = 0; rb < 2; ++rb)
+        for (int db = 0; db < DB; ++db)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int j = 8 * (i >> 2) + 4 * half + (i & 3);
-            if (!((valid >> j) & 1) || key0 + j >= limit[rb]) z[rb][i] = -INFINITY;
-          }
-      }
-      float p[2][16], sum[2];
-      float top = 0.0f;
-      auto form = [&]() {
-        top = 0.0f;
+          for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<u32x2*>(out + db * 32 + i * 8) =
+                u32x2{pack2(o[db][4 * i] * inv, o[db][4 * i + 1] * inv), pack2(o[db][4 * i + 2] * inv, o[db][4 * i + 3] * inv)};
+        if (a.lse && half == 0) a.lse[(int64_t)(q0 + t) * a.b.Hq + h] = sum == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kLn2;
+      } else if (row < of.rows) {
+        const int64_t part = (int64_t)slot * kManyRows + wave * 32 + l32;
 #pragma unroll
-        for (int rb = 0; rb < 2; ++rb) {
-          sum[rb] = 0.0f;
+        for (int db = 0; db < DB; ++db)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            p[rb][i] = __builtin_amdgcn_exp2f(fmaf(z[rb][i], a.c, -m[rb]));
-            sum[rb] += p[rb][i];
-            top = fmaxf(top, p[rb][i]);
-          }
-        }
-      };
-      form();
-      if (__builtin_expect(__ballot(top > 256.0f) != 0, 0)) {    // a logit far above its row's reference: move the references
-#pragma unroll
-        for (int rb = 0; rb < 2; ++rb) {
-          float t = -INFINITY;
-#pragma unroll
-          for (int i = 0; i < 16; ++i) t = fmaxf(t, z[rb][i]);
-          t *= a.c;
-          t = fmaxf(t, __shfl_xor(t, 32));
-          const float to = fmaxf(m[rb], t), old = to == m[rb] ? 1.0f : __builtin_amdgcn_exp2f(m[rb] - to);
-          m[rb] = to;
-          l[rb] *= old;
-#pragma unroll
-          for (int db = 0; db < DB; ++db)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) o[rb][db][i] *= old;
-        }
-        form();
-      }
-#pragma unroll
-      for (int rb = 0; rb < 2; ++rb) {
-        l[rb] += sum[rb];
-#pragma unroll
-        for (int k2 = 0; k2 < 2; ++k2) {
-          u32x4 w;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) w[i] = pack2(p[rb][8 * k2 + 2 * i], p[rb][8 * k2 + 2 * i + 1]);
-          p_prev[rb][k2] = frag(w);
-        }
-      }
-    };
-
-    // ---- tiles.  A tile's keys are in LDS a step before its values: while the weights of 32 keys are formed, the matrix cores form the
-    // logits of the next 32 and take in the values of the 32 before.
-    __syncthreads();                                             // the segment before is through with LDS
-    int page = look_up(tile0), page_next = look_up(tile0 + 1), page_prev = -1;
-    send_for(kb, kr, tile0, page);
-    send_for(vb, vr, tile0, page);
-    auto park_keys = [&](int tile, int pg) {
-      const uint64_t valid = __ballot(pg >= 0);
-      if (__builtin_expect(valid != ~0ull, 0)) {
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i)
-          if (!((valid >> (i * ROWS + tid / PIECES)) & 1)) kr[i] = u32x4{0, 0, 0, 0};
-      }
-      park(k_lds[tile & 1], K_ROW, kr);
-    };
-    auto park_values = [&](int tile, int pg) {
-      const uint64_t valid = __ballot(pg >= 0);
-      const bool partly = (tile + 1) * kManyKeys > seen_by_all && seen_by_all < of.len;
-      if (__builtin_expect(valid != ~0ull || partly, 0)) {
-        uint64_t apart = 0;
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-          const int row = i * ROWS + tid / PIECES;
-          if (!((valid >> row) & 1)) vr[i] = u32x4{0, 0, 0, 0};
-          const uint64_t bad = partly ? __ballot(not_finite<FP8>(vr[i])) : 0;
-#pragma unroll
-          for (int j = 0; j < 64 / PIECES; ++j)
-            if ((bad >> (j * PIECES)) & ((1ull << PIECES) - 1)) apart |= 1ull << (i * ROWS + wave * (64 / PIECES) + j);
-          if ((apart >> row) & 1) vr[i] = u32x4{0, 0, 0, 0};
-        }
-        if (lane == 0) apart_lds[tile & 1][wave] = apart;
-      }
-      park(v_lds[tile & 1], V_ROW, vr);
-    };
-    park_keys(tile0, page);
-    if (tile0 + 1 < tile1) send_for(kb, kr, tile0 + 1, page_next);
-    __syncthreads();
-    if (active) logits(s, k_lds[tile0 & 1]);
-    for (int tile = tile0; tile < tile1; ++tile) {
-      const uint64_t valid = __ballot(page >= 0);
-      const bool partly = (tile + 1) * kManyKeys > seen_by_all && seen_by_all < of.len;
-      const bool partly_before = tile > tile0 && tile * kManyKeys > seen_by_all && seen_by_all < of.len;
-      if (active) {
-        logits(s_next, k_lds[tile & 1] + 32 * K_ROW);
-        if (tile > tile0) weigh_values(v_lds[(tile + 1) & 1] + 32 * V_ROW);        // of the tile before
-        if (__builtin_expect(partly_before, 0)) {
-          const uint64_t* w = apart_lds[(tile + 1) & 1];
-          add_apart((unsigned)((w[0] | w[1] | w[2] | w[3]) >> 32), (tile - 1) * kManyKeys + 32, page_prev);
-        }
-        weights(s, tile * kManyKeys, (unsigned)valid);
-      }
-      // the next tile's keys and this one's values
-      if (tile + 1 < tile1) park_keys(tile + 1, page_next);
-      park_values(tile, page);
-      const int page_after = look_up(tile + 2);
-      if (tile + 2 < tile1) send_for(kb, kr, tile + 2, page_after);
-      if (tile + 1 < tile1) send_for(vb, vr, tile + 1, page_next);
-      __syncthreads();
-      if (active) {
-        if (tile + 1 < tile1) logits(s, k_lds[(tile + 1) & 1]);
-        weigh_values(v_lds[tile & 1]);
-        if (__builtin_expect(partly, 0)) {
-          const uint64_t* w = apart_lds[tile & 1];
-          add_apart((unsigned)(w[0] | w[1] | w[2] | w[3]), tile * kManyKeys, page);
-        }
-        weights(s_next, tile * kManyKeys + 32, (unsigned)(valid >> 32));
-      }
-      page_prev = page; page = page_next; page_next = page_after;
-    }
-    if (active) {
-      weigh_values(v_lds[(tile1 + 1) & 1] + 32 * V_ROW);
-      if (__builtin_expect(tile1 * kManyKeys > seen_by_all && seen_by_all < of.len, 0)) {
-        const uint64_t* w = apart_lds[(tile1 + 1) & 1];
-        add_apart((unsigned)((w[0] | w[1] | w[2] | w[3]) >> 32), (tile1 - 1) * kManyKeys + 32, page_prev);
-      }
-#pragma unroll
-      for (int rb = 0; rb < 2; ++rb) {
-        const float sum = l[rb] + __shfl_xor(l[rb], 32);
-        const int row = row0 + rb * 32 + l32;
-        if (row >= of.rows) continue;
-        if (whole) {
-          const int t = row / of.G, h = head * of.G + row - t * of.G;
-          const float inv = sum == 0.0f ? 0.0f : a.pool.v_scale / sum;
-          uint16_t* out = a.out + (q0 + t) * a.b.o_st + h * a.b.o_sh + half * 4;
-#pragma unroll
-          for (int db = 0; db < DB; ++db)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              *reinterpret_cast<u32x2*>(out + db * 32 + i * 8) = u32x2{pack2(o[rb][db][4 * i] * inv, o[rb][db][4 * i + 1] * inv),
-                                                                     pack2(o[rb][db][4 * i + 2] * inv, o[rb][db][4 * i + 3] * inv)};
-          if (a.lse && half == 0) a.lse[(int64_t)(q0 + t) * a.b.Hq + h] = sum == 0.0f ? -INFINITY : (m[rb] + __builtin_amdgcn_logf(sum)) * kLn2;
-        } else {
-          const int64_t part = (int64_t)slot * kManyRows + wave * 64 + rb * 32 + l32;
-#pragma unroll
-          for (int db = 0; db < DB; ++db)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              *reinterpret_cast<f32x4*>(a.part_o + part * D + db * 32 + i * 8 + half * 4) =
-                  f32x4{o[rb][db][4 * i], o[rb][db][4 * i + 1], o[rb][db][4 * i + 2], o[rb][db][4 * i + 3]};
-          if (half == 0) { a.part_ml[2 * part] = m[rb]; a.part_ml[2 * part + 1] = sum; }
-        }
+          for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<f32x4*>(a.part_o + part * D + db * 32 + i * 8 + half * 4) = f32x4{o[db][4 * i], o[db][4 * i + 1], o[db][4 * i + 2], o[db][4 * i + 3]};
+        if (half == 0) { a.part_ml[2 * part] = m; a.part_ml[2 * part + 1] = sum; }
       }
     }
     x += tile1 - tile0;
@@ -423,7 +397,7 @@ __global__ __launch_bounds__(256, D == 128 ? 1 : 2) void attend_many_kernel(cons
 
 template <int D, bool FP8>
 int launch_many_of(const ManyArgs& m, hipStream_t stream) {
-  attend_many_kernel<D, FP8><<<dim3(m.workgroups), dim3(256), 0, stream>>>(m);
+  attend_many_kernel<D, FP8><<<dim3(m.workgroups), dim3(kManyThreads), 0, stream>>>(m);
   return (int)hipGetLastError();
 }
 

@@ -29,7 +29,7 @@ int make_pool(const codecomp_pages* p, PagePool* pool) {
   const int64_t st = p->stride_tok ? p->stride_tok : d, sh = p->stride_head ? p->stride_head : p->page_size * d;
   const int64_t sp = p->stride_page ? p->stride_page : p->n_kv_heads * p->page_size * d;
   const int64_t sl = p->stride_layer ? p->stride_layer : p->n_pages * (p->n_kv_heads * (p->page_size * d));
-  if (st < d || st > (1 << 20)) return CODECOMP_EINVAL_SHAPE;
+  if (st < d || st * p->page_size * esz > INT32_MAX) return CODECOMP_EINVAL_SHAPE;       // places inside a page are counted in 32 bits
   pool->k = static_cast<unsigned char*>(p->k); pool->v = static_cast<unsigned char*>(p->v);
   pool->n_pages = p->n_pages; pool->page_log2 = __builtin_ctz((unsigned)p->page_size); pool->fp8 = esz == 1;
   pool->s_layer = sl * esz; pool->s_page = sp * esz; pool->s_head = sh * esz; pool->s_tok = st * esz;
