@@ -43,7 +43,7 @@ int make_attend_plan(const codecomp_batch* b, const codecomp_pages* p, AttendPla
   pl->off_few = off;
   if (pl->few_rows > 0 && pl->splits > 1) off = align256(off + (size_t)(items * pl->splits * 16 * pl->row_blocks) * (p->head_dim + 2) * sizeof(float));
   pl->off_many = off;
-  pl->workgroups = p->head_dim == 128 ? 256 : 512;
+  pl->workgroups = 256;
   if (pl->many_rows > 0)
     off = align256(off + (size_t)pl->workgroups * 2 * kManyRows * (p->head_dim + 2) * sizeof(float) + pl->workgroups * sizeof(CutBlock));
   pl->ws_bytes = off;

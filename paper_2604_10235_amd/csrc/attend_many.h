@@ -50,7 +50,7 @@ __device__ __forceinline__ Blocks uniform(Blocks x) {
 }
 
 template <int D, bool FP8>
-__global__ __launch_bounds__(kManyThreads, D == 128 ? 2 : 4) void attend_many_kernel(const ManyArgs ma) {
+__global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const ManyArgs ma) {
   const AttendArgs& a = ma.a;
   constexpr int PIECES = D * (FP8 ? 1 : 2) / 16;               // 16-byte pieces of a stored row
   constexpr int ROWS = kManyThreads / PIECES, LOADS = ROWS > kManyKeys ? 1 : kManyKeys / ROWS;      // rows per load of the workgroup, loads per tile
