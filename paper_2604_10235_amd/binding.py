@@ -331,14 +331,14 @@ def make_pages(k, v, *, k_scale: float = 1.0, v_scale: float = 1.0) -> codecomp_
     p.kv_dtype = KV_BF16 if k.dtype == torch.bfloat16 else KV_FP8_E4M3
     p.stride_layer, p.stride_page, p.stride_head, p.stride_tok = k.stride()[:4]
     p.k_scale, p.v_scale = k_scale, v_scale
-    p._keep, p._device = (k, v), k.device
+    p._keep, p._at = (k, v), k.get_device()
     return p
 
 
 def _int32(t, shape, what: str):
     import torch
-    if t.dtype != torch.int32 or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
-        raise ValueError(f"{what} must be a contiguous int32 tensor of shape {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
+    if t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous int32 tensor of shape {shape}, not {t.dtype} {tuple(t.shape)}")
 
 
 def make_batch(*, n_q_heads: int, cu_q_host: np.ndarray, cu_q, kv_lens, table, max_kv_len: int, causal: bool = True, softmax_scale: float = 0.0,
@@ -355,27 +355,31 @@ def make_batch(*, n_q_heads: int, cu_q_host: np.ndarray, cu_q, kv_lens, table, m
     b.cu_q_host, b.cu_q_dev, b.kv_lens_dev, b.table_dev = host.ctypes.data, cu_q.data_ptr(), kv_lens.data_ptr(), table.data_ptr()
     for name, val in strides.items():
         setattr(b, name, val)
-    b._keep, b._tokens, b._device = (host, cu_q, kv_lens, table), int(host[-1]), cu_q.device
+    b._keep, b._tokens, b._at = (host, cu_q, kv_lens, table), int(host[-1]), cu_q.get_device()
     return b
 
 
-def _on_current(*things) -> None:
-    """All on the device that the stream is of: the library launches on the current device."""
+def _launch_stream(*at: int) -> int:
+    """torch's current stream on the current device, where everything has to be (`at`: device numbers, -1 for the CPU): the library launches there."""
     import torch
-    at = torch.cuda.current_device()
-    for x in things:
-        dev = getattr(x, "_device", None) or x.device
-        if dev.type != "cuda" or dev.index != at:
-            raise ValueError(f"a tensor is on {dev}, the current device is cuda:{at}")
+    device = torch._C._cuda_getDevice()
+    for i in at:
+        if i != device:
+            raise ValueError(f"a tensor is on {'the CPU' if i < 0 else f'cuda:{i}'}, the current device is cuda:{device}")
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
+def _at(t, otherwise: int) -> int:
+    return otherwise if t is None else t.get_device()
 
 
 def _vectors(t, what: str, shape, stride_tok: int, stride_head: int) -> int:
     """bf16 [tokens, heads, head_dim] with the strides that the call will use (0 = dense)."""
     import torch
-    if t.dtype != torch.bfloat16 or tuple(t.shape) != shape:
+    if t.dtype != torch.bfloat16 or t.shape != shape:
         raise ValueError(f"{what} must be bfloat16 {shape}, not {t.dtype} {tuple(t.shape)}")
     want = (stride_tok or shape[1] * shape[2], stride_head or shape[2], 1)
-    if any(n > 1 and s != w for n, s, w in zip(t.shape, t.stride(), want)):
+    if t.stride() != want and any(n > 1 and s != w for n, s, w in zip(shape, t.stride(), want)):
         raise ValueError(f"{what} has strides {t.stride()}, the call goes by {want}")
     return t.data_ptr()
 
@@ -387,9 +391,9 @@ def codecomp_rotate(x, positions, rotary: codecomp_rotary, out) -> None:
         raise ValueError("x and out must be bfloat16 [tokens, heads, head_dim] with contiguous heads")
     T, H, d = x.shape
     _int32(positions, (T,), "positions")
-    _on_current(x, positions, out)
+    stream = _launch_stream(x.get_device(), positions.get_device(), out.get_device())
     xs, os_ = x.stride(), out.stride()
-    _check(lib().codecomp_rotate(x.data_ptr(), positions.data_ptr(), C.byref(rotary), T, H, d, xs[0], xs[1], out.data_ptr(), os_[0], os_[1], _stream()),
+    _check(lib().codecomp_rotate(x.data_ptr(), positions.data_ptr(), C.byref(rotary), T, H, d, xs[0], xs[1], out.data_ptr(), os_[0], os_[1], stream),
            "codecomp_rotate")
 
 
@@ -404,9 +408,10 @@ def codecomp_append(q, k, v, positions, rotary: Optional[codecomp_rotary], batch
         op = _vectors(q_out, "q_out", (T, batch.n_q_heads, d), batch.out_stride_tok, batch.out_stride_head)
     if positions is not None:
         _int32(positions, (T,), "positions")
-    _on_current(batch, pages, k, v, *(t for t in (q, q_out, positions) if t is not None))
+    at = pages._at
+    stream = _launch_stream(at, batch._at, k.get_device(), v.get_device(), _at(q, at), _at(q_out, at), _at(positions, at))
     _check(lib().codecomp_append(qp, kp, vp, _ptr(positions), None if rotary is None else C.byref(rotary), C.byref(batch), C.byref(pages), layer, op,
-                                 _stream()), "codecomp_append")
+                                 stream), "codecomp_append")
 
 
 def _rows(t, params, what: str, total: int, strides) -> int:
@@ -414,7 +419,7 @@ def _rows(t, params, what: str, total: int, strides) -> int:
     import torch
     fp8 = params.kv_dtype == KV_FP8_E4M3
     shape = (params.n_layers, params.n_kv_heads, total, params.head_dim)
-    if (t.dtype not in (torch.uint8, torch.float8_e4m3fn) if fp8 else t.dtype != torch.bfloat16) or tuple(t.shape) != shape:
+    if (t.dtype not in (torch.uint8, torch.float8_e4m3fn) if fp8 else t.dtype != torch.bfloat16) or t.shape != shape:
         raise ValueError(f"{what} must be {'8-bit' if fp8 else 'bfloat16'} {shape}, not {t.dtype} {tuple(t.shape)}")
     want = (strides[0] or shape[1] * shape[2] * shape[3], strides[1] or shape[2] * shape[3], strides[2] or shape[3], 1)
     if any(n > 1 and s != w for n, s, w in zip(t.shape, t.stride(), want)):
@@ -445,8 +450,9 @@ def codecomp_pages_store(k, v, idx, params, pages, table, first=None) -> None:
     if idx is not None:
         _idx(idx, params)
     kp, vp = _rows(k, params, "k", total, strides), _rows(v, params, "v", total, strides)
-    _on_current(pages, k, v, table, *(t for t in (idx, first) if t is not None))
-    _check(lib().codecomp_pages_store(kp, vp, _ptr(idx), C.byref(params), C.byref(pages), table.data_ptr(), table.shape[1], _ptr(first), _stream()),
+    at = pages._at
+    stream = _launch_stream(at, k.get_device(), v.get_device(), table.get_device(), _at(idx, at), _at(first, at))
+    _check(lib().codecomp_pages_store(kp, vp, _ptr(idx), C.byref(params), C.byref(pages), table.data_ptr(), table.shape[1], _ptr(first), stream),
            "codecomp_pages_store")
 
 
@@ -457,8 +463,9 @@ def codecomp_pages_load(pages, table, first, idx, params, k, v) -> None:
     if idx is not None:
         _idx(idx, params)
     kp, vp = _rows(k, params, "k", total, strides), _rows(v, params, "v", total, strides)
-    _on_current(pages, k, v, table, *(t for t in (idx, first) if t is not None))
-    _check(lib().codecomp_pages_load(C.byref(pages), table.data_ptr(), table.shape[1], _ptr(first), _ptr(idx), C.byref(params), kp, vp, _stream()),
+    at = pages._at
+    stream = _launch_stream(at, k.get_device(), v.get_device(), table.get_device(), _at(idx, at), _at(first, at))
+    _check(lib().codecomp_pages_load(C.byref(pages), table.data_ptr(), table.shape[1], _ptr(first), _ptr(idx), C.byref(params), kp, vp, stream),
            "codecomp_pages_load")
 
 
@@ -466,16 +473,17 @@ def codecomp_pages_compact(pages, table, first, idx, params, to, to_table, to_fi
     _table(table, first, params)
     _table(to_table, to_first, params)
     _idx(idx, params)
-    _on_current(pages, to, table, to_table, idx, *(t for t in (first, to_first) if t is not None))
+    at = pages._at
+    stream = _launch_stream(at, to._at, table.get_device(), to_table.get_device(), idx.get_device(), _at(first, at), _at(to_first, at))
     _check(lib().codecomp_pages_compact(C.byref(pages), table.data_ptr(), table.shape[1], _ptr(first), idx.data_ptr(), C.byref(params), C.byref(to),
-                                        to_table.data_ptr(), to_table.shape[1], _ptr(to_first), _stream()), "codecomp_pages_compact")
+                                        to_table.data_ptr(), to_table.shape[1], _ptr(to_first), stream), "codecomp_pages_compact")
 
 
 def codecomp_pages_copy(pages, pairs) -> None:
     """pairs: device int32 [n, 2], (source page, target page)."""
     _int32(pairs, (pairs.shape[0], 2), "pairs")
-    _on_current(pages, pairs)
-    _check(lib().codecomp_pages_copy(C.byref(pages), pairs.data_ptr(), pairs.shape[0], _stream()), "codecomp_pages_copy")
+    stream = _launch_stream(pages._at, pairs.get_device())
+    _check(lib().codecomp_pages_copy(C.byref(pages), pairs.data_ptr(), pairs.shape[0], stream), "codecomp_pages_copy")
 
 
 def codecomp_attend_workspace_bytes(batch, pages) -> int:
@@ -487,11 +495,12 @@ def codecomp_attend(q, batch: codecomp_batch, pages: codecomp_pages, layer: int,
     import torch
     shape = (batch._tokens, batch.n_q_heads, pages.head_dim)
     qp, op = _vectors(q, "q", shape, batch.q_stride_tok, batch.q_stride_head), _vectors(out, "out", shape, batch.out_stride_tok, batch.out_stride_head)
-    if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != shape[:2] or not lse.is_contiguous()):
+    if lse is not None and (lse.dtype != torch.float32 or lse.shape != shape[:2] or not lse.is_contiguous()):
         raise ValueError(f"lse must be a contiguous float32 tensor {shape[:2]}, not {lse.dtype} {tuple(lse.shape)}")
-    _on_current(batch, pages, q, out, *(t for t in (lse, workspace) if t is not None))
+    at = pages._at
+    stream = _launch_stream(at, batch._at, q.get_device(), out.get_device(), _at(lse, at), _at(workspace, at))
     size = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    _check(lib().codecomp_attend(qp, C.byref(batch), C.byref(pages), layer, op, _ptr(lse), _ptr(workspace), size, _stream()), "codecomp_attend")
+    _check(lib().codecomp_attend(qp, C.byref(batch), C.byref(pages), layer, op, _ptr(lse), _ptr(workspace), size, stream), "codecomp_attend")
 
 
 class DeviceProblem:

@@ -30,9 +30,10 @@ int make_attend_plan(const codecomp_batch* b, const codecomp_pages* p, AttendPla
     if (rows > few_most) few_most = (int)rows;
   }
   pl->row_blocks = few_most <= 16 ? 1 : few_most <= 32 ? 2 : 4;
+  pl->row_slots = few_most;
   const int64_t items = (int64_t)x.n_seqs * x.Hkv;
-  // chunks of keys: about four workgroups per compute unit if all requests are of the largest length, of at least 128 keys each
-  int64_t chunk = (items * x.max_kv / 1024 + 127) / 128 * 128;
+  // chunks of keys: about two workgroups per compute unit if all requests are of the largest length, of at least 128 keys each
+  int64_t chunk = (items * x.max_kv / 512 + 127) / 128 * 128;
   if (chunk < 128) chunk = 128;
   if (chunk > 2048) chunk = 2048;
   while ((x.max_kv + chunk - 1) / chunk > kFewMostSplits) chunk *= 2;
@@ -41,7 +42,7 @@ int make_attend_plan(const codecomp_batch* b, const codecomp_pages* p, AttendPla
   if (items * pl->splits * 64 > INT32_MAX) return CODECOMP_EINVAL_SHAPE;
   size_t off = 0;
   pl->off_few = off;
-  if (pl->few_rows > 0 && pl->splits > 1) off = align256(off + (size_t)(items * pl->splits * 16 * pl->row_blocks) * (p->head_dim + 2) * sizeof(float));
+  if (pl->few_rows > 0 && pl->splits > 1) off = align256(off + (size_t)(items * pl->splits * pl->row_slots) * (p->head_dim + 2) * sizeof(float));
   pl->off_many = off;
   pl->workgroups = 256;
   if (pl->many_rows > 0)
@@ -107,10 +108,10 @@ int launch_attend(const AttendPlan& pl, const void* q, int layer, void* out, flo
   a.pool = pl.pool; a.b = pl.batch; a.q = static_cast<const uint16_t*>(q); a.out = static_cast<uint16_t*>(out); a.lse = lse;
   a.layer = layer * pl.pool.s_layer;
   a.c = pl.scale * pl.pool.k_scale * kLog2e;
-  a.chunk = pl.chunk; a.splits = pl.splits;
+  a.chunk = pl.chunk; a.splits = pl.splits; a.row_slots = pl.row_slots;
   if (pl.few_rows > 0) {
     a.part_o = reinterpret_cast<float*>(static_cast<char*>(workspace) + pl.off_few);
-    a.part_ml = a.part_o + (size_t)pl.batch.n_seqs * pl.batch.Hkv * pl.splits * 16 * pl.row_blocks * pl.d;
+    a.part_ml = a.part_o + (size_t)pl.batch.n_seqs * pl.batch.Hkv * pl.splits * pl.row_slots * pl.d;
     if (int rc = launch_few(pl, a, stream)) return rc;
   }
   if (pl.many_rows > 0)

@@ -15,24 +15,34 @@ namespace codecomp {
 
 constexpr int kFewWaves = 4, kFewKeys = 32;
 
+// A lane loads 16-byte pieces of two keys of a tile, l16 and 16 + l16: those that its K fragments are made of, in registers as they come (the
+// order of a row's elements in the contraction is free as well: an 8-bit piece is the fragments of two steps), and the same ones of V, which go
+// through LDS.
 template <int D, bool FP8>
 struct FewTile {
-  static constexpr int PIECES = D * (FP8 ? 1 : 2) / 16;      // 16-byte pieces of a stored row
-  static constexpr int ROWS = 64 / PIECES;                    // rows that a load instruction of the wave takes
-  static constexpr int LOADS = kFewKeys / ROWS;
-  // Bytes between rows in LDS: 16 rows of K fragments, and two groups of four V rows, hit all banks once.
-  static constexpr int K_ROW = 2 * D + 16, V_ROW = 2 * D + 32;
-  static constexpr int BYTES = kFewKeys * (K_ROW + V_ROW);
+  static constexpr int LOADS = D * (FP8 ? 1 : 2) / 64;        // pieces of a row per lane
+  static constexpr int V_ROW = 2 * D + 32;                     // bytes between rows in LDS: two groups of four V rows hit all banks once
+  static constexpr int BYTES = kFewKeys * V_ROW;
+  static __device__ __forceinline__ int q_element(int ks, int quarter) {        // that goes with the K fragment of step ks
+    return FP8 ? (ks >> 1) * 64 + quarter * 16 + (ks & 1) * 8 : ks * 32 + quarter * 8;
+  }
+  static __device__ __forceinline__ u32x4 k_frag(const u32x4* piece, int ks) {
+    if constexpr (!FP8) return piece[ks];
+    const u32x4 x = piece[ks >> 1];
+    return ks & 1 ? widen8(x.z, x.w) : widen8(x.x, x.y);
+  }
 };
 
 template <int D, bool FP8, int RB>
-__global__ __launch_bounds__(64 * kFewWaves, RB == 4 ? 1 : 2) void attend_few_kernel(const AttendArgs a) {
+__global__ __launch_bounds__(64 * kFewWaves, RB == 4 ? 1 : RB == 2 ? 2 : 3) void attend_few_kernel(const AttendArgs a) {
   using T = FewTile<D, FP8>;
   constexpr int KS = D / 32, DB = D / 16;
   __shared__ __attribute__((aligned(16))) unsigned char lds[kFewWaves * T::BYTES];
   __shared__ float row_m[kFewWaves][16], row_l[kFewWaves][16];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, quarter = lane >> 4;
-  const int split = blockIdx.x % a.splits, item = blockIdx.x / a.splits;
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), l16 = lane & 15, quarter = lane >> 4;
+  // Chunk by chunk, all requests and heads of one: neighbouring workgroups run on different dies, and must not be the same chunks of all
+  // requests there (short requests lack the later ones).
+  const int items = a.b.n_seqs * a.b.Hkv, split = blockIdx.x / items, item = blockIdx.x - split * items;
   const int r = item / a.b.Hkv, head = item - r * a.b.Hkv;
   const int q0 = a.b.cu_q[r], nq = a.b.cu_q[r + 1] - q0, rows = nq * a.b.G;
   if (rows == 0 || rows > 16 * RB) return;
@@ -41,49 +51,48 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 4 ? 1 : 2) void attend_few_ke
   if (split > 0 && key0 >= len) return;
   const bool whole = len <= a.chunk;                            // the only chunk
 
-  // query rows as right operands: row r16 of block rb, elements 32 ks + 8 quarter ..
+  // query rows as right operands
   u32x4 qf[RB][KS];
   int limit[RB];                                                // keys that the lane's row sees
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
     const int row = rb * 16 + l16, t = min(row, rows - 1) / a.b.G, g = min(row, rows - 1) - t * a.b.G;
-    const uint16_t* p = a.q + (q0 + t) * a.b.q_st + (head * a.b.G + g) * a.b.q_sh + quarter * 8;
+    const uint16_t* p = a.q + (q0 + t) * a.b.q_st + (head * a.b.G + g) * a.b.q_sh;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
-      qf[rb][ks] = *reinterpret_cast<const u32x4*>(p + ks * 32);
+      qf[rb][ks] = *reinterpret_cast<const u32x4*>(p + T::q_element(ks, quarter));
       if (row >= rows) qf[rb][ks] = u32x4{0, 0, 0, 0};
     }
     limit[rb] = a.b.causal ? min(len, len - nq + t + 1) : len;
   }
   const int seen_by_all = a.b.causal ? len - nq + 1 : len;
 
-  const unsigned char* kb = a.pool.k + a.layer + head * a.pool.s_head + (lane % T::PIECES) * 16;
-  const unsigned char* vb = a.pool.v + a.layer + head * a.pool.s_head + (lane % T::PIECES) * 16;
+  const unsigned char* kb = a.pool.k + a.layer + head * a.pool.s_head + quarter * 16;
+  const unsigned char* vb = a.pool.v + a.layer + head * a.pool.s_head + quarter * 16;
   const int32_t* table = a.b.table + (int64_t)r * a.b.table_width;
   const int in_page = (1 << a.pool.page_log2) - 1;
-  unsigned char* ks_lds = lds + wave * T::BYTES;
-  unsigned char* vs_lds = ks_lds + kFewKeys * T::K_ROW;
+  unsigned char* vs_lds = lds + wave * T::BYTES;
 
-  // page of key tile + lane % 32; -1: no such key
-  auto look_up = [&](int tile) {
-    const int key = tile + (lane & 31);
-    int page = -1;
-    if (key < key1) {
-      page = table[key >> a.pool.page_log2];
-      if (page >= a.pool.n_pages) page = -1;
-    }
-    return page;
-  };
-  u32x4 kr[T::LOADS], vr[T::LOADS];
-  auto send_for = [&](int tile, int page) {
+  // Entries of the page table for keys tile + l16 and 16 + tile + l16 (the chunk's last one where there is none), not looked at before they are needed.
+  int page[2], next_page[2];
+  auto look_up = [&](int (&pg)[2], int tile) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < T::LOADS; ++i) {
-      const int row = i * T::ROWS + lane / T::PIECES;
-      const int at = max(__shfl(page, row), 0);                  // rows that are not there: page 0, zeroed below
-      const int64_t off = at * a.pool.s_page + ((tile + row) & in_page) * a.pool.s_tok;
-      kr[i] = *reinterpret_cast<const u32x4*>(kb + off);
-      vr[i] = *reinterpret_cast<const u32x4*>(vb + off);
-    }
+    for (int b = 0; b < 2; ++b) pg[b] = table[max(min(tile + 16 * b + l16, key1 - 1), 0) >> a.pool.page_log2];
+  };
+  u32x4 kr[2][T::LOADS], vr[2][T::LOADS];
+  auto send_for = [&](int tile, const int (&pg)[2]) __attribute__((always_inline)) {
+    int64_t off[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)                                  // rows that are not there: page 0, masked or zeroed below
+      off[b] = (pg[b] >= 0 && pg[b] < a.pool.n_pages ? pg[b] : 0) * a.pool.s_page + ((tile + 16 * b + l16) & in_page) * (int)a.pool.s_tok;
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int i = 0; i < T::LOADS; ++i) kr[b][i] = *reinterpret_cast<const u32x4*>(kb + off[b] + i * 64);
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int i = 0; i < T::LOADS; ++i) vr[b][i] = *reinterpret_cast<const u32x4*>(vb + off[b] + i * 64);
   };
 
   f32x4 o[RB][DB];
@@ -97,56 +106,61 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 4 ? 1 : 2) void attend_few_ke
 
   bool left_out = false;
   int tile = key0 + wave * kFewKeys;
-  int page = look_up(tile), next_page = 0;
-  if (tile < key1) {
-    send_for(tile, page);
-    next_page = look_up(tile + kFewWaves * kFewKeys);
-  }
+  look_up(page, tile);
+  look_up(next_page, tile + kFewWaves * kFewKeys);
+  if (tile < key1) send_for(tile, page);
   for (; tile < key1; tile += kFewWaves * kFewKeys) {
-    const unsigned valid = (unsigned)__ballot(page >= 0);        // lanes 0 .. 31: the keys of the tile
+    bool there[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) there[b] = tile + 16 * b + l16 < key1 && page[b] >= 0 && page[b] < a.pool.n_pages;
+    const unsigned valid = ((unsigned)__ballot(there[0]) & 0xFFFFu) | (unsigned)__ballot(there[1]) << 16;
     const bool plain = valid == 0xFFFFFFFFu && tile + kFewKeys <= seen_by_all;
+    f32x4 s[RB][2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb) s[rb][b] = f32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        const bf16x8 kf = frag(T::k_frag(kr[b], ks));
+#pragma unroll
+        for (int rb = 0; rb < RB; ++rb) s[rb][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, frag(qf[rb][ks]), s[rb][b], 0, 0, 0);
+      }
+    }
     if (__builtin_expect(!plain, 0)) {
 #pragma unroll
-      for (int i = 0; i < T::LOADS; ++i)
-        if (!((valid >> (i * T::ROWS + lane / T::PIECES)) & 1)) kr[i] = vr[i] = u32x4{0, 0, 0, 0};
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int i = 0; i < T::LOADS; ++i)
+          if (!there[b]) vr[b][i] = u32x4{0, 0, 0, 0};
       // a weight of zero must not meet an infinite or NaN value: such values are added at the end, to the rows that see them
       if (tile + kFewKeys > seen_by_all && seen_by_all < len) {
 #pragma unroll
-        for (int i = 0; i < T::LOADS; ++i) vr[i] = finite_part<FP8>(vr[i], left_out);
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int i = 0; i < T::LOADS; ++i) vr[b][i] = finite_part<FP8>(vr[b][i], left_out);
       }
     }
 #pragma unroll
-    for (int i = 0; i < T::LOADS; ++i) {
-      const int row = i * T::ROWS + lane / T::PIECES, col = lane % T::PIECES;
-      if constexpr (FP8) {
-        *reinterpret_cast<u32x4*>(ks_lds + row * T::K_ROW + col * 32) = widen8(kr[i].x, kr[i].y);
-        *reinterpret_cast<u32x4*>(ks_lds + row * T::K_ROW + col * 32 + 16) = widen8(kr[i].z, kr[i].w);
-        *reinterpret_cast<u32x4*>(vs_lds + row * T::V_ROW + col * 32) = widen8(vr[i].x, vr[i].y);
-        *reinterpret_cast<u32x4*>(vs_lds + row * T::V_ROW + col * 32 + 16) = widen8(vr[i].z, vr[i].w);
-      } else {
-        *reinterpret_cast<u32x4*>(ks_lds + row * T::K_ROW + col * 16) = kr[i];
-        *reinterpret_cast<u32x4*>(vs_lds + row * T::V_ROW + col * 16) = vr[i];
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int i = 0; i < T::LOADS; ++i) {
+        unsigned char* at = vs_lds + (16 * b + l16) * T::V_ROW + (i * 64 + quarter * 16) * (FP8 ? 2 : 1);
+        if constexpr (FP8) {
+          *reinterpret_cast<u32x4*>(at) = widen8(vr[b][i].x, vr[b][i].y);
+          *reinterpret_cast<u32x4*>(at + 16) = widen8(vr[b][i].z, vr[b][i].w);
+        } else {
+          *reinterpret_cast<u32x4*>(at) = vr[b][i];
+        }
       }
-    }
     __builtin_amdgcn_wave_barrier();
-    page = next_page;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) page[b] = next_page[b];
     if (tile + kFewWaves * kFewKeys < key1) {
       send_for(tile + kFewWaves * kFewKeys, page);
-      next_page = look_up(tile + 2 * kFewWaves * kFewKeys);
+      look_up(next_page, tile + 2 * kFewWaves * kFewKeys);
     }
 
-    f32x4 s[RB][2];
-#pragma unroll
-    for (int kb2 = 0; kb2 < 2; ++kb2) {
-#pragma unroll
-      for (int rb = 0; rb < RB; ++rb) s[rb][kb2] = f32x4{0, 0, 0, 0};
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        const u32x4 kf = *reinterpret_cast<const u32x4*>(ks_lds + (kb2 * 16 + l16) * T::K_ROW + ks * 64 + quarter * 16);
-#pragma unroll
-        for (int rb = 0; rb < RB; ++rb) s[rb][kb2] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(kf), frag(qf[rb][ks]), s[rb][kb2], 0, 0, 0);
-      }
-    }
     float p[RB][8];
     bool grows = false;
     float top[RB];
@@ -230,7 +244,7 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 4 ? 1 : 2) void attend_few_ke
   // the four waves' shares of every row, 16 rows at a time
   constexpr int O_ROW = D + 4;
   float* o_lds = reinterpret_cast<float*>(lds);
-  static_assert(kFewWaves * 16 * O_ROW * 4 <= kFewWaves * T::BYTES, "rows of a block fit the tiles");
+  static_assert(16 * O_ROW * 4 <= T::BYTES, "rows of a block fit the tiles");
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
     if (rb * 16 >= rows) break;
@@ -267,7 +281,7 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 4 ? 1 : 2) void attend_few_ke
         for (int i = 0; i < E; i += 2) *reinterpret_cast<unsigned*>(out + i) = pack2(x[i] * inv, x[i + 1] * inv);
         if (a.lse && (tid & 15) == 0) a.lse[(int64_t)(q0 + t) * a.b.Hq + h] = all == 0.0f ? -INFINITY : (to + __builtin_amdgcn_logf(all)) * kLn2;
       } else {
-        const int64_t part = (int64_t)blockIdx.x * (16 * RB) + row;
+        const int64_t part = ((int64_t)item * a.splits + split) * a.row_slots + row;
 #pragma unroll
         for (int i = 0; i < E; i += 4) *reinterpret_cast<f32x4*>(a.part_o + part * D + e + i) = f32x4{x[i], x[i + 1], x[i + 2], x[i + 3]};
         if ((tid & 15) == 0) { a.part_ml[2 * part] = to; a.part_ml[2 * part + 1] = all; }
@@ -279,12 +293,12 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 4 ? 1 : 2) void attend_few_ke
 // Chunks joined: a workgroup per row.  Weights of all chunks first, then the outputs, four elements a thread, the chunks shared out over
 // the workgroup's groups of D / 4 threads and these added up in order.
 template <int D>
-__global__ __launch_bounds__(256) void join_few_kernel(const AttendArgs a, int row_slots) {
+__global__ __launch_bounds__(256) void join_few_kernel(const AttendArgs a) {
   constexpr int GROUPS = 256 / (D / 4);
   __shared__ float weight[kFewMostSplits];
   __shared__ float red[4];
   __shared__ f32x4 sums[GROUPS][D / 4];
-  const int row = blockIdx.x % row_slots, item = blockIdx.x / row_slots, tid = threadIdx.x;
+  const int row_slots = a.row_slots, row = blockIdx.x % row_slots, item = blockIdx.x / row_slots, tid = threadIdx.x;
   const int r = item / a.b.Hkv, head = item - r * a.b.Hkv;
   const int q0 = a.b.cu_q[r], rows = (a.b.cu_q[r + 1] - q0) * a.b.G;
   if (rows > row_slots || row >= rows) return;
@@ -343,7 +357,7 @@ static int launch_few_of(const AttendPlan& pl, const AttendArgs& a, hipStream_t 
   else if (pl.row_blocks == 2) attend_few_kernel<D, FP8, 2><<<grid, block, 0, stream>>>(a);
   else attend_few_kernel<D, FP8, 4><<<grid, block, 0, stream>>>(a);
   if (hipError_t e = hipGetLastError()) return (int)e;
-  if (a.splits > 1) join_few_kernel<D><<<dim3((unsigned)(items * 16 * pl.row_blocks)), dim3(256), 0, stream>>>(a, 16 * pl.row_blocks);
+  if (a.splits > 1) join_few_kernel<D><<<dim3((unsigned)(items * a.row_slots)), dim3(256), 0, stream>>>(a);
   return (int)hipGetLastError();
 }
 

@@ -63,7 +63,7 @@ struct AttendPlan {
   int d;
   float scale;
   int few_rows, many_rows;     // requests of each kind (attend.hip)
-  int row_blocks;              // few rows: blocks of 16 rows of the largest
+  int row_blocks, row_slots;   // few rows: blocks of 16 rows of the largest, and its rows
   int chunk, splits;           // few rows: keys of a workgroup, and workgroups per request and head
   int workgroups;              // many rows
   size_t off_few, off_many, ws_bytes;
