@@ -88,16 +88,17 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
   per_head = uniform(per_head);
   const int64_t total = per_head * a.b.Hkv;
   const int64_t workgroups = min((int64_t)ma.workgroups, total);
-  const int g = blockIdx.x;
-  if (g >= workgroups) {
-    if (tid == 0) ma.cuts[g].r = -1;
-    return;
-  }
-  int64_t x = g * total / workgroups;
+  if (tid == 0 && blockIdx.x >= workgroups) ma.cuts[blockIdx.x].r = -1;
+  // neighbours in the sequence read the same keys: they run on the same die (workgroups go to the eight dies in turn)
+  const int per_die = ((int)workgroups + 7) / 8, g = (int)(blockIdx.x & 7) * per_die + (int)(blockIdx.x >> 3);
+  if ((int)(blockIdx.x >> 3) >= per_die || g >= workgroups) return;
   const int64_t x_end = (g + 1) * total / workgroups;
-  int head = (int)(x / per_head);
+  int left = (int)(x_end - g * total / workgroups);               // tiles still to be done
+  // From the end of the part back to its start: blocks are entered at their first keys, at about the same time by all workgroups, so
+  // that the keys and values of a head are read by many at a time.
+  int head = (int)((x_end - 1) / per_head);
   {
-    const int64_t at = x - head * per_head;
+    const int64_t at = x_end - 1 - head * per_head;
     int64_t start = before + incl - mine;
     if (at >= start && at < start + mine) {                      // one thread has it
       for (int r = tid * per;; ++r) {
@@ -115,27 +116,19 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
     }
   }
   __syncthreads();
-  int r = uniform(found[0]), block = uniform(found[1]), tile0 = uniform(found[2]);
+  int r = uniform(found[0]), block = uniform(found[1]), tile1 = uniform(found[2]) + 1;
   Blocks of = uniform(blocks_of(ma, r));
-  bool first_segment = true;
   CutBlock cut = {-1, 0, 0, 0, 0};
 
-  for (; x < x_end;) {
-    if (block >= of.count) {                                     // the next request that has blocks, or the next head
-      do {
-        if (++r == n) { r = 0; ++head; }
-        of = uniform(blocks_of(ma, r));
-      } while (of.count == 0);
-      block = 0;
-    }
+  while (left > 0) {
     const int tiles = of.tiles(block);
-    const int tile1 = (int)min((int64_t)tiles, tile0 + (x_end - x));
+    if (tile1 < 0) tile1 = tiles;
+    const int tile0 = max(0, tile1 - left);
+    left -= tile1 - tile0;
     const bool whole = tile0 == 0 && tile1 == tiles;
-    const int slot = first_segment ? 2 * g : 2 * g + 1;
-    if (tile0 == 0 && tile1 < tiles) {
-      const int64_t end = x + tiles;                             // position behind the block
-      cut = {r, block, head, slot, (int)((end * workgroups - 1) / total)};
-    }
+    const int slot = left == 0 ? 2 * g : 2 * g + 1;
+    if (tile0 == 0 && tile1 < tiles)                             // the rest of the block is the next workgroups'
+      cut = {r, block, head, slot, (int)(((x_end + tiles - tile1) * workgroups - 1) / total)};
     const int q0 = uniform(a.b.cu_q[r]), row0 = block * kManyRows + wave * 32, row = row0 + l32;
     const bool active = row0 < of.rows;
 
@@ -387,10 +380,14 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
         if (half == 0) { a.part_ml[2 * part] = m; a.part_ml[2 * part + 1] = sum; }
       }
     }
-    x += tile1 - tile0;
-    tile0 = 0;
-    ++block;
-    first_segment = false;
+    tile1 = -1;
+    if (left > 0 && --block < 0) {                               // the request before, or the head before
+      do {
+        if (--r < 0) { r = n - 1; --head; }
+        of = uniform(blocks_of(ma, r));
+      } while (of.count == 0);
+      block = of.count - 1;
+    }
   }
   if (tid == 0) ma.cuts[g] = cut;
 }
