@@ -249,6 +249,8 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
       sum += w[15];
       top = fmaxf(fmaxf(top, w[14]), w[15]);
       p[1][3] = pack2(w[14], w[15]);
+      // here, beside the MFMAs, not behind the branch
+      asm volatile("" ::"v"(sum), "v"(p[0][0]), "v"(p[0][1]), "v"(p[0][2]), "v"(p[0][3]), "v"(p[1][0]), "v"(p[1][1]), "v"(p[1][2]), "v"(p[1][3]));
       if (__builtin_expect(__ballot(top > 256.0f) != 0, 0)) {    // a logit far above its row's reference: move the references
         float t = -INFINITY;
 #pragma unroll
