@@ -49,16 +49,25 @@ __device__ __forceinline__ Blocks uniform(Blocks x) {
   return x;
 }
 
+// What a row's number is mixed into the numbers of its 16-byte pieces with, in LDS: 16 rows of K fragments, and four rows of a group of columns
+// of V, hit all banks once.
+template <int D>
+__device__ __forceinline__ int k_swap(int row) { return D == 128 ? row & 15 : (row >> 1) & 7; }
+template <int D>
+__device__ __forceinline__ int v_swap(int row) { return D == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2; }
+
 template <int D, bool FP8>
 __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const ManyArgs ma) {
   const AttendArgs& a = ma.a;
   constexpr int PIECES = D * (FP8 ? 1 : 2) / 16;               // 16-byte pieces of a stored row
-  constexpr int ROWS = kManyThreads / PIECES, LOADS = ROWS > kManyKeys ? 1 : kManyKeys / ROWS;      // rows per load of the workgroup, loads per tile
-  constexpr int K_ROW = 2 * D + 16, V_ROW = 2 * D + 64;          // bytes between rows in LDS: no bank conflicts in either read
+  // rows per load of the workgroup (8 bits) or of a wave, loads per thread and tile
+  constexpr int ROWS = (FP8 ? kManyThreads : 64) / PIECES, LOADS = FP8 ? (ROWS > kManyKeys ? 1 : kManyKeys / ROWS) : kManyKeys / (ROWS * kManyWaves);
   constexpr int KS = D / 16, DB = D / 32;
+  constexpr int TILE = kManyKeys * 2 * D;                        // bytes of the keys of a tile in LDS; its values stand behind them
   static_assert(kManyRows == 32 * kManyWaves, "a block of 32 rows per wave");
-  __shared__ __attribute__((aligned(16))) unsigned char k_lds[2][kManyKeys * K_ROW];
-  __shared__ __attribute__((aligned(16))) unsigned char v_lds[2][kManyKeys * V_ROW];
+  __shared__ __attribute__((aligned(1024))) unsigned char tiles_lds[4 * 2 * TILE];
+  __shared__ int entries[8][kManyKeys];                           // of the page table, for the keys of a tile
+  auto k_tile = [&](int tile) __attribute__((always_inline)) { return tiles_lds + (tile & 3) * (2 * TILE); };
   __shared__ int not_finite;
   __shared__ int64_t wave_sum[kManyWaves];
   __shared__ int found[4];
@@ -147,36 +156,67 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
     }
     const int seen_by_all = of.causal ? min(of.len, of.len - of.nq + block * kManyRows / of.G + 1) : of.len;
 
-    const unsigned char* kb = a.pool.k + a.layer + head * a.pool.s_head + (tid % PIECES) * 16;
-    const unsigned char* vb = a.pool.v + a.layer + head * a.pool.s_head + (tid % PIECES) * 16;
+    const unsigned char* kb = a.pool.k + a.layer + head * a.pool.s_head;
+    const unsigned char* vb = a.pool.v + a.layer + head * a.pool.s_head;
     const int32_t* table = a.b.table + (int64_t)r * a.b.table_width;
     const int in_page = (1 << a.pool.page_log2) - 1;
-    // Entry of the page table for key 64 tile + lane (for the last key where there is none), not looked at before it is needed.
-    auto look_up = [&](int tile) __attribute__((always_inline)) { return table[max(min(tile * kManyKeys + lane, of.len - 1), 0) >> a.pool.page_log2]; };
+
+    // ---- the way of keys and values.  The page table's entries of a tile's 64 keys go into LDS five tiles ahead, the tile itself three ahead: 16-bit
+    // rows straight from memory into one of four buffers, 8-bit rows by way of registers, where they are widened.  Rows of a buffer are not
+    // padded; their 16-byte pieces stand in another order from row to row (k_swap, v_swap), so that neither read meets bank conflicts.
+    auto fetch_entries = [&](int tile) __attribute__((always_inline)) {           // for the last key where a tile has none
+      const int32_t* from = table + (max(min(tile * kManyKeys + lane, of.len - 1), 0) >> a.pool.page_log2);
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds_address(entries[tile & 7])), "v"(from) : "memory", "m0");
+    };
+    auto row_of = [&](int i) __attribute__((always_inline)) { return ((FP8 ? i * ROWS + tid / PIECES : (wave * LOADS + i) * ROWS + lane / PIECES)) & (kManyKeys - 1); };
+    // where one of this thread's rows of a tile is; rows that are not there: in page 0, taken out of the tile when it is used
+    auto place = [&](int tile, int i) __attribute__((always_inline)) {
+      const int row = row_of(i), page = entries[tile & 7][row];
+      return (page >= 0 && page < a.pool.n_pages ? page : 0) * a.pool.s_page + ((tile * kManyKeys + row) & in_page) * (int)a.pool.s_tok;
+    };
+    u32x4 kr[FP8 ? LOADS : 1], vr[FP8 ? LOADS : 1];              // 8 bits: the tile after the next two, on its way
+    auto fetch_row = [&](int tile, int i, int64_t off) __attribute__((always_inline)) {
+      const int row = row_of(i);
+      if constexpr (FP8) {
+        kr[i] = *reinterpret_cast<const u32x4*>(kb + off + (tid % PIECES) * 16);
+        vr[i] = *reinterpret_cast<const u32x4*>(vb + off + (tid % PIECES) * 16);
+      } else {
+        const int slot = lane % PIECES;
+        const uint32_t to = lds_address(k_tile(tile)) + (wave * LOADS + i) * 1024;
+        const unsigned char* from = kb + off + (slot ^ k_swap<D>(row)) * 16;
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory", "m0");
+        from = vb + off + (slot ^ v_swap<D>(row)) * 16;
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to + TILE), "v"(from) : "memory", "m0");
+      }
+    };
+    auto park_row = [&](int tile, int i) __attribute__((always_inline)) {         // 8 bits
+      if constexpr (FP8) {
+        const int row = i * ROWS + tid / PIECES, piece = (tid % PIECES) * 2;
+        if (ROWS > kManyKeys && row >= kManyKeys) return;          // half of the threads have a row (head_dim 64)
+        unsigned char* at = k_tile(tile) + row * 2 * D;
+        *reinterpret_cast<u32x4*>(at + (piece ^ k_swap<D>(row)) * 16) = widen8(kr[i].x, kr[i].y);
+        *reinterpret_cast<u32x4*>(at + ((piece + 1) ^ k_swap<D>(row)) * 16) = widen8(kr[i].z, kr[i].w);
+        *reinterpret_cast<u32x4*>(at + TILE + (piece ^ v_swap<D>(row)) * 16) = widen8(vr[i].x, vr[i].y);
+        *reinterpret_cast<u32x4*>(at + TILE + ((piece + 1) ^ v_swap<D>(row)) * 16) = widen8(vr[i].z, vr[i].w);
+      }
+    };
     auto is_there = [&](int tile, int page) __attribute__((always_inline)) {
       return __ballot(tile < tile1 && tile * kManyKeys + lane < of.len && page >= 0 && page < a.pool.n_pages);
     };
-    // where this thread's rows of a tile are; rows that are not there: in page 0, zeroed before they are parked
-    auto places = [&](int64_t (&off)[LOADS], int tile, int page) __attribute__((always_inline)) {
-      if (page >= a.pool.n_pages) page = 0;
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        const int at = (i * ROWS + tid / PIECES) & (kManyKeys - 1);
-        off[i] = max(__shfl(page, at), 0) * a.pool.s_page + ((tile * kManyKeys + at) & in_page) * (int)a.pool.s_tok;
+    auto partly = [&](int tile) { return (tile + 1) * kManyKeys > seen_by_all && seen_by_all < of.len; };       // some rows do not see all of it
+    // Values of a tile that has keys that are not there, or that some rows do not see: a weight of zero must not meet what stands in the one, nor an
+    // infinite or NaN value in the other (added at the end, to the rows that see them).
+    auto clean_values = [&](int tile, uint64_t valid) __attribute__((always_inline)) {
+      bool any = false;
+      for (int i = tid; i < TILE / 16; i += kManyThreads) {
+        u32x4* at = reinterpret_cast<u32x4*>(k_tile(tile) + TILE + i * 16);
+        u32x4 v = *at;
+        if (!((valid >> (i / (D / 8))) & 1)) v = u32x4{0, 0, 0, 0};
+        if (partly(tile)) v = finite_part<false>(v, any);
+        *at = v;
       }
+      if (any) not_finite = 1;
     };
-    auto park = [&](unsigned char* lds, int row_bytes, u32x4 from, int i) __attribute__((always_inline)) {
-      if (ROWS > kManyKeys && tid / PIECES >= kManyKeys) return;           // half of the threads have a row (head_dim 64, 8 bits)
-      unsigned char* at = lds + (i * ROWS + tid / PIECES) * row_bytes + (tid % PIECES) * (FP8 ? 32 : 16);
-      if constexpr (FP8) {
-        *reinterpret_cast<u32x4*>(at) = widen8(from.x, from.y);
-        *reinterpret_cast<u32x4*>(at + 16) = widen8(from.z, from.w);
-      } else {
-        *reinterpret_cast<u32x4*>(at) = from;
-      }
-    };
-    u32x4 kr[LOADS], vr[LOADS];                                  // keys of the tile after the next, values of the next one, on their way
-    int64_t k_off[LOADS], v_off[LOADS];
 
     f32x16 o[DB];
     float m = -1.0e30f, l = 0.0f;                                // a row's reference, this half's sum of weights
@@ -188,29 +228,25 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
     u32x4 pa[2], pb[2] = {u32x4{0, 0, 0, 0}, u32x4{0, 0, 0, 0}}; // their weights, 16 keys each
 
     // Key fragment f (16 of a row's elements of 32 keys), value fragment f (32 columns of 16 keys).
-    auto key_frag = [&](const unsigned char* kt, int f) __attribute__((always_inline)) {
-      return *reinterpret_cast<const u32x4*>(kt + l32 * K_ROW + f * 32 + half * 16);
-    };
+    const int k_lane = l32 * 2 * D + (half ^ k_swap<D>(l32)) * 16;
+    const int v_lane = (half * 4 + ((lane >> 2) & 3)) * 2 * D + v_swap<D>((lane >> 2) & 3) * 16 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+    auto key_frag = [&](const unsigned char* kt, int f) __attribute__((always_inline)) { return *reinterpret_cast<const u32x4*>(kt + (k_lane ^ (f * 32))); };
     auto value_frag = [&](const unsigned char* vt, int f) __attribute__((always_inline)) {
-      const unsigned char* at = vt + ((f / DB) * 16 + half * 4 + ((lane >> 2) & 3)) * V_ROW + (f % DB) * 64 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
-      const s16x4 v0 = read_columns(at), v1 = read_columns(at + 8 * V_ROW);
+      const unsigned char* at = vt + (f / DB) * 32 * D + (v_lane ^ ((f % DB) * 64));
+      const s16x4 v0 = read_columns(at), v1 = read_columns(at + 16 * D);
       return __builtin_bit_cast(u32x4, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
     };
-    auto logits = [&](f32x16& z, const unsigned char* kt) __attribute__((always_inline)) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) z[i] = 0.0f;
-#pragma unroll
-      for (int f = 0; f < KS; ++f) z = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(key_frag(kt, f)), frag(qf[f]), z, 0, 0, 0);
-    };
-    auto weigh_values = [&](const unsigned char* vt, const u32x4 (&p)[2]) __attribute__((always_inline)) {
-#pragma unroll
-      for (int f = 0; f < KS; ++f) o[f % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(value_frag(vt, f)), frag(p[f / DB]), o[f % DB], 0, 0, 0);
+    constexpr int F = 2 * KS, RING = 4, PER = 16 / F, HALF = 64 * D;      // fragments of a step, those held, logits per fragment; bytes of 32 rows
+    u32x4 ring[RING];
+    auto fetch = [&](int f, const unsigned char* kt, const unsigned char* vt) __attribute__((always_inline)) {
+      ring[f % RING] = f & 1 ? value_frag(vt, f / 2) : key_frag(kt, f / 2);
     };
     // One step: the weights p of the 32 keys from key0 on, whose logits are z (`valid`: which of them there are); beside them, on the matrix cores,
-    // the logits zn of the next 32 keys and the outputs of the 32 before, whose weights are pp.  The order is the source's: an MFMA, the LDS read that
-    // one three further on needs, the vector work of a logit (two at head_dim 64), and what `beside` has for this place.
-    auto step = [&](f32x16& z, u32x4 (&p)[2], f32x16& zn, const unsigned char* kt, const u32x4 (&pp)[2], const unsigned char* vt, int key0, unsigned valid,
-                    auto&& beside) __attribute__((always_inline)) {
+    // the logits zn of the next 32 keys (kt) and the outputs of the 32 before (vt), whose weights are pp.  The order is the source's: the LDS read that
+    // the MFMA three further on needs (from the next step's tiles at the end), an MFMA, the vector work of a logit (two at head_dim 64), and
+    // what `beside` has for this place.
+    auto step = [&](f32x16& z, u32x4 (&p)[2], f32x16& zn, const unsigned char* kt, const u32x4 (&pp)[2], const unsigned char* vt, const unsigned char* kt_next,
+                    const unsigned char* vt_next, int key0, unsigned valid, auto&& beside) __attribute__((always_inline)) {
       if (__builtin_expect(valid != 0xFFFFFFFFu || key0 + 32 > seen_by_all, 0)) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
@@ -218,19 +254,15 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
           if (!((valid >> j) & 1) || key0 + j >= limit) z[i] = -INFINITY;
         }
       }
-      constexpr int F = 2 * KS, RING = 4, PER = 16 / F;
-      u32x4 ring[RING];
       float sum = 0.0f, top = 0.0f, w[16];
-      auto fetch = [&](int f) __attribute__((always_inline)) { ring[f % RING] = f & 1 ? value_frag(vt, f / 2) : key_frag(kt, f / 2); };
 #pragma unroll
       for (int i = 0; i < 16; ++i) zn[i] = 0.0f;
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int f = 0; f < RING - 1; ++f) fetch(f);
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
       for (int f = 0; f < F; ++f) {
-        if (f + RING - 1 < F) fetch(f + RING - 1);
+        beside(f);
+        if (f + RING - 1 < F) fetch(f + RING - 1, kt, vt);
+        else fetch(f + RING - 1 - F, kt_next, vt_next);
         const int i = f / 2;
         if (f & 1) o[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(ring[f % RING]), frag(pp[i / DB]), o[i % DB], 0, 0, 0);
         else zn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(ring[f % RING]), frag(qf[i]), zn, 0, 0, 0);
@@ -243,7 +275,6 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
             p[(e - 2) >> 3][((e - 2) & 7) >> 1] = pack2(w[e - 2], w[e - 1]);
           }
         }
-        beside(f);
         __builtin_amdgcn_sched_barrier(0);
       }
       sum += w[15];
@@ -274,77 +305,63 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
       }
       l += sum;
     };
-    auto zero_rows = [&](u32x4* into, uint64_t valid) {
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i)
-        if (!((valid >> ((i * ROWS + tid / PIECES) & (kManyKeys - 1))) & 1)) into[i] = u32x4{0, 0, 0, 0};
-    };
-    auto partly = [&](int tile) { return (tile + 1) * kManyKeys > seen_by_all && seen_by_all < of.len; };       // some rows do not see all of it
-    auto lds_barrier = [&]() __attribute__((always_inline)) { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
 
-    // ---- tiles.  A tile's keys are in LDS a step before its values.
-    lds_barrier();                                               // the segment before is through with LDS
+    // ---- before the first tile
+    __syncthreads();                                             // the segment before is through with LDS
     if (tid == 0) not_finite = 0;
-    int page = look_up(tile0), page_next = look_up(tile0 + 1);
-    places(k_off, tile0, page);
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) kr[i] = *reinterpret_cast<const u32x4*>(kb + k_off[i]);
+    for (int j = 0; j < 5; ++j) fetch_entries(tile0 + j);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) vr[i] = *reinterpret_cast<const u32x4*>(vb + k_off[i]);
-    // in front of the first tile: values of zero
-    for (int i = tid; i < 32 * V_ROW / 16; i += kManyThreads) *reinterpret_cast<u32x4*>(v_lds[(tile0 + 1) & 1] + 32 * V_ROW + i * 16) = u32x4{0, 0, 0, 0};
-    zero_rows(kr, is_there(tile0, page));
+    for (int j = 0; j < 3; ++j)
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) park(k_lds[tile0 & 1], K_ROW, kr[i], i);
-    places(v_off, tile0 + 1, page_next);
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) kr[i] = *reinterpret_cast<const u32x4*>(kb + v_off[i]);
-    lds_barrier();
-    if (active) logits(za, k_lds[tile0 & 1]);
-    for (int tile = tile0; tile < tile1; ++tile) {
-      const uint64_t valid = is_there(tile, page), valid_next = is_there(tile + 1, page_next);
-      // to be parked during the first step: the next tile's keys and this one's values
-      if (__builtin_expect(valid_next != ~0ull, 0)) zero_rows(kr, valid_next);
-      if (__builtin_expect(valid != ~0ull || partly(tile), 0)) {
-        zero_rows(vr, valid);
-        // a weight of zero must not meet an infinite or NaN value: such values are added at the end, to the rows that see them
-        if (partly(tile)) {
-          bool any = false;
-#pragma unroll
-          for (int i = 0; i < LOADS; ++i) vr[i] = finite_part<FP8>(vr[i], any);
-          if (any) not_finite = 1;
-        }
+      for (int i = 0; i < LOADS; ++i) {
+        fetch_row(tile0 + j, i, place(tile0 + j, i));
+        if (j < 2) park_row(tile0 + j, i);
       }
-      const int page_after = look_up(tile + 2);
-      unsigned char* next_keys = k_lds[(tile + 1) & 1];
-      unsigned char* these_values = v_lds[tile & 1];
-      auto park_some = [&](int f) __attribute__((always_inline)) {
-        constexpr int AT = 2 * KS - 2 * LOADS;                   // the last places of the step
-        if (f >= AT && f < AT + LOADS) park(next_keys, K_ROW, kr[f - AT], f - AT);
-        if (f >= AT + LOADS) park(these_values, V_ROW, vr[f - AT - LOADS], f - AT - LOADS);
-      };
-      auto send_some = [&](int f) __attribute__((always_inline)) {
-        if (f == 0) places(k_off, tile + 2, page_after);
-        if (f >= 1 && f <= LOADS) kr[f - 1] = *reinterpret_cast<const u32x4*>(kb + k_off[f - 1]);
-        if (f >= 1 + LOADS && f <= 2 * LOADS) vr[f - 1 - LOADS] = *reinterpret_cast<const u32x4*>(vb + v_off[f - 1 - LOADS]);
-        if (f == 2 * LOADS) {
-#pragma unroll
-          for (int i = 0; i < LOADS; ++i) v_off[i] = k_off[i];
-        }
-      };
-      if (active)
-        step(za, pa, zb, k_lds[tile & 1] + 32 * K_ROW, pb, v_lds[(tile + 1) & 1] + 32 * V_ROW, tile * kManyKeys, (unsigned)valid, park_some);
-      else
-        for (int f = 0; f < 2 * KS; ++f) park_some(f);
-      lds_barrier();
-      if (active)
-        step(zb, pb, za, next_keys, pa, these_values, tile * kManyKeys + 32, (unsigned)(valid >> 32), send_some);
-      else
-        for (int f = 0; f < 2 * KS; ++f) send_some(f);
-      page = page_next; page_next = page_after;
-    }
+    // in front of the first tile: values of zero
+    for (int i = tid; i < HALF / 16; i += kManyThreads) *reinterpret_cast<u32x4*>(k_tile(tile0 + 3) + TILE + HALF + i * 16) = u32x4{0, 0, 0, 0};
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * LOADS) : "memory");
+    uint64_t valid = is_there(tile0, entries[tile0 & 7][lane]);
     if (active) {
-      weigh_values(v_lds[(tile1 + 1) & 1] + 32 * V_ROW, pb);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) za[i] = 0.0f;
+#pragma unroll
+      for (int f = 0; f < KS; ++f) za = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(key_frag(k_tile(tile0), f)), frag(qf[f]), za, 0, 0, 0);
+#pragma unroll
+      for (int f = 0; f < RING - 1; ++f) fetch(f, k_tile(tile0) + HALF, k_tile(tile0 + 3) + TILE + HALF);
+    }
+    for (int tile = tile0; tile < tile1; ++tile) {
+      if (__builtin_expect(valid != ~0ull || partly(tile), 0)) clean_values(tile, valid);
+      const unsigned char *t0 = k_tile(tile), *t1 = k_tile(tile + 1), *before = k_tile(tile + 3);
+      // All of this step's LDS reads are on their way by the last places: from there on the tile before is nobody's, and the next one is everybody's.
+      auto pass_on = [&](int f) __attribute__((always_inline)) {
+        if (f == F - (RING - 1)) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * LOADS + 1) : "memory");
+      };
+      int64_t off[LOADS];
+      int next_entry = 0;
+      auto send_for = [&](int f) __attribute__((always_inline)) {
+        if (f == 0) next_entry = entries[(tile + 1) & 7][lane];
+        if (f < LOADS) park_row(tile + 2, f);
+        if (f >= 1 && f <= LOADS) off[f - 1] = place(tile + 3, f - 1);
+        if (f >= 3 && f < 3 + LOADS) fetch_row(tile + 3, f - 3, off[f - 3]);
+        if (f == 3 + LOADS) fetch_entries(tile + 5);
+      };
+      if (active) {
+        step(za, pa, zb, t0 + HALF, pb, before + TILE + HALF, t1, t0 + TILE, tile * kManyKeys, (unsigned)valid, pass_on);
+        step(zb, pb, za, t1, pa, t0 + TILE, t1 + HALF, t0 + TILE + HALF, tile * kManyKeys + 32, (unsigned)(valid >> 32), send_for);
+      } else {
+        pass_on(F - (RING - 1));
+#pragma unroll
+        for (int f = 0; f < F; ++f) send_for(f);
+      }
+      valid = is_there(tile + 1, next_entry);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // what was sent for beyond the last tile
+    if (active) {
+#pragma unroll
+      for (int f = 0; f < KS; ++f)
+        o[f % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(value_frag(k_tile(tile1 + 3) + TILE + HALF, f)), frag(pb[f / DB]), o[f % DB], 0, 0, 0);
       if (__builtin_expect(partly(tile1 - 1) && not_finite != 0, 0)) {
         for (int key = max(seen_by_all, tile0 * kManyKeys); key < min(of.len, tile1 * kManyKeys); ++key) {
           const int at = table[key >> a.pool.page_log2];
