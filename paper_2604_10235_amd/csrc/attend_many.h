@@ -49,19 +49,23 @@ __device__ __forceinline__ Blocks uniform(Blocks x) {
   return x;
 }
 
-// What a row's number is mixed into the numbers of its 16-byte pieces with, in LDS: 16 rows of K fragments, and four rows of a group of columns
-// of V, hit all banks once.
+// A tile in LDS: chunks of 1 KB, 16 rows of four 16-byte pieces, what a wave loads at a time.  Keys stand piece by piece in a chunk (16 rows of one,
+// then of the next: a fragment's read meets every bank once), values row by row (four rows are the 256 bytes that the transposing read takes from
+// half a wave).  Either way a fragment's number only adds a constant to a lane's address.
 template <int D>
-__device__ __forceinline__ int k_swap(int row) { return D == 128 ? row & 15 : (row >> 1) & 7; }
-template <int D>
-__device__ __forceinline__ int v_swap(int row) { return D == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2; }
+struct TileAt {
+  static constexpr int GROUP = D / 32 * 1024;          // bytes of 16 rows
+  static __device__ __forceinline__ int key(int row, int piece) { return (row >> 4) * GROUP + (piece >> 2) * 1024 + (piece & 3) * 256 + (row & 15) * 16; }
+  static __device__ __forceinline__ int value(int row, int piece) { return (row >> 4) * GROUP + (piece >> 2) * 1024 + (row & 15) * 64 + (piece & 3) * 16; }
+};
 
 template <int D, bool FP8>
 __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const ManyArgs ma) {
   const AttendArgs& a = ma.a;
   constexpr int PIECES = D * (FP8 ? 1 : 2) / 16;               // 16-byte pieces of a stored row
-  // rows per load of the workgroup (8 bits) or of a wave, loads per thread and tile
-  constexpr int ROWS = (FP8 ? kManyThreads : 64) / PIECES, LOADS = FP8 ? (ROWS > kManyKeys ? 1 : kManyKeys / ROWS) : kManyKeys / (ROWS * kManyWaves);
+  // 16-byte pieces of K and of V per thread and tile: of one row (8 bits), or of a wave's chunks, which lie side by side in 16 rows
+  constexpr int LOADS = FP8 ? 1 : D / 64;
+  using At = TileAt<D>;
   constexpr int KS = D / 16, DB = D / 32;
   constexpr int TILE = kManyKeys * 2 * D;                        // bytes of the keys of a tile in LDS; its values stand behind them
   static_assert(kManyRows == 32 * kManyWaves, "a block of 32 rows per wave");
@@ -162,42 +166,49 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
     const int in_page = (1 << a.pool.page_log2) - 1;
 
     // ---- the way of keys and values.  The page table's entries of a tile's 64 keys go into LDS five tiles ahead, the tile itself three ahead: 16-bit
-    // rows straight from memory into one of four buffers, 8-bit rows by way of registers, where they are widened.  Rows of a buffer are not
-    // padded; their 16-byte pieces stand in another order from row to row (k_swap, v_swap), so that neither read meets bank conflicts.
+    // rows straight from memory into one of four buffers, 8-bit rows by way of registers, where they are widened.
     auto fetch_entries = [&](int tile) __attribute__((always_inline)) {           // for the last key where a tile has none
       const int32_t* from = table + (max(min(tile * kManyKeys + lane, of.len - 1), 0) >> a.pool.page_log2);
       asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds_address(entries[tile & 7])), "v"(from) : "memory", "m0");
     };
-    auto row_of = [&](int i) __attribute__((always_inline)) { return ((FP8 ? i * ROWS + tid / PIECES : (wave * LOADS + i) * ROWS + lane / PIECES)) & (kManyKeys - 1); };
-    // where one of this thread's rows of a tile is; rows that are not there: in page 0, taken out of the tile when it is used
-    auto place = [&](int tile, int i) __attribute__((always_inline)) {
-      const int row = row_of(i), page = entries[tile & 7][row];
-      return (page >= 0 && page < a.pool.n_pages ? page : 0) * a.pool.s_page + ((tile * kManyKeys + row) & in_page) * (int)a.pool.s_tok;
+    // The rows of a tile that this thread loads pieces of: 8 bits, one and the same of K and V (the last ones by no thread at head_dim 64); 16 bits,
+    // of the wave's 16 rows, the lane % 16th of K and the lane / 4th of V.
+    const int k_row = FP8 ? (tid / PIECES) & (kManyKeys - 1) : (wave >> 1) * 16 + (lane & 15), v_row = FP8 ? k_row : (wave >> 1) * 16 + (lane >> 2);
+    const int k_piece = FP8 ? tid % PIECES : (wave & 1) * LOADS * 4 + (lane >> 4), v_piece = FP8 ? k_piece : (wave & 1) * LOADS * 4 + (lane & 3);
+    // where one of them is; rows that are not there: in page 0, taken out of the tile when it is used
+    auto place = [&](int tile, int row, int piece) __attribute__((always_inline)) {
+      const int page = entries[tile & 7][row];
+      return (page >= 0 && page < a.pool.n_pages ? page : 0) * a.pool.s_page + (((tile * kManyKeys + row) & in_page) * (int)a.pool.s_tok + piece * 16);
     };
-    u32x4 kr[FP8 ? LOADS : 1], vr[FP8 ? LOADS : 1];              // 8 bits: the tile after the next two, on its way
-    auto fetch_row = [&](int tile, int i, int64_t off) __attribute__((always_inline)) {
-      const int row = row_of(i);
+    u32x4 kr, vr;                                                // 8 bits: the tile after the next two, on its way
+    auto fetch_keys = [&](int tile, int64_t off) __attribute__((always_inline)) {
       if constexpr (FP8) {
-        kr[i] = *reinterpret_cast<const u32x4*>(kb + off + (tid % PIECES) * 16);
-        vr[i] = *reinterpret_cast<const u32x4*>(vb + off + (tid % PIECES) * 16);
+        kr = *reinterpret_cast<const u32x4*>(kb + off);
       } else {
-        const int slot = lane % PIECES;
-        const uint32_t to = lds_address(k_tile(tile)) + (wave * LOADS + i) * 1024;
-        const unsigned char* from = kb + off + (slot ^ k_swap<D>(row)) * 16;
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory", "m0");
-        from = vb + off + (slot ^ v_swap<D>(row)) * 16;
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to + TILE), "v"(from) : "memory", "m0");
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i)
+          asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_address(k_tile(tile)) + (wave * LOADS + i) * 1024),
+                       "v"(kb + off + i * 64) : "memory", "m0");
       }
     };
-    auto park_row = [&](int tile, int i) __attribute__((always_inline)) {         // 8 bits
+    auto fetch_values = [&](int tile, int64_t off) __attribute__((always_inline)) {
       if constexpr (FP8) {
-        const int row = i * ROWS + tid / PIECES, piece = (tid % PIECES) * 2;
-        if (ROWS > kManyKeys && row >= kManyKeys) return;          // half of the threads have a row (head_dim 64)
-        unsigned char* at = k_tile(tile) + row * 2 * D;
-        *reinterpret_cast<u32x4*>(at + (piece ^ k_swap<D>(row)) * 16) = widen8(kr[i].x, kr[i].y);
-        *reinterpret_cast<u32x4*>(at + ((piece + 1) ^ k_swap<D>(row)) * 16) = widen8(kr[i].z, kr[i].w);
-        *reinterpret_cast<u32x4*>(at + TILE + (piece ^ v_swap<D>(row)) * 16) = widen8(vr[i].x, vr[i].y);
-        *reinterpret_cast<u32x4*>(at + TILE + ((piece + 1) ^ v_swap<D>(row)) * 16) = widen8(vr[i].z, vr[i].w);
+        vr = *reinterpret_cast<const u32x4*>(vb + off);
+      } else {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i)
+          asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_address(k_tile(tile)) + TILE + (wave * LOADS + i) * 1024),
+                       "v"(vb + off + i * 64) : "memory", "m0");
+      }
+    };
+    auto park = [&](int tile) __attribute__((always_inline)) {                   // 8 bits
+      if constexpr (FP8) {
+        if (kManyThreads / PIECES > kManyKeys && tid / PIECES >= kManyKeys) return;
+        unsigned char* at = k_tile(tile);
+        *reinterpret_cast<u32x4*>(at + At::key(k_row, 2 * k_piece)) = widen8(kr.x, kr.y);
+        *reinterpret_cast<u32x4*>(at + At::key(k_row, 2 * k_piece + 1)) = widen8(kr.z, kr.w);
+        *reinterpret_cast<u32x4*>(at + TILE + At::value(v_row, 2 * v_piece)) = widen8(vr.x, vr.y);
+        *reinterpret_cast<u32x4*>(at + TILE + At::value(v_row, 2 * v_piece + 1)) = widen8(vr.z, vr.w);
       }
     };
     auto is_there = [&](int tile, int page) __attribute__((always_inline)) {
@@ -211,7 +222,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
       for (int i = tid; i < TILE / 16; i += kManyThreads) {
         u32x4* at = reinterpret_cast<u32x4*>(k_tile(tile) + TILE + i * 16);
         u32x4 v = *at;
-        if (!((valid >> (i / (D / 8))) & 1)) v = u32x4{0, 0, 0, 0};
+        if (!((valid >> (i * 16 / At::GROUP * 16 + ((i >> 2) & 15))) & 1)) v = u32x4{0, 0, 0, 0};
         if (partly(tile)) v = finite_part<false>(v, any);
         *at = v;
       }
@@ -228,15 +239,14 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
     u32x4 pa[2], pb[2] = {u32x4{0, 0, 0, 0}, u32x4{0, 0, 0, 0}}; // their weights, 16 keys each
 
     // Key fragment f (16 of a row's elements of 32 keys), value fragment f (32 columns of 16 keys).
-    const int k_lane = l32 * 2 * D + (half ^ k_swap<D>(l32)) * 16;
-    const int v_lane = (half * 4 + ((lane >> 2) & 3)) * 2 * D + v_swap<D>((lane >> 2) & 3) * 16 + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
-    auto key_frag = [&](const unsigned char* kt, int f) __attribute__((always_inline)) { return *reinterpret_cast<const u32x4*>(kt + (k_lane ^ (f * 32))); };
+    const int k_lane = At::key(l32, half), v_lane = At::value(half * 4 + ((lane >> 2) & 3), 0) + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+    auto key_frag = [&](const unsigned char* kt, int f) __attribute__((always_inline)) { return *reinterpret_cast<const u32x4*>(kt + k_lane + f * 512); };
     auto value_frag = [&](const unsigned char* vt, int f) __attribute__((always_inline)) {
-      const unsigned char* at = vt + (f / DB) * 32 * D + (v_lane ^ ((f % DB) * 64));
-      const s16x4 v0 = read_columns(at), v1 = read_columns(at + 16 * D);
+      const unsigned char* at = vt + v_lane + (f / DB) * At::GROUP + (f % DB) * 1024;
+      const s16x4 v0 = read_columns(at), v1 = read_columns(at + 512);
       return __builtin_bit_cast(u32x4, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
     };
-    constexpr int F = 2 * KS, RING = 4, PER = 16 / F, HALF = 64 * D;      // fragments of a step, those held, logits per fragment; bytes of 32 rows
+    constexpr int F = 2 * KS, RING = 4, PER = 16 / F, HALF = 2 * At::GROUP;      // fragments of a step, those held, logits per fragment; bytes of 32 rows
     u32x4 ring[RING];
     auto fetch = [&](int f, const unsigned char* kt, const unsigned char* vt) __attribute__((always_inline)) {
       ring[f % RING] = f & 1 ? value_frag(vt, f / 2) : key_frag(kt, f / 2);
@@ -254,7 +264,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
           if (!((valid >> j) & 1) || key0 + j >= limit) z[i] = -INFINITY;
         }
       }
-      float sum = 0.0f, top = 0.0f, w[16];
+      float sum = 0.0f, w[16];
 #pragma unroll
       for (int i = 0; i < 16; ++i) zn[i] = 0.0f;
       __builtin_amdgcn_sched_barrier(0);
@@ -270,19 +280,17 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
         for (int e = f * PER; e < (f + 1) * PER; ++e) {
           w[e] = __builtin_amdgcn_exp2f(fmaf(z[e], a.c, -m));
           if (e > 0) sum += w[e - 1];
-          if (e > 1 && (e & 1) == 0) {
-            top = fmaxf(fmaxf(top, w[e - 2]), w[e - 1]);
-            p[(e - 2) >> 3][((e - 2) & 7) >> 1] = pack2(w[e - 2], w[e - 1]);
-          }
+          if (e > 1 && (e & 1) == 0) p[(e - 2) >> 3][((e - 2) & 7) >> 1] = pack2(w[e - 2], w[e - 1]);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
       sum += w[15];
-      top = fmaxf(fmaxf(top, w[14]), w[15]);
       p[1][3] = pack2(w[14], w[15]);
       // here, beside the MFMAs, not behind the branch
       asm volatile("" ::"v"(sum), "v"(p[0][0]), "v"(p[0][1]), "v"(p[0][2]), "v"(p[0][3]), "v"(p[1][0]), "v"(p[1][1]), "v"(p[1][2]), "v"(p[1][3]));
-      if (__builtin_expect(__ballot(top > 256.0f) != 0, 0)) {    // a logit far above its row's reference: move the references
+      // A logit far above its row's reference: move the references.  (Weights are positive: none is larger than their sum, and as
+      // long as that is below 4096 nothing is lost in fp32 or bf16.)
+      if (__builtin_expect(__ballot(sum > 4096.0f) != 0, 0)) {
         float t = -INFINITY;
 #pragma unroll
         for (int i = 0; i < 16; ++i) t = fmaxf(t, z[i]);
@@ -313,12 +321,11 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
     for (int j = 0; j < 5; ++j) fetch_entries(tile0 + j);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
-    for (int j = 0; j < 3; ++j)
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        fetch_row(tile0 + j, i, place(tile0 + j, i));
-        if (j < 2) park_row(tile0 + j, i);
-      }
+    for (int j = 0; j < 3; ++j) {
+      fetch_keys(tile0 + j, place(tile0 + j, k_row, k_piece));
+      fetch_values(tile0 + j, place(tile0 + j, v_row, v_piece));
+      if (j < 2) park(tile0 + j);
+    }
     // in front of the first tile: values of zero
     for (int i = tid; i < HALF / 16; i += kManyThreads) *reinterpret_cast<u32x4*>(k_tile(tile0 + 3) + TILE + HALF + i * 16) = u32x4{0, 0, 0, 0};
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * LOADS) : "memory");
@@ -338,14 +345,16 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
       auto pass_on = [&](int f) __attribute__((always_inline)) {
         if (f == F - (RING - 1)) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * LOADS + 1) : "memory");
       };
-      int64_t off[LOADS];
+      int64_t k_off = 0, v_off = 0;
       int next_entry = 0;
       auto send_for = [&](int f) __attribute__((always_inline)) {
         if (f == 0) next_entry = entries[(tile + 1) & 7][lane];
-        if (f < LOADS) park_row(tile + 2, f);
-        if (f >= 1 && f <= LOADS) off[f - 1] = place(tile + 3, f - 1);
-        if (f >= 3 && f < 3 + LOADS) fetch_row(tile + 3, f - 3, off[f - 3]);
-        if (f == 3 + LOADS) fetch_entries(tile + 5);
+        if (f == 0) park(tile + 2);
+        if (f == 1) k_off = place(tile + 3, k_row, k_piece);
+        if (f == 2) v_off = FP8 ? k_off : place(tile + 3, v_row, v_piece);
+        if (f == 3) fetch_keys(tile + 3, k_off);
+        if (f == 4) fetch_values(tile + 3, v_off);
+        if (f == 5) fetch_entries(tile + 5);
       };
       if (active) {
         step(za, pa, zb, t0 + HALF, pb, before + TILE + HALF, t1, t0 + TILE, tile * kManyKeys, (unsigned)valid, pass_on);
