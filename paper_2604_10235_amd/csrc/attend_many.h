@@ -59,7 +59,8 @@ struct TileAt {
   static __device__ __forceinline__ int value(int row, int piece) { return (row >> 4) * GROUP + (piece >> 2) * 1024 + (row & 15) * 64 + (piece & 3) * 16; }
 };
 
-template <int D, bool FP8>
+// ROWWISE: pages of less than 16 rows; else the 16 rows that a wave loads of a tile lie in one page, whose place is worked out in scalar registers.
+template <int D, bool FP8, bool ROWWISE>
 __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const ManyArgs ma) {
   const AttendArgs& a = ma.a;
   constexpr int PIECES = D * (FP8 ? 1 : 2) / 16;               // 16-byte pieces of a stored row
@@ -175,32 +176,36 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
     // of the wave's 16 rows, the lane % 16th of K and the lane / 4th of V.
     const int k_row = FP8 ? (tid / PIECES) & (kManyKeys - 1) : (wave >> 1) * 16 + (lane & 15), v_row = FP8 ? k_row : (wave >> 1) * 16 + (lane >> 2);
     const int k_piece = FP8 ? tid % PIECES : (wave & 1) * LOADS * 4 + (lane >> 4), v_piece = FP8 ? k_piece : (wave & 1) * LOADS * 4 + (lane & 3);
-    // where one of them is; rows that are not there: in page 0, taken out of the tile when it is used
-    auto place = [&](int tile, int row, int piece) __attribute__((always_inline)) {
-      const int page = entries[tile & 7][row];
-      return (page >= 0 && page < a.pool.n_pages ? page : 0) * a.pool.s_page + (((tile * kManyKeys + row) & in_page) * (int)a.pool.s_tok + piece * 16);
+    // Where they are; rows that are not there: in page 0, taken out of the tile when it is used.  At `base` + `lane_off`.
+    struct Place { int64_t base; uint32_t lane_off; };
+    const int wave_row = FP8 ? (wave * (64 / PIECES)) & (kManyKeys - 1) : (wave >> 1) * 16;
+    const uint32_t k_lane_off = (k_row - wave_row) * (uint32_t)a.pool.s_tok + k_piece * 16, v_lane_off = (v_row - wave_row) * (uint32_t)a.pool.s_tok + v_piece * 16;
+    auto place = [&](int tile, int row, int piece, uint32_t lane_off) __attribute__((always_inline)) {
+      const int page = ROWWISE ? entries[tile & 7][row] : uniform(entries[tile & 7][wave_row]);
+      const int64_t at = (page >= 0 && page < a.pool.n_pages ? page : 0) * a.pool.s_page;
+      if constexpr (ROWWISE) return Place{at + ((tile * kManyKeys + row) & in_page) * (int)a.pool.s_tok, (uint32_t)piece * 16};
+      return Place{at + ((tile * kManyKeys + wave_row) & in_page) * (int)a.pool.s_tok, lane_off};
     };
+    auto k_place = [&](int tile) __attribute__((always_inline)) { return place(tile, k_row, k_piece, k_lane_off); };
+    auto v_place = [&](int tile) __attribute__((always_inline)) { return place(tile, v_row, v_piece, v_lane_off); };
     u32x4 kr, vr;                                                // 8 bits: the tile after the next two, on its way
-    auto fetch_keys = [&](int tile, int64_t off) __attribute__((always_inline)) {
+    auto fetch = [&](u32x4& into, uint32_t lds, const unsigned char* from, Place at) __attribute__((always_inline)) {
       if constexpr (FP8) {
-        kr = *reinterpret_cast<const u32x4*>(kb + off);
+        into = *reinterpret_cast<const u32x4*>(from + at.base + at.lane_off);
       } else {
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i)
-          asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_address(k_tile(tile)) + (wave * LOADS + i) * 1024),
-                       "v"(kb + off + i * 64) : "memory", "m0");
+        for (int i = 0; i < LOADS; ++i) {
+          if constexpr (ROWWISE)
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds + (wave * LOADS + i) * 1024),
+                         "v"(from + at.base + at.lane_off + i * 64) : "memory", "m0");
+          else
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds + (wave * LOADS + i) * 1024),
+                         "v"(at.lane_off), "s"(from + at.base + i * 64) : "memory", "m0");
+        }
       }
     };
-    auto fetch_values = [&](int tile, int64_t off) __attribute__((always_inline)) {
-      if constexpr (FP8) {
-        vr = *reinterpret_cast<const u32x4*>(vb + off);
-      } else {
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i)
-          asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_address(k_tile(tile)) + TILE + (wave * LOADS + i) * 1024),
-                       "v"(vb + off + i * 64) : "memory", "m0");
-      }
-    };
+    auto fetch_keys = [&](int tile, Place at) __attribute__((always_inline)) { fetch(kr, lds_address(k_tile(tile)), kb, at); };
+    auto fetch_values = [&](int tile, Place at) __attribute__((always_inline)) { fetch(vr, lds_address(k_tile(tile)) + TILE, vb, at); };
     auto park = [&](int tile) __attribute__((always_inline)) {                   // 8 bits
       if constexpr (FP8) {
         if (kManyThreads / PIECES > kManyKeys && tid / PIECES >= kManyKeys) return;
@@ -248,7 +253,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
     };
     constexpr int F = 2 * KS, RING = 4, PER = 16 / F, HALF = 2 * At::GROUP;      // fragments of a step, those held, logits per fragment; bytes of 32 rows
     u32x4 ring[RING];
-    auto fetch = [&](int f, const unsigned char* kt, const unsigned char* vt) __attribute__((always_inline)) {
+    auto fill = [&](int f, const unsigned char* kt, const unsigned char* vt) __attribute__((always_inline)) {
       ring[f % RING] = f & 1 ? value_frag(vt, f / 2) : key_frag(kt, f / 2);
     };
     // One step: the weights p of the 32 keys from key0 on, whose logits are z (`valid`: which of them there are); beside them, on the matrix cores,
@@ -271,8 +276,8 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
 #pragma unroll
       for (int f = 0; f < F; ++f) {
         beside(f);
-        if (f + RING - 1 < F) fetch(f + RING - 1, kt, vt);
-        else fetch(f + RING - 1 - F, kt_next, vt_next);
+        if (f + RING - 1 < F) fill(f + RING - 1, kt, vt);
+        else fill(f + RING - 1 - F, kt_next, vt_next);
         const int i = f / 2;
         if (f & 1) o[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(ring[f % RING]), frag(pp[i / DB]), o[i % DB], 0, 0, 0);
         else zn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(ring[f % RING]), frag(qf[i]), zn, 0, 0, 0);
@@ -322,8 +327,8 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
     for (int j = 0; j < 3; ++j) {
-      fetch_keys(tile0 + j, place(tile0 + j, k_row, k_piece));
-      fetch_values(tile0 + j, place(tile0 + j, v_row, v_piece));
+      fetch_keys(tile0 + j, k_place(tile0 + j));
+      fetch_values(tile0 + j, v_place(tile0 + j));
       if (j < 2) park(tile0 + j);
     }
     // in front of the first tile: values of zero
@@ -336,7 +341,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
 #pragma unroll
       for (int f = 0; f < KS; ++f) za = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(key_frag(k_tile(tile0), f)), frag(qf[f]), za, 0, 0, 0);
 #pragma unroll
-      for (int f = 0; f < RING - 1; ++f) fetch(f, k_tile(tile0) + HALF, k_tile(tile0 + 3) + TILE + HALF);
+      for (int f = 0; f < RING - 1; ++f) fill(f, k_tile(tile0) + HALF, k_tile(tile0 + 3) + TILE + HALF);
     }
     for (int tile = tile0; tile < tile1; ++tile) {
       if (__builtin_expect(valid != ~0ull || partly(tile), 0)) clean_values(tile, valid);
@@ -345,15 +350,15 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
       auto pass_on = [&](int f) __attribute__((always_inline)) {
         if (f == F - (RING - 1)) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * LOADS + 1) : "memory");
       };
-      int64_t k_off = 0, v_off = 0;
+      Place k_from = {0, 0}, v_from = {0, 0};
       int next_entry = 0;
       auto send_for = [&](int f) __attribute__((always_inline)) {
         if (f == 0) next_entry = entries[(tile + 1) & 7][lane];
         if (f == 0) park(tile + 2);
-        if (f == 1) k_off = place(tile + 3, k_row, k_piece);
-        if (f == 2) v_off = FP8 ? k_off : place(tile + 3, v_row, v_piece);
-        if (f == 3) fetch_keys(tile + 3, k_off);
-        if (f == 4) fetch_values(tile + 3, v_off);
+        if (f == 1) k_from = k_place(tile + 3);
+        if (f == 2) v_from = v_place(tile + 3);
+        if (f == 3) fetch_keys(tile + 3, k_from);
+        if (f == 4) fetch_values(tile + 3, v_from);
         if (f == 5) fetch_entries(tile + 5);
       };
       if (active) {
@@ -422,7 +427,8 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
 
 template <int D, bool FP8>
 int launch_many_of(const ManyArgs& m, hipStream_t stream) {
-  attend_many_kernel<D, FP8><<<dim3(m.workgroups), dim3(kManyThreads), 0, stream>>>(m);
+  if (m.a.pool.page_log2 < 4) attend_many_kernel<D, FP8, true><<<dim3(m.workgroups), dim3(kManyThreads), 0, stream>>>(m);
+  else attend_many_kernel<D, FP8, false><<<dim3(m.workgroups), dim3(kManyThreads), 0, stream>>>(m);
   return (int)hipGetLastError();
 }
 
