@@ -12,6 +12,8 @@ extern template int launch_many_of<128, true>(const ManyArgs&, hipStream_t);
 
 constexpr int kFewRowsMost = 64;          // rows of a request up to which it takes attend_few_kernel
 
+constexpr int kAlongTiles = 2048;
+
 static size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 int make_attend_plan(const codecomp_batch* b, const codecomp_pages* p, AttendPlan* pl) {
@@ -29,6 +31,13 @@ int make_attend_plan(const codecomp_batch* b, const codecomp_pages* p, AttendPla
     ++pl->few_rows;
     if (rows > few_most) few_most = (int)rows;
   }
+  // In a batch with longer chunks, a few short requests go along with them: up to kAlongTiles tiles of the many-row kernel, what the launches of
+  // the other two kernels cost.
+  if (pl->many_rows > 0 && (int64_t)pl->few_rows * x.Hkv * ((x.max_kv + kManyKeys - 1) / kManyKeys) <= kAlongTiles) {
+    pl->many_rows += pl->few_rows;
+    pl->few_rows = few_most = 0;
+  }
+  pl->many_from = pl->few_rows > 0 ? kFewRowsMost + 1 : 1;
   pl->row_blocks = few_most <= 16 ? 1 : few_most <= 32 ? 2 : 4;
   pl->row_slots = few_most;
   const int64_t items = (int64_t)x.n_seqs * x.Hkv;
@@ -61,20 +70,23 @@ __global__ __launch_bounds__(256) void join_many_kernel(const ManyArgs ma) {
   const int tid = threadIdx.x, in_block = blockIdx.y * 16 + (tid >> 4), e = (tid & 15) * E;
   const int q0 = a.b.cu_q[cut.r], rows = (a.b.cu_q[cut.r + 1] - q0) * a.b.G, row = cut.block * kManyRows + in_block;
   if (row >= rows) return;
+  // part of workgroup g: its rows of slot 2 g, but for the first
+  auto part_of = [&](int g) { return (int64_t)(g == (int)blockIdx.x ? cut.first_slot : 2 * g) * kManyRows + in_block; };
   float top = -1.0e30f, all = 0.0f, x[E];
+#pragma unroll 8
+  for (int g = blockIdx.x; g <= cut.last; ++g) top = fmaxf(top, a.part_ml[2 * part_of(g)]);
 #pragma unroll
   for (int i = 0; i < E; ++i) x[i] = 0.0f;
+#pragma unroll 4
   for (int g = blockIdx.x; g <= cut.last; ++g) {
-    const int64_t part = (int64_t)(g == (int)blockIdx.x ? cut.first_slot : 2 * g) * kManyRows + in_block;
-    const float m = a.part_ml[2 * part], l = a.part_ml[2 * part + 1];
-    const float to = fmaxf(top, m), old = top == to ? 1.0f : __builtin_amdgcn_exp2f(top - to), f = m == to ? 1.0f : __builtin_amdgcn_exp2f(m - to);
-    top = to;
-    all = all * old + l * f;
+    const int64_t part = part_of(g);
+    const float m = a.part_ml[2 * part], f = m == top ? 1.0f : __builtin_amdgcn_exp2f(m - top);
+    all += a.part_ml[2 * part + 1] * f;
 #pragma unroll
     for (int i = 0; i < E; i += 4) {
       const f32x4 v = *reinterpret_cast<const f32x4*>(a.part_o + part * D + e + i);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[i + j] = x[i + j] * old + v[j] * f;
+      for (int j = 0; j < 4; ++j) x[i + j] += v[j] * f;
     }
   }
   const int t = row / a.b.G, h = cut.head * a.b.G + row - t * a.b.G;
@@ -89,7 +101,7 @@ static int launch_many(const AttendPlan& pl, const AttendArgs& a, char* workspac
   ManyArgs m;
   m.a = a;
   m.workgroups = pl.workgroups;
-  m.few_rows_most = kFewRowsMost;
+  m.rows_from = pl.many_from;
   m.a.part_o = reinterpret_cast<float*>(workspace);
   m.a.part_ml = m.a.part_o + (size_t)pl.workgroups * 2 * kManyRows * pl.d;
   m.cuts = reinterpret_cast<CutBlock*>(m.a.part_ml + (size_t)pl.workgroups * 2 * kManyRows * 2);

@@ -21,7 +21,7 @@ struct CutBlock {
 struct ManyArgs {
   AttendArgs a;
   CutBlock* cuts;              // [workgroups]
-  int workgroups, few_rows_most;
+  int workgroups, rows_from;   // requests of fewer rows are not this kernel's
 };
 
 // Tiles of 64 keys that a block of rows of a request meets; at least one.
@@ -39,7 +39,7 @@ __device__ __forceinline__ Blocks blocks_of(const ManyArgs& m, int r) {
   x.nq = m.a.b.cu_q[r + 1] - m.a.b.cu_q[r];
   x.G = m.a.b.G;
   x.rows = x.nq * x.G;
-  x.count = x.rows > m.few_rows_most ? (x.rows + kManyRows - 1) / kManyRows : 0;
+  x.count = x.rows >= m.rows_from ? (x.rows + kManyRows - 1) / kManyRows : 0;
   x.causal = m.a.b.causal;
   return x;
 }
@@ -78,12 +78,46 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
   __shared__ int found[4];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), l32 = lane & 31, half = lane >> 5;
 
-  // ---- this workgroup's share: the tiles of all blocks of all heads form one sequence, cut into equal parts
+  // ---- this workgroup's share: the tiles of all blocks of all heads form one sequence, cut into equal parts.  Requests are shared out over the
+  // threads to count their blocks, then blocks to count their tiles (one each, mostly: a prompt alone has many).
   const int n = a.b.n_seqs, per = (n + kManyThreads - 1) / kManyThreads;
-  int64_t mine = 0;
-  for (int r = min(tid * per, n); r < min(tid * per + per, n); ++r) {
-    const Blocks x = blocks_of(ma, r);
-    for (int i = 0; i < x.count; ++i) mine += x.tiles(i);
+  int my_blocks = 0;
+  for (int r = min(tid * per, n); r < min(tid * per + per, n); ++r) my_blocks += blocks_of(ma, r).count;
+  int blocks = my_blocks;                                        // up to here, inclusive
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const int y = __shfl_up(blocks, off);
+    if (lane >= off) blocks += y;
+  }
+  if (lane == 63) wave_sum[wave] = blocks;
+  __syncthreads();
+  int all_blocks = 0;
+#pragma unroll
+  for (int w = 0; w < kManyWaves; ++w) {
+    if (w < wave) blocks += (int)wave_sum[w];
+    all_blocks += (int)wave_sum[w];
+  }
+  int* first_block = reinterpret_cast<int*>(tiles_lds);           // of a thread's requests
+  first_block[tid] = blocks - my_blocks;
+  __syncthreads();
+  const int block_per = (uniform(all_blocks) + kManyThreads - 1) / kManyThreads;
+  const int b0 = min(tid * block_per, all_blocks), b1 = min(b0 + block_per, all_blocks);
+  int my_r = 0, my_i = 0;                                         // request of block b0, and its number there
+  int64_t mine = 0;                                               // tiles of this thread's blocks
+  if (b0 < b1) {
+    int lo = 0;                                                  // last thread whose requests begin at b0 or before, and have blocks from there on
+#pragma unroll
+    for (int step = kManyThreads / 2; step > 0; step >>= 1)
+      if (first_block[lo + step] <= b0) lo += step;
+    my_r = lo * per;
+    my_i = b0 - first_block[lo];
+    Blocks x = blocks_of(ma, my_r);
+    while (my_i >= x.count) { my_i -= x.count; x = blocks_of(ma, ++my_r); }
+    int r = my_r, i = my_i;
+    for (int b = b0; b < b1; ++b, ++i) {
+      while (i >= x.count) { i = 0; x = blocks_of(ma, ++r); }
+      mine += x.tiles(i);
+    }
   }
   int64_t incl = mine;
 #pragma unroll
@@ -91,6 +125,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
     const int64_t y = __shfl_up(incl, off);
     if (lane >= off) incl += y;
   }
+  __syncthreads();
   if (lane == 63) wave_sum[wave] = incl;
   __syncthreads();
   int64_t before = 0, per_head = 0;
@@ -115,18 +150,15 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
     const int64_t at = x_end - 1 - head * per_head;
     int64_t start = before + incl - mine;
     if (at >= start && at < start + mine) {                      // one thread has it
-      for (int r = tid * per;; ++r) {
-        const Blocks y = blocks_of(ma, r);
-        int64_t t = 0;
-        int i = 0;
-        for (; i < y.count; ++i) {
-          const int tiles = y.tiles(i);
-          if (at < start + t + tiles) break;
-          t += tiles;
-        }
-        start += t;
-        if (i < y.count) { found[0] = r; found[1] = i; found[2] = (int)(at - start); break; }
+      Blocks y = blocks_of(ma, my_r);
+      int r = my_r, i = my_i;
+      for (;; ++i) {
+        while (i >= y.count) { i = 0; y = blocks_of(ma, ++r); }
+        const int tiles = y.tiles(i);
+        if (at < start + tiles) break;
+        start += tiles;
       }
+      found[0] = r; found[1] = i; found[2] = (int)(at - start);
     }
   }
   __syncthreads();
