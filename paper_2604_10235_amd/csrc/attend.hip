@@ -38,6 +38,12 @@ int make_attend_plan(const codecomp_batch* b, const codecomp_pages* p, AttendPla
     pl->few_rows = few_most = 0;
   }
   pl->many_from = pl->few_rows > 0 ? kFewRowsMost + 1 : 1;
+  int64_t blocks = 0;
+  for (int r = 0; r < x.n_seqs; ++r) {
+    const int64_t rows = (int64_t)(b->cu_q_host[r + 1] - b->cu_q_host[r]) * x.G;
+    if (rows >= pl->many_from) blocks += (rows + kManyRows - 1) / kManyRows;
+  }
+  pl->many_blocks = blocks * x.Hkv < INT32_MAX ? (int)(blocks * x.Hkv) : INT32_MAX;
   pl->row_blocks = few_most <= 16 ? 1 : few_most <= 32 ? 2 : 4;
   pl->row_slots = few_most;
   const int64_t items = (int64_t)x.n_seqs * x.Hkv;
@@ -60,41 +66,36 @@ int make_attend_plan(const codecomp_batch* b, const codecomp_pages* p, AttendPla
   return CODECOMP_OK;
 }
 
-// Blocks of rows whose keys several workgroups shared: blockIdx.x the workgroup that has a block's first part, blockIdx.y 16 of its rows.
+// Blocks of rows whose keys several workgroups shared: blockIdx.x the workgroup that has a block's first part, blockIdx.y some of its rows, one
+// after the other by D / 4 threads each.
 template <int D>
-__global__ __launch_bounds__(256) void join_many_kernel(const ManyArgs ma) {
+__global__ __launch_bounds__(256) void join_many_kernel(const ManyArgs ma, int rows_each) {
   const AttendArgs& a = ma.a;
   const CutBlock cut = ma.cuts[blockIdx.x];
   if (cut.r < 0) return;
-  constexpr int E = D / 16;
-  const int tid = threadIdx.x, in_block = blockIdx.y * 16 + (tid >> 4), e = (tid & 15) * E;
-  const int q0 = a.b.cu_q[cut.r], rows = (a.b.cu_q[cut.r + 1] - q0) * a.b.G, row = cut.block * kManyRows + in_block;
-  if (row >= rows) return;
-  // part of workgroup g: its rows of slot 2 g, but for the first
-  auto part_of = [&](int g) { return (int64_t)(g == (int)blockIdx.x ? cut.first_slot : 2 * g) * kManyRows + in_block; };
-  float top = -1.0e30f, all = 0.0f, x[E];
+  constexpr int THREADS = D / 4;
+  const int first = blockIdx.x, e = (threadIdx.x % THREADS) * 4;
+  const int q0 = a.b.cu_q[cut.r], rows = (a.b.cu_q[cut.r + 1] - q0) * a.b.G;
+  for (int i = threadIdx.x / THREADS; i < rows_each; i += 256 / THREADS) {
+    const int in_block = blockIdx.y * rows_each + i, row = cut.block * kManyRows + in_block;
+    if (row >= rows) return;
+    auto part_of = [&](int g) { return (int64_t)(g == first ? 2 * g + 1 : 2 * g) * kManyRows + in_block; };
+    float top = -1.0e30f, all = 0.0f;
 #pragma unroll 8
-  for (int g = blockIdx.x; g <= cut.last; ++g) top = fmaxf(top, a.part_ml[2 * part_of(g)]);
-#pragma unroll
-  for (int i = 0; i < E; ++i) x[i] = 0.0f;
-#pragma unroll 4
-  for (int g = blockIdx.x; g <= cut.last; ++g) {
-    const int64_t part = part_of(g);
-    const float m = a.part_ml[2 * part], f = m == top ? 1.0f : __builtin_amdgcn_exp2f(m - top);
-    all += a.part_ml[2 * part + 1] * f;
-#pragma unroll
-    for (int i = 0; i < E; i += 4) {
-      const f32x4 v = *reinterpret_cast<const f32x4*>(a.part_o + part * D + e + i);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) x[i + j] += v[j] * f;
+    for (int g = first; g <= cut.last; ++g) top = fmaxf(top, a.part_ml[2 * part_of(g)]);
+    f32x4 x = {0, 0, 0, 0};
+#pragma unroll 8
+    for (int g = first; g <= cut.last; ++g) {
+      const int64_t part = part_of(g);
+      const float m = a.part_ml[2 * part], f = m == top ? 1.0f : __builtin_amdgcn_exp2f(m - top);
+      all += a.part_ml[2 * part + 1] * f;
+      x += *reinterpret_cast<const f32x4*>(a.part_o + part * D + e) * f;
     }
+    const int t = row / a.b.G, h = cut.head * a.b.G + row - t * a.b.G;
+    const float inv = all == 0.0f ? 0.0f : a.pool.v_scale / all;
+    *reinterpret_cast<u32x2*>(a.out + (q0 + t) * a.b.o_st + h * a.b.o_sh + e) = u32x2{pack2(x.x * inv, x.y * inv), pack2(x.z * inv, x.w * inv)};
+    if (a.lse && e == 0) a.lse[(int64_t)(q0 + t) * a.b.Hq + h] = all == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(all)) * kLn2;
   }
-  const int t = row / a.b.G, h = cut.head * a.b.G + row - t * a.b.G;
-  const float inv = all == 0.0f ? 0.0f : a.pool.v_scale / all;
-  uint16_t* out = a.out + (q0 + t) * a.b.o_st + h * a.b.o_sh + e;
-#pragma unroll
-  for (int i = 0; i < E; i += 2) *reinterpret_cast<unsigned*>(out + i) = pack2(x[i] * inv, x[i + 1] * inv);
-  if (a.lse && (tid & 15) == 0) a.lse[(int64_t)(q0 + t) * a.b.Hq + h] = all == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(all)) * kLn2;
 }
 
 static int launch_many(const AttendPlan& pl, const AttendArgs& a, char* workspace, hipStream_t stream) {
@@ -109,9 +110,11 @@ static int launch_many(const AttendPlan& pl, const AttendArgs& a, char* workspac
   if (pl.d == 128) rc = pl.pool.fp8 ? launch_many_of<128, true>(m, stream) : launch_many_of<128, false>(m, stream);
   else rc = pl.pool.fp8 ? launch_many_of<64, true>(m, stream) : launch_many_of<64, false>(m, stream);
   if (rc) return rc;
-  const dim3 grid(pl.workgroups, kManyRows / 16), block(256);
-  if (pl.d == 128) join_many_kernel<128><<<grid, block, 0, stream>>>(m);
-  else join_many_kernel<64><<<grid, block, 0, stream>>>(m);
+  // a few blocks of many parts: their rows over more workgroups
+  const int rows_each = pl.many_blocks <= 32 ? 256 / (pl.d / 4) : 32;
+  const dim3 grid(pl.workgroups, kManyRows / rows_each), block(256);
+  if (pl.d == 128) join_many_kernel<128><<<grid, block, 0, stream>>>(m, rows_each);
+  else join_many_kernel<64><<<grid, block, 0, stream>>>(m, rows_each);
   return (int)hipGetLastError();
 }
 

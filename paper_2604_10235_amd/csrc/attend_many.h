@@ -14,9 +14,14 @@ constexpr int kManyRows = 256, kManyKeys = 64, kManyWaves = 8, kManyThreads = 64
 
 // What a workgroup leaves for the kernel that joins blocks of rows whose keys several workgroups share.
 struct CutBlock {
-  int32_t r, block, head;      // r < 0: none
-  int32_t first_slot, last;    // slot of this workgroup's part; last workgroup with a part (slot 2 * workgroup)
+  int32_t r, block, head;      // of the block whose first part is this workgroup's (slot 2 * workgroup + 1); r < 0: none
+  int32_t last;                // last workgroup with a part of it (those after the first in slot 2 * workgroup)
 };
+
+// Positions in front of the tiles of a block, in the sequence that is cut into equal parts: starting on a block (its queries, the first tiles) costs
+// about as much as that many tiles.
+constexpr int kManyLead = 4;
+constexpr int kManyLeast = 8;   // positions that a workgroup gets at least
 
 struct ManyArgs {
   AttendArgs a;
@@ -103,7 +108,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
   const int block_per = (uniform(all_blocks) + kManyThreads - 1) / kManyThreads;
   const int b0 = min(tid * block_per, all_blocks), b1 = min(b0 + block_per, all_blocks);
   int my_r = 0, my_i = 0;                                         // request of block b0, and its number there
-  int64_t mine = 0;                                               // tiles of this thread's blocks
+  int64_t mine = 0;                                               // positions of this thread's blocks
   if (b0 < b1) {
     int lo = 0;                                                  // last thread whose requests begin at b0 or before, and have blocks from there on
 #pragma unroll
@@ -116,7 +121,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
     int r = my_r, i = my_i;
     for (int b = b0; b < b1; ++b, ++i) {
       while (i >= x.count) { i = 0; x = blocks_of(ma, ++r); }
-      mine += x.tiles(i);
+      mine += kManyLead + x.tiles(i);
     }
   }
   int64_t incl = mine;
@@ -136,45 +141,45 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
   }
   per_head = uniform(per_head);
   const int64_t total = per_head * a.b.Hkv;
-  const int64_t workgroups = min((int64_t)ma.workgroups, total);
+  const int64_t workgroups = min((int64_t)ma.workgroups, (total + kManyLeast - 1) / kManyLeast);
   if (tid == 0 && blockIdx.x >= workgroups) ma.cuts[blockIdx.x].r = -1;
   // neighbours in the sequence read the same keys: they run on the same die (workgroups go to the eight dies in turn)
   const int per_die = ((int)workgroups + 7) / 8, g = (int)(blockIdx.x & 7) * per_die + (int)(blockIdx.x >> 3);
   if ((int)(blockIdx.x >> 3) >= per_die || g >= workgroups) return;
-  const int64_t x_end = (g + 1) * total / workgroups;
-  int left = (int)(x_end - g * total / workgroups);               // tiles still to be done
+  const int64_t x0 = uniform(g * total / workgroups), x1 = uniform((g + 1) * total / workgroups);
   // From the end of the part back to its start: blocks are entered at their first keys, at about the same time by all workgroups, so
   // that the keys and values of a head are read by many at a time.
-  int head = (int)((x_end - 1) / per_head);
+  int head = uniform((int)((x1 - 1) / per_head));
   {
-    const int64_t at = x_end - 1 - head * per_head;
+    const int64_t at = x1 - 1 - head * per_head;
     int64_t start = before + incl - mine;
     if (at >= start && at < start + mine) {                      // one thread has it
       Blocks y = blocks_of(ma, my_r);
       int r = my_r, i = my_i;
       for (;; ++i) {
         while (i >= y.count) { i = 0; y = blocks_of(ma, ++r); }
-        const int tiles = y.tiles(i);
-        if (at < start + tiles) break;
-        start += tiles;
+        const int positions = kManyLead + y.tiles(i);
+        if (at < start + positions) break;
+        start += positions;
       }
       found[0] = r; found[1] = i; found[2] = (int)(at - start);
     }
   }
   __syncthreads();
-  int r = uniform(found[0]), block = uniform(found[1]), tile1 = uniform(found[2]) + 1;
+  int r = uniform(found[0]), block = uniform(found[1]);
+  int64_t start = uniform(x1 - 1 - found[2]);                     // position of the block
   Blocks of = uniform(blocks_of(ma, r));
-  CutBlock cut = {-1, 0, 0, 0, 0};
+  CutBlock cut = {-1, 0, 0, 0};
 
-  while (left > 0) {
-    const int tiles = of.tiles(block);
-    if (tile1 < 0) tile1 = tiles;
-    const int tile0 = max(0, tile1 - left);
-    left -= tile1 - tile0;
+  for (;;) {
+    const int tiles = uniform(of.tiles(block));
+    const int64_t first = start + kManyLead;                      // position of its first tile
+    const int tile0 = uniform((int)max(x0 - first, (int64_t)0)), tile1 = uniform((int)min(x1 - first, (int64_t)tiles));
+    if (tile1 > tile0) {
     const bool whole = tile0 == 0 && tile1 == tiles;
-    const int slot = left == 0 ? 2 * g : 2 * g + 1;
+    const int slot = tile0 > 0 ? 2 * g : 2 * g + 1;
     if (tile0 == 0 && tile1 < tiles)                             // the rest of the block is the next workgroups'
-      cut = {r, block, head, slot, (int)(((x_end + tiles - tile1) * workgroups - 1) / total)};
+      cut = {r, block, head, (int)(((first + tiles) * workgroups - 1) / total)};
     const int q0 = uniform(a.b.cu_q[r]), row0 = block * kManyRows + wave * 32, row = row0 + l32;
     const bool active = row0 < of.rows;
 
@@ -445,14 +450,16 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
         if (half == 0) { a.part_ml[2 * part] = m; a.part_ml[2 * part + 1] = sum; }
       }
     }
-    tile1 = -1;
-    if (left > 0 && --block < 0) {                               // the request before, or the head before
+    }
+    if (start <= x0) break;
+    if (--block < 0) {                                           // the request before, or the head before
       do {
         if (--r < 0) { r = n - 1; --head; }
         of = uniform(blocks_of(ma, r));
       } while (of.count == 0);
       block = of.count - 1;
     }
+    start -= kManyLead + uniform(of.tiles(block));
   }
   if (tid == 0) ma.cuts[g] = cut;
 }
