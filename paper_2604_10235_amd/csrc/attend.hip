@@ -66,18 +66,18 @@ int make_attend_plan(const codecomp_batch* b, const codecomp_pages* p, AttendPla
   return CODECOMP_OK;
 }
 
-// Blocks of rows whose keys several workgroups shared: blockIdx.x the workgroup that has a block's first part, blockIdx.y some of its rows, one
-// after the other by D / 4 threads each.
+// Blocks of rows whose keys several workgroups shared: blockIdx.y the workgroup that has a block's first part, blockIdx.x some of its rows, one
+// after the other by D / 4 threads each.  (In that order: the first parts may be a multiple of eight workgroups apart, which would put all the work on one die.)
 template <int D>
 __global__ __launch_bounds__(256) void join_many_kernel(const ManyArgs ma, int rows_each) {
   const AttendArgs& a = ma.a;
-  const CutBlock cut = ma.cuts[blockIdx.x];
+  const CutBlock cut = ma.cuts[blockIdx.y];
   if (cut.r < 0) return;
   constexpr int THREADS = D / 4;
-  const int first = blockIdx.x, e = (threadIdx.x % THREADS) * 4;
+  const int first = blockIdx.y, e = (threadIdx.x % THREADS) * 4;
   const int q0 = a.b.cu_q[cut.r], rows = (a.b.cu_q[cut.r + 1] - q0) * a.b.G;
   for (int i = threadIdx.x / THREADS; i < rows_each; i += 256 / THREADS) {
-    const int in_block = blockIdx.y * rows_each + i, row = cut.block * kManyRows + in_block;
+    const int in_block = blockIdx.x * rows_each + i, row = cut.block * kManyRows + in_block;
     if (row >= rows) return;
     auto part_of = [&](int g) { return (int64_t)(g == first ? 2 * g + 1 : 2 * g) * kManyRows + in_block; };
     float top = -1.0e30f, all = 0.0f;
@@ -111,8 +111,8 @@ static int launch_many(const AttendPlan& pl, const AttendArgs& a, char* workspac
   else rc = pl.pool.fp8 ? launch_many_of<64, true>(m, stream) : launch_many_of<64, false>(m, stream);
   if (rc) return rc;
   // a few blocks of many parts: their rows over more workgroups
-  const int rows_each = pl.many_blocks <= 32 ? 256 / (pl.d / 4) : 32;
-  const dim3 grid(pl.workgroups, kManyRows / rows_each), block(256);
+  const int rows_each = pl.many_blocks <= 32 ? 256 / (pl.d / 4) : 16;
+  const dim3 grid(kManyRows / rows_each, pl.workgroups), block(256);
   if (pl.d == 128) join_many_kernel<128><<<grid, block, 0, stream>>>(m, rows_each);
   else join_many_kernel<64><<<grid, block, 0, stream>>>(m, rows_each);
   return (int)hipGetLastError();
