@@ -20,8 +20,8 @@ struct CutBlock {
 
 // Positions in front of the tiles of a block, in the sequence that is cut into equal parts: starting on a block (its queries, the first tiles) costs
 // about as much as that many tiles.
-constexpr int kManyLead = 4;
-constexpr int kManyLeast = 8;   // positions that a workgroup gets at least
+constexpr int kManyLead = 7;
+constexpr int kManyLeast = 4;   // positions that a workgroup gets at least
 
 struct ManyArgs {
   AttendArgs a;
