@@ -27,7 +27,7 @@ struct AttendArgs {
   float* part_ml;              // [part][rows of a part][2]: reference, sum of weights
   int64_t layer;               // byte offset of the layer in the pool
   float c;                     // softmax_scale * k_scale * log2(e): logits in powers of two
-  int chunk, splits, row_slots;        // few rows: keys of a chunk, most chunks, most rows
+  int chunk, splits, row_slots, row_parts;       // few rows: keys of a chunk, most chunks, most rows, workgroups that they are shared out to
 };
 
 // The same in all lanes, and known to be: in scalar registers.

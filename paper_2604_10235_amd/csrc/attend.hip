@@ -13,6 +13,7 @@ extern template int launch_many_of<128, true>(const ManyArgs&, hipStream_t);
 constexpr int kFewRowsMost = 64;          // rows of a request up to which it takes attend_few_kernel
 
 constexpr int kAlongTiles = 2048;
+constexpr int kWholeTiles = 8;            // tiles of the longest block up to which none is shared by workgroups
 
 static size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -44,7 +45,7 @@ int make_attend_plan(const codecomp_batch* b, const codecomp_pages* p, AttendPla
     if (rows >= pl->many_from) blocks += (rows + kManyRows - 1) / kManyRows;
   }
   pl->many_blocks = blocks * x.Hkv < INT32_MAX ? (int)(blocks * x.Hkv) : INT32_MAX;
-  pl->row_blocks = few_most <= 16 ? 1 : few_most <= 32 ? 2 : 4;
+  pl->row_parts = (few_most + 31) / 32;
   pl->row_slots = few_most;
   const int64_t items = (int64_t)x.n_seqs * x.Hkv;
   // chunks of keys: about two workgroups per compute unit if all requests are of the largest length, of at least 128 keys each
@@ -54,13 +55,14 @@ int make_attend_plan(const codecomp_batch* b, const codecomp_pages* p, AttendPla
   while ((x.max_kv + chunk - 1) / chunk > kFewMostSplits) chunk *= 2;
   pl->chunk = (int)chunk;
   pl->splits = x.max_kv > chunk ? (int)((x.max_kv + chunk - 1) / chunk) : 1;
-  if (items * pl->splits * 64 > INT32_MAX) return CODECOMP_EINVAL_SHAPE;
+  if (items * pl->splits * kFewRowsMost > INT32_MAX) return CODECOMP_EINVAL_SHAPE;
   size_t off = 0;
   pl->off_few = off;
   if (pl->few_rows > 0 && pl->splits > 1) off = align256(off + (size_t)(items * pl->splits * pl->row_slots) * (p->head_dim + 2) * sizeof(float));
   pl->off_many = off;
   pl->workgroups = 256;
-  if (pl->many_rows > 0)
+  pl->many_whole = x.max_kv <= kWholeTiles * kManyKeys;
+  if (pl->many_rows > 0 && !pl->many_whole)
     off = align256(off + (size_t)pl->workgroups * 2 * kManyRows * (p->head_dim + 2) * sizeof(float) + pl->workgroups * sizeof(CutBlock));
   pl->ws_bytes = off;
   return CODECOMP_OK;
@@ -103,13 +105,14 @@ static int launch_many(const AttendPlan& pl, const AttendArgs& a, char* workspac
   m.a = a;
   m.workgroups = pl.workgroups;
   m.rows_from = pl.many_from;
+  m.whole = pl.many_whole;
   m.a.part_o = reinterpret_cast<float*>(workspace);
   m.a.part_ml = m.a.part_o + (size_t)pl.workgroups * 2 * kManyRows * pl.d;
   m.cuts = reinterpret_cast<CutBlock*>(m.a.part_ml + (size_t)pl.workgroups * 2 * kManyRows * 2);
   int rc;
   if (pl.d == 128) rc = pl.pool.fp8 ? launch_many_of<128, true>(m, stream) : launch_many_of<128, false>(m, stream);
   else rc = pl.pool.fp8 ? launch_many_of<64, true>(m, stream) : launch_many_of<64, false>(m, stream);
-  if (rc) return rc;
+  if (rc || pl.many_whole) return rc;
   // a few blocks of many parts: their rows over more workgroups
   const int rows_each = pl.many_blocks <= 32 ? 256 / (pl.d / 4) : 16;
   const dim3 grid(kManyRows / rows_each, pl.workgroups), block(256);
@@ -123,7 +126,7 @@ int launch_attend(const AttendPlan& pl, const void* q, int layer, void* out, flo
   a.pool = pl.pool; a.b = pl.batch; a.q = static_cast<const uint16_t*>(q); a.out = static_cast<uint16_t*>(out); a.lse = lse;
   a.layer = layer * pl.pool.s_layer;
   a.c = pl.scale * pl.pool.k_scale * kLog2e;
-  a.chunk = pl.chunk; a.splits = pl.splits; a.row_slots = pl.row_slots;
+  a.chunk = pl.chunk; a.splits = pl.splits; a.row_slots = pl.row_slots; a.row_parts = pl.row_parts;
   if (pl.few_rows > 0) {
     a.part_o = reinterpret_cast<float*>(static_cast<char*>(workspace) + pl.off_few);
     a.part_ml = a.part_o + (size_t)pl.batch.n_seqs * pl.batch.Hkv * pl.splits * pl.row_slots * pl.d;

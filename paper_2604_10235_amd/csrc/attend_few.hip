@@ -34,7 +34,7 @@ struct FewTile {
 };
 
 template <int D, bool FP8, int RB>
-__global__ __launch_bounds__(64 * kFewWaves, RB == 4 ? 1 : RB == 2 ? 2 : 3) void attend_few_kernel(const AttendArgs a) {
+__global__ __launch_bounds__(64 * kFewWaves, RB == 2 ? 2 : 3) void attend_few_kernel(const AttendArgs a) {
   using T = FewTile<D, FP8>;
   constexpr int KS = D / 32, DB = D / 16;
   __shared__ __attribute__((aligned(16))) unsigned char lds[kFewWaves * T::BYTES];
@@ -42,10 +42,11 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 4 ? 1 : RB == 2 ? 2 : 3) void
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), l16 = lane & 15, quarter = lane >> 4;
   // Chunk by chunk, all requests and heads of one: neighbouring workgroups run on different dies, and must not be the same chunks of all
   // requests there (short requests lack the later ones).
-  const int items = a.b.n_seqs * a.b.Hkv, split = blockIdx.x / items, item = blockIdx.x - split * items;
+  const int items = a.b.n_seqs * a.b.Hkv, turn = blockIdx.x / items, item = blockIdx.x - turn * items;
+  const int split = turn / a.row_parts, row0 = (turn - split * a.row_parts) * (16 * RB);         // first of this workgroup's rows
   const int r = item / a.b.Hkv, head = item - r * a.b.Hkv;
   const int q0 = a.b.cu_q[r], nq = a.b.cu_q[r + 1] - q0, rows = nq * a.b.G;
-  if (rows == 0 || rows > 16 * RB) return;
+  if (rows <= row0 || rows > a.row_slots) return;
   const int len = kv_len_of(a.b, r);
   const int key0 = split * a.chunk, key1 = min(len, key0 + a.chunk);
   if (split > 0 && key0 >= len) return;
@@ -56,7 +57,7 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 4 ? 1 : RB == 2 ? 2 : 3) void
   int limit[RB];                                                // keys that the lane's row sees
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
-    const int row = rb * 16 + l16, t = min(row, rows - 1) / a.b.G, g = min(row, rows - 1) - t * a.b.G;
+    const int row = row0 + rb * 16 + l16, t = min(row, rows - 1) / a.b.G, g = min(row, rows - 1) - t * a.b.G;
     const uint16_t* p = a.q + (q0 + t) * a.b.q_st + (head * a.b.G + g) * a.b.q_sh;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
@@ -247,7 +248,7 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 4 ? 1 : RB == 2 ? 2 : 3) void
   static_assert(16 * O_ROW * 4 <= T::BYTES, "rows of a block fit the tiles");
 #pragma unroll
   for (int rb = 0; rb < RB; ++rb) {
-    if (rb * 16 >= rows) break;
+    if (row0 + rb * 16 >= rows) break;
     float sum = l[rb];
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
@@ -257,7 +258,7 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 4 ? 1 : RB == 2 ? 2 : 3) void
     for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4*>(o_lds + (wave * 16 + l16) * O_ROW + db * 16 + quarter * 4) = o[rb][db];
     __syncthreads();
     constexpr int E = D / 16;                                   // elements of a row per thread
-    const int n = tid >> 4, row = rb * 16 + n, e = (tid & 15) * E;
+    const int n = tid >> 4, row = row0 + rb * 16 + n, e = (tid & 15) * E;
     if (row < rows) {
       float to = -INFINITY;
 #pragma unroll
@@ -352,10 +353,9 @@ __global__ __launch_bounds__(256) void join_few_kernel(const AttendArgs a) {
 template <int D, bool FP8>
 static int launch_few_of(const AttendPlan& pl, const AttendArgs& a, hipStream_t stream) {
   const int64_t items = (int64_t)a.b.n_seqs * a.b.Hkv;
-  const dim3 grid((unsigned)(items * a.splits)), block(64 * kFewWaves);
-  if (pl.row_blocks == 1) attend_few_kernel<D, FP8, 1><<<grid, block, 0, stream>>>(a);
-  else if (pl.row_blocks == 2) attend_few_kernel<D, FP8, 2><<<grid, block, 0, stream>>>(a);
-  else attend_few_kernel<D, FP8, 4><<<grid, block, 0, stream>>>(a);
+  const dim3 grid((unsigned)(items * a.splits * a.row_parts)), block(64 * kFewWaves);
+  if (a.row_slots <= 16) attend_few_kernel<D, FP8, 1><<<grid, block, 0, stream>>>(a);
+  else attend_few_kernel<D, FP8, 2><<<grid, block, 0, stream>>>(a);
   if (hipError_t e = hipGetLastError()) return (int)e;
   if (a.splits > 1) join_few_kernel<D><<<dim3((unsigned)(items * a.row_slots)), dim3(256), 0, stream>>>(a);
   return (int)hipGetLastError();

@@ -27,6 +27,7 @@ struct ManyArgs {
   AttendArgs a;
   CutBlock* cuts;              // [workgroups]
   int workgroups, rows_from;   // requests of fewer rows are not this kernel's
+  int whole;                   // 1: no block is shared (all are short): nothing to be joined
 };
 
 // Tiles of 64 keys that a block of rows of a request meets; at least one.
@@ -86,6 +87,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
   // ---- this workgroup's share: the tiles of all blocks of all heads form one sequence, cut into equal parts.  Requests are shared out over the
   // threads to count their blocks, then blocks to count their tiles (one each, mostly: a prompt alone has many).
   const int n = a.b.n_seqs, per = (n + kManyThreads - 1) / kManyThreads;
+  auto weight = [&](int tiles) { return ma.whole ? 1 : kManyLead + tiles; };       // positions of a block
   int my_blocks = 0;
   for (int r = min(tid * per, n); r < min(tid * per + per, n); ++r) my_blocks += blocks_of(ma, r).count;
   int blocks = my_blocks;                                        // up to here, inclusive
@@ -121,7 +123,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
     int r = my_r, i = my_i;
     for (int b = b0; b < b1; ++b, ++i) {
       while (i >= x.count) { i = 0; x = blocks_of(ma, ++r); }
-      mine += kManyLead + x.tiles(i);
+      mine += weight(x.tiles(i));
     }
   }
   int64_t incl = mine;
@@ -141,8 +143,8 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
   }
   per_head = uniform(per_head);
   const int64_t total = per_head * a.b.Hkv;
-  const int64_t workgroups = min((int64_t)ma.workgroups, (total + kManyLeast - 1) / kManyLeast);
-  if (tid == 0 && blockIdx.x >= workgroups) ma.cuts[blockIdx.x].r = -1;
+  const int64_t workgroups = min((int64_t)ma.workgroups, ma.whole ? total : (total + kManyLeast - 1) / kManyLeast);
+  if (tid == 0 && blockIdx.x >= workgroups && !ma.whole) ma.cuts[blockIdx.x].r = -1;
   // neighbours in the sequence read the same keys: they run on the same die (workgroups go to the eight dies in turn)
   const int per_die = ((int)workgroups + 7) / 8, g = (int)(blockIdx.x & 7) * per_die + (int)(blockIdx.x >> 3);
   if ((int)(blockIdx.x >> 3) >= per_die || g >= workgroups) return;
@@ -158,7 +160,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
       int r = my_r, i = my_i;
       for (;; ++i) {
         while (i >= y.count) { i = 0; y = blocks_of(ma, ++r); }
-        const int positions = kManyLead + y.tiles(i);
+        const int positions = weight(y.tiles(i));
         if (at < start + positions) break;
         start += positions;
       }
@@ -174,7 +176,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
   for (;;) {
     const int tiles = uniform(of.tiles(block));
     const int64_t first = start + kManyLead;                      // position of its first tile
-    const int tile0 = uniform((int)max(x0 - first, (int64_t)0)), tile1 = uniform((int)min(x1 - first, (int64_t)tiles));
+    const int tile0 = ma.whole ? 0 : uniform((int)max(x0 - first, (int64_t)0)), tile1 = ma.whole ? tiles : uniform((int)min(x1 - first, (int64_t)tiles));
     if (tile1 > tile0) {
     const bool whole = tile0 == 0 && tile1 == tiles;
     const int slot = tile0 > 0 ? 2 * g : 2 * g + 1;
@@ -459,9 +461,9 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
       } while (of.count == 0);
       block = of.count - 1;
     }
-    start -= kManyLead + uniform(of.tiles(block));
+    start -= weight(uniform(of.tiles(block)));
   }
-  if (tid == 0) ma.cuts[g] = cut;
+  if (tid == 0 && !ma.whole) ma.cuts[g] = cut;
 }
 
 template <int D, bool FP8>

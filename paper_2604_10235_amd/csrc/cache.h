@@ -63,9 +63,9 @@ struct AttendPlan {
   int d;
   float scale;
   int few_rows, many_rows;     // requests of each kind (attend.hip)
-  int row_blocks, row_slots;   // few rows: blocks of 16 rows of the largest, and its rows
+  int row_slots, row_parts;    // few rows: rows of the largest, workgroups that they are shared out to
   int chunk, splits;           // few rows: keys of a workgroup, and workgroups per request and head
-  int workgroups, many_from, many_blocks;      // many rows: workgroups, rows from which a request is of this kind, blocks of rows
+  int workgroups, many_from, many_blocks, many_whole;        // many rows: workgroups, rows from which a request is of this kind, blocks of rows, none of them shared
   size_t off_few, off_many, ws_bytes;
 };
 int make_attend_plan(const codecomp_batch* b, const codecomp_pages* p, AttendPlan* plan);
