@@ -67,19 +67,22 @@ def attend(q, k_pages, v_pages, table, kv_lens, cu_q, *, max_kv_len, causal=True
         n = min(max(int(kv_lens[r]), 0), max_kv_len)
         rows = [(j, place(table, r, j, ps, n_pages)) for j in range(n)]
         held = [(j, p) for j, p in rows if p is not None]
-        for t in range(cu_q[r], cu_q[r + 1]):
-            mine = [p for j, p in held if not causal or j <= n - cu_q[r + 1] + t]
-            if not mine:
-                continue
-            pages, at = np.array([p[0] for p in mine]), np.array([p[1] for p in mine])
-            for h in range(Hq):
-                kk, vv = k_pages[pages, h // (Hq // Hkv), at], v_pages[pages, h // (Hq // Hkv), at]
-                z = scale * (kk @ q[t, h])
-                m = z.max()
-                p = np.exp(z - m)
-                lse[t, h] = m + np.log(p.sum())
-                p /= p.sum()
-                out[t, h] = p @ vv
-                spread[t, h] = p @ np.abs(vv)
-                reach[t, h] = scale * (np.abs(kk) @ np.abs(q[t, h])).max()
+        if not held or cu_q[r] == cu_q[r + 1]:
+            continue
+        slots, pages, at = (np.array(x) for x in ([j for j, _ in held], [p[0] for _, p in held], [p[1] for _, p in held]))
+        tokens = np.arange(cu_q[r], cu_q[r + 1])
+        sees = slots[None, :] <= n - cu_q[r + 1] + tokens[:, None] if causal else np.ones((len(tokens), len(slots)), bool)
+        some = sees.any(axis=1)
+        for h in range(Hq):
+            kk, vv, qq = k_pages[pages, h // (Hq // Hkv), at], v_pages[pages, h // (Hq // Hkv), at], q[tokens, h]
+            z = np.where(sees, scale * (qq @ kk.T), -np.inf)
+            m = np.where(some, z.max(axis=1), 0.0)[:, None]
+            p = np.exp(z - m)
+            total = p.sum(axis=1, keepdims=True)
+            with np.errstate(divide="ignore"):
+                lse[tokens, h] = (m + np.log(total))[:, 0]
+            p /= np.where(some[:, None], total, 1.0)
+            out[tokens, h] = p @ vv
+            spread[tokens, h] = p @ np.abs(vv)
+            reach[tokens, h] = np.where(sees, scale * (np.abs(qq) @ np.abs(kk).T), 0.0).max(axis=1)
     return out, lse, spread, reach

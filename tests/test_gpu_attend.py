@@ -55,6 +55,26 @@ def test_many_rows(lens, news, n_q, n_kv, d, page, fp8, causal):
     check(rng, c, news, n_q, causal=causal)
 
 
+# How the work is shared out: blocks of rows cut by several workgroups, shared by none, more blocks than threads that count them, more
+# requests than such threads, requests without tokens among them, short requests beside long ones and along with them.
+@pytest.mark.parametrize("lens, news, n_q, n_kv, d, page", [
+    ([9000], [70], 1, 1, 64, 64), ([5000, 100], [300, 90], 7, 1, 128, 16), ([700] * 3, [700, 650, 600], 2, 2, 64, 4), ([500] * 4, [500, 1, 70, 300], 4, 1, 128, 16),
+    ([2100, 2100], [2100, 1], 2, 1, 64, 32), ([300, 900] * 12, [1, 80] * 12, 4, 2, 64, 16), ([3000] + [2600] * 40, [90] + [1] * 40, 8, 8, 64, 128),
+    ([40] * 700, [0, 1, 0, 33, 2, 0, 0] * 100, 4, 2, 64, 8), ([200] * 520, [9] * 519 + [200], 2, 1, 64, 16)])
+def test_shares(lens, news, n_q, n_kv, d, page):
+    rng = np.random.default_rng([sum(lens), n_q, page, 2])
+    c = cu_.Cache(rng, lens, n_kv=n_kv, d=d, page=page)
+    check(rng, c, news, n_q)
+
+
+def test_many_tokens_of_one_prompt():
+    """More blocks of rows than a workgroup has threads: 66000 tokens of two heads, which see few keys each."""
+    rng = np.random.default_rng(21)
+    c = cu_.Cache(rng, [130], n_kv=2, d=64, page=16)
+    check(rng, c, [66000], 4, causal=False)
+    check(rng, c, [66000], 4)                  # all but the last 130 see nothing
+
+
 @pytest.mark.parametrize("news", [[1, 2, 1], [100, 40, 1]])
 def test_logits_of_hundreds(news):
     """Maxima that keep growing along the keys, and rows that see one key only."""
