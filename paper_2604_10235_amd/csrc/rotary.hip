@@ -15,6 +15,7 @@ typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kRotaryThreads = 256;
+constexpr int kRotaryFew = 3 << 16;      // units up to which every thread takes one head
 
 struct Vectors {               // bf16 [tokens][heads][d]
   const uint16_t* p;
@@ -83,6 +84,22 @@ __global__ __launch_bounds__(kRotaryThreads) void rotary_kernel(const RotateArgs
   const int group = (int)rest - t * a.groups;
   const bool there = t < a.T;
   t = min(t, a.T - 1);
+  const bool turned = u * 16 < a.rot.dim;
+  const int e0 = turned && !INTERLEAVED ? u * 8 : u * 16, e1 = turned && !INTERLEAVED ? a.rot.dim / 2 + u * 8 : u * 16 + 8;
+  // The vectors are sent for first: what follows up to their use is a chain of small loads, and the angles.
+  const int kv = APPEND ? a.b.Hkv : 0;
+  u32x4 lo[HPT], hi[HPT];
+#pragma unroll
+  for (int j = 0; j < HPT; ++j) {
+    const int h = group * HPT + j;
+    if (h >= a.heads || !there) continue;
+    const uint16_t* p;
+    if (!APPEND || h < a.q_heads) p = a.x.p + t * a.x.st + h * a.x.sh;
+    else if (h < a.q_heads + kv) p = a.k.p + t * a.k.st + (h - a.q_heads) * a.k.sh;
+    else p = a.v.p + t * a.v.st + (h - a.q_heads - kv) * a.v.sh;
+    lo[j] = *reinterpret_cast<const u32x4*>(p + e0);
+    hi[j] = *reinterpret_cast<const u32x4*>(p + e1);
+  }
   int64_t row = -1;            // where the token's K and V go
   if constexpr (APPEND) {
     int r = request_of(a.b.cu_q, a.b.n_seqs, __builtin_amdgcn_readfirstlane(t));
@@ -94,26 +111,11 @@ __global__ __launch_bounds__(kRotaryThreads) void rotary_kernel(const RotateArgs
     }
   }
   if (!there) return;
-  const bool turned = u * 16 < a.rot.dim;
-  const int e0 = turned && !INTERLEAVED ? u * 8 : u * 16, e1 = turned && !INTERLEAVED ? a.rot.dim / 2 + u * 8 : u * 16 + 8;
   float s[8], c[8];
   if (turned) {
     const uint64_t p = (uint64_t)(int64_t)a.positions[t];
 #pragma unroll
     for (int i = 0; i < 8; ++i) sine_cosine(p * a.rot.turns[u * 8 + i], a.rot.magnitude, s[i], c[i]);
-  }
-  const int kv = APPEND ? a.b.Hkv : 0;
-  u32x4 lo[HPT], hi[HPT];
-#pragma unroll
-  for (int j = 0; j < HPT; ++j) {
-    const int h = group * HPT + j;
-    if (h >= a.heads) continue;
-    const uint16_t* p;
-    if (!APPEND || h < a.q_heads) p = a.x.p + t * a.x.st + h * a.x.sh;
-    else if (h < a.q_heads + kv) p = a.k.p + t * a.k.st + (h - a.q_heads) * a.k.sh;
-    else p = a.v.p + t * a.v.st + (h - a.q_heads - kv) * a.v.sh;
-    lo[j] = *reinterpret_cast<const u32x4*>(p + e0);
-    hi[j] = *reinterpret_cast<const u32x4*>(p + e1);
   }
 #pragma unroll
   for (int j = 0; j < HPT; ++j) {
@@ -155,16 +157,21 @@ __global__ __launch_bounds__(kRotaryThreads) void rotary_kernel(const RotateArgs
   }
 }
 
+template <int HPT, bool APPEND>
+static int launch_rotary_of(RotateArgs& a, int units_log2, hipStream_t stream) {
+  a.groups = (a.heads + HPT - 1) / HPT;
+  const int64_t threads = ((int64_t)a.T * a.groups) << units_log2;
+  const dim3 grid((unsigned)((threads + kRotaryThreads - 1) / kRotaryThreads)), block(kRotaryThreads);
+  if (a.rot.interleaved) rotary_kernel<HPT, true, APPEND><<<grid, block, 0, stream>>>(a, units_log2);
+  else rotary_kernel<HPT, false, APPEND><<<grid, block, 0, stream>>>(a, units_log2);
+  return (int)hipGetLastError();
+}
+
 template <bool APPEND>
 static int launch_rotary(RotateArgs& a, int d, hipStream_t stream) {
   const int units_log2 = d == 128 ? 3 : 2;
-  constexpr int hpt = 4;
-  a.groups = (a.heads + hpt - 1) / hpt;
-  const int64_t threads = ((int64_t)a.T * a.groups) << units_log2;
-  const dim3 grid((unsigned)((threads + kRotaryThreads - 1) / kRotaryThreads)), block(kRotaryThreads);
-  if (a.rot.interleaved) rotary_kernel<hpt, true, APPEND><<<grid, block, 0, stream>>>(a, units_log2);
-  else rotary_kernel<hpt, false, APPEND><<<grid, block, 0, stream>>>(a, units_log2);
-  return (int)hipGetLastError();
+  if (((int64_t)a.T * a.heads << units_log2) <= kRotaryFew) return launch_rotary_of<1, APPEND>(a, units_log2, stream);
+  return launch_rotary_of<4, APPEND>(a, units_log2, stream);
 }
 
 int launch_rotate(const RotaryArgs& rot, const void* x, const int32_t* positions, int T, int H, int d, int64_t x_st, int64_t x_sh, void* out, int64_t o_st,
