@@ -148,8 +148,13 @@ __global__ __launch_bounds__(kRotaryThreads) void rotary_kernel(const RotateArgs
     unsigned char* o = (value ? a.pool.v : a.pool.k) + row + (h - a.q_heads - (value ? kv : 0)) * a.pool.s_head;
     // a value head's unit has the same elements as a key head's: e0 and e1
     if (a.pool.fp8) {
-      *reinterpret_cast<u32x2*>(o + e0) = narrow8(f);
-      *reinterpret_cast<u32x2*>(o + e1) = narrow8(f + 8);
+      const u32x2 x = narrow8(f), y = narrow8(f + 8);
+      if (e1 == e0 + 8) {
+        *reinterpret_cast<u32x4*>(o + e0) = u32x4{x.x, x.y, y.x, y.y};
+      } else {
+        *reinterpret_cast<u32x2*>(o + e0) = x;
+        *reinterpret_cast<u32x2*>(o + e1) = y;
+      }
     } else {
       *reinterpret_cast<u32x4*>(o + 2 * e0) = narrow(f);
       *reinterpret_cast<u32x4*>(o + 2 * e1) = narrow(f + 8);
