@@ -45,10 +45,21 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 ? 2 : 3) void attend_few_ke
   const int items = a.b.n_seqs * a.b.Hkv, turn = blockIdx.x / items, item = blockIdx.x - turn * items;
   const int split = turn / a.row_parts, row0 = (turn - split * a.row_parts) * (16 * RB);         // first of this workgroup's rows
   const int r = item / a.b.Hkv, head = item - r * a.b.Hkv;
+  // Entries of the page table for keys tile + l16 and 16 + tile + l16, not looked at before they are needed.  Those of the first two tiles are sent for
+  // before it is known how many keys there are: one wait less.
+  const int32_t* table = a.b.table + (int64_t)r * a.b.table_width;
+  const int key0 = split * a.chunk;
+  int page[2], next_page[2];
+  auto look_up = [&](int (&pg)[2], int tile, int end) __attribute__((always_inline)) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b) pg[b] = table[max(min(tile + 16 * b + l16, end - 1), 0) >> a.pool.page_log2];
+  };
+  look_up(page, key0 + wave * kFewKeys, a.b.max_kv);
+  look_up(next_page, key0 + (kFewWaves + wave) * kFewKeys, a.b.max_kv);
   const int q0 = a.b.cu_q[r], nq = a.b.cu_q[r + 1] - q0, rows = nq * a.b.G;
   if (rows <= row0 || rows > a.row_slots) return;
   const int len = kv_len_of(a.b, r);
-  const int key0 = split * a.chunk, key1 = min(len, key0 + a.chunk);
+  const int key1 = min(len, key0 + a.chunk);
   if (split > 0 && key0 >= len) return;
   const bool whole = len <= a.chunk;                            // the only chunk
 
@@ -70,16 +81,9 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 ? 2 : 3) void attend_few_ke
 
   const unsigned char* kb = a.pool.k + a.layer + head * a.pool.s_head + quarter * 16;
   const unsigned char* vb = a.pool.v + a.layer + head * a.pool.s_head + quarter * 16;
-  const int32_t* table = a.b.table + (int64_t)r * a.b.table_width;
   const int in_page = (1 << a.pool.page_log2) - 1;
   unsigned char* vs_lds = lds + wave * T::BYTES;
 
-  // Entries of the page table for keys tile + l16 and 16 + tile + l16 (the chunk's last one where there is none), not looked at before they are needed.
-  int page[2], next_page[2];
-  auto look_up = [&](int (&pg)[2], int tile) __attribute__((always_inline)) {
-#pragma unroll
-    for (int b = 0; b < 2; ++b) pg[b] = table[max(min(tile + 16 * b + l16, key1 - 1), 0) >> a.pool.page_log2];
-  };
   u32x4 kr[2][T::LOADS], vr[2][T::LOADS];
   auto send_for = [&](int tile, const int (&pg)[2]) __attribute__((always_inline)) {
     int64_t off[2];
@@ -107,8 +111,6 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 ? 2 : 3) void attend_few_ke
 
   bool left_out = false;
   int tile = key0 + wave * kFewKeys;
-  look_up(page, tile);
-  look_up(next_page, tile + kFewWaves * kFewKeys);
   if (tile < key1) send_for(tile, page);
   for (; tile < key1; tile += kFewWaves * kFewKeys) {
     bool there[2];
@@ -159,7 +161,7 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 ? 2 : 3) void attend_few_ke
     for (int b = 0; b < 2; ++b) page[b] = next_page[b];
     if (tile + kFewWaves * kFewKeys < key1) {
       send_for(tile + kFewWaves * kFewKeys, page);
-      look_up(next_page, tile + 2 * kFewWaves * kFewKeys);
+      look_up(next_page, tile + 2 * kFewWaves * kFewKeys, key1);
     }
 
     float p[RB][8];
@@ -299,17 +301,28 @@ __global__ __launch_bounds__(256) void join_few_kernel(const AttendArgs a) {
   __shared__ float weight[kFewMostSplits];
   __shared__ float red[4];
   __shared__ f32x4 sums[GROUPS][D / 4];
+  constexpr int AHEAD = 4;
   const int row_slots = a.row_slots, row = blockIdx.x % row_slots, item = blockIdx.x / row_slots, tid = threadIdx.x;
-  const int r = item / a.b.Hkv, head = item - r * a.b.Hkv;
+  const int r = item / a.b.Hkv, head = item - r * a.b.Hkv, group = tid / (D / 4), e = tid % (D / 4);
+  const int64_t part0 = (int64_t)item * a.splits * row_slots + row;       // of chunk s: + s * row_slots
+  // What a thread needs first is sent for before it is known how many chunks there are (workspace, whatever stands there).
+  float m0 = 0.0f, l0 = 0.0f;
+  f32x4 ahead[AHEAD];
+  if (tid < a.splits) {
+    m0 = a.part_ml[2 * (part0 + (int64_t)tid * row_slots)];
+    l0 = a.part_ml[2 * (part0 + (int64_t)tid * row_slots) + 1];
+  }
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i)
+    ahead[i] = *reinterpret_cast<const f32x4*>(a.part_o + (part0 + (int64_t)min(group + i * GROUPS, a.splits - 1) * row_slots) * D + e * 4);
   const int q0 = a.b.cu_q[r], rows = (a.b.cu_q[r + 1] - q0) * a.b.G;
   if (rows > row_slots || row >= rows) return;
   const int len = kv_len_of(a.b, r);
   if (len <= a.chunk) return;                                  // written by its only chunk
   const int n = (len + a.chunk - 1) / a.chunk;
-  const int64_t part0 = (int64_t)item * a.splits * row_slots + row;       // of chunk s: + s * row_slots
   float top = -INFINITY;
   for (int s = tid; s < n; s += 256) {
-    const float m = a.part_ml[2 * (part0 + (int64_t)s * row_slots)];
+    const float m = s < 256 ? m0 : a.part_ml[2 * (part0 + (int64_t)s * row_slots)];
     weight[s] = m;
     top = fmaxf(top, m);
   }
@@ -322,7 +335,7 @@ __global__ __launch_bounds__(256) void join_few_kernel(const AttendArgs a) {
   float all = 0.0f;
   for (int s = tid; s < n; s += 256) {
     const float f = weight[s] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(weight[s] - top);
-    const float l = a.part_ml[2 * (part0 + (int64_t)s * row_slots) + 1];
+    const float l = s < 256 ? l0 : a.part_ml[2 * (part0 + (int64_t)s * row_slots) + 1];
     weight[s] = f;
     all += l != l ? l : f * l;
   }
@@ -331,10 +344,12 @@ __global__ __launch_bounds__(256) void join_few_kernel(const AttendArgs a) {
   if ((tid & 63) == 0) red[tid >> 6] = all;
   __syncthreads();
   all = red[0] + red[1] + red[2] + red[3];
-  const int group = tid / (D / 4), e = tid % (D / 4);
   f32x4 x = {0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i)
+    if (group + i * GROUPS < n) x += ahead[i] * weight[group + i * GROUPS];
 #pragma unroll 8
-  for (int s = group; s < n; s += GROUPS) {
+  for (int s = group + AHEAD * GROUPS; s < n; s += GROUPS) {
     const f32x4 v = *reinterpret_cast<const f32x4*>(a.part_o + (part0 + (int64_t)s * row_slots) * D + e * 4);
     x += v * weight[s];
   }
