@@ -44,7 +44,7 @@ typedef struct codecomp_pages {
   int32_t n_kv_heads;
   int32_t head_dim;            /* 64 or 128                                                                      */
   int32_t kv_dtype;            /* CODECOMP_KV_BF16 or CODECOMP_KV_FP8_E4M3                                       */
-  int64_t stride_layer, stride_page, stride_head, stride_tok; /* elements, multiples of 16 bytes; 0 = dense
+  int64_t stride_layer, stride_page, stride_head, stride_tok; /* elements, multiples of 16 bytes; a page's rows within 2^31 bytes; 0 = dense
                                   [n_layers][n_pages][n_kv_heads][page_size][head_dim]                           */
   float k_scale, v_scale;      /* finite, > 0; 0 = 1                                                             */
 } codecomp_pages;
@@ -100,7 +100,7 @@ int codecomp_rotary_init(codecomp_rotary* rotary, int32_t dim, int32_t interleav
 
 /* out[t][h][:] = rotary(x[t][h][:], positions[t]) for n_tokens tokens of n_heads heads; x and out bf16, rotated in fp32 and
  * rounded once.  positions: DEVICE int32 [n_tokens], any value.  Strides in elements, multiples of 8; 0 = dense.
- * out may be x with the same strides.  n_tokens = 0 is a call that does nothing. */
+ * out may be x with the same strides.  n_tokens = 0 is a call that does nothing (as is a batch without new tokens below): vectors may be NULL then. */
 int codecomp_rotate(const void* x, const int32_t* positions, const codecomp_rotary* rotary, int32_t n_tokens, int32_t n_heads,
                     int32_t head_dim, int64_t x_stride_tok, int64_t x_stride_head, void* out, int64_t out_stride_tok,
                     int64_t out_stride_head, void* hip_stream);
@@ -150,7 +150,7 @@ size_t codecomp_attend_workspace_bytes(const codecomp_batch* batch, const codeco
  * lse[t][h] = ln sum_j exp(softmax_scale * q . k_j) (f32, dense [T][n_q_heads]; may be NULL): two caches attended to apart are joined with it.
  * A token that sees no row (or rows of pages that are not held alone) gets out = 0, lse = -inf.  What stands in rows that a token
  * does not see, NaN and infinities too, has no part in its result.  Logits, sums and outputs are fp32; the weights enter the second
- * product rounded to bf16 (requests of up to 64 rows, rows = new tokens * query heads per KV head: as two bf16, 16 bits together).
+ * product rounded to bf16, or as two bf16, 16 bits together, where all requests of the batch have up to 64 rows (new tokens * query heads per KV head).
  * workspace: >= codecomp_attend_workspace_bytes(), 256-byte aligned, contents on entry do not matter; NULL when that is 0.
  * Calls that may run at the same time need workspaces of their own. */
 int codecomp_attend(const void* q, const codecomp_batch* batch, const codecomp_pages* pages, int32_t layer, void* out, float* lse,

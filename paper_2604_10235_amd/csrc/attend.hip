@@ -1,4 +1,5 @@
 // codecomp_attend: which kernels a batch takes, and the workspace they share.
+#include <float.h>
 #include <math.h>
 
 #include "attend_many.h"
@@ -12,6 +13,7 @@ extern template int launch_many_of<128, true>(const ManyArgs&, hipStream_t);
 
 constexpr int kFewRowsMost = 64;          // rows of a request up to which it takes attend_few_kernel
 
+constexpr int64_t kMostFewBlocks = (1 << 24) - 1;
 constexpr int kAlongTiles = 2048;
 constexpr int kWholeTiles = 8;            // tiles of the longest block up to which none is shared by workgroups
 
@@ -52,10 +54,11 @@ int make_attend_plan(const codecomp_batch* b, const codecomp_pages* p, AttendPla
   int64_t chunk = (items * x.max_kv / 512 + 127) / 128 * 128;
   if (chunk < 128) chunk = 128;
   if (chunk > 2048) chunk = 2048;
-  while ((x.max_kv + chunk - 1) / chunk > kFewMostSplits) chunk *= 2;
+  // so many at most: the list of a row's chunks stands in LDS, and an axis of a grid holds 2^32 threads
+  while ((x.max_kv + chunk - 1) / chunk > kFewMostSplits || (x.max_kv > chunk && items * pl->row_parts * ((x.max_kv + chunk - 1) / chunk) > kMostFewBlocks)) chunk *= 2;
   pl->chunk = (int)chunk;
   pl->splits = x.max_kv > chunk ? (int)((x.max_kv + chunk - 1) / chunk) : 1;
-  if (items * pl->splits * kFewRowsMost > INT32_MAX) return CODECOMP_EINVAL_SHAPE;
+  if (pl->few_rows > 0 && (items * pl->row_parts > kMostFewBlocks || items * pl->row_slots > kMostFewBlocks)) return CODECOMP_EINVAL_SHAPE;
   size_t off = 0;
   pl->off_few = off;
   if (pl->few_rows > 0 && pl->splits > 1) off = align256(off + (size_t)(items * pl->splits * pl->row_slots) * (p->head_dim + 2) * sizeof(float));
@@ -125,7 +128,7 @@ int launch_attend(const AttendPlan& pl, const void* q, int layer, void* out, flo
   AttendArgs a = {};
   a.pool = pl.pool; a.b = pl.batch; a.q = static_cast<const uint16_t*>(q); a.out = static_cast<uint16_t*>(out); a.lse = lse;
   a.layer = layer * pl.pool.s_layer;
-  a.c = pl.scale * pl.pool.k_scale * kLog2e;
+  a.c = fminf(fmaxf(pl.scale * pl.pool.k_scale * kLog2e, FLT_MIN), FLT_MAX);       // a hidden logit of minus infinity times it stays one
   a.chunk = pl.chunk; a.splits = pl.splits; a.row_slots = pl.row_slots; a.row_parts = pl.row_parts;
   if (pl.few_rows > 0) {
     a.part_o = reinterpret_cast<float*>(static_cast<char*>(workspace) + pl.off_few);

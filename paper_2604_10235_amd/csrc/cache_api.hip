@@ -165,7 +165,7 @@ int codecomp_rotary_init(codecomp_rotary* r, int32_t dim, int32_t interleaved, d
 
 int codecomp_rotate(const void* x, const int32_t* positions, const codecomp_rotary* rotary, int32_t n_tokens, int32_t n_heads, int32_t head_dim,
                     int64_t x_stride_tok, int64_t x_stride_head, void* out, int64_t out_stride_tok, int64_t out_stride_head, void* hip_stream) {
-  if (!x || !positions || !rotary || !out) return CODECOMP_EINVAL_NULL;
+  if (!rotary || (n_tokens > 0 && (!x || !positions || !out))) return CODECOMP_EINVAL_NULL;
   if (head_dim != 64 && head_dim != 128) return CODECOMP_EINVAL_HEADDIM;
   if (n_heads < 1) return CODECOMP_EINVAL_HEADS;
   if (n_tokens < 0 || (int64_t)n_tokens * n_heads * (head_dim / 16) > INT32_MAX) return CODECOMP_EINVAL_SHAPE;
@@ -181,11 +181,11 @@ int codecomp_rotate(const void* x, const int32_t* positions, const codecomp_rota
 
 int codecomp_append(const void* q, const void* k, const void* v, const int32_t* positions, const codecomp_rotary* rotary, const codecomp_batch* batch,
                     const codecomp_pages* pages, int32_t layer, void* q_out, void* hip_stream) {
-  if (!k || !v || (!q) != (!q_out) || (rotary && !positions)) return CODECOMP_EINVAL_NULL;
   PagePool pool;
   PagedBatch b;
   if (int rc = make_pool(pages, &pool)) return rc;
   if (int rc = make_batch(batch, pages, &b)) return rc;
+  if (b.T > 0 && (!k || !v || (!q) != (!q_out) || (rotary && !positions))) return CODECOMP_EINVAL_NULL;
   if (layer < 0 || layer >= pages->n_layers) return CODECOMP_EINVAL_PAGES;
   if (misaligned16(q) || misaligned16(k) || misaligned16(v) || misaligned16(q_out)) return CODECOMP_EINVAL_SHAPE;
   RotaryArgs rot = {};
@@ -266,9 +266,9 @@ size_t codecomp_attend_workspace_bytes(const codecomp_batch* batch, const codeco
 
 int codecomp_attend(const void* q, const codecomp_batch* batch, const codecomp_pages* pages, int32_t layer, void* out, float* lse, void* workspace,
                     size_t workspace_bytes, void* hip_stream) {
-  if (!q || !out) return CODECOMP_EINVAL_NULL;
   AttendPlan pl;
   if (int rc = make_attend_plan(batch, pages, &pl)) return rc;
+  if (pl.batch.T > 0 && (!q || !out)) return CODECOMP_EINVAL_NULL;
   if (layer < 0 || layer >= pages->n_layers) return CODECOMP_EINVAL_PAGES;
   if (misaligned16(q) || misaligned16(out) || ((uintptr_t)lse & 3) != 0) return CODECOMP_EINVAL_SHAPE;
   if (pl.ws_bytes > 0 && (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < pl.ws_bytes)) return CODECOMP_EINVAL_WORKSPACE;

@@ -7,6 +7,7 @@ namespace codecomp {
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kMoveThreads = 256;
+constexpr int64_t kMostBlocks = (1 << 24) - 1;         // of 256 threads: an axis of a grid holds 2^32 threads
 constexpr int kMoveRows = 2;          // rows of K and of V that a thread has in flight
 
 // Byte offset of a request's row; -1 where there is none.
@@ -57,8 +58,9 @@ __global__ __launch_bounds__(kMoveThreads) void move_kernel(const MoveArgs a) {
 }
 
 int launch_move(const MoveArgs& a, int problems, hipStream_t stream) {
-  const int per_block = (kMoveThreads >> a.pieces_log2) * kMoveRows;
-  const dim3 grid((a.rows + per_block - 1) / per_block, problems), block(kMoveThreads);
+  const int64_t per_block = (kMoveThreads >> a.pieces_log2) * kMoveRows, blocks = (a.rows + per_block - 1) / per_block;
+  if (blocks > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
+  const dim3 grid((unsigned)blocks, problems), block(kMoveThreads);
   if (a.from.table && a.to.table) move_kernel<true, true><<<grid, block, 0, stream>>>(a);
   else if (a.from.table) move_kernel<true, false><<<grid, block, 0, stream>>>(a);
   else move_kernel<false, true><<<grid, block, 0, stream>>>(a);
@@ -108,7 +110,7 @@ int launch_pages_copy(const PagePool& pool, int L, int Hkv, int d, const int32_t
   if (pieces > INT32_MAX - per_block) return CODECOMP_EINVAL_SHAPE;
   a.pieces = (int)pieces;
   a.blocks = (int)((pieces + per_block - 1) / per_block);
-  if ((int64_t)a.blocks * n_pairs > INT32_MAX) return CODECOMP_EINVAL_SHAPE;
+  if ((int64_t)a.blocks * n_pairs > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
   copy_kernel<<<dim3((unsigned)(a.blocks * n_pairs), L), dim3(kMoveThreads), 0, stream>>>(a);
   return (int)hipGetLastError();
 }

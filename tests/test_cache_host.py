@@ -154,6 +154,32 @@ def test_calls_without_tokens_do_nothing():
     assert b.lib().codecomp_pages_copy(C.byref(p), None, 0, None) == 0
     r = b.make_rotary(64)
     assert b.lib().codecomp_rotate(D, D, C.byref(r), 0, 4, 128, 0, 0, D, 0, 0, None) == 0
+    # empty tensors have no address
+    assert b.lib().codecomp_rotate(None, None, C.byref(r), 0, 4, 128, 0, 0, None, 0, 0, None) == 0
+    assert attend(x, p, q=None, out=None) == 0 and append(x, p, q=None, k=None, v=None, pos=None, q_out=None) == 0
+    assert attend(x, p, layer=7) == -12 and append(x, p, layer=7) == -12
+    assert b.lib().codecomp_attend_workspace_bytes(C.byref(x), C.byref(p)) == 0
+
+
+def test_sizes_beyond_a_launch_are_refused():
+    huge = pool(n_kv_heads=4096, n_layers=1)
+    x = batch([0] + [1] * 60000, n_q_heads=4096)
+    assert attend(x, huge) == -2 and b.lib().codecomp_attend_validate(C.byref(x), C.byref(huge)) == -2
+    wide = pool(n_layers=1, n_kv_heads=65535, page_size=65536, head_dim=64, stride_tok=64, n_pages=1)
+    assert b.lib().codecomp_pages_copy(C.byref(wide), D, 2, None) == -2
+    assert b.lib().codecomp_pages_copy(C.byref(pool()), D, 2**30, None) == -2
+    assert attend(batch(), pool(page_size=65536, stride_tok=1 << 16)) == -2          # 8 GB in a page
+    # many requests of long tables: chunks grow until a launch holds them
+    x = batch(list(range(60001)), table_width=1 << 16, max_kv_len=1 << 20)
+    assert 0 < b.lib().codecomp_attend_workspace_bytes(C.byref(x), C.byref(pool()))
+
+
+def test_workspace_follows_lengths_and_tokens():
+    size = lambda cu, **kw: b.lib().codecomp_attend_workspace_bytes(C.byref(batch(cu, table_width=1 << 14, **kw)), C.byref(pool()))  # noqa: E731
+    assert size((0, 1), max_kv_len=100) == 0                                          # one chunk: written at once
+    assert 0 < size((0, 1), max_kv_len=5000) < size((0, 1), max_kv_len=100000)
+    assert size((0, 400), max_kv_len=500) == 0                                        # blocks of rows that nobody shares
+    assert size((0, 400), max_kv_len=5000) > 0
 
 
 def test_append_refuses():

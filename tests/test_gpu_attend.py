@@ -47,7 +47,7 @@ def test_few_rows(lens, news, n_q, n_kv, d, page, fp8, causal):
 @pytest.mark.parametrize("lens, news, n_q, n_kv, d, page, fp8", [
     ([65], [65], 1, 1, 64, 16, False), ([300], [300], 7, 1, 128, 16, False), ([1000, 130], [100, 130], 8, 2, 128, 64, True),
     ([700, 64, 20, 1500], [70, 64, 20, 1], 14, 2, 64, 1, False), ([50, 10, 333], [90, 90, 333], 4, 4, 128, 32, False),
-    ([2049], [33], 28, 4, 128, 128, False), ([900], [257], 2, 1, 128, 256, True), ([0, 129, 128, 127], [80, 80, 80, 80], 6, 3, 64, 8, True)])
+    ([2049], [33], 28, 4, 128, 128, False), ([500, 90], [200, 90], 7, 1, 128, 8, False), ([500, 90], [200, 90], 4, 2, 128, 2, True), ([900], [257], 2, 1, 128, 256, True), ([0, 129, 128, 127], [80, 80, 80, 80], 6, 3, 64, 8, True)])
 @pytest.mark.parametrize("causal", [True, False])
 def test_many_rows(lens, news, n_q, n_kv, d, page, fp8, causal):
     rng = np.random.default_rng([sum(lens), n_q, page, 1])
@@ -147,6 +147,27 @@ def test_garbage_in_places_that_are_not_seen(news, n_q, d, fp8):
         b.codecomp_attend(q, batch, c.pages(), 0, got, ws)
         c.v.copy_(keep)
         assert torch.equal(got[:at_token], clean[:at_token]) and not bool(torch.isfinite(got[at_token: news[0]]).any())
+
+
+@pytest.mark.parametrize("news", [[1, 2], [100, 40]])
+def test_scales_at_the_ends_of_fp32(news):
+    """Logits that all vanish: every key weighs the same, hidden ones still nothing."""
+    rng = np.random.default_rng(22)
+    c = cu_.Cache(rng, [200, 77], n_kv=2, d=64, page=16, fp8=True, k_scale=1e-30)
+    check(rng, c, news, 4, softmax_scale=1e-30)
+
+
+def test_a_batch_without_tokens():
+    c = cu_.Cache(np.random.default_rng(23), [40, 3], n_kv=2, d=64, page=16)
+    batch, _ = cu_.make_batch(c, [0, 0], 4)
+    q, k = (torch.empty((0, h, 64), dtype=torch.bfloat16, device="cuda") for h in (4, 2))
+    pos = torch.empty(0, dtype=torch.int32, device="cuda")
+    before = c.k.clone()
+    b.codecomp_append(q, k, k, pos, b.make_rotary(64), batch, c.pages(), 0, q)
+    b.codecomp_attend(q, batch, c.pages(), 0, q, None, lse=torch.empty((0, 4), device="cuda"))
+    b.codecomp_rotate(q, pos, b.make_rotary(64), q)
+    b.codecomp_pages_copy(c.pages(), torch.empty((0, 2), dtype=torch.int32, device="cuda"))
+    assert torch.equal(c.k, before)
 
 
 def test_strides_scale_and_layers():
