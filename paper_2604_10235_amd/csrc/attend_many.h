@@ -77,7 +77,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
   constexpr int TILE = kManyKeys * 2 * D;                        // bytes of the keys of a tile in LDS; its values stand behind them
   static_assert(kManyRows == 32 * kManyWaves, "a block of 32 rows per wave");
   __shared__ __attribute__((aligned(1024))) unsigned char tiles_lds[4 * 2 * TILE];
-  __shared__ int entries[8][kManyKeys];                           // of the page table, for the keys of a tile
+  __shared__ int entries[ROWWISE ? 8 : 4][64];                    // of the page table: below
   auto k_tile = [&](int tile) __attribute__((always_inline)) { return tiles_lds + (tile & 3) * (2 * TILE); };
   __shared__ int not_finite;
   __shared__ int64_t wave_sum[kManyWaves];
@@ -205,12 +205,15 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
     const int32_t* table = a.b.table + (int64_t)r * a.b.table_width;
     const int in_page = (1 << a.pool.page_log2) - 1;
 
-    // ---- the way of keys and values.  The page table's entries of a tile's 64 keys go into LDS five tiles ahead, the tile itself three ahead: 16-bit
-    // rows straight from memory into one of four buffers, 8-bit rows by way of registers, where they are widened.
-    auto fetch_entries = [&](int tile) __attribute__((always_inline)) {           // for the last key where a tile has none
-      const int32_t* from = table + (max(min(tile * kManyKeys + lane, of.len - 1), 0) >> a.pool.page_log2);
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds_address(entries[tile & 7])), "v"(from) : "memory", "m0");
+    // ---- the way of keys and values.  A tile goes into one of four LDS buffers three tiles ahead: 16-bit rows straight from memory, 8-bit rows by
+    // way of registers, where they are widened.  Entries of the page table go ahead of them, 64 at a time: one for every 16 keys, the 16 tiles of a
+    // stretch of 1024 keys at once (or, ROWWISE, one for every key of a tile, five tiles ahead).
+    auto fetch_entries = [&](int stretch) __attribute__((always_inline)) {        // for the last key where there is none
+      const int32_t* from = table + (max(min((stretch * 64 + lane) * (ROWWISE ? 1 : 16), of.len - 1), 0) >> a.pool.page_log2);
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds_address(entries[stretch & (ROWWISE ? 7 : 3)])), "v"(from) : "memory", "m0");
     };
+    auto entry = [&](int tile, int row) __attribute__((always_inline)) { return ROWWISE ? entries[tile & 7][row] : entries[(tile >> 4) & 3][(tile & 15) * 4 + (row >> 4)]; };
+    auto is_page = [&](int page) __attribute__((always_inline)) { return (unsigned)page < (unsigned)a.pool.n_pages; };
     // The rows of a tile that this thread loads pieces of: 8 bits, one and the same of K and V (the last ones by no thread at head_dim 64); 16 bits,
     // of the wave's 16 rows, the lane % 16th of K and the lane / 4th of V.
     const int k_row = FP8 ? (tid / PIECES) & (kManyKeys - 1) : (wave >> 1) * 16 + (lane & 15), v_row = FP8 ? k_row : (wave >> 1) * 16 + (lane >> 2);
@@ -220,13 +223,16 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
     const int wave_row = FP8 ? (wave * (64 / PIECES)) & (kManyKeys - 1) : (wave >> 1) * 16;
     const uint32_t k_lane_off = (k_row - wave_row) * (uint32_t)a.pool.s_tok + k_piece * 16, v_lane_off = (v_row - wave_row) * (uint32_t)a.pool.s_tok + v_piece * 16;
     auto place = [&](int tile, int row, int piece, uint32_t lane_off) __attribute__((always_inline)) {
-      const int page = ROWWISE ? entries[tile & 7][row] : uniform(entries[tile & 7][wave_row]);
-      const int64_t at = (page >= 0 && page < a.pool.n_pages ? page : 0) * a.pool.s_page;
-      if constexpr (ROWWISE) return Place{at + ((tile * kManyKeys + row) & in_page) * (int)a.pool.s_tok, (uint32_t)piece * 16};
-      return Place{at + ((tile * kManyKeys + wave_row) & in_page) * (int)a.pool.s_tok, lane_off};
+      const int page = ROWWISE ? entry(tile, row) : uniform(entry(tile, wave_row));
+      const int64_t at = (uint64_t)(unsigned)(is_page(page) ? page : 0) * (uint64_t)a.pool.s_page;
+      if constexpr (ROWWISE) return Place{at + (unsigned)((tile * kManyKeys + row) & in_page) * (unsigned)a.pool.s_tok, (uint32_t)piece * 16};
+      return Place{at + (unsigned)((tile * kManyKeys + wave_row) & in_page) * (unsigned)a.pool.s_tok, lane_off};
     };
     auto k_place = [&](int tile) __attribute__((always_inline)) { return place(tile, k_row, k_piece, k_lane_off); };
-    auto v_place = [&](int tile) __attribute__((always_inline)) { return place(tile, v_row, v_piece, v_lane_off); };
+    auto v_place = [&](int tile, Place k) __attribute__((always_inline)) {
+      if constexpr (!ROWWISE) return Place{k.base, v_lane_off};
+      return place(tile, v_row, v_piece, v_lane_off);
+    };
     u32x4 kr, vr;                                                // 8 bits: the tile after the next two, on its way
     auto fetch = [&](u32x4& into, uint32_t lds, const unsigned char* from, Place at) __attribute__((always_inline)) {
       if constexpr (FP8) {
@@ -255,9 +261,9 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
         *reinterpret_cast<u32x4*>(at + TILE + At::value(v_row, 2 * v_piece + 1)) = widen8(vr.z, vr.w);
       }
     };
-    auto is_there = [&](int tile, int page) __attribute__((always_inline)) {
-      return __ballot(tile < tile1 && tile * kManyKeys + lane < of.len && page >= 0 && page < a.pool.n_pages);
-    };
+    // The keys of a tile that there are; the tiles from `plain_end` on have keys that are not there, or that some rows do not see.
+    auto is_there = [&](int tile, int page) __attribute__((always_inline)) { return __ballot(tile * kManyKeys + lane < of.len && is_page(page)); };
+    const int plain_end = min(seen_by_all, of.len) >> 6;
     auto partly = [&](int tile) { return (tile + 1) * kManyKeys > seen_by_all && seen_by_all < of.len; };       // some rows do not see all of it
     // Values of a tile that has keys that are not there, or that some rows do not see: a weight of zero must not meet what stands in the one, nor an
     // infinite or NaN value in the other (added at the end, to the rows that see them).
@@ -295,13 +301,13 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
     auto fill = [&](int f, const unsigned char* kt, const unsigned char* vt) __attribute__((always_inline)) {
       ring[f % RING] = f & 1 ? value_frag(vt, f / 2) : key_frag(kt, f / 2);
     };
-    // One step: the weights p of the 32 keys from key0 on, whose logits are z (`valid`: which of them there are); beside them, on the matrix cores,
+    // One step: the weights p of the 32 keys from key0 on, whose logits are z (`masked`: not all rows see all of them; `valid`: which of them there are); beside them, on the matrix cores,
     // the logits zn of the next 32 keys (kt) and the outputs of the 32 before (vt), whose weights are pp.  The order is the source's: the LDS read that
     // the MFMA three further on needs (from the next step's tiles at the end), an MFMA, the vector work of a logit (two at head_dim 64), and
     // what `beside` has for this place.
     auto step = [&](f32x16& z, u32x4 (&p)[2], f32x16& zn, const unsigned char* kt, const u32x4 (&pp)[2], const unsigned char* vt, const unsigned char* kt_next,
-                    const unsigned char* vt_next, int key0, unsigned valid, auto&& beside) __attribute__((always_inline)) {
-      if (__builtin_expect(valid != 0xFFFFFFFFu || key0 + 32 > seen_by_all, 0)) {
+                    const unsigned char* vt_next, int key0, bool masked, unsigned valid, auto&& beside) __attribute__((always_inline)) {
+      if (__builtin_expect(masked, 0)) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int j = 8 * (i >> 2) + 4 * half + (i & 3);
@@ -362,18 +368,20 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
     __syncthreads();                                             // the segment before is through with LDS
     if (tid == 0) not_finite = 0;
 #pragma unroll
-    for (int j = 0; j < 5; ++j) fetch_entries(tile0 + j);
+    for (int j = 0; j < (ROWWISE ? 5 : 3); ++j) fetch_entries((ROWWISE ? tile0 : tile0 >> 4) + j);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
     for (int j = 0; j < 3; ++j) {
-      fetch_keys(tile0 + j, k_place(tile0 + j));
-      fetch_values(tile0 + j, v_place(tile0 + j));
+      const Place from = k_place(tile0 + j);
+      fetch_keys(tile0 + j, from);
+      fetch_values(tile0 + j, v_place(tile0 + j, from));
       if (j < 2) park(tile0 + j);
     }
     // in front of the first tile: values of zero
     for (int i = tid; i < HALF / 16; i += kManyThreads) *reinterpret_cast<u32x4*>(k_tile(tile0 + 3) + TILE + HALF + i * 16) = u32x4{0, 0, 0, 0};
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * LOADS) : "memory");
-    uint64_t valid = is_there(tile0, entries[tile0 & 7][lane]);
+    uint64_t valid = ROWWISE ? is_there(tile0, entry(tile0, lane)) : 0;
+    uint64_t held = ROWWISE ? 0 : __ballot(is_page(entries[(tile0 >> 4) & 3][lane]));          // groups of 16 keys of the stretch whose pages there are
     if (active) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) za[i] = 0.0f;
@@ -383,32 +391,41 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
       for (int f = 0; f < RING - 1; ++f) fill(f, k_tile(tile0) + HALF, k_tile(tile0 + 3) + TILE + HALF);
     }
     for (int tile = tile0; tile < tile1; ++tile) {
-      if (__builtin_expect(valid != ~0ull || partly(tile), 0)) clean_values(tile, valid);
+      bool masked = tile >= plain_end;
+      if constexpr (ROWWISE) {
+        masked |= valid != ~0ull;
+      } else {
+        if ((tile & 15) == 13) fetch_entries((tile >> 4) + 2);   // three tiles ahead a new stretch begins: the one after it
+        if ((tile & 15) == 0) held = __ballot(is_page(entries[(tile >> 4) & 3][lane]));
+        masked |= (((unsigned)(held >> ((tile & 15) * 4)) & 15u) != 15u);
+        if (masked) valid = is_there(tile, entry(tile, lane));
+      }
+      if (__builtin_expect(masked, 0)) clean_values(tile, valid);
       const unsigned char *t0 = k_tile(tile), *t1 = k_tile(tile + 1), *before = k_tile(tile + 3);
       // All of this step's LDS reads are on their way by the last places: from there on the tile before is nobody's, and the next one is everybody's.
       auto pass_on = [&](int f) __attribute__((always_inline)) {
-        if (f == F - (RING - 1)) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * LOADS + 1) : "memory");
+        if (f == F - (RING - 1)) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * LOADS + (ROWWISE ? 1 : 0)) : "memory");
       };
       Place k_from = {0, 0}, v_from = {0, 0};
       int next_entry = 0;
       auto send_for = [&](int f) __attribute__((always_inline)) {
-        if (f == 0) next_entry = entries[(tile + 1) & 7][lane];
+        if (ROWWISE && f == 0) next_entry = entry(tile + 1, lane);
         if (f == 0) park(tile + 2);
         if (f == 1) k_from = k_place(tile + 3);
-        if (f == 2) v_from = v_place(tile + 3);
+        if (f == 2) v_from = v_place(tile + 3, k_from);
         if (f == 3) fetch_keys(tile + 3, k_from);
         if (f == 4) fetch_values(tile + 3, v_from);
-        if (f == 5) fetch_entries(tile + 5);
+        if (f == 5 && ROWWISE) fetch_entries(tile + 5);
       };
       if (active) {
-        step(za, pa, zb, t0 + HALF, pb, before + TILE + HALF, t1, t0 + TILE, tile * kManyKeys, (unsigned)valid, pass_on);
-        step(zb, pb, za, t1, pa, t0 + TILE, t1 + HALF, t0 + TILE + HALF, tile * kManyKeys + 32, (unsigned)(valid >> 32), send_for);
+        step(za, pa, zb, t0 + HALF, pb, before + TILE + HALF, t1, t0 + TILE, tile * kManyKeys, masked, (unsigned)valid, pass_on);
+        step(zb, pb, za, t1, pa, t0 + TILE, t1 + HALF, t0 + TILE + HALF, tile * kManyKeys + 32, masked, (unsigned)(valid >> 32), send_for);
       } else {
         pass_on(F - (RING - 1));
 #pragma unroll
         for (int f = 0; f < F; ++f) send_for(f);
       }
-      valid = is_there(tile + 1, next_entry);
+      if constexpr (ROWWISE) valid = is_there(tile + 1, next_entry);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // what was sent for beyond the last tile
     if (active) {
