@@ -85,7 +85,7 @@ __global__ __launch_bounds__(256) void join_many_kernel(const ManyArgs ma, int r
     const int in_block = blockIdx.x * rows_each + i, row = cut.block * kManyRows + in_block;
     if (row >= rows) return;
     auto part_of = [&](int g) { return (int64_t)(g == first ? 2 * g + 1 : 2 * g) * kManyRows + in_block; };
-    float top = -1.0e30f, all = 0.0f;
+    float top = kNoReference, all = 0.0f;
 #pragma unroll 8
     for (int g = first; g <= cut.last; ++g) top = fmaxf(top, a.part_ml[2 * part_of(g)]);
     f32x4 x = {0, 0, 0, 0};

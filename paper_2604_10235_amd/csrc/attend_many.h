@@ -21,6 +21,9 @@ struct CutBlock {
 // Positions in front of the tiles of a block, in the sequence that is cut into equal parts: starting on a block (its queries, the first tiles) costs
 // about as much as that many tiles.
 constexpr int kManyLead = 7;
+// Reference of a row before its first visible key: finite, so that hidden logits (minus infinity) less it still are minus infinity, and so low that a
+// visible one's weight overflows, which makes it the reference.
+constexpr float kNoReference = -3.402823466e38f;
 constexpr int kManyLeast = 4;   // positions that a workgroup gets at least
 
 struct ManyArgs {
@@ -198,7 +201,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
       }
       limit = of.causal ? min(of.len, of.len - of.nq + t + 1) : of.len;
     }
-    const int seen_by_all = of.causal ? min(of.len, of.len - of.nq + block * kManyRows / of.G + 1) : of.len;
+    const int seen_by_all = uniform(of.causal ? min(of.len, of.len - of.nq + block * kManyRows / of.G + 1) : of.len);
 
     const unsigned char* kb = a.pool.k + a.layer + head * a.pool.s_head;
     const unsigned char* vb = a.pool.v + a.layer + head * a.pool.s_head;
@@ -280,7 +283,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
     };
 
     f32x16 o[DB];
-    float m = -1.0e30f, l = 0.0f;                                // a row's reference, this half's sum of weights
+    float m = kNoReference, l = 0.0f;                            // a row's reference, this half's sum of weights
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll

@@ -157,6 +157,29 @@ def test_scales_at_the_ends_of_fp32(news):
     check(rng, c, news, 4, softmax_scale=1e-30)
 
 
+@pytest.mark.parametrize("sign", [-1.0, 1.0])
+@pytest.mark.parametrize("news", [[1, 2], [100, 40]])
+def test_logits_near_the_ends_of_fp32(news, sign):
+    """Logits of +-2^117: all keys weigh the same, and no row counts as one that sees nothing.  The mean of n values is off by half a step and by the
+    rounding of n fp32 sums and of a quotient."""
+    rng = np.random.default_rng(23)
+    c = cu_.Cache(rng, [2000, 777], n_kv=2, d=64, page=16)
+    c.k[:] = 0.0
+    c.k[..., 5] = sign * 2.0**60
+    batch, cu = cu_.make_batch(c, news, 4, causal=False)
+    q = torch.zeros(int(cu[-1]), 4, 64, dtype=torch.bfloat16, device="cuda")
+    q[..., 5] = 2.0**60
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+    b.codecomp_attend(q, batch, c.pages(), 0, out, cu_.workspace(batch, c.pages()), lse=lse)
+    assert bool((lse / (sign * 2.0**117) - 1).abs().max() < 2.0**-20)          # 2^120 / sqrt(64); ln 2000 is nothing beside it
+    v = c.values()[1]
+    for r, n in enumerate(c.lens):
+        rows = np.stack([v[c.table[r, j // 16], :, j % 16] for j in range(n)])                       # [keys, KV heads, d]
+        mean, spread = rows.mean(0).repeat(2, 0), np.abs(rows).mean(0).repeat(2, 0)
+        got = cu_.f64(out[cu[r]: cu[r + 1]])
+        assert np.all(np.abs(got - mean) <= 2.0**-8 * np.abs(mean) + 1.01 * (n + 4) * 2.0**-24 * spread)
+
+
 def test_a_batch_without_tokens():
     c = cu_.Cache(np.random.default_rng(23), [40, 3], n_kv=2, d=64, page=16)
     batch, _ = cu_.make_batch(c, [0, 0], 4)
