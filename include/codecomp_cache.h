@@ -55,7 +55,7 @@ typedef struct codecomp_pages {
  * kv_lens[r] - cu_q[r + 1] + t.  Row j lies in page table[r][j / page_size]. */
 typedef struct codecomp_batch {
   int32_t n_seqs;              /* 1 .. 65535                                                                     */
-  int32_t n_q_heads;           /* a multiple of the pool's n_kv_heads                                            */
+  int32_t n_q_heads;           /* a multiple of the pool's n_kv_heads, at most 65535                              */
   int32_t table_width;         /* entries of a request's row of the table                                        */
   int32_t max_kv_len;          /* HOST bound of kv_lens, <= table_width * page_size: sizes launches and workspace */
   int32_t causal;              /* 1: a new token sees the rows up to its own; 0: all rows of its request (attention
@@ -99,7 +99,7 @@ int codecomp_rotary_init(codecomp_rotary* rotary, int32_t dim, int32_t interleav
                          double context, double low, double high);
 
 /* out[t][h][:] = rotary(x[t][h][:], positions[t]) for n_tokens tokens of n_heads heads; x and out bf16, rotated in fp32 and
- * rounded once.  positions: DEVICE int32 [n_tokens], any value.  Strides in elements, multiples of 8; 0 = dense.
+ * rounded once; n_heads at most 65535.  positions: DEVICE int32 [n_tokens], any value.  Strides in elements, multiples of 8; 0 = dense.
  * out may be x with the same strides.  n_tokens = 0 is a call that does nothing (as is a batch without new tokens below): vectors may be NULL then. */
 int codecomp_rotate(const void* x, const int32_t* positions, const codecomp_rotary* rotary, int32_t n_tokens, int32_t n_heads,
                     int32_t head_dim, int64_t x_stride_tok, int64_t x_stride_head, void* out, int64_t out_stride_tok,

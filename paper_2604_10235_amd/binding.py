@@ -316,6 +316,15 @@ def make_rotary(dim: int, *, base: float = 10000.0, interleaved: bool = False, i
     return r
 
 
+def _own_strides(t, what: str):
+    """Strides for the library: 0 (dense) where there is one place only; a stride of 0 between several would be taken for dense."""
+    if t.is_contiguous():
+        return (0,) * t.dim()
+    if any(n > 1 and s == 0 for n, s in zip(t.shape, t.stride())):
+        raise ValueError(f"{what} must not be a broadcast tensor (strides {t.stride()})")
+    return [s if n > 1 else 0 for n, s in zip(t.shape, t.stride())]
+
+
 def make_pages(k, v, *, k_scale: float = 1.0, v_scale: float = 1.0) -> codecomp_pages:
     """A pool over two tensors [layers, pages, KV heads, page size, head_dim] with the same strides, bf16 or 8-bit (float8_e4m3fn, or codes as uint8)."""
     import torch
@@ -325,11 +334,12 @@ def make_pages(k, v, *, k_scale: float = 1.0, v_scale: float = 1.0) -> codecomp_
         raise ValueError(f"a cache holds bfloat16 or 8-bit (float8_e4m3fn, uint8) elements, not {k.dtype}")
     if k.stride(4) != 1:
         raise ValueError("the elements of a row must be contiguous")
+    strides = _own_strides(k, "a pool")
     p = codecomp_pages()
     p.k, p.v = k.data_ptr(), v.data_ptr()
     p.n_layers, p.n_pages, p.n_kv_heads, p.page_size, p.head_dim = k.shape
     p.kv_dtype = KV_BF16 if k.dtype == torch.bfloat16 else KV_FP8_E4M3
-    p.stride_layer, p.stride_page, p.stride_head, p.stride_tok = k.stride()[:4]
+    p.stride_layer, p.stride_page, p.stride_head, p.stride_tok = strides[:4]
     p.k_scale, p.v_scale = k_scale, v_scale
     p._keep, p._at = (k, v), k.get_device()
     return p
@@ -350,10 +360,14 @@ def make_batch(*, n_q_heads: int, cu_q_host: np.ndarray, cu_q, kv_lens, table, m
     _int32(cu_q, (n + 1,), "cu_q")
     _int32(kv_lens, (n,), "kv_lens")
     _int32(table, (n, table.shape[-1]), "table")
+    if len({t.device for t in (cu_q, kv_lens, table)}) > 1:
+        raise ValueError("cu_q, kv_lens and table must be on the same device")
     b = codecomp_batch()
     b.n_seqs, b.n_q_heads, b.table_width, b.max_kv_len, b.causal, b.softmax_scale = n, n_q_heads, table.shape[1], max_kv_len, int(causal), softmax_scale
     b.cu_q_host, b.cu_q_dev, b.kv_lens_dev, b.table_dev = host.ctypes.data, cu_q.data_ptr(), kv_lens.data_ptr(), table.data_ptr()
     for name, val in strides.items():
+        if "_stride_" not in name or not hasattr(b, name):
+            raise TypeError(f"codecomp_batch has no stride {name}")
         setattr(b, name, val)
     b._keep, b._tokens, b._at = (host, cu_q, kv_lens, table), int(host[-1]), cu_q.get_device()
     return b
@@ -391,8 +405,8 @@ def codecomp_rotate(x, positions, rotary: codecomp_rotary, out) -> None:
         raise ValueError("x and out must be bfloat16 [tokens, heads, head_dim] with contiguous heads")
     T, H, d = x.shape
     _int32(positions, (T,), "positions")
+    xs, os_ = _own_strides(x, "x"), _own_strides(out, "out")
     stream = _launch_stream(x.get_device(), positions.get_device(), out.get_device())
-    xs, os_ = x.stride(), out.stride()
     _check(lib().codecomp_rotate(x.data_ptr(), positions.data_ptr(), C.byref(rotary), T, H, d, xs[0], xs[1], out.data_ptr(), os_[0], os_[1], stream),
            "codecomp_rotate")
 
@@ -497,6 +511,8 @@ def codecomp_attend(q, batch: codecomp_batch, pages: codecomp_pages, layer: int,
     qp, op = _vectors(q, "q", shape, batch.q_stride_tok, batch.q_stride_head), _vectors(out, "out", shape, batch.out_stride_tok, batch.out_stride_head)
     if lse is not None and (lse.dtype != torch.float32 or lse.shape != shape[:2] or not lse.is_contiguous()):
         raise ValueError(f"lse must be a contiguous float32 tensor {shape[:2]}, not {lse.dtype} {tuple(lse.shape)}")
+    if workspace is not None and not workspace.is_contiguous():
+        raise ValueError("the workspace must be contiguous")
     at = pages._at
     stream = _launch_stream(at, batch._at, q.get_device(), out.get_device(), _at(lse, at), _at(workspace, at))
     size = 0 if workspace is None else workspace.numel() * workspace.element_size()

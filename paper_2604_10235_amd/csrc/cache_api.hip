@@ -7,6 +7,8 @@
 
 namespace codecomp {
 
+constexpr int kMostHeads = 65535;      // with which sizes can be multiplied in 64 bits
+
 static bool misaligned16(const void* p) { return ((uintptr_t)p & 15) != 0; }
 static bool bad_strides(std::initializer_list<int64_t> strides, int multiple) {
   for (int64_t s : strides)
@@ -29,7 +31,7 @@ int make_pool(const codecomp_pages* p, PagePool* pool) {
   const int64_t st = p->stride_tok ? p->stride_tok : d, sh = p->stride_head ? p->stride_head : p->page_size * d;
   const int64_t sp = p->stride_page ? p->stride_page : p->n_kv_heads * p->page_size * d;
   const int64_t sl = p->stride_layer ? p->stride_layer : p->n_pages * (p->n_kv_heads * (p->page_size * d));
-  if (st < d || st * p->page_size * esz > INT32_MAX) return CODECOMP_EINVAL_SHAPE;       // places inside a page are counted in 32 bits
+  if (st < d || st > INT32_MAX / (p->page_size * esz)) return CODECOMP_EINVAL_SHAPE;       // places inside a page are counted in 32 bits
   pool->k = static_cast<unsigned char*>(p->k); pool->v = static_cast<unsigned char*>(p->v);
   pool->n_pages = p->n_pages; pool->page_log2 = __builtin_ctz((unsigned)p->page_size); pool->fp8 = esz == 1;
   pool->s_layer = sl * esz; pool->s_page = sp * esz; pool->s_head = sh * esz; pool->s_tok = st * esz;
@@ -41,7 +43,7 @@ int make_pool(const codecomp_pages* p, PagePool* pool) {
 int make_batch(const codecomp_batch* b, const codecomp_pages* p, PagedBatch* out) {
   if (!b || !b->cu_q_host || !b->cu_q_dev || !b->kv_lens_dev || !b->table_dev) return CODECOMP_EINVAL_NULL;
   if (b->n_seqs < 1 || b->n_seqs > 65535) return CODECOMP_EINVAL_SHAPE;
-  if (b->n_q_heads < 1 || b->n_q_heads % p->n_kv_heads != 0) return CODECOMP_EINVAL_HEADS;
+  if (b->n_q_heads < 1 || b->n_q_heads > kMostHeads || b->n_q_heads % p->n_kv_heads != 0) return CODECOMP_EINVAL_HEADS;
   if (b->causal != 0 && b->causal != 1) return CODECOMP_EINVAL_MODE;
   if (!(b->softmax_scale >= 0.0f) || !isfinite(b->softmax_scale)) return CODECOMP_EINVAL_PRIOR;
   if (b->table_width < 1 || b->max_kv_len < 0 || b->max_kv_len > (int64_t)b->table_width * p->page_size) return CODECOMP_EINVAL_PAGES;
@@ -167,7 +169,7 @@ int codecomp_rotate(const void* x, const int32_t* positions, const codecomp_rota
                     int64_t x_stride_tok, int64_t x_stride_head, void* out, int64_t out_stride_tok, int64_t out_stride_head, void* hip_stream) {
   if (!rotary || (n_tokens > 0 && (!x || !positions || !out))) return CODECOMP_EINVAL_NULL;
   if (head_dim != 64 && head_dim != 128) return CODECOMP_EINVAL_HEADDIM;
-  if (n_heads < 1) return CODECOMP_EINVAL_HEADS;
+  if (n_heads < 1 || n_heads > kMostHeads) return CODECOMP_EINVAL_HEADS;
   if (n_tokens < 0 || (int64_t)n_tokens * n_heads * (head_dim / 16) > INT32_MAX) return CODECOMP_EINVAL_SHAPE;
   if (bad_strides({x_stride_tok, x_stride_head, out_stride_tok, out_stride_head}, 8) || misaligned16(x) || misaligned16(out)) return CODECOMP_EINVAL_SHAPE;
   const int64_t x_sh = x_stride_head ? x_stride_head : head_dim, o_sh = out_stride_head ? out_stride_head : head_dim;

@@ -263,3 +263,42 @@ def test_binding_refuses_tensors_that_do_not_fit():
         return
     with pytest.raises(ValueError):           # everything there, but on the CPU
         b.codecomp_attend(q, x, p, 0, q.clone(), None)
+
+
+def test_products_of_sizes_that_wrap_around_are_refused():
+    """Each of these passes every bound by itself; multiplied in 64 bits they would come out small or negative."""
+    r, most = b.make_rotary(64), 2**31 - 1
+    rotate = lambda T, H: b.lib().codecomp_rotate(D, D, C.byref(r), T, H, 128, 0, 0, D, 0, 0, None)  # noqa: E731
+    assert rotate(most, most) == -6 and rotate(2**30, 2**30) == -6 and rotate(1, 65536) == -6 and rotate(most, 65535) == -2
+    for cu, heads, code in [((0, 2**30), 2**30, -6), ((0, 1), 1 << 16, -6), ((0, most), 65532, -2)]:
+        x, p = batch(cu, n_q_heads=heads), pool()
+        assert attend(x, p) == code and append(x, p) == code
+    for stride in (2**62, 2**47, 2**31):
+        assert attend(batch(), pool(stride_tok=stride, page_size=65536)) == -2
+
+
+def test_binding_refuses_broadcast_and_scattered_tensors():
+    """A stride of zero is not the dense layout that a zero stands for in the C interface."""
+    import torch
+    bf = lambda *s: torch.zeros(*s, dtype=torch.bfloat16)  # noqa: E731
+    r, pos = b.make_rotary(64), torch.zeros(5, dtype=torch.int32)
+    for bad in (bf(1, 4, 64).expand(5, 4, 64), bf(5, 1, 64).expand(5, 4, 64)):
+        with pytest.raises(ValueError, match="broadcast"):
+            b.codecomp_rotate(bad, pos, r, bf(5, 4, 64))
+        with pytest.raises(ValueError, match="broadcast"):
+            b.codecomp_rotate(bf(5, 4, 64), pos, r, bad)
+    for bad in (bf(1, 3, 2, 16, 64).expand(2, 3, 2, 16, 64), bf(2, 3, 1, 16, 64).expand(2, 3, 2, 16, 64), bf(2, 3, 2, 1, 64).expand(2, 3, 2, 16, 64)):
+        with pytest.raises(ValueError, match="broadcast"):
+            b.make_pages(bad, bad)
+    one = b.make_pages(*[bf(1, 3, 1, 16, 64).as_strided((1, 3, 1, 16, 64), (3, 1024, 5, 64, 1))] * 2)          # strides of single places say nothing
+    assert (one.stride_layer, one.stride_page, one.stride_head, one.stride_tok) == (0, 1024, 0, 64)
+    i32 = lambda *s: torch.zeros(*s, dtype=torch.int32)  # noqa: E731
+    good = dict(n_q_heads=4, cu_q_host=np.array([0, 2, 3], np.int32), cu_q=i32(3), kv_lens=i32(2), table=i32(2, 3), max_kv_len=48)
+    for name in ("cu_q", "kv_lens", "table"):                                                                     # not all on one device
+        with pytest.raises(ValueError, match="device"):
+            b.make_batch(**{**good, name: good[name].to("meta")})
+    with pytest.raises(TypeError):
+        b.make_batch(**good, q_strides_tok=8)
+    x, p = b.make_batch(**good), b.make_pages(bf(1, 3, 2, 16, 64), bf(1, 3, 2, 16, 64))
+    with pytest.raises(ValueError, match="workspace"):
+        b.codecomp_attend(bf(3, 4, 64), x, p, 0, bf(3, 4, 64), torch.zeros(1, dtype=torch.uint8).expand(1 << 20))
