@@ -11,11 +11,24 @@ extern template int launch_many_of<64, true>(const ManyArgs&, hipStream_t);
 extern template int launch_many_of<128, false>(const ManyArgs&, hipStream_t);
 extern template int launch_many_of<128, true>(const ManyArgs&, hipStream_t);
 
-constexpr int kFewRowsMost = 64;          // rows of a request up to which it takes attend_few_kernel
+// Which kernel a request takes goes by its rows (new tokens x query heads per KV head).  Up to kFewRows it is attend_few_kernel's, which gives a
+// chunk of keys to a workgroup (28 query heads on 4 KV heads of 128 elements, us, few | many rows' kernel: 4 tokens over 8192 keys 15 | 23, over 131072 60 |
+// 72; the last has the better of it from a few GB on, 64 requests over 8192 keys 212 | 190, with weights of half the digits).  Up to kFewRowsMost two
+// workgroups share the rows and both read the keys, which pays while these are few (9 tokens over 8192 keys 19 | 24, over 32768 38 | 41, over 131072 92 |
+// 75; 64 requests over 8192 keys 353 | 191), and always from an 8-bit cache, whose rows cost the other kernel as much as 16-bit ones
+// (131072 keys 57 | 78; 64 requests 198 | 219).  Beyond, a third and a fourth workgroup never pay from 8000 keys on (18 tokens over 32768 keys 57 | 44).
+constexpr int kFewRows = 32, kFewRowsMost = 64;
+constexpr int64_t kFewKeysMost = 1 << 17;        // keys of all requests and KV heads, at their largest, up to which kFewRowsMost holds for bf16
+// In a batch with longer chunks, the short requests of a bf16 cache go along with them, with fewer launches and at the bandwidth that long ones have
+// (512 tokens over 4096 keys and 64 steps of one over 4096: 161 us apart, 138 together; 10 tokens and 64 steps over 16384: 399, 369).  From an 8-bit
+// cache only so many of them as the launches cost, in tiles of the many-row kernel (4 steps over 4096 keys 79 apart, 75 together; 8 of them 80, 85; 10
+// tokens and 64 steps over 16384 226, 422).
+constexpr int64_t kAlongTiles = 1024;
 
 constexpr int64_t kMostFewBlocks = (1 << 24) - 1;
-constexpr int kAlongTiles = 2048;
-constexpr int kWholeTiles = 8;            // tiles of the longest block up to which none is shared by workgroups
+// Tiles of the longest block of rows up to which blocks are not shared by workgroups: no parts to be joined (a prompt of 500 tokens 27 us, 32 with
+// sharing; of 100 19, 23).
+constexpr int kWholeTiles = 8;
 
 static size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
@@ -25,22 +38,24 @@ int make_attend_plan(const codecomp_batch* b, const codecomp_pages* p, AttendPla
   const PagedBatch& x = pl->batch;
   pl->d = p->head_dim;
   pl->scale = b->softmax_scale > 0.0f ? b->softmax_scale : 1.0f / sqrtf((float)p->head_dim);
-  int few_most = 0;
-  pl->few_rows = pl->many_rows = 0;
-  for (int r = 0; r < x.n_seqs; ++r) {
-    const int64_t rows = (int64_t)(b->cu_q_host[r + 1] - b->cu_q_host[r]) * x.G;
-    if (rows == 0) continue;
-    if (rows > kFewRowsMost) { ++pl->many_rows; continue; }
-    ++pl->few_rows;
-    if (rows > few_most) few_most = (int)rows;
+  int few_most, few_limit = kFewRowsMost;
+  for (;;) {
+    few_most = pl->few_rows = pl->many_rows = 0;
+    for (int r = 0; r < x.n_seqs; ++r) {
+      const int64_t rows = (int64_t)(b->cu_q_host[r + 1] - b->cu_q_host[r]) * x.G;
+      if (rows == 0) continue;
+      if (rows > few_limit) { ++pl->many_rows; continue; }
+      ++pl->few_rows;
+      if (rows > few_most) few_most = (int)rows;
+    }
+    if (few_most <= kFewRows || pl->pool.fp8 || (int64_t)pl->few_rows * x.Hkv * x.max_kv <= kFewKeysMost) break;
+    few_limit = kFewRows;
   }
-  // In a batch with longer chunks, a few short requests go along with them: up to kAlongTiles tiles of the many-row kernel, what the launches of
-  // the other two kernels cost.
-  if (pl->many_rows > 0 && (int64_t)pl->few_rows * x.Hkv * ((x.max_kv + kManyKeys - 1) / kManyKeys) <= kAlongTiles) {
+  if (pl->many_rows > 0 && (!pl->pool.fp8 || (int64_t)pl->few_rows * x.Hkv * ((x.max_kv + kManyKeys - 1) / kManyKeys) <= kAlongTiles)) {
     pl->many_rows += pl->few_rows;
     pl->few_rows = few_most = 0;
   }
-  pl->many_from = pl->few_rows > 0 ? kFewRowsMost + 1 : 1;
+  pl->many_from = pl->few_rows > 0 ? few_limit + 1 : 1;
   int64_t blocks = 0;
   for (int r = 0; r < x.n_seqs; ++r) {
     const int64_t rows = (int64_t)(b->cu_q_host[r + 1] - b->cu_q_host[r]) * x.G;
@@ -50,7 +65,9 @@ int make_attend_plan(const codecomp_batch* b, const codecomp_pages* p, AttendPla
   pl->row_parts = (few_most + 31) / 32;
   pl->row_slots = few_most;
   const int64_t items = (int64_t)x.n_seqs * x.Hkv;
-  // chunks of keys: about two workgroups per compute unit if all requests are of the largest length, of at least 128 keys each
+  // chunks of keys: about two workgroups per compute unit if all requests are of the largest length, of at least 128 keys each (one tile for each wave)
+  // and at most 2048 (one token over 131072 keys, 4 KV heads: chunks of 512 58 us, of 1024 55, of 4096 68; 64 requests of 500 .. 16384 keys, 8 bits: 512
+  // 215, 1024 200, 2048 199, 4096 209)
   int64_t chunk = (items * x.max_kv / 512 + 127) / 128 * 128;
   if (chunk < 128) chunk = 128;
   if (chunk > 2048) chunk = 2048;
@@ -116,7 +133,8 @@ static int launch_many(const AttendPlan& pl, const AttendArgs& a, char* workspac
   if (pl.d == 128) rc = pl.pool.fp8 ? launch_many_of<128, true>(m, stream) : launch_many_of<128, false>(m, stream);
   else rc = pl.pool.fp8 ? launch_many_of<64, true>(m, stream) : launch_many_of<64, false>(m, stream);
   if (rc || pl.many_whole) return rc;
-  // a few blocks of many parts: their rows over more workgroups
+  // A few blocks of many parts: their rows over more workgroups (20 tokens over 131072 keys 83 us, 16 rows each 96, 64 rows each 213); many blocks of
+  // a part or two: fewer workgroups (12 x 1024 tokens over 4096 keys, head_dim 64: 8 rows each 125, 16 124).
   const int rows_each = pl.many_blocks <= 32 ? 256 / (pl.d / 4) : 16;
   const dim3 grid(kManyRows / rows_each, pl.workgroups), block(256);
   if (pl.d == 128) join_many_kernel<128><<<grid, block, 0, stream>>>(m, rows_each);

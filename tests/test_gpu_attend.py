@@ -67,6 +67,17 @@ def test_shares(lens, news, n_q, n_kv, d, page):
     check(rng, c, news, n_q)
 
 
+# 33 .. 64 rows, alone and beside single tokens, where the bound on lengths makes the batch a small one and a large one.
+@pytest.mark.parametrize("news", [[9, 0, 16], [9, 1, 16], [1, 2, 5], [13, 1, 3]])
+@pytest.mark.parametrize("fp8", [False, True])
+def test_middle_sized_chunks_of_long_caches(news, fp8):
+    rng = np.random.default_rng([24, news[0]])
+    c = cu_.Cache(rng, [1300, 140, 16], n_kv=2, d=128, page=256, fp8=fp8, width_more=300, k_scale=0.03 if fp8 else 1.0, v_scale=0.02 if fp8 else 1.0)
+    for max_kv in (1300, 70000):
+        check(rng, c, news, 8, max_kv=max_kv)
+        check(rng, c, news, 8, max_kv=max_kv, causal=False)
+
+
 def test_many_tokens_of_one_prompt():
     """More blocks of rows than a workgroup has threads: 66000 tokens of two heads, which see few keys each."""
     rng = np.random.default_rng(21)
