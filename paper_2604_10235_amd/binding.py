@@ -318,8 +318,6 @@ def make_rotary(dim: int, *, base: float = 10000.0, interleaved: bool = False, i
 
 def _own_strides(t, what: str):
     """Strides for the library: 0 (dense) where there is one place only; a stride of 0 between several would be taken for dense."""
-    if t.is_contiguous():
-        return (0,) * t.dim()
     if any(n > 1 and s == 0 for n, s in zip(t.shape, t.stride())):
         raise ValueError(f"{what} must not be a broadcast tensor (strides {t.stride()})")
     return [s if n > 1 else 0 for n, s in zip(t.shape, t.stride())]
@@ -405,7 +403,7 @@ def codecomp_rotate(x, positions, rotary: codecomp_rotary, out) -> None:
         raise ValueError("x and out must be bfloat16 [tokens, heads, head_dim] with contiguous heads")
     T, H, d = x.shape
     _int32(positions, (T,), "positions")
-    xs, os_ = _own_strides(x, "x"), _own_strides(out, "out")
+    xs, os_ = ((0, 0) if y.is_contiguous() else _own_strides(y, what) for y, what in ((x, "x"), (out, "out")))
     stream = _launch_stream(x.get_device(), positions.get_device(), out.get_device())
     _check(lib().codecomp_rotate(x.data_ptr(), positions.data_ptr(), C.byref(rotary), T, H, d, xs[0], xs[1], out.data_ptr(), os_[0], os_[1], stream),
            "codecomp_rotate")
