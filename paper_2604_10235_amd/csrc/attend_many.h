@@ -75,6 +75,9 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
   constexpr int PIECES = D * (FP8 ? 1 : 2) / 16;               // 16-byte pieces of a stored row
   // 16-byte pieces of K and of V per thread and tile: of one row (8 bits), or of a wave's chunks, which lie side by side in 16 rows
   constexpr int LOADS = FP8 ? 1 : D / 64;
+  // 8 bits at head_dim 64: half of the waves have the keys, the others the values
+  constexpr bool HALVES = FP8 && D == 64;
+  constexpr int SENT = HALVES ? 1 : 2 * LOADS;                    // loads of a wave for a tile
   using At = TileAt<D>;
   constexpr int KS = D / 16, DB = D / 32;
   constexpr int TILE = kManyKeys * 2 * D;                        // bytes of the keys of a tile in LDS; its values stand behind them
@@ -217,13 +220,16 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
     };
     auto entry = [&](int tile, int row) __attribute__((always_inline)) { return ROWWISE ? entries[tile & 7][row] : entries[(tile >> 4) & 3][(tile & 15) * 4 + (row >> 4)]; };
     auto is_page = [&](int page) __attribute__((always_inline)) { return (unsigned)page < (unsigned)a.pool.n_pages; };
-    // The rows of a tile that this thread loads pieces of: 8 bits, one and the same of K and V (the last ones by no thread at head_dim 64); 16 bits,
-    // of the wave's 16 rows, the lane % 16th of K and the lane / 4th of V.
-    const int k_row = FP8 ? (tid / PIECES) & (kManyKeys - 1) : (wave >> 1) * 16 + (lane & 15), v_row = FP8 ? k_row : (wave >> 1) * 16 + (lane >> 2);
-    const int k_piece = FP8 ? tid % PIECES : (wave & 1) * LOADS * 4 + (lane >> 4), v_piece = FP8 ? k_piece : (wave & 1) * LOADS * 4 + (lane & 3);
+    // The rows of a tile that this thread loads pieces of.  16 bits: of the wave's 16 rows, the lane % 16th of K and the lane / 4th of V.  8 bits: of its
+    // 8 or 16, in an order that makes the stores of eight lanes to LDS meet different banks: rows side by side in K, four rows and two pieces in V.
+    constexpr int ROWS = FP8 ? 64 / PIECES : 16;
+    const int wave_row = FP8 ? (wave * ROWS) & (kManyKeys - 1) : (wave >> 1) * 16;
+    const int k_row = wave_row + (lane & (ROWS - 1)), v_row = wave_row + (FP8 ? (lane & 3) + ((lane >> 3) & (ROWS / 4 - 1)) * 4 : lane >> 2);
+    const int k_piece = FP8 ? lane / ROWS : (wave & 1) * LOADS * 4 + (lane >> 4);
+    const int v_piece = FP8 ? ((lane >> 2) & 1) + (lane >> 3) / (ROWS / 4) * 2 : (wave & 1) * LOADS * 4 + (lane & 3);
+    const bool has_values = HALVES && wave >= kManyWaves / 2;
     // Where they are; rows that are not there: in page 0, taken out of the tile when it is used.  At `base` + `lane_off`.
     struct Place { int64_t base; uint32_t lane_off; };
-    const int wave_row = FP8 ? (wave * (64 / PIECES)) & (kManyKeys - 1) : (wave >> 1) * 16;
     const uint32_t k_lane_off = (k_row - wave_row) * (uint32_t)a.pool.s_tok + k_piece * 16, v_lane_off = (v_row - wave_row) * (uint32_t)a.pool.s_tok + v_piece * 16;
     auto place = [&](int tile, int row, int piece, uint32_t lane_off) __attribute__((always_inline)) {
       const int page = ROWWISE ? entry(tile, row) : uniform(entry(tile, wave_row));
@@ -231,8 +237,11 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
       if constexpr (ROWWISE) return Place{at + (unsigned)((tile * kManyKeys + row) & in_page) * (unsigned)a.pool.s_tok, (uint32_t)piece * 16};
       return Place{at + (unsigned)((tile * kManyKeys + wave_row) & in_page) * (unsigned)a.pool.s_tok, lane_off};
     };
-    auto k_place = [&](int tile) __attribute__((always_inline)) { return place(tile, k_row, k_piece, k_lane_off); };
+    auto k_place = [&](int tile) __attribute__((always_inline)) {
+      return has_values ? place(tile, v_row, v_piece, v_lane_off) : place(tile, k_row, k_piece, k_lane_off);
+    };
     auto v_place = [&](int tile, Place k) __attribute__((always_inline)) {
+      if constexpr (HALVES) return k;
       if constexpr (!ROWWISE) return Place{k.base, v_lane_off};
       return place(tile, v_row, v_piece, v_lane_off);
     };
@@ -252,16 +261,20 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
         }
       }
     };
-    auto fetch_keys = [&](int tile, Place at) __attribute__((always_inline)) { fetch(kr, lds_address(k_tile(tile)), kb, at); };
-    auto fetch_values = [&](int tile, Place at) __attribute__((always_inline)) { fetch(vr, lds_address(k_tile(tile)) + TILE, vb, at); };
-    auto park = [&](int tile) __attribute__((always_inline)) {                   // 8 bits
+    auto fetch_keys = [&](int tile, Place at) __attribute__((always_inline)) { fetch(kr, lds_address(k_tile(tile)), has_values ? vb : kb, at); };
+    auto fetch_values = [&](int tile, Place at) __attribute__((always_inline)) {
+      if constexpr (!HALVES) fetch(vr, lds_address(k_tile(tile)) + TILE, vb, at);
+    };
+    const int park_at = has_values ? TILE + At::value(v_row, 2 * v_piece) : At::key(k_row, 2 * k_piece);
+    const int park_at2 = has_values ? TILE + At::value(v_row, 2 * v_piece + 1) : At::key(k_row, 2 * k_piece + 1);
+    auto park = [&](int tile, int quarter) __attribute__((always_inline)) {      // 8 bits: a half of the piece of K, or of that of V
       if constexpr (FP8) {
-        if (kManyThreads / PIECES > kManyKeys && tid / PIECES >= kManyKeys) return;
         unsigned char* at = k_tile(tile);
-        *reinterpret_cast<u32x4*>(at + At::key(k_row, 2 * k_piece)) = widen8(kr.x, kr.y);
-        *reinterpret_cast<u32x4*>(at + At::key(k_row, 2 * k_piece + 1)) = widen8(kr.z, kr.w);
-        *reinterpret_cast<u32x4*>(at + TILE + At::value(v_row, 2 * v_piece)) = widen8(vr.x, vr.y);
-        *reinterpret_cast<u32x4*>(at + TILE + At::value(v_row, 2 * v_piece + 1)) = widen8(vr.z, vr.w);
+        if (quarter == 0) *reinterpret_cast<u32x4*>(at + park_at) = widen8(kr.x, kr.y);
+        if (quarter == 1) *reinterpret_cast<u32x4*>(at + park_at2) = widen8(kr.z, kr.w);
+        if constexpr (HALVES) return;
+        if (quarter == 2) *reinterpret_cast<u32x4*>(at + TILE + At::value(v_row, 2 * v_piece)) = widen8(vr.x, vr.y);
+        if (quarter == 3) *reinterpret_cast<u32x4*>(at + TILE + At::value(v_row, 2 * v_piece + 1)) = widen8(vr.z, vr.w);
       }
     };
     // The keys of a tile that there are; the tiles from `plain_end` on have keys that are not there, or that some rows do not see.
@@ -378,11 +391,11 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
       const Place from = k_place(tile0 + j);
       fetch_keys(tile0 + j, from);
       fetch_values(tile0 + j, v_place(tile0 + j, from));
-      if (j < 2) park(tile0 + j);
+      if (j < 2) { park(tile0 + j, 0); park(tile0 + j, 1); park(tile0 + j, 2); park(tile0 + j, 3); }
     }
     // in front of the first tile: values of zero
     for (int i = tid; i < HALF / 16; i += kManyThreads) *reinterpret_cast<u32x4*>(k_tile(tile0 + 3) + TILE + HALF + i * 16) = u32x4{0, 0, 0, 0};
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * LOADS) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(SENT) : "memory");
     uint64_t valid = ROWWISE ? is_there(tile0, entry(tile0, lane)) : 0;
     uint64_t held = ROWWISE ? 0 : __ballot(is_page(entries[(tile0 >> 4) & 3][lane]));          // groups of 16 keys of the stretch whose pages there are
     if (active) {
@@ -407,13 +420,13 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
       const unsigned char *t0 = k_tile(tile), *t1 = k_tile(tile + 1), *before = k_tile(tile + 3);
       // All of this step's LDS reads are on their way by the last places: from there on the tile before is nobody's, and the next one is everybody's.
       auto pass_on = [&](int f) __attribute__((always_inline)) {
-        if (f == F - (RING - 1)) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * LOADS + (ROWWISE ? 1 : 0)) : "memory");
+        if (f == F - (RING - 1)) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(SENT + (ROWWISE ? 1 : 0)) : "memory");
       };
       Place k_from = {0, 0}, v_from = {0, 0};
       int next_entry = 0;
       auto send_for = [&](int f) __attribute__((always_inline)) {
         if (ROWWISE && f == 0) next_entry = entry(tile + 1, lane);
-        if (f == 0) park(tile + 2);
+        if (f < 4) park(tile + 2, f);                            // before the next ones are sent for below
         if (f == 1) k_from = k_place(tile + 3);
         if (f == 2) v_from = v_place(tile + 3, k_from);
         if (f == 3) fetch_keys(tile + 3, k_from);
