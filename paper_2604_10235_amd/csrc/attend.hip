@@ -11,18 +11,18 @@ extern template int launch_many_of<64, true>(const ManyArgs&, hipStream_t);
 extern template int launch_many_of<128, false>(const ManyArgs&, hipStream_t);
 extern template int launch_many_of<128, true>(const ManyArgs&, hipStream_t);
 
-// Which kernel a request takes goes by its rows (new tokens x query heads per KV head).  Up to kFewRows it is attend_few_kernel's, which gives a
-// chunk of keys to a workgroup (28 query heads on 4 KV heads of 128 elements, us, few | many rows' kernel: 4 tokens over 8192 keys 15 | 23, over 131072 60 |
-// 72; the last has the better of it from a few GB on, 64 requests over 8192 keys 212 | 190, with weights of half the digits).  Up to kFewRowsMost two
-// workgroups share the rows and both read the keys, which pays while these are few (9 tokens over 8192 keys 19 | 24, over 32768 38 | 41, over 131072 92 |
-// 75; 64 requests over 8192 keys 353 | 191), and always from an 8-bit cache, whose rows cost the other kernel as much as 16-bit ones
-// (131072 keys 57 | 78; 64 requests 198 | 219).  Beyond, a third and a fourth workgroup never pay from 8000 keys on (18 tokens over 32768 keys 57 | 44).
+// Which kernel a request takes goes by its rows (new tokens x query heads per KV head; figures in us for 28 query heads on 4 KV heads of 128
+// elements, few | many rows' kernel).  Up to kFewRows it is attend_few_kernel's, which gives a chunk of keys to a workgroup: 4 tokens over 8192 keys 15 |
+// 23, over 131072 60 | 72; only from a few GB on the other is ahead (64 requests over 8192 keys 212 | 190), with weights of half the digits.  Up to
+// kFewRowsMost two workgroups share the rows and both read the keys, which pays while these are few: 9 tokens over 8192 keys 19 | 24, over 32768 38 | 41,
+// over 131072 92 | 75; 64 requests over 8192 keys 353 | 191; from an 8-bit cache 17 | 24, 31 | 39, 59 | 69, 205 | 185.  Beyond, a third and a fourth
+// workgroup do not pay from 8192 keys on (18 tokens over 32768 keys 57 | 44; over 2000 15 | 21).
 constexpr int kFewRows = 32, kFewRowsMost = 64;
-constexpr int64_t kFewKeysMost = 1 << 17;        // keys of all requests and KV heads, at their largest, up to which kFewRowsMost holds for bf16
+constexpr int64_t kFewKeysMost = 1 << 17;        // keys of all requests and KV heads, at their largest, up to which kFewRowsMost holds; 8 bits: eight times as many
 // In a batch with longer chunks, the short requests of a bf16 cache go along with them, with fewer launches and at the bandwidth that long ones have
 // (512 tokens over 4096 keys and 64 steps of one over 4096: 161 us apart, 138 together; 10 tokens and 64 steps over 16384: 399, 369).  From an 8-bit
-// cache only so many of them as the launches cost, in tiles of the many-row kernel (4 steps over 4096 keys 79 apart, 75 together; 8 of them 80, 85; 10
-// tokens and 64 steps over 16384 226, 422).
+// cache only so many of them as the launches cost, in tiles of the many-row kernel, which widens every tile for a whole block's rows (4 steps over 4096
+// keys 76 apart, 71 together; 8 of them 78, 79; 64 of them 114, 192).
 constexpr int64_t kAlongTiles = 1024;
 
 constexpr int64_t kMostFewBlocks = (1 << 24) - 1;
@@ -48,7 +48,7 @@ int make_attend_plan(const codecomp_batch* b, const codecomp_pages* p, AttendPla
       ++pl->few_rows;
       if (rows > few_most) few_most = (int)rows;
     }
-    if (few_most <= kFewRows || pl->pool.fp8 || (int64_t)pl->few_rows * x.Hkv * x.max_kv <= kFewKeysMost) break;
+    if (few_most <= kFewRows || (int64_t)pl->few_rows * x.Hkv * x.max_kv <= kFewKeysMost << (pl->pool.fp8 ? 3 : 0)) break;
     few_limit = kFewRows;
   }
   if (pl->many_rows > 0 && (!pl->pool.fp8 || (int64_t)pl->few_rows * x.Hkv * ((x.max_kv + kManyKeys - 1) / kManyKeys) <= kAlongTiles)) {

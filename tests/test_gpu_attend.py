@@ -78,6 +78,13 @@ def test_middle_sized_chunks_of_long_caches(news, fp8):
         check(rng, c, news, 8, max_kv=max_kv, causal=False)
 
 
+@pytest.mark.parametrize("news", [[9, 16], [1, 16]])
+def test_middle_sized_chunks_of_very_long_8_bit_caches(news):
+    rng = np.random.default_rng([25, news[0]])
+    c = cu_.Cache(rng, [1300, 140], n_kv=2, d=64, page=4096, fp8=True, width_more=200, k_scale=0.03, v_scale=0.02)
+    check(rng, c, news, 8, max_kv=700000)
+
+
 def test_many_tokens_of_one_prompt():
     """More blocks of rows than a workgroup has threads: 66000 tokens of two heads, which see few keys each."""
     rng = np.random.default_rng(21)
