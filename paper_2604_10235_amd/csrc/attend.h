@@ -17,6 +17,12 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // lose nothing in fp32 or in bf16, and most tiles then leave the sums and the outputs as they are.
 constexpr float kSlack = 8.0f;
 
+// What a workgroup leaves for the kernel that joins rows whose keys several workgroups had.
+struct CutBlock {
+  int32_t r, block, head;      // of the block of rows whose first part is this workgroup's (slot 2 * workgroup + 1); r < 0: none
+  int32_t last;                // last workgroup with a part of it (those after the first in slot 2 * workgroup)
+};
+
 struct AttendArgs {
   PagePool pool;
   PagedBatch b;
@@ -28,6 +34,8 @@ struct AttendArgs {
   int64_t layer;               // byte offset of the layer in the pool
   float c;                     // softmax_scale * k_scale * log2(e): logits in powers of two
   int chunk, splits, row_slots, row_parts;       // few rows: keys of a chunk, most chunks, most rows, workgroups that they are shared out to
+  int shares;                  // few rows: equal parts that all keys are cut into; 0: chunks
+  CutBlock* cuts;              // [shares]
 };
 
 // The same in all lanes, and known to be: in scalar registers.
@@ -51,20 +59,16 @@ __device__ __forceinline__ u32x4 widen8(unsigned a, unsigned b) {
   return r;
 }
 
-// A 16-byte piece with zeros for its infinities and NaN (E4M3 has no infinity); `any`: whether there were some.
+// A 16-byte piece with zeros for its infinities and NaN (E4M3 has no infinity); `any`: not 0 where there were some.  Their exponents are all ones
+// (E4M3: all bits but the sign), to which one at the bottom makes a carry into the sign's place.
 template <bool FP8>
-__device__ __forceinline__ u32x4 finite_part(u32x4 v, bool& any) {
+__device__ __forceinline__ u32x4 finite_part(u32x4 v, unsigned& any) {
+  constexpr unsigned ONES = FP8 ? 0x7F7F7F7Fu : 0x7F807F80u, ONE = FP8 ? 0x01010101u : 0x00800080u, SIGNS = FP8 ? 0x80808080u : 0x80008000u;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    unsigned mask = 0;
-    if constexpr (FP8) {
-#pragma unroll
-      for (int j = 0; j < 32; j += 8) mask |= ((v[i] >> j) & 0x7Fu) == 0x7Fu ? 0xFFu << j : 0u;
-    } else {
-      mask = ((v[i] & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((v[i] & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
-    }
-    any |= mask != 0;
-    v[i] &= ~mask;
+    const unsigned found = ((v[i] & ONES) + ONE) & SIGNS;
+    any |= found;
+    v[i] &= ~((found >> (FP8 ? 7 : 15)) * (FP8 ? 0xFFu : 0xFFFFu));
   }
   return v;
 }
@@ -94,6 +98,6 @@ __device__ __forceinline__ s16x4 read_columns(const unsigned char* lds) {
   return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)lds);
 }
 
-int launch_few(const AttendPlan& pl, AttendArgs a, hipStream_t stream);
+int launch_few(const AttendPlan& pl, const AttendArgs& a, hipStream_t stream);
 
 }  // namespace codecomp

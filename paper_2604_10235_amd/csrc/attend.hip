@@ -25,6 +25,12 @@ constexpr int64_t kFewKeysMost = 1 << 17;        // keys of all requests and KV 
 // keys 76 apart, 71 together; 8 of them 78, 79; 64 of them 114, 192).
 constexpr int64_t kAlongTiles = 1024;
 
+// Cache bytes (at the largest lengths) from which the keys of several requests of few rows are cut into equal parts instead of chunks: all workgroups
+// run at once and end together, for 5 us more before the first key and for the parts (64 steps over 500 .. 16384 keys, 4 KV heads of 128: 210 us in
+// chunks, 190 in parts; 8 bits 118, 103; 16 over 300 .. 9000 45, 37, 8 bits 25.7, 25.9; 64 over 8192 192, 196; one over 131072 57, 64).  Two workgroups
+// per compute unit: with three or four 195 and 198.
+constexpr int64_t kEvenBytes = 1 << 28;
+constexpr int kShares = 512;
 constexpr int64_t kMostFewBlocks = (1 << 24) - 1;
 // Tiles of the longest block of rows up to which blocks are not shared by workgroups: no parts to be joined (a prompt of 500 tokens 27 us, 32 with
 // sharing; of 100 19, 23).
@@ -76,9 +82,12 @@ int make_attend_plan(const codecomp_batch* b, const codecomp_pages* p, AttendPla
   pl->chunk = (int)chunk;
   pl->splits = x.max_kv > chunk ? (int)((x.max_kv + chunk - 1) / chunk) : 1;
   if (pl->few_rows > 0 && (items * pl->row_parts > kMostFewBlocks || items * pl->row_slots > kMostFewBlocks)) return CODECOMP_EINVAL_SHAPE;
+  const int64_t bytes = (int64_t)pl->few_rows * x.Hkv * x.max_kv * p->head_dim * (pl->pool.fp8 ? 2 : 4);
+  pl->shares = pl->few_rows > 1 && pl->row_parts == 1 && bytes > kEvenBytes ? kShares : 0;
   size_t off = 0;
   pl->off_few = off;
-  if (pl->few_rows > 0 && pl->splits > 1) off = align256(off + (size_t)(items * pl->splits * pl->row_slots) * (p->head_dim + 2) * sizeof(float));
+  if (pl->shares > 0) off = align256(off + (size_t)pl->shares * (2 * (size_t)pl->row_slots * (p->head_dim + 2) * sizeof(float) + sizeof(CutBlock)));
+  else if (pl->few_rows > 0 && pl->splits > 1) off = align256(off + (size_t)(items * pl->splits * pl->row_slots) * (p->head_dim + 2) * sizeof(float));
   pl->off_many = off;
   pl->workgroups = 256;
   pl->many_whole = x.max_kv <= kWholeTiles * kManyKeys;
@@ -147,10 +156,12 @@ int launch_attend(const AttendPlan& pl, const void* q, int layer, void* out, flo
   a.pool = pl.pool; a.b = pl.batch; a.q = static_cast<const uint16_t*>(q); a.out = static_cast<uint16_t*>(out); a.lse = lse;
   a.layer = layer * pl.pool.s_layer;
   a.c = fminf(fmaxf(pl.scale * pl.pool.k_scale * kLog2e, FLT_MIN), FLT_MAX);       // a hidden logit of minus infinity times it stays one
-  a.chunk = pl.chunk; a.splits = pl.splits; a.row_slots = pl.row_slots; a.row_parts = pl.row_parts;
+  a.chunk = pl.chunk; a.splits = pl.splits; a.row_slots = pl.row_slots; a.row_parts = pl.row_parts; a.shares = pl.shares;
   if (pl.few_rows > 0) {
     a.part_o = reinterpret_cast<float*>(static_cast<char*>(workspace) + pl.off_few);
-    a.part_ml = a.part_o + (size_t)pl.batch.n_seqs * pl.batch.Hkv * pl.splits * pl.row_slots * pl.d;
+    const size_t parts = (pl.shares > 0 ? 2 * (size_t)pl.shares : (size_t)pl.batch.n_seqs * pl.batch.Hkv * pl.splits) * pl.row_slots;
+    a.part_ml = a.part_o + parts * pl.d;
+    a.cuts = reinterpret_cast<CutBlock*>(a.part_ml + parts * 2);
     if (int rc = launch_few(pl, a, stream)) return rc;
   }
   if (pl.many_rows > 0)

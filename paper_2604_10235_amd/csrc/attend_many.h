@@ -12,12 +12,6 @@ namespace codecomp {
 
 constexpr int kManyRows = 256, kManyKeys = 64, kManyWaves = 8, kManyThreads = 64 * kManyWaves;
 
-// What a workgroup leaves for the kernel that joins blocks of rows whose keys several workgroups share.
-struct CutBlock {
-  int32_t r, block, head;      // of the block whose first part is this workgroup's (slot 2 * workgroup + 1); r < 0: none
-  int32_t last;                // last workgroup with a part of it (those after the first in slot 2 * workgroup)
-};
-
 // Positions in front of the tiles of a block, in the sequence that is cut into equal parts: starting on a block (its queries, the first tiles) costs
 // about as much as that many tiles.
 constexpr int kManyLead = 7;
@@ -284,7 +278,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
     // Values of a tile that has keys that are not there, or that some rows do not see: a weight of zero must not meet what stands in the one, nor an
     // infinite or NaN value in the other (added at the end, to the rows that see them).
     auto clean_values = [&](int tile, uint64_t valid) __attribute__((always_inline)) {
-      bool any = false;
+      unsigned any = 0;
       for (int i = tid; i < TILE / 16; i += kManyThreads) {
         u32x4* at = reinterpret_cast<u32x4*>(k_tile(tile) + TILE + i * 16);
         u32x4 v = *at;
@@ -292,7 +286,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
         if (partly(tile)) v = finite_part<false>(v, any);
         *at = v;
       }
-      if (any) not_finite = 1;
+      if (any != 0) not_finite = 1;
     };
 
     f32x16 o[DB];

@@ -64,7 +64,8 @@ struct AttendPlan {
   float scale;
   int few_rows, many_rows;     // requests of each kind (attend.hip)
   int row_slots, row_parts;    // few rows: rows of the largest, workgroups that they are shared out to
-  int chunk, splits;           // few rows: keys of a workgroup, and workgroups per request and head
+  int chunk, splits;           // few rows: keys of a workgroup, and workgroups per request and head,
+  int shares;                  // or (not 0) equal parts of the keys of all requests and heads, one for each workgroup
   int workgroups, many_from, many_blocks, many_whole;        // many rows: workgroups, rows from which a request is of this kind, blocks of rows, none of them shared
   size_t off_few, off_many, ws_bytes;
 };

@@ -67,6 +67,20 @@ def test_shares(lens, news, n_q, n_kv, d, page):
     check(rng, c, news, n_q)
 
 
+# Requests of few rows whose bound on lengths makes the batch a large one: keys of all of them cut into equal parts, which end inside requests, hold
+# several, or are less than 128 keys; requests without keys or tokens, more of them than a workgroup has threads, pages that are not held.
+@pytest.mark.parametrize("lens, news, n_q, n_kv, d, fp8", [
+    ([1300, 140, 16], [1, 1, 1], 8, 2, 128, False), ([1300, 140, 16], [4, 1, 3], 8, 1, 128, False), ([40000, 3, 0, 517, 30000], [1, 1, 1, 0, 1], 4, 2, 64, False),
+    ([40000, 3, 0, 517, 30000], [2, 2, 2, 0, 4], 14, 2, 128, True), ([0, 0, 0], [1, 2, 1], 4, 2, 64, True), ([65000, 900], [1, 1], 7, 1, 128, False),
+    ([5, 300, 0, 129] * 160, [1, 0, 1, 1] * 160, 2, 1, 64, True)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_equal_parts(lens, news, n_q, n_kv, d, fp8, causal):
+    rng = np.random.default_rng([26, len(lens), d])
+    c = cu_.Cache(rng, lens, n_kv=n_kv, d=d, page=256, fp8=fp8, width_more=6000, k_scale=0.03 if fp8 else 1.0, v_scale=0.02 if fp8 else 1.0)
+    c.table[0, 2:4] = [-1, c.n_pages]
+    check(rng, c, news, n_q, causal=causal, weight_bits=16, max_kv=1 << 20)
+
+
 # 33 .. 64 rows, alone and beside single tokens, where the bound on lengths makes the batch a small one and a large one.
 @pytest.mark.parametrize("news", [[9, 0, 16], [9, 1, 16], [1, 2, 5], [13, 1, 3]])
 @pytest.mark.parametrize("fp8", [False, True])
