@@ -1,5 +1,9 @@
 // Rows between dense caches and pages, and whole pages: copies of 16-byte pieces, bit for bit.  Bound by memory; K and V go together, since a
-// row's two places are found once.
+// row's two places are found once.  One piece of each in flight per thread and many threads are enough (two rows a thread: store 4.3 GB 742 -> 794
+// us; whole pages, 350 MB, one piece 62, two 64, four 73), and stores go past the caches, which could not hold the rows until they are read (store 760 ->
+// 740 us, pages 70 -> 64).
+// Measured: 4.3 GB from dense rows into pages of 16 rows 740 us, 5.8 TB/s (a large copy reaches 5.0); 236 MB of kept rows from pages to pages 47 us,
+// 5.0; 350 MB of whole pages 62 us, 5.7.
 #include "cache.h"
 
 namespace codecomp {
@@ -8,7 +12,6 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kMoveThreads = 256;
 constexpr int64_t kMostBlocks = (1 << 24) - 1;         // of 256 threads: an axis of a grid holds 2^32 threads
-constexpr int kMoveRows = 2;          // rows of K and of V that a thread has in flight
 
 // Byte offset of a request's row; -1 where there is none.
 template <bool PAGED>
@@ -24,41 +27,30 @@ __device__ __forceinline__ int64_t place(const RowSide& s, int r, int64_t row) {
 // blockIdx.x: rows of all requests, blockIdx.y: (layer, head).  Consecutive threads take the pieces of a row.
 template <bool FROM_PAGES, bool TO_PAGES>
 __global__ __launch_bounds__(kMoveThreads) void move_kernel(const MoveArgs a) {
-  const int per_pass = kMoveThreads >> a.pieces_log2;
-  const int first = blockIdx.x * per_pass * kMoveRows, at = first + (threadIdx.x >> a.pieces_log2);
+  const int first = blockIdx.x * (kMoveThreads >> a.pieces_log2), row = first + (threadIdx.x >> a.pieces_log2);
   const int layer = blockIdx.y / a.Hkv, head = blockIdx.y - layer * a.Hkv;
   const int64_t in_row = (threadIdx.x & ((1 << a.pieces_log2) - 1)) * 16;
-  const int64_t from0 = layer * a.from.s_layer + head * a.from.s_head + in_row, to0 = layer * a.to.s_layer + head * a.to.s_head + in_row;
   int r = request_of(a.cu_rows, a.n_seqs, first);          // the rows of a workgroup walk forward from there
-  int64_t to[kMoveRows];
-  u32x4 k[kMoveRows], v[kMoveRows];
-#pragma unroll
-  for (int i = 0; i < kMoveRows; ++i) {
-    const int row = at + i * per_pass;
-    to[i] = -1;
-    if (row >= a.rows) continue;
-    while (r + 1 < a.n_seqs && a.cu_rows[r + 1] <= row) ++r;
-    const int in_request = row - a.cu_rows[r];
-    int64_t source = in_request;
-    if (a.idx) source = min(max(a.idx[(int64_t)blockIdx.y * a.rows + row], 0), a.cu_source[r + 1] - a.cu_source[r] - 1);
-    const int64_t from = place<FROM_PAGES>(a.from, r, source);
-    to[i] = place<TO_PAGES>(a.to, r, in_request);
-    k[i] = v[i] = u32x4{0, 0, 0, 0};
-    if (from >= 0 && to[i] >= 0) {
-      k[i] = *reinterpret_cast<const u32x4*>(a.from.k + from0 + from);
-      v[i] = *reinterpret_cast<const u32x4*>(a.from.v + from0 + from);
-    }
+  if (row >= a.rows) return;
+  while (r + 1 < a.n_seqs && a.cu_rows[r + 1] <= row) ++r;
+  const int in_request = row - a.cu_rows[r];
+  int64_t source = in_request;
+  if (a.idx) source = min(max(a.idx[(int64_t)blockIdx.y * a.rows + row], 0), a.cu_source[r + 1] - a.cu_source[r] - 1);
+  const int64_t from = place<FROM_PAGES>(a.from, r, source), to = place<TO_PAGES>(a.to, r, in_request);
+  if (to < 0) return;
+  u32x4 k = {0, 0, 0, 0}, v = {0, 0, 0, 0};
+  if (from >= 0) {
+    const int64_t at = layer * a.from.s_layer + head * a.from.s_head + in_row + from;
+    k = *reinterpret_cast<const u32x4*>(a.from.k + at);
+    v = *reinterpret_cast<const u32x4*>(a.from.v + at);
   }
-#pragma unroll
-  for (int i = 0; i < kMoveRows; ++i)
-    if (to[i] >= 0) {
-      *reinterpret_cast<u32x4*>(a.to.k + to0 + to[i]) = k[i];
-      *reinterpret_cast<u32x4*>(a.to.v + to0 + to[i]) = v[i];
-    }
+  const int64_t at = layer * a.to.s_layer + head * a.to.s_head + in_row + to;
+  __builtin_nontemporal_store(k, reinterpret_cast<u32x4*>(a.to.k + at));
+  __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(a.to.v + at));
 }
 
 int launch_move(const MoveArgs& a, int problems, hipStream_t stream) {
-  const int64_t per_block = (kMoveThreads >> a.pieces_log2) * kMoveRows, blocks = (a.rows + per_block - 1) / per_block;
+  const int64_t per_block = kMoveThreads >> a.pieces_log2, blocks = (a.rows + per_block - 1) / per_block;
   if (blocks > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
   const dim3 grid((unsigned)blocks, problems), block(kMoveThreads);
   if (a.from.table && a.to.table) move_kernel<true, true><<<grid, block, 0, stream>>>(a);
@@ -66,8 +58,6 @@ int launch_move(const MoveArgs& a, int problems, hipStream_t stream) {
   else move_kernel<false, true><<<grid, block, 0, stream>>>(a);
   return (int)hipGetLastError();
 }
-
-constexpr int kCopyPieces = 4;        // 16-byte pieces of K and of V that a thread has in flight
 
 struct CopyArgs {
   PagePool pool;
@@ -81,24 +71,13 @@ __global__ __launch_bounds__(kMoveThreads) void copy_kernel(const CopyArgs a) {
   const int from = a.pairs[2 * (int64_t)pair], to = a.pairs[2 * (int64_t)pair + 1];
   if (from < 0 || from >= a.pool.n_pages || to < 0 || to >= a.pool.n_pages || from == to) return;
   const int64_t layer = blockIdx.y * a.pool.s_layer, source = layer + from * a.pool.s_page, target = layer + to * a.pool.s_page;
-  int64_t off[kCopyPieces];
-  u32x4 k[kCopyPieces], v[kCopyPieces];
-#pragma unroll
-  for (int i = 0; i < kCopyPieces; ++i) {
-    const int piece = (share * kCopyPieces + i) * kMoveThreads + threadIdx.x;
-    off[i] = -1;
-    if (piece >= a.pieces) continue;
-    const int head = piece >> a.page_log2, row = (piece & ((1 << a.page_log2) - 1)) >> a.row_log2;
-    off[i] = head * a.pool.s_head + row * a.pool.s_tok + (piece & ((1 << a.row_log2) - 1)) * 16;
-    k[i] = *reinterpret_cast<const u32x4*>(a.pool.k + source + off[i]);
-    v[i] = *reinterpret_cast<const u32x4*>(a.pool.v + source + off[i]);
-  }
-#pragma unroll
-  for (int i = 0; i < kCopyPieces; ++i)
-    if (off[i] >= 0) {
-      *reinterpret_cast<u32x4*>(a.pool.k + target + off[i]) = k[i];
-      *reinterpret_cast<u32x4*>(a.pool.v + target + off[i]) = v[i];
-    }
+  const int piece = share * kMoveThreads + threadIdx.x;
+  if (piece >= a.pieces) return;
+  const int head = piece >> a.page_log2, row = (piece & ((1 << a.page_log2) - 1)) >> a.row_log2;
+  const int64_t off = head * a.pool.s_head + row * a.pool.s_tok + (piece & ((1 << a.row_log2) - 1)) * 16;
+  const u32x4 k = *reinterpret_cast<const u32x4*>(a.pool.k + source + off), v = *reinterpret_cast<const u32x4*>(a.pool.v + source + off);
+  __builtin_nontemporal_store(k, reinterpret_cast<u32x4*>(a.pool.k + target + off));
+  __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(a.pool.v + target + off));
 }
 
 int launch_pages_copy(const PagePool& pool, int L, int Hkv, int d, const int32_t* pairs, int n_pairs, hipStream_t stream) {
@@ -106,7 +85,7 @@ int launch_pages_copy(const PagePool& pool, int L, int Hkv, int d, const int32_t
   a.pool = pool; a.pairs = pairs;
   a.row_log2 = (d == 128 ? 4 : 3) - (pool.fp8 ? 1 : 0);
   a.page_log2 = pool.page_log2 + a.row_log2;
-  const int64_t pieces = (int64_t)Hkv << a.page_log2, per_block = kMoveThreads * kCopyPieces;
+  const int64_t pieces = (int64_t)Hkv << a.page_log2, per_block = kMoveThreads;
   if (pieces > INT32_MAX - per_block) return CODECOMP_EINVAL_SHAPE;
   a.pieces = (int)pieces;
   a.blocks = (int)((pieces + per_block - 1) / per_block);
