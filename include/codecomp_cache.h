@@ -150,8 +150,7 @@ size_t codecomp_attend_workspace_bytes(const codecomp_batch* batch, const codeco
  * lse[t][h] = ln sum_j exp(softmax_scale * q . k_j) (f32, dense [T][n_q_heads]; may be NULL): two caches attended to apart are joined with it.
  * A token that sees no row (or rows of pages that are not held alone) gets out = 0, lse = -inf.  What stands in rows that a token
  * does not see, NaN and infinities too, has no part in its result.  Logits, sums and outputs are fp32; the weights enter the second
- * product rounded to bf16, or as two bf16, 16 bits together, where all requests of the batch have up to 32 rows (new tokens * query heads per KV
- * head), and up to 64 where n_seqs * n_kv_heads * max_kv_len is at most 2^17 (in an FP8 cache 2^20).
+ * product rounded to bf16, or as two bf16, 16 bits together, where all requests of the batch have up to 64 rows (new tokens * query heads per KV head).
  * workspace: >= codecomp_attend_workspace_bytes(), 256-byte aligned, contents on entry do not matter; NULL when that is 0.
  * Calls that may run at the same time need workspaces of their own. */
 int codecomp_attend(const void* q, const codecomp_batch* batch, const codecomp_pages* pages, int32_t layer, void* out, float* lse,

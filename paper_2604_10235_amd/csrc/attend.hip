@@ -6,19 +6,22 @@
 
 namespace codecomp {
 
-extern template int launch_many_of<64, false>(const ManyArgs&, hipStream_t);
-extern template int launch_many_of<64, true>(const ManyArgs&, hipStream_t);
-extern template int launch_many_of<128, false>(const ManyArgs&, hipStream_t);
-extern template int launch_many_of<128, true>(const ManyArgs&, hipStream_t);
+extern template int launch_many_of<64, false, false>(const ManyArgs&, hipStream_t);
+extern template int launch_many_of<64, false, true>(const ManyArgs&, hipStream_t);
+extern template int launch_many_of<64, true, false>(const ManyArgs&, hipStream_t);
+extern template int launch_many_of<128, false, false>(const ManyArgs&, hipStream_t);
+extern template int launch_many_of<128, false, true>(const ManyArgs&, hipStream_t);
+extern template int launch_many_of<128, true, false>(const ManyArgs&, hipStream_t);
 
 // Which kernel a request takes goes by its rows (new tokens x query heads per KV head; figures in us for 28 query heads on 4 KV heads of 128
 // elements, few | many rows' kernel).  Up to kFewRows it is attend_few_kernel's, which gives a chunk of keys to a workgroup: 4 tokens over 8192 keys 15 |
-// 23, over 131072 60 | 72; only from a few GB on the other is ahead (64 requests over 8192 keys 212 | 190), with weights of half the digits.  Up to
-// kFewRowsMost two workgroups share the rows and both read the keys, which pays while these are few: 9 tokens over 8192 keys 19 | 24, over 32768 38 | 41,
-// over 131072 92 | 75; 64 requests over 8192 keys 353 | 191; from an 8-bit cache 17 | 24, 31 | 39, 59 | 69, 205 | 185.  Beyond, a third and a fourth
-// workgroup do not pay from 8192 keys on (18 tokens over 32768 keys 57 | 44; over 2000 15 | 21).
+// 23, over 131072 60 | 72; only from a few GB on the other is ahead (64 requests over 8192 keys 212 | 190).  Up to kFewRowsMost two workgroups share the
+// rows and both read the keys, which pays while these are few: 9 tokens over 8192 keys 19 | 24, over 32768 38 | 41, over 131072 92 | 76; 64 requests
+// over 8192 keys 353 | 204; and always from an 8-bit cache: 17 | 24, 31 | 39, 59 | 69, 205 | 205.  Beyond, a third and a fourth workgroup do not pay
+// from 8192 keys on (18 tokens over 32768 keys 57 | 44; over 2000 15 | 21).  Up to kFewRowsMost, weights enter the product as two bf16 in either kernel
+// (the many-row one with rounded ones: 64 requests 191).
 constexpr int kFewRows = 32, kFewRowsMost = 64;
-constexpr int64_t kFewKeysMost = 1 << 17;        // keys of all requests and KV heads, at their largest, up to which kFewRowsMost holds; 8 bits: eight times as many
+constexpr int64_t kFewKeysMost = 1 << 17;        // keys of all requests and KV heads, at their largest, up to which kFewRowsMost holds for bf16
 // In a batch with longer chunks, the short requests of a bf16 cache go along with them, with fewer launches and at the bandwidth that long ones have
 // (512 tokens over 4096 keys and 64 steps of one over 4096: 161 us apart, 138 together; 10 tokens and 64 steps over 16384: 399, 369).  From an 8-bit
 // cache only so many of them as the launches cost, in tiles of the many-row kernel, which widens every tile for a whole block's rows (4 steps over 4096
@@ -54,7 +57,7 @@ int make_attend_plan(const codecomp_batch* b, const codecomp_pages* p, AttendPla
       ++pl->few_rows;
       if (rows > few_most) few_most = (int)rows;
     }
-    if (few_most <= kFewRows || (int64_t)pl->few_rows * x.Hkv * x.max_kv <= kFewKeysMost << (pl->pool.fp8 ? 3 : 0)) break;
+    if (few_most <= kFewRows || pl->pool.fp8 || (int64_t)pl->few_rows * x.Hkv * x.max_kv <= kFewKeysMost) break;
     few_limit = kFewRows;
   }
   if (pl->many_rows > 0 && (!pl->pool.fp8 || (int64_t)pl->few_rows * x.Hkv * ((x.max_kv + kManyKeys - 1) / kManyKeys) <= kAlongTiles)) {
@@ -63,8 +66,10 @@ int make_attend_plan(const codecomp_batch* b, const codecomp_pages* p, AttendPla
   }
   pl->many_from = pl->few_rows > 0 ? few_limit + 1 : 1;
   int64_t blocks = 0;
+  pl->many_fine = !pl->pool.fp8;       // (an 8-bit cache's requests of up to 64 rows are the other kernel's)
   for (int r = 0; r < x.n_seqs; ++r) {
     const int64_t rows = (int64_t)(b->cu_q_host[r + 1] - b->cu_q_host[r]) * x.G;
+    if (rows > kFewRowsMost) pl->many_fine = 0;
     if (rows >= pl->many_from) blocks += (rows + kManyRows - 1) / kManyRows;
   }
   pl->many_blocks = blocks * x.Hkv < INT32_MAX ? (int)(blocks * x.Hkv) : INT32_MAX;
@@ -139,8 +144,12 @@ static int launch_many(const AttendPlan& pl, const AttendArgs& a, char* workspac
   m.a.part_ml = m.a.part_o + (size_t)pl.workgroups * 2 * kManyRows * pl.d;
   m.cuts = reinterpret_cast<CutBlock*>(m.a.part_ml + (size_t)pl.workgroups * 2 * kManyRows * 2);
   int rc;
-  if (pl.d == 128) rc = pl.pool.fp8 ? launch_many_of<128, true>(m, stream) : launch_many_of<128, false>(m, stream);
-  else rc = pl.pool.fp8 ? launch_many_of<64, true>(m, stream) : launch_many_of<64, false>(m, stream);
+  if (pl.many_fine) {
+    rc = pl.d == 128 ? launch_many_of<128, false, true>(m, stream) : launch_many_of<64, false, true>(m, stream);
+  } else {
+    if (pl.d == 128) rc = pl.pool.fp8 ? launch_many_of<128, true, false>(m, stream) : launch_many_of<128, false, false>(m, stream);
+    else rc = pl.pool.fp8 ? launch_many_of<64, true, false>(m, stream) : launch_many_of<64, false, false>(m, stream);
+  }
   if (rc || pl.many_whole) return rc;
   // A few blocks of many parts: their rows over more workgroups (20 tokens over 131072 keys 83 us, 16 rows each 96, 64 rows each 213); many blocks of
   // a part or two: fewer workgroups (12 x 1024 tokens over 4096 keys, head_dim 64: 8 rows each 125, 16 124).

@@ -63,7 +63,8 @@ struct TileAt {
 };
 
 // ROWWISE: pages of less than 16 rows; else the 16 rows that a wave loads of a tile lie in one page, whose place is worked out in scalar registers.
-template <int D, bool FP8, bool ROWWISE>
+// FINE: weights as two bf16.
+template <int D, bool FP8, bool ROWWISE, bool FINE>
 __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const ManyArgs ma) {
   const AttendArgs& a = ma.a;
   constexpr int PIECES = D * (FP8 ? 1 : 2) / 16;               // 16-byte pieces of a stored row
@@ -296,7 +297,14 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[db][i] = 0.0f;
     f32x16 za, zb;                                               // logits of the first and of the second 32 keys of a tile
-    u32x4 pa[2], pb[2] = {u32x4{0, 0, 0, 0}, u32x4{0, 0, 0, 0}}; // their weights, 16 keys each
+    struct Weights {                                             // their weights, 16 keys each; FINE: rounded, and the rest
+      u32x4 p[2], rest[FINE ? 2 : 1];
+    } pa, pb = {};
+    auto pack = [&](Weights& to, int i, float x, float y) __attribute__((always_inline)) {      // of logits i and i + 1
+      const unsigned p = pack2(x, y);
+      to.p[i >> 3][(i & 7) >> 1] = p;
+      if constexpr (FINE) to.rest[i >> 3][(i & 7) >> 1] = pack2(x - __uint_as_float(p << 16), y - __uint_as_float(p & 0xFFFF0000u));
+    };
 
     // Key fragment f (16 of a row's elements of 32 keys), value fragment f (32 columns of 16 keys).
     const int k_lane = At::key(l32, half), v_lane = At::value(half * 4 + ((lane >> 2) & 3), 0) + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
@@ -315,7 +323,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
     // the logits zn of the next 32 keys (kt) and the outputs of the 32 before (vt), whose weights are pp.  The order is the source's: the LDS read that
     // the MFMA three further on needs (from the next step's tiles at the end), an MFMA, the vector work of a logit (two at head_dim 64), and
     // what `beside` has for this place.
-    auto step = [&](f32x16& z, u32x4 (&p)[2], f32x16& zn, const unsigned char* kt, const u32x4 (&pp)[2], const unsigned char* vt, const unsigned char* kt_next,
+    auto step = [&](f32x16& z, Weights& p, f32x16& zn, const unsigned char* kt, const Weights& pp, const unsigned char* vt, const unsigned char* kt_next,
                     const unsigned char* vt_next, int key0, bool masked, unsigned valid, auto&& beside) __attribute__((always_inline)) {
       if (__builtin_expect(masked, 0)) {
 #pragma unroll
@@ -334,20 +342,23 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
         if (f + RING - 1 < F) fill(f + RING - 1, kt, vt);
         else fill(f + RING - 1 - F, kt_next, vt_next);
         const int i = f / 2;
-        if (f & 1) o[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(ring[f % RING]), frag(pp[i / DB]), o[i % DB], 0, 0, 0);
-        else zn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(ring[f % RING]), frag(qf[i]), zn, 0, 0, 0);
+        if (f & 1) {
+          o[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(ring[f % RING]), frag(pp.p[i / DB]), o[i % DB], 0, 0, 0);
+          if constexpr (FINE) o[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(ring[f % RING]), frag(pp.rest[i / DB]), o[i % DB], 0, 0, 0);
+        } else zn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(ring[f % RING]), frag(qf[i]), zn, 0, 0, 0);
 #pragma unroll
         for (int e = f * PER; e < (f + 1) * PER; ++e) {
           w[e] = __builtin_amdgcn_exp2f(fmaf(z[e], a.c, -m));
           if (e > 0) sum += w[e - 1];
-          if (e > 1 && (e & 1) == 0) p[(e - 2) >> 3][((e - 2) & 7) >> 1] = pack2(w[e - 2], w[e - 1]);
+          if (e > 1 && (e & 1) == 0) pack(p, e - 2, w[e - 2], w[e - 1]);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
       sum += w[15];
-      p[1][3] = pack2(w[14], w[15]);
+      pack(p, 14, w[14], w[15]);
       // here, beside the MFMAs, not behind the branch
-      asm volatile("" ::"v"(sum), "v"(p[0][0]), "v"(p[0][1]), "v"(p[0][2]), "v"(p[0][3]), "v"(p[1][0]), "v"(p[1][1]), "v"(p[1][2]), "v"(p[1][3]));
+      asm volatile("" ::"v"(sum), "v"(p.p[0]), "v"(p.p[1]));
+      if constexpr (FINE) asm volatile("" ::"v"(p.rest[0]), "v"(p.rest[1]));
       // A logit far above its row's reference: move the references.  (Weights are positive: none is larger than their sum, and as
       // long as that is below 4096 nothing is lost in fp32 or bf16.)
       if (__builtin_expect(__ballot(sum > 4096.0f) != 0, 0)) {
@@ -368,7 +379,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
         for (int i = 0; i < 16; i += 2) {
           const float x = __builtin_amdgcn_exp2f(fmaf(z[i], a.c, -m)), y = __builtin_amdgcn_exp2f(fmaf(z[i + 1], a.c, -m));
           sum += x + y;
-          p[i >> 3][(i & 7) >> 1] = pack2(x, y);
+          pack(p, i, x, y);
         }
       }
       l += sum;
@@ -441,7 +452,11 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
     if (active) {
 #pragma unroll
       for (int f = 0; f < KS; ++f)
-        o[f % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(value_frag(k_tile(tile1 + 3) + TILE + HALF, f)), frag(pb[f / DB]), o[f % DB], 0, 0, 0);
+        {
+          const bf16x8 v = frag(value_frag(k_tile(tile1 + 3) + TILE + HALF, f));
+          o[f % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, frag(pb.p[f / DB]), o[f % DB], 0, 0, 0);
+          if constexpr (FINE) o[f % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, frag(pb.rest[f / DB]), o[f % DB], 0, 0, 0);
+        }
       if (__builtin_expect(partly(tile1 - 1) && not_finite != 0, 0)) {
         for (int key = max(seen_by_all, tile0 * kManyKeys); key < min(of.len, tile1 * kManyKeys); ++key) {
           const int at = table[key >> a.pool.page_log2];
@@ -493,10 +508,10 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
   if (tid == 0 && !ma.whole) ma.cuts[g] = cut;
 }
 
-template <int D, bool FP8>
+template <int D, bool FP8, bool FINE>
 int launch_many_of(const ManyArgs& m, hipStream_t stream) {
-  if (m.a.pool.page_log2 < 4) attend_many_kernel<D, FP8, true><<<dim3(m.workgroups), dim3(kManyThreads), 0, stream>>>(m);
-  else attend_many_kernel<D, FP8, false><<<dim3(m.workgroups), dim3(kManyThreads), 0, stream>>>(m);
+  if (m.a.pool.page_log2 < 4) attend_many_kernel<D, FP8, true, FINE><<<dim3(m.workgroups), dim3(kManyThreads), 0, stream>>>(m);
+  else attend_many_kernel<D, FP8, false, FINE><<<dim3(m.workgroups), dim3(kManyThreads), 0, stream>>>(m);
   return (int)hipGetLastError();
 }
 

@@ -1,0 +1,5 @@
+#include "attend_many.h"
+
+namespace codecomp {
+template int launch_many_of<128, false, true>(const ManyArgs&, hipStream_t);
+}

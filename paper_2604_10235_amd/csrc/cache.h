@@ -66,7 +66,8 @@ struct AttendPlan {
   int row_slots, row_parts;    // few rows: rows of the largest, workgroups that they are shared out to
   int chunk, splits;           // few rows: keys of a workgroup, and workgroups per request and head,
   int shares;                  // or (not 0) equal parts of the keys of all requests and heads, one for each workgroup
-  int workgroups, many_from, many_blocks, many_whole;        // many rows: workgroups, rows from which a request is of this kind, blocks of rows, none of them shared
+  int workgroups, many_from, many_blocks;        // many rows: workgroups, rows from which a request is of this kind, blocks of rows,
+  int many_whole, many_fine;   // none of them shared, weights as two bf16
   size_t off_few, off_many, ws_bytes;
 };
 int make_attend_plan(const codecomp_batch* b, const codecomp_pages* p, AttendPlan* plan);

@@ -92,6 +92,17 @@ def test_middle_sized_chunks_of_long_caches(news, fp8):
         check(rng, c, news, 8, max_kv=max_kv, causal=False)
 
 
+# Up to 64 rows have weights of 16 bits whatever kernel they take.
+@pytest.mark.parametrize("news, n_q, d", [([9, 1, 16], 8, 128), ([13, 1, 3], 8, 64), ([64, 2, 16], 2, 64), ([9, 2, 9], 14, 128)])
+@pytest.mark.parametrize("fp8, max_kv", [(False, 100000), (True, 700000)])
+@pytest.mark.parametrize("page", [2048, 8])
+def test_middle_sized_chunks_have_fine_weights(news, n_q, d, fp8, max_kv, page):
+    rng = np.random.default_rng([27, news[0], n_q, page])
+    c = cu_.Cache(rng, [1300, 140, 16], n_kv=2, d=d, page=page, fp8=fp8, width_more=max_kv // page, k_scale=0.03 if fp8 else 1.0, v_scale=0.02 if fp8 else 1.0)
+    check(rng, c, news, n_q, max_kv=max_kv, weight_bits=16)
+    check(rng, c, news, n_q, max_kv=max_kv, weight_bits=16, causal=False)
+
+
 @pytest.mark.parametrize("news", [[9, 16], [1, 16]])
 def test_middle_sized_chunks_of_very_long_8_bit_caches(news):
     rng = np.random.default_rng([25, news[0]])
