@@ -303,6 +303,18 @@ def codecomp_chunk_budgets(sigma, chunk_len, *, ratio, m_min, m_max, r_max, eps,
 # ---- serving from a compressed cache (codecomp_cache.h).  Sizes and strides come from the tensors' shapes, so that a call cannot
 # reach outside of them; tensors of another type, shape or device than the call needs are refused with ValueError.
 
+_torch_module = None
+
+
+def _torch():
+    """torch, imported by the first call that is given tensors (a global is looked up several times faster than an import statement runs)."""
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
+
+
 ROTARY_PLAIN, ROTARY_LINEAR, ROTARY_BASE, ROTARY_WAVELENGTH, ROTARY_RAMP = 0, 1, 2, 3, 4
 ROTARY_SCALINGS = {"plain": ROTARY_PLAIN, "linear": ROTARY_LINEAR, "base": ROTARY_BASE, "wavelength": ROTARY_WAVELENGTH, "ramp": ROTARY_RAMP}
 
@@ -325,7 +337,7 @@ def _own_strides(t, what: str):
 
 def make_pages(k, v, *, k_scale: float = 1.0, v_scale: float = 1.0) -> codecomp_pages:
     """A pool over two tensors [layers, pages, KV heads, page size, head_dim] with the same strides, bf16 or 8-bit (float8_e4m3fn, or codes as uint8)."""
-    import torch
+    torch = _torch()
     if k.dim() != 5 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.device != v.device:
         raise ValueError("k and v must be tensors [layers, pages, KV heads, page size, head_dim] of the same shape, strides, type and device")
     if k.dtype not in (torch.bfloat16, torch.uint8, torch.float8_e4m3fn):
@@ -344,8 +356,7 @@ def make_pages(k, v, *, k_scale: float = 1.0, v_scale: float = 1.0) -> codecomp_
 
 
 def _int32(t, shape, what: str):
-    import torch
-    if t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous():
+    if t.dtype is not (_torch_module or _torch()).int32 or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{what} must be a contiguous int32 tensor of shape {shape}, not {t.dtype} {tuple(t.shape)}")
 
 
@@ -373,12 +384,12 @@ def make_batch(*, n_q_heads: int, cu_q_host: np.ndarray, cu_q, kv_lens, table, m
 
 def _launch_stream(*at: int) -> int:
     """torch's current stream on the current device, where everything has to be (`at`: device numbers, -1 for the CPU): the library launches there."""
-    import torch
-    device = torch._C._cuda_getDevice()
+    c = (_torch_module or _torch())._C
+    device = c._cuda_getDevice()
     for i in at:
         if i != device:
             raise ValueError(f"a tensor is on {'the CPU' if i < 0 else f'cuda:{i}'}, the current device is cuda:{device}")
-    return torch._C._cuda_getCurrentRawStream(device)
+    return c._cuda_getCurrentRawStream(device)
 
 
 def _at(t, otherwise: int) -> int:
@@ -387,25 +398,38 @@ def _at(t, otherwise: int) -> int:
 
 def _vectors(t, what: str, shape, stride_tok: int, stride_head: int) -> int:
     """bf16 [tokens, heads, head_dim] with the strides that the call will use (0 = dense)."""
-    import torch
-    if t.dtype != torch.bfloat16 or t.shape != shape:
+    if t.dtype is not (_torch_module or _torch()).bfloat16 or t.shape != shape:
         raise ValueError(f"{what} must be bfloat16 {shape}, not {t.dtype} {tuple(t.shape)}")
+    if not stride_tok and not stride_head and t.is_contiguous():
+        return t.data_ptr()
     want = (stride_tok or shape[1] * shape[2], stride_head or shape[2], 1)
     if t.stride() != want and any(n > 1 and s != w for n, s, w in zip(shape, t.stride(), want)):
         raise ValueError(f"{what} has strides {t.stride()}, the call goes by {want}")
     return t.data_ptr()
 
 
+def _row_strides(t, what: str):
+    """Of tokens and heads, for vectors that are not dense."""
+    tok, head, one = t.stride()
+    if one != 1 and t.shape[2] > 1:
+        raise ValueError(f"{what} must have contiguous heads (strides {t.stride()})")
+    if (tok == 0 and t.shape[0] > 1) or (head == 0 and t.shape[1] > 1):
+        raise ValueError(f"{what} must not be a broadcast tensor (strides {t.stride()})")
+    return tok if t.shape[0] > 1 else 0, head if t.shape[1] > 1 else 0
+
+
 def codecomp_rotate(x, positions, rotary: codecomp_rotary, out) -> None:
     """x, out: bf16 [tokens, heads, head_dim], any strides of tokens and heads."""
-    import torch
-    if x.dim() != 3 or x.shape != out.shape or x.dtype != torch.bfloat16 or out.dtype != torch.bfloat16 or x.stride(2) != 1 or out.stride(2) != 1:
-        raise ValueError("x and out must be bfloat16 [tokens, heads, head_dim] with contiguous heads")
-    T, H, d = x.shape
+    bf16 = (_torch_module or _torch()).bfloat16
+    shape = x.shape
+    if len(shape) != 3 or shape != out.shape or x.dtype is not bf16 or out.dtype is not bf16:
+        raise ValueError("x and out must be bfloat16 [tokens, heads, head_dim]")
+    T, H, d = shape
     _int32(positions, (T,), "positions")
-    xs, os_ = ((0, 0) if y.is_contiguous() else _own_strides(y, what) for y, what in ((x, "x"), (out, "out")))
+    x_tok, x_head = (0, 0) if x.is_contiguous() else _row_strides(x, "x")
+    o_tok, o_head = (0, 0) if out.is_contiguous() else _row_strides(out, "out")
     stream = _launch_stream(x.get_device(), positions.get_device(), out.get_device())
-    _check(lib().codecomp_rotate(x.data_ptr(), positions.data_ptr(), C.byref(rotary), T, H, d, xs[0], xs[1], out.data_ptr(), os_[0], os_[1], stream),
+    _check(lib().codecomp_rotate(x.data_ptr(), positions.data_ptr(), C.byref(rotary), T, H, d, x_tok, x_head, out.data_ptr(), o_tok, o_head, stream),
            "codecomp_rotate")
 
 
@@ -428,7 +452,7 @@ def codecomp_append(q, k, v, positions, rotary: Optional[codecomp_rotary], batch
 
 def _rows(t, params, what: str, total: int, strides) -> int:
     """Dense rows [layers, KV heads, total, head_dim] in the cache's type with the strides that `params` says."""
-    import torch
+    torch = _torch()
     fp8 = params.kv_dtype == KV_FP8_E4M3
     shape = (params.n_layers, params.n_kv_heads, total, params.head_dim)
     if (t.dtype not in (torch.uint8, torch.float8_e4m3fn) if fp8 else t.dtype != torch.bfloat16) or t.shape != shape:
@@ -504,7 +528,7 @@ def codecomp_attend_workspace_bytes(batch, pages) -> int:
 
 
 def codecomp_attend(q, batch: codecomp_batch, pages: codecomp_pages, layer: int, out, workspace, lse=None) -> None:
-    import torch
+    torch = _torch_module or _torch()
     shape = (batch._tokens, batch.n_q_heads, pages.head_dim)
     qp, op = _vectors(q, "q", shape, batch.q_stride_tok, batch.q_stride_head), _vectors(out, "out", shape, batch.out_stride_tok, batch.out_stride_head)
     if lse is not None and (lse.dtype != torch.float32 or lse.shape != shape[:2] or not lse.is_contiguous()):

@@ -12,7 +12,7 @@
 // and 16 + 4 q + i of lane group q); V^T is read from LDS by the transposing read.  A weight enters the product as two bf16, its
 // rounded value and the rest: 16 bits of it, for MFMA time that memory hides.
 //
-// Measured (large copies read 6.4 TB/s here): 64 steps over 500 .. 16384 keys, 4 KV heads of 128 elements, bf16: 187 us, 5.3 TB/s; with 8 KV heads, 8
+// Measured (a kernel that only reads reaches 6.4 TB/s): 64 steps over 500 .. 16384 keys, 4 KV heads of 128 elements, bf16: 187 us, 5.3 TB/s; with 8 KV heads, 8
 // bits: 187 us, 5.4 TB/s; one step over 131072 keys: 51 us and 6 us for the join, 4.8 TB/s; one over 2113: 7 us and 3 us, a chain of small loads
 // (lengths, table, rows, parts) that nothing hides.
 #include "attend.h"

@@ -1,10 +1,19 @@
-// Internal header: attention of requests with many rows (new tokens x query heads per KV head, more than 64): prefill chunks and prompts.
-// Instantiated per head_dim and cache type in attend_many_*.hip, so that they compile side by side.
+// Internal header: attention of requests with many rows (new tokens x query heads per KV head; attend.hip says from how many on): prefill chunks and
+// prompts.  Instantiated per head_dim, cache type and weights in attend_many_*.hip, so that they compile side by side.
 //
 // The rows of a KV head, token by token and its query heads within, are cut into blocks of 256: eight waves of 32 rows,
 // which share the keys and values that go through LDS in tiles of 64.  S^T = K Q^T leaves a row's logits in one lane of each half of the wave;
 // O^T += V^T P^T takes them from there: the order of keys in a contraction is free, and chosen so that a lane's weights are its right operand as
-// they stand.  V^T comes from LDS by the transposing read.
+// they stand.  V^T comes from LDS by the transposing read.  A row's reference (what is subtracted before exp2) moves only when a weight grows large, so
+// that most steps neither look for a maximum nor touch the outputs.
+//
+// Bound by the matrix units and the vector instructions beside them, under the chip's power limit.  2048 tokens over 32768 keys, 28 query heads on 4 KV
+// heads of 128: 760 to 810 us by the device, 1.15 to 1.23 PFLOP/s, where the library's product of two 8192 x 8192 matrices reaches 1.21 to 1.27 on the
+// same devices; the matrix units are busy 69 % of the time at 1.5 to 1.9 GHz, 94 % of the reads meet L2, no LDS bank conflict.  head_dim 64 has as many
+// vector instructions for half the products: 480 to 505 us, 0.93 to 0.97 PFLOP/s.  8-bit caches: 815 and 516 us, the codes are widened on the way to LDS.
+// Before it: waves with 512 registers (the compiler keeps the accumulators in the half that vector instructions do not reach, and copies them); the page
+// table looked up key by key (790 us; as one load per 1024 keys 760).
+// Sending for a part's first tiles behind the last ones of the part before took as much time in the loop as it saved between parts.
 #pragma once
 #include "attend.h"
 
@@ -12,13 +21,14 @@ namespace codecomp {
 
 constexpr int kManyRows = 256, kManyKeys = 64, kManyWaves = 8, kManyThreads = 64 * kManyWaves;
 
-// Positions in front of the tiles of a block, in the sequence that is cut into equal parts: starting on a block (its queries, the first tiles) costs
-// about as much as that many tiles.
+// Positions in front of the tiles of a block, in the sequence that is cut into equal parts: starting on a block (its queries, the first tiles) and
+// ending it cost 11 us at head_dim 128 and 5 at 64, of 1.65 and 1.2 us a tile (a prompt of 4096 tokens, us, with 3 | 4 | 5 | 7 | 10 | 14 positions: 185 |
+// 170 | 155 | 141 | 146 | 149; head_dim 64 114 | 103 | 97 | 95).
 constexpr int kManyLead = 7;
 // Reference of a row before its first visible key: finite, so that hidden logits (minus infinity) less it still are minus infinity, and so low that a
 // visible one's weight overflows, which makes it the reference.
 constexpr float kNoReference = -3.402823466e38f;
-constexpr int kManyLeast = 4;   // positions that a workgroup gets at least
+constexpr int kManyLeast = 4;   // positions that a workgroup gets at least (with 8 a prompt of 100 tokens takes 32 us instead of 23)
 
 struct ManyArgs {
   AttendArgs a;
@@ -179,321 +189,321 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
     const int64_t first = start + kManyLead;                      // position of its first tile
     const int tile0 = ma.whole ? 0 : uniform((int)max(x0 - first, (int64_t)0)), tile1 = ma.whole ? tiles : uniform((int)min(x1 - first, (int64_t)tiles));
     if (tile1 > tile0) {
-    const bool whole = tile0 == 0 && tile1 == tiles;
-    const int slot = tile0 > 0 ? 2 * g : 2 * g + 1;
-    if (tile0 == 0 && tile1 < tiles)                             // the rest of the block is the next workgroups'
-      cut = {r, block, head, (int)(((first + tiles) * workgroups - 1) / total)};
-    const int q0 = uniform(a.b.cu_q[r]), row0 = block * kManyRows + wave * 32, row = row0 + l32;
-    const bool active = row0 < of.rows;
+      const bool whole = tile0 == 0 && tile1 == tiles;
+      const int slot = tile0 > 0 ? 2 * g : 2 * g + 1;
+      if (tile0 == 0 && tile1 < tiles)                             // the rest of the block is the next workgroups'
+        cut = {r, block, head, (int)(((first + tiles) * workgroups - 1) / total)};
+      const int q0 = uniform(a.b.cu_q[r]), row0 = block * kManyRows + wave * 32, row = row0 + l32;
+      const bool active = row0 < of.rows;
 
-    // query rows as right operands, and the keys that the lane's rows see
-    u32x4 qf[KS];
-    int limit;
-    {
-      const int rr = min(row, of.rows - 1), t = rr / of.G;
-      const uint16_t* p = a.q + (q0 + t) * a.b.q_st + (head * of.G + rr - t * of.G) * a.b.q_sh + half * 8;
+      // query rows as right operands, and the keys that the lane's rows see
+      u32x4 qf[KS];
+      int limit;
+      {
+        const int rr = min(row, of.rows - 1), t = rr / of.G;
+        const uint16_t* p = a.q + (q0 + t) * a.b.q_st + (head * of.G + rr - t * of.G) * a.b.q_sh + half * 8;
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        qf[ks] = *reinterpret_cast<const u32x4*>(p + ks * 16);
-        if (row >= of.rows) qf[ks] = u32x4{0, 0, 0, 0};
-      }
-      limit = of.causal ? min(of.len, of.len - of.nq + t + 1) : of.len;
-    }
-    const int seen_by_all = uniform(of.causal ? min(of.len, of.len - of.nq + block * kManyRows / of.G + 1) : of.len);
-
-    const unsigned char* kb = a.pool.k + a.layer + head * a.pool.s_head;
-    const unsigned char* vb = a.pool.v + a.layer + head * a.pool.s_head;
-    const int32_t* table = a.b.table + (int64_t)r * a.b.table_width;
-    const int in_page = (1 << a.pool.page_log2) - 1;
-
-    // ---- the way of keys and values.  A tile goes into one of four LDS buffers three tiles ahead: 16-bit rows straight from memory, 8-bit rows by
-    // way of registers, where they are widened.  Entries of the page table go ahead of them, 64 at a time: one for every 16 keys, the 16 tiles of a
-    // stretch of 1024 keys at once (or, ROWWISE, one for every key of a tile, five tiles ahead).
-    auto fetch_entries = [&](int stretch) __attribute__((always_inline)) {        // for the last key where there is none
-      const int32_t* from = table + (max(min((stretch * 64 + lane) * (ROWWISE ? 1 : 16), of.len - 1), 0) >> a.pool.page_log2);
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds_address(entries[stretch & (ROWWISE ? 7 : 3)])), "v"(from) : "memory", "m0");
-    };
-    auto entry = [&](int tile, int row) __attribute__((always_inline)) { return ROWWISE ? entries[tile & 7][row] : entries[(tile >> 4) & 3][(tile & 15) * 4 + (row >> 4)]; };
-    auto is_page = [&](int page) __attribute__((always_inline)) { return (unsigned)page < (unsigned)a.pool.n_pages; };
-    // The rows of a tile that this thread loads pieces of.  16 bits: of the wave's 16 rows, the lane % 16th of K and the lane / 4th of V.  8 bits: of its
-    // 8 or 16, in an order that makes the stores of eight lanes to LDS meet different banks: rows side by side in K, four rows and two pieces in V.
-    constexpr int ROWS = FP8 ? 64 / PIECES : 16;
-    const int wave_row = FP8 ? (wave * ROWS) & (kManyKeys - 1) : (wave >> 1) * 16;
-    const int k_row = wave_row + (lane & (ROWS - 1)), v_row = wave_row + (FP8 ? (lane & 3) + ((lane >> 3) & (ROWS / 4 - 1)) * 4 : lane >> 2);
-    const int k_piece = FP8 ? lane / ROWS : (wave & 1) * LOADS * 4 + (lane >> 4);
-    const int v_piece = FP8 ? ((lane >> 2) & 1) + (lane >> 3) / (ROWS / 4) * 2 : (wave & 1) * LOADS * 4 + (lane & 3);
-    const bool has_values = HALVES && wave >= kManyWaves / 2;
-    // Where they are; rows that are not there: in page 0, taken out of the tile when it is used.  At `base` + `lane_off`.
-    struct Place { int64_t base; uint32_t lane_off; };
-    const uint32_t k_lane_off = (k_row - wave_row) * (uint32_t)a.pool.s_tok + k_piece * 16, v_lane_off = (v_row - wave_row) * (uint32_t)a.pool.s_tok + v_piece * 16;
-    auto place = [&](int tile, int row, int piece, uint32_t lane_off) __attribute__((always_inline)) {
-      const int page = ROWWISE ? entry(tile, row) : uniform(entry(tile, wave_row));
-      const int64_t at = (uint64_t)(unsigned)(is_page(page) ? page : 0) * (uint64_t)a.pool.s_page;
-      if constexpr (ROWWISE) return Place{at + (unsigned)((tile * kManyKeys + row) & in_page) * (unsigned)a.pool.s_tok, (uint32_t)piece * 16};
-      return Place{at + (unsigned)((tile * kManyKeys + wave_row) & in_page) * (unsigned)a.pool.s_tok, lane_off};
-    };
-    auto k_place = [&](int tile) __attribute__((always_inline)) {
-      return has_values ? place(tile, v_row, v_piece, v_lane_off) : place(tile, k_row, k_piece, k_lane_off);
-    };
-    auto v_place = [&](int tile, Place k) __attribute__((always_inline)) {
-      if constexpr (HALVES) return k;
-      if constexpr (!ROWWISE) return Place{k.base, v_lane_off};
-      return place(tile, v_row, v_piece, v_lane_off);
-    };
-    u32x4 kr, vr;                                                // 8 bits: the tile after the next two, on its way
-    auto fetch = [&](u32x4& into, uint32_t lds, const unsigned char* from, Place at) __attribute__((always_inline)) {
-      if constexpr (FP8) {
-        into = *reinterpret_cast<const u32x4*>(from + at.base + at.lane_off);
-      } else {
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-          if constexpr (ROWWISE)
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds + (wave * LOADS + i) * 1024),
-                         "v"(from + at.base + at.lane_off + i * 64) : "memory", "m0");
-          else
-            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds + (wave * LOADS + i) * 1024),
-                         "v"(at.lane_off), "s"(from + at.base + i * 64) : "memory", "m0");
+        for (int ks = 0; ks < KS; ++ks) {
+          qf[ks] = *reinterpret_cast<const u32x4*>(p + ks * 16);
+          if (row >= of.rows) qf[ks] = u32x4{0, 0, 0, 0};
         }
+        limit = of.causal ? min(of.len, of.len - of.nq + t + 1) : of.len;
       }
-    };
-    auto fetch_keys = [&](int tile, Place at) __attribute__((always_inline)) { fetch(kr, lds_address(k_tile(tile)), has_values ? vb : kb, at); };
-    auto fetch_values = [&](int tile, Place at) __attribute__((always_inline)) {
-      if constexpr (!HALVES) fetch(vr, lds_address(k_tile(tile)) + TILE, vb, at);
-    };
-    const int park_at = has_values ? TILE + At::value(v_row, 2 * v_piece) : At::key(k_row, 2 * k_piece);
-    const int park_at2 = has_values ? TILE + At::value(v_row, 2 * v_piece + 1) : At::key(k_row, 2 * k_piece + 1);
-    auto park = [&](int tile, int quarter) __attribute__((always_inline)) {      // 8 bits: a half of the piece of K, or of that of V
-      if constexpr (FP8) {
-        unsigned char* at = k_tile(tile);
-        if (quarter == 0) *reinterpret_cast<u32x4*>(at + park_at) = widen8(kr.x, kr.y);
-        if (quarter == 1) *reinterpret_cast<u32x4*>(at + park_at2) = widen8(kr.z, kr.w);
-        if constexpr (HALVES) return;
-        if (quarter == 2) *reinterpret_cast<u32x4*>(at + TILE + At::value(v_row, 2 * v_piece)) = widen8(vr.x, vr.y);
-        if (quarter == 3) *reinterpret_cast<u32x4*>(at + TILE + At::value(v_row, 2 * v_piece + 1)) = widen8(vr.z, vr.w);
-      }
-    };
-    // The keys of a tile that there are; the tiles from `plain_end` on have keys that are not there, or that some rows do not see.
-    auto is_there = [&](int tile, int page) __attribute__((always_inline)) { return __ballot(tile * kManyKeys + lane < of.len && is_page(page)); };
-    const int plain_end = min(seen_by_all, of.len) >> 6;
-    auto partly = [&](int tile) { return (tile + 1) * kManyKeys > seen_by_all && seen_by_all < of.len; };       // some rows do not see all of it
-    // Values of a tile that has keys that are not there, or that some rows do not see: a weight of zero must not meet what stands in the one, nor an
-    // infinite or NaN value in the other (added at the end, to the rows that see them).
-    auto clean_values = [&](int tile, uint64_t valid) __attribute__((always_inline)) {
-      unsigned any = 0;
-      for (int i = tid; i < TILE / 16; i += kManyThreads) {
-        u32x4* at = reinterpret_cast<u32x4*>(k_tile(tile) + TILE + i * 16);
-        u32x4 v = *at;
-        if (!((valid >> (i * 16 / At::GROUP * 16 + ((i >> 2) & 15))) & 1)) v = u32x4{0, 0, 0, 0};
-        if (partly(tile)) v = finite_part<false>(v, any);
-        *at = v;
-      }
-      if (any != 0) not_finite = 1;
-    };
+      const int seen_by_all = uniform(of.causal ? min(of.len, of.len - of.nq + block * kManyRows / of.G + 1) : of.len);
 
-    f32x16 o[DB];
-    float m = kNoReference, l = 0.0f;                            // a row's reference, this half's sum of weights
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) o[db][i] = 0.0f;
-    f32x16 za, zb;                                               // logits of the first and of the second 32 keys of a tile
-    struct Weights {                                             // their weights, 16 keys each; FINE: rounded, and the rest
-      u32x4 p[2], rest[FINE ? 2 : 1];
-    } pa, pb = {};
-    auto pack = [&](Weights& to, int i, float x, float y) __attribute__((always_inline)) {      // of logits i and i + 1
-      const unsigned p = pack2(x, y);
-      to.p[i >> 3][(i & 7) >> 1] = p;
-      if constexpr (FINE) to.rest[i >> 3][(i & 7) >> 1] = pack2(x - __uint_as_float(p << 16), y - __uint_as_float(p & 0xFFFF0000u));
-    };
+      const unsigned char* kb = a.pool.k + a.layer + head * a.pool.s_head;
+      const unsigned char* vb = a.pool.v + a.layer + head * a.pool.s_head;
+      const int32_t* table = a.b.table + (int64_t)r * a.b.table_width;
+      const int in_page = (1 << a.pool.page_log2) - 1;
 
-    // Key fragment f (16 of a row's elements of 32 keys), value fragment f (32 columns of 16 keys).
-    const int k_lane = At::key(l32, half), v_lane = At::value(half * 4 + ((lane >> 2) & 3), 0) + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
-    auto key_frag = [&](const unsigned char* kt, int f) __attribute__((always_inline)) { return *reinterpret_cast<const u32x4*>(kt + k_lane + f * 512); };
-    auto value_frag = [&](const unsigned char* vt, int f) __attribute__((always_inline)) {
-      const unsigned char* at = vt + v_lane + (f / DB) * At::GROUP + (f % DB) * 1024;
-      const s16x4 v0 = read_columns(at), v1 = read_columns(at + 512);
-      return __builtin_bit_cast(u32x4, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-    };
-    constexpr int F = 2 * KS, RING = 4, PER = 16 / F, HALF = 2 * At::GROUP;      // fragments of a step, those held, logits per fragment; bytes of 32 rows
-    u32x4 ring[RING];
-    auto fill = [&](int f, const unsigned char* kt, const unsigned char* vt) __attribute__((always_inline)) {
-      ring[f % RING] = f & 1 ? value_frag(vt, f / 2) : key_frag(kt, f / 2);
-    };
-    // One step: the weights p of the 32 keys from key0 on, whose logits are z (`masked`: not all rows see all of them; `valid`: which of them there are); beside them, on the matrix cores,
-    // the logits zn of the next 32 keys (kt) and the outputs of the 32 before (vt), whose weights are pp.  The order is the source's: the LDS read that
-    // the MFMA three further on needs (from the next step's tiles at the end), an MFMA, the vector work of a logit (two at head_dim 64), and
-    // what `beside` has for this place.
-    auto step = [&](f32x16& z, Weights& p, f32x16& zn, const unsigned char* kt, const Weights& pp, const unsigned char* vt, const unsigned char* kt_next,
-                    const unsigned char* vt_next, int key0, bool masked, unsigned valid, auto&& beside) __attribute__((always_inline)) {
-      if (__builtin_expect(masked, 0)) {
+      // ---- the way of keys and values.  A tile goes into one of four LDS buffers three tiles ahead: 16-bit rows straight from memory, 8-bit rows by
+      // way of registers, where they are widened.  Entries of the page table go ahead of them, 64 at a time: one for every 16 keys, the 16 tiles of a
+      // stretch of 1024 keys at once (or, ROWWISE, one for every key of a tile, five tiles ahead).
+      auto fetch_entries = [&](int stretch) __attribute__((always_inline)) {        // for the last key where there is none
+        const int32_t* from = table + (max(min((stretch * 64 + lane) * (ROWWISE ? 1 : 16), of.len - 1), 0) >> a.pool.page_log2);
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds_address(entries[stretch & (ROWWISE ? 7 : 3)])), "v"(from) : "memory", "m0");
+      };
+      auto entry = [&](int tile, int row) __attribute__((always_inline)) { return ROWWISE ? entries[tile & 7][row] : entries[(tile >> 4) & 3][(tile & 15) * 4 + (row >> 4)]; };
+      auto is_page = [&](int page) __attribute__((always_inline)) { return (unsigned)page < (unsigned)a.pool.n_pages; };
+      // The rows of a tile that this thread loads pieces of.  16 bits: of the wave's 16 rows, the lane % 16th of K and the lane / 4th of V.  8 bits: of its
+      // 8 or 16, in an order that makes the stores of eight lanes to LDS meet different banks: rows side by side in K, four rows and two pieces in V.
+      constexpr int ROWS = FP8 ? 64 / PIECES : 16;
+      const int wave_row = FP8 ? (wave * ROWS) & (kManyKeys - 1) : (wave >> 1) * 16;
+      const int k_row = wave_row + (lane & (ROWS - 1)), v_row = wave_row + (FP8 ? (lane & 3) + ((lane >> 3) & (ROWS / 4 - 1)) * 4 : lane >> 2);
+      const int k_piece = FP8 ? lane / ROWS : (wave & 1) * LOADS * 4 + (lane >> 4);
+      const int v_piece = FP8 ? ((lane >> 2) & 1) + (lane >> 3) / (ROWS / 4) * 2 : (wave & 1) * LOADS * 4 + (lane & 3);
+      const bool has_values = HALVES && wave >= kManyWaves / 2;
+      // Where they are; rows that are not there: in page 0, taken out of the tile when it is used.  At `base` + `lane_off`.
+      struct Place { int64_t base; uint32_t lane_off; };
+      const uint32_t k_lane_off = (k_row - wave_row) * (uint32_t)a.pool.s_tok + k_piece * 16, v_lane_off = (v_row - wave_row) * (uint32_t)a.pool.s_tok + v_piece * 16;
+      auto place = [&](int tile, int row, int piece, uint32_t lane_off) __attribute__((always_inline)) {
+        const int page = ROWWISE ? entry(tile, row) : uniform(entry(tile, wave_row));
+        const int64_t at = (uint64_t)(unsigned)(is_page(page) ? page : 0) * (uint64_t)a.pool.s_page;
+        if constexpr (ROWWISE) return Place{at + (unsigned)((tile * kManyKeys + row) & in_page) * (unsigned)a.pool.s_tok, (uint32_t)piece * 16};
+        return Place{at + (unsigned)((tile * kManyKeys + wave_row) & in_page) * (unsigned)a.pool.s_tok, lane_off};
+      };
+      auto k_place = [&](int tile) __attribute__((always_inline)) {
+        return has_values ? place(tile, v_row, v_piece, v_lane_off) : place(tile, k_row, k_piece, k_lane_off);
+      };
+      auto v_place = [&](int tile, Place k) __attribute__((always_inline)) {
+        if constexpr (HALVES) return k;
+        if constexpr (!ROWWISE) return Place{k.base, v_lane_off};
+        return place(tile, v_row, v_piece, v_lane_off);
+      };
+      u32x4 kr, vr;                                                // 8 bits: the tile after the next two, on its way
+      auto fetch = [&](u32x4& into, uint32_t lds, const unsigned char* from, Place at) __attribute__((always_inline)) {
+        if constexpr (FP8) {
+          into = *reinterpret_cast<const u32x4*>(from + at.base + at.lane_off);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int j = 8 * (i >> 2) + 4 * half + (i & 3);
-          if (!((valid >> j) & 1) || key0 + j >= limit) z[i] = -INFINITY;
+          for (int i = 0; i < LOADS; ++i) {
+            if constexpr (ROWWISE)
+              asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds + (wave * LOADS + i) * 1024),
+                           "v"(from + at.base + at.lane_off + i * 64) : "memory", "m0");
+            else
+              asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds + (wave * LOADS + i) * 1024),
+                           "v"(at.lane_off), "s"(from + at.base + i * 64) : "memory", "m0");
+          }
         }
-      }
-      float sum = 0.0f, w[16];
-#pragma unroll
-      for (int i = 0; i < 16; ++i) zn[i] = 0.0f;
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int f = 0; f < F; ++f) {
-        beside(f);
-        if (f + RING - 1 < F) fill(f + RING - 1, kt, vt);
-        else fill(f + RING - 1 - F, kt_next, vt_next);
-        const int i = f / 2;
-        if (f & 1) {
-          o[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(ring[f % RING]), frag(pp.p[i / DB]), o[i % DB], 0, 0, 0);
-          if constexpr (FINE) o[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(ring[f % RING]), frag(pp.rest[i / DB]), o[i % DB], 0, 0, 0);
-        } else zn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(ring[f % RING]), frag(qf[i]), zn, 0, 0, 0);
-#pragma unroll
-        for (int e = f * PER; e < (f + 1) * PER; ++e) {
-          w[e] = __builtin_amdgcn_exp2f(fmaf(z[e], a.c, -m));
-          if (e > 0) sum += w[e - 1];
-          if (e > 1 && (e & 1) == 0) pack(p, e - 2, w[e - 2], w[e - 1]);
+      };
+      auto fetch_keys = [&](int tile, Place at) __attribute__((always_inline)) { fetch(kr, lds_address(k_tile(tile)), has_values ? vb : kb, at); };
+      auto fetch_values = [&](int tile, Place at) __attribute__((always_inline)) {
+        if constexpr (!HALVES) fetch(vr, lds_address(k_tile(tile)) + TILE, vb, at);
+      };
+      const int park_at = has_values ? TILE + At::value(v_row, 2 * v_piece) : At::key(k_row, 2 * k_piece);
+      const int park_at2 = has_values ? TILE + At::value(v_row, 2 * v_piece + 1) : At::key(k_row, 2 * k_piece + 1);
+      auto park = [&](int tile, int quarter) __attribute__((always_inline)) {      // 8 bits: a half of the piece of K, or of that of V
+        if constexpr (FP8) {
+          unsigned char* at = k_tile(tile);
+          if (quarter == 0) *reinterpret_cast<u32x4*>(at + park_at) = widen8(kr.x, kr.y);
+          if (quarter == 1) *reinterpret_cast<u32x4*>(at + park_at2) = widen8(kr.z, kr.w);
+          if constexpr (HALVES) return;
+          if (quarter == 2) *reinterpret_cast<u32x4*>(at + TILE + At::value(v_row, 2 * v_piece)) = widen8(vr.x, vr.y);
+          if (quarter == 3) *reinterpret_cast<u32x4*>(at + TILE + At::value(v_row, 2 * v_piece + 1)) = widen8(vr.z, vr.w);
         }
+      };
+      // The keys of a tile that there are; the tiles from `plain_end` on have keys that are not there, or that some rows do not see.
+      auto is_there = [&](int tile, int page) __attribute__((always_inline)) { return __ballot(tile * kManyKeys + lane < of.len && is_page(page)); };
+      const int plain_end = min(seen_by_all, of.len) >> 6;
+      auto partly = [&](int tile) { return (tile + 1) * kManyKeys > seen_by_all && seen_by_all < of.len; };       // some rows do not see all of it
+      // Values of a tile that has keys that are not there, or that some rows do not see: a weight of zero must not meet what stands in the one, nor an
+      // infinite or NaN value in the other (added at the end, to the rows that see them).
+      auto clean_values = [&](int tile, uint64_t valid) __attribute__((always_inline)) {
+        unsigned any = 0;
+        for (int i = tid; i < TILE / 16; i += kManyThreads) {
+          u32x4* at = reinterpret_cast<u32x4*>(k_tile(tile) + TILE + i * 16);
+          u32x4 v = *at;
+          if (!((valid >> (i * 16 / At::GROUP * 16 + ((i >> 2) & 15))) & 1)) v = u32x4{0, 0, 0, 0};
+          if (partly(tile)) v = finite_part<false>(v, any);
+          *at = v;
+        }
+        if (any != 0) not_finite = 1;
+      };
+
+      f32x16 o[DB];
+      float m = kNoReference, l = 0.0f;                            // a row's reference, this half's sum of weights
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[db][i] = 0.0f;
+      f32x16 za, zb;                                               // logits of the first and of the second 32 keys of a tile
+      struct Weights {                                             // their weights, 16 keys each; FINE: rounded, and the rest
+        u32x4 p[2], rest[FINE ? 2 : 1];
+      } pa, pb = {};
+      auto pack = [&](Weights& to, int i, float x, float y) __attribute__((always_inline)) {      // of logits i and i + 1
+        const unsigned p = pack2(x, y);
+        to.p[i >> 3][(i & 7) >> 1] = p;
+        if constexpr (FINE) to.rest[i >> 3][(i & 7) >> 1] = pack2(x - __uint_as_float(p << 16), y - __uint_as_float(p & 0xFFFF0000u));
+      };
+
+      // Key fragment f (16 of a row's elements of 32 keys), value fragment f (32 columns of 16 keys).
+      const int k_lane = At::key(l32, half), v_lane = At::value(half * 4 + ((lane >> 2) & 3), 0) + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+      auto key_frag = [&](const unsigned char* kt, int f) __attribute__((always_inline)) { return *reinterpret_cast<const u32x4*>(kt + k_lane + f * 512); };
+      auto value_frag = [&](const unsigned char* vt, int f) __attribute__((always_inline)) {
+        const unsigned char* at = vt + v_lane + (f / DB) * At::GROUP + (f % DB) * 1024;
+        const s16x4 v0 = read_columns(at), v1 = read_columns(at + 512);
+        return __builtin_bit_cast(u32x4, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+      };
+      constexpr int F = 2 * KS, RING = 4, PER = 16 / F, HALF = 2 * At::GROUP;      // fragments of a step, those held, logits per fragment; bytes of 32 rows
+      u32x4 ring[RING];
+      auto fill = [&](int f, const unsigned char* kt, const unsigned char* vt) __attribute__((always_inline)) {
+        ring[f % RING] = f & 1 ? value_frag(vt, f / 2) : key_frag(kt, f / 2);
+      };
+      // One step: the weights p of the 32 keys from key0 on, whose logits are z (`masked`: not all rows see all of them; `valid`: which of them there are); beside them, on the matrix cores,
+      // the logits zn of the next 32 keys (kt) and the outputs of the 32 before (vt), whose weights are pp.  The order is the source's: the LDS read that
+      // the MFMA three further on needs (from the next step's tiles at the end), an MFMA, the vector work of a logit (two at head_dim 64), and
+      // what `beside` has for this place.
+      auto step = [&](f32x16& z, Weights& p, f32x16& zn, const unsigned char* kt, const Weights& pp, const unsigned char* vt, const unsigned char* kt_next,
+                      const unsigned char* vt_next, int key0, bool masked, unsigned valid, auto&& beside) __attribute__((always_inline)) {
+        if (__builtin_expect(masked, 0)) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int j = 8 * (i >> 2) + 4 * half + (i & 3);
+            if (!((valid >> j) & 1) || key0 + j >= limit) z[i] = -INFINITY;
+          }
+        }
+        float sum = 0.0f, w[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) zn[i] = 0.0f;
         __builtin_amdgcn_sched_barrier(0);
-      }
-      sum += w[15];
-      pack(p, 14, w[14], w[15]);
-      // here, beside the MFMAs, not behind the branch
-      asm volatile("" ::"v"(sum), "v"(p.p[0]), "v"(p.p[1]));
-      if constexpr (FINE) asm volatile("" ::"v"(p.rest[0]), "v"(p.rest[1]));
-      // A logit far above its row's reference: move the references.  (Weights are positive: none is larger than their sum, and as
-      // long as that is below 4096 nothing is lost in fp32 or bf16.)
-      if (__builtin_expect(__ballot(sum > 4096.0f) != 0, 0)) {
-        float t = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) t = fmaxf(t, z[i]);
-        t *= a.c;
-        t = fmaxf(t, __shfl_xor(t, 32));
-        const float to = fmaxf(m, t), old = to == m ? 1.0f : __builtin_amdgcn_exp2f(m - to);
-        m = to;
-        l *= old;
+        for (int f = 0; f < F; ++f) {
+          beside(f);
+          if (f + RING - 1 < F) fill(f + RING - 1, kt, vt);
+          else fill(f + RING - 1 - F, kt_next, vt_next);
+          const int i = f / 2;
+          if (f & 1) {
+            o[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(ring[f % RING]), frag(pp.p[i / DB]), o[i % DB], 0, 0, 0);
+            if constexpr (FINE) o[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(ring[f % RING]), frag(pp.rest[i / DB]), o[i % DB], 0, 0, 0);
+          } else zn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(ring[f % RING]), frag(qf[i]), zn, 0, 0, 0);
 #pragma unroll
-        for (int db = 0; db < DB; ++db)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[db][i] *= old;
-        sum = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 16; i += 2) {
-          const float x = __builtin_amdgcn_exp2f(fmaf(z[i], a.c, -m)), y = __builtin_amdgcn_exp2f(fmaf(z[i + 1], a.c, -m));
-          sum += x + y;
-          pack(p, i, x, y);
+          for (int e = f * PER; e < (f + 1) * PER; ++e) {
+            w[e] = __builtin_amdgcn_exp2f(fmaf(z[e], a.c, -m));
+            if (e > 0) sum += w[e - 1];
+            if (e > 1 && (e & 1) == 0) pack(p, e - 2, w[e - 2], w[e - 1]);
+          }
+          __builtin_amdgcn_sched_barrier(0);
         }
-      }
-      l += sum;
-    };
-
-    // ---- before the first tile
-    __syncthreads();                                             // the segment before is through with LDS
-    if (tid == 0) not_finite = 0;
+        sum += w[15];
+        pack(p, 14, w[14], w[15]);
+        // here, beside the MFMAs, not behind the branch
+        asm volatile("" ::"v"(sum), "v"(p.p[0]), "v"(p.p[1]));
+        if constexpr (FINE) asm volatile("" ::"v"(p.rest[0]), "v"(p.rest[1]));
+        // A logit far above its row's reference: move the references.  (Weights are positive: none is larger than their sum, and as
+        // long as that is below 4096 nothing is lost in fp32 or bf16.)
+        if (__builtin_expect(__ballot(sum > 4096.0f) != 0, 0)) {
+          float t = -INFINITY;
 #pragma unroll
-    for (int j = 0; j < (ROWWISE ? 5 : 3); ++j) fetch_entries((ROWWISE ? tile0 : tile0 >> 4) + j);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-#pragma unroll
-    for (int j = 0; j < 3; ++j) {
-      const Place from = k_place(tile0 + j);
-      fetch_keys(tile0 + j, from);
-      fetch_values(tile0 + j, v_place(tile0 + j, from));
-      if (j < 2) { park(tile0 + j, 0); park(tile0 + j, 1); park(tile0 + j, 2); park(tile0 + j, 3); }
-    }
-    // in front of the first tile: values of zero
-    for (int i = tid; i < HALF / 16; i += kManyThreads) *reinterpret_cast<u32x4*>(k_tile(tile0 + 3) + TILE + HALF + i * 16) = u32x4{0, 0, 0, 0};
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(SENT) : "memory");
-    uint64_t valid = ROWWISE ? is_there(tile0, entry(tile0, lane)) : 0;
-    uint64_t held = ROWWISE ? 0 : __ballot(is_page(entries[(tile0 >> 4) & 3][lane]));          // groups of 16 keys of the stretch whose pages there are
-    if (active) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) za[i] = 0.0f;
-#pragma unroll
-      for (int f = 0; f < KS; ++f) za = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(key_frag(k_tile(tile0), f)), frag(qf[f]), za, 0, 0, 0);
-#pragma unroll
-      for (int f = 0; f < RING - 1; ++f) fill(f, k_tile(tile0) + HALF, k_tile(tile0 + 3) + TILE + HALF);
-    }
-    for (int tile = tile0; tile < tile1; ++tile) {
-      bool masked = tile >= plain_end;
-      if constexpr (ROWWISE) {
-        masked |= valid != ~0ull;
-      } else {
-        if ((tile & 15) == 13) fetch_entries((tile >> 4) + 2);   // three tiles ahead a new stretch begins: the one after it
-        if ((tile & 15) == 0) held = __ballot(is_page(entries[(tile >> 4) & 3][lane]));
-        masked |= (((unsigned)(held >> ((tile & 15) * 4)) & 15u) != 15u);
-        if (masked) valid = is_there(tile, entry(tile, lane));
-      }
-      if (__builtin_expect(masked, 0)) clean_values(tile, valid);
-      const unsigned char *t0 = k_tile(tile), *t1 = k_tile(tile + 1), *before = k_tile(tile + 3);
-      // All of this step's LDS reads are on their way by the last places: from there on the tile before is nobody's, and the next one is everybody's.
-      auto pass_on = [&](int f) __attribute__((always_inline)) {
-        if (f == F - (RING - 1)) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(SENT + (ROWWISE ? 1 : 0)) : "memory");
-      };
-      Place k_from = {0, 0}, v_from = {0, 0};
-      int next_entry = 0;
-      auto send_for = [&](int f) __attribute__((always_inline)) {
-        if (ROWWISE && f == 0) next_entry = entry(tile + 1, lane);
-        if (f < 4) park(tile + 2, f);                            // before the next ones are sent for below
-        if (f == 1) k_from = k_place(tile + 3);
-        if (f == 2) v_from = v_place(tile + 3, k_from);
-        if (f == 3) fetch_keys(tile + 3, k_from);
-        if (f == 4) fetch_values(tile + 3, v_from);
-        if (f == 5 && ROWWISE) fetch_entries(tile + 5);
-      };
-      if (active) {
-        step(za, pa, zb, t0 + HALF, pb, before + TILE + HALF, t1, t0 + TILE, tile * kManyKeys, masked, (unsigned)valid, pass_on);
-        step(zb, pb, za, t1, pa, t0 + TILE, t1 + HALF, t0 + TILE + HALF, tile * kManyKeys + 32, masked, (unsigned)(valid >> 32), send_for);
-      } else {
-        pass_on(F - (RING - 1));
-#pragma unroll
-        for (int f = 0; f < F; ++f) send_for(f);
-      }
-      if constexpr (ROWWISE) valid = is_there(tile + 1, next_entry);
-    }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // what was sent for beyond the last tile
-    if (active) {
-#pragma unroll
-      for (int f = 0; f < KS; ++f)
-        {
-          const bf16x8 v = frag(value_frag(k_tile(tile1 + 3) + TILE + HALF, f));
-          o[f % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, frag(pb.p[f / DB]), o[f % DB], 0, 0, 0);
-          if constexpr (FINE) o[f % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, frag(pb.rest[f / DB]), o[f % DB], 0, 0, 0);
-        }
-      if (__builtin_expect(partly(tile1 - 1) && not_finite != 0, 0)) {
-        for (int key = max(seen_by_all, tile0 * kManyKeys); key < min(of.len, tile1 * kManyKeys); ++key) {
-          const int at = table[key >> a.pool.page_log2];
-          if (at < 0 || at >= a.pool.n_pages || key >= limit) continue;
-          const unsigned char* from = a.pool.v + a.layer + head * a.pool.s_head + at * a.pool.s_page + (key & in_page) * a.pool.s_tok;
+          for (int i = 0; i < 16; ++i) t = fmaxf(t, z[i]);
+          t *= a.c;
+          t = fmaxf(t, __shfl_xor(t, 32));
+          const float to = fmaxf(m, t), old = to == m ? 1.0f : __builtin_amdgcn_exp2f(m - to);
+          m = to;
+          l *= old;
 #pragma unroll
           for (int db = 0; db < DB; ++db)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const f32x4 v = row4<FP8>(from + (db * 32 + i * 8 + half * 4) * (FP8 ? 1 : 2));
+            for (int i = 0; i < 16; ++i) o[db][i] *= old;
+          sum = 0.0f;
 #pragma unroll
-              for (int e = 0; e < 4; ++e) o[db][4 * i + e] = with_the_rest(o[db][4 * i + e], v[e]);
-            }
+          for (int i = 0; i < 16; i += 2) {
+            const float x = __builtin_amdgcn_exp2f(fmaf(z[i], a.c, -m)), y = __builtin_amdgcn_exp2f(fmaf(z[i + 1], a.c, -m));
+            sum += x + y;
+            pack(p, i, x, y);
+          }
+        }
+        l += sum;
+      };
+
+      // ---- before the first tile
+      __syncthreads();                                             // the segment before is through with LDS
+      if (tid == 0) not_finite = 0;
+#pragma unroll
+      for (int j = 0; j < (ROWWISE ? 5 : 3); ++j) fetch_entries((ROWWISE ? tile0 : tile0 >> 4) + j);
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+      for (int j = 0; j < 3; ++j) {
+        const Place from = k_place(tile0 + j);
+        fetch_keys(tile0 + j, from);
+        fetch_values(tile0 + j, v_place(tile0 + j, from));
+        if (j < 2) { park(tile0 + j, 0); park(tile0 + j, 1); park(tile0 + j, 2); park(tile0 + j, 3); }
+      }
+      // in front of the first tile: values of zero
+      for (int i = tid; i < HALF / 16; i += kManyThreads) *reinterpret_cast<u32x4*>(k_tile(tile0 + 3) + TILE + HALF + i * 16) = u32x4{0, 0, 0, 0};
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(SENT) : "memory");
+      uint64_t valid = ROWWISE ? is_there(tile0, entry(tile0, lane)) : 0;
+      uint64_t held = ROWWISE ? 0 : __ballot(is_page(entries[(tile0 >> 4) & 3][lane]));          // groups of 16 keys of the stretch whose pages there are
+      if (active) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) za[i] = 0.0f;
+#pragma unroll
+        for (int f = 0; f < KS; ++f) za = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(key_frag(k_tile(tile0), f)), frag(qf[f]), za, 0, 0, 0);
+#pragma unroll
+        for (int f = 0; f < RING - 1; ++f) fill(f, k_tile(tile0) + HALF, k_tile(tile0 + 3) + TILE + HALF);
+      }
+      for (int tile = tile0; tile < tile1; ++tile) {
+        bool masked = tile >= plain_end;
+        if constexpr (ROWWISE) {
+          masked |= valid != ~0ull;
+        } else {
+          if ((tile & 15) == 13) fetch_entries((tile >> 4) + 2);   // three tiles ahead a new stretch begins: the one after it
+          if ((tile & 15) == 0) held = __ballot(is_page(entries[(tile >> 4) & 3][lane]));
+          masked |= (((unsigned)(held >> ((tile & 15) * 4)) & 15u) != 15u);
+          if (masked) valid = is_there(tile, entry(tile, lane));
+        }
+        if (__builtin_expect(masked, 0)) clean_values(tile, valid);
+        const unsigned char *t0 = k_tile(tile), *t1 = k_tile(tile + 1), *before = k_tile(tile + 3);
+        // All of this step's LDS reads are on their way by the last places: from there on the tile before is nobody's, and the next one is everybody's.
+        auto pass_on = [&](int f) __attribute__((always_inline)) {
+          if (f == F - (RING - 1)) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(SENT + (ROWWISE ? 1 : 0)) : "memory");
+        };
+        Place k_from = {0, 0}, v_from = {0, 0};
+        int next_entry = 0;
+        auto send_for = [&](int f) __attribute__((always_inline)) {
+          if (ROWWISE && f == 0) next_entry = entry(tile + 1, lane);
+          if (f < 4) park(tile + 2, f);                            // before the next ones are sent for below
+          if (f == 1) k_from = k_place(tile + 3);
+          if (f == 2) v_from = v_place(tile + 3, k_from);
+          if (f == 3) fetch_keys(tile + 3, k_from);
+          if (f == 4) fetch_values(tile + 3, v_from);
+          if (f == 5 && ROWWISE) fetch_entries(tile + 5);
+        };
+        if (active) {
+          step(za, pa, zb, t0 + HALF, pb, before + TILE + HALF, t1, t0 + TILE, tile * kManyKeys, masked, (unsigned)valid, pass_on);
+          step(zb, pb, za, t1, pa, t0 + TILE, t1 + HALF, t0 + TILE + HALF, tile * kManyKeys + 32, masked, (unsigned)(valid >> 32), send_for);
+        } else {
+          pass_on(F - (RING - 1));
+#pragma unroll
+          for (int f = 0; f < F; ++f) send_for(f);
+        }
+        if constexpr (ROWWISE) valid = is_there(tile + 1, next_entry);
+      }
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // what was sent for beyond the last tile
+      if (active) {
+#pragma unroll
+        for (int f = 0; f < KS; ++f)
+          {
+            const bf16x8 v = frag(value_frag(k_tile(tile1 + 3) + TILE + HALF, f));
+            o[f % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, frag(pb.p[f / DB]), o[f % DB], 0, 0, 0);
+            if constexpr (FINE) o[f % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, frag(pb.rest[f / DB]), o[f % DB], 0, 0, 0);
+          }
+        if (__builtin_expect(partly(tile1 - 1) && not_finite != 0, 0)) {
+          for (int key = max(seen_by_all, tile0 * kManyKeys); key < min(of.len, tile1 * kManyKeys); ++key) {
+            const int at = table[key >> a.pool.page_log2];
+            if (at < 0 || at >= a.pool.n_pages || key >= limit) continue;
+            const unsigned char* from = a.pool.v + a.layer + head * a.pool.s_head + at * a.pool.s_page + (key & in_page) * a.pool.s_tok;
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const f32x4 v = row4<FP8>(from + (db * 32 + i * 8 + half * 4) * (FP8 ? 1 : 2));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[db][4 * i + e] = with_the_rest(o[db][4 * i + e], v[e]);
+              }
+          }
+        }
+        const float sum = l + __shfl_xor(l, 32);
+        if (row < of.rows && whole) {
+          const int t = row / of.G, h = head * of.G + row - t * of.G;
+          const float inv = sum == 0.0f ? 0.0f : a.pool.v_scale / sum;
+          uint16_t* out = a.out + (q0 + t) * a.b.o_st + h * a.b.o_sh + half * 4;
+#pragma unroll
+          for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              *reinterpret_cast<u32x2*>(out + db * 32 + i * 8) =
+                  u32x2{pack2(o[db][4 * i] * inv, o[db][4 * i + 1] * inv), pack2(o[db][4 * i + 2] * inv, o[db][4 * i + 3] * inv)};
+          if (a.lse && half == 0) a.lse[(int64_t)(q0 + t) * a.b.Hq + h] = sum == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kLn2;
+        } else if (row < of.rows) {
+          const int64_t part = (int64_t)slot * kManyRows + wave * 32 + l32;
+#pragma unroll
+          for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              *reinterpret_cast<f32x4*>(a.part_o + part * D + db * 32 + i * 8 + half * 4) = f32x4{o[db][4 * i], o[db][4 * i + 1], o[db][4 * i + 2], o[db][4 * i + 3]};
+          if (half == 0) { a.part_ml[2 * part] = m; a.part_ml[2 * part + 1] = sum; }
         }
       }
-      const float sum = l + __shfl_xor(l, 32);
-      if (row < of.rows && whole) {
-        const int t = row / of.G, h = head * of.G + row - t * of.G;
-        const float inv = sum == 0.0f ? 0.0f : a.pool.v_scale / sum;
-        uint16_t* out = a.out + (q0 + t) * a.b.o_st + h * a.b.o_sh + half * 4;
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<u32x2*>(out + db * 32 + i * 8) =
-                u32x2{pack2(o[db][4 * i] * inv, o[db][4 * i + 1] * inv), pack2(o[db][4 * i + 2] * inv, o[db][4 * i + 3] * inv)};
-        if (a.lse && half == 0) a.lse[(int64_t)(q0 + t) * a.b.Hq + h] = sum == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kLn2;
-      } else if (row < of.rows) {
-        const int64_t part = (int64_t)slot * kManyRows + wave * 32 + l32;
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<f32x4*>(a.part_o + part * D + db * 32 + i * 8 + half * 4) = f32x4{o[db][4 * i], o[db][4 * i + 1], o[db][4 * i + 2], o[db][4 * i + 3]};
-        if (half == 0) { a.part_ml[2 * part] = m; a.part_ml[2 * part + 1] = sum; }
-      }
-    }
     }
     if (start <= x0) break;
     if (--block < 0) {                                           // the request before, or the head before
