@@ -2,6 +2,8 @@
 #include <float.h>
 #include <math.h>
 
+#include <algorithm>
+
 #include "attend_many.h"
 
 namespace codecomp {
@@ -23,7 +25,8 @@ extern template int launch_many_of<128, true, false>(const ManyArgs&, hipStream_
 constexpr int kFewRows = 32, kFewRowsMost = 64;
 constexpr int64_t kFewKeysMost = 1 << 17;        // keys of all requests and KV heads, at their largest, up to which kFewRowsMost holds for bf16
 // In a batch with longer chunks, the short requests of a bf16 cache go along with them, with fewer launches and at the bandwidth that long ones have
-// (512 tokens over 4096 keys and 64 steps of one over 4096: 161 us apart, 138 together; 10 tokens and 64 steps over 16384: 399, 369).  From an 8-bit
+// (512 tokens over 4096 keys and 64 steps over 500 .. 4096: 132 us apart, 103 together; 2048 over 8192 and 64 over 500 .. 16384: 393, 328; 10 tokens over
+// 100 and the same 250, 226; head_dim 64 73, 73; 245, 251; 131, 112).  From an 8-bit
 // cache only so many of them as the launches cost, in tiles of the many-row kernel, which widens every tile for a whole block's rows (4 steps over 4096
 // keys 76 apart, 71 together; 8 of them 78, 79; 64 of them 114, 192).
 constexpr int64_t kAlongTiles = 1024;
@@ -76,12 +79,17 @@ int make_attend_plan(const codecomp_batch* b, const codecomp_pages* p, AttendPla
   pl->row_parts = (few_most + 31) / 32;
   pl->row_slots = few_most;
   const int64_t items = (int64_t)x.n_seqs * x.Hkv;
-  // chunks of keys: about two workgroups per compute unit if all requests are of the largest length, of at least 128 keys each (one tile for each wave)
+  // chunks of keys: about two workgroups per compute unit if all requests are of the largest length, of at least 128 keys each (one tile for each wave; 256: 1 us more for one request)
   // and at most 2048 (one token over 131072 keys, 4 KV heads: chunks of 512 58 us, of 1024 55, of 4096 68; 64 requests of 500 .. 16384 keys, 8 bits: 512
   // 215, 1024 200, 2048 199, 4096 209)
   int64_t chunk = (items * x.max_kv / 512 + 127) / 128 * 128;
   if (chunk < 128) chunk = 128;
   if (chunk > 2048) chunk = 2048;
+  // One chunk of short caches: no join, which costs 4 us and more with many requests (one step, us, one chunk | several: 200 keys, 1 request 8.3 | 11.9;
+  // 400 keys 11 | 11, 64 requests 13.9 | 19; 800 keys 15 | 11.7, 21 | 27; 8 bits 400 keys 8.4 | 10, 10.5 | 15; 800 keys 10.8 | 10.2, 13.4 | 18; 4 tokens
+  // over 400 keys, 64 requests 16 | 30).
+  const int once = (p->head_dim * (pl->pool.fp8 ? 1 : 2) <= 128 ? 512 : 256) << (items >= 256 ? 2 : items >= 64 ? 1 : 0);
+  if (x.max_kv <= std::min(once, 1024)) chunk = 1024;
   // so many at most: the list of a row's chunks stands in LDS, and an axis of a grid holds 2^32 threads
   while ((x.max_kv + chunk - 1) / chunk > kFewMostSplits || (x.max_kv > chunk && items * pl->row_parts * ((x.max_kv + chunk - 1) / chunk) > kMostFewBlocks)) chunk *= 2;
   pl->chunk = (int)chunk;
