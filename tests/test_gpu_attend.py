@@ -192,6 +192,16 @@ def test_garbage_in_places_that_are_not_seen(news, n_q, d, fp8):
         assert torch.equal(got[:at_token], clean[:at_token]) and not bool(torch.isfinite(got[at_token: news[0]]).any())
 
 
+@pytest.mark.parametrize("news, n_q", [([1, 1], 8), ([6, 3], 8), ([9, 14], 8), ([3, 14], 8)])
+@pytest.mark.parametrize("d, fp8", [(128, False), (64, True), (64, False)])
+def test_garbage_where_lengths_may_be_long(monkeypatch, news, n_q, d, fp8):
+    """The same with a bound on lengths that selects equal parts, and fine weights in the many-row kernel."""
+    cache, batch = cu_.Cache, cu_.make_batch
+    monkeypatch.setattr(cu_, "Cache", lambda rng, lens, **kw: cache(rng, lens, width_more=1 << 16, **kw))
+    monkeypatch.setattr(cu_, "make_batch", lambda c, news, n_q: batch(c, news, n_q, max_kv=1 << 20))
+    test_garbage_in_places_that_are_not_seen(news, n_q, d, fp8)
+
+
 @pytest.mark.parametrize("news", [[1, 2], [100, 40]])
 def test_scales_at_the_ends_of_fp32(news):
     """Logits that all vanish: every key weighs the same, hidden ones still nothing."""
@@ -311,6 +321,39 @@ def test_parts_are_joined_by_their_log_sum_exp():
     assert torch.allclose(top, lse, atol=2e-6, rtol=0)
     bound = cu_.HALF_BF16 * (whole.abs() + a.abs() + z.abs()) + 1e-4
     assert bool(((joined - whole).abs() <= bound).all())
+
+
+@pytest.mark.parametrize("news", [[1, 1, 1], [4, 1, 0], [9, 1, 2], [70, 1, 1]])
+def test_captured_calls_of_large_batches(news):
+    """As below, for what a large bound on lengths selects: equal parts of all keys, chunks in the many-row kernel, and steps beside them."""
+    rng = np.random.default_rng([28, news[0]])
+    top = [3000, 500, 200]
+    c = cu_.Cache(rng, top, n_kv=2, d=128, page=64, width_more=17000)
+    batch, cu = cu_.make_batch(c, news, 8, max_kv=1 << 20)
+    lens, table, pages = batch._keep[2], batch._keep[3], c.pages()
+    q = cu_.bf16(rng.standard_normal((sum(news), 8, 128))).cuda()
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:2], device="cuda")
+    ws = cu_.workspace(batch, pages)
+    run = lambda: b.codecomp_attend(q, batch, pages, 0, out, ws, lse=lse)  # noqa: E731
+    run()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        run()
+    for i in range(4):
+        now = [max(n, int(x)) for n, x in zip(news, rng.integers(0, top))]
+        lens.copy_(torch.tensor(now, dtype=torch.int32))
+        c.table[c.table >= 0] = rng.permutation(c.n_pages).astype(np.int32)[: int((c.table >= 0).sum())]
+        table.copy_(torch.from_numpy(c.table))
+        q.copy_(cu_.bf16(rng.standard_normal(q.shape)))
+        ws.fill_(0xFF)
+        g.replay()
+        torch.cuda.synchronize()
+        got, got_lse = out.clone(), lse.clone()
+        run()
+        assert torch.equal(out, got) and torch.equal(lse, got_lse)
+        want = orc.attend(cu_.f64(q), *c.values(), c.table, now, cu, max_kv_len=1 << 20)
+        cu_.assert_attended(got, got_lse, want, 128)
 
 
 @pytest.mark.parametrize("news", [[1, 1, 1], [40, 1, 30]])
