@@ -39,26 +39,28 @@ struct ManyArgs {
 
 // Tiles of 64 keys that a block of rows of a request meets; at least one.
 struct Blocks {
-  int len, nq, G, rows, count, causal;
+  int len, q0, nq, G, rows, count, causal;       // keys, first new token, new tokens, query heads per KV head, rows, blocks of them
   __device__ __forceinline__ int tiles(int block) const {
     int keys = len;
     if (causal) keys = min(len, len - nq + (min(block * kManyRows + kManyRows, rows) - 1) / G + 1);
     return max(1, (keys + kManyKeys - 1) / kManyKeys);
   }
 };
-__device__ __forceinline__ Blocks blocks_of(const ManyArgs& m, int r) {
+__device__ __forceinline__ Blocks blocks_of(const ManyArgs& m, int len, int q0, int nq) {
   Blocks x;
-  x.len = kv_len_of(m.a.b, r);
-  x.nq = m.a.b.cu_q[r + 1] - m.a.b.cu_q[r];
+  x.len = len; x.q0 = q0; x.nq = nq;
   x.G = m.a.b.G;
   x.rows = x.nq * x.G;
   x.count = x.rows >= m.rows_from ? (x.rows + kManyRows - 1) / kManyRows : 0;
   x.causal = m.a.b.causal;
   return x;
 }
+__device__ __forceinline__ Blocks blocks_of(const ManyArgs& m, int r) {
+  return blocks_of(m, kv_len_of(m.a.b, r), m.a.b.cu_q[r], m.a.b.cu_q[r + 1] - m.a.b.cu_q[r]);
+}
 
 __device__ __forceinline__ Blocks uniform(Blocks x) {
-  x.len = uniform(x.len); x.nq = uniform(x.nq); x.rows = uniform(x.rows); x.count = uniform(x.count);
+  x.len = uniform(x.len); x.q0 = uniform(x.q0); x.nq = uniform(x.nq); x.rows = uniform(x.rows); x.count = uniform(x.count);
   return x;
 }
 
@@ -99,8 +101,16 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
   // threads to count their blocks, then blocks to count their tiles (one each, mostly: a prompt alone has many).
   const int n = a.b.n_seqs, per = (n + kManyThreads - 1) / kManyThreads;
   auto weight = [&](int tiles) { return ma.whole ? 1 : kManyLead + tiles; };       // positions of a block
+  // Up to 512 requests are kept in LDS: the loads of what follows are short then.
+  __shared__ int requests[3][kManyThreads];
+  const bool kept = n <= kManyThreads;
+  auto request = [&](int r) __attribute__((always_inline)) { return kept ? blocks_of(ma, requests[0][r], requests[1][r], requests[2][r]) : blocks_of(ma, r); };
   int my_blocks = 0;
-  for (int r = min(tid * per, n); r < min(tid * per + per, n); ++r) my_blocks += blocks_of(ma, r).count;
+  for (int r = min(tid * per, n); r < min(tid * per + per, n); ++r) {
+    const Blocks x = blocks_of(ma, r);
+    my_blocks += x.count;
+    if (kept) { requests[0][r] = x.len; requests[1][r] = x.q0; requests[2][r] = x.nq; }
+  }
   int blocks = my_blocks;                                        // up to here, inclusive
 #pragma unroll
   for (int off = 1; off < 64; off <<= 1) {
@@ -129,11 +139,11 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
       if (first_block[lo + step] <= b0) lo += step;
     my_r = lo * per;
     my_i = b0 - first_block[lo];
-    Blocks x = blocks_of(ma, my_r);
-    while (my_i >= x.count) { my_i -= x.count; x = blocks_of(ma, ++my_r); }
+    Blocks x = request(my_r);
+    while (my_i >= x.count) { my_i -= x.count; x = request(++my_r); }
     int r = my_r, i = my_i;
     for (int b = b0; b < b1; ++b, ++i) {
-      while (i >= x.count) { i = 0; x = blocks_of(ma, ++r); }
+      while (i >= x.count) { i = 0; x = request(++r); }
       mine += weight(x.tiles(i));
     }
   }
@@ -167,10 +177,10 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
     const int64_t at = x1 - 1 - head * per_head;
     int64_t start = before + incl - mine;
     if (at >= start && at < start + mine) {                      // one thread has it
-      Blocks y = blocks_of(ma, my_r);
+      Blocks y = request(my_r);
       int r = my_r, i = my_i;
       for (;; ++i) {
-        while (i >= y.count) { i = 0; y = blocks_of(ma, ++r); }
+        while (i >= y.count) { i = 0; y = request(++r); }
         const int positions = weight(y.tiles(i));
         if (at < start + positions) break;
         start += positions;
@@ -181,7 +191,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
   __syncthreads();
   int r = uniform(found[0]), block = uniform(found[1]);
   int64_t start = uniform(x1 - 1 - found[2]);                     // position of the block
-  Blocks of = uniform(blocks_of(ma, r));
+  Blocks of = uniform(request(r));
   CutBlock cut = {-1, 0, 0, 0};
 
   for (;;) {
@@ -193,7 +203,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
       const int slot = tile0 > 0 ? 2 * g : 2 * g + 1;
       if (tile0 == 0 && tile1 < tiles)                             // the rest of the block is the next workgroups'
         cut = {r, block, head, (int)(((first + tiles) * workgroups - 1) / total)};
-      const int q0 = uniform(a.b.cu_q[r]), row0 = block * kManyRows + wave * 32, row = row0 + l32;
+      const int q0 = of.q0, row0 = block * kManyRows + wave * 32, row = row0 + l32;
       const bool active = row0 < of.rows;
 
       // query rows as right operands, and the keys that the lane's rows see
@@ -509,7 +519,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
     if (--block < 0) {                                           // the request before, or the head before
       do {
         if (--r < 0) { r = n - 1; --head; }
-        of = uniform(blocks_of(ma, r));
+        of = uniform(request(r));
       } while (of.count == 0);
       block = of.count - 1;
     }
