@@ -13,7 +13,8 @@
 // vector instructions for half the products: 480 to 505 us, 0.93 to 0.97 PFLOP/s.  8-bit caches: 815 and 516 us, the codes are widened on the way to LDS.
 // Before it: waves with 512 registers (the compiler keeps the accumulators in the half that vector instructions do not reach, and copies them); the page
 // table looked up key by key (790 us; as one load per 1024 keys 760).
-// Sending for a part's first tiles behind the last ones of the part before took as much time in the loop as it saved between parts.
+// Sending for a part's first tiles behind the last ones of the part before took as much time in the loop as it saved between parts; sending for them
+// before the outputs are written, and writing these in whole rows by way of LDS, changed nothing or took registers that the loop needs.
 #pragma once
 #include "attend.h"
 
