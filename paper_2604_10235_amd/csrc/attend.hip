@@ -24,16 +24,16 @@ extern template int launch_many_of<128, true, false>(const ManyArgs&, hipStream_
 // (the many-row one with rounded ones: 64 requests 191).
 constexpr int kFewRows = 32, kFewRowsMost = 64;
 constexpr int64_t kFewKeysMost = 1 << 17;        // keys of all requests and KV heads, at their largest, up to which kFewRowsMost holds for bf16
-// In a batch with longer chunks, the short requests of a bf16 cache go along with them, with fewer launches and at the bandwidth that long ones have
-// (512 tokens over 4096 keys and 64 steps over 500 .. 4096: 132 us apart, 103 together; 2048 over 8192 and 64 over 500 .. 16384: 393, 328; 10 tokens over
-// 100 and the same 250, 226; head_dim 64 73, 73; 245, 251; 131, 112).  From an 8-bit
-// cache only so many of them as the launches cost, in tiles of the many-row kernel, which widens every tile for a whole block's rows (4 steps over 4096
-// keys 76 apart, 71 together; 8 of them 78, 79; 64 of them 114, 192).
-constexpr int64_t kAlongTiles = 1024;
+// In a batch with longer chunks, up to kAlongBlocks short requests (times KV heads) of a bf16 cache go along with them, with fewer launches and at the
+// bandwidth that long ones have (512 tokens over 4096 keys and 64 steps over 500 .. 4096: 132 us apart, 90 together; 2048 over 8192 and 64 over 500 ..
+// 16384: 393, 354; head_dim 64 73, 59; 245, 226; and 256 steps over 100 .. 1000 125, 109; over 50 .. 300 87, 91; but 1000 over 50 .. 300 158, 229: a block
+// of rows that is cut short costs its start).  From an 8-bit
+constexpr int64_t kAlongTiles = 1024, kAlongBlocks = 1024;
 
 // Cache bytes (at the largest lengths) from which the keys of several requests of few rows are cut into equal parts instead of chunks: all workgroups
 // run at once and end together, for 5 us more before the first key and for the parts (64 steps over 500 .. 16384 keys, 4 KV heads of 128: 210 us in
-// chunks, 190 in parts; 8 bits 118, 103; 16 over 300 .. 9000 45, 37, 8 bits 25.7, 25.9; 64 over 8192 192, 196; one over 131072 57, 64).  Two workgroups
+// chunks, 190 in parts; 8 bits 118, 103; 16 over 300 .. 9000 45, 37, 8 bits 25.7, 25.9; 64 over 8192 192, 196; one over 131072 57, 64).  Not where a
+// request is one chunk: no join to begin with (1000 steps over 100 .. 1000 keys 223, 235; 8 bits, head_dim 64 52, 87).  Two workgroups
 // per compute unit: with three or four 195 and 198.
 constexpr int64_t kEvenBytes = 1 << 28;
 constexpr int kShares = 512;
@@ -63,7 +63,8 @@ int make_attend_plan(const codecomp_batch* b, const codecomp_pages* p, AttendPla
     if (few_most <= kFewRows || pl->pool.fp8 || (int64_t)pl->few_rows * x.Hkv * x.max_kv <= kFewKeysMost) break;
     few_limit = kFewRows;
   }
-  if (pl->many_rows > 0 && (!pl->pool.fp8 || (int64_t)pl->few_rows * x.Hkv * ((x.max_kv + kManyKeys - 1) / kManyKeys) <= kAlongTiles)) {
+  const int64_t few_blocks = (int64_t)pl->few_rows * x.Hkv, few_tiles = few_blocks * ((x.max_kv + kManyKeys - 1) / kManyKeys);
+  if (pl->many_rows > 0 && (pl->pool.fp8 ? few_tiles <= kAlongTiles : few_blocks <= kAlongBlocks)) {
     pl->many_rows += pl->few_rows;
     pl->few_rows = few_most = 0;
   }
@@ -96,7 +97,7 @@ int make_attend_plan(const codecomp_batch* b, const codecomp_pages* p, AttendPla
   pl->splits = x.max_kv > chunk ? (int)((x.max_kv + chunk - 1) / chunk) : 1;
   if (pl->few_rows > 0 && (items * pl->row_parts > kMostFewBlocks || items * pl->row_slots > kMostFewBlocks)) return CODECOMP_EINVAL_SHAPE;
   const int64_t bytes = (int64_t)pl->few_rows * x.Hkv * x.max_kv * p->head_dim * (pl->pool.fp8 ? 2 : 4);
-  pl->shares = pl->few_rows > 1 && pl->row_parts == 1 && bytes > kEvenBytes ? kShares : 0;
+  pl->shares = pl->few_rows > 1 && pl->row_parts == 1 && pl->splits > 1 && bytes > kEvenBytes ? kShares : 0;
   size_t off = 0;
   pl->off_few = off;
   if (pl->shares > 0) off = align256(off + (size_t)pl->shares * (2 * (size_t)pl->row_slots * (p->head_dim + 2) * sizeof(float) + sizeof(CutBlock)));

@@ -374,9 +374,12 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void atten
     if constexpr (!EVEN) return;
     if (left <= 0) break;
     strip = 0;
-    do {                                                           // the next request, or the next head
-      if (++r == a.b.n_seqs) { r = 0; ++head; }
-    } while (uniform(strips_of(a, r)) == 0);
+    for (++r;;) {                                                  // the next request with strips, or the first one of the next head: 64 at a time
+      const uint64_t some = __ballot(r + lane < a.b.n_seqs && strips_of(a, min(r + lane, a.b.n_seqs - 1)) > 0);
+      if (some != 0) { r += __builtin_ctzll(some); break; }
+      r += 64;
+      if (r >= a.b.n_seqs) { r = 0; ++head; }
+    }
     __syncthreads();                                               // through with LDS
   }
   if (tid == 0) a.cuts[share] = cut;

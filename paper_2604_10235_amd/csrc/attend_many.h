@@ -22,14 +22,17 @@ namespace codecomp {
 
 constexpr int kManyRows = 256, kManyKeys = 64, kManyWaves = 8, kManyThreads = 64 * kManyWaves;
 
-// Positions in front of the tiles of a block, in the sequence that is cut into equal parts: starting on a block (its queries, the first tiles) and
-// ending it cost 11 us at head_dim 128 and 5 at 64, of 1.65 and 1.2 us a tile (a prompt of 4096 tokens, us, with 3 | 4 | 5 | 7 | 10 | 14 positions: 185 |
+// Blocks of rows are cut into equal parts by positions, kManyTile of them to a tile, and fewer to a tile of a block of up to 32 rows, which
+// takes as long as its keys need (512 tokens over 4096 keys and 64 steps over 500 .. 4096, head_dim 64: 70 us with 8 positions each, 59; 128: 98, 90).
+constexpr int kManyTile = 8, kManyLight64 = 5, kManyLight128 = 6;
+// Tiles' worth of positions in front of a block's tiles: starting on a block (its queries, the first tiles) and
+// ending it cost 11 us at head_dim 128 and 5 at 64, of 1.65 and 1.2 us a tile (a prompt of 4096 tokens, us, with 3 | 4 | 5 | 7 | 10 | 14: 185 |
 // 170 | 155 | 141 | 146 | 149; head_dim 64 114 | 103 | 97 | 95).
 constexpr int kManyLead = 7;
 // Reference of a row before its first visible key: finite, so that hidden logits (minus infinity) less it still are minus infinity, and so low that a
 // visible one's weight overflows, which makes it the reference.
 constexpr float kNoReference = -3.402823466e38f;
-constexpr int kManyLeast = 4;   // positions that a workgroup gets at least (with 8 a prompt of 100 tokens takes 32 us instead of 23)
+constexpr int kManyLeast = 4;   // tiles' worth that a workgroup gets at least (with 8 a prompt of 100 tokens takes 32 us instead of 23)
 
 struct ManyArgs {
   AttendArgs a;
@@ -101,10 +104,12 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
   // ---- this workgroup's share: the tiles of all blocks of all heads form one sequence, cut into equal parts.  Requests are shared out over the
   // threads to count their blocks, then blocks to count their tiles (one each, mostly: a prompt alone has many).
   const int n = a.b.n_seqs, per = (n + kManyThreads - 1) / kManyThreads;
-  auto weight = [&](int tiles) { return ma.whole ? 1 : kManyLead + tiles; };       // positions of a block
-  // Up to 512 requests are kept in LDS: the loads of what follows are short then.
-  __shared__ int requests[3][kManyThreads];
-  const bool kept = n <= kManyThreads;
+  // positions of a tile and of a block
+  auto per_tile = [&](const Blocks& x, int block) { return x.rows - block * kManyRows > 32 ? kManyTile : D == 64 ? kManyLight64 : kManyLight128; };
+  auto weight = [&](const Blocks& x, int block) { return ma.whole ? 1 : kManyLead * kManyTile + x.tiles(block) * per_tile(x, block); };
+  // Up to 2048 requests are kept in LDS: the loads of what follows are short then.
+  __shared__ int requests[3][4 * kManyThreads];
+  const bool kept = n <= 4 * kManyThreads;
   auto request = [&](int r) __attribute__((always_inline)) { return kept ? blocks_of(ma, requests[0][r], requests[1][r], requests[2][r]) : blocks_of(ma, r); };
   int my_blocks = 0;
   for (int r = min(tid * per, n); r < min(tid * per + per, n); ++r) {
@@ -145,7 +150,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
     int r = my_r, i = my_i;
     for (int b = b0; b < b1; ++b, ++i) {
       while (i >= x.count) { i = 0; x = request(++r); }
-      mine += weight(x.tiles(i));
+      mine += weight(x, i);
     }
   }
   int64_t incl = mine;
@@ -165,7 +170,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
   }
   per_head = uniform(per_head);
   const int64_t total = per_head * a.b.Hkv;
-  const int64_t workgroups = min((int64_t)ma.workgroups, ma.whole ? total : (total + kManyLeast - 1) / kManyLeast);
+  const int64_t workgroups = min((int64_t)ma.workgroups, ma.whole ? total : (total + kManyLeast * kManyTile - 1) / (kManyLeast * kManyTile));
   if (tid == 0 && blockIdx.x >= workgroups && !ma.whole) ma.cuts[blockIdx.x].r = -1;
   // neighbours in the sequence read the same keys: they run on the same die (workgroups go to the eight dies in turn)
   const int per_die = ((int)workgroups + 7) / 8, g = (int)(blockIdx.x & 7) * per_die + (int)(blockIdx.x >> 3);
@@ -182,7 +187,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
       int r = my_r, i = my_i;
       for (;; ++i) {
         while (i >= y.count) { i = 0; y = request(++r); }
-        const int positions = weight(y.tiles(i));
+        const int positions = weight(y, i);
         if (at < start + positions) break;
         start += positions;
       }
@@ -197,13 +202,15 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
 
   for (;;) {
     const int tiles = uniform(of.tiles(block));
-    const int64_t first = start + kManyLead;                      // position of its first tile
-    const int tile0 = ma.whole ? 0 : uniform((int)max(x0 - first, (int64_t)0)), tile1 = ma.whole ? tiles : uniform((int)min(x1 - first, (int64_t)tiles));
+    const int64_t first = start + kManyLead * kManyTile;          // position of its first tile
+    const int each = uniform(per_tile(of, block));
+    auto tiles_before = [&](int64_t x) { return uniform((int)min((max(x - first, (int64_t)0) + each - 1) / each, (int64_t)tiles)); };        // that begin before x
+    const int tile0 = ma.whole ? 0 : tiles_before(x0), tile1 = ma.whole ? tiles : tiles_before(x1);
     if (tile1 > tile0) {
       const bool whole = tile0 == 0 && tile1 == tiles;
       const int slot = tile0 > 0 ? 2 * g : 2 * g + 1;
       if (tile0 == 0 && tile1 < tiles)                             // the rest of the block is the next workgroups'
-        cut = {r, block, head, (int)(((first + tiles) * workgroups - 1) / total)};
+        cut = {r, block, head, (int)(((first + (int64_t)(tiles - 1) * each + 1) * workgroups - 1) / total)};
       const int q0 = of.q0, row0 = block * kManyRows + wave * 32, row = row0 + l32;
       const bool active = row0 < of.rows;
 
@@ -517,14 +524,18 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
       }
     }
     if (start <= x0) break;
-    if (--block < 0) {                                           // the request before, or the head before
-      do {
-        if (--r < 0) { r = n - 1; --head; }
-        of = uniform(request(r));
-      } while (of.count == 0);
+    if (--block < 0) {                                           // the request before that has blocks, or the last one of the head before: 64 at a time
+      for (;;) {
+        const int candidate = r - 1 - lane;
+        const uint64_t some = __ballot(candidate >= 0 && request(max(candidate, 0)).count > 0);
+        if (some != 0) { r -= 1 + __builtin_ctzll(some); break; }
+        r -= 64;
+        if (r <= 0) { r = n; --head; }
+      }
+      of = uniform(request(r));
       block = of.count - 1;
     }
-    start -= weight(uniform(of.tiles(block)));
+    start -= uniform(weight(of, block));
   }
   if (tid == 0 && !ma.whole) ma.cuts[g] = cut;
 }

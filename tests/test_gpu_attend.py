@@ -67,6 +67,20 @@ def test_shares(lens, news, n_q, n_kv, d, page):
     check(rng, c, news, n_q)
 
 
+@pytest.mark.parametrize("n", [600, 3000])
+@pytest.mark.parametrize("fp8", [False, True])
+def test_many_requests_and_few_tokens(n, fp8):
+    """Runs of requests without tokens, between ones with few and with many, over two heads."""
+    rng = np.random.default_rng([29, n])
+    news = [90 if r % 290 == 7 else 1 if r % 3 == 0 and r % 500 < 200 else 0 for r in range(n)]
+    lens = [int(x) for x in rng.integers(0, 40, n)]
+    lens[7], lens[297] = 400, 131
+    c = cu_.Cache(rng, lens, n_kv=2, d=64, page=16, fp8=fp8, width_more=40, k_scale=0.03 if fp8 else 1.0, v_scale=0.02 if fp8 else 1.0)
+    check(rng, c, news, 4)                                        # short lengths: blocks that are not shared
+    check(rng, c, news, 4, max_kv=1000)
+    check(rng, c, [1 if x == 1 or r == 7 else 0 for r, x in enumerate(news)], 4, weight_bits=16)
+
+
 # Requests of few rows whose bound on lengths makes the batch a large one: keys of all of them cut into equal parts, which end inside requests, hold
 # several, or are less than 128 keys; requests without keys or tokens, more of them than a workgroup has threads, pages that are not held.
 @pytest.mark.parametrize("lens, news, n_q, n_kv, d, fp8", [
