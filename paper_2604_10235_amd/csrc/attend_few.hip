@@ -307,7 +307,8 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void atten
     }
 
     if (__builtin_expect(__ballot(left_out != 0) != 0, 0)) {
-      for (int key = max(seen_by_all, key0); key < key1; ++key) {
+      // from the first tile that was cleaned on: the keys before seen_by_all in it were as well
+      for (int key = max(seen_by_all & -kFewKeys, key0); key < key1; ++key) {
         const int at = table[key >> a.pool.page_log2];
         if ((key - key0) / kFewKeys % kFewWaves != wave || at < 0 || at >= a.pool.n_pages) continue;          // another wave's
         const unsigned char* row = a.pool.v + a.layer + head * a.pool.s_head + at * a.pool.s_page + (key & in_page) * a.pool.s_tok;

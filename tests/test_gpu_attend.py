@@ -506,3 +506,33 @@ def test_from_compression_to_single_steps(fp8):
     b.codecomp_pages_compact(pages, dev(table[:1]), None, dev(kept), again, pages, dev(new_table))
     caches[:] = [[[[a[::2] for a in caches[0][l][h]] for h in range(Hkv)] for l in range(L)]]
     tokens(1, 1, m, new_table)
+
+
+# Values of rows that all new tokens see, in the tile where some rows are not seen by all, and before it; chunks, equal parts, both kernels, small pages.
+@pytest.mark.parametrize("news, n_q", [([1, 1], 8), ([6, 3], 8), ([9, 14], 8), ([150, 90], 1), ([40, 300], 8)])
+@pytest.mark.parametrize("d, fp8", [(128, False), (64, True), (64, False), (128, True)])
+@pytest.mark.parametrize("page, max_kv", [(16, 400), (8, 400), (256, 1 << 20)])
+def test_infinities_and_nan_among_values_that_are_seen(news, n_q, d, fp8, page, max_kv):
+    """One element of one value row: that element of every token that sees the row is infinite or NaN, everything else keeps its bits."""
+    rng = np.random.default_rng([31, d, page, news[0]])
+    lens = [333, 310]
+    c = cu_.Cache(rng, lens, n_kv=1, d=d, page=page, fp8=fp8, width_more=max_kv // page + 1, k_scale=0.03 if fp8 else 1.0, v_scale=0.02 if fp8 else 1.0)
+    batch, cu = cu_.make_batch(c, news, n_q, max_kv=max_kv)
+    q = cu_.bf16(rng.standard_normal((sum(news), n_q, d))).cuda()
+    ws = cu_.workspace(batch, c.pages())
+    clean, lse, got, got_lse = torch.empty_like(q), torch.empty(sum(news), n_q, device="cuda"), torch.empty_like(q), torch.empty(sum(news), n_q, device="cuda")
+    b.codecomp_attend(q, batch, c.pages(), 0, clean, ws, lse=lse)
+    raw = c.v.view(torch.uint8) if fp8 else c.v
+    own = lens[0] - news[0]                                             # row of the first new token: the last that all see
+    for key in sorted({0, own - 1, own, (own + 1) // 32 * 32, (own + 1) // 64 * 64, (own + 1) // 64 * 64 - 1, own + news[0] // 2, lens[0] - 1}):
+        p, at = orc.place(c.table, 0, key, page, c.n_pages)
+        for x in [0x7F, 0xFF] if fp8 else [float("nan"), float("inf"), -float("inf")]:
+            keep, e = raw[0, p, 0, at].clone(), int(rng.integers(d))
+            raw[0, p, 0, at, e] = x
+            b.codecomp_attend(q, batch, c.pages(), 0, got, ws, lse=got_lse)
+            raw[0, p, 0, at] = keep
+            sees = max(0, key - own)                                    # tokens of request 0 from there on
+            hit = torch.zeros_like(got, dtype=torch.bool)
+            hit[sees: news[0], :, e] = True
+            assert not bool(torch.isfinite(got[hit]).any()), (key, x)
+            assert torch.equal(got[~hit], clean[~hit]) and torch.equal(got_lse, lse), (key, x)
