@@ -351,8 +351,7 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void atten
         for (int i = 0; i < E; ++i) x[i] = 0.0f;
 #pragma unroll
         for (int w = 0; w < kFewWaves; ++w) {
-          const float f = row_m[w][n] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(row_m[w][n] - to);
-          if (row_m[w][n] == -INFINITY && !(row_l[w][n] != row_l[w][n])) continue;          // saw nothing
+          const float f = row_m[w][n] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(row_m[w][n] - to);       // times zeros, or an infinity or NaN that it saw
           all += f * row_l[w][n];
 #pragma unroll
           for (int i = 0; i < E; ++i) x[i] += f * o_lds[(w * 16 + n) * O_ROW + e + i];

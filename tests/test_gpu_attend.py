@@ -536,3 +536,24 @@ def test_infinities_and_nan_among_values_that_are_seen(news, n_q, d, fp8, page, 
             hit[sees: news[0], :, e] = True
             assert not bool(torch.isfinite(got[hit]).any()), (key, x)
             assert torch.equal(got[~hit], clean[~hit]) and torch.equal(got_lse, lse), (key, x)
+
+
+@pytest.mark.parametrize("news", [1, 90])
+@pytest.mark.parametrize("max_kv", [200, 5000])
+def test_infinite_values_of_weight_zero(news, max_kv):
+    """Keys that give a logit of minus infinity weigh nothing, and nothing times an infinite value is NaN."""
+    rng = np.random.default_rng(32)
+    c = cu_.Cache(rng, [152], n_kv=1, d=64, page=8, width_more=max_kv // 8)
+    batch, _ = cu_.make_batch(c, [news], 2, max_kv=max_kv, causal=False)
+    q = cu_.bf16(rng.standard_normal((news, 2, 64))).cuda()
+    q[..., 3] = 1.0
+    for j in range(32, 64):                       # all keys that a wave has
+        p, at = orc.place(c.table, 0, j, 8, c.n_pages)
+        c.k[0, p, 0, at, 3] = -float("inf")
+    out, ws = torch.empty_like(q), cu_.workspace(batch, c.pages())
+    b.codecomp_attend(q, batch, c.pages(), 0, out, ws)
+    assert bool(torch.isfinite(out).all())
+    p, at = orc.place(c.table, 0, 40, 8, c.n_pages)
+    c.v[0, p, 0, at, 7] = float("inf")
+    b.codecomp_attend(q, batch, c.pages(), 0, out, ws)
+    assert bool(torch.isnan(out[..., 7]).all()) and bool(torch.isfinite(out[..., :7]).all())
