@@ -76,7 +76,8 @@ typedef struct codecomp_batch {
  *   (x0, x1) -> magnitude * (x0 cos a - x1 sin a, x0 sin a + x1 cos a)
  * Pairs are elements (i, i + dim / 2), or (2 i, 2 i + 1) when interleaved.  inverse: by -a, which with the same
  * magnitude is the gradient at the input from the gradient at the output (the transpose).
- * Angles are reduced exactly, in turns of 64 bits: a position of 2^31 is as good as one of 1. */
+ * Angles are reduced in turns of 64 bits, to which any frequency is rounded once: at position 2^31 they are off by 2^-34 of a turn, less than fp32 can
+ * tell.  The inverse at a position is bit for bit the rotation at minus the position. */
 typedef struct codecomp_rotary {
   int32_t dim;                 /* a multiple of 16, 0 .. head_dim                                                */
   int32_t interleaved;

@@ -5,8 +5,8 @@
 // Measured: 32768 tokens of 40 heads of 128 elements 115 us, 5.8 TB/s (a large copy reaches 5.0); four chunks of together 10500 tokens into an FP8
 // cache 62 us, 4.2 TB/s; 16 tokens 3.3 us, of which the launch and one chain of loads are all.
 // The angle of a far position loses all its digits in fp32 (p * freq at 10^6 has steps of 0.06 rad): it is formed in turns as a 64-bit
-// fraction, whose product with a whole position wraps around where the angle does, exactly.  What is left of it after taking out the nearest
-// quarter turn is at most pi / 4, known to 2^-27 of a turn, where the Taylor series of sine and cosine to the 9th and 10th power are good to 2e-9 and 2e-9
+// fraction (rounded once, on the host), whose product with a whole position wraps around where the angle does.  What is left of it after taking out the nearest
+// quarter turn is at most pi / 4, known to 2^-27 of a turn, where the Taylor series of sine and cosine to the 9th and 10th power are good to 2e-9 and 1.2e-10
 // (pi/4^11 / 11!, pi/4^12 / 12!).
 #include "cache.h"
 

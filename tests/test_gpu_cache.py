@@ -279,3 +279,48 @@ def test_pages_copy(fp8, d, page, n_kv, layers):
         want_k[:, z], want_v[:, z] = want_k[:, a], want_v[:, a]
     b.codecomp_pages_copy(c.pages(), torch.from_numpy(pairs).cuda())
     assert np.array_equal(raw(c.k), want_k) and np.array_equal(raw(c.v), want_v)
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_angles_of_far_positions_and_any_frequency(interleaved):
+    """Against angles reduced with 1 / (2 pi) in whole numbers of 1500 bits (pi by Machin's formula): the error does not grow with the position or the
+    frequency, and the inverse is the rotation at minus the position."""
+    bits = 1500
+    def arctan_of_one_over(x):
+        term = total = (1 << bits + 64) // x
+        k, sign = 3, -1
+        while term:
+            term //= x * x
+            total, sign, k = total + sign * (term // k), -sign, k + 2
+        return total
+    pi = (16 * arctan_of_one_over(5) - 4 * arctan_of_one_over(239)) >> 64
+    per_radian = (1 << 2 * bits) // (2 * pi)                              # 2^1500 / (2 pi)
+    freqs = [1.0, 12345.678, 1e6 + 0.1, 2.0 ** 52 + 1, 2.0 ** 53 + 2, 1e15, 1e22, 1e100, 1e300, 1.7e308, 5e-324, 2.0 ** -70, 3e-11, 1e-5, 0.7, 0.0, -0.3, -98765.4, -1e40,
+             3.0, 6.283185307179586, 100.0, 2.0 ** 63 + 2048, 1e-3, 1e-8, 2.0 ** 64, 1e19, 2.0 ** 117, 31.4159, 1e9, 7e4, 1e-19]
+    pos = np.array(POSITIONS + [2**31 - 2, -(2**31) + 1, 987654321], np.int32)
+    rng = np.random.default_rng(33)
+    x = cu_.bf16(rng.standard_normal((len(pos), 3, 64)))
+    rot = b.make_rotary(64, interleaved=interleaved)
+    rot.freq[:32] = freqs
+    out = torch.empty_like(x, device="cuda")
+    b.codecomp_rotate(x.cuda(), torch.from_numpy(pos).cuda(), rot, out)
+    angle = np.zeros((len(pos), 32))
+    for i, p in enumerate(pos):
+        for j, f in enumerate(freqs):
+            num, den = float(f).as_integer_ratio()
+            turns = (num * int(p) * per_radian // den) & ((1 << bits) - 1)
+            angle[i, j] = 2 * np.pi * ((turns >> (bits - 64)) / 2.0 ** 64)
+    xf = cu_.f64(x)
+    x0, x1 = (xf[..., 0::2], xf[..., 1::2]) if interleaved else (xf[..., :32], xf[..., 32:])
+    c, s = np.cos(angle)[:, None], np.sin(angle)[:, None]
+    y0, y1 = x0 * c - x1 * s, x0 * s + x1 * c
+    want = np.stack([y0, y1], -1).reshape(xf.shape) if interleaved else np.concatenate([y0, y1], -1)
+    off, tol = np.abs(cu_.f64(out) - want), rotary_tolerance(want, xf, pos * 0, np.zeros(1), 1.0)
+    assert np.all(off <= tol), (float((off / tol).max()), np.unravel_index(np.argmax(off / tol), off.shape))
+    # the transpose, exactly: also for the smallest frequencies
+    near = pos[pos > -(2**31)]
+    back, turned = torch.empty_like(out[: len(near)]), torch.empty_like(out[: len(near)])
+    b.codecomp_rotate(x[: len(near)].cuda(), torch.from_numpy(-near).cuda(), rot, turned)
+    rot.inverse = 1
+    b.codecomp_rotate(x[: len(near)].cuda(), torch.from_numpy(near).cuda(), rot, back)
+    assert torch.equal(back, turned)
