@@ -363,8 +363,8 @@ def _int32(t, shape, what: str):
 def make_batch(*, n_q_heads: int, cu_q_host: np.ndarray, cu_q, kv_lens, table, max_kv_len: int, causal: bool = True, softmax_scale: float = 0.0,
                **strides) -> codecomp_batch:
     """New tokens of n_seqs requests over their caches.  cu_q, kv_lens, table: device int32 tensors [n_seqs + 1], [n_seqs], [n_seqs, width]; the host
-    array cu_q_host (same values as cu_q) sizes the launches.  Strides of q, of new k and v, and of what comes out: 0 or left out = dense."""
-    host = np.ascontiguousarray(cu_q_host, dtype=np.int32)
+    array cu_q_host (same values as cu_q; copied) sizes the launches.  Strides of q, of new k and v, and of what comes out: 0 or left out = dense."""
+    host = np.array(cu_q_host, dtype=np.int32, order="C")        # a copy: calls read it, long after the tensors were checked against it
     n = len(host) - 1
     _int32(cu_q, (n + 1,), "cu_q")
     _int32(kv_lens, (n,), "kv_lens")

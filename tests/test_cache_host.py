@@ -302,3 +302,13 @@ def test_binding_refuses_broadcast_and_scattered_tensors():
     x, p = b.make_batch(**good), b.make_pages(bf(1, 3, 2, 16, 64), bf(1, 3, 2, 16, 64))
     with pytest.raises(ValueError, match="workspace"):
         b.codecomp_attend(bf(3, 4, 64), x, p, 0, bf(3, 4, 64), torch.zeros(1, dtype=torch.uint8).expand(1 << 20))
+
+
+def test_a_batch_keeps_its_own_token_offsets():
+    """The array that sizes the launches may be used again for the next batch: the tensors of the first are still checked against what it was made with."""
+    import torch
+    i32 = lambda *s: torch.zeros(*s, dtype=torch.int32)  # noqa: E731
+    cu = np.array([0, 2, 3], np.int32)
+    x = b.make_batch(n_q_heads=4, cu_q_host=cu, cu_q=i32(3), kv_lens=i32(2), table=i32(2, 3), max_kv_len=48)
+    cu[1:] = 1000, 2000
+    assert (C.c_int32 * 3).from_address(x.cu_q_host)[:] == [0, 2, 3] and x._tokens == 3
