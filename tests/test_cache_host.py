@@ -304,6 +304,17 @@ def test_binding_refuses_broadcast_and_scattered_tensors():
         b.codecomp_attend(bf(3, 4, 64), x, p, 0, bf(3, 4, 64), torch.zeros(1, dtype=torch.uint8).expand(1 << 20))
 
 
+@pytest.mark.parametrize("cu, over, kv", [((0, 1), dict(max_kv_len=5000), {}), ((0, 1, 2), dict(max_kv_len=1 << 18), {}), ((0, 400), dict(max_kv_len=5000), {}),
+                                           ((0, 9), dict(max_kv_len=1 << 18), {}), ((0, 9, 400), dict(max_kv_len=1 << 18), dict(kv_dtype=1))])
+def test_attend_refuses_workspaces_that_do_not_hold_its_parts(cu, over, kv):
+    """One token over chunks of keys, tokens over equal parts, a prompt, a short chunk, both kernels."""
+    x, p = batch(cu, table_width=1 << 14, **over), pool(**kv)
+    need = b.lib().codecomp_attend_workspace_bytes(C.byref(x), C.byref(p))
+    assert need > 0
+    for bad in (dict(ws=None), dict(ws=D + 16), dict(ws=D + 128), dict(size=need - 1), dict(size=0)):
+        assert attend(x, p, **bad) == -9, bad
+
+
 def test_a_batch_keeps_its_own_token_offsets():
     """The array that sizes the launches may be used again for the next batch: the tensors of the first are still checked against what it was made with."""
     import torch

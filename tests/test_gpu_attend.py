@@ -557,3 +557,50 @@ def test_infinite_values_of_weight_zero(news, max_kv):
     c.v[0, p, 0, at, 7] = float("inf")
     b.codecomp_attend(q, batch, c.pages(), 0, out, ws)
     assert bool(torch.isnan(out[..., 7]).all()) and bool(torch.isfinite(out[..., :7]).all())
+
+
+def guarded(monkeypatch):
+    """Workspaces of exactly the bytes asked for, with a pattern behind them; returns what checks the pattern."""
+    made = []
+    def workspace(batch, pages):
+        n = b.codecomp_attend_workspace_bytes(batch, pages)
+        whole = torch.full((n + (1 << 16),), 0xFF, dtype=torch.uint8, device="cuda")
+        whole[n:] = 0xA5
+        made.append((whole, n))
+        return whole[:n]
+    monkeypatch.setattr(cu_, "workspace", workspace)
+    def intact():
+        assert made and all(bool((w[n:] == 0xA5).all()) for w, n in made)
+        return [n for _, n in made]
+    return intact
+
+
+# Both kernels in one call, each with a workspace: equal parts of many steps beside a chunk, chunks of keys beside one (up to 32 rows, and 33 to 64), from 8 bits
+# equal parts as well.
+@pytest.mark.parametrize("short, count, long, n_q, n_kv, d, fp8, max_kv", [
+    (1, 300, 90, 8, 4, 64, False, 5000), (2, 260, 40, 16, 4, 128, False, 3000), (1, 12, 90, 4, 2, 64, True, 4096), (5, 12, 90, 16, 2, 128, True, 4096),
+    (9, 12, 70, 8, 2, 64, True, 4096), (1, 12, 90, 4, 2, 128, True, 1 << 20)])
+@pytest.mark.parametrize("causal", [True, False])
+def test_both_kernels_share_a_workspace(monkeypatch, short, count, long, n_q, n_kv, d, fp8, max_kv, causal):
+    intact = guarded(monkeypatch)
+    rng = np.random.default_rng([35, count, d])
+    news = [short] * count
+    news[count // 2], news[3] = long, 0
+    lens = [int(x) for x in rng.integers(0, 60, count)]
+    lens[0], lens[count // 2], lens[-1] = min(max_kv, 2700), min(max_kv, 1900), 1100
+    c = cu_.Cache(rng, lens, n_kv=n_kv, d=d, page=64, fp8=fp8, width_more=max_kv // 64 - 40, k_scale=0.03 if fp8 else 1.0, v_scale=0.02 if fp8 else 1.0)
+    check(rng, c, news, n_q, causal=causal, max_kv=max_kv)
+    both, = intact()
+    alone, _ = cu_.make_batch(c, [long if r == count // 2 else 0 for r in range(count)], n_q, max_kv=max_kv)
+    assert both > b.codecomp_attend_workspace_bytes(alone, c.pages()) > 0
+
+
+@pytest.mark.parametrize("lens, news, n_q, n_kv, d, fp8, max_kv", [
+    ([3000, 90], [1, 2], 4, 2, 64, False, 3000), ([3000, 900, 7], [9, 1, 3], 4, 1, 128, True, 3000), ([3000, 90, 0], [1, 1, 1], 8, 2, 128, False, 1 << 20),
+    ([3000, 800], [300, 90], 2, 2, 128, False, 3000), ([3000, 800], [700, 1], 4, 2, 64, True, 3000), ([1300, 140], [9, 16], 8, 2, 64, False, 100000)])
+def test_workspaces_are_not_written_beyond(monkeypatch, lens, news, n_q, n_kv, d, fp8, max_kv):
+    intact = guarded(monkeypatch)
+    rng = np.random.default_rng([36, d, news[0]])
+    c = cu_.Cache(rng, lens, n_kv=n_kv, d=d, page=256, fp8=fp8, width_more=max_kv // 256, k_scale=0.03 if fp8 else 1.0, v_scale=0.02 if fp8 else 1.0)
+    check(rng, c, news, n_q, max_kv=max_kv)
+    assert intact()[0] > 0
