@@ -324,3 +324,81 @@ def test_angles_of_far_positions_and_any_frequency(interleaved):
     rot.inverse = 1
     b.codecomp_rotate(x[: len(near)].cuda(), torch.from_numpy(near).cuda(), rot, back)
     assert torch.equal(back, turned)
+
+
+# Calls long enough for four heads a thread (more than 3 * 2^16 units of 16 elements), whose last group is not full; append: groups of query, key and value heads.
+@pytest.mark.parametrize("T, H, d, dim, inter, inverse, scaling, magnitude", [
+    (1401, 18, 128, 128, False, False, "plain", 1.0), (1401, 18, 128, 64, True, True, "wavelength", 1.0), (10007, 5, 64, 64, True, False, "ramp", 1.1386),
+    (7111, 7, 64, 32, False, True, "base", 0.5), (24600, 1, 128, 96, False, False, "linear", 1.0)])
+def test_rotate_of_long_calls(T, H, d, dim, inter, inverse, scaling, magnitude):
+    assert T * H * (d // 16) > 3 << 16
+    rng = np.random.default_rng([T, H, dim])
+    fused = cu_.bf16(rng.standard_normal((T, H + 2, d))).cuda()                 # strided: two more heads behind those that are rotated
+    x, pos = fused[:, :H], rng.integers(-(2**31), 2**31, T).astype(np.int32)
+    kw = dict(factor=4.0, context=8192.0, low=1.0, high=32.0)
+    rot = b.make_rotary(dim, scaling=b.ROTARY_SCALINGS[scaling], interleaved=inter, inverse=inverse, magnitude=magnitude, **kw)
+    freq = orc.frequencies(dim, 10000.0, scaling, **kw)
+    out, dev_pos = torch.full((T + 1, H, d), 7.0, dtype=torch.bfloat16, device="cuda"), torch.from_numpy(pos).cuda()
+    b.codecomp_rotate(x, dev_pos, rot, out[:T])
+    xf, got = cu_.f64(x), cu_.f64(out[:T])
+    want = orc.rotate(xf, pos, freq, interleaved=inter, inverse=inverse, magnitude=magnitude)
+    off, tol = np.abs(got - want), rotary_tolerance(want, xf, pos, freq, magnitude)
+    assert np.all(off <= tol), float((off / tol).max())
+    assert np.array_equal(got[..., dim:], xf[..., dim:]) and bool((out[T] == 7.0).all())
+    few = torch.empty((50, H, d), dtype=torch.bfloat16, device="cuda")              # a short call of the same tokens: the same bits
+    b.codecomp_rotate(x[-50:], dev_pos[-50:], rot, few)
+    assert torch.equal(few, out[T - 50: T])
+    behind = fused[:, H:].clone()
+    b.codecomp_rotate(x, dev_pos, rot, x)                                           # in place
+    assert torch.equal(x, out[:T]) and torch.equal(fused[:, H:], behind)
+
+
+LONG_APPENDS = [
+    ([701, 0, 33, 650], [901, 5, 33, 650], 14, 2, 128, 128, False, False, 16), ([701, 0, 33, 650], [901, 5, 40, 650], 14, 2, 128, 64, True, True, 64),
+    ([5001, 4990], [5001, 6000], 3, 1, 64, 64, False, True, 8), ([1, 5003, 2, 5001], [9, 5010, 2, 5001], 3, 1, 64, 32, True, False, 1),
+    ([1300, 1301], [1300, 1400], 5, 5, 128, 0, False, False, 32)]
+
+
+@pytest.mark.parametrize("news, lens, n_q, n_kv, d, dim, inter, fp8, page", LONG_APPENDS)
+def test_append_of_long_chunks(news, lens, n_q, n_kv, d, dim, inter, fp8, page):
+    assert sum(news) * (n_q + 2 * n_kv) * (d // 16) > 3 << 16 and (n_q + 2 * n_kv) % 4 != 0
+    test_append(news, lens, n_q, n_kv, d, dim, inter, fp8, page)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_append_of_long_chunks_in_place_and_without_queries(fp8):
+    """Queries rotated in place, or none given: the pages get the same bits as from the call that writes elsewhere, and as from short calls."""
+    rng = np.random.default_rng(34)
+    news, n_q, n_kv, d = [4100, 4301], 6, 3, 64
+    scales = dict(k_scale=0.02, v_scale=0.0125) if fp8 else {}
+    c = cu_.Cache(rng, [4200, 4301], n_kv=n_kv, d=d, page=32, fp8=fp8, **scales)
+    T, rot, pages = sum(news), b.make_rotary(d), c.pages()
+    fused = cu_.bf16(rng.standard_normal((T, n_q + 2 * n_kv, d))).cuda()
+    wide = (n_q + 2 * n_kv) * d
+    q, k, v = fused[:, :n_q], fused[:, n_q: n_q + n_kv], fused[:, n_q + n_kv:]
+    pos = torch.from_numpy(rng.integers(0, 10**6, T).astype(np.int32)).cuda()
+    apart, cu = cu_.make_batch(c, news, n_q, q_stride_tok=wide, new_stride_tok=wide)
+    inside, _ = cu_.make_batch(c, news, n_q, q_stride_tok=wide, new_stride_tok=wide, out_stride_tok=wide)
+    was = raw(c.k).copy(), raw(c.v).copy()
+    out = torch.empty((T, n_q, d), dtype=torch.bfloat16, device="cuda")
+    b.codecomp_append(q, k, v, pos, rot, apart, pages, 0, out)
+    want = raw(c.k).copy(), raw(c.v).copy()
+    def again(run):
+        for t, x in ((c.k, was[0]), (c.v, was[1])):
+            (t.view(torch.uint8) if fp8 else t.view(torch.int16)).copy_(torch.from_numpy(x))
+        run()
+        assert np.array_equal(raw(c.k), want[0]) and np.array_equal(raw(c.v), want[1])
+    behind = fused[:, n_q:].clone()
+    keep = q.clone()
+    again(lambda: b.codecomp_append(q, k, v, pos, rot, inside, pages, 0, q))
+    assert torch.equal(q, out) and torch.equal(fused[:, n_q:], behind)
+    q.copy_(keep)
+    assert T * 2 * n_kv * (d // 16) > 3 << 16
+    again(lambda: b.codecomp_append(None, k, v, pos, rot, apart, pages, 0, None))
+    def by_parts():
+        for lo in range(0, 4400, 400):
+            part = [max(0, min(400, n - lo)) for n in news]
+            at = torch.cat([torch.arange(cu[r] + lo, cu[r] + lo + n) for r, n in enumerate(part)]).cuda()
+            x, _ = cu_.make_batch(c, part, n_q, lens=[length - n + lo + m for length, n, m in zip(c.lens, news, part)])
+            b.codecomp_append(None, k[at].contiguous(), v[at].contiguous(), pos[at].contiguous(), rot, x, pages, 0, None)
+    again(by_parts)
