@@ -152,7 +152,7 @@ size_t codecomp_attend_workspace_bytes(const codecomp_batch* batch, const codeco
  * A token that sees no row (or rows of pages that are not held alone) gets out = 0, lse = -inf.  What stands in rows that a token
  * does not see, NaN and infinities too, has no part in its result.  An infinity or NaN in a value that it does see makes that element of its result infinite or NaN, whatever the
  * weight; one in its query or in a key that it sees may make all of it so.  Logits, sums and outputs are fp32; the weights enter the second
- * product rounded to bf16, or as two bf16, 16 bits together, where all requests of the batch have up to 64 rows (new tokens * query heads per KV head).
+ * product rounded to bf16, or as two bf16, 16 bits together, for requests of up to 64 rows (new tokens * query heads per KV head).
  * workspace: >= codecomp_attend_workspace_bytes(), 256-byte aligned, contents on entry do not matter; NULL when that is 0.
  * Calls that may run at the same time need workspaces of their own. */
 int codecomp_attend(const void* q, const codecomp_batch* batch, const codecomp_pages* pages, int32_t layer, void* out, float* lse,

@@ -18,8 +18,7 @@ ROCM = os.environ.get("ROCM_PATH", "/opt/rocm")
 SOURCES = ["score_pass_d128_bf16.hip", "score_pass_d128_fp8.hip", "score_pass_d64_bf16.hip", "score_pass_d64_fp8.hip",
            "score_team_d128_bf16.hip", "score_team_d128_fp8.hip", "score_once_d128.hip", "score_once_d64.hip", "api.hip", "score.hip", "select.hip", "gather.hip", "structure.hip", "static_scratch.hip",
            "cache_api.hip", "rotary.hip", "pages.hip", "attend.hip", "attend_few.hip",
-           "attend_many_d128_bf16.hip", "attend_many_d128_fp8.hip", "attend_many_d64_bf16.hip", "attend_many_d64_fp8.hip",
-           "attend_many_d128_bf16_fine.hip", "attend_many_d64_bf16_fine.hip"]
+           "attend_many_d128_bf16.hip", "attend_many_d128_fp8.hip", "attend_many_d64_bf16.hip", "attend_many_d64_fp8.hip"]
 # packed fp32 VALU ops are switched off on purpose (device pass only; the host pass ignores it)
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-I", os.path.join(ROOT, "include"),
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wno-unused-command-line-argument"]

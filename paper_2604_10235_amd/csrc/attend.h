@@ -17,6 +17,8 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // lose nothing in fp32 or in bf16, and most tiles then leave the sums and the outputs as they are.
 constexpr float kSlack = 8.0f;
 
+constexpr int kFewRowsMost = 64;          // rows of a request up to which weights are two bf16, in either kernel, and most rows that the one for few takes
+
 // What a workgroup leaves for the kernel that joins rows whose keys several workgroups had.
 struct CutBlock {
   int32_t r, block, head;      // of the block of rows whose first part is this workgroup's (slot 2 * workgroup + 1); r < 0: none

@@ -8,12 +8,10 @@
 
 namespace codecomp {
 
-extern template int launch_many_of<64, false, false>(const ManyArgs&, hipStream_t);
-extern template int launch_many_of<64, false, true>(const ManyArgs&, hipStream_t);
-extern template int launch_many_of<64, true, false>(const ManyArgs&, hipStream_t);
-extern template int launch_many_of<128, false, false>(const ManyArgs&, hipStream_t);
-extern template int launch_many_of<128, false, true>(const ManyArgs&, hipStream_t);
-extern template int launch_many_of<128, true, false>(const ManyArgs&, hipStream_t);
+extern template int launch_many_of<64, false>(const ManyArgs&, hipStream_t);
+extern template int launch_many_of<64, true>(const ManyArgs&, hipStream_t);
+extern template int launch_many_of<128, false>(const ManyArgs&, hipStream_t);
+extern template int launch_many_of<128, true>(const ManyArgs&, hipStream_t);
 
 // Which kernel a request takes goes by its rows (new tokens x query heads per KV head; figures in us for 28 query heads on 4 KV heads of 128
 // elements, few | many rows' kernel).  Up to kFewRows it is attend_few_kernel's, which gives a chunk of keys to a workgroup: 4 tokens over 8192 keys 15 |
@@ -22,13 +20,19 @@ extern template int launch_many_of<128, true, false>(const ManyArgs&, hipStream_
 // over 8192 keys 353 | 204; and always from an 8-bit cache: 17 | 24, 31 | 39, 59 | 69, 205 | 205.  Beyond, a third and a fourth workgroup do not pay
 // from 8192 keys on (18 tokens over 32768 keys 57 | 44; over 2000 15 | 21).  Up to kFewRowsMost, weights enter the product as two bf16 in either kernel
 // (the many-row one with rounded ones: 64 requests 191).
-constexpr int kFewRows = 32, kFewRowsMost = 64;
+constexpr int kFewRows = 32;
 constexpr int64_t kFewKeysMost = 1 << 17;        // keys of all requests and KV heads, at their largest, up to which kFewRowsMost holds for bf16
-// In a batch with longer chunks, up to kAlongBlocks short requests (times KV heads) of a bf16 cache go along with them, with fewer launches and at the
-// bandwidth that long ones have (512 tokens over 4096 keys and 64 steps over 500 .. 4096: 132 us apart, 90 together; 2048 over 8192 and 64 over 500 ..
-// 16384: 393, 354; head_dim 64 73, 59; 245, 226; and 256 steps over 100 .. 1000 125, 109; over 50 .. 300 87, 91; but 1000 over 50 .. 300 158, 229: a block
-// of rows that is cut short costs its start).  From an 8-bit
-constexpr int64_t kAlongTiles = 1024, kAlongBlocks = 1024;
+// In a batch with longer chunks, short requests go along with them while they are few: fewer launches, and the bandwidth that long ones have.  Beyond, what
+// starting on a block costs, and one wave's work for its tiles, take longer than a kernel and a join of their own.  Most of them, as blocks of rows (requests times KV
+// heads) and as tiles of keys (at the largest length); us, 4 KV heads, apart | along.
+// head_dim 128: beside 512 tokens over 4096 keys 64 steps over 500 .. 4000 125 | 95, 256 of them 277 | 242; beside 2048 over 8192 64 over 8000 .. 16384
+// 502 | 436; beside a prompt of 20 64 over 300 .. 1000 41 | 37, 256 97 | 101; 256 over 50 .. 300 beside 512 tokens 88 | 91, 1000 158 | 229.
+// head_dim 64 has half the bytes for as much of a wave's work: 64 over 500 .. 4000 73 | 66, 128 94 | 104; 64 over 300 .. 1000 beside a prompt of 20 29 | 29, 128 37 | 45;
+// 16 over 8000 .. 16384 beside 512 tokens 86 | 78, 64 196 | 214; (lost: 128 over 300 .. 1000 beside 2048 over 8192 158 | 145).
+// 8 bits, every tile of which is widened for a whole block's rows: beside 512 tokens over 4096 keys 4 over 4000 67 | 57 (head_dim 64 49 | 44), 16 72 | 69 (50 | 50), 64
+// 102 | 135 (64 | 97); beside a prompt of 20 33 | 27 (27 | 22), 39 | 41 (31 | 33), 69 | 107 (45 | 81).
+struct Along { int64_t blocks, tiles; };
+constexpr Along kAlong128 = {1024, INT64_MAX}, kAlong64 = {256, 1 << 15}, kAlongFp8 = {INT64_MAX, 1 << 10};
 
 // Cache bytes (at the largest lengths) from which the keys of several requests of few rows are cut into equal parts instead of chunks: all workgroups
 // run at once and end together, for 5 us more before the first key and for the parts (64 steps over 500 .. 16384 keys, 4 KV heads of 128: 210 us in
@@ -63,17 +67,16 @@ int make_attend_plan(const codecomp_batch* b, const codecomp_pages* p, AttendPla
     if (few_most <= kFewRows || pl->pool.fp8 || (int64_t)pl->few_rows * x.Hkv * x.max_kv <= kFewKeysMost) break;
     few_limit = kFewRows;
   }
+  const Along along = pl->pool.fp8 ? kAlongFp8 : pl->d == 64 ? kAlong64 : kAlong128;
   const int64_t few_blocks = (int64_t)pl->few_rows * x.Hkv, few_tiles = few_blocks * ((x.max_kv + kManyKeys - 1) / kManyKeys);
-  if (pl->many_rows > 0 && (pl->pool.fp8 ? few_tiles <= kAlongTiles : few_blocks <= kAlongBlocks)) {
+  if (pl->many_rows > 0 && few_blocks <= along.blocks && few_tiles <= along.tiles) {
     pl->many_rows += pl->few_rows;
     pl->few_rows = few_most = 0;
   }
   pl->many_from = pl->few_rows > 0 ? few_limit + 1 : 1;
   int64_t blocks = 0;
-  pl->many_fine = !pl->pool.fp8;       // (an 8-bit cache's requests of up to 64 rows are the other kernel's)
   for (int r = 0; r < x.n_seqs; ++r) {
     const int64_t rows = (int64_t)(b->cu_q_host[r + 1] - b->cu_q_host[r]) * x.G;
-    if (rows > kFewRowsMost) pl->many_fine = 0;
     if (rows >= pl->many_from) blocks += (rows + kManyRows - 1) / kManyRows;
   }
   pl->many_blocks = blocks * x.Hkv < INT32_MAX ? (int)(blocks * x.Hkv) : INT32_MAX;
@@ -153,12 +156,8 @@ static int launch_many(const AttendPlan& pl, const AttendArgs& a, char* workspac
   m.a.part_ml = m.a.part_o + (size_t)pl.workgroups * 2 * kManyRows * pl.d;
   m.cuts = reinterpret_cast<CutBlock*>(m.a.part_ml + (size_t)pl.workgroups * 2 * kManyRows * 2);
   int rc;
-  if (pl.many_fine) {
-    rc = pl.d == 128 ? launch_many_of<128, false, true>(m, stream) : launch_many_of<64, false, true>(m, stream);
-  } else {
-    if (pl.d == 128) rc = pl.pool.fp8 ? launch_many_of<128, true, false>(m, stream) : launch_many_of<128, false, false>(m, stream);
-    else rc = pl.pool.fp8 ? launch_many_of<64, true, false>(m, stream) : launch_many_of<64, false, false>(m, stream);
-  }
+  if (pl.d == 128) rc = pl.pool.fp8 ? launch_many_of<128, true>(m, stream) : launch_many_of<128, false>(m, stream);
+  else rc = pl.pool.fp8 ? launch_many_of<64, true>(m, stream) : launch_many_of<64, false>(m, stream);
   if (rc || pl.many_whole) return rc;
   // A few blocks of many parts: their rows over more workgroups (20 tokens over 131072 keys 83 us, 16 rows each 96, 64 rows each 213); many blocks of
   // a part or two: fewer workgroups (12 x 1024 tokens over 4096 keys, head_dim 64: 8 rows each 125, 16 124).

@@ -16,15 +16,18 @@
 // Sending for a part's first tiles behind the last ones of the part before took as much time in the loop as it saved between parts; sending for them
 // before the outputs are written, and writing these in whole rows by way of LDS, changed nothing or took registers that the loop needs.
 #pragma once
+#include <type_traits>
+
 #include "attend.h"
 
 namespace codecomp {
 
 constexpr int kManyRows = 256, kManyKeys = 64, kManyWaves = 8, kManyThreads = 64 * kManyWaves;
 
-// Blocks of rows are cut into equal parts by positions, kManyTile of them to a tile, and fewer to a tile of a block of up to 32 rows, which
-// takes as long as its keys need (512 tokens over 4096 keys and 64 steps over 500 .. 4096, head_dim 64: 70 us with 8 positions each, 59; 128: 98, 90).
-constexpr int kManyTile = 8, kManyLight64 = 5, kManyLight128 = 6;
+// Blocks of rows are cut into equal parts by positions, kManyTile of them to a tile, and kManyLight to a tile of a block of up to 32 rows, one wave's, whose
+// weights are two bf16 (512 tokens over 4096 keys and 64 steps over 500 .. 4096, us, with 5 | 6 | 7 | 8 | 9: 76 | 73 | 70 | 74 | 77 at head_dim 64,
+// - | 102 | 102 | 107 | 109 at 128; 2048 over 8192 and 64 over 500 .. 16384: 279 | 255 | 247 | 244 | 255; - | 372 | 356 | 353 | 370).
+constexpr int kManyTile = 8, kManyLight = 7;
 // Tiles' worth of positions in front of a block's tiles: starting on a block (its queries, the first tiles) and
 // ending it cost 11 us at head_dim 128 and 5 at 64, of 1.65 and 1.2 us a tile (a prompt of 4096 tokens, us, with 3 | 4 | 5 | 7 | 10 | 14: 185 |
 // 170 | 155 | 141 | 146 | 149; head_dim 64 114 | 103 | 97 | 95).
@@ -79,8 +82,7 @@ struct TileAt {
 };
 
 // ROWWISE: pages of less than 16 rows; else the 16 rows that a wave loads of a tile lie in one page, whose place is worked out in scalar registers.
-// FINE: weights as two bf16.
-template <int D, bool FP8, bool ROWWISE, bool FINE>
+template <int D, bool FP8, bool ROWWISE>
 __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const ManyArgs ma) {
   const AttendArgs& a = ma.a;
   constexpr int PIECES = D * (FP8 ? 1 : 2) / 16;               // 16-byte pieces of a stored row
@@ -105,7 +107,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
   // threads to count their blocks, then blocks to count their tiles (one each, mostly: a prompt alone has many).
   const int n = a.b.n_seqs, per = (n + kManyThreads - 1) / kManyThreads;
   // positions of a tile and of a block
-  auto per_tile = [&](const Blocks& x, int block) { return x.rows - block * kManyRows > 32 ? kManyTile : D == 64 ? kManyLight64 : kManyLight128; };
+  auto per_tile = [&](const Blocks& x, int block) { return x.rows - block * kManyRows > 32 ? kManyTile : kManyLight; };
   auto weight = [&](const Blocks& x, int block) { return ma.whole ? 1 : kManyLead * kManyTile + x.tiles(block) * per_tile(x, block); };
   // Up to 2048 requests are kept in LDS: the loads of what follows are short then.
   __shared__ int requests[3][4 * kManyThreads];
@@ -325,7 +327,11 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[db][i] = 0.0f;
       f32x16 za, zb;                                               // logits of the first and of the second 32 keys of a tile
-      struct Weights {                                             // their weights, 16 keys each; FINE: rounded, and the rest
+      // The tiles, with weights rounded to bf16, or (FINE) as two bf16, the rounded one and the rest: what requests of as many rows as the other kernel takes
+      // have there, they have here as well, whatever is in the batch with them.
+      auto walk = [&](auto two) __attribute__((always_inline)) {
+      constexpr bool FINE = decltype(two)::value;
+      struct Weights {                                             // of 16 keys each
         u32x4 p[2], rest[FINE ? 2 : 1];
       } pa, pb = {};
       auto pack = [&](Weights& to, int i, float x, float y) __attribute__((always_inline)) {      // of logits i and i + 1
@@ -354,9 +360,11 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
       auto step = [&](f32x16& z, Weights& p, f32x16& zn, const unsigned char* kt, const Weights& pp, const unsigned char* vt, const unsigned char* kt_next,
                       const unsigned char* vt_next, int key0, bool masked, unsigned valid, auto&& beside) __attribute__((always_inline)) {
         if (__builtin_expect(masked, 0)) {
+          int first = 4 * half;
+          asm("" : "+v"(first));                                     // the places that follow from it are worked out here, not held in registers
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            const int j = 8 * (i >> 2) + 4 * half + (i & 3);
+            const int j = 8 * (i >> 2) + first + (i & 3);
             if (!((valid >> j) & 1) || key0 + j >= limit) z[i] = -INFINITY;
           }
         }
@@ -479,12 +487,16 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // what was sent for beyond the last tile
       if (active) {
 #pragma unroll
-        for (int f = 0; f < KS; ++f)
-          {
-            const bf16x8 v = frag(value_frag(k_tile(tile1 + 3) + TILE + HALF, f));
-            o[f % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, frag(pb.p[f / DB]), o[f % DB], 0, 0, 0);
-            if constexpr (FINE) o[f % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, frag(pb.rest[f / DB]), o[f % DB], 0, 0, 0);
-          }
+        for (int f = 0; f < KS; ++f) {
+          const bf16x8 v = frag(value_frag(k_tile(tile1 + 3) + TILE + HALF, f));
+          o[f % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, frag(pb.p[f / DB]), o[f % DB], 0, 0, 0);
+          if constexpr (FINE) o[f % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, frag(pb.rest[f / DB]), o[f % DB], 0, 0, 0);
+        }
+      }
+      };
+      if (of.rows <= kFewRowsMost) walk(std::true_type{});
+      else walk(std::false_type{});
+      if (active) {
         if (__builtin_expect(partly(tile1 - 1) && not_finite != 0, 0)) {
           // from the first tile that was cleaned on: the keys before seen_by_all in it were as well
           for (int key = max(seen_by_all & -kManyKeys, tile0 * kManyKeys); key < min(of.len, tile1 * kManyKeys); ++key) {
@@ -541,10 +553,10 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
   if (tid == 0 && !ma.whole) ma.cuts[g] = cut;
 }
 
-template <int D, bool FP8, bool FINE>
+template <int D, bool FP8>
 int launch_many_of(const ManyArgs& m, hipStream_t stream) {
-  if (m.a.pool.page_log2 < 4) attend_many_kernel<D, FP8, true, FINE><<<dim3(m.workgroups), dim3(kManyThreads), 0, stream>>>(m);
-  else attend_many_kernel<D, FP8, false, FINE><<<dim3(m.workgroups), dim3(kManyThreads), 0, stream>>>(m);
+  if (m.a.pool.page_log2 < 4) attend_many_kernel<D, FP8, true><<<dim3(m.workgroups), dim3(kManyThreads), 0, stream>>>(m);
+  else attend_many_kernel<D, FP8, false><<<dim3(m.workgroups), dim3(kManyThreads), 0, stream>>>(m);
   return (int)hipGetLastError();
 }
 

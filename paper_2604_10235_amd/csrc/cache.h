@@ -67,7 +67,7 @@ struct AttendPlan {
   int chunk, splits;           // few rows: keys of a workgroup, and workgroups per request and head,
   int shares;                  // or (not 0) equal parts of the keys of all requests and heads, one for each workgroup
   int workgroups, many_from, many_blocks;        // many rows: workgroups, rows from which a request is of this kind, blocks of rows,
-  int many_whole, many_fine;   // none of them shared, weights as two bf16
+  int many_whole;              // none of them shared
   size_t off_few, off_many, ws_bytes;
 };
 int make_attend_plan(const codecomp_batch* b, const codecomp_pages* p, AttendPlan* plan);

@@ -604,3 +604,22 @@ def test_workspaces_are_not_written_beyond(monkeypatch, lens, news, n_q, n_kv, d
     c = cu_.Cache(rng, lens, n_kv=n_kv, d=d, page=256, fp8=fp8, width_more=max_kv // 256, k_scale=0.03 if fp8 else 1.0, v_scale=0.02 if fp8 else 1.0)
     check(rng, c, news, n_q, max_kv=max_kv)
     assert intact()[0] > 0
+
+
+# Beside a long chunk as well a request of up to 64 rows has weights of 16 bits: it goes along with the chunk or takes the other kernel, over caches that are short
+# and long by the host's bound, in pages of more and of less than 16 rows.
+@pytest.mark.parametrize("news, n_q, n_kv, d", [([1, 90, 2, 8], 8, 2, 128), ([16, 1, 70, 9], 8, 2, 64), ([64, 65, 1, 33], 1, 1, 64), ([1, 300, 9, 4], 14, 2, 128)])
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("page, max_kv", [(16, 1300), (8, 1300), (256, 1 << 20)])
+def test_weights_of_short_requests_beside_long_ones(news, n_q, n_kv, d, fp8, page, max_kv):
+    rng = np.random.default_rng([37, d, page, news[0]])
+    lens = [1300, 700, 290, 900]
+    c = cu_.Cache(rng, lens, n_kv=n_kv, d=d, page=page, fp8=fp8, width_more=max_kv // page, k_scale=0.03 if fp8 else 1.0, v_scale=0.02 if fp8 else 1.0)
+    for causal in (True, False):
+        _, _, out, lse, want = check(rng, c, news, n_q, causal=causal, max_kv=max_kv)
+        cu = np.concatenate([[0], np.cumsum(news)])
+        short = [r for r, n in enumerate(news) if n * n_q // n_kv <= 64]
+        assert 0 < len(short) < len(news)
+        for r in short:
+            part = slice(int(cu[r]), int(cu[r + 1]))
+            cu_.assert_attended(out[part], lse[part], tuple(x[part] for x in want), d, 16)
