@@ -400,7 +400,7 @@ def _vectors(t, what: str, shape, stride_tok: int, stride_head: int) -> int:
     """bf16 [tokens, heads, head_dim] with the strides that the call will use (0 = dense)."""
     if t.dtype is not (_torch_module or _torch()).bfloat16 or t.shape != shape:
         raise ValueError(f"{what} must be bfloat16 {shape}, not {t.dtype} {tuple(t.shape)}")
-    if not stride_tok and not stride_head and t.is_contiguous():
+    if not shape[0] or (not stride_tok and not stride_head and t.is_contiguous()):          # strides of nothing say nothing
         return t.data_ptr()
     want = (stride_tok or shape[1] * shape[2], stride_head or shape[2], 1)
     if t.stride() != want and any(n > 1 and s != w for n, s, w in zip(shape, t.stride(), want)):

@@ -323,3 +323,11 @@ def test_a_batch_keeps_its_own_token_offsets():
     x = b.make_batch(n_q_heads=4, cu_q_host=cu, cu_q=i32(3), kv_lens=i32(2), table=i32(2, 3), max_kv_len=48)
     cu[1:] = 1000, 2000
     assert (C.c_int32 * 3).from_address(x.cu_q_host)[:] == [0, 2, 3] and x._tokens == 3
+
+
+def test_tensors_of_no_tokens_have_no_strides_to_be_checked():
+    import torch
+    for t in (torch.from_numpy(np.empty((0, 6, 64), np.float32)).bfloat16()[:, :4], torch.empty(0, 4, 64, dtype=torch.bfloat16).as_strided((0, 4, 64), (0, 0, 0))):
+        b._vectors(t, "q", (0, 4, 64), 6 * 64, 0)
+    with pytest.raises(ValueError):
+        b._vectors(torch.empty(1, 4, 64, dtype=torch.bfloat16).as_strided((1, 4, 64), (0, 0, 0)), "q", (1, 4, 64), 0, 0)
