@@ -29,7 +29,7 @@ int make_pool(const codecomp_pages* p, PagePool* pool) {
   if (!(p->k_scale >= 0.0f) || !(p->v_scale >= 0.0f) || !isfinite(p->k_scale) || !isfinite(p->v_scale)) return CODECOMP_EINVAL_PRIOR;
   const int64_t d = p->head_dim;
   const int64_t st = p->stride_tok ? p->stride_tok : d, sh = p->stride_head ? p->stride_head : p->page_size * d;
-  const int64_t sp = p->stride_page ? p->stride_page : p->n_kv_heads * p->page_size * d;
+  const int64_t sp = p->stride_page ? p->stride_page : p->n_kv_heads * (p->page_size * d);
   const int64_t sl = p->stride_layer ? p->stride_layer : p->n_pages * (p->n_kv_heads * (p->page_size * d));
   if (st < d || st > INT32_MAX / (p->page_size * esz)) return CODECOMP_EINVAL_SHAPE;       // places inside a page are counted in 32 bits
   pool->k = static_cast<unsigned char*>(p->k); pool->v = static_cast<unsigned char*>(p->v);
