@@ -18,8 +18,8 @@ extern template int launch_many_of<128, true>(const ManyArgs&, hipStream_t);
 // 23, over 131072 60 | 72; only from a few GB on the other is ahead (64 requests over 8192 keys 212 | 190).  Up to kFewRowsMost two workgroups share the
 // rows and both read the keys, which pays while these are few: 9 tokens over 8192 keys 19 | 24, over 32768 38 | 41, over 131072 92 | 76; 64 requests
 // over 8192 keys 353 | 204; and always from an 8-bit cache: 17 | 24, 31 | 39, 59 | 69, 205 | 205.  Beyond, a third and a fourth workgroup do not pay
-// from 8192 keys on (18 tokens over 32768 keys 57 | 44; over 2000 15 | 21).  Up to kFewRowsMost, weights enter the product as two bf16 in either kernel
-// (the many-row one with rounded ones: 64 requests 191).
+// from 8192 keys on (18 tokens over 32768 keys 57 | 44; over 2000 15 | 21).  Up to kFewRowsMost, weights enter the product as two bf16 in either kernel,
+// by a request's own rows alone (the many-row one with rounded ones: 64 requests 191).
 constexpr int kFewRows = 32;
 constexpr int64_t kFewKeysMost = 1 << 17;        // keys of all requests and KV heads, at their largest, up to which kFewRowsMost holds for bf16
 // In a batch with longer chunks, short requests go along with them while they are few: fewer launches, and the bandwidth that long ones have.  Beyond, what

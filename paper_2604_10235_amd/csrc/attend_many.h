@@ -1,5 +1,5 @@
 // Internal header: attention of requests with many rows (new tokens x query heads per KV head; attend.hip says from how many on): prefill chunks and
-// prompts.  Instantiated per head_dim, cache type and weights in attend_many_*.hip, so that they compile side by side.
+// prompts.  Instantiated per head_dim and cache type in attend_many_*.hip, so that they compile side by side.
 //
 // The rows of a KV head, token by token and its query heads within, are cut into blocks of 256: eight waves of 32 rows,
 // which share the keys and values that go through LDS in tiles of 64.  S^T = K Q^T leaves a row's logits in one lane of each half of the wave;
@@ -10,8 +10,11 @@
 // Bound by the matrix units and the vector instructions beside them, under the chip's power limit.  2048 tokens over 32768 keys, 28 query heads on 4 KV
 // heads of 128: 760 to 810 us by the device, 1.15 to 1.23 PFLOP/s, where the library's product of two 8192 x 8192 matrices reaches 1.21 to 1.27 on the
 // same devices; the matrix units are busy 69 % of the time at 1.5 to 1.9 GHz, 94 % of the reads meet L2, no LDS bank conflict.  head_dim 64 has as many
-// vector instructions for half the products: 480 to 505 us, 0.93 to 0.97 PFLOP/s.  8-bit caches: 815 and 516 us, the codes are widened on the way to LDS.
-// Before it: waves with 512 registers (the compiler keeps the accumulators in the half that vector instructions do not reach, and copies them); the page
+// vector instructions for half the products: 480 to 505 us, 0.93 to 0.97 PFLOP/s.  8-bit caches: 785 to 815 and 500 to 516 us, the codes are widened on the way to LDS.
+// Weights are rounded to bf16 for the second product, which puts a bf16 output 1.3 to 1.45 times as far from the exact one as rounding alone; as two bf16, which
+// requests of up to 64 rows have (they wait for memory), these chunks would take 1124 us instead of 783, and 712 instead of 494.
+// The 50 to 75 scalar registers that do not fit are kept in lanes of vector registers and come back between parts: none in a step's instructions.
+// Tried before: waves with 512 registers (the compiler keeps the accumulators in the half that vector instructions do not reach, and copies them); the page
 // table looked up key by key (790 us; as one load per 1024 keys 760).
 // Sending for a part's first tiles behind the last ones of the part before took as much time in the loop as it saved between parts; sending for them
 // before the outputs are written, and writing these in whole rows by way of LDS, changed nothing or took registers that the loop needs.
@@ -330,172 +333,172 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
       // The tiles, with weights rounded to bf16, or (FINE) as two bf16, the rounded one and the rest: what requests of as many rows as the other kernel takes
       // have there, they have here as well, whatever is in the batch with them.
       auto walk = [&](auto two) __attribute__((always_inline)) {
-      constexpr bool FINE = decltype(two)::value;
-      struct Weights {                                             // of 16 keys each
-        u32x4 p[2], rest[FINE ? 2 : 1];
-      } pa, pb = {};
-      auto pack = [&](Weights& to, int i, float x, float y) __attribute__((always_inline)) {      // of logits i and i + 1
-        const unsigned p = pack2(x, y);
-        to.p[i >> 3][(i & 7) >> 1] = p;
-        if constexpr (FINE) to.rest[i >> 3][(i & 7) >> 1] = pack2(x - __uint_as_float(p << 16), y - __uint_as_float(p & 0xFFFF0000u));
-      };
+        constexpr bool FINE = decltype(two)::value;
+        struct Weights {                                             // of 16 keys each
+          u32x4 p[2], rest[FINE ? 2 : 1];
+        } pa, pb = {};
+        auto pack = [&](Weights& to, int i, float x, float y) __attribute__((always_inline)) {      // of logits i and i + 1
+          const unsigned p = pack2(x, y);
+          to.p[i >> 3][(i & 7) >> 1] = p;
+          if constexpr (FINE) to.rest[i >> 3][(i & 7) >> 1] = pack2(x - __uint_as_float(p << 16), y - __uint_as_float(p & 0xFFFF0000u));
+        };
 
-      // Key fragment f (16 of a row's elements of 32 keys), value fragment f (32 columns of 16 keys).
-      const int k_lane = At::key(l32, half), v_lane = At::value(half * 4 + ((lane >> 2) & 3), 0) + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
-      auto key_frag = [&](const unsigned char* kt, int f) __attribute__((always_inline)) { return *reinterpret_cast<const u32x4*>(kt + k_lane + f * 512); };
-      auto value_frag = [&](const unsigned char* vt, int f) __attribute__((always_inline)) {
-        const unsigned char* at = vt + v_lane + (f / DB) * At::GROUP + (f % DB) * 1024;
-        const s16x4 v0 = read_columns(at), v1 = read_columns(at + 512);
-        return __builtin_bit_cast(u32x4, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-      };
-      constexpr int F = 2 * KS, RING = 4, PER = 16 / F, HALF = 2 * At::GROUP;      // fragments of a step, those held, logits per fragment; bytes of 32 rows
-      u32x4 ring[RING];
-      auto fill = [&](int f, const unsigned char* kt, const unsigned char* vt) __attribute__((always_inline)) {
-        ring[f % RING] = f & 1 ? value_frag(vt, f / 2) : key_frag(kt, f / 2);
-      };
-      // One step: the weights p of the 32 keys from key0 on, whose logits are z (`masked`: not all rows see all of them; `valid`: which of them there are); beside them, on the matrix cores,
-      // the logits zn of the next 32 keys (kt) and the outputs of the 32 before (vt), whose weights are pp.  The order is the source's: the LDS read that
-      // the MFMA three further on needs (from the next step's tiles at the end), an MFMA, the vector work of a logit (two at head_dim 64), and
-      // what `beside` has for this place.
-      auto step = [&](f32x16& z, Weights& p, f32x16& zn, const unsigned char* kt, const Weights& pp, const unsigned char* vt, const unsigned char* kt_next,
-                      const unsigned char* vt_next, int key0, bool masked, unsigned valid, auto&& beside) __attribute__((always_inline)) {
-        if (__builtin_expect(masked, 0)) {
-          int first = 4 * half;
-          asm("" : "+v"(first));                                     // the places that follow from it are worked out here, not held in registers
+        // Key fragment f (16 of a row's elements of 32 keys), value fragment f (32 columns of 16 keys).
+        const int k_lane = At::key(l32, half), v_lane = At::value(half * 4 + ((lane >> 2) & 3), 0) + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+        auto key_frag = [&](const unsigned char* kt, int f) __attribute__((always_inline)) { return *reinterpret_cast<const u32x4*>(kt + k_lane + f * 512); };
+        auto value_frag = [&](const unsigned char* vt, int f) __attribute__((always_inline)) {
+          const unsigned char* at = vt + v_lane + (f / DB) * At::GROUP + (f % DB) * 1024;
+          const s16x4 v0 = read_columns(at), v1 = read_columns(at + 512);
+          return __builtin_bit_cast(u32x4, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+        };
+        constexpr int F = 2 * KS, RING = 4, PER = 16 / F, HALF = 2 * At::GROUP;      // fragments of a step, those held, logits per fragment; bytes of 32 rows
+        u32x4 ring[RING];
+        auto fill = [&](int f, const unsigned char* kt, const unsigned char* vt) __attribute__((always_inline)) {
+          ring[f % RING] = f & 1 ? value_frag(vt, f / 2) : key_frag(kt, f / 2);
+        };
+        // One step: the weights p of the 32 keys from key0 on, whose logits are z (`masked`: not all rows see all of them; `valid`: which of them there are); beside them, on the matrix cores,
+        // the logits zn of the next 32 keys (kt) and the outputs of the 32 before (vt), whose weights are pp.  The order is the source's: the LDS read that
+        // the MFMA three further on needs (from the next step's tiles at the end), an MFMA, the vector work of a logit (two at head_dim 64), and
+        // what `beside` has for this place.
+        auto step = [&](f32x16& z, Weights& p, f32x16& zn, const unsigned char* kt, const Weights& pp, const unsigned char* vt, const unsigned char* kt_next,
+                        const unsigned char* vt_next, int key0, bool masked, unsigned valid, auto&& beside) __attribute__((always_inline)) {
+          if (__builtin_expect(masked, 0)) {
+            int first = 4 * half;
+            asm("" : "+v"(first));                                     // the places that follow from it are worked out here, not held in registers
 #pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int j = 8 * (i >> 2) + first + (i & 3);
-            if (!((valid >> j) & 1) || key0 + j >= limit) z[i] = -INFINITY;
+            for (int i = 0; i < 16; ++i) {
+              const int j = 8 * (i >> 2) + first + (i & 3);
+              if (!((valid >> j) & 1) || key0 + j >= limit) z[i] = -INFINITY;
+            }
           }
-        }
-        float sum = 0.0f, w[16];
+          float sum = 0.0f, w[16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) zn[i] = 0.0f;
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int f = 0; f < F; ++f) {
-          beside(f);
-          if (f + RING - 1 < F) fill(f + RING - 1, kt, vt);
-          else fill(f + RING - 1 - F, kt_next, vt_next);
-          const int i = f / 2;
-          if (f & 1) {
-            o[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(ring[f % RING]), frag(pp.p[i / DB]), o[i % DB], 0, 0, 0);
-            if constexpr (FINE) o[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(ring[f % RING]), frag(pp.rest[i / DB]), o[i % DB], 0, 0, 0);
-          } else zn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(ring[f % RING]), frag(qf[i]), zn, 0, 0, 0);
-#pragma unroll
-          for (int e = f * PER; e < (f + 1) * PER; ++e) {
-            w[e] = __builtin_amdgcn_exp2f(fmaf(z[e], a.c, -m));
-            if (e > 0) sum += w[e - 1];
-            if (e > 1 && (e & 1) == 0) pack(p, e - 2, w[e - 2], w[e - 1]);
-          }
+          for (int i = 0; i < 16; ++i) zn[i] = 0.0f;
           __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int f = 0; f < F; ++f) {
+            beside(f);
+            if (f + RING - 1 < F) fill(f + RING - 1, kt, vt);
+            else fill(f + RING - 1 - F, kt_next, vt_next);
+            const int i = f / 2;
+            if (f & 1) {
+              o[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(ring[f % RING]), frag(pp.p[i / DB]), o[i % DB], 0, 0, 0);
+              if constexpr (FINE) o[i % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(ring[f % RING]), frag(pp.rest[i / DB]), o[i % DB], 0, 0, 0);
+            } else zn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(ring[f % RING]), frag(qf[i]), zn, 0, 0, 0);
+#pragma unroll
+            for (int e = f * PER; e < (f + 1) * PER; ++e) {
+              w[e] = __builtin_amdgcn_exp2f(fmaf(z[e], a.c, -m));
+              if (e > 0) sum += w[e - 1];
+              if (e > 1 && (e & 1) == 0) pack(p, e - 2, w[e - 2], w[e - 1]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+          }
+          sum += w[15];
+          pack(p, 14, w[14], w[15]);
+          // here, beside the MFMAs, not behind the branch
+          asm volatile("" ::"v"(sum), "v"(p.p[0]), "v"(p.p[1]));
+          if constexpr (FINE) asm volatile("" ::"v"(p.rest[0]), "v"(p.rest[1]));
+          // A logit far above its row's reference: move the references.  (Weights are positive: none is larger than their sum, and as
+          // long as that is below 4096 nothing is lost in fp32 or bf16.)
+          if (__builtin_expect(__ballot(sum > 4096.0f) != 0, 0)) {
+            float t = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) t = fmaxf(t, z[i]);
+            t *= a.c;
+            t = fmaxf(t, __shfl_xor(t, 32));
+            const float to = fmaxf(m, t), old = to == m ? 1.0f : __builtin_amdgcn_exp2f(m - to);
+            m = to;
+            l *= old;
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+              for (int i = 0; i < 16; ++i) o[db][i] *= old;
+            sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+              const float x = __builtin_amdgcn_exp2f(fmaf(z[i], a.c, -m)), y = __builtin_amdgcn_exp2f(fmaf(z[i + 1], a.c, -m));
+              sum += x + y;
+              pack(p, i, x, y);
+            }
+          }
+          l += sum;
+        };
+
+        // ---- before the first tile
+        __syncthreads();                                             // the segment before is through with LDS
+        if (tid == 0) not_finite = 0;
+#pragma unroll
+        for (int j = 0; j < (ROWWISE ? 5 : 3); ++j) fetch_entries((ROWWISE ? tile0 : tile0 >> 4) + j);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int j = 0; j < 3; ++j) {
+          const Place from = k_place(tile0 + j);
+          fetch_keys(tile0 + j, from);
+          fetch_values(tile0 + j, v_place(tile0 + j, from));
+          if (j < 2) { park(tile0 + j, 0); park(tile0 + j, 1); park(tile0 + j, 2); park(tile0 + j, 3); }
         }
-        sum += w[15];
-        pack(p, 14, w[14], w[15]);
-        // here, beside the MFMAs, not behind the branch
-        asm volatile("" ::"v"(sum), "v"(p.p[0]), "v"(p.p[1]));
-        if constexpr (FINE) asm volatile("" ::"v"(p.rest[0]), "v"(p.rest[1]));
-        // A logit far above its row's reference: move the references.  (Weights are positive: none is larger than their sum, and as
-        // long as that is below 4096 nothing is lost in fp32 or bf16.)
-        if (__builtin_expect(__ballot(sum > 4096.0f) != 0, 0)) {
-          float t = -INFINITY;
+        // in front of the first tile: values of zero
+        for (int i = tid; i < HALF / 16; i += kManyThreads) *reinterpret_cast<u32x4*>(k_tile(tile0 + 3) + TILE + HALF + i * 16) = u32x4{0, 0, 0, 0};
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(SENT) : "memory");
+        uint64_t valid = ROWWISE ? is_there(tile0, entry(tile0, lane)) : 0;
+        uint64_t held = ROWWISE ? 0 : __ballot(is_page(entries[(tile0 >> 4) & 3][lane]));          // groups of 16 keys of the stretch whose pages there are
+        if (active) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i) t = fmaxf(t, z[i]);
-          t *= a.c;
-          t = fmaxf(t, __shfl_xor(t, 32));
-          const float to = fmaxf(m, t), old = to == m ? 1.0f : __builtin_amdgcn_exp2f(m - to);
-          m = to;
-          l *= old;
+          for (int i = 0; i < 16; ++i) za[i] = 0.0f;
 #pragma unroll
-          for (int db = 0; db < DB; ++db)
+          for (int f = 0; f < KS; ++f) za = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(key_frag(k_tile(tile0), f)), frag(qf[f]), za, 0, 0, 0);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[db][i] *= old;
-          sum = 0.0f;
+          for (int f = 0; f < RING - 1; ++f) fill(f, k_tile(tile0) + HALF, k_tile(tile0 + 3) + TILE + HALF);
+        }
+        for (int tile = tile0; tile < tile1; ++tile) {
+          bool masked = tile >= plain_end;
+          if constexpr (ROWWISE) {
+            masked |= valid != ~0ull;
+          } else {
+            if ((tile & 15) == 13) fetch_entries((tile >> 4) + 2);   // three tiles ahead a new stretch begins: the one after it
+            if ((tile & 15) == 0) held = __ballot(is_page(entries[(tile >> 4) & 3][lane]));
+            masked |= (((unsigned)(held >> ((tile & 15) * 4)) & 15u) != 15u);
+            if (masked) valid = is_there(tile, entry(tile, lane));
+          }
+          if (__builtin_expect(masked, 0)) clean_values(tile, valid);
+          const unsigned char *t0 = k_tile(tile), *t1 = k_tile(tile + 1), *before = k_tile(tile + 3);
+          // All of this step's LDS reads are on their way by the last places: from there on the tile before is nobody's, and the next one is everybody's.
+          auto pass_on = [&](int f) __attribute__((always_inline)) {
+            if (f == F - (RING - 1)) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(SENT + (ROWWISE ? 1 : 0)) : "memory");
+          };
+          Place k_from = {0, 0}, v_from = {0, 0};
+          int next_entry = 0;
+          auto send_for = [&](int f) __attribute__((always_inline)) {
+            if (ROWWISE && f == 0) next_entry = entry(tile + 1, lane);
+            if (f < 4) park(tile + 2, f);                            // before the next ones are sent for below
+            if (f == 1) k_from = k_place(tile + 3);
+            if (f == 2) v_from = v_place(tile + 3, k_from);
+            if (f == 3) fetch_keys(tile + 3, k_from);
+            if (f == 4) fetch_values(tile + 3, v_from);
+            if (f == 5 && ROWWISE) fetch_entries(tile + 5);
+          };
+          if (active) {
+            step(za, pa, zb, t0 + HALF, pb, before + TILE + HALF, t1, t0 + TILE, tile * kManyKeys, masked, (unsigned)valid, pass_on);
+            step(zb, pb, za, t1, pa, t0 + TILE, t1 + HALF, t0 + TILE + HALF, tile * kManyKeys + 32, masked, (unsigned)(valid >> 32), send_for);
+          } else {
+            pass_on(F - (RING - 1));
 #pragma unroll
-          for (int i = 0; i < 16; i += 2) {
-            const float x = __builtin_amdgcn_exp2f(fmaf(z[i], a.c, -m)), y = __builtin_amdgcn_exp2f(fmaf(z[i + 1], a.c, -m));
-            sum += x + y;
-            pack(p, i, x, y);
+            for (int f = 0; f < F; ++f) send_for(f);
+          }
+          if constexpr (ROWWISE) valid = is_there(tile + 1, next_entry);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // what was sent for beyond the last tile
+        if (active) {
+#pragma unroll
+          for (int f = 0; f < KS; ++f) {
+            const bf16x8 v = frag(value_frag(k_tile(tile1 + 3) + TILE + HALF, f));
+            o[f % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, frag(pb.p[f / DB]), o[f % DB], 0, 0, 0);
+            if constexpr (FINE) o[f % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, frag(pb.rest[f / DB]), o[f % DB], 0, 0, 0);
           }
         }
-        l += sum;
       };
-
-      // ---- before the first tile
-      __syncthreads();                                             // the segment before is through with LDS
-      if (tid == 0) not_finite = 0;
-#pragma unroll
-      for (int j = 0; j < (ROWWISE ? 5 : 3); ++j) fetch_entries((ROWWISE ? tile0 : tile0 >> 4) + j);
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-#pragma unroll
-      for (int j = 0; j < 3; ++j) {
-        const Place from = k_place(tile0 + j);
-        fetch_keys(tile0 + j, from);
-        fetch_values(tile0 + j, v_place(tile0 + j, from));
-        if (j < 2) { park(tile0 + j, 0); park(tile0 + j, 1); park(tile0 + j, 2); park(tile0 + j, 3); }
-      }
-      // in front of the first tile: values of zero
-      for (int i = tid; i < HALF / 16; i += kManyThreads) *reinterpret_cast<u32x4*>(k_tile(tile0 + 3) + TILE + HALF + i * 16) = u32x4{0, 0, 0, 0};
-      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(SENT) : "memory");
-      uint64_t valid = ROWWISE ? is_there(tile0, entry(tile0, lane)) : 0;
-      uint64_t held = ROWWISE ? 0 : __ballot(is_page(entries[(tile0 >> 4) & 3][lane]));          // groups of 16 keys of the stretch whose pages there are
-      if (active) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) za[i] = 0.0f;
-#pragma unroll
-        for (int f = 0; f < KS; ++f) za = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(key_frag(k_tile(tile0), f)), frag(qf[f]), za, 0, 0, 0);
-#pragma unroll
-        for (int f = 0; f < RING - 1; ++f) fill(f, k_tile(tile0) + HALF, k_tile(tile0 + 3) + TILE + HALF);
-      }
-      for (int tile = tile0; tile < tile1; ++tile) {
-        bool masked = tile >= plain_end;
-        if constexpr (ROWWISE) {
-          masked |= valid != ~0ull;
-        } else {
-          if ((tile & 15) == 13) fetch_entries((tile >> 4) + 2);   // three tiles ahead a new stretch begins: the one after it
-          if ((tile & 15) == 0) held = __ballot(is_page(entries[(tile >> 4) & 3][lane]));
-          masked |= (((unsigned)(held >> ((tile & 15) * 4)) & 15u) != 15u);
-          if (masked) valid = is_there(tile, entry(tile, lane));
-        }
-        if (__builtin_expect(masked, 0)) clean_values(tile, valid);
-        const unsigned char *t0 = k_tile(tile), *t1 = k_tile(tile + 1), *before = k_tile(tile + 3);
-        // All of this step's LDS reads are on their way by the last places: from there on the tile before is nobody's, and the next one is everybody's.
-        auto pass_on = [&](int f) __attribute__((always_inline)) {
-          if (f == F - (RING - 1)) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(SENT + (ROWWISE ? 1 : 0)) : "memory");
-        };
-        Place k_from = {0, 0}, v_from = {0, 0};
-        int next_entry = 0;
-        auto send_for = [&](int f) __attribute__((always_inline)) {
-          if (ROWWISE && f == 0) next_entry = entry(tile + 1, lane);
-          if (f < 4) park(tile + 2, f);                            // before the next ones are sent for below
-          if (f == 1) k_from = k_place(tile + 3);
-          if (f == 2) v_from = v_place(tile + 3, k_from);
-          if (f == 3) fetch_keys(tile + 3, k_from);
-          if (f == 4) fetch_values(tile + 3, v_from);
-          if (f == 5 && ROWWISE) fetch_entries(tile + 5);
-        };
-        if (active) {
-          step(za, pa, zb, t0 + HALF, pb, before + TILE + HALF, t1, t0 + TILE, tile * kManyKeys, masked, (unsigned)valid, pass_on);
-          step(zb, pb, za, t1, pa, t0 + TILE, t1 + HALF, t0 + TILE + HALF, tile * kManyKeys + 32, masked, (unsigned)(valid >> 32), send_for);
-        } else {
-          pass_on(F - (RING - 1));
-#pragma unroll
-          for (int f = 0; f < F; ++f) send_for(f);
-        }
-        if constexpr (ROWWISE) valid = is_there(tile + 1, next_entry);
-      }
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");             // what was sent for beyond the last tile
-      if (active) {
-#pragma unroll
-        for (int f = 0; f < KS; ++f) {
-          const bf16x8 v = frag(value_frag(k_tile(tile1 + 3) + TILE + HALF, f));
-          o[f % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, frag(pb.p[f / DB]), o[f % DB], 0, 0, 0);
-          if constexpr (FINE) o[f % DB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, frag(pb.rest[f / DB]), o[f % DB], 0, 0, 0);
-        }
-      }
-      };
-      if (of.rows <= kFewRowsMost) walk(std::true_type{});
-      else walk(std::false_type{});
+      if (__builtin_expect(of.rows > kFewRowsMost, 1)) walk(std::false_type{});
+      else walk(std::true_type{});
       if (active) {
         if (__builtin_expect(partly(tile1 - 1) && not_finite != 0, 0)) {
           // from the first tile that was cleaned on: the keys before seen_by_all in it were as well
