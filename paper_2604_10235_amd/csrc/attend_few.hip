@@ -13,7 +13,7 @@
 // rounded value and the rest: 16 bits of it, for MFMA time that memory hides.
 //
 // Measured (a kernel that only reads reaches 6.4 TB/s): 64 steps over 500 .. 16384 keys, 4 KV heads of 128 elements, bf16: 187 us, 5.3 TB/s; with 8 KV heads, 8
-// bits: 187 us, 5.4 TB/s; one step over 131072 keys: 51 us and 6 us for the join, 4.8 TB/s; one over 2113: 7 us and 3 us, a chain of small loads
+// bits: 184 us, 5.5 TB/s; one step over 131072 keys: 56 us, 4.8 TB/s (51 the kernel, 6 the join); one over 2113: 10 us (7 and 4), a chain of small loads
 // (lengths, table, rows, parts) that nothing hides.
 #include "attend.h"
 

@@ -2,8 +2,8 @@
 // row's two places are found once.  One piece of each in flight per thread and many threads are enough (two rows a thread: store 4.3 GB 742 -> 794
 // us; whole pages, 350 MB, one piece 62, two 64, four 73), and stores go past the caches, which could not hold the rows until they are read (store 760 ->
 // 740 us, pages 70 -> 64).
-// Measured: 4.3 GB from dense rows into pages of 16 rows 740 us, 5.8 TB/s (a large copy reaches 5.0); 236 MB of kept rows from pages to pages 47 us,
-// 5.0; 350 MB of whole pages 62 us, 5.7.
+// Measured: 4.3 GB from dense rows into pages of 16 rows 750 us, 5.7 TB/s; 3.8 GB from pages into dense rows 647 us, 5.8; 236 MB of kept rows from pages to
+// pages 44 us, 5.4; 350 MB of whole pages 63 us, 5.6.
 #include "cache.h"
 
 namespace codecomp {

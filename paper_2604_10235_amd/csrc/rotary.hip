@@ -2,8 +2,8 @@
 //
 // A pair (x0, x1) at position p becomes magnitude * (x0 cos a - x1 sin a, x0 sin a + x1 cos a), a = p * freq.  Both kernels only
 // move memory: 4 bytes per element against a few operations, and what the angles cost is shared by the heads that a thread takes.
-// Measured: 32768 tokens of 40 heads of 128 elements 115 us, 5.8 TB/s (a large copy reaches 5.0); four chunks of together 10500 tokens into an FP8
-// cache 62 us, 4.2 TB/s; 16 tokens 3.3 us, of which the launch and one chain of loads are all.
+// Measured: 32768 tokens of 40 heads of 128 elements 115 us, 5.8 TB/s (as much as any copy here); four chunks of together 10500 tokens into an FP8
+// cache 58 us, 4.5 TB/s; 16 tokens 3.3 us, of which the launch and one chain of loads are all.
 // The angle of a far position loses all its digits in fp32 (p * freq at 10^6 has steps of 0.06 rad): it is formed in turns as a 64-bit
 // fraction (rounded once, on the host), whose product with a whole position wraps around where the angle does.  What is left of it after taking out the nearest
 // quarter turn is at most pi / 4, known to 2^-27 of a turn, where the Taylor series of sine and cosine to the 9th and 10th power are good to 2e-9 and 1.2e-10
