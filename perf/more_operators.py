@@ -1,0 +1,463 @@
+"""Long and branching service from a compressed cache, as measurable cases: attention of requests that share the start of their caches, attention
+weights summed up per cached row, eviction in place by these sums.
+
+A case is one call.  Head shapes are those of `paper_2604_10235_amd/workloads.py` and the tests; lengths those of the compression workloads and of what
+stands behind a compressed prompt once requests fork from it and answer.
+
+Three operators:
+  shared  softmax attention of new tokens over pages, of groups of requests whose tables begin with the same pages: read once for a group.
+  mass    the weights that a call's new tokens give to every cached row, added to sums kept per request, head and row.
+  evict   of the rows behind a protected start: the last few and those of the largest sums stay, moved together in their pages, sums along with them.
+"""
+import math
+import random
+
+import numpy as np
+import torch
+
+own = False
+
+DEFAULTS = dict(op="shared", q_heads=28, kv_heads=4, head_dim=128, kv="bf16", page=64, layers=1, seqs=1,
+                # shared: groups that the requests fall into, the shared rows of a group
+                groups=1, prefix_min=1, prefix=1,
+                # shared, mass: new tokens of a request; rows behind the shared ones, with the new tokens
+                new_min=1, new=1, own_min=1, own_len=1, causal=True,
+                # mass, evict: protected rows at the start, which take no part
+                first=0, decay=1.0,
+                # evict: rows kept behind them, those that stay because they are the last
+                budget=1024, recent=32)
+
+
+def case(name=None, **over):
+    c = dict(DEFAULTS, **over)
+    if name is not None:
+        c["name"] = name
+    return c
+
+
+def listed():
+    return [
+        # four answers sampled from one short compressed prompt: launches and latency are all there is
+        case("shared_four", op="shared", seqs=4, prefix_min=2049, prefix=2049, own_min=1, own_len=90),
+        # a server's step: 64 agents that work on the same 32K context, each with some hundred tokens of its own
+        case("shared_step_32k", op="shared", seqs=64, prefix_min=32768, prefix=32768, own_min=1, own_len=700),
+        # eight contexts of odd lengths, a dozen requests each, 8-bit cache
+        case("shared_groups_fp8", op="shared", q_heads=32, kv_heads=8, kv="fp8_e4m3", page=32, seqs=96, groups=8, prefix_min=2001, prefix=9001, own_min=20, own_len=2000),
+        # questions of odd lengths behind one document, small heads and pages
+        case("shared_questions_d64", op="shared", q_heads=8, kv_heads=4, head_dim=64, page=16, seqs=24, groups=2, prefix_min=14001, prefix=16001, new_min=1, new=401,
+             own_min=401, own_len=600),
+        # one request, one token, a compressed 32K context: the smallest step
+        case("mass_one_token", op="mass", own_len=2113),
+        # the weights of a server's step: 64 requests of half a thousand to 16K rows, 8-bit cache, older weight fades
+        case("mass_steps_fp8", op="mass", q_heads=32, kv_heads=8, kv="fp8_e4m3", page=32, seqs=64, own_min=500, own_len=16384, decay=0.98),
+        # of 64 forked requests, the rows behind the shared ones only
+        case("mass_forks", op="mass", seqs=64, first=8192, own_min=300, own_len=4100),
+        # all weights of a prompt
+        case("mass_prompt_8k", op="mass", new_min=8191, new=8191, own_len=8191),
+        # one layer of one request, a few rows too many: the smallest eviction
+        case("evict_one", op="evict", seqs=1, own_min=1088, own_len=1088, budget=1024),
+        # all layers of 32 requests, between 0 and some hundred rows too many, behind protected first rows
+        case("evict_steps", op="evict", layers=28, seqs=32, own_min=900, own_len=1500, budget=1024, first=4),
+        # a whole prompt's cache down to 2048 rows by the weights of all of its tokens
+        case("evict_32k", op="evict", layers=28, seqs=1, own_min=32768, own_len=32768, budget=2048, recent=64),
+        # forked requests, 8-bit cache, small pages
+        case("evict_forks_fp8", op="evict", q_heads=32, kv_heads=8, kv="fp8_e4m3", page=16, layers=32, seqs=48, first=2049, own_min=1025, own_len=2300, budget=1000, recent=128),
+    ]
+
+
+MOST_PAIRS = 8 * 64 * 60 * 10 ** 6            # head_dim elements times (query, key) pairs, somewhat less than shared_questions_d64 has
+MOST_MASS = 28 * 128 * 8191 * 4096            # the same of mass_prompt_8k
+MOST_CACHE = 131072 * 4 * 128                 # elements of K or V that are read, all requests together
+MOST_ROWS = 28 * 32 * 4 * 128 * 1500          # elements of K or V that evict_steps holds
+
+
+def log_int(rng, low, high):
+    return int(round(2 ** rng.uniform(math.log2(low), math.log2(high))))
+
+
+def draw(rng):
+    op = rng.choice(["shared"] * 5 + ["mass"] * 4 + ["evict"] * 3)
+    q_heads, kv_heads, head_dim = rng.choice([(28, 4, 128), (28, 4, 128), (32, 8, 128), (8, 2, 128), (14, 2, 128), (4, 4, 64), (8, 4, 64)])
+    c = case(op=op, q_heads=q_heads, kv_heads=kv_heads, head_dim=head_dim, page=rng.choice([16, 16, 32, 64, 128, 256]))
+    c["kv"] = "fp8_e4m3" if rng.random() < 0.35 else "bf16"
+    c["causal"] = op == "evict" or rng.random() < 0.85
+    wide = kv_heads * head_dim
+    if op == "evict":
+        c["layers"], c["seqs"] = log_int(rng, 1, 32), log_int(rng, 1, 64)
+        c["own_len"] = log_int(rng, 16, 32768)
+        c["own_min"] = max(1, c["own_len"] // rng.randint(1, 4))
+        c["budget"] = log_int(rng, 1, c["own_len"])
+        c["recent"] = rng.choice([0, 1, c["budget"] // 8, c["budget"] // 2, c["budget"]])
+        c["first"] = rng.choice([0, 0, 4, 513])
+        while c["layers"] * c["seqs"] * wide * (c["own_len"] + c["first"]) > MOST_ROWS:
+            c["layers"], c["seqs"] = (c["layers"], c["seqs"] // 2) if c["seqs"] > 1 and rng.random() < 0.6 else (max(1, c["layers"] // 2), c["seqs"])
+        return c
+    kind = rng.choice(["step", "step", "step", "few", "chunk"])
+    c["new"] = 1 if kind == "step" else log_int(rng, 2, 16) if kind == "few" else log_int(rng, 16, 4096 if op == "mass" else 512)
+    c["new_min"] = max(1, c["new"] // rng.randint(1, 4))
+    if op == "mass":
+        c["seqs"] = log_int(rng, 1, 64)
+        c["first"] = rng.choice([0, 0, 0, 129, 4096])
+        c["decay"] = rng.choice([1.0, 1.0, 0.9, 0.0])
+        c["own_len"] = c["new"] + log_int(rng, 1, 65536)
+        c["own_min"] = max(c["new"], c["own_len"] // rng.randint(1, 8))
+        while c["seqs"] > 1 and (c["seqs"] * (c["own_len"] + c["first"]) * wide > MOST_CACHE or c["seqs"] * c["new"] * c["own_len"] * q_heads * head_dim > MOST_MASS):
+            c["seqs"] = (c["seqs"] + 1) // 2 if c["seqs"] > 2 else 1
+        c["own_len"] = max(c["new"], min(c["own_len"], MOST_MASS // (c["new"] * q_heads * head_dim), MOST_CACHE // wide - c["first"]))
+        c["own_min"] = min(c["own_min"], c["own_len"])
+        return c
+    c["groups"] = log_int(rng, 1, 8)
+    c["seqs"] = c["groups"] * log_int(rng, 1, 48)
+    c["prefix"] = log_int(rng, 16, 65536)
+    c["prefix_min"] = max(1, c["prefix"] // rng.randint(1, 4))
+    c["own_len"] = c["new"] + log_int(rng, 1, 2048)
+    c["own_min"] = c["new"]
+    while c["seqs"] > c["groups"] and c["seqs"] * c["new"] * (c["prefix"] + c["own_len"]) * q_heads * head_dim > MOST_PAIRS:
+        c["seqs"] = max(c["groups"], c["seqs"] // 2)
+    while c["groups"] * c["prefix"] * wide > MOST_CACHE or c["groups"] * c["new"] * c["prefix"] * q_heads * head_dim > MOST_PAIRS:
+        c["prefix"] //= 2
+        c["prefix_min"] = min(c["prefix_min"], c["prefix"])
+    return c
+
+
+def spread(c, count, low, high, salt):
+    """One length for each of `count` between two bounds: part of the case, the same for every seed."""
+    r = random.Random(1000003 * count + 101 * high + low + salt)
+    return [high] + [r.randint(low, high) for _ in range(count - 1)]
+
+
+def lengths(c):
+    """New tokens, rows behind the shared or protected ones (the new tokens' among them), rows before them, and the group, of every request."""
+    news = spread(c, c["seqs"], c["new_min"], c["new"], 1)
+    owns = [max(n, k) for n, k in zip(news, spread(c, c["seqs"], c["own_min"], c["own_len"], 2))]
+    of = [r * c["groups"] // c["seqs"] for r in range(c["seqs"])]
+    prefixes = spread(c, c["groups"], c["prefix_min"], c["prefix"], 3)
+    before = [prefixes[g] for g in of] if c["op"] == "shared" else [c["first"]] * c["seqs"]
+    return news, owns, before, of
+
+
+def cu(counts):
+    return np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+
+
+def on_gpu(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+# ---------------------------------------------------------------- inputs
+
+K_SCALE, V_SCALE = 0.02, 0.0125               # of the 8-bit cache: a value is its code times this
+
+
+def pool(c, pages, gen):
+    """K or V pages [layers, pages, heads, page, d] of N(0, 1) rows, in the cache's type."""
+    shape = (pages, c["kv_heads"], c["page"], c["head_dim"])
+    out = torch.empty((c["layers"], *shape), dtype=torch.float8_e4m3fn if c["kv"] == "fp8_e4m3" else torch.bfloat16, device="cuda")
+    for x in out:
+        x.copy_(torch.randn(shape, generator=gen, device="cuda") * (40.0 if c["kv"] == "fp8_e4m3" else 1.0))
+    return out
+
+
+def bits(x):
+    """8-bit floats as bytes, which can be indexed."""
+    return x.view(torch.uint8) if x.dtype == torch.float8_e4m3fn else x
+
+
+def prepare(c, seed):
+    """Pages in no order; a group's requests (all requests, of protected rows) begin with the same whole pages, the page that a shared start ends in among them."""
+    c = dict(DEFAULTS, **c)
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    news, owns, before, of = lengths(c)
+    s = {"case": c, "news": news, "owns": owns, "before": before, "of": of}
+    n, page = c["seqs"], c["page"]
+    total = [a + b for a, b in zip(before, owns)]
+    # a request's pages behind the shared whole ones are its own; the last shared page, if it is not full, has been copied
+    whole = [b // page for b in before] if c["op"] == "shared" else [0] * n
+    need = [-(-t // page) - w for t, w in zip(total, whole)]
+    heads = {g: w for g, w in zip(of, whole)}
+    pages = int((sum(need) + sum(heads.values())) * 1.07) + 3
+    order = torch.randperm(pages, generator=gen, device="cuda").int()
+    table = torch.full((n, max(-(-t // page) for t in total)), -1, dtype=torch.int32, device="cuda")
+    starts, at = {}, 0
+    for g, w in heads.items():
+        starts[g], at = at, at + w
+    for r in range(n):
+        table[r, : whole[r]] = order[starts[of[r]] : starts[of[r]] + whole[r]]
+        table[r, whole[r] : whole[r] + need[r]] = order[at : at + need[r]]
+        at += need[r]
+    s["table"], s["k_pages"], s["v_pages"] = table, pool(c, pages, gen), pool(c, pages, gen)
+    s["total"], s["kv_lens"] = total, on_gpu(np.array(total, np.int32))
+    if c["op"] == "shared":                   # the page in which the shared rows end holds the same rows for all of a group
+        lead = [of.index(g) for g in of]
+        for r in range(n):
+            rest = before[r] % page
+            if rest and lead[r] != r:
+                a, b = table[lead[r], whole[r]].long(), table[r, whole[r]].long()
+                for p in (s["k_pages"], s["v_pages"]):
+                    bits(p)[:, b, :, :rest] = bits(p)[:, a, :, :rest]
+    {"shared": prepare_shared, "mass": prepare_mass, "evict": prepare_evict}[c["op"]](c, s, gen)
+    return s
+
+
+def queries(c, s, gen):
+    s["cu_host"] = cu(s["news"])
+    s["cu"], T = on_gpu(s["cu_host"]), sum(s["news"])
+    # logits of a few units, some queries that look at single keys
+    sharp = 1.0 + 2.0 * (torch.rand((T, c["q_heads"], 1), generator=gen, device="cuda") < 0.1)
+    s["q"] = (sharp * torch.randn((T, c["q_heads"], c["head_dim"]), generator=gen, device="cuda")).bfloat16()
+    if own:
+        from paper_2604_10235_amd import binding as cc
+        fp8 = c["kv"] == "fp8_e4m3"
+        s["pages"] = cc.make_pages(s["k_pages"], s["v_pages"], k_scale=K_SCALE if fp8 else 1.0, v_scale=V_SCALE if fp8 else 1.0)
+        s["batch"] = cc.make_batch(n_q_heads=c["q_heads"], cu_q_host=s["cu_host"], cu_q=s["cu"], kv_lens=s["kv_lens"], table=s["table"], max_kv_len=max(s["total"]),
+                                   causal=c["causal"])
+
+
+def prepare_shared(c, s, gen):
+    queries(c, s, gen)
+    s["members"] = cu([s["of"].count(g) for g in range(c["groups"])])
+    s["prefixes"] = [s["before"][s["of"].index(g)] for g in range(c["groups"])]
+    s["cu_groups"], s["prefix_lens"] = on_gpu(s["members"]), on_gpu(np.array(s["prefixes"], np.int32))
+    s["out"] = torch.empty_like(s["q"])
+    s["lse"] = torch.empty((sum(s["news"]), c["q_heads"]), dtype=torch.float32, device="cuda")
+    if own:
+        from paper_2604_10235_amd import binding as cc
+        s["shared"] = cc.make_groups(cu_groups_host=s["members"], cu_groups=s["cu_groups"], prefix_lens=s["prefix_lens"], max_prefix_len=max(s["prefixes"]))
+        s["workspace"] = torch.empty(max(256, cc.codecomp_attend_shared_workspace_bytes(s["batch"], s["shared"], s["pages"])), dtype=torch.uint8, device="cuda")
+
+
+def rows_of(c, s, r, which):
+    """Rows of a request in 64 bits [heads, rows, d], layer 0."""
+    slots = torch.arange(s["total"][r], device="cuda")
+    p = s["k_pages"] if which == "k" else s["v_pages"]
+    x = bits(p)[0][s["table"][r].long()[slots // c["page"]], :, slots % c["page"]].view(p.dtype).float().double().transpose(0, 1)
+    return x * ((K_SCALE if which == "k" else V_SCALE) if c["kv"] == "fp8_e4m3" else 1.0)
+
+
+def logits_of(c, s, r, h, k, kind):
+    """Of a request's tokens, one query head [new tokens, rows]; minus infinity where a token does not see a row."""
+    a, n, kept = int(s["cu_host"][r]), s["news"][r], s["total"][r]
+    z = (s["q"][a : a + n, h].to(kind) @ k[h // (c["q_heads"] // c["kv_heads"])].to(kind).T) / math.sqrt(c["head_dim"])
+    if not c["causal"]:
+        return z
+    return torch.where(torch.arange(kept, device="cuda")[None, :] < torch.arange(kept - n + 1, kept + 1, device="cuda")[:, None], z, -torch.inf)
+
+
+def prepare_mass(c, s, gen):
+    """The log-sum-exp of every row stands there: attention goes before.  Sums of some earlier steps."""
+    queries(c, s, gen)
+    T, Hq, longest = sum(s["news"]), c["q_heads"], max(s["total"])
+    s["lse"] = torch.full((T, Hq), -torch.inf, dtype=torch.float32, device="cuda")
+    for r in range(c["seqs"]):
+        k, a, n = rows_of(c, s, r, "k").float(), int(s["cu_host"][r]), s["news"][r]
+        for h in range(Hq):
+            s["lse"][a : a + n, h] = torch.logsumexp(logits_of(c, s, r, h, k, torch.float32), 1)
+    s["sums"] = torch.randn((c["layers"], c["seqs"], c["kv_heads"], longest), generator=gen, device="cuda").exp() * (8.0 / longest)
+    s["first"] = torch.full((c["seqs"],), c["first"], dtype=torch.int32, device="cuda")
+    if own:
+        from paper_2604_10235_amd import binding as cc
+        s["mass"] = cc.make_mass(s["sums"])
+        s["workspace"] = torch.empty(max(256, cc.codecomp_attend_mass_workspace_bytes(s["batch"], s["pages"], s["mass"])), dtype=torch.uint8, device="cuda")
+
+
+def prepare_evict(c, s, gen):
+    """Sums with a long tail; rows that nothing has looked at yet are all zero."""
+    shape = (c["layers"], c["seqs"], c["kv_heads"], max(s["total"]))
+    s["sums"] = (torch.randn(shape, generator=gen, device="cuda") * 2.0 - 5.0).exp() * (torch.rand(shape, generator=gen, device="cuda") > 0.05)
+    s["kept_sums"] = torch.zeros_like(s["sums"])
+    s["first"] = torch.full((c["seqs"],), c["first"], dtype=torch.int32, device="cuda")
+    s["budgets"] = torch.full((c["seqs"],), c["budget"], dtype=torch.int32, device="cuda")
+    s["kept"] = torch.empty((c["layers"], c["seqs"], c["kv_heads"], c["budget"]), dtype=torch.int32, device="cuda")
+    s["new_lens"] = torch.empty((c["seqs"],), dtype=torch.int32, device="cuda")
+    if own:
+        from paper_2604_10235_amd import binding as cc
+        s["pages"] = cc.make_pages(s["k_pages"], s["v_pages"])
+        s["mass"], s["kept_mass"] = cc.make_mass(s["sums"]), cc.make_mass(s["kept_sums"])
+        s["eviction"] = cc.make_eviction(kv_lens=s["kv_lens"], table=s["table"], budgets=s["budgets"], max_kv_len=max(s["total"]), max_budget=c["budget"],
+                                         recent=c["recent"], first=s["first"])
+
+
+# ---------------------------------------------------------------- one pass
+
+def run(s):
+    return {"shared": run_shared, "mass": run_mass, "evict": run_evict}[s["case"]["op"]](s)
+
+
+def gathered(s, which, table, slots, there):
+    """Rows [requests or groups, heads, rows, d] in 32 bits; zeros where none is there."""
+    c = s["case"]
+    p, scale = (s["k_pages"], K_SCALE) if which == "k" else (s["v_pages"], V_SCALE)
+    page = torch.gather(table, 1, (slots // c["page"]).clamp_max(table.shape[1] - 1)).clamp_min(0).long()
+    x = bits(p)[0][page, :, slots % c["page"]].view(p.dtype).float()
+    x = x.mul_(scale if c["kv"] == "fp8_e4m3" else 1.0).masked_fill_(~there[:, :, None, None], 0.0)
+    return x.transpose(1, 2).contiguous()
+
+
+def by_owner(s, counts, offsets):
+    """Queries [owners, heads, most tokens * group, d] in 32 bits, and which tokens there are."""
+    c = s["case"]
+    most, H, G = int(max(counts)), c["kv_heads"], c["q_heads"] // c["kv_heads"]
+    there = torch.arange(most, device="cuda")[None, :] < offsets.diff()[:, None]
+    q = torch.zeros((len(counts), most, H, G, c["head_dim"]), device="cuda")
+    q[there] = s["q"].float().unflatten(1, (H, G))
+    return q.permute(0, 2, 1, 3, 4).reshape(len(counts), H, most * G, c["head_dim"]), there
+
+
+def part(s, q, there, k, v, hidden):
+    """Of one set of rows: largest logit, sum of weights relative to it and weighted values, packed [tokens, heads, ...].  hidden [owners, most tokens, rows]."""
+    c = s["case"]
+    n, H, _, d = q.shape
+    G, most, keys = c["q_heads"] // c["kv_heads"], there.shape[1], k.shape[2]
+    logits = (q @ k.transpose(2, 3).contiguous()).mul_(d ** -0.5).view(n, H, most, G, keys)
+    logits.masked_fill_(hidden[:, None, :, None, :], -torch.inf)
+    top = logits.amax(-1, keepdim=True).clamp_min(-1e30)
+    p = logits.sub_(top).exp_()
+    total = p.sum(-1)
+    o = (p.view(n, H, most * G, keys) @ v).view(n, H, most, G, d)
+    packed = lambda x: x.transpose(1, 2)[there].flatten(1, 2)  # noqa: E731
+    return packed(top[..., 0]), packed(total), packed(o)
+
+
+def run_shared(s):
+    if own:
+        from paper_2604_10235_amd import binding as cc
+        cc.codecomp_attend_shared(s["q"], s["batch"], s["shared"], s["pages"], 0, s["out"], s["workspace"], lse=s["lse"])
+        return {"out": s["out"], "lse": s["lse"]}
+    c = s["case"]
+    # shared rows, once for a group: all of its tokens see all of them
+    key = torch.arange(max(s["prefixes"]), device="cuda")[None, :].expand(c["groups"], -1)
+    held = key < s["prefix_lens"][:, None]
+    table = s["table"][s["cu_groups"][:-1].long()]
+    offsets = s["cu"][s["cu_groups"].long()]
+    q, there = by_owner(s, np.diff(s["cu_host"][s["members"]]), offsets)
+    k, v = gathered(s, "k", table, key, held), gathered(s, "v", table, key, held)
+    top_a, total_a, o_a = part(s, q, there, k, v, (~held)[:, None, :].expand(-1, there.shape[1], -1))
+    # each request's own rows
+    start = s["prefix_lens"][torch.repeat_interleave(torch.arange(c["groups"], device="cuda"), s["cu_groups"].diff(), output_size=c["seqs"])]
+    key = start[:, None] + torch.arange(max(s["owns"]), device="cuda")[None, :]
+    held = key < s["kv_lens"][:, None]
+    q, there = by_owner(s, s["news"], s["cu"])
+    k, v = gathered(s, "k", s["table"], key, held), gathered(s, "v", s["table"], key, held)
+    new = torch.arange(there.shape[1], device="cuda")
+    last = s["kv_lens"][:, None] - s["cu"].diff()[:, None] + new[None, :] + 1 if c["causal"] else s["kv_lens"][:, None].expand(-1, len(new))
+    hidden = key[:, None, :] >= torch.minimum(last, s["kv_lens"][:, None])[:, :, None]
+    top_b, total_b, o_b = part(s, q, there, k, v, hidden)
+    top = torch.maximum(top_a, top_b)
+    a, b = (top_a - top).exp(), (top_b - top).exp()
+    total = a * total_a + b * total_b
+    s["out"].copy_((a[..., None] * o_a + b[..., None] * o_b) / total[..., None])
+    s["lse"].copy_(top + total.log())
+    return {"out": s["out"], "lse": s["lse"]}
+
+
+def run_mass(s):
+    c = s["case"]
+    if own:
+        from paper_2604_10235_amd import binding as cc
+        cc.codecomp_attend_mass(s["q"], s["lse"], s["batch"], s["pages"], 0, s["mass"], s["workspace"], first=s["first"], decay=c["decay"])
+        return {"sums": s["sums"]}
+    H, G, n = c["kv_heads"], c["q_heads"] // c["kv_heads"], c["seqs"]
+    key = c["first"] + torch.arange(max(s["owns"]), device="cuda")[None, :].expand(n, -1)
+    held = key < s["kv_lens"][:, None]
+    counts = s["cu"].diff()
+    q, there = by_owner(s, s["news"], s["cu"])
+    most = there.shape[1]
+    k = gathered(s, "k", s["table"], key, held)
+    logits = (q @ k.transpose(2, 3).contiguous()).mul_(c["head_dim"] ** -0.5).view(n, H, most, G, -1)
+    new = torch.arange(most, device="cuda")
+    last = s["kv_lens"][:, None] - counts[:, None] + new[None, :] + 1 if c["causal"] else s["kv_lens"][:, None].expand(n, most)
+    hidden = (key[:, None, :] >= torch.minimum(last, s["kv_lens"][:, None])[:, :, None]) | ~there[:, :, None]
+    lse = torch.zeros((n, most, H, G), device="cuda")
+    lse[there] = s["lse"].unflatten(1, (H, G))
+    logits.masked_fill_(hidden[:, None, :, None, :], -torch.inf).sub_(lse.permute(0, 2, 1, 3)[..., None])
+    add = logits.exp_().view(n, H, most * G, -1).sum(2) / G                                       # [n, H, rows behind the first]
+    old = key < (s["kv_lens"] - counts)[:, None] if c["causal"] else held
+    part_of = s["sums"][0, :, :, c["first"] :]
+    now = torch.where(old[:, None, :], c["decay"] * part_of, 0.0) + add
+    part_of.copy_(torch.where(held[:, None, :], now, part_of))
+    return {"sums": s["sums"]}
+
+
+def run_evict(s):
+    c = s["case"]
+    if own:
+        from paper_2604_10235_amd import binding as cc
+        cc.codecomp_evict(s["mass"], s["eviction"], s["pages"], s["kept"], s["new_lens"], kept_mass=s["kept_mass"])
+    else:
+        L, H, n, longest, most = c["layers"], c["kv_heads"], c["seqs"], max(s["total"]), c["budget"]
+        row = torch.arange(longest, device="cuda")
+        behind = s["kv_lens"] - s["first"]
+        # rank by sums, protected rows out of it, the last ones first of all; equal ones in their order
+        keys = s["sums"].masked_fill(row[None, :] >= s["kv_lens"][:, None, None], -torch.inf)
+        keys.masked_fill_((row[None, :] < s["first"][:, None])[:, None, :], -torch.inf)
+        keys.masked_fill_(((row[None, :] >= (s["kv_lens"] - c["recent"])[:, None]) & (row[None, :] >= s["first"][:, None]) & (row[None, :] < s["kv_lens"][:, None]))[:, None, :], torch.inf)
+        count = torch.minimum(behind, s["budgets"])
+        best = keys.sort(dim=-1, descending=True, stable=True).indices[..., :most]
+        there = torch.arange(best.shape[-1], device="cuda")[None, :] < count[:, None]                 # [n, most]
+        kept = best.masked_fill(~there[:, None, :], longest).sort(dim=-1).values
+        s["kept"].fill_(-1)
+        s["kept"][..., : kept.shape[-1]] = kept.masked_fill(~there[:, None, :], -1).int()
+        s["new_lens"].copy_(s["first"] + count)
+        # rows [l, r, h, i] <- kept[l, r, h, i]; all are read before any is written
+        l, r, h, i = there[None, :, None, :].expand(L, n, H, -1).nonzero(as_tuple=True)
+        source, target = kept[l, r, h, i], s["first"][r] + i
+        a, b = s["table"][r, source // c["page"]].long(), s["table"][r, target // c["page"]].long()
+        for p in (bits(s["k_pages"]), bits(s["v_pages"])):
+            p[l, b, h, target % c["page"]] = p[l, a, h, source % c["page"]]
+        s["kept_sums"][l, r, h, target] = s["sums"][l, r, h, source]
+    return {"kept": s["kept"], "new_lens": s["new_lens"], "kept_sums": s["kept_sums"], "k_pages": s["k_pages"], "v_pages": s["v_pages"]}
+
+
+# ---------------------------------------------------------------- work and exact values
+
+def work(c):
+    c = dict(DEFAULTS, **c)
+    d, Hq, Hkv, esz = c["head_dim"], c["q_heads"], c["kv_heads"], 1 if c["kv"] == "fp8_e4m3" else 2
+    news, owns, before, of = lengths(c)
+    if c["op"] == "evict":
+        # a row moves if one before it goes: behind the first of (rows - budget) evicted ones
+        moved = [0 if n <= c["budget"] else c["budget"] - min(c["budget"], n // (n - c["budget"] + 1)) for n in owns]
+        kept = sum(min(n, c["budget"]) for n in owns)
+        return {"bytes": c["layers"] * Hkv * (4 * sum(owns) + 8 * kept + sum(moved) * 4 * d * esz), "flops": 0}
+    pairs = sum(n * k - (n * (n - 1) // 2 if c["causal"] else 0) for n, k in zip(news, owns))
+    if c["op"] == "mass":
+        sums = sum(owns) * 8
+        return {"bytes": sum(owns) * Hkv * d * esz + Hkv * sums + sum(news) * Hq * (2 * d + 4), "flops": 2 * pairs * Hq * d}
+    pairs += sum(n * b for n, b in zip(news, before))
+    rows = sum(owns) + sum({g: b for g, b in zip(of, before)}.values())
+    return {"bytes": 2 * rows * Hkv * d * esz + sum(news) * Hq * (4 * d + 4), "flops": 4 * pairs * Hq * d}
+
+
+def exact(c, seed):
+    """Copies of rows have nothing computed: no value in 64 bits is asked for."""
+    c = dict(DEFAULTS, **c)
+    if c["op"] == "evict":
+        return None
+    global own
+    was, own = own, False
+    try:
+        s = prepare(c, seed)
+    finally:
+        own = was
+    T, Hq, d, G = sum(s["news"]), c["q_heads"], c["head_dim"], c["q_heads"] // c["kv_heads"]
+    if c["op"] == "mass":
+        sums = s["sums"].double()
+        for r in range(c["seqs"]):
+            a, n, kept = int(s["cu_host"][r]), s["news"][r], s["total"][r]
+            k, old = rows_of(c, s, r, "k"), kept - n if c["causal"] else kept
+            for h in range(c["kv_heads"]):
+                now = torch.cat([c["decay"] * sums[0, r, h, :old], torch.zeros(kept - old, dtype=torch.float64, device="cuda")])
+                for g in range(G):
+                    z = logits_of(c, s, r, h * G + g, k, torch.float64)
+                    now += torch.exp(z - s["lse"][a : a + n, h * G + g].double()[:, None]).sum(0) / G
+                sums[0, r, h, c["first"] : kept] = now[c["first"] :]
+        return {"sums": sums}
+    out, lse = torch.zeros((T, Hq, d), dtype=torch.float64, device="cuda"), torch.full((T, Hq), -torch.inf, dtype=torch.float64, device="cuda")
+    for r in range(c["seqs"]):
+        a, n = int(s["cu_host"][r]), s["news"][r]
+        k, v = rows_of(c, s, r, "k"), rows_of(c, s, r, "v")
+        for h in range(Hq):
+            z = logits_of(c, s, r, h, k, torch.float64)
+            lse[a : a + n, h] = torch.logsumexp(z, 1)
+            out[a : a + n, h] = torch.softmax(z, 1) @ v[h // G]
+    return {"out": out, "lse": lse}
