@@ -222,7 +222,8 @@ def prepare_shared(c, s, gen):
     s["lse"] = torch.empty((sum(s["news"]), c["q_heads"]), dtype=torch.float32, device="cuda")
     if own:
         from paper_2604_10235_amd import binding as cc
-        s["shared"] = cc.make_groups(cu_groups_host=s["members"], cu_groups=s["cu_groups"], prefix_lens=s["prefix_lens"], max_prefix_len=max(s["prefixes"]))
+        s["shared"] = cc.make_groups(cu_groups_host=s["members"], cu_groups=s["cu_groups"], prefix_lens=s["prefix_lens"], max_prefix_len=max(s["prefixes"]),
+                                    max_own_len=max(s["owns"]))
         s["workspace"] = torch.empty(max(256, cc.codecomp_attend_shared_workspace_bytes(s["batch"], s["shared"], s["pages"])), dtype=torch.uint8, device="cuda")
 
 
