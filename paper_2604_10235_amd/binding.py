@@ -64,6 +64,21 @@ class codecomp_rotary(C.Structure):
     _fields_ = [("dim", C.c_int32), ("interleaved", C.c_int32), ("inverse", C.c_int32), ("magnitude", C.c_float), ("freq", C.c_double * 64)]
 
 
+class codecomp_groups(C.Structure):
+    _fields_ = [("n_groups", C.c_int32), ("max_prefix_len", C.c_int32), ("max_own_len", C.c_int32), ("cu_groups_host", C.c_void_p), ("cu_groups_dev", C.c_void_p),
+                ("prefix_lens_dev", C.c_void_p)]
+
+
+class codecomp_mass(C.Structure):
+    _fields_ = [("sums", C.c_void_p), ("n_layers", C.c_int32), ("n_seqs", C.c_int32), ("n_kv_heads", C.c_int32), ("width", C.c_int32),
+                ("stride_layer", C.c_int64), ("stride_seq", C.c_int64), ("stride_head", C.c_int64)]
+
+
+class codecomp_eviction(C.Structure):
+    _fields_ = [("n_seqs", C.c_int32), ("table_width", C.c_int32), ("max_kv_len", C.c_int32), ("max_budget", C.c_int32), ("recent", C.c_int32),
+                ("kv_lens_dev", C.c_void_p), ("table_dev", C.c_void_p), ("budgets_dev", C.c_void_p), ("first_dev", C.c_void_p)]
+
+
 class CodecompError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -125,6 +140,7 @@ def lib() -> C.CDLL:
         l.codecomp_chunk_budgets.argtypes = [DP, IP, C.c_int32, C.c_double, C.c_double, C.c_double, C.c_double,
                                              C.c_double, C.c_int32, IP]
         PP, BP, RP, V = C.POINTER(codecomp_pages), C.POINTER(codecomp_batch), C.POINTER(codecomp_rotary), C.c_void_p
+        GP, MP = C.POINTER(codecomp_groups), C.POINTER(codecomp_mass)
         for name, args in {
             "rotary_init": [RP, C.c_int32, C.c_int32, C.c_double, C.c_int32] + [C.c_double] * 4,
             "rotate": [V, V, RP, C.c_int32, C.c_int32, C.c_int32, C.c_int64, C.c_int64, V, C.c_int64, C.c_int64, V],
@@ -135,11 +151,20 @@ def lib() -> C.CDLL:
             "pages_copy": [PP, V, C.c_int32, V],
             "attend_validate": [BP, PP],
             "attend": [V, BP, PP, C.c_int32, V, V, V, C.c_size_t, V],
+            "attend_shared_validate": [BP, GP, PP],
+            "attend_shared": [V, BP, GP, PP, C.c_int32, V, V, V, C.c_size_t, V],
+            "attend_mass_validate": [BP, PP, MP],
+            "attend_mass": [V, V, BP, PP, C.c_int32, V, C.c_float, MP, V, C.c_size_t, V],
+            "evict": [MP, C.POINTER(codecomp_eviction), PP, V, V, MP, V],
         }.items():
             f = getattr(l, "codecomp_" + name)
             f.restype, f.argtypes = C.c_int, args
         l.codecomp_attend_workspace_bytes.restype = C.c_size_t
         l.codecomp_attend_workspace_bytes.argtypes = [BP, PP]
+        l.codecomp_attend_shared_workspace_bytes.restype = C.c_size_t
+        l.codecomp_attend_shared_workspace_bytes.argtypes = [BP, GP, PP]
+        l.codecomp_attend_mass_workspace_bytes.restype = C.c_size_t
+        l.codecomp_attend_mass_workspace_bytes.argtypes = [BP, PP, MP]
         l.codecomp_status_string.restype = C.c_char_p
         l.codecomp_status_string.argtypes = [C.c_int]
         l.codecomp_version.restype = C.c_int
@@ -539,6 +564,120 @@ def codecomp_attend(q, batch: codecomp_batch, pages: codecomp_pages, layer: int,
     stream = _launch_stream(at, batch._at, q.get_device(), out.get_device(), _at(lse, at), _at(workspace, at))
     size = 0 if workspace is None else workspace.numel() * workspace.element_size()
     _check(lib().codecomp_attend(qp, C.byref(batch), C.byref(pages), layer, op, _ptr(lse), _ptr(workspace), size, stream), "codecomp_attend")
+
+
+# ---- long and branching service (codecomp_serve.h)
+
+def make_groups(*, cu_groups_host: np.ndarray, cu_groups, prefix_lens, max_prefix_len: int, max_own_len: int) -> codecomp_groups:
+    """Groups of requests that share their first rows.  cu_groups, prefix_lens: device int32 tensors [n_groups + 1], [n_groups]; the host array cu_groups_host
+    (same values as cu_groups; copied) and the two bounds size the launches."""
+    host = np.array(cu_groups_host, dtype=np.int32, order="C")
+    n = len(host) - 1
+    _int32(cu_groups, (n + 1,), "cu_groups")
+    _int32(prefix_lens, (n,), "prefix_lens")
+    if cu_groups.device != prefix_lens.device:
+        raise ValueError("cu_groups and prefix_lens must be on the same device")
+    g = codecomp_groups()
+    g.n_groups, g.max_prefix_len, g.max_own_len = n, max_prefix_len, max_own_len
+    g.cu_groups_host, g.cu_groups_dev, g.prefix_lens_dev = host.ctypes.data, cu_groups.data_ptr(), prefix_lens.data_ptr()
+    g._keep, g._at = (host, cu_groups, prefix_lens), cu_groups.get_device()
+    return g
+
+
+def codecomp_attend_shared_workspace_bytes(batch, groups, pages) -> int:
+    args = C.byref(batch), C.byref(groups), C.byref(pages)
+    _check(lib().codecomp_attend_shared_validate(*args), "codecomp_attend_shared_validate")
+    return lib().codecomp_attend_shared_workspace_bytes(*args)
+
+
+def _workspace(workspace):
+    """Address and bytes."""
+    if workspace is None:
+        return 0, 0
+    if not workspace.is_contiguous():
+        raise ValueError("the workspace must be contiguous")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _row_floats(t, shape, what: str) -> int:
+    if t.dtype is not (_torch_module or _torch()).float32 or t.shape != shape or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous float32 tensor {shape}, not {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def codecomp_attend_shared(q, batch: codecomp_batch, groups: codecomp_groups, pages: codecomp_pages, layer: int, out, workspace, lse=None) -> None:
+    """codecomp_attend, with the rows that the requests of a group share read once for all of them."""
+    shape = (batch._tokens, batch.n_q_heads, pages.head_dim)
+    qp, op = _vectors(q, "q", shape, batch.q_stride_tok, batch.q_stride_head), _vectors(out, "out", shape, batch.out_stride_tok, batch.out_stride_head)
+    lp = 0 if lse is None else _row_floats(lse, shape[:2], "lse")
+    wp, size = _workspace(workspace)
+    at = pages._at
+    stream = _launch_stream(at, batch._at, groups._at, q.get_device(), out.get_device(), _at(lse, at), _at(workspace, at))
+    _check(lib().codecomp_attend_shared(qp, C.byref(batch), C.byref(groups), C.byref(pages), layer, op, lp, wp, size, stream), "codecomp_attend_shared")
+
+
+def make_mass(sums) -> codecomp_mass:
+    """Sums of attention weights over a float32 tensor [layers, requests, KV heads, rows], contiguous in its rows."""
+    torch = _torch()
+    if sums.dim() != 4 or sums.dtype != torch.float32:
+        raise ValueError("sums must be a float32 tensor [layers, requests, KV heads, rows]")
+    if sums.stride(3) != 1 and sums.shape[3] > 1:
+        raise ValueError("the sums of a head must be contiguous")
+    m = codecomp_mass()
+    m.stride_layer, m.stride_seq, m.stride_head = _own_strides(sums, "sums")[:3]
+    extent = 1                                    # no two elements at one place: every stride spans what the smaller ones reach
+    for stride, n in sorted((s, n) for n, s in zip(sums.shape, sums.stride()) if n > 1):
+        if stride < extent:
+            raise ValueError(f"sums must not overlap (strides {sums.stride()})")
+        extent = stride * n
+    m.sums = sums.data_ptr()
+    m.n_layers, m.n_seqs, m.n_kv_heads, m.width = sums.shape
+    m._keep, m._at = sums, sums.get_device()
+    return m
+
+
+def codecomp_attend_mass_workspace_bytes(batch, pages, mass) -> int:
+    args = C.byref(batch), C.byref(pages), C.byref(mass)
+    _check(lib().codecomp_attend_mass_validate(*args), "codecomp_attend_mass_validate")
+    return lib().codecomp_attend_mass_workspace_bytes(*args)
+
+
+def codecomp_attend_mass(q, lse, batch: codecomp_batch, pages: codecomp_pages, layer: int, mass: codecomp_mass, workspace, first=None, decay: float = 1.0) -> None:
+    """Weights of the new tokens of `batch`, whose queries q and log-sum-exps lse attention had, added to the sums of the rows from first[r] on."""
+    shape = (batch._tokens, batch.n_q_heads, pages.head_dim)
+    qp, lp = _vectors(q, "q", shape, batch.q_stride_tok, batch.q_stride_head), _row_floats(lse, shape[:2], "lse")
+    if first is not None:
+        _int32(first, (batch.n_seqs,), "first")
+    wp, size = _workspace(workspace)
+    at = pages._at
+    stream = _launch_stream(at, batch._at, mass._at, q.get_device(), lse.get_device(), _at(first, at), _at(workspace, at))
+    _check(lib().codecomp_attend_mass(qp, lp, C.byref(batch), C.byref(pages), layer, _ptr(first), decay, C.byref(mass), wp, size, stream), "codecomp_attend_mass")
+
+
+def make_eviction(*, kv_lens, table, budgets, max_kv_len: int, max_budget: int, recent: int, first=None) -> codecomp_eviction:
+    """What codecomp_evict keeps of n_seqs requests: kv_lens, budgets, first: device int32 tensors [n_seqs], table [n_seqs, width]."""
+    n = kv_lens.shape[0]
+    _int32(kv_lens, (n,), "kv_lens")
+    _int32(budgets, (n,), "budgets")
+    _int32(table, (n, table.shape[-1]), "table")
+    if first is not None:
+        _int32(first, (n,), "first")
+    if len({t.device for t in (kv_lens, table, budgets, *([] if first is None else [first]))}) > 1:
+        raise ValueError("kv_lens, table, budgets and first must be on the same device")
+    e = codecomp_eviction()
+    e.n_seqs, e.table_width, e.max_kv_len, e.max_budget, e.recent = n, table.shape[1], max_kv_len, max_budget, recent
+    e.kv_lens_dev, e.table_dev, e.budgets_dev, e.first_dev = kv_lens.data_ptr(), table.data_ptr(), budgets.data_ptr(), _ptr(first)
+    e._keep, e._at = (kv_lens, table, budgets, first), kv_lens.get_device()
+    return e
+
+
+def codecomp_evict(mass: codecomp_mass, eviction: codecomp_eviction, pages: codecomp_pages, kept, new_lens, kept_mass: Optional[codecomp_mass] = None) -> None:
+    """kept: int32 [layers, requests, KV heads, max_budget]; new_lens: int32 [requests], not the eviction's kv_lens.  kept_mass None: the sums move in place."""
+    _int32(kept, (mass.n_layers, mass.n_seqs, mass.n_kv_heads, eviction.max_budget), "kept")
+    _int32(new_lens, (mass.n_seqs,), "new_lens")
+    stream = _launch_stream(pages._at, mass._at, eviction._at, kept.get_device(), new_lens.get_device(), pages._at if kept_mass is None else kept_mass._at)
+    _check(lib().codecomp_evict(C.byref(mass), C.byref(eviction), C.byref(pages), kept.data_ptr(), new_lens.data_ptr(),
+                                None if kept_mass is None else C.byref(kept_mass), stream), "codecomp_evict")
 
 
 class DeviceProblem:

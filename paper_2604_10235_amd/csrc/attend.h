@@ -25,6 +25,18 @@ struct CutBlock {
   int32_t last;                // last workgroup with a part of it (those after the first in slot 2 * workgroup)
 };
 
+// Groups of requests that share the rows at the start of their caches (attend_shared.hip).
+struct SharedRows {
+  const int32_t* cu_groups;
+  const int32_t* prefix_lens;
+  int n_groups, max_prefix, max_own;
+  int few_units, few_parts, few_chunk, few_splits;       // shared rows of groups of few rows: workgroups, parts of the rows, keys of a chunk, chunks
+  int many_units, many_blocks, many_tiles, many_splits;  // of many: workgroups, most blocks of rows of a group, tiles of a chunk, chunks
+  int splits;                  // the larger one: parts of shared rows that every row has
+};
+// What a row's parts say that had no keys: not to be read any further.
+constexpr float kNoPart = -1.0f;
+
 struct AttendArgs {
   PagePool pool;
   PagedBatch b;
@@ -39,6 +51,24 @@ struct AttendArgs {
   int shares;                  // few rows: equal parts that all keys are cut into; 0: chunks
   CutBlock* cuts;              // [shares]
 };
+// Part p of row t * Hq + h is part_o[(p * T * Hq + row)].
+struct SharedArgs : AttendArgs {
+  SharedRows sh;
+};
+
+__device__ __forceinline__ int prefix_of(const SharedRows& sh, int g) { return min(max(sh.prefix_lens[g], 0), sh.max_prefix); }
+// Parts first .. last - 1 of rows row0 .. row1 - 1 of a KV head, which has tokens from q0 on: nothing in them.
+template <int THREADS>
+__device__ __forceinline__ void no_parts(const AttendArgs& a, int first, int last, int q0, int head, int row0, int row1) {
+  const int64_t all = (int64_t)a.b.T * a.b.Hq;
+  for (int row = row0 + threadIdx.x; row < row1; row += THREADS) {
+    const int t = row / a.b.G, h = head * a.b.G + row - t * a.b.G;
+    for (int p = first; p < last; ++p) {
+      const int64_t part = p * all + (int64_t)(q0 + t) * a.b.Hq + h;
+      a.part_ml[2 * part] = -INFINITY; a.part_ml[2 * part + 1] = kNoPart;
+    }
+  }
+}
 
 // The same in all lanes, and known to be: in scalar registers.
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
@@ -101,5 +131,6 @@ __device__ __forceinline__ s16x4 read_columns(const unsigned char* lds) {
 }
 
 int launch_few(const AttendPlan& pl, const AttendArgs& a, hipStream_t stream);
+int launch_few_shared(int d, bool fp8, bool two_blocks, int64_t units, const SharedArgs& a, hipStream_t stream);
 
 }  // namespace codecomp

@@ -15,6 +15,8 @@
 // Measured (a kernel that only reads reaches 6.4 TB/s): 64 steps over 500 .. 16384 keys, 4 KV heads of 128 elements, bf16: 187 us, 5.3 TB/s; with 8 KV heads, 8
 // bits: 184 us, 5.5 TB/s; one step over 131072 keys: 56 us, 4.8 TB/s (51 the kernel, 6 the join); one over 2113: 10 us (7 and 4), a chain of small loads
 // (lengths, table, rows, parts) that nothing hides.
+#include <type_traits>
+
 #include "attend.h"
 
 namespace codecomp {
@@ -45,9 +47,10 @@ __device__ __forceinline__ int strips_of(const AttendArgs& a, int r) {
   return rows <= 0 || rows > a.row_slots ? 0 : max(1, (kv_len_of(a.b, r) + kFewStrip - 1) / kFewStrip);
 }
 
-// EVEN: the strips of all requests and heads form one sequence, cut into equal parts; else a workgroup has one chunk of a request.
-template <int D, bool FP8, int RB, bool EVEN>
-__global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void attend_few_kernel(const AttendArgs a) {
+// EVEN: the strips of all requests and heads form one sequence, cut into equal parts; else a workgroup has one chunk of a request, or (SHARED) of the rows that
+// a group shares, or of a request's rows behind them, and leaves parts of all rows.
+template <int D, bool FP8, int RB, bool EVEN, bool SHARED = false>
+__global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void attend_few_kernel(const std::conditional_t<SHARED, SharedArgs, AttendArgs> a) {
   using T = FewTile<D, FP8>;
   constexpr int KS = D / 32, DB = D / 16;
   __shared__ __attribute__((aligned(16))) unsigned char lds[kFewWaves * T::BYTES];
@@ -66,6 +69,8 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void atten
   };
   int64_t total = 0, shares = 0, at_strip = 0;
   CutBlock cut = {-1, 0, 0, 0};
+  int shared_q0 = 0, shared_nq = 0, shared_len = 0, shared_part = 0, key_end = 0;        // SHARED: tokens of the group or request, keys up to which there are some, number of the part
+  int causal = SHARED ? 0 : a.b.causal;
   if constexpr (EVEN) {
     share = blockIdx.x;
     row0 = 0;
@@ -106,6 +111,43 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void atten
     }
     __syncthreads();
     r = uniform(found[0]); strip = uniform(found[1]);
+  } else if constexpr (SHARED) {
+    const bool group = (int)blockIdx.x < a.sh.few_units;
+    const int unit = group ? blockIdx.x : blockIdx.x - a.sh.few_units, parts = group ? a.sh.few_parts : a.row_parts;
+    const int items = (group ? a.sh.n_groups : a.b.n_seqs) * a.b.Hkv, turn = unit / items, item = unit - turn * items, split = turn / parts;
+    row0 = (turn - split * parts) * (16 * RB);
+    r = item / a.b.Hkv; head = item - r * a.b.Hkv;
+    if (group) {
+      const int g = r, end = a.sh.cu_groups[g + 1];
+      r = a.sh.cu_groups[g];
+      if (r >= end) return;
+      shared_q0 = a.b.cu_q[r];
+      shared_nq = a.b.cu_q[end] - shared_q0;
+      if (shared_nq > kFewRowsMost || shared_nq * a.b.G > kFewRowsMost || shared_nq * a.b.G <= row0) return;
+      shared_len = uniform(prefix_of(a.sh, g));
+      key0 = split * a.sh.few_chunk;
+      key_end = key0 + a.sh.few_chunk;
+      shared_part = split;
+      if (split == 0) no_parts<64 * kFewWaves>(a, a.sh.few_splits, a.sh.splits, shared_q0, head, row0, min(shared_nq * a.b.G, row0 + 16 * RB));
+    } else {
+      shared_q0 = a.b.cu_q[r];
+      shared_nq = a.b.cu_q[r + 1] - shared_q0;
+      if (shared_nq * a.b.G <= row0) return;
+      const int before = uniform(prefix_of(a.sh, request_of(a.sh.cu_groups, a.sh.n_groups, r)));
+      shared_len = uniform((int)min((int64_t)kv_len_of(a.b, r), (int64_t)before + a.sh.max_own));
+      key0 = (int)min(before + (int64_t)split * a.chunk, (int64_t)INT32_MAX);
+      key_end = (int)min((int64_t)key0 + a.chunk, (int64_t)INT32_MAX);
+      shared_part = a.sh.splits + split;
+      causal = a.b.causal;
+    }
+    if (key0 >= shared_len) {
+      no_parts<64 * kFewWaves>(a, shared_part, shared_part + 1, shared_q0, head, row0, min(shared_nq * a.b.G, row0 + 16 * RB));
+      return;
+    }
+    table = a.b.table + (int64_t)r * a.b.table_width;
+    key_end = min(key_end, shared_len);
+    look_up(page, key0 + wave * kFewKeys, key_end);
+    look_up(next_page, key0 + (kFewWaves + wave) * kFewKeys, key_end);
   } else {
     // Chunk by chunk, all requests and heads of one: neighbouring workgroups run on different dies, and must not be the same chunks of all
     // requests there (short requests lack the later ones).
@@ -120,8 +162,8 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void atten
   }
   for (;;) {
     if constexpr (EVEN) asm("" : "+v"(l16), "+v"(quarter));         // what follows from them is worked out per piece, not held in registers from piece to piece
-    const int q0 = a.b.cu_q[r], nq = a.b.cu_q[r + 1] - q0, rows = nq * a.b.G;
-    const int len = uniform(kv_len_of(a.b, r));
+    const int q0 = SHARED ? shared_q0 : a.b.cu_q[r], nq = SHARED ? shared_nq : a.b.cu_q[r + 1] - q0, rows = nq * a.b.G;
+    const int len = SHARED ? shared_len : uniform(kv_len_of(a.b, r));
     int key1;
     bool whole;                                                    // no other workgroup has keys of these rows
     if constexpr (EVEN) {
@@ -136,6 +178,9 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void atten
       at_strip += end - strip;
       look_up(page, key0 + wave * kFewKeys, key1);
       look_up(next_page, key0 + (kFewWaves + wave) * kFewKeys, key1);
+    } else if constexpr (SHARED) {
+      key1 = key_end;
+      whole = false;
     } else {
       if (rows <= row0 || rows > a.row_slots) return;
       key1 = min(len, key0 + a.chunk);
@@ -155,9 +200,9 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void atten
         qf[rb][ks] = *reinterpret_cast<const u32x4*>(p + T::q_element(ks, quarter));
         if (row >= rows) qf[rb][ks] = u32x4{0, 0, 0, 0};
       }
-      limit[rb] = a.b.causal ? min(len, len - nq + t + 1) : len;
+      limit[rb] = causal ? min(len, len - nq + t + 1) : len;
     }
-    const int seen_by_all = a.b.causal ? len - nq + 1 : len;
+    const int seen_by_all = causal ? len - nq + 1 : len;
 
     const unsigned char* kb = a.pool.k + a.layer + head * a.pool.s_head + quarter * 16;
     const unsigned char* vb = a.pool.v + a.layer + head * a.pool.s_head + quarter * 16;
@@ -308,7 +353,7 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void atten
 
     if (__builtin_expect(__ballot(left_out != 0) != 0, 0)) {
       // from the first tile that was cleaned on: the keys before seen_by_all in it were as well
-      for (int key = max(seen_by_all & -kFewKeys, key0); key < key1; ++key) {
+      for (int key = SHARED ? key0 + (max(seen_by_all - key0, 0) & -kFewKeys) : max(seen_by_all & -kFewKeys, key0); key < key1; ++key) {
         const int at = table[key >> a.pool.page_log2];
         if ((key - key0) / kFewKeys % kFewWaves != wave || at < 0 || at >= a.pool.n_pages) continue;          // another wave's
         const unsigned char* row = a.pool.v + a.layer + head * a.pool.s_head + at * a.pool.s_page + (key & in_page) * a.pool.s_tok;
@@ -364,7 +409,7 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void atten
           for (int i = 0; i < E; i += 2) *reinterpret_cast<unsigned*>(out + i) = pack2(x[i] * inv, x[i + 1] * inv);
           if (a.lse && (tid & 15) == 0) a.lse[(int64_t)(q0 + t) * a.b.Hq + h] = all == 0.0f ? -INFINITY : (to + __builtin_amdgcn_logf(all)) * kLn2;
         } else {
-          const int64_t part = part0 + row;
+          const int64_t part = SHARED ? ((int64_t)shared_part * a.b.T + q0 + row / a.b.G) * a.b.Hq + head * a.b.G + row % a.b.G : part0 + row;
 #pragma unroll
           for (int i = 0; i < E; i += 4) *reinterpret_cast<f32x4*>(a.part_o + part * D + e + i) = f32x4{x[i], x[i + 1], x[i + 2], x[i + 3]};
           if ((tid & 15) == 0) { a.part_ml[2 * part] = to; a.part_ml[2 * part + 1] = all; }
@@ -488,6 +533,19 @@ static int launch_few_rows(const AttendArgs& a, hipStream_t stream) {
 int launch_few(const AttendPlan& pl, const AttendArgs& a, hipStream_t stream) {
   if (pl.d == 128) return pl.pool.fp8 ? launch_few_rows<128, true>(a, stream) : launch_few_rows<128, false>(a, stream);
   return pl.pool.fp8 ? launch_few_rows<64, true>(a, stream) : launch_few_rows<64, false>(a, stream);
+}
+
+template <int D, bool FP8>
+static int launch_few_shared_of(bool two_blocks, int64_t units, const SharedArgs& a, hipStream_t stream) {
+  const dim3 grid((unsigned)units), block(64 * kFewWaves);
+  if (two_blocks) attend_few_kernel<D, FP8, 2, false, true><<<grid, block, 0, stream>>>(a);
+  else attend_few_kernel<D, FP8, 1, false, true><<<grid, block, 0, stream>>>(a);
+  return (int)hipGetLastError();
+}
+
+int launch_few_shared(int d, bool fp8, bool two_blocks, int64_t units, const SharedArgs& a, hipStream_t stream) {
+  if (d == 128) return fp8 ? launch_few_shared_of<128, true>(two_blocks, units, a, stream) : launch_few_shared_of<128, false>(two_blocks, units, a, stream);
+  return fp8 ? launch_few_shared_of<64, true>(two_blocks, units, a, stream) : launch_few_shared_of<64, false>(two_blocks, units, a, stream);
 }
 
 }  // namespace codecomp

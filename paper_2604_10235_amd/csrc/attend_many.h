@@ -45,6 +45,7 @@ struct ManyArgs {
   CutBlock* cuts;              // [workgroups]
   int workgroups, rows_from;   // requests of fewer rows are not this kernel's
   int whole;                   // 1: no block is shared (all are short): nothing to be joined
+  SharedRows sh;               // SHARED
 };
 
 // Tiles of 64 keys that a block of rows of a request meets; at least one.
@@ -85,7 +86,8 @@ struct TileAt {
 };
 
 // ROWWISE: pages of less than 16 rows; else the 16 rows that a wave loads of a tile lie in one page, whose place is worked out in scalar registers.
-template <int D, bool FP8, bool ROWWISE>
+// SHARED: a workgroup has a chunk of the rows that a group of requests shares, for a block of the group's rows, and leaves parts of them.
+template <int D, bool FP8, bool ROWWISE, bool SHARED = false>
 __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const ManyArgs ma) {
   const AttendArgs& a = ma.a;
   constexpr int PIECES = D * (FP8 ? 1 : 2) / 16;               // 16-byte pieces of a stored row
@@ -120,7 +122,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
   for (int r = min(tid * per, n); r < min(tid * per + per, n); ++r) {
     const Blocks x = blocks_of(ma, r);
     my_blocks += x.count;
-    if (kept) { requests[0][r] = x.len; requests[1][r] = x.q0; requests[2][r] = x.nq; }
+    if (!SHARED && kept) { requests[0][r] = x.len; requests[1][r] = x.q0; requests[2][r] = x.nq; }
   }
   int blocks = my_blocks;                                        // up to here, inclusive
 #pragma unroll
@@ -128,8 +130,10 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
     const int y = __shfl_up(blocks, off);
     if (lane >= off) blocks += y;
   }
-  if (lane == 63) wave_sum[wave] = blocks;
-  __syncthreads();
+  if constexpr (!SHARED) {
+    if (lane == 63) wave_sum[wave] = blocks;
+    __syncthreads();
+  }
   int all_blocks = 0;
 #pragma unroll
   for (int w = 0; w < kManyWaves; ++w) {
@@ -137,13 +141,15 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
     all_blocks += (int)wave_sum[w];
   }
   int* first_block = reinterpret_cast<int*>(tiles_lds);           // of a thread's requests
-  first_block[tid] = blocks - my_blocks;
-  __syncthreads();
+  if constexpr (!SHARED) {
+    first_block[tid] = blocks - my_blocks;
+    __syncthreads();
+  }
   const int block_per = (uniform(all_blocks) + kManyThreads - 1) / kManyThreads;
   const int b0 = min(tid * block_per, all_blocks), b1 = min(b0 + block_per, all_blocks);
   int my_r = 0, my_i = 0;                                         // request of block b0, and its number there
   int64_t mine = 0;                                               // positions of this thread's blocks
-  if (b0 < b1) {
+  if (!SHARED && b0 < b1) {
     int lo = 0;                                                  // last thread whose requests begin at b0 or before, and have blocks from there on
 #pragma unroll
     for (int step = kManyThreads / 2; step > 0; step >>= 1)
@@ -164,9 +170,11 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
     const int64_t y = __shfl_up(incl, off);
     if (lane >= off) incl += y;
   }
-  __syncthreads();
-  if (lane == 63) wave_sum[wave] = incl;
-  __syncthreads();
+  if constexpr (!SHARED) {
+    __syncthreads();
+    if (lane == 63) wave_sum[wave] = incl;
+    __syncthreads();
+  }
   int64_t before = 0, per_head = 0;
 #pragma unroll
   for (int w = 0; w < kManyWaves; ++w) {
@@ -176,15 +184,16 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
   per_head = uniform(per_head);
   const int64_t total = per_head * a.b.Hkv;
   const int64_t workgroups = min((int64_t)ma.workgroups, ma.whole ? total : (total + kManyLeast * kManyTile - 1) / (kManyLeast * kManyTile));
-  if (tid == 0 && blockIdx.x >= workgroups && !ma.whole) ma.cuts[blockIdx.x].r = -1;
+  if (!SHARED && tid == 0 && blockIdx.x >= workgroups && !ma.whole) ma.cuts[blockIdx.x].r = -1;
   // neighbours in the sequence read the same keys: they run on the same die (workgroups go to the eight dies in turn)
-  const int per_die = ((int)workgroups + 7) / 8, g = (int)(blockIdx.x & 7) * per_die + (int)(blockIdx.x >> 3);
-  if ((int)(blockIdx.x >> 3) >= per_die || g >= workgroups) return;
+  const int per_die = ((int)workgroups + 7) / 8;
+  int g = (int)(blockIdx.x & 7) * per_die + (int)(blockIdx.x >> 3);
+  if (!SHARED && ((int)(blockIdx.x >> 3) >= per_die || g >= workgroups)) return;
   const int64_t x0 = uniform(g * total / workgroups), x1 = uniform((g + 1) * total / workgroups);
   // From the end of the part back to its start: blocks are entered at their first keys, at about the same time by all workgroups, so
   // that the keys and values of a head are read by many at a time.
   int head = uniform((int)((x1 - 1) / per_head));
-  {
+  if constexpr (!SHARED) {
     const int64_t at = x1 - 1 - head * per_head;
     int64_t start = before + incl - mine;
     if (at >= start && at < start + mine) {                      // one thread has it
@@ -199,22 +208,49 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
       found[0] = r; found[1] = i; found[2] = (int)(at - start);
     }
   }
-  __syncthreads();
+  if constexpr (!SHARED) __syncthreads();
   int r = uniform(found[0]), block = uniform(found[1]);
   int64_t start = uniform(x1 - 1 - found[2]);                     // position of the block
-  Blocks of = uniform(request(r));
+  Blocks of = uniform(request(SHARED ? 0 : r));
   CutBlock cut = {-1, 0, 0, 0};
+  int chunk_tile0 = 0, chunk_tile1 = 0;
+  if constexpr (SHARED) {
+    // Blocks of rows of one chunk side by side, on one die: they read the same keys.
+    const int on_die = (ma.sh.many_units + 7) / 8, unit = (int)(blockIdx.x & 7) * on_die + (int)(blockIdx.x >> 3);
+    if ((int)(blockIdx.x >> 3) >= on_die || unit >= ma.sh.many_units) return;
+    block = unit % ma.sh.many_blocks;
+    int rest = unit / ma.sh.many_blocks;
+    g = rest % ma.sh.many_splits;                                  // number of the part
+    rest /= ma.sh.many_splits;
+    head = rest % a.b.Hkv;
+    const int group = rest / a.b.Hkv, end = ma.sh.cu_groups[group + 1];
+    r = ma.sh.cu_groups[group];
+    if (r >= end) return;
+    of = blocks_of(ma, prefix_of(ma.sh, group), a.b.cu_q[r], a.b.cu_q[end] - a.b.cu_q[r]);
+    of = uniform(of);
+    of.causal = 0;
+    if (block >= of.count) return;
+    const int tiles = (of.len + kManyKeys - 1) / kManyKeys;
+    chunk_tile0 = g * ma.sh.many_tiles;
+    chunk_tile1 = min(tiles, chunk_tile0 + ma.sh.many_tiles);
+    const int row0 = block * kManyRows, row1 = min(of.rows, row0 + kManyRows);
+    if (g == 0) no_parts<kManyThreads>(a, ma.sh.many_splits, ma.sh.splits, of.q0, head, row0, row1);
+    if (chunk_tile0 >= chunk_tile1) {
+      no_parts<kManyThreads>(a, g, g + 1, of.q0, head, row0, row1);
+      return;
+    }
+  }
 
   for (;;) {
     const int tiles = uniform(of.tiles(block));
     const int64_t first = start + kManyLead * kManyTile;          // position of its first tile
     const int each = uniform(per_tile(of, block));
     auto tiles_before = [&](int64_t x) { return uniform((int)min((max(x - first, (int64_t)0) + each - 1) / each, (int64_t)tiles)); };        // that begin before x
-    const int tile0 = ma.whole ? 0 : tiles_before(x0), tile1 = ma.whole ? tiles : tiles_before(x1);
+    const int tile0 = SHARED ? chunk_tile0 : ma.whole ? 0 : tiles_before(x0), tile1 = SHARED ? chunk_tile1 : ma.whole ? tiles : tiles_before(x1);
     if (tile1 > tile0) {
-      const bool whole = tile0 == 0 && tile1 == tiles;
+      const bool whole = !SHARED && tile0 == 0 && tile1 == tiles;
       const int slot = tile0 > 0 ? 2 * g : 2 * g + 1;
-      if (tile0 == 0 && tile1 < tiles)                             // the rest of the block is the next workgroups'
+      if (!SHARED && tile0 == 0 && tile1 < tiles)                  // the rest of the block is the next workgroups'
         cut = {r, block, head, (int)(((first + (int64_t)(tiles - 1) * each + 1) * workgroups - 1) / total)};
       const int q0 = of.q0, row0 = block * kManyRows + wave * 32, row = row0 + l32;
       const bool active = row0 < of.rows;
@@ -497,7 +533,8 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
           }
         }
       };
-      if (__builtin_expect(of.rows > kFewRowsMost, 1)) walk(std::false_type{});
+      if constexpr (SHARED) walk(std::false_type{});
+      else if (__builtin_expect(of.rows > kFewRowsMost, 1)) walk(std::false_type{});
       else walk(std::true_type{});
       if (active) {
         if (__builtin_expect(partly(tile1 - 1) && not_finite != 0, 0)) {
@@ -529,7 +566,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
                   u32x2{pack2(o[db][4 * i] * inv, o[db][4 * i + 1] * inv), pack2(o[db][4 * i + 2] * inv, o[db][4 * i + 3] * inv)};
           if (a.lse && half == 0) a.lse[(int64_t)(q0 + t) * a.b.Hq + h] = sum == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kLn2;
         } else if (row < of.rows) {
-          const int64_t part = (int64_t)slot * kManyRows + wave * 32 + l32;
+          const int64_t part = SHARED ? ((int64_t)g * a.b.T + of.q0 + row / of.G) * a.b.Hq + head * of.G + row % of.G : (int64_t)slot * kManyRows + wave * 32 + l32;
 #pragma unroll
           for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -539,6 +576,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
         }
       }
     }
+    if constexpr (SHARED) return;
     if (start <= x0) break;
     if (--block < 0) {                                           // the request before that has blocks, or the last one of the head before: 64 at a time
       for (;;) {
@@ -560,6 +598,14 @@ template <int D, bool FP8>
 int launch_many_of(const ManyArgs& m, hipStream_t stream) {
   if (m.a.pool.page_log2 < 4) attend_many_kernel<D, FP8, true><<<dim3(m.workgroups), dim3(kManyThreads), 0, stream>>>(m);
   else attend_many_kernel<D, FP8, false><<<dim3(m.workgroups), dim3(kManyThreads), 0, stream>>>(m);
+  return (int)hipGetLastError();
+}
+
+template <int D, bool FP8>
+int launch_many_shared_of(const ManyArgs& m, hipStream_t stream) {
+  const dim3 grid((unsigned)((m.sh.many_units + 7) / 8 * 8)), block(kManyThreads);
+  if (m.a.pool.page_log2 < 4) attend_many_kernel<D, FP8, true, true><<<grid, block, 0, stream>>>(m);
+  else attend_many_kernel<D, FP8, false, true><<<grid, block, 0, stream>>>(m);
   return (int)hipGetLastError();
 }
 

@@ -1,0 +1,167 @@
+// codecomp_attend_shared: attention of requests whose caches begin with the same rows.
+//
+// The shared rows are attended to once for a group, by the rows (new tokens x query heads of a KV head) of all of its requests together: they lie side by
+// side in the packed batch, and all of them see all of the shared rows.  What a request has behind them is its own.  Both leave parts of every row (reference, sum
+// of weights, unscaled output, fp32), which a last kernel joins in order.
+//
+// Groups of many rows: the kernel of attend_many.h, whose blocks of 256 rows share keys and values through LDS.  Groups of up to 64 rows, and all rows behind the
+// shared ones: that of attend_few.hip, which reads keys and values once for up to 32 rows; both in one launch.
+#include <float.h>
+#include <math.h>
+
+#include <algorithm>
+
+#include "attend_many.h"
+#include "serve.h"
+
+namespace codecomp {
+
+extern template int launch_many_shared_of<64, false>(const ManyArgs&, hipStream_t);
+extern template int launch_many_shared_of<64, true>(const ManyArgs&, hipStream_t);
+extern template int launch_many_shared_of<128, false>(const ManyArgs&, hipStream_t);
+extern template int launch_many_shared_of<128, true>(const ManyArgs&, hipStream_t);
+
+constexpr int kChip = 256;                       // compute units: workgroups of the kernel for many rows that run at once
+constexpr int64_t kMostBlocks = (1 << 23) - 1;    // of up to 512 threads: an axis of a grid holds 2^32 threads
+constexpr int kMostSplits = 1024;
+
+int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const codecomp_pages* p, SharedPlan* pl) {
+  if (int rc = make_pool(p, &pl->pool)) return rc;
+  if (int rc = make_batch(b, p, &pl->batch)) return rc;
+  const PagedBatch& x = pl->batch;
+  if (!g || !g->cu_groups_host || !g->cu_groups_dev || !g->prefix_lens_dev) return CODECOMP_EINVAL_NULL;
+  if (g->n_groups < 1 || g->n_groups > 65535) return CODECOMP_EINVAL_SHAPE;
+  if (g->max_prefix_len < 0 || g->max_prefix_len > b->max_kv_len || g->max_own_len < 0 || g->max_own_len > b->max_kv_len) return CODECOMP_EINVAL_PAGES;
+  if (g->cu_groups_host[0] != 0 || g->cu_groups_host[g->n_groups] != b->n_seqs) return CODECOMP_EINVAL_SEQLENS;
+  for (int i = 0; i < g->n_groups; ++i)
+    if (g->cu_groups_host[i + 1] < g->cu_groups_host[i]) return CODECOMP_EINVAL_SEQLENS;
+  pl->d = p->head_dim;
+  pl->scale = b->softmax_scale > 0.0f ? b->softmax_scale : 1.0f / sqrtf((float)p->head_dim);
+  SharedRows& s = pl->sh;
+  s = SharedRows{};
+  s.cu_groups = g->cu_groups_dev; s.prefix_lens = g->prefix_lens_dev;
+  s.n_groups = g->n_groups; s.max_prefix = g->max_prefix_len; s.max_own = g->max_own_len;
+  int64_t few_most = 0, many_most = 0, blocks = 0, own_most = 0;
+  pl->few_groups = pl->many_groups = 0;
+  for (int i = 0; i < g->n_groups; ++i) {
+    const int64_t rows = (int64_t)(b->cu_q_host[g->cu_groups_host[i + 1]] - b->cu_q_host[g->cu_groups_host[i]]) * x.G;
+    if (rows > kFewRowsMost) {
+      ++pl->many_groups;
+      blocks += (rows + kManyRows - 1) / kManyRows;
+      many_most = std::max(many_most, rows);
+    } else if (rows > 0) {
+      ++pl->few_groups;
+      few_most = std::max(few_most, rows);
+    }
+  }
+  for (int r = 0; r < x.n_seqs; ++r) own_most = std::max(own_most, (int64_t)(b->cu_q_host[r + 1] - b->cu_q_host[r]) * x.G);
+  blocks *= x.Hkv;
+  pl->two_blocks = std::max(few_most, own_most) > 16;
+  const int rows_each = pl->two_blocks ? 32 : 16;
+
+  // shared rows, many: chunks such that all workgroups run at once and end together
+  s.many_splits = s.few_splits = 0;
+  if (pl->many_groups > 0) {
+    const int tiles = std::max(1, (s.max_prefix + kManyKeys - 1) / kManyKeys);
+    s.many_blocks = (int)((many_most + kManyRows - 1) / kManyRows);
+    const int64_t grid = (int64_t)s.n_groups * x.Hkv * s.many_blocks;       // with a place for blocks that a group does not have
+    if (grid > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
+    int best = 1;
+    double least = 0.0;
+    for (int n = 1; n <= std::min(tiles, kChip) && grid * n <= kMostBlocks; ++n) {
+      const int each = (tiles + n - 1) / n;
+      const double time = (double)((blocks * n + kChip - 1) / kChip) * (each + 4) + 0.02 * n;
+      if (n == 1 || time < least) { best = n; least = time; }
+    }
+    s.many_tiles = (tiles + best - 1) / best;
+    s.many_splits = (tiles + s.many_tiles - 1) / s.many_tiles;
+    s.many_units = (int)(grid * s.many_splits);
+  }
+  auto cut = [&](int64_t items, int most, int* chunk, int* splits) {
+    int64_t keys = (items * most / 512 + 127) / 128 * 128;
+    keys = std::min<int64_t>(std::max<int64_t>(keys, 128), 2048);
+    while ((most + keys - 1) / keys > kMostSplits || (items * ((most + keys - 1) / keys) > kMostBlocks && keys < most)) keys *= 2;
+    *chunk = (int)std::min<int64_t>(keys, 1 << 30);
+    *splits = (int)((most + keys - 1) / keys);
+  };
+  // shared rows, few
+  s.few_parts = std::max<int>(1, (int)((few_most + rows_each - 1) / rows_each));
+  int64_t few_units = 0;
+  if (pl->few_groups > 0) {
+    const int64_t items = (int64_t)s.n_groups * x.Hkv * s.few_parts;
+    cut((int64_t)pl->few_groups * x.Hkv * s.few_parts, s.max_prefix, &s.few_chunk, &s.few_splits);
+    s.few_splits = std::max(s.few_splits, 1);
+    few_units = items * s.few_splits;
+    if (few_units > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
+  }
+  s.few_units = (int)few_units;
+  s.splits = std::max(s.many_splits, s.few_splits);
+  // rows behind them
+  pl->row_parts = std::max<int>(1, (int)std::min<int64_t>((own_most + rows_each - 1) / rows_each, INT32_MAX));
+  const int64_t items = (int64_t)x.n_seqs * x.Hkv;
+  if (items * pl->row_parts > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
+  cut(items * pl->row_parts, s.max_own, &pl->chunk, &pl->own_splits);
+  pl->own_units = items * pl->row_parts * pl->own_splits;
+  if (pl->own_units + few_units > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
+  if ((int64_t)x.T * x.Hq > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
+  pl->ws_bytes = x.T == 0 ? 0 : ((size_t)(s.splits + pl->own_splits) * x.T * x.Hq * (p->head_dim + 2) * sizeof(float) + 255) & ~(size_t)255;
+  return CODECOMP_OK;
+}
+
+// A row's parts, those of the shared rows first; D / 4 threads a row.
+template <int D>
+__global__ __launch_bounds__(256) void join_shared_kernel(const AttendArgs a, int parts) {
+  constexpr int THREADS = D / 4;
+  const int64_t rows = (int64_t)a.b.T * a.b.Hq, row = (int64_t)blockIdx.x * (256 / THREADS) + threadIdx.x / THREADS;
+  const int e = (threadIdx.x % THREADS) * 4;
+  if (row >= rows) return;
+  float top = -INFINITY, all = 0.0f;
+#pragma unroll 8
+  for (int p = 0; p < parts; ++p) top = fmaxf(top, a.part_ml[2 * (p * rows + row)]);
+  f32x4 x = {0, 0, 0, 0};
+#pragma unroll 4
+  for (int p = 0; p < parts; ++p) {
+    const int64_t part = p * rows + row;
+    const float m = a.part_ml[2 * part], l = a.part_ml[2 * part + 1];
+    if (l == kNoPart) continue;
+    const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - top);       // times zeros, or an infinity or NaN that it saw
+    all += l * f;
+    x += *reinterpret_cast<const f32x4*>(a.part_o + part * D + e) * f;
+  }
+  const int64_t t = row / a.b.Hq, h = row - t * a.b.Hq;
+  const float inv = all == 0.0f ? 0.0f : a.pool.v_scale / all;
+  *reinterpret_cast<u32x2*>(a.out + t * a.b.o_st + h * a.b.o_sh + e) = u32x2{pack2(x.x * inv, x.y * inv), pack2(x.z * inv, x.w * inv)};
+  if (a.lse && e == 0) a.lse[row] = all == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(all)) * kLn2;
+}
+
+int launch_shared(const SharedPlan& pl, const void* q, int layer, void* out, float* lse, void* workspace, hipStream_t stream) {
+  SharedArgs a = {};
+  a.pool = pl.pool; a.b = pl.batch; a.q = static_cast<const uint16_t*>(q); a.out = static_cast<uint16_t*>(out); a.lse = lse;
+  a.layer = layer * pl.pool.s_layer;
+  a.c = fminf(fmaxf(pl.scale * pl.pool.k_scale * kLog2e, FLT_MIN), FLT_MAX);       // a hidden logit of minus infinity times it stays one
+  a.chunk = pl.chunk; a.row_parts = pl.row_parts;
+  a.sh = pl.sh;
+  const int parts = pl.sh.splits + pl.own_splits;
+  const int64_t rows = (int64_t)pl.batch.T * pl.batch.Hq;
+  a.part_o = static_cast<float*>(workspace);
+  a.part_ml = a.part_o + parts * rows * pl.d;
+  if (pl.many_groups > 0) {
+    ManyArgs m = {};
+    m.a = a;
+    m.sh = a.sh;
+    m.rows_from = kFewRowsMost + 1;
+    int rc;
+    if (pl.d == 128) rc = pl.pool.fp8 ? launch_many_shared_of<128, true>(m, stream) : launch_many_shared_of<128, false>(m, stream);
+    else rc = pl.pool.fp8 ? launch_many_shared_of<64, true>(m, stream) : launch_many_shared_of<64, false>(m, stream);
+    if (rc) return rc;
+  }
+  if (pl.sh.few_units + pl.own_units > 0)
+    if (int rc = launch_few_shared(pl.d, pl.pool.fp8, pl.two_blocks, pl.sh.few_units + pl.own_units, a, stream)) return rc;
+  const int each = 256 / (pl.d / 4);
+  const dim3 grid((unsigned)((rows + each - 1) / each)), block(256);
+  if (pl.d == 128) join_shared_kernel<128><<<grid, block, 0, stream>>>(a, parts);
+  else join_shared_kernel<64><<<grid, block, 0, stream>>>(a, parts);
+  return (int)hipGetLastError();
+}
+
+}  // namespace codecomp
