@@ -8,7 +8,8 @@
 
 namespace codecomp {
 
-constexpr int kMoveThreads = 256, kMoveDeep = 8;       // pieces of 16 bytes that a thread has in flight
+constexpr int kMoveDeep = 8;                             // pieces of 16 bytes that a thread has in flight
+constexpr int kFewMoves = 1024;                          // workgroups up to which they are of 1024 threads, not 256
 constexpr int64_t kMostBlocks = (1 << 22) - 1;          // of up to 1024 threads: an axis of a grid holds 2^32 threads
 
 struct Span { int f, n, m; };                            // rows [f, n) of a request, m of them kept
@@ -26,11 +27,12 @@ __device__ __forceinline__ unsigned ordered(float x) {
   return x != x ? 0u : u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-template <int THREADS>
+// A thread has PER rows in registers; a request that has more is read again for the rest of them, as often as they are looked at.
+template <int THREADS, int PER>
 __global__ __launch_bounds__(THREADS) void keep_kernel(const EvictArgs a) {
-  constexpr int WAVES = THREADS / 64;
-  __shared__ int counts[WAVES][256];
-  __shared__ int found[2];
+  constexpr int WAVES = THREADS / 64, COPIES = 4, ENTRIES = WAVES * PER;
+  __shared__ __attribute__((aligned(16))) int counts[4][COPIES][256];       // of a digit's values, for each of the four digits
+  __shared__ int2 before[ENTRIES];                        // rows above the border and at it: of a wave's strip, then of all before it
   __shared__ int2 strip[2][WAVES];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int problem = blockIdx.x, head = problem % a.Hkv, rest = problem / a.Hkv, r = rest % a.n_seqs, layer = rest / a.n_seqs;
@@ -41,79 +43,140 @@ __global__ __launch_bounds__(THREADS) void keep_kernel(const EvictArgs a) {
   int32_t* kept = a.kept + (int64_t)problem * a.max_budget;
   const bool all = s.m == s.n - s.f;
   const int last = all ? s.f : s.n - a.recent;           // rows from there on stay
+  for (int i = tid; i < 4 * COPIES * 256; i += THREADS) (&counts[0][0][0])[i] = 0;
+  float x[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int j = s.f + i * THREADS + tid;
+    x[i] = j < s.n ? sums[j] : 0.0f;
+  }
+  const int beyond = s.f + PER * THREADS;                // first row that is in no register
   unsigned border = all ? 0 : ~0u;                       // rows above it stay, and the first `equal` of those at it
   int equal = 0;
+  __syncthreads();
   if (!all && s.m > a.recent) {
     unsigned prefix = 0;
     int want = s.m - a.recent;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      for (int i = tid; i < WAVES * 256; i += THREADS) counts[i >> 8][i & 255] = 0;
+#pragma unroll
+    for (int digit = 0; digit < 4; ++digit) {
+      const int shift = 24 - 8 * digit;
+      int* count = counts[digit][wave % COPIES];
+      auto look = [&](float v) __attribute__((always_inline)) {
+        const unsigned key = ordered(v);
+        if (digit == 0 || key >> ((shift + 8) & 31) == prefix) atomicAdd(&count[(key >> shift) & 255], 1);
+      };
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        if (s.f + i * THREADS + tid < last) look(x[i]);
+      for (int j = beyond + tid; j < last; j += THREADS) look(sums[j]);
       __syncthreads();
-      for (int j = s.f + tid; j < last; j += THREADS) {
-        const unsigned key = ordered(sums[j]);
-        if (shift == 24 || key >> (shift + 8) == prefix) atomicAdd(&counts[wave][(key >> shift) & 255], 1);
+      int4 of = {0, 0, 0, 0};                            // four digits a lane, the largest first; every wave for itself
+#pragma unroll
+      for (int c = 0; c < COPIES; ++c) {
+        const int4 y = *reinterpret_cast<const int4*>(&counts[digit][c][252 - 4 * lane]);
+        of.x += y.w; of.y += y.z; of.z += y.y; of.w += y.x;
       }
-      __syncthreads();
-      if (wave == 0) {                                   // four digits a lane, the largest first
-        int of[4], mine = 0;
+      int above = of.x + of.y + of.z + of.w;
+      const int mine = above;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          of[i] = 0;
-#pragma unroll
-          for (int w = 0; w < WAVES; ++w) of[i] += counts[w][255 - 4 * lane - i];
-          mine += of[i];
-        }
-        int before = mine;
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-          const int y = __shfl_up(before, off);
-          if (lane >= off) before += y;
-        }
-        before -= mine;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (before < want && want <= before + of[i]) { found[0] = 255 - 4 * lane - i; found[1] = want - before; }
-          before += of[i];
-        }
+      for (int off = 1; off < 64; off <<= 1) {
+        const int y = __shfl_up(above, off);
+        if (lane >= off) above += y;
       }
-      __syncthreads();
-      prefix = prefix << 8 | (unsigned)found[0];
-      want = found[1];
+      const int owner = __builtin_ctzll(__ballot(above >= want));       // the first lane up to which there are enough
+      above -= mine;
+      int at = 255 - 4 * lane, left = want - above;
+      if (left > of.x) { left -= of.x; --at;
+        if (left > of.y) { left -= of.y; --at;
+          if (left > of.z) { left -= of.z; --at; } } }
+      prefix = prefix << 8 | (unsigned)__shfl(at, owner);
+      want = __shfl(left, owner);
     }
     border = prefix;
     equal = want;
   }
-  int above = 0, at_border = 0;                          // rows before this strip
-  for (int first = s.f, turn = 0; first < s.n; first += THREADS, turn ^= 1) {
-    const int j = first + tid;
-    const bool there = j < s.n;
-    const float x = there ? sums[j] : 0.0f;
-    const unsigned key = ordered(x);
-    const bool more = there && (j >= last || key > border), same = there && j < last && key == border;
-    const uint64_t more_mask = __ballot(more), same_mask = __ballot(same);
-    if (lane == 0) strip[turn][wave] = make_int2(__popcll(more_mask), __popcll(same_mask));
-    __syncthreads();                                     // all sums of the strip have been read
-    const uint64_t below = ((uint64_t)1 << lane) - 1;
-    int m = above + __popcll(more_mask & below), e = at_border + __popcll(same_mask & below);
+  auto kind = [&](int j, float v, bool& more, bool& same) __attribute__((always_inline)) {
+    const unsigned key = ordered(v);
+    more = j < s.n && (j >= last || key > border);
+    same = j < last && key == border;
+  };
+  const uint64_t below = ((uint64_t)1 << lane) - 1;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-      const int2 c = strip[turn][w];
-      if (w < wave) { m += c.x; e += c.y; }
-      above += c.x; at_border += c.y;
+  for (int i = 0; i < PER; ++i) {
+    bool more, same;
+    kind(s.f + i * THREADS + tid, x[i], more, same);
+    const uint64_t m = __ballot(more), e = __ballot(same);
+    if (lane == 0) before[i * WAVES + wave] = make_int2(__popcll(m), __popcll(e));
+  }
+  __syncthreads();                                       // all sums that are in registers have been read as well
+  int2 sum = {0, 0};
+  if (wave == 0) {
+    constexpr int EACH = (ENTRIES + 63) / 64;
+    int2 own[EACH];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      own[i] = lane * EACH + i < ENTRIES ? before[lane * EACH + i] : make_int2(0, 0);
+      sum.x += own[i].x; sum.y += own[i].y;
     }
+    int2 upto = sum;
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const int px = __shfl_up(upto.x, off), py = __shfl_up(upto.y, off);
+      if (lane >= off) { upto.x += px; upto.y += py; }
+    }
+    upto.x -= sum.x; upto.y -= sum.y;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      if (lane * EACH + i < ENTRIES) before[lane * EACH + i] = upto;
+      upto.x += own[i].x; upto.y += own[i].y;
+    }
+    if (lane == 63) strip[0][0] = upto;
+  }
+  __syncthreads();
+  auto keep = [&](int j, float v, bool more, bool same, int m, int e) __attribute__((always_inline)) {
     if (more || (same && e < equal)) {
       const int i = m + min(e, equal);
       kept[i] = j;
-      to[i] = x;
+      to[i] = v;
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    bool more, same;
+    const int j = s.f + i * THREADS + tid;
+    kind(j, x[i], more, same);
+    const uint64_t m = __ballot(more), e = __ballot(same);
+    const int2 b = before[i * WAVES + wave];
+    keep(j, x[i], more, same, b.x + __popcll(m & below), b.y + __popcll(e & below));
+  }
+  if (beyond < s.n) {
+    int above = strip[0][0].x, at_border = strip[0][0].y;
+    __syncthreads();
+    for (int first = beyond, turn = 0; first < s.n; first += THREADS, turn ^= 1) {
+      const int j = first + tid;
+      const float v = j < s.n ? sums[j] : 0.0f;
+      bool more, same;
+      kind(j, v, more, same);
+      const uint64_t more_mask = __ballot(more), same_mask = __ballot(same);
+      if (lane == 0) strip[turn][wave] = make_int2(__popcll(more_mask), __popcll(same_mask));
+      __syncthreads();                                   // all sums of the strip have been read
+      int m = above + __popcll(more_mask & below), e = at_border + __popcll(same_mask & below);
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) {
+        const int2 c = strip[turn][w];
+        if (w < wave) { m += c.x; e += c.y; }
+        above += c.x; at_border += c.y;
+      }
+      keep(j, v, more, same, m, e);
     }
   }
   for (int i = s.m + tid; i < a.max_budget; i += THREADS) kept[i] = -1;
 }
 
 // PIECES: 16-byte pieces of a row that a workgroup moves.
-template <int PIECES>
-__global__ __launch_bounds__(kMoveThreads) void close_up_kernel(const EvictArgs a, int slices) {
-  constexpr int ROWS = kMoveThreads / PIECES;
+template <int PIECES, int THREADS>
+__global__ __launch_bounds__(THREADS) void close_up_kernel(const EvictArgs a, int slices) {
+  constexpr int ROWS = THREADS / PIECES;
   const int tid = threadIdx.x, part = blockIdx.x % (2 * slices), problem = blockIdx.x / (2 * slices);
   const int head = problem % a.Hkv, rest = problem / a.Hkv, r = rest % a.n_seqs, layer = rest / a.n_seqs;
   const Span s = span_of(a, r);
@@ -151,20 +214,27 @@ __global__ __launch_bounds__(kMoveThreads) void close_up_kernel(const EvictArgs 
   }
 }
 
+template <int PIECES>
+static void launch_close_up(const EvictArgs& a, int64_t problems, int slices, hipStream_t stream) {
+  const dim3 grid((unsigned)(problems * 2 * slices));
+  if (problems * 2 * slices < kFewMoves) close_up_kernel<PIECES, 1024><<<grid, dim3(1024), 0, stream>>>(a, slices);
+  else close_up_kernel<PIECES, 256><<<grid, dim3(256), 0, stream>>>(a, slices);
+}
+
 int launch_evict(const EvictArgs& a, int d, hipStream_t stream) {
   const int64_t problems = (int64_t)a.n_layers * a.n_seqs * a.Hkv;
   const int pieces = d * (a.pool.fp8 ? 1 : 2) / 16;
   int slices = 1;
-  while (slices < pieces / 4 && problems * 2 * slices < 1024) slices *= 2;
+  while (slices < pieces / 8 && problems * 2 * slices < 64) slices *= 2;
   if (problems * 2 * slices > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
-  if (a.max_kv > 4096) keep_kernel<1024><<<dim3((unsigned)problems), dim3(1024), 0, stream>>>(a);
-  else keep_kernel<256><<<dim3((unsigned)problems), dim3(256), 0, stream>>>(a);
+  if (a.max_kv > 8192) keep_kernel<1024, 32><<<dim3((unsigned)problems), dim3(1024), 0, stream>>>(a);
+  else if (a.max_kv > 2048) keep_kernel<256, 16><<<dim3((unsigned)problems), dim3(256), 0, stream>>>(a);
+  else keep_kernel<256, 8><<<dim3((unsigned)problems), dim3(256), 0, stream>>>(a);
   if (hipError_t e = hipGetLastError()) return (int)e;
-  const dim3 grid((unsigned)(problems * 2 * slices)), block(kMoveThreads);
   switch (pieces / slices) {
-    case 16: close_up_kernel<16><<<grid, block, 0, stream>>>(a, slices); break;
-    case 8: close_up_kernel<8><<<grid, block, 0, stream>>>(a, slices); break;
-    default: close_up_kernel<4><<<grid, block, 0, stream>>>(a, slices); break;
+    case 16: launch_close_up<16>(a, problems, slices, stream); break;
+    case 8: launch_close_up<8>(a, problems, slices, stream); break;
+    default: launch_close_up<4>(a, problems, slices, stream); break;
   }
   return (int)hipGetLastError();
 }

@@ -20,6 +20,12 @@
 
 namespace codecomp {
 
+// A block of keys whose rows several workgroups share: the first one has part 2 * share + 1, those after it 2 * share.
+struct CutKeys {
+  int32_t r, block, head;      // r < 0: none begins in this share
+  int32_t last;                // share with the last rows
+};
+
 struct MassArgs {
   PagePool pool;
   PagedBatch b;
@@ -28,15 +34,18 @@ struct MassArgs {
   const int32_t* first;
   float* sums;                 // of the layer
   int64_t s_seq, s_head;
-  float* part;                 // many rows: [split][request * head][row]
+  float* part;                 // many rows: [2 * share][key of the block]
+  CutKeys* cuts;               // [shares]
   int64_t layer;               // byte offset of the layer in the pool
   float c, decay, share;       // softmax_scale * k_scale * log2(e); 1 / G
-  int chunk, splits, rows_each;
+  int chunk, shares;
 };
 
 constexpr int kMassWaves = 4, kMassThreads = 64 * kMassWaves;
-constexpr int kMassKeys = 64 * kMassWaves;      // many rows: keys of a workgroup
+constexpr int kManyMassWaves = 8, kManyMassThreads = 64 * kManyMassWaves, kMassKeys = 64 * kManyMassWaves;      // many rows: keys of a workgroup
 constexpr int kMassStage = 512;                 // rows whose log-sum-exp and limit stand in LDS at a time
+constexpr int kMassLead = 768;                  // rows' worth of positions in front of a block's rows, for starting on its keys and ending it
+constexpr int kMassLeast = 1024;                // rows' worth that a workgroup gets at least
 
 __device__ __forceinline__ int first_of(const MassArgs& a, int r) { return a.first ? max(a.first[r], 0) : 0; }
 
@@ -173,166 +182,325 @@ __global__ __launch_bounds__(kMassThreads, FP8 && D == 128 ? 3 : 4) void mass_fe
   }
 }
 
-// Rows that see the first key of a block of keys begin here.
-__device__ __forceinline__ int first_row(const MassArgs& a, int len, int nq, int key) { return a.b.causal ? max(key - (len - nq), 0) * a.b.G : 0; }
+// Blocks of 256 keys of a request, and the rows that see them: of block b those from row_of(b) on, the first one's first key being seen by the most.
+struct KeyBlocks {
+  int len, nq, G, q0, rows, first, count, off;       // keys, tokens, ..., first block that is not of protected rows alone, blocks from there on, rows before the new ones
+  __device__ __forceinline__ int row_of(int b) const { return off == INT32_MAX ? 0 : max(b * kMassKeys - off, 0) * G; }
+  __device__ __forceinline__ int64_t weight(int b) const { return kMassLead + rows - row_of(b); }
+  __device__ __forceinline__ int64_t before(int n) const {       // weight of the first n blocks
+    int64_t rest = 0;
+    if (off != INT32_MAX) {
+      const int end = first + n, c = min(max(first, off < 0 ? 0 : off / kMassKeys + 1), end);       // blocks from c on are not seen by all rows
+      rest = (int64_t)(end - 1 + c) * (end - c) / 2 * kMassKeys - (int64_t)off * (end - c);
+    }
+    return (int64_t)n * (kMassLead + rows) - rest * G;
+  }
+};
+__device__ __forceinline__ KeyBlocks blocks_of(const MassArgs& a, int r) {
+  KeyBlocks x;
+  x.len = kv_len_of(a.b, r);
+  x.q0 = a.b.cu_q[r];
+  x.nq = a.b.cu_q[r + 1] - x.q0;
+  x.G = a.b.G;
+  x.rows = x.nq * x.G;
+  x.off = a.b.causal ? x.len - x.nq : INT32_MAX;
+  x.first = first_of(a, r) / kMassKeys;
+  x.count = x.rows <= kFewRowsMost || first_of(a, r) >= x.len ? 0 : (x.len + kMassKeys - 1) / kMassKeys - x.first;
+  return x;
+}
 
 template <int D, bool FP8>
-__global__ __launch_bounds__(kMassThreads, 2) void mass_many_kernel(const MassArgs a) {
+__global__ __launch_bounds__(kManyMassThreads, 2) void mass_many_kernel(const MassArgs a) {
   constexpr int KS = D / 16, LOADS = D * (FP8 ? 1 : 2) / 32;       // fragments of a key; 16-byte pieces of it that a lane has
   constexpr int GROUP = D / 32 * 1024, TILE = 2 * GROUP;            // bytes of 16 rows and of 32 in LDS: chunks of 1 KB, 16 rows of four 16-byte pieces, piece by piece
-  constexpr int SENT = TILE / 1024 / kMassWaves;                    // chunks of a tile that a wave sends for
+  constexpr int TILES = 8, AHEAD = TILES - 1;                       // in LDS, and on their way there
+  constexpr int SENDERS = TILE / 1024;                              // waves that send for a chunk of a tile each
   constexpr int RED = 33;                                           // floats between keys where lanes are added up
-  constexpr int LDS = 4 * TILE > kMassKeys * RED * 4 ? 4 * TILE : kMassKeys * RED * 4;
+  constexpr int LDS = TILES * TILE > kMassKeys * RED * 4 ? TILES * TILE : kMassKeys * RED * 4;
   __shared__ __attribute__((aligned(1024))) unsigned char lds[LDS];
   __shared__ float row_lse[2][kMassStage];
   __shared__ int row_limit[2][kMassStage];
+  __shared__ int64_t wave_sum[kManyMassWaves], found_at;
+  __shared__ int found[2];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), l32 = lane & 31, half = lane >> 5;
-  // blocks of keys of one part of the rows side by side: they read the same queries
-  const int blocks = (a.b.max_kv + kMassKeys - 1) / kMassKeys;
-  const int block = blockIdx.x % blocks, rest = blockIdx.x / blocks, items = a.b.n_seqs * a.b.Hkv, split = rest / items, item = rest - split * items;
-  const int r = item / a.b.Hkv, head = item - r * a.b.Hkv;
-  const int q0 = a.b.cu_q[r], nq = a.b.cu_q[r + 1] - q0, rows = nq * a.b.G;
-  if (rows <= kFewRowsMost) return;
-  const int len = uniform(kv_len_of(a.b, r)), from = uniform(first_of(a, r)), key0 = block * kMassKeys;
-  if (key0 >= len || key0 + kMassKeys <= from) return;
-  const int row0 = uniform(max(first_row(a, len, nq, key0) & -32, split * a.rows_each)), row1 = uniform(min(rows, (split + 1) * a.rows_each));
-  if (row0 >= row1) return;
 
-  // keys as left operands
-  const int wave_key = key0 + wave * 64;
-  const int32_t* table = a.b.table + (int64_t)r * a.b.table_width;
-  u32x4 kf[2][KS];
-  unsigned there[2];
+  // ---- this workgroup's share: the rows of all blocks of keys of all requests and heads form one sequence, cut into equal parts
+  const int n = a.b.n_seqs, per = (n + kManyMassThreads - 1) / kManyMassThreads, r0 = min(tid * per, n), r1 = min(r0 + per, n);
+  auto weight_of = [&](int i) __attribute__((always_inline)) {
+    const KeyBlocks x = blocks_of(a, i);
+    return x.before(x.count);
+  };
+  int64_t mine = 0;
+  for (int i = r0; i < r1; ++i) mine += weight_of(i);
+  int64_t incl = mine;
 #pragma unroll
-  for (int g = 0; g < 2; ++g) {
-    const int key = wave_key + g * 32 + l32, at = table[min(key, len - 1) >> a.pool.page_log2];
-    const bool held = at >= 0 && at < a.pool.n_pages;
-    there[g] = (unsigned)__ballot(held && key < len);
-    const unsigned char* p = a.pool.k + a.layer + head * a.pool.s_head + (held ? at : 0) * a.pool.s_page + (min(key, len - 1) & ((1 << a.pool.page_log2) - 1)) * a.pool.s_tok + half * 16;
+  for (int off = 1; off < 64; off <<= 1) {
+    const int64_t y = __shfl_up(incl, off);
+    if (lane >= off) incl += y;
+  }
+  if (lane == 63) wave_sum[wave] = incl;
+  __syncthreads();
+  int64_t before = incl - mine, per_head = 0;
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const u32x4 x = *reinterpret_cast<const u32x4*>(p + i * 32);
-      if constexpr (FP8) {
-        kf[g][2 * i] = widen8(x.x, x.y);
-        kf[g][2 * i + 1] = widen8(x.z, x.w);
+  for (int w = 0; w < kManyMassWaves; ++w) {
+    if (w < wave) before += wave_sum[w];
+    per_head += wave_sum[w];
+  }
+  per_head = uniform(per_head);
+  const int64_t total = per_head * a.b.Hkv, shares = uniform(min((int64_t)a.shares, (total + kMassLeast - 1) / kMassLeast));
+  if (tid == 0 && blockIdx.x >= shares) a.cuts[blockIdx.x].r = -1;
+  // neighbours in the sequence read the same queries: they run on the same die (workgroups go to the eight dies in turn)
+  const int per_die = ((int)shares + 7) / 8, share = (int)(blockIdx.x & 7) * per_die + (int)(blockIdx.x >> 3);
+  if ((int)(blockIdx.x >> 3) >= per_die || share >= shares) return;
+  const int64_t x0 = uniform(share * total / shares), x1 = uniform((share + 1) * total / shares);
+  int head = uniform((int)(x0 / per_head));
+  {
+    int64_t at = x0 - head * per_head - before;
+    if (at >= 0 && at < mine) {                                  // one thread has it
+      int i = r0;
+      for (int64_t w = weight_of(i); at >= w; w = weight_of(i)) { at -= w; ++i; }
+      found[0] = i; found_at = at;
+    }
+  }
+  __syncthreads();
+  int r = uniform(found[0]);
+  KeyBlocks of = blocks_of(a, r);
+  {
+    const int64_t at = found_at;
+    for (int i = tid; i < of.count; i += kManyMassThreads) {
+      const int64_t w = of.before(i);
+      if (at >= w && at < w + of.weight(of.first + i)) { found[1] = of.first + i; wave_sum[0] = at - w; }
+    }
+  }
+  __syncthreads();
+  int block = uniform(found[1]);
+  int64_t start = uniform(x0 - wave_sum[0]);                       // position of the block
+  CutKeys cut = {-1, 0, 0, 0};
+
+  for (;;) {
+    const int len = uniform(of.len), nq = uniform(of.nq), q0 = uniform(of.q0), rows = uniform(of.rows), from = uniform(first_of(a, r)), G = a.b.G;
+    const int key0 = block * kMassKeys, first_row = uniform(of.row_of(block)), all = rows - first_row;
+    const int64_t front = start + kMassLead;                       // position of the block's first row
+    const int row0 = uniform(first_row + (int)min((max(x0 - front, (int64_t)0) + 31) & -32, (int64_t)all));
+    const int row1 = uniform(x1 >= front + all ? rows : first_row + (int)min((max(x1 - front, (int64_t)0) + 31) & -32, (int64_t)all));
+    const int64_t next_block = front + all;
+    if (row0 < row1) {
+      const bool whole = row0 == first_row && row1 == rows;
+      const int slot = row0 > first_row ? 2 * share : 2 * share + 1;
+      if (row0 == first_row && row1 < rows)                        // the rest of the rows is the next workgroups'
+        cut = {r, block, head, uniform((int)(((front + (all - 1) / 32 * 32 + 1) * shares - 1) / total))};
+      __syncthreads();                                             // through with LDS
+      // keys as left operands
+      const int wave_key = key0 + wave * 64;
+      const int32_t* table = a.b.table + (int64_t)r * a.b.table_width;
+      u32x4 kf[2][KS];
+      unsigned there[2];
+#pragma unroll
+      for (int g = 0; g < 2; ++g) {
+        const int key = wave_key + g * 32 + l32, at = table[min(key, len - 1) >> a.pool.page_log2];
+        const bool held = at >= 0 && at < a.pool.n_pages;
+        there[g] = (unsigned)__ballot(held && key < len);
+        const unsigned char* p = a.pool.k + a.layer + head * a.pool.s_head + (held ? at : 0) * a.pool.s_page + (min(key, len - 1) & ((1 << a.pool.page_log2) - 1)) * a.pool.s_tok + half * 16;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+          const u32x4 x = *reinterpret_cast<const u32x4*>(p + i * 32);
+          if constexpr (FP8) {
+            kf[g][2 * i] = widen8(x.x, x.y);
+            kf[g][2 * i + 1] = widen8(x.z, x.w);
+          } else {
+            kf[g][i] = x;
+          }
+        }
+      }
+      const bool all_there = there[0] == 0xFFFFFFFFu && there[1] == 0xFFFFFFFFu;
+
+      // They have come before the loop, whose own waits count what it sends for.
+#pragma unroll
+      for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) asm volatile("" ::"v"(kf[g][ks]));
+
+      // ---- rows.  Step s has rows row0 + 32 s and on; the last row stands for those behind it, without weight.
+      const int steps = (row1 - row0 + 31) >> 5;
+      const int piece = wave % (D / 32) * 4 + (lane >> 4);
+      int load_row = row0 + wave / (D / 32) * 16 + (lane & 15), load_g = load_row % G;        // of the next tile that is sent for
+      const int64_t step_row = (32 / G) * a.b.q_st + (32 % G) * a.b.q_sh, wrap = a.b.q_st - G * a.b.q_sh;
+      const uint16_t* queries = a.q + q0 * a.b.q_st + head * G * a.b.q_sh + piece * 8;
+      const uint16_t* load_at = queries + (load_row / G) * a.b.q_st + load_g * a.b.q_sh;
+      const uint16_t* last_at = queries + (nq - 1) * a.b.q_st + (G - 1) * a.b.q_sh;
+      auto fetch = [&](int step) __attribute__((always_inline)) {
+        const uint16_t* p = load_row < rows ? load_at : last_at;
+        if (wave < SENDERS)
+          asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_address(lds) + (step & (TILES - 1)) * TILE + wave * 1024), "v"(p) : "memory", "m0");
+        load_row += 32;
+        load_g += 32 % G;
+        load_at += step_row;
+        if (load_g >= G) { load_g -= G; load_at += wrap; }
+      };
+      auto stage = [&](int number) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < kMassStage / kManyMassThreads; ++i) {
+          const int at = i * kManyMassThreads + tid, row = row0 + number * kMassStage + at, rr = min(row, rows - 1), t = rr / G, g = rr - t * G;
+          const float x = a.lse[(int64_t)(q0 + t) * a.b.Hq + head * G + g];
+          row_lse[number & 1][at] = x == -INFINITY ? 0.0f : x * kLog2e;
+          row_limit[number & 1][at] = row < row1 ? limit_of(a, len, nq, t, x) : 0;
+        }
+      };
+      f32x16 sum[2], za[2], zb[2];
+#pragma unroll
+      for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum[g][i] = zb[g][i] = 0.0f;
+      stage(0);
+#pragma unroll
+      for (int f = 0; f < AHEAD; ++f) fetch(f);
+      const unsigned char* q_lane = lds + (l32 >> 4) * GROUP + (l32 & 15) * 16 + half * (FP8 ? 512 : 256);
+      auto query_frag = [&](const unsigned char* qt, int ks) __attribute__((always_inline)) {
+        const int p = FP8 ? (ks >> 1) * 4 + (ks & 1) : 2 * ks;         // piece of the lower half of the lanes
+        return *reinterpret_cast<const u32x4*>(qt + (p >> 2) * 1024 + (p & 3) * 256);
+      };
+      // One step: the logits z of its rows on the matrix cores, beside them the weights of the rows before, whose logits are zp and log-sum-exp lp.  The order is the
+      // source's: an LDS read for some fragments further on (from the next tile at the end), two MFMAs, the vector work of some logits.
+      float lp = INFINITY;                                             // before the first step: no weight
+      int limit_p = INT32_MAX;
+      constexpr int RING = D == 128 ? 6 : 4, PER = 16 / KS;                           // fragments held; logits of each 32 keys beside a fragment
+      u32x4 ring[RING];
+      auto weigh = [&](f32x16 (&zp)[2], int f) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = f * PER; i < (f + 1) * PER; ++i)
+#pragma unroll
+          for (int g = 0; g < 2; ++g) sum[g][i] += __builtin_amdgcn_exp2f(fmaf(zp[g][i], a.c, -lp));
+      };
+      // Logits of keys that a row does not see.
+      auto mask = [&](f32x16 (&zp)[2]) __attribute__((always_inline)) {
+        if (__builtin_expect(all_there && __ballot(limit_p < wave_key + 64) == 0, 1)) return;
+        const bool odd = lp != lp;                                     // a row whose log-sum-exp is NaN: what it sees is, what it does not see is not
+        if (__builtin_expect(__ballot(odd) != 0, 0)) {
+#pragma unroll
+          for (int g = 0; g < 2; ++g)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) zp[g][i] = odd ? lp : zp[g][i];
+          if (odd) lp = 0.0f;
+        }
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          const int n = min(max(limit_p - (wave_key + g * 32), 0), 32);
+          const unsigned seen = (there[g] & (unsigned)(((uint64_t)1 << n) - 1)) >> (4 * half);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int m = (int)(seen << (31 - 8 * (i >> 2) - (i & 3))) >> 31;       // all ones or zeros
+            zp[g][i] = __int_as_float((m & __float_as_int(zp[g][i])) | (~m & 0xFF800000));
+          }
+        }
+      };
+      auto step = [&](int s, f32x16 (&z)[2], f32x16 (&zp)[2]) __attribute__((always_inline)) {
+        const unsigned char *qt = q_lane + (s & (TILES - 1)) * TILE, *next = q_lane + ((s + 1) & (TILES - 1)) * TILE;
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(AHEAD - 2) : "memory");       // tile s + 1 has come, and tile s - 1 is nobody's
+        mask(zp);
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) z[g][i] = 0.0f;
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int f = 0; f < KS; ++f) {
+          ring[(f + RING - 1) % RING] = f + RING - 1 < KS ? query_frag(qt, f + RING - 1) : query_frag(next, f + RING - 1 - KS);
+#pragma unroll
+          for (int g = 0; g < 2; ++g) z[g] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(kf[g][f]), frag(ring[f % RING]), z[g], 0, 0, 0);
+          weigh(zp, f);
+          if (f == 0) fetch(s + AHEAD);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+        asm volatile("" ::"v"(sum[0]), "v"(sum[1]));                   // here, beside the MFMAs, not behind the next step's branch
+        // fragment f of the next step is in place f
+        if constexpr (KS % RING != 0) {
+          u32x4 turned[RING - 1];
+#pragma unroll
+          for (int f = 0; f < RING - 1; ++f) turned[f] = ring[(KS + f) % RING];
+#pragma unroll
+          for (int f = 0; f < RING - 1; ++f) ring[f] = turned[f];
+        }
+        if ((s & 15) == 8) stage((s >> 4) + 1);
+        const int at = (s & 15) * 32 + l32;
+        lp = row_lse[(s >> 4) & 1][at];
+        limit_p = row_limit[(s >> 4) & 1][at];
+      };
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(AHEAD - 1) : "memory");
+#pragma unroll
+      for (int f = 0; f < RING - 1; ++f) ring[f] = query_frag(q_lane, f);
+      int s = 0;
+      for (; s + 1 < steps; s += 2) {
+        step(s, za, zb);
+        step(s + 1, zb, za);
+      }
+      if (s < steps) {
+        step(s, za, zb);
+        mask(za);
+#pragma unroll
+        for (int f = 0; f < KS; ++f) weigh(za, f);
       } else {
-        kf[g][i] = x;
+        mask(zb);
+#pragma unroll
+        for (int f = 0; f < KS; ++f) weigh(zb, f);
+      }
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                  // what was sent for beyond the last row
+      __syncthreads();
+      // lanes added up: key by key, the 32 lanes of one side by side
+      float* red = reinterpret_cast<float*>(lds) + wave * 64 * RED;
+#pragma unroll
+      for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) red[(g * 32 + 8 * (i >> 2) + 4 * half + (i & 3)) * RED + l32] = sum[g][i];
+      __syncthreads();
+      float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int i = 0; i < 32; ++i) x[i & 3] += red[lane * RED + i];
+      const float mine = (x[0] + x[1]) + (x[2] + x[3]);
+      const int j = wave_key + lane;
+      if (!whole) {
+        a.part[(int64_t)slot * kMassKeys + wave * 64 + lane] = mine;
+      } else if (j >= from && j < len) {
+        float* sums = a.sums + r * a.s_seq + head * a.s_head;
+        sums[j] = fmaf(a.decay, old_sum(a, sums, j, len, nq), a.share * mine);
       }
     }
-  }
-  const bool all_there = there[0] == 0xFFFFFFFFu && there[1] == 0xFFFFFFFFu;
-
-  // ---- rows.  Step s has rows row0 + 32 s and on; the last row stands for those behind it, without weight.
-  const int steps = (row1 - row0 + 31) >> 5, G = a.b.G;
-  const int load_row = row0 + (wave >> 1) * 16 + (lane & 15), piece = (wave & 1) * SENT * 4 + (lane >> 4);
-  int load_t = load_row / G, load_g = load_row - load_t * G;        // of the next tile that is sent for
-  const int step_t = 32 / G, step_g = 32 - step_t * G, last_t = (rows - 1) / G, last_g = rows - 1 - last_t * G;
-  const uint16_t* queries = a.q + q0 * a.b.q_st + head * G * a.b.q_sh + piece * 8;
-  auto fetch = [&](int step) __attribute__((always_inline)) {
-    const bool behind = load_t > last_t || (load_t == last_t && load_g > last_g);
-    const uint16_t* p = queries + (behind ? last_t : load_t) * a.b.q_st + (behind ? last_g : load_g) * a.b.q_sh;
-    const uint32_t to = lds_address(lds) + (step & 3) * TILE + wave * SENT * 1024;
-#pragma unroll
-    for (int i = 0; i < SENT; ++i)
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to + i * 1024), "v"(p + i * 32) : "memory", "m0");
-    load_t += step_t;
-    load_g += step_g;
-    if (load_g >= G) { load_g -= G; ++load_t; }
-  };
-  auto stage = [&](int number) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < kMassStage / kMassThreads; ++i) {
-      const int at = i * kMassThreads + tid, row = row0 + number * kMassStage + at, rr = min(row, rows - 1), t = rr / G, g = rr - t * G;
-      const float x = a.lse[(int64_t)(q0 + t) * a.b.Hq + head * G + g];
-      row_lse[number & 1][at] = x * kLog2e;
-      row_limit[number & 1][at] = row < row1 ? limit_of(a, len, nq, t, x) : 0;
+    if (next_block >= x1) break;
+    start = next_block;
+    if (++block >= of.first + of.count) {                          // the next request with blocks, or the first one of the next head: 64 at a time
+      for (++r;;) {
+        const uint64_t some = __ballot(r + lane < n && blocks_of(a, min(r + lane, n - 1)).count > 0);
+        if (some != 0) { r += __builtin_ctzll(some); break; }
+        r += 64;
+        if (r >= n) { r = 0; ++head; }
+      }
+      of = blocks_of(a, r);
+      block = of.first;
     }
-  };
-  f32x16 sum[2];
-#pragma unroll
-  for (int g = 0; g < 2; ++g)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) sum[g][i] = 0.0f;
-  stage(0);
-  fetch(0); fetch(1); fetch(2);
-  const unsigned char* q_lane = lds + (l32 >> 4) * GROUP + (l32 & 15) * 16 + half * (FP8 ? 512 : 256);
-  for (int s = 0; s < steps; ++s) {
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * SENT) : "memory");       // tile s has come, and tile s - 1 is nobody's
-    fetch(s + 3);
-    if ((s & 15) == 8) stage((s >> 4) + 1);
-    const unsigned char* qt = q_lane + (s & 3) * TILE;
-    f32x16 z[2];
-#pragma unroll
-    for (int g = 0; g < 2; ++g)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) z[g][i] = 0.0f;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      const int p = FP8 ? (ks >> 1) * 4 + (ks & 1) : 2 * ks;       // piece of the lower half of the lanes
-      const bf16x8 qf = frag(*reinterpret_cast<const u32x4*>(qt + (p >> 2) * 1024 + (p & 3) * 256));
-#pragma unroll
-      for (int g = 0; g < 2; ++g) z[g] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(kf[g][ks]), qf, z[g], 0, 0, 0);
-    }
-    const int at = (s & 15) * 32 + l32;
-    const float l = row_lse[(s >> 4) & 1][at];
-    const int limit = row_limit[(s >> 4) & 1][at];
-    if (__builtin_expect(all_there && __ballot(limit < wave_key + 64) == 0, 1)) {
-#pragma unroll
-      for (int g = 0; g < 2; ++g)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sum[g][i] += __builtin_amdgcn_exp2f(fmaf(z[g][i], a.c, -l));
-    } else {
-#pragma unroll
-      for (int g = 0; g < 2; ++g)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int j = 8 * (i >> 2) + 4 * half + (i & 3);
-          const float w = __builtin_amdgcn_exp2f(fmaf(z[g][i], a.c, -l));
-          sum[g][i] += ((there[g] >> j) & 1) && wave_key + g * 32 + j < limit ? w : 0.0f;
-        }
-    }
+    block = uniform(block);
   }
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");                  // what was sent for beyond the last row
-  __syncthreads();
-  // lanes added up: key by key, the 32 lanes of one side by side
-  float* red = reinterpret_cast<float*>(lds) + wave * 64 * RED;
-#pragma unroll
-  for (int g = 0; g < 2; ++g)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) red[(g * 32 + 8 * (i >> 2) + 4 * half + (i & 3)) * RED + l32] = sum[g][i];
-  __syncthreads();
-  float x[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-  for (int i = 0; i < 32; ++i) x[i & 3] += red[lane * RED + i];
-  const float mine = (x[0] + x[1]) + (x[2] + x[3]);
-  const int j = wave_key + lane;
-  if (j < from || j >= len) return;
-  if (a.splits > 1) {
-    a.part[((int64_t)split * items + item) * a.b.max_kv + j] = mine;
-    return;
-  }
-  float* sums = a.sums + r * a.s_seq + head * a.s_head;
-  sums[j] = fmaf(a.decay, old_sum(a, sums, j, len, nq), a.share * mine);
+  if (tid == 0) a.cuts[share] = cut;
 }
 
-// Parts of the rows added up, a thread for each key.
-__global__ __launch_bounds__(kMassThreads) void mass_join_kernel(const MassArgs a) {
-  const int items = a.b.n_seqs * a.b.Hkv, blocks = (a.b.max_kv + kMassKeys - 1) / kMassKeys, item = blockIdx.x / blocks, block = blockIdx.x - item * blocks;
-  const int r = item / a.b.Hkv, head = item - r * a.b.Hkv, nq = a.b.cu_q[r + 1] - a.b.cu_q[r], rows = nq * a.b.G;
-  if (rows <= kFewRowsMost) return;
-  const int len = kv_len_of(a.b, r), j = block * kMassKeys + threadIdx.x;
-  if (j < first_of(a, r) || j >= len) return;
-  const int s0 = (first_row(a, len, nq, block * kMassKeys) & -32) / a.rows_each, s1 = (rows + a.rows_each - 1) / a.rows_each;
+// Parts of a block of keys added up, in the order of the rows: two threads a key, each some of the parts.
+__global__ __launch_bounds__(2 * kMassKeys) void mass_join_kernel(const MassArgs a) {
+  __shared__ float sum_of[2][kMassKeys];
+  const int first = blockIdx.x;
+  const CutKeys cut = a.cuts[first];
+  if (cut.r < 0) return;
+  const int key = threadIdx.x & (kMassKeys - 1), q = threadIdx.x / kMassKeys, parts = cut.last - first + 1;
   float x = 0.0f;
 #pragma unroll 8
-  for (int s = s0; s < s1; ++s) x += a.part[((int64_t)s * items + item) * a.b.max_kv + j];
-  float* sums = a.sums + r * a.s_seq + head * a.s_head;
-  sums[j] = fmaf(a.decay, old_sum(a, sums, j, len, nq), a.share * x);
+  for (int p = q * parts / 2; p < (q + 1) * parts / 2; ++p) x += a.part[(int64_t)(p == 0 ? 2 * first + 1 : 2 * (first + p)) * kMassKeys + key];
+  sum_of[q][key] = x;
+  __syncthreads();
+  const KeyBlocks of = blocks_of(a, cut.r);
+  const int j = cut.block * kMassKeys + key;
+  if (q != 0 || j < first_of(a, cut.r) || j >= of.len) return;
+  float* sums = a.sums + cut.r * a.s_seq + cut.head * a.s_head;
+  sums[j] = fmaf(a.decay, old_sum(a, sums, j, of.len, of.nq), a.share * (sum_of[0][key] + sum_of[1][key]));
 }
 
-// Workgroups that a call of many rows is cut into where it can be.
-constexpr int64_t kMassUnits = 2048;
-constexpr int kMassLeastRows = 1024;             // of a part
+constexpr int kMassShares = 256;                 // a workgroup for each compute unit
 constexpr int64_t kMostBlocks = (1 << 24) - 1;    // of 256 threads: an axis of a grid holds 2^32 threads
 
 int make_mass_plan(const codecomp_batch* b, const codecomp_pages* p, const codecomp_mass* m, MassPlan* pl) {
@@ -344,10 +512,9 @@ int make_mass_plan(const codecomp_batch* b, const codecomp_pages* p, const codec
   pl->d = p->head_dim;
   pl->scale = b->softmax_scale > 0.0f ? b->softmax_scale : 1.0f / sqrtf((float)p->head_dim);
   pl->few_rows = pl->many_rows = 0;
-  int64_t most = 0;
   for (int r = 0; r < x.n_seqs; ++r) {
     const int64_t rows = (int64_t)(b->cu_q_host[r + 1] - b->cu_q_host[r]) * x.G;
-    if (rows > kFewRowsMost) { ++pl->many_rows; most = std::max(most, rows); }
+    if (rows > kFewRowsMost) ++pl->many_rows;
     else if (rows > 0) ++pl->few_rows;
   }
   const int64_t items = (int64_t)x.n_seqs * x.Hkv;
@@ -357,18 +524,7 @@ int make_mass_plan(const codecomp_batch* b, const codecomp_pages* p, const codec
   pl->chunk = (int)std::min<int64_t>(chunk, 1 << 30);
   pl->chunks = (int)((x.max_kv + chunk - 1) / chunk);
   if (pl->few_rows > 0 && items * pl->chunks > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
-  pl->blocks = (x.max_kv + kMassKeys - 1) / kMassKeys;
-  pl->splits = pl->rows_each = 0;
-  pl->ws_bytes = 0;
-  if (pl->many_rows > 0 && pl->blocks > 0) {
-    if (items * pl->blocks > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
-    const int64_t units = (int64_t)pl->many_rows * x.Hkv * pl->blocks;
-    int64_t splits = std::max<int64_t>(1, std::min(kMassUnits / units, most / kMassLeastRows));
-    splits = std::min(splits, std::max<int64_t>(1, kMostBlocks / (items * pl->blocks)));
-    pl->rows_each = (int)std::min<int64_t>(((most + splits - 1) / splits + 31) / 32 * 32, INT32_MAX & -32);
-    pl->splits = (int)((most + pl->rows_each - 1) / pl->rows_each);
-    if (pl->splits > 1) pl->ws_bytes = ((size_t)pl->splits * items * x.max_kv * sizeof(float) + 255) & ~(size_t)255;
-  }
+  pl->ws_bytes = pl->many_rows > 0 && x.max_kv > 0 ? kMassShares * (2 * kMassKeys * sizeof(float) + sizeof(CutKeys)) : 0;
   return CODECOMP_OK;
 }
 
@@ -381,9 +537,9 @@ static int launch_mass_of(const MassPlan& pl, const MassArgs& a, hipStream_t str
     if (hipError_t e = hipGetLastError()) return (int)e;
   }
   if (pl.many_rows > 0) {
-    mass_many_kernel<D, FP8><<<dim3((unsigned)(items * pl.blocks * pl.splits)), block, 0, stream>>>(a);
+    mass_many_kernel<D, FP8><<<dim3(kMassShares), dim3(kManyMassThreads), 0, stream>>>(a);
     if (hipError_t e = hipGetLastError()) return (int)e;
-    if (pl.splits > 1) mass_join_kernel<<<dim3((unsigned)(items * pl.blocks)), block, 0, stream>>>(a);
+    mass_join_kernel<<<dim3(kMassShares), dim3(2 * kMassKeys), 0, stream>>>(a);
   }
   return (int)hipGetLastError();
 }
@@ -397,7 +553,8 @@ int launch_mass(const MassPlan& pl, const void* q, const float* lse, int layer, 
   a.layer = layer * pl.pool.s_layer;
   a.c = fminf(fmaxf(pl.scale * pl.pool.k_scale * kLog2e, FLT_MIN), FLT_MAX);
   a.decay = decay; a.share = 1.0f / pl.batch.G;
-  a.chunk = pl.chunk; a.splits = pl.splits; a.rows_each = pl.rows_each;
+  a.cuts = reinterpret_cast<CutKeys*>(a.part + 2 * kMassShares * kMassKeys);
+  a.chunk = pl.chunk; a.shares = kMassShares;
   if (pl.d == 128) return pl.pool.fp8 ? launch_mass_of<128, true>(pl, a, stream) : launch_mass_of<128, false>(pl, a, stream);
   return pl.pool.fp8 ? launch_mass_of<64, true>(pl, a, stream) : launch_mass_of<64, false>(pl, a, stream);
 }

@@ -37,7 +37,6 @@ struct MassPlan {
   float scale;
   int few_rows, many_rows;     // requests of each kind (mass.hip)
   int chunk, chunks;           // few rows: keys of a workgroup, and workgroups for a request and head
-  int blocks, splits, rows_each;       // many rows: blocks of keys, parts that the rows are cut into, rows of a part
   size_t ws_bytes;
 };
 int make_mass_plan(const codecomp_batch* b, const codecomp_pages* p, const codecomp_mass* m, MassPlan* plan);
