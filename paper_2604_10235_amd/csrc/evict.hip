@@ -9,6 +9,8 @@
 namespace codecomp {
 
 constexpr int kMoveDeep = 8;                             // pieces of 16 bytes that a thread has in flight
+constexpr int kBothDeep = 4, kBothThreads = 512;
+constexpr int kManyProblems = 1024;
 constexpr int kFewMoves = 1024;                          // workgroups up to which they are of 1024 threads, not 256
 constexpr int64_t kMostBlocks = (1 << 22) - 1;          // of up to 1024 threads: an axis of a grid holds 2^32 threads
 
@@ -29,18 +31,16 @@ __device__ __forceinline__ unsigned ordered(float x) {
 
 // A thread has PER rows in registers; a request that has more is read again for the rest of them, as often as they are looked at.
 template <int THREADS, int PER>
-__global__ __launch_bounds__(THREADS) void keep_kernel(const EvictArgs a) {
+__device__ __forceinline__ void keep_rows(const EvictArgs& a, const Span s, int layer, int r, int head) {
   constexpr int WAVES = THREADS / 64, COPIES = 4, ENTRIES = WAVES * PER;
   __shared__ __attribute__((aligned(16))) int counts[4][COPIES][256];       // of a digit's values, for each of the four digits
   __shared__ int2 before[ENTRIES];                        // rows above the border and at it: of a wave's strip, then of all before it
   __shared__ int2 strip[2][WAVES];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int problem = blockIdx.x, head = problem % a.Hkv, rest = problem / a.Hkv, r = rest % a.n_seqs, layer = rest / a.n_seqs;
-  const Span s = span_of(a, r);
   if (tid == 0 && head == 0 && layer == 0) a.new_lens[r] = s.f + s.m;
   const float* sums = a.from.sums + layer * a.from.s_layer + r * a.from.s_seq + head * a.from.s_head;
   float* to = a.to.sums + layer * a.to.s_layer + r * a.to.s_seq + head * a.to.s_head + s.f;
-  int32_t* kept = a.kept + (int64_t)problem * a.max_budget;
+  int32_t* kept = a.kept + (((int64_t)layer * a.n_seqs + r) * a.Hkv + head) * a.max_budget;
   const bool all = s.m == s.n - s.f;
   const int last = all ? s.f : s.n - a.recent;           // rows from there on stay
   for (int i = tid; i < 4 * COPIES * 256; i += THREADS) (&counts[0][0][0])[i] = 0;
@@ -173,45 +173,77 @@ __global__ __launch_bounds__(THREADS) void keep_kernel(const EvictArgs a) {
   for (int i = s.m + tid; i < a.max_budget; i += THREADS) kept[i] = -1;
 }
 
-// PIECES: 16-byte pieces of a row that a workgroup moves.
-template <int PIECES, int THREADS>
-__global__ __launch_bounds__(THREADS) void close_up_kernel(const EvictArgs a, int slices) {
+// Rows move together, DEEP pieces of 16 bytes of a pool a thread at a time.  PIECES: of a row that a workgroup moves; POOLS: one pool, or K and V.
+template <int PIECES, int THREADS, int DEEP, int POOLS>
+__device__ __forceinline__ void close_up(const EvictArgs& a, const Span s, int layer, int r, int head, unsigned char* const (&pool)[POOLS], int slice) {
   constexpr int ROWS = THREADS / PIECES;
-  const int tid = threadIdx.x, part = blockIdx.x % (2 * slices), problem = blockIdx.x / (2 * slices);
-  const int head = problem % a.Hkv, rest = problem / a.Hkv, r = rest % a.n_seqs, layer = rest / a.n_seqs;
-  const Span s = span_of(a, r);
-  if (s.m == s.n - s.f) return;
-  unsigned char* base = (part & 1 ? a.pool.v : a.pool.k) + layer * a.pool.s_layer + head * a.pool.s_head + ((part >> 1) * PIECES + tid % PIECES) * 16;
-  const int32_t* kept = a.kept + (int64_t)problem * a.max_budget;
+  const int tid = threadIdx.x;
+  const int64_t base = layer * a.pool.s_layer + head * a.pool.s_head + (slice * PIECES + tid % PIECES) * 16;
+  const int32_t* kept = a.kept + (((int64_t)layer * a.n_seqs + r) * a.Hkv + head) * a.max_budget;
   const int32_t* table = a.table + (int64_t)r * a.table_width;
   const int in_page = (1 << a.pool.page_log2) - 1;
   auto place = [&](int row) __attribute__((always_inline)) {
     const int page = table[row >> a.pool.page_log2];
     return page < 0 || page >= a.pool.n_pages ? (int64_t)-1 : page * a.pool.s_page + (row & in_page) * a.pool.s_tok;
   };
-  for (int first = 0; first < s.m; first += ROWS * kMoveDeep) {
-    u32x4 x[kMoveDeep];
-    int64_t to[kMoveDeep];
+  for (int first = 0; first < s.m; first += ROWS * DEEP) {
+    u32x4 x[DEEP][POOLS];
+    int64_t to[DEEP];
 #pragma unroll
-    for (int u = 0; u < kMoveDeep; ++u) {
+    for (int u = 0; u < DEEP; ++u) {
       const int i = first + u * ROWS + tid / PIECES;
       to[u] = -1;
-      x[u] = u32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int p = 0; p < POOLS; ++p) x[u][p] = u32x4{0, 0, 0, 0};
       if (i < s.m) {
         const int row = kept[i];
         if (row != s.f + i) {                            // else it stays where it is
           const int64_t from = place(row);
           to[u] = place(s.f + i);
-          if (from >= 0) x[u] = *reinterpret_cast<const u32x4*>(base + from);
+          if (from >= 0) {
+#pragma unroll
+            for (int p = 0; p < POOLS; ++p) x[u][p] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(pool[p] + base + from));
+          }
         }
       }
     }
     // All rows of the batch are in registers before one is overwritten; rows of later batches lie behind those that this one writes.
     asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
 #pragma unroll
-    for (int u = 0; u < kMoveDeep; ++u)
-      if (to[u] >= 0) __builtin_nontemporal_store(x[u], reinterpret_cast<u32x4*>(base + to[u]));
+    for (int u = 0; u < DEEP; ++u)
+      if (to[u] >= 0) {
+#pragma unroll
+        for (int p = 0; p < POOLS; ++p) __builtin_nontemporal_store(x[u][p], reinterpret_cast<u32x4*>(pool[p] + base + to[u]));
+      }
   }
+}
+
+template <int THREADS, int PER>
+__global__ __launch_bounds__(THREADS) void keep_kernel(const EvictArgs a) {
+  const int head = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv, r = rest % a.n_seqs;
+  keep_rows<THREADS, PER>(a, span_of(a, r), rest / a.n_seqs, r, head);
+}
+
+template <int PIECES, int THREADS>
+__global__ __launch_bounds__(THREADS) void close_up_kernel(const EvictArgs a, int slices) {
+  const int part = blockIdx.x % (2 * slices), problem = blockIdx.x / (2 * slices);
+  const int head = problem % a.Hkv, rest = problem / a.Hkv, r = rest % a.n_seqs;
+  const Span s = span_of(a, r);
+  if (s.m == s.n - s.f) return;
+  unsigned char* const pool[1] = {part & 1 ? a.pool.v : a.pool.k};
+  close_up<PIECES, THREADS, kMoveDeep, 1>(a, s, rest / a.n_seqs, r, head, pool, part >> 1);
+}
+
+// Both, for many problems: what one workgroup waits for while it finds its border is hidden behind the rows of others.
+template <int PIECES, int THREADS, int PER>
+__global__ __launch_bounds__(THREADS) void evict_kernel(const EvictArgs a) {
+  const int head = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv, r = rest % a.n_seqs, layer = rest / a.n_seqs;
+  const Span s = span_of(a, r);
+  keep_rows<THREADS, PER>(a, s, layer, r, head);
+  if (s.m == s.n - s.f) return;
+  __syncthreads();
+  unsigned char* const pool[2] = {a.pool.k, a.pool.v};
+  close_up<PIECES, THREADS, kBothDeep, 2>(a, s, layer, r, head, pool, 0);
 }
 
 template <int PIECES>
@@ -227,6 +259,13 @@ int launch_evict(const EvictArgs& a, int d, hipStream_t stream) {
   int slices = 1;
   while (slices < pieces / 8 && problems * 2 * slices < 64) slices *= 2;
   if (problems * 2 * slices > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
+  if (problems >= kManyProblems && a.max_kv <= 8192) {
+    const dim3 grid((unsigned)problems), block(kBothThreads);
+    if (pieces == 16) evict_kernel<16, kBothThreads, 8><<<grid, block, 0, stream>>>(a);
+    else if (pieces == 8) evict_kernel<8, kBothThreads, 8><<<grid, block, 0, stream>>>(a);
+    else evict_kernel<4, kBothThreads, 8><<<grid, block, 0, stream>>>(a);
+    return (int)hipGetLastError();
+  }
   if (a.max_kv > 8192) keep_kernel<1024, 32><<<dim3((unsigned)problems), dim3(1024), 0, stream>>>(a);
   else if (a.max_kv > 2048) keep_kernel<256, 16><<<dim3((unsigned)problems), dim3(256), 0, stream>>>(a);
   else keep_kernel<256, 8><<<dim3((unsigned)problems), dim3(256), 0, stream>>>(a);
