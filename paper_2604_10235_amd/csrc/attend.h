@@ -33,6 +33,7 @@ struct SharedRows {
   int few_units, few_parts, few_chunk, few_splits;       // shared rows of groups of few rows: workgroups, parts of the rows, keys of a chunk, chunks
   int many_units, many_blocks, many_tiles, many_splits;  // of many: workgroups, most blocks of rows of a group, tiles of a chunk, chunks
   int splits;                  // the larger one: parts of shared rows that every row has
+  int join;                    // 1: whoever has a request's own rows joins the parts of the shared ones to them, and writes the outputs
 };
 // What a row's parts say that had no keys: not to be read any further.
 constexpr float kNoPart = -1.0f;
@@ -57,14 +58,15 @@ struct SharedArgs : AttendArgs {
 };
 
 __device__ __forceinline__ int prefix_of(const SharedRows& sh, int g) { return min(max(sh.prefix_lens[g], 0), sh.max_prefix); }
+// The place of part p of a row among all parts.
+__device__ __forceinline__ int64_t part_at(const AttendArgs& a, int p, int token, int head) { return ((int64_t)p * a.b.T + token) * a.b.Hq + head; }
 // Parts first .. last - 1 of rows row0 .. row1 - 1 of a KV head, which has tokens from q0 on: nothing in them.
 template <int THREADS>
 __device__ __forceinline__ void no_parts(const AttendArgs& a, int first, int last, int q0, int head, int row0, int row1) {
-  const int64_t all = (int64_t)a.b.T * a.b.Hq;
   for (int row = row0 + threadIdx.x; row < row1; row += THREADS) {
     const int t = row / a.b.G, h = head * a.b.G + row - t * a.b.G;
     for (int p = first; p < last; ++p) {
-      const int64_t part = p * all + (int64_t)(q0 + t) * a.b.Hq + h;
+      const int64_t part = part_at(a, p, q0 + t, h);
       a.part_ml[2 * part] = -INFINITY; a.part_ml[2 * part + 1] = kNoPart;
     }
   }

@@ -71,6 +71,7 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void atten
   CutBlock cut = {-1, 0, 0, 0};
   int shared_q0 = 0, shared_nq = 0, shared_len = 0, shared_part = 0, key_end = 0;        // SHARED: tokens of the group or request, keys up to which there are some, number of the part
   int causal = SHARED ? 0 : a.b.causal;
+  bool shared_join = false;                                       // these are a request's own rows, and the parts of the shared ones are joined to them
   if constexpr (EVEN) {
     share = blockIdx.x;
     row0 = 0;
@@ -139,8 +140,9 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void atten
       key_end = (int)min((int64_t)key0 + a.chunk, (int64_t)INT32_MAX);
       shared_part = a.sh.splits + split;
       causal = a.b.causal;
+      shared_join = a.sh.join != 0;
     }
-    if (key0 >= shared_len) {
+    if (key0 >= shared_len && (group || !a.sh.join)) {
       no_parts<64 * kFewWaves>(a, shared_part, shared_part + 1, shared_q0, head, row0, min(shared_nq * a.b.G, row0 + 16 * RB));
       return;
     }
@@ -180,7 +182,7 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void atten
       look_up(next_page, key0 + (kFewWaves + wave) * kFewKeys, key1);
     } else if constexpr (SHARED) {
       key1 = key_end;
-      whole = false;
+      whole = shared_join;
     } else {
       if (rows <= row0 || rows > a.row_slots) return;
       key1 = min(len, key0 + a.chunk);
@@ -391,6 +393,16 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void atten
         float to = -INFINITY;
 #pragma unroll
         for (int w = 0; w < kFewWaves; ++w) to = fmaxf(to, row_m[w][n]);
+        int64_t shared_row = 0, shared_rows = 0;
+        if constexpr (SHARED) {
+          if (shared_join) {                                      // parts' references: the 16 threads of a row take them in turn
+            shared_row = part_at(a, 0, q0 + row / a.b.G, head * a.b.G + row % a.b.G);
+            shared_rows = (int64_t)a.b.T * a.b.Hq;
+            for (int p = tid & 15; p < a.sh.splits; p += 16) to = fmaxf(to, a.part_ml[2 * (p * shared_rows + shared_row)]);
+#pragma unroll
+            for (int off = 1; off < 16; off <<= 1) to = fmaxf(to, __shfl_xor(to, off));
+          }
+        }
         float all = 0.0f, x[E];
 #pragma unroll
         for (int i = 0; i < E; ++i) x[i] = 0.0f;
@@ -401,6 +413,24 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void atten
 #pragma unroll
           for (int i = 0; i < E; ++i) x[i] += f * o_lds[(w * 16 + n) * O_ROW + e + i];
         }
+        if constexpr (SHARED) {
+          if (shared_join) {
+#pragma unroll 8
+            for (int p = 0; p < a.sh.splits; ++p) {
+              const int64_t part = p * shared_rows + shared_row;
+              const float pm = a.part_ml[2 * part], pl = a.part_ml[2 * part + 1];
+              const bool some = pl != kNoPart;
+              const float f = some && pm != -INFINITY ? __builtin_amdgcn_exp2f(pm - to) : 0.0f;
+              if (some) all += f * pl;
+#pragma unroll
+              for (int i = 0; i < E; i += 4) {
+                const f32x4 v = *reinterpret_cast<const f32x4*>(a.part_o + part * D + e + i);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) x[i + k] += some ? f * v[k] : 0.0f;
+              }
+            }
+          }
+        }
         if (whole) {
           const int t = row / a.b.G, h = head * a.b.G + row - t * a.b.G;
           const float inv = all == 0.0f ? 0.0f : a.pool.v_scale / all;
@@ -409,7 +439,7 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void atten
           for (int i = 0; i < E; i += 2) *reinterpret_cast<unsigned*>(out + i) = pack2(x[i] * inv, x[i + 1] * inv);
           if (a.lse && (tid & 15) == 0) a.lse[(int64_t)(q0 + t) * a.b.Hq + h] = all == 0.0f ? -INFINITY : (to + __builtin_amdgcn_logf(all)) * kLn2;
         } else {
-          const int64_t part = SHARED ? ((int64_t)shared_part * a.b.T + q0 + row / a.b.G) * a.b.Hq + head * a.b.G + row % a.b.G : part0 + row;
+          const int64_t part = SHARED ? part_at(a, shared_part, q0 + row / a.b.G, head * a.b.G + row % a.b.G) : part0 + row;
 #pragma unroll
           for (int i = 0; i < E; i += 4) *reinterpret_cast<f32x4*>(a.part_o + part * D + e + i) = f32x4{x[i], x[i + 1], x[i + 2], x[i + 3]};
           if ((tid & 15) == 0) { a.part_ml[2 * part] = to; a.part_ml[2 * part + 1] = all; }

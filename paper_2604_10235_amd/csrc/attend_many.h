@@ -566,7 +566,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
                   u32x2{pack2(o[db][4 * i] * inv, o[db][4 * i + 1] * inv), pack2(o[db][4 * i + 2] * inv, o[db][4 * i + 3] * inv)};
           if (a.lse && half == 0) a.lse[(int64_t)(q0 + t) * a.b.Hq + h] = sum == 0.0f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * kLn2;
         } else if (row < of.rows) {
-          const int64_t part = SHARED ? ((int64_t)g * a.b.T + of.q0 + row / of.G) * a.b.Hq + head * of.G + row % of.G : (int64_t)slot * kManyRows + wave * 32 + l32;
+          const int64_t part = SHARED ? part_at(a, g, of.q0 + row / of.G, head * of.G + row % of.G) : (int64_t)slot * kManyRows + wave * 32 + l32;
 #pragma unroll
           for (int db = 0; db < DB; ++db)
 #pragma unroll

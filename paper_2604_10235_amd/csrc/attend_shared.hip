@@ -24,6 +24,10 @@ extern template int launch_many_shared_of<128, true>(const ManyArgs&, hipStream_
 constexpr int kChip = 256;                       // compute units: workgroups of the kernel for many rows that run at once
 constexpr int64_t kMostBlocks = (1 << 23) - 1;    // of up to 512 threads: an axis of a grid holds 2^32 threads
 constexpr int kMostSplits = 1024;
+constexpr int kJoinParts = 6;
+constexpr int64_t kJoinRows = 16384;
+constexpr int kJoinKeys = 512;
+constexpr int64_t kJoinItems = 192;
 
 int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const codecomp_pages* p, SharedPlan* pl) {
   if (int rc = make_pool(p, &pl->pool)) return rc;
@@ -56,8 +60,12 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
   }
   for (int r = 0; r < x.n_seqs; ++r) own_most = std::max(own_most, (int64_t)(b->cu_q_host[r + 1] - b->cu_q_host[r]) * x.G);
   blocks *= x.Hkv;
-  pl->two_blocks = std::max(few_most, own_most) > 16;
-  const int rows_each = pl->two_blocks ? 32 : 16;
+  const int64_t items = (int64_t)x.n_seqs * x.Hkv;
+  // Where one workgroup has all own rows of a request's head, it joins the parts of the shared ones to them as well.
+  s.join = s.max_own <= kJoinKeys || items >= kJoinItems;
+  pl->few_two = s.join ? few_most > 16 : std::max(few_most, own_most) > 16;
+  pl->own_two = s.join ? own_most > 16 : pl->few_two;
+  const int few_each = pl->few_two ? 32 : 16, own_each = pl->own_two ? 32 : 16;
 
   // shared rows, many: chunks such that all workgroups run at once and end together
   s.many_splits = s.few_splits = 0;
@@ -85,53 +93,88 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
     *splits = (int)((most + keys - 1) / keys);
   };
   // shared rows, few
-  s.few_parts = std::max<int>(1, (int)((few_most + rows_each - 1) / rows_each));
+  s.few_parts = std::max<int>(1, (int)((few_most + few_each - 1) / few_each));
   int64_t few_units = 0;
   if (pl->few_groups > 0) {
-    const int64_t items = (int64_t)s.n_groups * x.Hkv * s.few_parts;
+    const int64_t units = (int64_t)s.n_groups * x.Hkv * s.few_parts;
     cut((int64_t)pl->few_groups * x.Hkv * s.few_parts, s.max_prefix, &s.few_chunk, &s.few_splits);
     s.few_splits = std::max(s.few_splits, 1);
-    few_units = items * s.few_splits;
+    few_units = units * s.few_splits;
     if (few_units > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
   }
   s.few_units = (int)few_units;
   s.splits = std::max(s.many_splits, s.few_splits);
   // rows behind them
-  pl->row_parts = std::max<int>(1, (int)std::min<int64_t>((own_most + rows_each - 1) / rows_each, INT32_MAX));
-  const int64_t items = (int64_t)x.n_seqs * x.Hkv;
+  pl->row_parts = std::max<int>(1, (int)std::min<int64_t>((own_most + own_each - 1) / own_each, INT32_MAX));
   if (items * pl->row_parts > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
-  cut(items * pl->row_parts, s.max_own, &pl->chunk, &pl->own_splits);
+  if (s.join) {
+    pl->chunk = s.max_own;
+    pl->own_splits = 1;
+  } else {
+    cut(items * pl->row_parts, s.max_own, &pl->chunk, &pl->own_splits);
+  }
   pl->own_units = items * pl->row_parts * pl->own_splits;
   if (pl->own_units + few_units > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
-  if ((int64_t)x.T * x.Hq > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
-  pl->ws_bytes = x.T == 0 ? 0 : ((size_t)(s.splits + pl->own_splits) * x.T * x.Hq * (p->head_dim + 2) * sizeof(float) + 255) & ~(size_t)255;
+  if (!s.join && (int64_t)x.T * x.Hq >= (1 << 24)) return CODECOMP_EINVAL_SHAPE;       // workgroups of the joining kernel
+  pl->ws_bytes = x.T == 0 ? 0 : ((size_t)(s.splits + (s.join ? 0 : pl->own_splits)) * x.T * x.Hq * (p->head_dim + 2) * sizeof(float) + 255) & ~(size_t)255;
   return CODECOMP_OK;
 }
 
-// A row's parts, those of the shared rows first; D / 4 threads a row.
-template <int D>
+// A row's parts, those of the shared rows first: GROUPS times D / 4 threads a row, the parts shared out over the groups and these added up in order.
+template <int D, int GROUPS>
 __global__ __launch_bounds__(256) void join_shared_kernel(const AttendArgs a, int parts) {
-  constexpr int THREADS = D / 4;
-  const int64_t rows = (int64_t)a.b.T * a.b.Hq, row = (int64_t)blockIdx.x * (256 / THREADS) + threadIdx.x / THREADS;
-  const int e = (threadIdx.x % THREADS) * 4;
-  if (row >= rows) return;
+  constexpr int THREADS = D / 4, ROWS = 256 / THREADS / GROUPS;
+  __shared__ f32x4 sums[GROUPS][ROWS][THREADS];
+  __shared__ float tops[GROUPS][ROWS], alls[GROUPS][ROWS];
+  const int in = threadIdx.x / THREADS, group = in % GROUPS, slot = in / GROUPS, th = threadIdx.x % THREADS, e = th * 4;
+  const int64_t rows = (int64_t)a.b.T * a.b.Hq, row = (int64_t)blockIdx.x * ROWS + slot;
+  const bool there = row < rows;
   float top = -INFINITY, all = 0.0f;
+  if (there) {
 #pragma unroll 8
-  for (int p = 0; p < parts; ++p) top = fmaxf(top, a.part_ml[2 * (p * rows + row)]);
-  f32x4 x = {0, 0, 0, 0};
-#pragma unroll 4
-  for (int p = 0; p < parts; ++p) {
-    const int64_t part = p * rows + row;
-    const float m = a.part_ml[2 * part], l = a.part_ml[2 * part + 1];
-    if (l == kNoPart) continue;
-    const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - top);       // times zeros, or an infinity or NaN that it saw
-    all += l * f;
-    x += *reinterpret_cast<const f32x4*>(a.part_o + part * D + e) * f;
+    for (int p = group; p < parts; p += GROUPS) top = fmaxf(top, a.part_ml[2 * (p * rows + row)]);
   }
+  if constexpr (GROUPS > 1) {
+    if (th == 0) tops[group][slot] = top;
+    __syncthreads();
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) top = fmaxf(top, tops[g][slot]);
+  }
+  f32x4 x = {0, 0, 0, 0};
+  if (there) {
+#pragma unroll 4
+    for (int p = group; p < parts; p += GROUPS) {
+      const int64_t part = p * rows + row;
+      const float m = a.part_ml[2 * part], l = a.part_ml[2 * part + 1];
+      const f32x4 v = *reinterpret_cast<const f32x4*>(a.part_o + part * D + e);
+      if (l == kNoPart) continue;
+      const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - top);       // times zeros, or an infinity or NaN that it saw
+      all += l * f;
+      x += v * f;
+    }
+  }
+  if constexpr (GROUPS > 1) {
+    sums[group][slot][th] = x;
+    if (th == 0) alls[group][slot] = all;
+    __syncthreads();
+    if (group > 0) return;
+    x = sums[0][slot][th]; all = alls[0][slot];
+#pragma unroll
+    for (int g = 1; g < GROUPS; ++g) { x += sums[g][slot][th]; all += alls[g][slot]; }
+  }
+  if (!there) return;
   const int64_t t = row / a.b.Hq, h = row - t * a.b.Hq;
   const float inv = all == 0.0f ? 0.0f : a.pool.v_scale / all;
   *reinterpret_cast<u32x2*>(a.out + t * a.b.o_st + h * a.b.o_sh + e) = u32x2{pack2(x.x * inv, x.y * inv), pack2(x.z * inv, x.w * inv)};
   if (a.lse && e == 0) a.lse[row] = all == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(all)) * kLn2;
+}
+
+template <int D, int GROUPS>
+static int launch_join(const AttendArgs& a, int parts, hipStream_t stream) {
+  constexpr int ROWS = 256 / (D / 4) / GROUPS;
+  const int64_t rows = (int64_t)a.b.T * a.b.Hq;
+  join_shared_kernel<D, GROUPS><<<dim3((unsigned)((rows + ROWS - 1) / ROWS)), dim3(256), 0, stream>>>(a, parts);
+  return (int)hipGetLastError();
 }
 
 int launch_shared(const SharedPlan& pl, const void* q, int layer, void* out, float* lse, void* workspace, hipStream_t stream) {
@@ -141,7 +184,7 @@ int launch_shared(const SharedPlan& pl, const void* q, int layer, void* out, flo
   a.c = fminf(fmaxf(pl.scale * pl.pool.k_scale * kLog2e, FLT_MIN), FLT_MAX);       // a hidden logit of minus infinity times it stays one
   a.chunk = pl.chunk; a.row_parts = pl.row_parts;
   a.sh = pl.sh;
-  const int parts = pl.sh.splits + pl.own_splits;
+  const int parts = pl.sh.splits + (pl.sh.join ? 0 : pl.own_splits);
   const int64_t rows = (int64_t)pl.batch.T * pl.batch.Hq;
   a.part_o = static_cast<float*>(workspace);
   a.part_ml = a.part_o + parts * rows * pl.d;
@@ -155,13 +198,17 @@ int launch_shared(const SharedPlan& pl, const void* q, int layer, void* out, flo
     else rc = pl.pool.fp8 ? launch_many_shared_of<64, true>(m, stream) : launch_many_shared_of<64, false>(m, stream);
     if (rc) return rc;
   }
+  if (pl.sh.join) {
+    if (pl.sh.few_units > 0)
+      if (int rc = launch_few_shared(pl.d, pl.pool.fp8, pl.few_two, pl.sh.few_units, a, stream)) return rc;
+    a.sh.few_units = 0;
+    return launch_few_shared(pl.d, pl.pool.fp8, pl.own_two, pl.own_units, a, stream);
+  }
   if (pl.sh.few_units + pl.own_units > 0)
-    if (int rc = launch_few_shared(pl.d, pl.pool.fp8, pl.two_blocks, pl.sh.few_units + pl.own_units, a, stream)) return rc;
-  const int each = 256 / (pl.d / 4);
-  const dim3 grid((unsigned)((rows + each - 1) / each)), block(256);
-  if (pl.d == 128) join_shared_kernel<128><<<grid, block, 0, stream>>>(a, parts);
-  else join_shared_kernel<64><<<grid, block, 0, stream>>>(a, parts);
-  return (int)hipGetLastError();
+    if (int rc = launch_few_shared(pl.d, pl.pool.fp8, pl.few_two, pl.sh.few_units + pl.own_units, a, stream)) return rc;
+  const bool many = parts >= kJoinParts && rows <= kJoinRows;
+  if (pl.d == 128) return many ? launch_join<128, 8>(a, parts, stream) : launch_join<128, 1>(a, parts, stream);
+  return many ? launch_join<64, 16>(a, parts, stream) : launch_join<64, 1>(a, parts, stream);
 }
 
 }  // namespace codecomp

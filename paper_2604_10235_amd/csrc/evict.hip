@@ -10,6 +10,7 @@ namespace codecomp {
 
 constexpr int kMoveDeep = 8;                             // pieces of 16 bytes that a thread has in flight
 constexpr int kBothDeep = 4, kBothThreads = 512;
+constexpr int kFewest = 256;
 constexpr int kManyProblems = 1024;
 constexpr int kFewMoves = 1024;                          // workgroups up to which they are of 1024 threads, not 256
 constexpr int64_t kMostBlocks = (1 << 22) - 1;          // of up to 1024 threads: an axis of a grid holds 2^32 threads
@@ -257,7 +258,7 @@ int launch_evict(const EvictArgs& a, int d, hipStream_t stream) {
   const int64_t problems = (int64_t)a.n_layers * a.n_seqs * a.Hkv;
   const int pieces = d * (a.pool.fp8 ? 1 : 2) / 16;
   int slices = 1;
-  while (slices < pieces / 8 && problems * 2 * slices < 64) slices *= 2;
+  while (slices < pieces / 8 && problems * 2 * slices < kFewest) slices *= 2;
   if (problems * 2 * slices > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
   if (problems >= kManyProblems && a.max_kv <= 8192) {
     const dim3 grid((unsigned)problems), block(kBothThreads);

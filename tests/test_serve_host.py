@@ -121,7 +121,7 @@ def test_shared_refuses_pointers_layers_and_workspaces():
     assert shared(x, g, p, layer=2) == -12 and shared(x, g, p, layer=-1) == -12
     assert shared(x, g, p, q=D + 2) == -2 and shared(x, g, p, out=D + 8) == -2 and shared(x, g, p, lse=D + 2) == -2
     need = b.lib().codecomp_attend_shared_workspace_bytes(ref(x), ref(g), ref(p))
-    assert need >= 2 * 3 * 28 * 130 * 4                              # two parts at least of every row
+    assert need >= 3 * 28 * 130 * 4                                  # a part at least of every row
     for bad in (dict(ws=None), dict(ws=D + 16), dict(ws=D + 128), dict(size=need - 1), dict(size=0)):
         assert shared(x, g, p, **bad) == -9, bad
 
