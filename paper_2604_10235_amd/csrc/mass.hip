@@ -38,7 +38,7 @@ struct MassArgs {
   CutKeys* cuts;               // [shares]
   int64_t layer;               // byte offset of the layer in the pool
   float c, decay, share;       // softmax_scale * k_scale * log2(e); 1 / G
-  int chunk, shares;
+  int chunk, shares, few_shares;
 };
 
 constexpr int kMassWaves = 4, kMassThreads = 64 * kMassWaves;
@@ -59,126 +59,198 @@ __device__ __forceinline__ float old_sum(const MassArgs& a, const float* sums, i
   return a.decay != 0.0f && j < (a.b.causal ? len - nq : len) ? sums[j] : 0.0f;
 }
 
-template <int D, bool FP8>
-__global__ __launch_bounds__(kMassThreads, FP8 && D == 128 ? 3 : 4) void mass_few_kernel(const MassArgs a) {
-  constexpr int LOADS = D * (FP8 ? 1 : 2) / 64, KS = D / 32, CG = LOADS >= 4 ? 2 : 4, KEYS = 16 * CG, STRIP = kMassWaves * KEYS;
+// Keys of a request that the kernel for few rows takes, in strips of what four waves read at a time: from the one with the first that counts on.
+template <int STRIP>
+__device__ __forceinline__ int mass_strips(const MassArgs& a, int r) {
+  const int nq = a.b.cu_q[r + 1] - a.b.cu_q[r], len = kv_len_of(a.b, r), from = first_of(a, r);
+  return nq <= 0 || nq > kFewRowsMost || nq * a.b.G > kFewRowsMost || from >= len ? 0 : (len + STRIP - 1) / STRIP - from / STRIP;
+}
+
+// EVEN: the strips of all requests and heads form one sequence, cut into equal parts; else a workgroup has one chunk of a request.
+template <int D, bool FP8, bool EVEN>
+__global__ __launch_bounds__(kMassThreads, 4) void mass_few_kernel(const MassArgs a) {
+  constexpr int LOADS = D * (FP8 ? 1 : 2) / 64, KS = D / 32, CG = D == 128 ? 2 : 4, KEYS = 16 * CG, STRIP = kMassWaves * KEYS;
   __shared__ __attribute__((aligned(16))) float row_lse[kFewRowsMost];
   __shared__ __attribute__((aligned(16))) int row_limit[kFewRowsMost];
-  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), l16 = lane & 15, quarter = lane >> 4;
-  // chunk by chunk, all requests and heads of one: short requests lack the later ones
-  const int items = a.b.n_seqs * a.b.Hkv, turn = blockIdx.x / items, item = blockIdx.x - turn * items;
-  const int r = item / a.b.Hkv, head = item - r * a.b.Hkv;
-  const int64_t chunk0 = (int64_t)turn * a.chunk;
-  const int key0 = (int)chunk0;
-  const int32_t* table = a.b.table + (int64_t)r * a.b.table_width;
-  // Page entries for keys tile + 16 g + l16.  Those of the first two tiles are sent for before it is known how many keys there are: one wait less.
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+  int l16 = lane & 15, quarter = lane >> 4;
+  int r, head, key0, strip = 0;
+  int64_t left = 0;                                              // EVEN: strips that are left
+  const int32_t* table;
+  // Page entries for keys tile + 16 g + l16.  Those of a chunk's first two tiles are sent for before it is known how many keys there are: one wait less.
   int page[CG], next_page[CG];
   auto look_up = [&](int (&pg)[CG], int64_t tile, int end) __attribute__((always_inline)) {
 #pragma unroll
     for (int g = 0; g < CG; ++g) pg[g] = table[max((int)min(tile + 16 * g + l16, (int64_t)end - 1), 0) >> a.pool.page_log2];
   };
-  look_up(page, chunk0 + wave * KEYS, a.b.max_kv);
-  look_up(next_page, chunk0 + (kMassWaves + wave) * KEYS, a.b.max_kv);
-  const int q0 = a.b.cu_q[r], nq = a.b.cu_q[r + 1] - q0, rows = nq * a.b.G;
-  if (nq <= 0 || nq > kFewRowsMost || rows > kFewRowsMost) return;
-  const int len = uniform(kv_len_of(a.b, r)), from = uniform(first_of(a, r)), key1 = (int)min((int64_t)len, chunk0 + a.chunk);
-  if (key0 >= key1 || key1 <= from) return;
-  if (tid < kFewRowsMost) {
-    const int t = min(tid, rows - 1) / a.b.G, g = min(tid, rows - 1) - t * a.b.G;
-    const float x = a.lse[(int64_t)(q0 + t) * a.b.Hq + head * a.b.G + g];
-    row_lse[tid] = x * kLog2e;
-    row_limit[tid] = tid < rows ? limit_of(a, len, nq, t, x) : 0;
-  }
-  u32x4 qf[KS];
-  auto queries = [&](int rb) __attribute__((always_inline)) {
-    const int row = min(rb * 16 + l16, rows - 1), t = row / a.b.G, g = row - t * a.b.G;
-    const uint16_t* p = a.q + (q0 + t) * a.b.q_st + (head * a.b.G + g) * a.b.q_sh;
+  if constexpr (EVEN) {
+    __shared__ int64_t wave_sum[kMassWaves];
+    __shared__ int found[2];
+    const int n = a.b.n_seqs, per = (n + kMassThreads - 1) / kMassThreads, r0 = min(tid * per, n), r1 = min(r0 + per, n);
+    int64_t mine = 0;
+    for (int i = r0; i < r1; ++i) mine += mass_strips<STRIP>(a, i);
+    int64_t incl = mine;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks)              // an 8-bit piece of a key is the fragments of two steps
-      qf[ks] = *reinterpret_cast<const u32x4*>(p + (FP8 ? (ks >> 1) * 64 + quarter * 16 + (ks & 1) * 8 : ks * 32 + quarter * 8));
-  };
-  queries(0);
-  __syncthreads();
-  const int blocks = uniform((rows + 15) >> 4);
+    for (int off = 1; off < 64; off <<= 1) {
+      const int64_t y = __shfl_up(incl, off);
+      if (lane >= off) incl += y;
+    }
+    if (lane == 63) wave_sum[wave] = incl;
+    __syncthreads();
+    int64_t before = incl - mine, per_head = 0;
+#pragma unroll
+    for (int w = 0; w < kMassWaves; ++w) {
+      if (w < wave) before += wave_sum[w];
+      per_head += wave_sum[w];
+    }
+    per_head = uniform(per_head);
+    const int64_t total = per_head * a.b.Hkv, shares = uniform(min((int64_t)a.few_shares, total)), share = blockIdx.x;
+    if (share >= shares) return;
+    const int64_t at_strip = uniform(share * total / shares);
+    left = uniform((share + 1) * total / shares) - at_strip;
+    head = uniform((int)(at_strip / per_head));
+    int64_t at = at_strip - head * per_head - before;
+    if (at >= 0 && at < mine) {                                  // one thread has it
+      int i = r0;
+      for (int w = mass_strips<STRIP>(a, i); at >= w; w = mass_strips<STRIP>(a, i)) { at -= w; ++i; }
+      found[0] = i; found[1] = (int)at;
+    }
+    __syncthreads();
+    r = uniform(found[0]); strip = uniform(found[1]);
+  } else {
+    // chunk by chunk, all requests and heads of one: short requests lack the later ones
+    const int items = a.b.n_seqs * a.b.Hkv, turn = blockIdx.x / items, item = blockIdx.x - turn * items;
+    r = item / a.b.Hkv; head = item - r * a.b.Hkv;
+    key0 = (int)min((int64_t)turn * a.chunk, (int64_t)a.b.max_kv);
+    table = a.b.table + (int64_t)r * a.b.table_width;
+    look_up(page, key0 + wave * KEYS, a.b.max_kv);
+    look_up(next_page, key0 + (kMassWaves + wave) * KEYS, a.b.max_kv);
+  }
+  for (;;) {
+    if constexpr (EVEN) asm("" : "+v"(l16), "+v"(quarter));         // what follows from them is worked out per piece, not held in registers from piece to piece
+    const int q0 = uniform(a.b.cu_q[r]), nq = uniform(a.b.cu_q[r + 1]) - q0, rows = nq * a.b.G;
+    const int len = uniform(kv_len_of(a.b, r)), from = uniform(first_of(a, r));
+    int key1;
+    if constexpr (EVEN) {
+      const int strips = uniform(mass_strips<STRIP>(a, r)), end = (int)min((int64_t)strips, strip + left), at = from / STRIP;
+      key0 = (at + strip) * STRIP;
+      key1 = (int)min((int64_t)len, (int64_t)(at + end) * STRIP);
+      left -= end - strip;
+      table = a.b.table + (int64_t)r * a.b.table_width;
+      look_up(page, (int64_t)key0 + wave * KEYS, key1);
+      look_up(next_page, (int64_t)key0 + (kMassWaves + wave) * KEYS, key1);
+    } else {
+      if (nq <= 0 || nq > kFewRowsMost || rows > kFewRowsMost) return;
+      key1 = (int)min((int64_t)len, (int64_t)key0 + a.chunk);
+      if (key0 >= key1 || key1 <= from) return;
+    }
+    if (tid < kFewRowsMost) {
+      const int t = min(tid, rows - 1) / a.b.G, g = min(tid, rows - 1) - t * a.b.G;
+      const float x = a.lse[(int64_t)(q0 + t) * a.b.Hq + head * a.b.G + g];
+      row_lse[tid] = x * kLog2e;
+      row_limit[tid] = tid < rows ? limit_of(a, len, nq, t, x) : 0;
+    }
+    u32x4 qf[KS];
+    auto queries = [&](int rb) __attribute__((always_inline)) {
+      const int row = min(rb * 16 + l16, rows - 1), t = row / a.b.G, g = row - t * a.b.G;
+      const uint16_t* p = a.q + (q0 + t) * a.b.q_st + (head * a.b.G + g) * a.b.q_sh;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)              // an 8-bit piece of a key is the fragments of two steps
+        qf[ks] = *reinterpret_cast<const u32x4*>(p + (FP8 ? (ks >> 1) * 64 + quarter * 16 + (ks & 1) * 8 : ks * 32 + quarter * 8));
+    };
+    queries(0);
+    const int blocks = uniform((rows + 15) >> 4);
 
-  const unsigned char* kb = a.pool.k + a.layer + head * a.pool.s_head + quarter * 16;
-  float* sums = a.sums + r * a.s_seq + head * a.s_head;
-  const int in_page = (1 << a.pool.page_log2) - 1;
-  u32x4 kr[CG][LOADS];
-  float old;
-  auto send_for = [&](int tile, const int (&pg)[CG]) __attribute__((always_inline)) {
-    const int j = tile + lane;
-    old = lane < KEYS && j >= from && j < key1 ? old_sum(a, sums, j, len, nq) : 0.0f;
-    int64_t off[CG];
+    const unsigned char* kb = a.pool.k + a.layer + head * a.pool.s_head + quarter * 16;
+    float* sums = a.sums + r * a.s_seq + head * a.s_head;
+    const int in_page = (1 << a.pool.page_log2) - 1;
+    u32x4 kr[CG][LOADS];
+    float old;
+    auto send_for = [&](int tile, const int (&pg)[CG]) __attribute__((always_inline)) {
+      const int j = tile + lane;
+      old = lane < KEYS && j >= from && j < key1 ? old_sum(a, sums, j, len, nq) : 0.0f;
+      int64_t off[CG];
 #pragma unroll
-    for (int g = 0; g < CG; ++g)                 // rows that are not there: page 0, without weight below
-      off[g] = (pg[g] >= 0 && pg[g] < a.pool.n_pages ? pg[g] : 0) * a.pool.s_page + ((tile + 16 * g + l16) & in_page) * (int)a.pool.s_tok;
+      for (int g = 0; g < CG; ++g)                 // rows that are not there: page 0, without weight below
+        off[g] = (pg[g] >= 0 && pg[g] < a.pool.n_pages ? pg[g] : 0) * a.pool.s_page + ((tile + 16 * g + l16) & in_page) * (int)a.pool.s_tok;
 #pragma unroll
-    for (int g = 0; g < CG; ++g)
+      for (int g = 0; g < CG; ++g)
 #pragma unroll
-      for (int i = 0; i < LOADS; ++i) kr[g][i] = *reinterpret_cast<const u32x4*>(kb + off[g] + i * 64);
-  };
-  int tile = key0 + wave * KEYS;
-  while (tile + KEYS <= from && tile < key1) {   // protected rows: the first tile that is not of them alone
-    tile += (from - tile) / STRIP * STRIP;
-    if (tile + KEYS <= from) tile += STRIP;
-    look_up(page, tile, key1);
-    look_up(next_page, (int64_t)tile + STRIP, key1);
-  }
-  if (tile < key1) send_for(tile, page);
-  while (tile < key1) {
-    int limit_key[CG];                           // the key, or one that nothing sees
-#pragma unroll
-    for (int g = 0; g < CG; ++g) limit_key[g] = page[g] >= 0 && page[g] < a.pool.n_pages ? tile + 16 * g + l16 : INT32_MAX;
-    u32x4 kf[CG][KS];
-#pragma unroll
-    for (int g = 0; g < CG; ++g)
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        if constexpr (FP8) kf[g][ks] = ks & 1 ? widen8(kr[g][ks >> 1].z, kr[g][ks >> 1].w) : widen8(kr[g][ks >> 1].x, kr[g][ks >> 1].y);
-        else kf[g][ks] = kr[g][ks];
-      }
-    const float before = old;
-    const int next = tile + STRIP;
-#pragma unroll
-    for (int g = 0; g < CG; ++g) page[g] = next_page[g];
-    if (next < key1) {
-      send_for(next, page);
-      look_up(next_page, (int64_t)next + STRIP, key1);
+        for (int i = 0; i < LOADS; ++i) kr[g][i] = *reinterpret_cast<const u32x4*>(kb + off[g] + i * 64);
+    };
+    int tile = key0 + wave * KEYS;
+    while (tile + KEYS <= from && tile < key1) {   // protected rows: the first tile that is not of them alone
+      tile += (from - tile) / STRIP * STRIP;
+      if (tile + KEYS <= from) tile += STRIP;
+      look_up(page, tile, key1);
+      look_up(next_page, (int64_t)tile + STRIP, key1);
     }
-    float sum[CG];
+    if (tile < key1) send_for(tile, page);
+    __syncthreads();
+    while (tile < key1) {
+      int limit_key[CG];                           // the key, or one that nothing sees
 #pragma unroll
-    for (int g = 0; g < CG; ++g) sum[g] = 0.0f;
-    for (int rb = 0; rb < blocks; ++rb) {
-      if (blocks > 1) queries(rb);
-      f32x4 s[CG];
+      for (int g = 0; g < CG; ++g) limit_key[g] = page[g] >= 0 && page[g] < a.pool.n_pages ? tile + 16 * g + l16 : INT32_MAX;
+      u32x4 kf[CG][KS];
+#pragma unroll
+      for (int g = 0; g < CG; ++g)
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          if constexpr (FP8) kf[g][ks] = ks & 1 ? widen8(kr[g][ks >> 1].z, kr[g][ks >> 1].w) : widen8(kr[g][ks >> 1].x, kr[g][ks >> 1].y);
+          else kf[g][ks] = kr[g][ks];
+        }
+      const float before = old;
+      const int64_t next = (int64_t)tile + STRIP;
+#pragma unroll
+      for (int g = 0; g < CG; ++g) page[g] = next_page[g];
+      if (next < key1) {
+        send_for((int)next, page);
+        look_up(next_page, next + STRIP, key1);
+      }
+      float sum[CG];
+#pragma unroll
+      for (int g = 0; g < CG; ++g) sum[g] = 0.0f;
+      for (int rb = 0; rb < blocks; ++rb) {
+        if (blocks > 1) queries(rb);
+        f32x4 s[CG];
+#pragma unroll
+        for (int g = 0; g < CG; ++g) {
+          s[g] = f32x4{0, 0, 0, 0};
+#pragma unroll
+          for (int ks = 0; ks < KS; ++ks) s[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(qf[ks]), frag(kf[g][ks]), s[g], 0, 0, 0);
+        }
+        const f32x4 l = *reinterpret_cast<const f32x4*>(row_lse + rb * 16 + quarter * 4);
+        const int4 limit = *reinterpret_cast<const int4*>(row_limit + rb * 16 + quarter * 4);
+#pragma unroll
+        for (int g = 0; g < CG; ++g) {
+          float w[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_exp2f(fmaf(s[g][i], a.c, -l[i]));
+          sum[g] += (limit_key[g] < limit.x ? w[0] : 0.0f) + (limit_key[g] < limit.y ? w[1] : 0.0f);
+          sum[g] += (limit_key[g] < limit.z ? w[2] : 0.0f) + (limit_key[g] < limit.w ? w[3] : 0.0f);
+        }
+      }
+      float mine = 0.0f;
 #pragma unroll
       for (int g = 0; g < CG; ++g) {
-        s[g] = f32x4{0, 0, 0, 0};
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) s[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(frag(qf[ks]), frag(kf[g][ks]), s[g], 0, 0, 0);
+        float x = sum[g] + __shfl_xor(sum[g], 16);
+        x += __shfl_xor(x, 32);
+        if (quarter == g) mine = x;
       }
-      const f32x4 l = *reinterpret_cast<const f32x4*>(row_lse + rb * 16 + quarter * 4);
-      const int4 limit = *reinterpret_cast<const int4*>(row_limit + rb * 16 + quarter * 4);
-#pragma unroll
-      for (int g = 0; g < CG; ++g) {
-        float w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = __builtin_amdgcn_exp2f(fmaf(s[g][i], a.c, -l[i]));
-        sum[g] += (limit_key[g] < limit.x ? w[0] : 0.0f) + (limit_key[g] < limit.y ? w[1] : 0.0f);
-        sum[g] += (limit_key[g] < limit.z ? w[2] : 0.0f) + (limit_key[g] < limit.w ? w[3] : 0.0f);
-      }
+      const int j = tile + lane;
+      if (lane < KEYS && j >= from && j < key1) sums[j] = fmaf(a.decay, before, a.share * mine);
+      tile = (int)min(next, (int64_t)key1);
     }
-    float mine = 0.0f;
-#pragma unroll
-    for (int g = 0; g < CG; ++g) {
-      float x = sum[g] + __shfl_xor(sum[g], 16);
-      x += __shfl_xor(x, 32);
-      if (quarter == g) mine = x;
+    if constexpr (!EVEN) return;
+    if (left <= 0) break;
+    strip = 0;
+    for (++r;;) {                                                  // the next request with strips, or the first one of the next head: 64 at a time
+      const uint64_t some = __ballot(r + lane < a.b.n_seqs && mass_strips<STRIP>(a, min(r + lane, a.b.n_seqs - 1)) > 0);
+      if (some != 0) { r += __builtin_ctzll(some); break; }
+      r += 64;
+      if (r >= a.b.n_seqs) { r = 0; ++head; }
     }
-    const int j = tile + lane;
-    if (lane < KEYS && j >= from && j < key1) sums[j] = fmaf(a.decay, before, a.share * mine);
-    tile = next;
+    __syncthreads();                                               // through with LDS
   }
 }
 
@@ -500,6 +572,8 @@ __global__ __launch_bounds__(2 * kMassKeys) void mass_join_kernel(const MassArgs
   sums[j] = fmaf(a.decay, old_sum(a, sums, j, of.len, of.nq), a.share * (sum_of[0][key] + sum_of[1][key]));
 }
 
+constexpr int64_t kMassEvenBytes = 1 << 24;
+constexpr int kMassFewShares = 1024;
 constexpr int kMassShares = 256;                 // a workgroup for each compute unit
 constexpr int64_t kMostBlocks = (1 << 24) - 1;    // of 256 threads: an axis of a grid holds 2^32 threads
 
@@ -519,11 +593,13 @@ int make_mass_plan(const codecomp_batch* b, const codecomp_pages* p, const codec
   }
   const int64_t items = (int64_t)x.n_seqs * x.Hkv;
   int64_t chunk = (items * x.max_kv / 2048 + 255) / 256 * 256;
-  chunk = std::min<int64_t>(std::max<int64_t>(chunk, 256), 2048);
+  chunk = std::min<int64_t>(std::max<int64_t>(chunk, 256), 512);
   while (items * ((x.max_kv + chunk - 1) / chunk) > kMostBlocks && chunk < x.max_kv) chunk *= 2;
   pl->chunk = (int)std::min<int64_t>(chunk, 1 << 30);
   pl->chunks = (int)((x.max_kv + chunk - 1) / chunk);
-  if (pl->few_rows > 0 && items * pl->chunks > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
+  const int64_t bytes = (int64_t)pl->few_rows * x.Hkv * x.max_kv * p->head_dim * (pl->pool.fp8 ? 1 : 2);
+  pl->shares = bytes > kMassEvenBytes ? kMassFewShares : 0;
+  if (pl->few_rows > 0 && pl->shares == 0 && items * pl->chunks > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
   pl->ws_bytes = pl->many_rows > 0 && x.max_kv > 0 ? kMassShares * (2 * kMassKeys * sizeof(float) + sizeof(CutKeys)) : 0;
   return CODECOMP_OK;
 }
@@ -533,7 +609,8 @@ static int launch_mass_of(const MassPlan& pl, const MassArgs& a, hipStream_t str
   const int64_t items = (int64_t)pl.batch.n_seqs * pl.batch.Hkv;
   const dim3 block(kMassThreads);
   if (pl.few_rows > 0) {
-    mass_few_kernel<D, FP8><<<dim3((unsigned)(items * pl.chunks)), block, 0, stream>>>(a);
+    if (pl.shares > 0) mass_few_kernel<D, FP8, true><<<dim3((unsigned)pl.shares), block, 0, stream>>>(a);
+    else mass_few_kernel<D, FP8, false><<<dim3((unsigned)(items * pl.chunks)), block, 0, stream>>>(a);
     if (hipError_t e = hipGetLastError()) return (int)e;
   }
   if (pl.many_rows > 0) {
@@ -554,7 +631,7 @@ int launch_mass(const MassPlan& pl, const void* q, const float* lse, int layer, 
   a.c = fminf(fmaxf(pl.scale * pl.pool.k_scale * kLog2e, FLT_MIN), FLT_MAX);
   a.decay = decay; a.share = 1.0f / pl.batch.G;
   a.cuts = reinterpret_cast<CutKeys*>(a.part + 2 * kMassShares * kMassKeys);
-  a.chunk = pl.chunk; a.shares = kMassShares;
+  a.chunk = pl.chunk; a.shares = kMassShares; a.few_shares = pl.shares;
   if (pl.d == 128) return pl.pool.fp8 ? launch_mass_of<128, true>(pl, a, stream) : launch_mass_of<128, false>(pl, a, stream);
   return pl.pool.fp8 ? launch_mass_of<64, true>(pl, a, stream) : launch_mass_of<64, false>(pl, a, stream);
 }

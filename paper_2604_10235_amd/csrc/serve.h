@@ -36,7 +36,8 @@ struct MassPlan {
   int d;
   float scale;
   int few_rows, many_rows;     // requests of each kind (mass.hip)
-  int chunk, chunks;           // few rows: keys of a workgroup, and workgroups for a request and head
+  int chunk, chunks;           // few rows: keys of a workgroup, and workgroups for a request and head,
+  int shares;                  // or (not 0) equal parts of the keys of all requests and heads
   size_t ws_bytes;
 };
 int make_mass_plan(const codecomp_batch* b, const codecomp_pages* p, const codecomp_mass* m, MassPlan* plan);
