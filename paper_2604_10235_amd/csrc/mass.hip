@@ -67,7 +67,8 @@ __device__ __forceinline__ int mass_strips(const MassArgs& a, int r) {
 }
 
 // EVEN: the strips of all requests and heads form one sequence, cut into equal parts; else a workgroup has one chunk of a request.
-template <int D, bool FP8, bool EVEN>
+// ROWWISE: pages of less than 16 rows; else 16 rows of a tile lie in one page, whose place is worked out in scalar registers.
+template <int D, bool FP8, bool EVEN, bool ROWWISE>
 __global__ __launch_bounds__(kMassThreads, 4) void mass_few_kernel(const MassArgs a) {
   constexpr int LOADS = D * (FP8 ? 1 : 2) / 64, KS = D / 32, CG = D == 128 ? 2 : 4, KEYS = 16 * CG, STRIP = kMassWaves * KEYS;
   __shared__ __attribute__((aligned(16))) float row_lse[kFewRowsMost];
@@ -81,7 +82,11 @@ __global__ __launch_bounds__(kMassThreads, 4) void mass_few_kernel(const MassArg
   int page[CG], next_page[CG];
   auto look_up = [&](int (&pg)[CG], int64_t tile, int end) __attribute__((always_inline)) {
 #pragma unroll
-    for (int g = 0; g < CG; ++g) pg[g] = table[max((int)min(tile + 16 * g + l16, (int64_t)end - 1), 0) >> a.pool.page_log2];
+    for (int g = 0; g < CG; ++g) {
+      const int at = max((int)min(tile + 16 * g + (ROWWISE ? l16 : 0), (int64_t)end - 1), 0) >> a.pool.page_log2;
+      if constexpr (ROWWISE) pg[g] = table[at];
+      else pg[g] = ((const __attribute__((address_space(4))) int32_t*)table)[at];
+    }
   };
   if constexpr (EVEN) {
     __shared__ int64_t wave_sum[kMassWaves];
@@ -161,9 +166,10 @@ __global__ __launch_bounds__(kMassThreads, 4) void mass_few_kernel(const MassArg
     queries(0);
     const int blocks = uniform((rows + 15) >> 4);
 
-    const unsigned char* kb = a.pool.k + a.layer + head * a.pool.s_head + quarter * 16;
+    const unsigned char* kb = a.pool.k + a.layer + head * a.pool.s_head;
     float* sums = a.sums + r * a.s_seq + head * a.s_head;
     const int in_page = (1 << a.pool.page_log2) - 1;
+    const uint32_t lane_off = quarter * 16 + (ROWWISE ? 0 : l16 * (uint32_t)a.pool.s_tok);
     u32x4 kr[CG][LOADS];
     float old;
     auto send_for = [&](int tile, const int (&pg)[CG]) __attribute__((always_inline)) {
@@ -172,11 +178,11 @@ __global__ __launch_bounds__(kMassThreads, 4) void mass_few_kernel(const MassArg
       int64_t off[CG];
 #pragma unroll
       for (int g = 0; g < CG; ++g)                 // rows that are not there: page 0, without weight below
-        off[g] = (pg[g] >= 0 && pg[g] < a.pool.n_pages ? pg[g] : 0) * a.pool.s_page + ((tile + 16 * g + l16) & in_page) * (int)a.pool.s_tok;
+        off[g] = (pg[g] >= 0 && pg[g] < a.pool.n_pages ? pg[g] : 0) * a.pool.s_page + ((tile + 16 * g + (ROWWISE ? l16 : 0)) & in_page) * (int)a.pool.s_tok;
 #pragma unroll
       for (int g = 0; g < CG; ++g)
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) kr[g][i] = *reinterpret_cast<const u32x4*>(kb + off[g] + i * 64);
+        for (int i = 0; i < LOADS; ++i) kr[g][i] = *reinterpret_cast<const u32x4*>(kb + off[g] + lane_off + i * 64);
     };
     int tile = key0 + wave * KEYS;
     while (tile + KEYS <= from && tile < key1) {   // protected rows: the first tile that is not of them alone
@@ -609,8 +615,14 @@ static int launch_mass_of(const MassPlan& pl, const MassArgs& a, hipStream_t str
   const int64_t items = (int64_t)pl.batch.n_seqs * pl.batch.Hkv;
   const dim3 block(kMassThreads);
   if (pl.few_rows > 0) {
-    if (pl.shares > 0) mass_few_kernel<D, FP8, true><<<dim3((unsigned)pl.shares), block, 0, stream>>>(a);
-    else mass_few_kernel<D, FP8, false><<<dim3((unsigned)(items * pl.chunks)), block, 0, stream>>>(a);
+    const dim3 even((unsigned)pl.shares), chunks((unsigned)(items * pl.chunks));
+    if (pl.pool.page_log2 < 4) {
+      if (pl.shares > 0) mass_few_kernel<D, FP8, true, true><<<even, block, 0, stream>>>(a);
+      else mass_few_kernel<D, FP8, false, true><<<chunks, block, 0, stream>>>(a);
+    } else {
+      if (pl.shares > 0) mass_few_kernel<D, FP8, true, false><<<even, block, 0, stream>>>(a);
+      else mass_few_kernel<D, FP8, false, false><<<chunks, block, 0, stream>>>(a);
+    }
     if (hipError_t e = hipGetLastError()) return (int)e;
   }
   if (pl.many_rows > 0) {
