@@ -31,7 +31,7 @@ struct SharedRows {
   const int32_t* prefix_lens;
   int n_groups, max_prefix, max_own;
   int few_units, few_parts, few_chunk, few_splits;       // shared rows of groups of few rows: workgroups, parts of the rows, keys of a chunk, chunks
-  int many_units, many_blocks, many_tiles, many_splits;  // of many: workgroups, most blocks of rows of a group, tiles of a chunk, chunks
+  int many_units, many_tiles, many_splits;               // of many: workgroups, tiles of a chunk, chunks
   int splits;                  // the larger one: parts of shared rows that every row has
   int join;                    // 1: whoever has a request's own rows joins the parts of the shared ones to them, and writes the outputs
 };

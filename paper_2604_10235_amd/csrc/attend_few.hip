@@ -181,7 +181,7 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void atten
       look_up(page, key0 + wave * kFewKeys, key1);
       look_up(next_page, key0 + (kFewWaves + wave) * kFewKeys, key1);
     } else if constexpr (SHARED) {
-      key1 = key_end;
+      key1 = causal ? min(key_end, len - nq + (min(row0 + 16 * RB, rows) - 1) / a.b.G + 1) : key_end;       // nothing behind what the last row sees
       whole = shared_join;
     } else {
       if (rows <= row0 || rows > a.row_slots) return;

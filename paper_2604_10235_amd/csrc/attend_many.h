@@ -218,18 +218,34 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
     // Blocks of rows of one chunk side by side, on one die: they read the same keys.
     const int on_die = (ma.sh.many_units + 7) / 8, unit = (int)(blockIdx.x & 7) * on_die + (int)(blockIdx.x >> 3);
     if ((int)(blockIdx.x >> 3) >= on_die || unit >= ma.sh.many_units) return;
-    block = unit % ma.sh.many_blocks;
-    int rest = unit / ma.sh.many_blocks;
-    g = rest % ma.sh.many_splits;                                  // number of the part
-    rest /= ma.sh.many_splits;
-    head = rest % a.b.Hkv;
-    const int group = rest / a.b.Hkv, end = ma.sh.cu_groups[group + 1];
+    // its group: 64 of them at a time are asked for their blocks
+    int group = -1, rest = unit;
+    for (int g0 = 0; group < 0 && g0 < ma.sh.n_groups; g0 += 64) {
+      const int at = min(g0 + lane, ma.sh.n_groups - 1), q0 = a.b.cu_q[ma.sh.cu_groups[at]], nq = a.b.cu_q[ma.sh.cu_groups[at + 1]] - q0;
+      const int units = g0 + lane < ma.sh.n_groups ? blocks_of(ma, 0, q0, nq).count * ma.sh.many_splits * a.b.Hkv : 0;
+      int upto = units;
+#pragma unroll
+      for (int off = 1; off < 64; off <<= 1) {
+        const int y = __shfl_up(upto, off);
+        if (lane >= off) upto += y;
+      }
+      const uint64_t reached = __ballot(upto > rest);
+      if (reached == 0) { rest -= __shfl(upto, 63); continue; }
+      const int owner = __builtin_ctzll(reached);
+      group = g0 + owner;
+      rest -= __shfl(upto - units, owner);
+      of = blocks_of(ma, 0, __shfl(q0, owner), __shfl(nq, owner));
+    }
+    if (group < 0) return;
+    group = uniform(group); rest = uniform(rest);
     r = ma.sh.cu_groups[group];
-    if (r >= end) return;
-    of = blocks_of(ma, prefix_of(ma.sh, group), a.b.cu_q[r], a.b.cu_q[end] - a.b.cu_q[r]);
+    of.len = prefix_of(ma.sh, group);
     of = uniform(of);
     of.causal = 0;
-    if (block >= of.count) return;
+    block = rest % of.count;
+    rest /= of.count;
+    g = rest % ma.sh.many_splits;                                 // number of the part
+    head = rest / ma.sh.many_splits;
     const int tiles = (of.len + kManyKeys - 1) / kManyKeys;
     chunk_tile0 = g * ma.sh.many_tiles;
     chunk_tile1 = min(tiles, chunk_tile0 + ma.sh.many_tiles);

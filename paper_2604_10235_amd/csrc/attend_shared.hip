@@ -24,6 +24,7 @@ extern template int launch_many_shared_of<128, true>(const ManyArgs&, hipStream_
 constexpr int kChip = 256;                       // compute units: workgroups of the kernel for many rows that run at once
 constexpr int64_t kMostBlocks = (1 << 23) - 1;    // of up to 512 threads: an axis of a grid holds 2^32 threads
 constexpr int kMostSplits = 1024;
+constexpr int kFewChunk = 2048;
 constexpr int kJoinParts = 6;
 constexpr int64_t kJoinRows = 16384;
 constexpr int kJoinKeys = 512;
@@ -45,14 +46,13 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
   s = SharedRows{};
   s.cu_groups = g->cu_groups_dev; s.prefix_lens = g->prefix_lens_dev;
   s.n_groups = g->n_groups; s.max_prefix = g->max_prefix_len; s.max_own = g->max_own_len;
-  int64_t few_most = 0, many_most = 0, blocks = 0, own_most = 0;
+  int64_t few_most = 0, blocks = 0, own_most = 0;
   pl->few_groups = pl->many_groups = 0;
   for (int i = 0; i < g->n_groups; ++i) {
     const int64_t rows = (int64_t)(b->cu_q_host[g->cu_groups_host[i + 1]] - b->cu_q_host[g->cu_groups_host[i]]) * x.G;
     if (rows > kFewRowsMost) {
       ++pl->many_groups;
       blocks += (rows + kManyRows - 1) / kManyRows;
-      many_most = std::max(many_most, rows);
     } else if (rows > 0) {
       ++pl->few_groups;
       few_most = std::max(few_most, rows);
@@ -60,9 +60,9 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
   }
   for (int r = 0; r < x.n_seqs; ++r) own_most = std::max(own_most, (int64_t)(b->cu_q_host[r + 1] - b->cu_q_host[r]) * x.G);
   blocks *= x.Hkv;
-  const int64_t items = (int64_t)x.n_seqs * x.Hkv;
+  const int64_t items = (int64_t)x.n_seqs * x.Hkv, own_parts = (own_most + 31) / 32;
   // Where one workgroup has all own rows of a request's head, it joins the parts of the shared ones to them as well.
-  s.join = s.max_own <= kJoinKeys || items >= kJoinItems;
+  s.join = s.max_own <= kJoinKeys || items * own_parts >= kJoinItems;
   pl->few_two = s.join ? few_most > 16 : std::max(few_most, own_most) > 16;
   pl->own_two = s.join ? own_most > 16 : pl->few_two;
   const int few_each = pl->few_two ? 32 : 16, own_each = pl->own_two ? 32 : 16;
@@ -71,23 +71,21 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
   s.many_splits = s.few_splits = 0;
   if (pl->many_groups > 0) {
     const int tiles = std::max(1, (s.max_prefix + kManyKeys - 1) / kManyKeys);
-    s.many_blocks = (int)((many_most + kManyRows - 1) / kManyRows);
-    const int64_t grid = (int64_t)s.n_groups * x.Hkv * s.many_blocks;       // with a place for blocks that a group does not have
-    if (grid > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
+    if (blocks > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
     int best = 1;
     double least = 0.0;
-    for (int n = 1; n <= std::min(tiles, kChip) && grid * n <= kMostBlocks; ++n) {
-      const int each = (tiles + n - 1) / n;
-      const double time = (double)((blocks * n + kChip - 1) / kChip) * (each + 4) + 0.02 * n;
+    for (int n = 1; n <= std::min(tiles, kChip) && blocks * n <= kMostBlocks; ++n) {
+      const int64_t rounds = ((blocks * n + 7) / 8 + kChip / 8 - 1) / (kChip / 8);       // of a die's compute units
+      const double time = (double)rounds * ((tiles + n - 1) / n + 5) + 0.02 * n;
       if (n == 1 || time < least) { best = n; least = time; }
     }
     s.many_tiles = (tiles + best - 1) / best;
     s.many_splits = (tiles + s.many_tiles - 1) / s.many_tiles;
-    s.many_units = (int)(grid * s.many_splits);
+    s.many_units = (int)(blocks * s.many_splits);
   }
-  auto cut = [&](int64_t items, int most, int* chunk, int* splits) {
+  auto cut = [&](int64_t items, int most, int64_t largest, int* chunk, int* splits) {
     int64_t keys = (items * most / 512 + 127) / 128 * 128;
-    keys = std::min<int64_t>(std::max<int64_t>(keys, 128), 2048);
+    keys = std::min<int64_t>(std::max<int64_t>(keys, 128), largest);
     while ((most + keys - 1) / keys > kMostSplits || (items * ((most + keys - 1) / keys) > kMostBlocks && keys < most)) keys *= 2;
     *chunk = (int)std::min<int64_t>(keys, 1 << 30);
     *splits = (int)((most + keys - 1) / keys);
@@ -97,7 +95,7 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
   int64_t few_units = 0;
   if (pl->few_groups > 0) {
     const int64_t units = (int64_t)s.n_groups * x.Hkv * s.few_parts;
-    cut((int64_t)pl->few_groups * x.Hkv * s.few_parts, s.max_prefix, &s.few_chunk, &s.few_splits);
+    cut((int64_t)pl->few_groups * x.Hkv * s.few_parts, s.max_prefix, kFewChunk, &s.few_chunk, &s.few_splits);
     s.few_splits = std::max(s.few_splits, 1);
     few_units = units * s.few_splits;
     if (few_units > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
@@ -111,7 +109,7 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
     pl->chunk = s.max_own;
     pl->own_splits = 1;
   } else {
-    cut(items * pl->row_parts, s.max_own, &pl->chunk, &pl->own_splits);
+    cut(items * pl->row_parts, s.max_own, 2048, &pl->chunk, &pl->own_splits);
   }
   pl->own_units = items * pl->row_parts * pl->own_splits;
   if (pl->own_units + few_units > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
