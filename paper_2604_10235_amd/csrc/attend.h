@@ -30,6 +30,7 @@ struct SharedRows {
   const int32_t* cu_groups;
   const int32_t* prefix_lens;
   int n_groups, max_prefix, max_own;
+  int few_rows;                // rows of a group up to which the kernel for few rows has its shared rows
   int few_units, few_parts, few_chunk, few_splits;       // shared rows of groups of few rows: workgroups, parts of the rows, keys of a chunk, chunks
   int many_units, many_tiles, many_splits;               // of many: workgroups, tiles of a chunk, chunks
   int splits;                  // the larger one: parts of shared rows that every row has

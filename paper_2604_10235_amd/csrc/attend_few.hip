@@ -47,6 +47,49 @@ __device__ __forceinline__ int strips_of(const AttendArgs& a, int r) {
   return rows <= 0 || rows > a.row_slots ? 0 : max(1, (kv_len_of(a.b, r) + kFewStrip - 1) / kFewStrip);
 }
 
+// 16 rows of a request's own keys, from row0 on, joined to the parts of the shared ones: D / 4 threads a row.  Parts come from memory (other dies wrote them):
+// as many as registers hold are sent for at a time, and the reference moves on from one lot to the next.
+template <int D>
+__device__ __forceinline__ void join_rows(const SharedArgs& a, const float (&own_o)[16][D], const float (&own_ml)[16][2], int q0, int head, int row0, int rows) {
+  constexpr int THREADS = D / 4, LOT = 16;
+  const int e = threadIdx.x % THREADS * 4;
+  for (int n = threadIdx.x / THREADS; n < 16; n += 64 * kFewWaves / THREADS) {
+    const int row = row0 + n, t = row / a.b.G, h = head * a.b.G + row - t * a.b.G;
+    if (row >= rows) return;
+    const int64_t at = part_at(a, 0, q0 + t, h), step = (int64_t)a.b.T * a.b.Hq;
+    float top = own_ml[n][0], all = own_ml[n][1];
+    f32x4 x = *reinterpret_cast<const f32x4*>(&own_o[n][e]);
+    for (int p0 = 0; p0 < a.sh.splits; p0 += LOT) {
+      f32x4 v[LOT];
+      float m[LOT], l[LOT], to = top;
+#pragma unroll
+      for (int i = 0; i < LOT; ++i) {
+        const int64_t part = at + min(p0 + i, a.sh.splits - 1) * step;
+        m[i] = a.part_ml[2 * part];
+        l[i] = p0 + i < a.sh.splits ? a.part_ml[2 * part + 1] : kNoPart;
+        v[i] = *reinterpret_cast<const f32x4*>(a.part_o + part * D + e);
+      }
+#pragma unroll
+      for (int i = 0; i < LOT; ++i) to = fmaxf(to, l[i] == kNoPart ? -INFINITY : m[i]);
+      const float old = to == top ? 1.0f : __builtin_amdgcn_exp2f(top - to);
+      top = to;
+      x *= old;
+      all *= old;
+#pragma unroll
+      for (int i = 0; i < LOT; ++i) {
+        const float f = m[i] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m[i] - to);       // times zeros, or an infinity or NaN that it saw
+        const bool some = l[i] != kNoPart;
+        all += some ? f * l[i] : 0.0f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] += some ? f * v[i][k] : 0.0f;
+      }
+    }
+    const float inv = all == 0.0f ? 0.0f : a.pool.v_scale / all;
+    *reinterpret_cast<u32x2*>(a.out + (q0 + t) * a.b.o_st + h * a.b.o_sh + e) = u32x2{pack2(x.x * inv, x.y * inv), pack2(x.z * inv, x.w * inv)};
+    if (a.lse && e == 0) a.lse[at] = all == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(all)) * kLn2;
+  }
+}
+
 // EVEN: the strips of all requests and heads form one sequence, cut into equal parts; else a workgroup has one chunk of a request, or (SHARED) of the rows that
 // a group shares, or of a request's rows behind them, and leaves parts of all rows.
 template <int D, bool FP8, int RB, bool EVEN, bool SHARED = false>
@@ -55,6 +98,7 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void atten
   constexpr int KS = D / 32, DB = D / 16;
   __shared__ __attribute__((aligned(16))) unsigned char lds[kFewWaves * T::BYTES];
   __shared__ float row_m[kFewWaves][16], row_l[kFewWaves][16];
+  __shared__ __attribute__((aligned(16))) float own_o[SHARED ? 16 : 1][D], own_ml[SHARED ? 16 : 1][2];       // what the workgroup joins the shared rows' parts to
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   int l16 = lane & 15, quarter = lane >> 4;
   int r, head, row0, key0, share = 0, strip = 0;                 // request, head, first of this workgroup's rows, first of its keys
@@ -124,7 +168,7 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void atten
       if (r >= end) return;
       shared_q0 = a.b.cu_q[r];
       shared_nq = a.b.cu_q[end] - shared_q0;
-      if (shared_nq > kFewRowsMost || shared_nq * a.b.G > kFewRowsMost || shared_nq * a.b.G <= row0) return;
+      if (shared_nq * a.b.G > a.sh.few_rows || shared_nq * a.b.G <= row0) return;
       shared_len = uniform(prefix_of(a.sh, g));
       key0 = split * a.sh.few_chunk;
       key_end = key0 + a.sh.few_chunk;
@@ -393,16 +437,6 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void atten
         float to = -INFINITY;
 #pragma unroll
         for (int w = 0; w < kFewWaves; ++w) to = fmaxf(to, row_m[w][n]);
-        int64_t shared_row = 0, shared_rows = 0;
-        if constexpr (SHARED) {
-          if (shared_join) {                                      // parts' references: the 16 threads of a row take them in turn
-            shared_row = part_at(a, 0, q0 + row / a.b.G, head * a.b.G + row % a.b.G);
-            shared_rows = (int64_t)a.b.T * a.b.Hq;
-            for (int p = tid & 15; p < a.sh.splits; p += 16) to = fmaxf(to, a.part_ml[2 * (p * shared_rows + shared_row)]);
-#pragma unroll
-            for (int off = 1; off < 16; off <<= 1) to = fmaxf(to, __shfl_xor(to, off));
-          }
-        }
         float all = 0.0f, x[E];
 #pragma unroll
         for (int i = 0; i < E; ++i) x[i] = 0.0f;
@@ -413,25 +447,11 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void atten
 #pragma unroll
           for (int i = 0; i < E; ++i) x[i] += f * o_lds[(w * 16 + n) * O_ROW + e + i];
         }
-        if constexpr (SHARED) {
-          if (shared_join) {
-#pragma unroll 8
-            for (int p = 0; p < a.sh.splits; ++p) {
-              const int64_t part = p * shared_rows + shared_row;
-              const float pm = a.part_ml[2 * part], pl = a.part_ml[2 * part + 1];
-              const bool some = pl != kNoPart;
-              const float f = some && pm != -INFINITY ? __builtin_amdgcn_exp2f(pm - to) : 0.0f;
-              if (some) all += f * pl;
+        if (SHARED && whole) {                                     // joined below
 #pragma unroll
-              for (int i = 0; i < E; i += 4) {
-                const f32x4 v = *reinterpret_cast<const f32x4*>(a.part_o + part * D + e + i);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) x[i + k] += some ? f * v[k] : 0.0f;
-              }
-            }
-          }
-        }
-        if (whole) {
+          for (int i = 0; i < E; ++i) own_o[n][e + i] = x[i];
+          if ((tid & 15) == 0) { own_ml[n][0] = to; own_ml[n][1] = all; }
+        } else if (whole) {
           const int t = row / a.b.G, h = head * a.b.G + row - t * a.b.G;
           const float inv = all == 0.0f ? 0.0f : a.pool.v_scale / all;
           uint16_t* out = a.out + (q0 + t) * a.b.o_st + h * a.b.o_sh + e;
@@ -443,6 +463,12 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void atten
 #pragma unroll
           for (int i = 0; i < E; i += 4) *reinterpret_cast<f32x4*>(a.part_o + part * D + e + i) = f32x4{x[i], x[i + 1], x[i + 2], x[i + 3]};
           if ((tid & 15) == 0) { a.part_ml[2 * part] = to; a.part_ml[2 * part + 1] = all; }
+        }
+      }
+      if constexpr (SHARED) {
+        if (shared_join) {
+          __syncthreads();
+          join_rows<D>(a, own_o, own_ml, q0, head, row0 + rb * 16, rows);
         }
       }
     }

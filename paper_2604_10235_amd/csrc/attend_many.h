@@ -549,8 +549,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
           }
         }
       };
-      if constexpr (SHARED) walk(std::false_type{});
-      else if (__builtin_expect(of.rows > kFewRowsMost, 1)) walk(std::false_type{});
+      if (__builtin_expect(of.rows > kFewRowsMost, 1)) walk(std::false_type{});
       else walk(std::true_type{});
       if (active) {
         if (__builtin_expect(partly(tile1 - 1) && not_finite != 0, 0)) {

@@ -24,6 +24,8 @@ extern template int launch_many_shared_of<128, true>(const ManyArgs&, hipStream_
 constexpr int kChip = 256;                       // compute units: workgroups of the kernel for many rows that run at once
 constexpr int64_t kMostBlocks = (1 << 23) - 1;    // of up to 512 threads: an axis of a grid holds 2^32 threads
 constexpr int kMostSplits = 1024;
+constexpr int kFewRows = 32;
+constexpr int64_t kFewKeys8 = INT64_MAX, kFewKeys16 = 1 << 17;
 constexpr int kFewChunk = 2048;
 constexpr int kJoinParts = 6;
 constexpr int64_t kJoinRows = 16384;
@@ -48,9 +50,15 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
   s.n_groups = g->n_groups; s.max_prefix = g->max_prefix_len; s.max_own = g->max_own_len;
   int64_t few_most = 0, blocks = 0, own_most = 0;
   pl->few_groups = pl->many_groups = 0;
+  int middle = 0;                                  // groups of more than 32 rows that either kernel can take
   for (int i = 0; i < g->n_groups; ++i) {
     const int64_t rows = (int64_t)(b->cu_q_host[g->cu_groups_host[i + 1]] - b->cu_q_host[g->cu_groups_host[i]]) * x.G;
-    if (rows > kFewRowsMost) {
+    middle += rows > kFewRows && rows <= kFewRowsMost;
+  }
+  s.few_rows = (int64_t)middle * x.Hkv * s.max_prefix > (pl->pool.fp8 ? kFewKeys8 : kFewKeys16) ? kFewRows : kFewRowsMost;
+  for (int i = 0; i < g->n_groups; ++i) {
+    const int64_t rows = (int64_t)(b->cu_q_host[g->cu_groups_host[i + 1]] - b->cu_q_host[g->cu_groups_host[i]]) * x.G;
+    if (rows > s.few_rows) {
       ++pl->many_groups;
       blocks += (rows + kManyRows - 1) / kManyRows;
     } else if (rows > 0) {
@@ -190,7 +198,7 @@ int launch_shared(const SharedPlan& pl, const void* q, int layer, void* out, flo
     ManyArgs m = {};
     m.a = a;
     m.sh = a.sh;
-    m.rows_from = kFewRowsMost + 1;
+    m.rows_from = a.sh.few_rows + 1;
     int rc;
     if (pl.d == 128) rc = pl.pool.fp8 ? launch_many_shared_of<128, true>(m, stream) : launch_many_shared_of<128, false>(m, stream);
     else rc = pl.pool.fp8 ? launch_many_shared_of<64, true>(m, stream) : launch_many_shared_of<64, false>(m, stream);
