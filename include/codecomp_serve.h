@@ -34,7 +34,7 @@ extern "C" {
 typedef struct codecomp_groups {
   int32_t n_groups;                /* 1 .. 65535                                                                  */
   int32_t max_prefix_len;          /* HOST bound of prefix_lens, 0 .. the batch's max_kv_len: sizes launches and workspace, as does */
-  int32_t max_own_len;             /* HOST bound of the rows behind the shared ones, kv_lens[r] - prefix_lens[g], 0 .. the batch's max_kv_len: rows beyond it are not read */
+  int32_t max_own_len;             /* HOST bound of the rows behind the shared ones, 0 .. the batch's max_kv_len: kv_lens[r] is cut to prefix_lens[g] + max_own_len */
   const int32_t* cu_groups_host;   /* [n_groups + 1] HOST, from 0 to n_seqs, not decreasing                        */
   const int32_t* cu_groups_dev;    /* [n_groups + 1] DEVICE copy of the same values                                */
   const int32_t* prefix_lens_dev;  /* [n_groups], cut to [0, max_prefix_len]                                       */

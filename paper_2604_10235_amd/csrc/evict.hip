@@ -242,6 +242,7 @@ __global__ __launch_bounds__(THREADS) void evict_kernel(const EvictArgs a) {
   const Span s = span_of(a, r);
   keep_rows<THREADS, PER>(a, s, layer, r, head);
   if (s.m == s.n - s.f) return;
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // the numbers of the kept rows are where the others read them
   __syncthreads();
   unsigned char* const pool[2] = {a.pool.k, a.pool.v};
   close_up<PIECES, THREADS, kBothDeep, 2>(a, s, layer, r, head, pool, 0);
