@@ -24,17 +24,20 @@ __device__ __forceinline__ Span span_of(const EvictArgs& a, int r) {
   return s;
 }
 
-// Floats as unsigned numbers of the same order; -0 as 0, NaN below all.
+// Floats as unsigned numbers of the same order, from 1 on; -0 as 0, NaN below all.
 __device__ __forceinline__ unsigned ordered(float x) {
   const unsigned u = __float_as_uint(x + 0.0f);
-  return x != x ? 0u : u & 0x80000000u ? ~u : u | 0x80000000u;
+  return x != x ? 1u : u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// A thread has PER rows in registers; a request that has more is read again for the rest of them, as often as they are looked at.
+// A thread has PER rows in registers, as numbers in the order in which rows stay: 0 for what is no row, the largest for the last `recent` ones.  A request that has
+// more rows is read again for the rest of them, as often as they are looked at.
 template <int THREADS, int PER>
 __device__ __forceinline__ void keep_rows(const EvictArgs& a, const Span s, int layer, int r, int head) {
-  constexpr int WAVES = THREADS / 64, COPIES = 4, ENTRIES = WAVES * PER;
-  __shared__ __attribute__((aligned(16))) int counts[4][COPIES][256];       // of a digit's values, for each of the four digits
+  constexpr int WAVES = THREADS / 64, ENTRIES = WAVES * PER;
+  // Counts of a digit's values, for each of the four digits.  Of the first one, which mostly is one of a handful, every value has eight, side by side, which lanes
+  // take in turn: additions of a wave to one of them wait for one another.
+  __shared__ __attribute__((aligned(16))) int counts[(8 + 1 + 1 + 1) * 256];
   __shared__ int2 before[ENTRIES];                        // rows above the border and at it: of a wave's strip, then of all before it
   __shared__ int2 strip[2][WAVES];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -43,39 +46,52 @@ __device__ __forceinline__ void keep_rows(const EvictArgs& a, const Span s, int 
   float* to = a.to.sums + layer * a.to.s_layer + r * a.to.s_seq + head * a.to.s_head + s.f;
   int32_t* kept = a.kept + (((int64_t)layer * a.n_seqs + r) * a.Hkv + head) * a.max_budget;
   const bool all = s.m == s.n - s.f;
-  const int last = all ? s.f : s.n - a.recent;           // rows from there on stay
-  for (int i = tid; i < 4 * COPIES * 256; i += THREADS) (&counts[0][0][0])[i] = 0;
-  float x[PER];
+  const int last = s.n - a.recent;                       // rows from there on stay
+  auto key_of = [&](int j) __attribute__((always_inline)) { return j >= s.n ? 0u : all || j >= last ? ~0u : ordered(sums[j]); };
+  unsigned key[PER] = {};
+  if (s.n > s.f) {
+    float x[PER];
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int j = s.f + i * THREADS + tid;
-    x[i] = j < s.n ? sums[j] : 0.0f;
+    for (int i = 0; i < PER; ++i) x[i] = sums[min(s.f + i * THREADS + tid, s.n - 1)];
+    for (int i = tid; i < 11 * 64; i += THREADS) reinterpret_cast<int4*>(counts)[i] = int4{0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int j = s.f + i * THREADS + tid;
+      key[i] = j >= s.n ? 0u : all || j >= last ? ~0u : ordered(x[i]);
+    }
   }
   const int beyond = s.f + PER * THREADS;                // first row that is in no register
-  unsigned border = all ? 0 : ~0u;                       // rows above it stay, and the first `equal` of those at it
+  unsigned border = 0;                                   // rows above it stay, and the first `equal` of those at it
   int equal = 0;
   __syncthreads();
-  if (!all && s.m > a.recent) {
-    unsigned prefix = 0;
-    int want = s.m - a.recent;
+  if (!all && s.m > 0) {
+    int want = s.m;
 #pragma unroll
     for (int digit = 0; digit < 4; ++digit) {
       const int shift = 24 - 8 * digit;
-      int* count = counts[digit][wave % COPIES];
-      auto look = [&](float v) __attribute__((always_inline)) {
-        const unsigned key = ordered(v);
-        if (digit == 0 || key >> ((shift + 8) & 31) == prefix) atomicAdd(&count[(key >> shift) & 255], 1);
+      constexpr int kAt[4] = {0, 8, 9, 10};
+      int* count = counts + kAt[digit] * 256;
+      auto look = [&](unsigned k) __attribute__((always_inline)) {
+        const int value = (k >> shift) & 255;
+        if (digit == 0) atomicAdd(&count[value * 8 + (lane & 7)], 1);
+        else if (k >> ((shift + 8) & 31) == border) atomicAdd(&count[value], 1);
       };
 #pragma unroll
-      for (int i = 0; i < PER; ++i)
-        if (s.f + i * THREADS + tid < last) look(x[i]);
-      for (int j = beyond + tid; j < last; j += THREADS) look(sums[j]);
+      for (int i = 0; i < PER; ++i) look(key[i]);
+      for (int j = beyond + tid; j < s.n; j += THREADS) look(key_of(j));
       __syncthreads();
-      int4 of = {0, 0, 0, 0};                            // four digits a lane, the largest first; every wave for itself
+      int4 of;                                           // four values a lane, the largest first; every wave for itself
+      if (digit == 0) {
+        int y[4];
 #pragma unroll
-      for (int c = 0; c < COPIES; ++c) {
-        const int4 y = *reinterpret_cast<const int4*>(&counts[digit][c][252 - 4 * lane]);
-        of.x += y.w; of.y += y.z; of.z += y.y; of.w += y.x;
+        for (int v = 0; v < 4; ++v) {
+          const int4 lo = *reinterpret_cast<const int4*>(&count[(255 - 4 * lane - v) * 8]), hi = *reinterpret_cast<const int4*>(&count[(255 - 4 * lane - v) * 8 + 4]);
+          y[v] = ((lo.x + lo.y) + (lo.z + lo.w)) + ((hi.x + hi.y) + (hi.z + hi.w));
+        }
+        of = int4{y[0], y[1], y[2], y[3]};
+      } else {
+        const int4 y = *reinterpret_cast<const int4*>(&count[252 - 4 * lane]);
+        of = int4{y.w, y.z, y.y, y.x};
       }
       int above = of.x + of.y + of.z + of.w;
       const int mine = above;
@@ -90,30 +106,22 @@ __device__ __forceinline__ void keep_rows(const EvictArgs& a, const Span s, int 
       if (left > of.x) { left -= of.x; --at;
         if (left > of.y) { left -= of.y; --at;
           if (left > of.z) { left -= of.z; --at; } } }
-      prefix = prefix << 8 | (unsigned)__shfl(at, owner);
+      border = border << 8 | (unsigned)__shfl(at, owner);
       want = __shfl(left, owner);
     }
-    border = prefix;
     equal = want;
+  } else if (!all) {
+    border = ~0u;
   }
-  auto kind = [&](int j, float v, bool& more, bool& same) __attribute__((always_inline)) {
-    const unsigned key = ordered(v);
-    more = j < s.n && (j >= last || key > border);
-    same = j < last && key == border;
-  };
-  const uint64_t below = ((uint64_t)1 << lane) - 1;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    bool more, same;
-    kind(s.f + i * THREADS + tid, x[i], more, same);
-    const uint64_t m = __ballot(more), e = __ballot(same);
+    const uint64_t m = __ballot(key[i] > border), e = __ballot(key[i] == border);
     if (lane == 0) before[i * WAVES + wave] = make_int2(__popcll(m), __popcll(e));
   }
-  __syncthreads();                                       // all sums that are in registers have been read as well
-  int2 sum = {0, 0};
+  __syncthreads();
   if (wave == 0) {
     constexpr int EACH = (ENTRIES + 63) / 64;
-    int2 own[EACH];
+    int2 own[EACH], sum = {0, 0};
 #pragma unroll
     for (int i = 0; i < EACH; ++i) {
       own[i] = lane * EACH + i < ENTRIES ? before[lane * EACH + i] : make_int2(0, 0);
@@ -134,33 +142,27 @@ __device__ __forceinline__ void keep_rows(const EvictArgs& a, const Span s, int 
     if (lane == 63) strip[0][0] = upto;
   }
   __syncthreads();
-  auto keep = [&](int j, float v, bool more, bool same, int m, int e) __attribute__((always_inline)) {
-    if (more || (same && e < equal)) {
-      const int i = m + min(e, equal);
-      kept[i] = j;
-      to[i] = v;
-    }
+  auto keep = [&](int j, bool more, bool same, int m, int e) __attribute__((always_inline)) {
+    if (more || (same && e < equal)) kept[m + min(e, equal)] = j;
   };
+  const uint64_t below = ((uint64_t)1 << lane) - 1;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    bool more, same;
-    const int j = s.f + i * THREADS + tid;
-    kind(j, x[i], more, same);
+    const bool more = key[i] > border, same = key[i] == border;
     const uint64_t m = __ballot(more), e = __ballot(same);
     const int2 b = before[i * WAVES + wave];
-    keep(j, x[i], more, same, b.x + __popcll(m & below), b.y + __popcll(e & below));
+    keep(s.f + i * THREADS + tid, more, same, b.x + __popcll(m & below), b.y + __popcll(e & below));
   }
   if (beyond < s.n) {
     int above = strip[0][0].x, at_border = strip[0][0].y;
     __syncthreads();
     for (int first = beyond, turn = 0; first < s.n; first += THREADS, turn ^= 1) {
       const int j = first + tid;
-      const float v = j < s.n ? sums[j] : 0.0f;
-      bool more, same;
-      kind(j, v, more, same);
+      const unsigned k = key_of(j);
+      const bool more = k > border, same = k == border;
       const uint64_t more_mask = __ballot(more), same_mask = __ballot(same);
       if (lane == 0) strip[turn][wave] = make_int2(__popcll(more_mask), __popcll(same_mask));
-      __syncthreads();                                   // all sums of the strip have been read
+      __syncthreads();
       int m = above + __popcll(more_mask & below), e = at_border + __popcll(same_mask & below);
 #pragma unroll
       for (int w = 0; w < WAVES; ++w) {
@@ -168,10 +170,26 @@ __device__ __forceinline__ void keep_rows(const EvictArgs& a, const Span s, int 
         if (w < wave) { m += c.x; e += c.y; }
         above += c.x; at_border += c.y;
       }
-      keep(j, v, more, same, m, e);
+      keep(j, more, same, m, e);
     }
   }
   for (int i = s.m + tid; i < a.max_budget; i += THREADS) kept[i] = -1;
+  // The kept rows' sums, in lots: all of one have been read before any is written, and those of later ones stand behind what it writes.
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // the numbers of the kept rows are where the others read them
+  __syncthreads();
+  constexpr int LOT = 2;
+  for (int first = 0; first < s.m; first += LOT * THREADS) {
+    float v[LOT];
+#pragma unroll
+    for (int i = 0; i < LOT; ++i) {
+      const int at = first + i * THREADS + tid;
+      v[i] = at < s.m ? sums[kept[at]] : 0.0f;
+    }
+    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < LOT; ++i)
+      if (first + i * THREADS + tid < s.m) to[first + i * THREADS + tid] = v[i];
+  }
 }
 
 // Rows move together, DEEP pieces of 16 bytes of a pool a thread at a time.  PIECES: of a row that a workgroup moves; POOLS: one pool, or K and V.
@@ -242,8 +260,6 @@ __global__ __launch_bounds__(THREADS) void evict_kernel(const EvictArgs a) {
   const Span s = span_of(a, r);
   keep_rows<THREADS, PER>(a, s, layer, r, head);
   if (s.m == s.n - s.f) return;
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // the numbers of the kept rows are where the others read them
-  __syncthreads();
   unsigned char* const pool[2] = {a.pool.k, a.pool.v};
   close_up<PIECES, THREADS, kBothDeep, 2>(a, s, layer, r, head, pool, 0);
 }
