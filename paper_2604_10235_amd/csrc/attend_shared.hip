@@ -70,7 +70,7 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
   blocks *= x.Hkv;
   const int64_t items = (int64_t)x.n_seqs * x.Hkv, own_parts = (own_most + 31) / 32;
   // Where one workgroup has all own rows of a request's head, it joins the parts of the shared ones to them as well.
-  s.join = s.max_own <= kJoinKeys || items * own_parts >= kJoinItems;
+  s.join = pl->many_groups > 0 && (s.max_own <= kJoinKeys || items * own_parts >= kJoinItems);
   pl->few_two = s.join ? few_most > 16 : std::max(few_most, own_most) > 16;
   pl->own_two = s.join ? own_most > 16 : pl->few_two;
   const int few_each = pl->few_two ? 32 : 16, own_each = pl->own_two ? 32 : 16;

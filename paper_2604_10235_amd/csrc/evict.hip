@@ -8,9 +8,9 @@
 
 namespace codecomp {
 
-constexpr int kMoveDeep = 8;                             // pieces of 16 bytes that a thread has in flight
+constexpr int kMoveDeep = 2;                             // pieces of 16 bytes that a thread has in flight
 constexpr int kBothDeep = 4, kBothThreads = 512;
-constexpr int kFewest = 256;
+constexpr int kFewest = 256, kFewer = 64;
 constexpr int kManyProblems = 1024;
 constexpr int kFewMoves = 1024;                          // workgroups up to which they are of 1024 threads, not 256
 constexpr int64_t kMostBlocks = (1 << 22) - 1;          // of up to 1024 threads: an axis of a grid holds 2^32 threads
@@ -194,7 +194,7 @@ __device__ __forceinline__ void keep_rows(const EvictArgs& a, const Span s, int 
 
 // Rows move together, DEEP pieces of 16 bytes of a pool a thread at a time.  PIECES: of a row that a workgroup moves; POOLS: one pool, or K and V.
 template <int PIECES, int THREADS, int DEEP, int POOLS>
-__device__ __forceinline__ void close_up(const EvictArgs& a, const Span s, int layer, int r, int head, unsigned char* const (&pool)[POOLS], int slice) {
+__device__ __forceinline__ void close_up(const EvictArgs& a, int layer, int r, int head, unsigned char* const (&pool)[POOLS], int slice) {
   constexpr int ROWS = THREADS / PIECES;
   const int tid = threadIdx.x;
   const int64_t base = layer * a.pool.s_layer + head * a.pool.s_head + (slice * PIECES + tid % PIECES) * 16;
@@ -205,6 +205,15 @@ __device__ __forceinline__ void close_up(const EvictArgs& a, const Span s, int l
     const int page = table[row >> a.pool.page_log2];
     return page < 0 || page >= a.pool.n_pages ? (int64_t)-1 : page * a.pool.s_page + (row & in_page) * a.pool.s_tok;
   };
+  // Numbers of the first batch's rows are sent for before it is known how many there are: one wait less; -1 where there is none.
+  int row[DEEP];
+  auto numbers = [&](int first) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < DEEP; ++u) row[u] = kept[min(first + u * ROWS + tid / PIECES, a.max_budget - 1)];
+  };
+  numbers(0);
+  const Span s = span_of(a, r);
+  if (s.m == s.n - s.f) return;
   for (int first = 0; first < s.m; first += ROWS * DEEP) {
     u32x4 x[DEEP][POOLS];
     int64_t to[DEEP];
@@ -214,18 +223,16 @@ __device__ __forceinline__ void close_up(const EvictArgs& a, const Span s, int l
       to[u] = -1;
 #pragma unroll
       for (int p = 0; p < POOLS; ++p) x[u][p] = u32x4{0, 0, 0, 0};
-      if (i < s.m) {
-        const int row = kept[i];
-        if (row != s.f + i) {                            // else it stays where it is
-          const int64_t from = place(row);
-          to[u] = place(s.f + i);
-          if (from >= 0) {
+      if (i < s.m && row[u] != s.f + i) {                // else it stays where it is
+        const int64_t from = place(row[u]);
+        to[u] = place(s.f + i);
+        if (from >= 0) {
 #pragma unroll
-            for (int p = 0; p < POOLS; ++p) x[u][p] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(pool[p] + base + from));
-          }
+          for (int p = 0; p < POOLS; ++p) x[u][p] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(pool[p] + base + from));
         }
       }
     }
+    numbers(first + ROWS * DEEP);
     // All rows of the batch are in registers before one is overwritten; rows of later batches lie behind those that this one writes.
     asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
 #pragma unroll
@@ -247,10 +254,8 @@ template <int PIECES, int THREADS>
 __global__ __launch_bounds__(THREADS) void close_up_kernel(const EvictArgs a, int slices) {
   const int part = blockIdx.x % (2 * slices), problem = blockIdx.x / (2 * slices);
   const int head = problem % a.Hkv, rest = problem / a.Hkv, r = rest % a.n_seqs;
-  const Span s = span_of(a, r);
-  if (s.m == s.n - s.f) return;
   unsigned char* const pool[1] = {part & 1 ? a.pool.v : a.pool.k};
-  close_up<PIECES, THREADS, kMoveDeep, 1>(a, s, rest / a.n_seqs, r, head, pool, part >> 1);
+  close_up<PIECES, THREADS, kMoveDeep, 1>(a, rest / a.n_seqs, r, head, pool, part >> 1);
 }
 
 // Both, for many problems: what one workgroup waits for while it finds its border is hidden behind the rows of others.
@@ -259,9 +264,8 @@ __global__ __launch_bounds__(THREADS) void evict_kernel(const EvictArgs a) {
   const int head = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv, r = rest % a.n_seqs, layer = rest / a.n_seqs;
   const Span s = span_of(a, r);
   keep_rows<THREADS, PER>(a, s, layer, r, head);
-  if (s.m == s.n - s.f) return;
   unsigned char* const pool[2] = {a.pool.k, a.pool.v};
-  close_up<PIECES, THREADS, kBothDeep, 2>(a, s, layer, r, head, pool, 0);
+  close_up<PIECES, THREADS, kBothDeep, 2>(a, layer, r, head, pool, 0);
 }
 
 template <int PIECES>
@@ -275,7 +279,7 @@ int launch_evict(const EvictArgs& a, int d, hipStream_t stream) {
   const int64_t problems = (int64_t)a.n_layers * a.n_seqs * a.Hkv;
   const int pieces = d * (a.pool.fp8 ? 1 : 2) / 16;
   int slices = 1;
-  while (slices < pieces / 8 && problems * 2 * slices < kFewest) slices *= 2;
+  while (problems * 2 * slices < (slices < pieces / 8 ? kFewest : slices < pieces / 2 ? kFewer : 0)) slices *= 2;
   if (problems * 2 * slices > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
   if (problems >= kManyProblems && a.max_kv <= 8192) {
     const dim3 grid((unsigned)problems), block(kBothThreads);
@@ -291,7 +295,8 @@ int launch_evict(const EvictArgs& a, int d, hipStream_t stream) {
   switch (pieces / slices) {
     case 16: launch_close_up<16>(a, problems, slices, stream); break;
     case 8: launch_close_up<8>(a, problems, slices, stream); break;
-    default: launch_close_up<4>(a, problems, slices, stream); break;
+    case 4: launch_close_up<4>(a, problems, slices, stream); break;
+    default: launch_close_up<2>(a, problems, slices, stream); break;
   }
   return (int)hipGetLastError();
 }
