@@ -16,7 +16,7 @@
  *
  * Everything said at the heads of codecomp.h and codecomp_cache.h holds here as well: device pointers unless the name ends in _host, nothing is
  * allocated, nothing synchronises, work goes to `hip_stream`, calls are re-entrant and deterministic, a rejected call has enqueued nothing, device data is
- * not validated, what a corrupt table, length, budget or group can do is bounded.  Calls may be captured into a graph; lengths, budgets,
+ * not validated, what a corrupt table, length or budget can do is bounded.  Calls may be captured into a graph; lengths, budgets,
  * tables and tokens may then change between replays (what has a copy on the host may not).
  */
 #ifndef CODECOMP_SERVE_H

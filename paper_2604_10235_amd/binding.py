@@ -629,7 +629,7 @@ def make_mass(sums) -> codecomp_mass:
     for stride, n in sorted((s, n) for n, s in zip(sums.shape, sums.stride()) if n > 1):
         if stride < extent:
             raise ValueError(f"sums must not overlap (strides {sums.stride()})")
-        extent = stride * n
+        extent += stride * (n - 1)
     m.sums = sums.data_ptr()
     m.n_layers, m.n_seqs, m.n_kv_heads, m.width = sums.shape
     m._keep, m._at = sums, sums.get_device()

@@ -120,8 +120,7 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
     cut(items * pl->row_parts, s.max_own, 2048, &pl->chunk, &pl->own_splits);
   }
   pl->own_units = items * pl->row_parts * pl->own_splits;
-  if (pl->own_units + few_units > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
-  if (!s.join && (int64_t)x.T * x.Hq >= (1 << 24)) return CODECOMP_EINVAL_SHAPE;       // workgroups of the joining kernel
+  if (pl->own_units + few_units > kMostBlocks) return CODECOMP_EINVAL_SHAPE;        // with which the kernel that joins has less than 2^27 rows, 8 or more a workgroup
   pl->ws_bytes = x.T == 0 ? 0 : ((size_t)(s.splits + (s.join ? 0 : pl->own_splits)) * x.T * x.Hq * (p->head_dim + 2) * sizeof(float) + 255) & ~(size_t)255;
   return CODECOMP_OK;
 }

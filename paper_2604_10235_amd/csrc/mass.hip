@@ -600,12 +600,10 @@ int make_mass_plan(const codecomp_batch* b, const codecomp_pages* p, const codec
   const int64_t items = (int64_t)x.n_seqs * x.Hkv;
   int64_t chunk = (items * x.max_kv / 2048 + 255) / 256 * 256;
   chunk = std::min<int64_t>(std::max<int64_t>(chunk, 256), 512);
-  while (items * ((x.max_kv + chunk - 1) / chunk) > kMostBlocks && chunk < x.max_kv) chunk *= 2;
-  pl->chunk = (int)std::min<int64_t>(chunk, 1 << 30);
+  pl->chunk = (int)chunk;
   pl->chunks = (int)((x.max_kv + chunk - 1) / chunk);
   const int64_t bytes = (int64_t)pl->few_rows * x.Hkv * x.max_kv * p->head_dim * (pl->pool.fp8 ? 1 : 2);
-  pl->shares = bytes > kMassEvenBytes ? kMassFewShares : 0;
-  if (pl->few_rows > 0 && pl->shares == 0 && items * pl->chunks > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
+  pl->shares = bytes > kMassEvenBytes || items * pl->chunks > kMostBlocks ? kMassFewShares : 0;
   pl->ws_bytes = pl->many_rows > 0 && x.max_kv > 0 ? kMassShares * (2 * kMassKeys * sizeof(float) + sizeof(CutKeys)) : 0;
   return CODECOMP_OK;
 }

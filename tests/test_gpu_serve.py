@@ -258,6 +258,88 @@ def test_shared_without_tokens_and_many_groups():
     check_shared(f)
 
 
+# requests that have their groups' tables, and no new tokens; groups of 33 to 64 rows under a loose bound (weights of 16 bits in the kernel for many rows); own rows that are joined
+# in one workgroup although there are many of them
+@pytest.mark.parametrize("members, prefixes, news, own, n_q, n_kv, d, page, bounds", [
+    ([3, 30], [140, 333], [0, 1, 2] + [0] + [1] * 29, 9, 8, 2, 64, 16, {}),
+    ([9], [700], [1] * 9, 40, 28, 4, 128, 32, dict(max_kv=70000, max_prefix=60000, max_own=300)),
+    ([16, 10, 3], [65, 700, 90], [4] * 16 + [4] * 10 + [4] * 3, 60, 8, 8, 64, 8, dict(max_kv=70000, max_prefix=60000, max_own=9000)),
+    ([60], [300], [1] * 60, 1500, 16, 4, 64, 64, {}), ([60], [300], [2] * 60, 700, 32, 4, 128, 16, dict(max_kv=9000, max_own=3000))])
+@pytest.mark.parametrize("causal", [True, False])
+def test_shared_kinds_of_groups(members, prefixes, news, own, n_q, n_kv, d, page, bounds, causal):
+    rng = np.random.default_rng([47, own, page])
+    owns = [max(n, int(x)) for n, x in zip(news, rng.integers(0, own, sum(members)))]
+    more = (bounds.get("max_kv", 0)) // page
+    check_shared(Forked(rng, members, prefixes, news, owns, n_q=n_q, n_kv=n_kv, d=d, page=page, width_more=more), causal=causal, **bounds)
+
+
+def test_shared_pool_with_strides_of_its_own():
+    rng = np.random.default_rng(48)
+    f = Forked(rng, [3, 30], [140, 333], [1, 3, 2] + [1] * 30, [7] * 33, n_q=8, n_kv=2, d=64, page=16, layers=2)
+    dense, lse = check_shared(f, layer=1)
+    f.cache.k, f.cache.v = (t.permute(1, 3, 0, 2, 4).contiguous().permute(2, 0, 3, 1, 4) for t in (f.cache.k, f.cache.v))
+    again, lse2 = check_shared(f, layer=1)
+    assert torch.equal(again, dense) and torch.equal(lse, lse2)
+
+
+@pytest.mark.parametrize("members", [[3], [30], [2, 28]])
+def test_shared_two_graphs_and_two_streams(members):
+    """Graphs replayed one after the other on one workspace; calls at the same time on workspaces of their own."""
+    rng = np.random.default_rng([49, members[0]])
+    n = sum(members)
+    fs = [Forked(rng, members, [500 + 33 * g for g in range(len(members))], [1] * n, [70] * n, n_q=8, n_kv=2, d=64, page=16) for _ in range(2)]
+    want = [check_shared(f) for f in fs]
+    calls = [(f.batch(), f.cache.pages(), f.groups()) for f in fs]
+    shared = shared_workspace(calls[0][0], calls[0][2], calls[0][1])[0]
+    alone = [shared_workspace(x, g, p)[0] for x, p, g in calls]
+    outs, lses, graphs = [torch.empty_like(f.q) for f in fs], [torch.empty(f.T, 8, device="cuda") for f in fs], [torch.cuda.CUDAGraph() for _ in fs]
+    torch.cuda.synchronize()
+    for i, (x, p, g) in enumerate(calls):
+        with torch.cuda.graph(graphs[i]):
+            b.codecomp_attend_shared(fs[i].q, x, g, p, 0, outs[i], shared, lse=lses[i])
+    for turn in range(6):
+        outs[turn % 2].fill_(9.0)
+        graphs[turn % 2].replay()
+        assert torch.equal(outs[turn % 2], want[turn % 2][0]) and torch.equal(lses[turn % 2], want[turn % 2][1])
+    streams = [torch.cuda.Stream() for _ in fs]
+    torch.cuda.synchronize()
+    for turn in range(20):
+        for i, (x, p, g) in enumerate(calls):
+            with torch.cuda.stream(streams[i]):
+                outs[i].fill_(9.0)
+                b.codecomp_attend_shared(fs[i].q, x, g, p, 0, outs[i], alone[i], lse=lses[i])
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert torch.equal(outs[i], want[i][0]) and torch.equal(lses[i], want[i][1])
+
+
+def far_away(cache):
+    """The same rows where offsets are beyond 2^32 bytes and elements: in the last pages of a pool of 2^33 elements, and in its second layer."""
+    n = cache.n_pages
+    _, _, h, page, d = cache.k.shape
+    more = 2**32 // (h * page * d) + 1
+    big = [torch.empty((2, more + n, h, page, d), dtype=cache.k.dtype, device="cuda") for _ in range(2)]
+    for to, x in zip(big, (cache.k, cache.v)):
+        to[1, more:] = x[0]
+    cache.k, cache.v = big
+    cache.table = np.where(cache.table >= 0, cache.table + more, -1).astype(np.int32)
+    cache.n_pages += more
+
+
+@pytest.mark.parametrize("members", [[3], [30]])
+@pytest.mark.parametrize("fp8", [False, True])
+def test_shared_offsets_beyond_32_bits(members, fp8):
+    rng = np.random.default_rng([50, members[0]])
+    n = members[0]
+    f = Forked(rng, members, [300], [1] * n, [20] * n, n_q=8, n_kv=2, d=64, page=16, fp8=fp8, wrong_entries=False)
+    near, near_lse = check_shared(f)
+    far_away(f.cache)
+    batch, pages, groups = f.batch(), f.cache.pages(), f.groups()
+    out, lse = torch.empty_like(f.q), torch.empty(f.T, 8, device="cuda")
+    b.codecomp_attend_shared(f.q, batch, groups, pages, 1, out, shared_workspace(batch, groups, pages)[0], lse=lse)
+    assert torch.equal(out, near) and torch.equal(lse, near_lse)
+
+
 # ---------------------------------------------------------------- sums of attention weights
 
 def mass_setup(rng, lens, news, n_q, *, n_kv, d, page, fp8=False, layers=1, first=None, width=None, causal=True, softmax_scale=0.0, max_kv=None, sharp=1.0, width_more=0):
@@ -428,6 +510,149 @@ def test_mass_captured_strided_and_on_another_stream(news):
     assert bool((wide[:, :, 0] == 0).all()) and bool((wide[..., :7] == 0).all()) and bool((wide[..., 450:] == 0).all())
 
 
+@pytest.mark.parametrize("lens, news, n_q, n_kv, d, page, fp8, first", [
+    ([3000, 5, 0, 1500, 64, 700], [1, 1, 1, 0, 5, 2], 8, 2, 128, 16, False, [130, 0, 5, 0, 64, -3]), ([3000, 5, 0, 1500, 64, 700], [1, 1, 1, 0, 5, 2], 8, 2, 64, 4, True, [1, 4, 0, 9, 0, 513]),
+    ([3000, 5, 0, 1500, 64, 700], [1, 1, 1, 0, 5, 2], 12, 2, 64, 64, True, None), ([2100, 40, 777], [3, 2, 4], 14, 2, 128, 1, False, [2099, 41, 12]),
+    ([23, 0, 41, 7] * 75, [1, 1, 2, 1] * 75, 8, 8, 128, 16, False, None), ([23, 0, 41, 7] * 75, [1, 1, 0, 3] * 75, 8, 8, 64, 8, False, [3, 1, 32, 7] * 75),
+    ([9000, 4001], [1, 2], 8, 8, 128, 32, True, [0, 257])])
+def test_mass_of_few_rows_in_equal_shares(lens, news, n_q, n_kv, d, page, fp8, first):
+    """A bound on lengths under which there may be many keys: strips of all requests and heads in a row, several of them for a workgroup, or few."""
+    rng = np.random.default_rng([56, len(lens), n_q, page])
+    check_mass(rng, lens, news, n_q, n_kv=n_kv, d=d, page=page, fp8=fp8, first=first, decay=0.5, max_kv=70000, width=70000, width_more=70000 // page + 1)
+
+
+def test_mass_of_a_few_among_very_many_requests():
+    """More requests and heads than a launch has workgroups; those with a token as they would be alone."""
+    rng = np.random.default_rng(62)
+    H, n, who = 1024, 20000, [0, 7000, 19999]
+    k = torch.from_numpy(rng.standard_normal((1, 4, H, 16, 64), dtype=np.float32)).bfloat16().cuda()
+    q, lse = cu_.bf16(rng.standard_normal((3, H, 64))).cuda(), torch.full((3, H), 3.0, device="cuda")
+    pages, sums = b.make_pages(k, k), torch.full((1, n, H, 16), 0.25, device="cuda")
+    lens, table, news = np.full(n, 5), np.zeros((n, 1)), np.zeros(n, int)
+    lens[who], table[who, 0], news[who] = [16, 1, 9], [3, 1, 2], 1
+    make = lambda news, lens, table: b.make_batch(n_q_heads=H, cu_q_host=cum(news), cu_q=dev(cum(news)), kv_lens=dev(lens), table=dev(table), max_kv_len=16)  # noqa: E731
+    b.codecomp_attend_mass(q, lse, make(news, lens, table), pages, 0, b.make_mass(sums), None, decay=0.5)
+    alone = torch.full((1, 3, H, 16), 0.25, device="cuda")
+    b.codecomp_attend_mass(q, lse, make(news[who], lens[who], table[who]), pages, 0, b.make_mass(alone), None, decay=0.5)
+    assert torch.equal(sums[:, who], alone) and not bool((alone[0, 0] == 0.25).any())
+    sums[:, who] = 0.25
+    assert bool((sums == 0.25).all())
+
+
+@pytest.mark.parametrize("d, fp8", [(64, True), (128, False)])
+def test_mass_of_many_short_prompts(d, fp8):
+    """More blocks of keys than workgroups: several for each, of requests and heads one after the other, some without any, and a few rows here and there."""
+    rng = np.random.default_rng([57, d])
+    lens, news = [int(x) for x in rng.integers(34, 80, 220)], [33, 34, 33, 0, 33, 1, 33, 36, 33, 33] * 22
+    check_mass(rng, lens, news, 4, n_kv=2, d=d, page=8, fp8=fp8, first=[0, 5, 0, 0, 0, 0, 90, 0, 33, 1] * 22)
+
+
+@pytest.mark.parametrize("news", [[1, 3], [40, 60]])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+def test_mass_queries_and_sums_of_weights_that_are_no_numbers(news, bad):
+    """A token and head whose log-sum-exp is NaN, or whose query has an infinity or NaN: sums of the rows that it sees are no numbers, others keep their bits."""
+    rng = np.random.default_rng([58, news[0]])
+    c, batch, cu, q, sums = mass_setup(rng, [333, 260], news, 8, n_kv=2, d=64, page=16)
+    pages, m, lse = c.pages(), b.make_mass(sums), torch.full((sum(news), 8), 2.0, device="cuda")
+    ws, _ = mass_workspace(batch, pages, m)
+
+    def call():
+        sums.fill_(0.5)
+        b.codecomp_attend_mass(q, lse, batch, pages, 0, m, ws)
+        return sums.clone()
+
+    clean = call()
+    t, h = news[0], 5                                                  # the second request's first token, of the second KV head
+    sees = 260 - news[1] + 1
+    hit = torch.zeros_like(clean, dtype=torch.bool)
+    hit[0, 1, 1, :sees] = True
+    keep = q[t, h, 3].clone()
+    q[t, h, 3] = bad
+    x = call()
+    q[t, h, 3] = keep
+    assert torch.equal(x[~hit], clean[~hit])
+    if bad != bad:
+        assert bool(torch.isnan(x[hit]).all())
+    else:                                                              # the key's sign says which infinity the logit is: a weight of infinity or of zero
+        assert bool(torch.isinf(x[hit]).any()) and not bool(torch.isnan(x[hit]).any())
+    lse[t, h] = float("nan")
+    x = call()
+    assert bool(torch.isnan(x[hit]).all()) and torch.equal(x[~hit], clean[~hit])
+    lse[t, h] = float("inf")                                          # no weight
+    x = call()
+    lse[t, h] = -float("inf")
+    assert torch.equal(call(), x)
+
+
+@pytest.mark.parametrize("news", [[1, 3, 1], [90, 40, 70]])
+def test_mass_strides_of_queries_and_pool(news):
+    rng = np.random.default_rng([59, news[0]])
+    c, batch, cu, q, sums = mass_setup(rng, [400, 300, 200], news, 8, n_kv=2, d=64, page=16, layers=2)
+    pages, m, lse = c.pages(), b.make_mass(sums), torch.full((sum(news), 8), 2.0, device="cuda")
+    ws, _ = mass_workspace(batch, pages, m)
+    before = sums.clone()
+    b.codecomp_attend_mass(q, lse, batch, pages, 1, m, ws, decay=0.5)
+    want = sums.clone()
+    wide = torch.zeros((9, sum(news), 72), dtype=torch.bfloat16, device="cuda")
+    wide[:8, :, :64] = q.transpose(0, 1)
+    x, _ = cu_.make_batch(c, news, 8, q_stride_tok=72, q_stride_head=72 * sum(news))
+    c.k, c.v = (t.permute(1, 3, 0, 2, 4).contiguous().permute(2, 0, 3, 1, 4) for t in (c.k, c.v))
+    sums.copy_(before)
+    b.codecomp_attend_mass(wide.transpose(0, 1)[:, :8, :64], lse, x, c.pages(), 1, m, ws, decay=0.5)
+    assert torch.equal(sums, want)
+
+
+@pytest.mark.parametrize("news", [[1, 3], [90, 40]])
+@pytest.mark.parametrize("fp8", [False, True])
+def test_mass_offsets_beyond_32_bits(news, fp8):
+    rng = np.random.default_rng([60, news[0]])
+    c, batch, cu, q, sums = mass_setup(rng, [400, 300], news, 8, n_kv=2, d=64, page=16, fp8=fp8)
+    lse = torch.full((sum(news), 8), 2.0, device="cuda")
+    m = b.make_mass(sums)
+    ws, _ = mass_workspace(batch, c.pages(), m)
+    before = sums.clone()
+    b.codecomp_attend_mass(q, lse, batch, c.pages(), 0, m, ws, decay=0.5)
+    far_away(c)
+    batch = cu_.make_batch(c, news, 8)[0]
+    at = torch.empty(2**32 + 2**31 + 2000, device="cuda").as_strided((2, 2, 2, 403), (2**32, 2**31, 1000, 1))
+    at[1] = before[0]
+    b.codecomp_attend_mass(q, lse, batch, c.pages(), 1, b.make_mass(at), ws, decay=0.5)
+    assert torch.equal(at[1], sums[0])
+
+
+def test_mass_two_graphs_and_two_streams():
+    rng = np.random.default_rng(61)
+    news = [90, 2, 70]
+    xs = [mass_setup(rng, [700, 300, 500], news, 8, n_kv=2, d=64, page=16) for _ in range(2)]
+    lse = torch.full((sum(news), 8), 4.0, device="cuda")
+    ms, pages, graphs, want = [b.make_mass(x[4]) for x in xs], [x[0].pages() for x in xs], [torch.cuda.CUDAGraph() for _ in xs], []
+    shared = mass_workspace(xs[0][1], pages[0], ms[0])[0]
+    alone = [mass_workspace(x[1], p, m)[0] for x, p, m in zip(xs, pages, ms)]
+    call = lambda i, ws: b.codecomp_attend_mass(xs[i][3], lse, xs[i][1], pages[i], 0, ms[i], ws, decay=0.0)  # noqa: E731
+    for i in range(2):
+        call(i, shared)
+        want.append(xs[i][4].clone())
+    torch.cuda.synchronize()
+    for i in range(2):
+        with torch.cuda.graph(graphs[i]):
+            call(i, shared)
+    for turn in range(6):
+        xs[turn % 2][4].copy_(want[1 - turn % 2])
+        xs[turn % 2][4][:, :, :, 700:] = want[turn % 2][:, :, :, 700:]
+        for r, n in enumerate([700, 300, 500]):
+            xs[turn % 2][4][:, r, :, n:] = want[turn % 2][:, r, :, n:]
+        graphs[turn % 2].replay()
+        assert torch.equal(xs[turn % 2][4], want[turn % 2])
+    streams = [torch.cuda.Stream() for _ in xs]
+    torch.cuda.synchronize()
+    for turn in range(20):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                call(i, alone[i])
+    torch.cuda.synchronize()
+    assert all(torch.equal(xs[i][4], want[i]) for i in range(2))
+
+
 # ---------------------------------------------------------------- eviction
 
 def evict_setup(rng, lens, budgets, *, n_kv=2, d=64, page=16, fp8=False, layers=2, width=None, values="tail"):
@@ -562,6 +787,116 @@ def test_evict_of_a_long_request_on_another_stream_and_captured():
         target = 1000 + torch.arange(len(at), device="cuda")
         assert torch.equal(rows(work_k, target), rows(k, at)) and torch.equal(work_v, work_k)
         assert torch.equal(to[0, 0, 0, target], sums[0, 0, 0, at])
+
+
+@pytest.mark.parametrize("d, fp8, page, n_kv", [(128, False, 16, 2), (64, True, 8, 4), (64, False, 1, 2), (128, True, 64, 8)])
+@pytest.mark.parametrize("elsewhere", [False, True])
+def test_evict_of_very_many_problems(d, fp8, page, n_kv, elsewhere):
+    """Numbers and rows in one kernel: a workgroup for each of 1024 problems and more; one request has more rows than a workgroup holds."""
+    rng = np.random.default_rng([66, d, page])
+    n = 1024 // (2 * n_kv) + 1
+    lens = [int(x) for x in rng.integers(0, 60, n)]
+    lens[n // 2], lens[3], lens[4] = 5200, 2, 0
+    first = [int(x) for x in rng.integers(-2, 20, n)]
+    budgets = [int(x) for x in rng.integers(0, 40, n)]
+    budgets[n // 2] = 900
+    for values in ("ties", "tail"):
+        check_evict(rng, lens, budgets, recent=5, max_budget=900, first=first, n_kv=n_kv, d=d, page=page, fp8=fp8, layers=2, elsewhere=elsewhere, values=values)
+
+
+def test_evict_largest_and_smallest_numbers():
+    """Budgets, numbers of protected rows and lengths at the ends of their type."""
+    low, high = -(2**31), 2**31 - 1
+    for problems in (1, 520):
+        rng = np.random.default_rng([67, problems])
+        n = 4 * problems
+        check_evict(rng, [90, 33, 90, 90] * problems, [high, low, low, high] * problems, recent=3, max_budget=30, first=[low, 5, high, 80] * problems, n_kv=1, d=64, layers=1 if problems > 1 else 3)
+
+
+def test_evict_strides_of_pool_and_sums():
+    rng = np.random.default_rng(68)
+    c, x = evict_setup(rng, [200, 150], None, layers=2)
+    table, budgets, lens = c.dev_table(), dev([64, 30]), dev([200, 150])
+    kept, new_lens = torch.empty((2, 2, 2, 64), dtype=torch.int32, device="cuda"), torch.empty(2, dtype=torch.int32, device="cuda")
+    e = b.make_eviction(kv_lens=lens, table=table, budgets=budgets, max_kv_len=200, max_budget=64, recent=4)
+    k, v = (t.permute(1, 3, 0, 2, 4).contiguous().permute(2, 0, 3, 1, 4) for t in (c.k, c.v))
+    wide = torch.zeros((2, 2, 2, 300), device="cuda")                    # [requests][heads][layers][rows] in memory
+    sums = wide.permute(2, 0, 1, 3)[..., 7: 7 + x.shape[3]]
+    sums.copy_(torch.from_numpy(x))
+    to = torch.zeros((2, 2, 2, x.shape[3] + 9), device="cuda").permute(1, 0, 2, 3)[..., : x.shape[3]]
+    dense, dense_kept, dense_lens = torch.from_numpy(x).cuda(), torch.empty_like(kept), torch.empty_like(new_lens)
+    b.codecomp_evict(b.make_mass(sums), e, b.make_pages(k, v), kept, new_lens, kept_mass=b.make_mass(to))
+    assert torch.equal(sums, dense)
+    b.codecomp_evict(b.make_mass(dense), e, c.pages(), dense_kept, dense_lens)
+    assert torch.equal(kept, dense_kept) and torch.equal(new_lens, dense_lens) and torch.equal(k, c.k) and torch.equal(v, c.v)
+    for r, n in enumerate(dense_lens.tolist()):
+        assert torch.equal(to[:, r, :, :n], dense[:, r, :, :n])
+    b.codecomp_evict(b.make_mass(sums), e, c.pages(), kept, new_lens)    # in place, strided
+    assert torch.equal(kept, dense_kept) and torch.equal(sums, dense)
+    assert bool((wide[..., :7] == 0).all()) and bool((wide[..., 7 + x.shape[3]:] == 0).all())
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_evict_offsets_beyond_32_bits(fp8):
+    rng = np.random.default_rng([69, fp8])
+    for n in (2, 300):                                                  # two kernels, one
+        c, x = evict_setup(rng, [90] * n, None, fp8=fp8, layers=1)
+        far_away(c)
+        wide = torch.empty(2**32 + 2**31 + 1000 * n, device="cuda")
+        sums = wide.as_strided((2, n, 2, x.shape[3]), (2**32, 200, 2**31, 1))
+        sums[1] = torch.from_numpy(x[0]).cuda()
+        sums[0] = 0
+        kept, lens = torch.empty((2, n, 2, 40), dtype=torch.int32, device="cuda"), torch.empty(n, dtype=torch.int32, device="cuda")
+        e = b.make_eviction(kv_lens=dev([90] * n), table=c.dev_table(), budgets=dev([40] * n), max_kv_len=90, max_budget=40, recent=4)
+        more = c.k.shape[1] - 6 * n - 3
+        was = c.k[1, more:].clone()
+        b.codecomp_evict(b.make_mass(sums), e, c.pages(), kept, lens)
+        want, _ = srv.evict(np.stack([np.zeros_like(x[0]), x[0]]), [90] * n, [40] * n, recent=4, max_budget=40)
+        assert np.array_equal(kept.cpu().numpy(), want)
+        table = torch.from_numpy(c.table).cuda().long()
+        for r in range(0, n, 7):
+            for h in range(2):
+                j = kept[1, r, h].long()
+                i = torch.arange(40, device="cuda")
+                rows = lambda pool, at: pool[table[r, at // 16], h, at % 16]  # noqa: E731
+                assert torch.equal(rows(c.k[1], i), was[table[r, j // 16] - more, h, j % 16])
+                assert torch.equal(sums[1, r, h, :40].cpu(), torch.from_numpy(x[0, r, h])[j.cpu()])
+        del wide, sums, c
+        torch.cuda.empty_cache()
+
+
+def test_evict_twice_at_once():
+    """Two calls at the same time, on caches of their own; and two graphs."""
+    rng = np.random.default_rng(70)
+    xs = []
+    for _ in range(2):
+        c, x = evict_setup(rng, [500, 300], None, layers=2)
+        xs.append((c, x, torch.from_numpy(x).cuda(), c.k.clone(), c.v.clone(), torch.empty((2, 2, 2, 80), dtype=torch.int32, device="cuda"), torch.empty(2, dtype=torch.int32, device="cuda"),
+                   b.make_eviction(kv_lens=dev([500, 300]), table=c.dev_table(), budgets=dev([80, 60]), max_kv_len=500, max_budget=80, recent=4)))
+    call = lambda x: b.codecomp_evict(b.make_mass(x[2]), x[7], x[0].pages(), x[5], x[6])  # noqa: E731
+    reset = lambda x: (x[2].copy_(torch.from_numpy(x[1])), x[0].k.copy_(x[3]), x[0].v.copy_(x[4]), x[5].fill_(-7))  # noqa: E731
+    want, graphs, streams = [], [torch.cuda.CUDAGraph() for _ in xs], [torch.cuda.Stream() for _ in xs]
+    for x in xs:
+        call(x)
+        want.append([t.clone() for t in (x[2], x[0].k, x[0].v, x[5], x[6])])
+        assert np.array_equal(x[5].cpu().numpy(), srv.evict(x[1], [500, 300], [80, 60], recent=4, max_budget=80)[0])
+    same = lambda i: all(torch.equal(t, w) for t, w in zip((xs[i][2], xs[i][0].k, xs[i][0].v, xs[i][5], xs[i][6]), want[i]))  # noqa: E731
+    torch.cuda.synchronize()
+    for g, x in zip(graphs, xs):
+        with torch.cuda.graph(g):
+            call(x)
+    for turn in range(4):
+        reset(xs[turn % 2])
+        graphs[turn % 2].replay()
+        assert same(turn % 2)
+    for x in xs:
+        reset(x)
+    torch.cuda.synchronize()
+    for s, x in zip(streams, xs):
+        with torch.cuda.stream(s):
+            call(x)
+    torch.cuda.synchronize()
+    assert same(0) and same(1)
 
 
 # ---------------------------------------------------------------- together

@@ -175,8 +175,12 @@ def test_calls_without_tokens_do_nothing():
 def test_sizes_beyond_a_launch_are_refused():
     huge = pool(n_kv_heads=4096, n_layers=1)
     x = batch([0] + [1] * 60000, n_q_heads=4096)
-    assert shared(x, groups((0, 60000)), huge) == -2 and weigh(x, huge, mass(n_layers=1, n_seqs=60000, n_kv_heads=4096)) == -2
+    assert shared(x, groups((0, 60000)), huge) == -2
+    for n in (x, batch([0] * 60000 + [1], n_q_heads=4096)):                               # shares of all work: as many workgroups whatever there is
+        assert b.lib().codecomp_attend_mass_validate(ref(n), ref(huge), ref(mass(n_layers=1, n_seqs=60000, n_kv_heads=4096))) == 0
     assert evict(mass(n_layers=15, n_seqs=65535, n_kv_heads=4096), eviction(n_seqs=65535), pool(n_kv_heads=4096, n_layers=15)) == -2
+    # one prompt of very many tokens is none too many: what is behind the shared rows is joined where it is attended to
+    assert b.lib().codecomp_attend_shared_validate(ref(batch([0, 1 << 20], n_q_heads=64)), ref(groups((0, 1))), ref(pool(head_dim=128))) == 0
     # many requests of long tables: chunks grow until a launch holds them
     x = batch(list(range(60001)), table_width=1 << 16, max_kv_len=1 << 20)
     assert b.lib().codecomp_attend_shared_workspace_bytes(ref(x), ref(groups((0, 60000), max_prefix_len=1 << 20, max_own_len=1 << 20)), ref(pool())) > 0
