@@ -34,6 +34,7 @@ struct SharedRows {
   int few_units, few_parts, few_chunk, few_splits;       // shared rows of groups of few rows: workgroups, parts of the rows, keys of a chunk, chunks
   int many_units, many_tiles, many_splits;               // of many: workgroups, tiles of a chunk, chunks
   int splits;                  // the larger one: parts of shared rows that every row has
+  int own_units;               // workgroups of the kernel for many rows for what requests have behind the shared rows (one more part); 0: the kernel for few has it
   int join;                    // 1: whoever has a request's own rows joins the parts of the shared ones to them, and writes the outputs
 };
 // What a row's parts say that had no keys: not to be read any further.
@@ -134,6 +135,7 @@ __device__ __forceinline__ s16x4 read_columns(const unsigned char* lds) {
 }
 
 int launch_few(const AttendPlan& pl, const AttendArgs& a, hipStream_t stream);
+int launch_join_own(int d, int64_t units, const SharedArgs& a, hipStream_t stream);
 int launch_few_shared(int d, bool fp8, bool two_blocks, int64_t units, const SharedArgs& a, hipStream_t stream);
 
 }  // namespace codecomp

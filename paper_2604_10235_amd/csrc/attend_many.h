@@ -86,7 +86,8 @@ struct TileAt {
 };
 
 // ROWWISE: pages of less than 16 rows; else the 16 rows that a wave loads of a tile lie in one page, whose place is worked out in scalar registers.
-// SHARED: a workgroup has a chunk of the rows that a group of requests shares, for a block of the group's rows, and leaves parts of them.
+// SHARED: a workgroup has a chunk of the rows that a group of requests shares, for a block of the group's rows, or what a request has behind them, for a block of
+// its rows, and leaves parts of them.
 template <int D, bool FP8, bool ROWWISE, bool SHARED = false>
 __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const ManyArgs ma) {
   const AttendArgs& a = ma.a;
@@ -213,8 +214,9 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
   int64_t start = uniform(x1 - 1 - found[2]);                     // position of the block
   Blocks of = uniform(request(SHARED ? 0 : r));
   CutBlock cut = {-1, 0, 0, 0};
-  int chunk_tile0 = 0, chunk_tile1 = 0;
-  if constexpr (SHARED) {
+  int chunk_tile0 = 0, chunk_tile1 = 0, key_low = 0;               // SHARED: the tiles, and the first key of them that counts
+  const int group_blocks = SHARED ? (ma.sh.many_units + 7) / 8 * 8 : 0;
+  if (SHARED && (int)blockIdx.x < group_blocks) {
     // Blocks of rows of one chunk side by side, on one die: they read the same keys.
     const int on_die = (ma.sh.many_units + 7) / 8, unit = (int)(blockIdx.x & 7) * on_die + (int)(blockIdx.x >> 3);
     if ((int)(blockIdx.x >> 3) >= on_die || unit >= ma.sh.many_units) return;
@@ -253,6 +255,44 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
     if (g == 0) no_parts<kManyThreads>(a, ma.sh.many_splits, ma.sh.splits, of.q0, head, row0, row1);
     if (chunk_tile0 >= chunk_tile1) {
       no_parts<kManyThreads>(a, g, g + 1, of.q0, head, row0, row1);
+      return;
+    }
+  } else if constexpr (SHARED) {
+    const int on_die = (ma.sh.own_units + 7) / 8, turn = (int)blockIdx.x - group_blocks, unit = (turn & 7) * on_die + (turn >> 3);
+    if (unit >= ma.sh.own_units) return;
+    int rest = unit;
+    r = -1;
+    for (int r0 = 0; r < 0 && r0 < n; r0 += 64) {
+      const int at = min(r0 + lane, n - 1), q0 = a.b.cu_q[at], nq = a.b.cu_q[at + 1] - q0;
+      const Blocks x = blocks_of(ma, 0, q0, nq);
+      const int units = r0 + lane < n && x.rows > 0 ? (x.rows + kManyRows - 1) / kManyRows * a.b.Hkv : 0;
+      int upto = units;
+#pragma unroll
+      for (int off = 1; off < 64; off <<= 1) {
+        const int y = __shfl_up(upto, off);
+        if (lane >= off) upto += y;
+      }
+      const uint64_t reached = __ballot(upto > rest);
+      if (reached == 0) { rest -= __shfl(upto, 63); continue; }
+      const int owner = __builtin_ctzll(reached);
+      r = r0 + owner;
+      rest -= __shfl(upto - units, owner);
+      of = blocks_of(ma, 0, __shfl(q0, owner), __shfl(nq, owner));
+    }
+    if (r < 0) return;
+    r = uniform(r); rest = uniform(rest);
+    of.count = (of.rows + kManyRows - 1) / kManyRows;
+    key_low = uniform(prefix_of(ma.sh, request_of(ma.sh.cu_groups, ma.sh.n_groups, r)));
+    of.len = (int)min((int64_t)kv_len_of(a.b, r), (int64_t)key_low + ma.sh.max_own);
+    of = uniform(of);
+    block = of.count - 1 - rest % of.count;                       // those that see the most keys first
+    head = rest / of.count;
+    g = ma.sh.splits;
+    chunk_tile0 = key_low / kManyKeys;
+    chunk_tile1 = of.len > key_low ? of.tiles(block) : 0;
+    if (chunk_tile0 >= chunk_tile1) {
+      const int row0 = block * kManyRows;
+      no_parts<kManyThreads>(a, g, g + 1, of.q0, head, row0, min(of.rows, row0 + kManyRows));
       return;
     }
   }
@@ -358,7 +398,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
         }
       };
       // The keys of a tile that there are; the tiles from `plain_end` on have keys that are not there, or that some rows do not see.
-      auto is_there = [&](int tile, int page) __attribute__((always_inline)) { return __ballot(tile * kManyKeys + lane < of.len && is_page(page)); };
+      auto is_there = [&](int tile, int page) __attribute__((always_inline)) { return __ballot(tile * kManyKeys + lane < of.len && (!SHARED || tile * kManyKeys + lane >= key_low) && is_page(page)); };
       const int plain_end = min(seen_by_all, of.len) >> 6;
       auto partly = [&](int tile) { return (tile + 1) * kManyKeys > seen_by_all && seen_by_all < of.len; };       // some rows do not see all of it
       // Values of a tile that has keys that are not there, or that some rows do not see: a weight of zero must not meet what stands in the one, nor an
@@ -510,6 +550,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
             if ((tile & 15) == 13) fetch_entries((tile >> 4) + 2);   // three tiles ahead a new stretch begins: the one after it
             if ((tile & 15) == 0) held = __ballot(is_page(entries[(tile >> 4) & 3][lane]));
             masked |= (((unsigned)(held >> ((tile & 15) * 4)) & 15u) != 15u);
+            if constexpr (SHARED) masked |= tile * kManyKeys < key_low;
             if (masked) valid = is_there(tile, entry(tile, lane));
           }
           if (__builtin_expect(masked, 0)) clean_values(tile, valid);
@@ -554,7 +595,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
       if (active) {
         if (__builtin_expect(partly(tile1 - 1) && not_finite != 0, 0)) {
           // from the first tile that was cleaned on: the keys before seen_by_all in it were as well
-          for (int key = max(seen_by_all & -kManyKeys, tile0 * kManyKeys); key < min(of.len, tile1 * kManyKeys); ++key) {
+          for (int key = max(max(seen_by_all & -kManyKeys, tile0 * kManyKeys), key_low); key < min(of.len, tile1 * kManyKeys); ++key) {
             const int at = table[key >> a.pool.page_log2];
             if (at < 0 || at >= a.pool.n_pages || key >= limit) continue;
             const unsigned char* from = a.pool.v + a.layer + head * a.pool.s_head + at * a.pool.s_page + (key & in_page) * a.pool.s_tok;
@@ -618,7 +659,7 @@ int launch_many_of(const ManyArgs& m, hipStream_t stream) {
 
 template <int D, bool FP8>
 int launch_many_shared_of(const ManyArgs& m, hipStream_t stream) {
-  const dim3 grid((unsigned)((m.sh.many_units + 7) / 8 * 8)), block(kManyThreads);
+  const dim3 grid((unsigned)((m.sh.many_units + 7) / 8 * 8 + (m.sh.own_units + 7) / 8 * 8)), block(kManyThreads);
   if (m.a.pool.page_log2 < 4) attend_many_kernel<D, FP8, true, true><<<grid, block, 0, stream>>>(m);
   else attend_many_kernel<D, FP8, false, true><<<grid, block, 0, stream>>>(m);
   return (int)hipGetLastError();

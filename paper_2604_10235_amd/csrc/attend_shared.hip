@@ -25,6 +25,7 @@ constexpr int kChip = 256;                       // compute units: workgroups of
 constexpr int64_t kMostBlocks = (1 << 23) - 1;    // of up to 512 threads: an axis of a grid holds 2^32 threads
 constexpr int kMostSplits = 1024;
 constexpr int kFewRows = 32;
+constexpr int kOwnRows = 64;
 constexpr int64_t kFewKeys8 = INT64_MAX, kFewKeys16 = 1 << 17;
 constexpr int kFewChunk = 2048;
 constexpr int kJoinParts = 6;
@@ -66,11 +67,20 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
       few_most = std::max(few_most, rows);
     }
   }
-  for (int r = 0; r < x.n_seqs; ++r) own_most = std::max(own_most, (int64_t)(b->cu_q_host[r + 1] - b->cu_q_host[r]) * x.G);
+  int64_t own_blocks = 0;                          // of rows, if the kernel for many rows has the own ones too
+  for (int r = 0; r < x.n_seqs; ++r) {
+    const int64_t rows = (int64_t)(b->cu_q_host[r + 1] - b->cu_q_host[r]) * x.G;
+    own_most = std::max(own_most, rows);
+    own_blocks += (rows + kManyRows - 1) / kManyRows;
+  }
+  if (own_most <= kOwnRows || s.max_own == 0) own_blocks = 0;
+  own_blocks *= x.Hkv;
   blocks *= x.Hkv;
+  if (blocks + own_blocks > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
+  s.own_units = (int)own_blocks;
   const int64_t items = (int64_t)x.n_seqs * x.Hkv, own_parts = (own_most + 31) / 32;
   // Where one workgroup has all own rows of a request's head, it joins the parts of the shared ones to them as well.
-  s.join = pl->many_groups > 0 && (s.max_own <= kJoinKeys || items * own_parts >= kJoinItems);
+  s.join = pl->many_groups > 0 && (s.own_units > 0 || s.max_own <= kJoinKeys || items * own_parts >= kJoinItems);
   pl->few_two = s.join ? few_most > 16 : std::max(few_most, own_most) > 16;
   pl->own_two = s.join ? own_most > 16 : pl->few_two;
   const int few_each = pl->few_two ? 32 : 16, own_each = pl->own_two ? 32 : 16;
@@ -79,10 +89,9 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
   s.many_splits = s.few_splits = 0;
   if (pl->many_groups > 0) {
     const int tiles = std::max(1, (s.max_prefix + kManyKeys - 1) / kManyKeys);
-    if (blocks > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
     int best = 1;
     double least = 0.0;
-    for (int n = 1; n <= std::min(tiles, kChip) && blocks * n <= kMostBlocks; ++n) {
+    for (int n = 1; n <= std::min(tiles, kChip) && blocks * n + own_blocks <= kMostBlocks; ++n) {
       const int64_t rounds = ((blocks * n + 7) / 8 + kChip / 8 - 1) / (kChip / 8);       // of a die's compute units
       const double time = (double)rounds * ((tiles + n - 1) / n + 5) + 0.02 * n;
       if (n == 1 || time < least) { best = n; least = time; }
@@ -121,7 +130,7 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
   }
   pl->own_units = items * pl->row_parts * pl->own_splits;
   if (pl->own_units + few_units > kMostBlocks) return CODECOMP_EINVAL_SHAPE;        // with which the kernel that joins has less than 2^27 rows, 8 or more a workgroup
-  pl->ws_bytes = x.T == 0 ? 0 : ((size_t)(s.splits + (s.join ? 0 : pl->own_splits)) * x.T * x.Hq * (p->head_dim + 2) * sizeof(float) + 255) & ~(size_t)255;
+  pl->ws_bytes = x.T == 0 ? 0 : ((size_t)(s.splits + (s.join ? s.own_units > 0 : pl->own_splits)) * x.T * x.Hq * (p->head_dim + 2) * sizeof(float) + 255) & ~(size_t)255;
   return CODECOMP_OK;
 }
 
@@ -189,7 +198,7 @@ int launch_shared(const SharedPlan& pl, const void* q, int layer, void* out, flo
   a.c = fminf(fmaxf(pl.scale * pl.pool.k_scale * kLog2e, FLT_MIN), FLT_MAX);       // a hidden logit of minus infinity times it stays one
   a.chunk = pl.chunk; a.row_parts = pl.row_parts;
   a.sh = pl.sh;
-  const int parts = pl.sh.splits + (pl.sh.join ? 0 : pl.own_splits);
+  const int parts = pl.sh.splits + (pl.sh.join ? pl.sh.own_units > 0 : pl.own_splits);
   const int64_t rows = (int64_t)pl.batch.T * pl.batch.Hq;
   a.part_o = static_cast<float*>(workspace);
   a.part_ml = a.part_o + parts * rows * pl.d;
@@ -207,6 +216,7 @@ int launch_shared(const SharedPlan& pl, const void* q, int layer, void* out, flo
     if (pl.sh.few_units > 0)
       if (int rc = launch_few_shared(pl.d, pl.pool.fp8, pl.few_two, pl.sh.few_units, a, stream)) return rc;
     a.sh.few_units = 0;
+    if (a.sh.own_units > 0) return launch_join_own(pl.d, pl.own_units, a, stream);
     return launch_few_shared(pl.d, pl.pool.fp8, pl.own_two, pl.own_units, a, stream);
   }
   if (pl.sh.few_units + pl.own_units > 0)
