@@ -25,7 +25,8 @@ constexpr int kChip = 256;                       // compute units: workgroups of
 constexpr int64_t kMostBlocks = (1 << 23) - 1;    // of up to 512 threads: an axis of a grid holds 2^32 threads
 constexpr int kMostSplits = 1024;
 constexpr int kFewRows = 32;
-constexpr int kOwnRows = 64;
+constexpr int kOwnRows = 32;
+constexpr double kLead = 5.0, kPartElements = 600000.0;
 constexpr int64_t kFewKeys8 = INT64_MAX, kFewKeys16 = 1 << 17;
 constexpr int kFewChunk = 2048;
 constexpr int kJoinParts = 6;
@@ -73,7 +74,7 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
     own_most = std::max(own_most, rows);
     own_blocks += (rows + kManyRows - 1) / kManyRows;
   }
-  if (own_most <= kOwnRows || s.max_own == 0) own_blocks = 0;
+  if (own_most <= kOwnRows || s.max_own == 0 || pl->many_groups == 0) own_blocks = 0;
   own_blocks *= x.Hkv;
   blocks *= x.Hkv;
   if (blocks + own_blocks > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
@@ -89,11 +90,15 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
   s.many_splits = s.few_splits = 0;
   if (pl->many_groups > 0) {
     const int tiles = std::max(1, (s.max_prefix + kManyKeys - 1) / kManyKeys);
+    const double own = 0.75 * ((s.max_own + kManyKeys - 1) / kManyKeys) + kLead, part = (double)x.T * x.Hq * p->head_dim / kPartElements;
     int best = 1;
     double least = 0.0;
     for (int n = 1; n <= std::min(tiles, kChip) && blocks * n + own_blocks <= kMostBlocks; ++n) {
+      const double each = (tiles + n - 1) / n + kLead;
       const int64_t rounds = ((blocks * n + 7) / 8 + kChip / 8 - 1) / (kChip / 8);       // of a die's compute units
-      const double time = (double)rounds * ((tiles + n - 1) / n + 5) + 0.02 * n;
+      const int64_t left = own_blocks - (rounds * kChip - blocks * n) * (int64_t)(each / own);
+      const double end = rounds * each + (left > 0 ? (left + kChip - 1) / kChip * own : 0.0), work = (blocks * n * each + own_blocks * own) / kChip;
+      const double time = end + work + n * (0.04 + part);
       if (n == 1 || time < least) { best = n; least = time; }
     }
     s.many_tiles = (tiles + best - 1) / best;

@@ -174,7 +174,7 @@ def check_shared_bits(f, causal=True):
     return out, lse
 
 
-@pytest.mark.parametrize("members, news, n_q", [([3], [1, 4, 1], 8), ([30], [1] * 30, 8), ([2], [60, 33], 4)])
+@pytest.mark.parametrize("members, news, n_q", [([3], [1, 4, 1], 8), ([30], [1] * 30, 8), ([2], [60, 33], 4), ([3], [90, 40, 1], 3)])
 @pytest.mark.parametrize("fp8, d, page", [(False, 128, 32), (True, 64, 8), (False, 64, 256)])
 def test_shared_infinities_and_nan_among_values_that_are_seen(members, news, n_q, fp8, d, page):
     """One element of one value row: that element of every token that sees the row is infinite or NaN, everything else keeps its bits."""
@@ -264,7 +264,10 @@ def test_shared_without_tokens_and_many_groups():
     ([3, 30], [140, 333], [0, 1, 2] + [0] + [1] * 29, 9, 8, 2, 64, 16, {}),
     ([9], [700], [1] * 9, 40, 28, 4, 128, 32, dict(max_kv=70000, max_prefix=60000, max_own=300)),
     ([16, 10, 3], [65, 700, 90], [4] * 16 + [4] * 10 + [4] * 3, 60, 8, 8, 64, 8, dict(max_kv=70000, max_prefix=60000, max_own=9000)),
-    ([60], [300], [1] * 60, 1500, 16, 4, 64, 64, {}), ([60], [300], [2] * 60, 700, 32, 4, 128, 16, dict(max_kv=9000, max_own=3000))])
+    ([60], [300], [1] * 60, 1500, 16, 4, 64, 64, {}), ([60], [300], [2] * 60, 700, 32, 4, 128, 16, dict(max_kv=9000, max_own=3000)),
+    # own rows in the kernel for many rows: of single tokens and prompts beside one another, causal within a block and behind its end, shared rows that end inside a tile
+    ([9, 2, 1], [205, 90, 0], [1, 70, 0, 3, 1, 33, 1, 9, 1, 1, 2, 150], 300, 8, 2, 64, 16, {}), ([5, 4], [1000, 63], [300, 1, 129, 2, 40, 1, 1, 1, 90], 400, 14, 2, 128, 1, {}),
+    ([30], [129], [1, 9] * 15, 200, 16, 4, 128, 128, dict(max_kv=5000, max_prefix=5000, max_own=4000)), ([2, 1], [320, 64], [65, 64, 300], 1, 4, 4, 64, 64, {})])
 @pytest.mark.parametrize("causal", [True, False])
 def test_shared_kinds_of_groups(members, prefixes, news, own, n_q, n_kv, d, page, bounds, causal):
     rng = np.random.default_rng([47, own, page])
