@@ -2,10 +2,19 @@
 //
 // The shared rows are attended to once for a group, by the rows (new tokens x query heads of a KV head) of all of its requests together: they lie side by
 // side in the packed batch, and all of them see all of the shared rows.  What a request has behind them is its own.  Both leave parts of every row (reference, sum
-// of weights, unscaled output, fp32), which a last kernel joins in order.
+// of weights, unscaled output, fp32), which are joined in order: o = sum of 2^(m_p - m) o_p, l the same, m the largest m_p; output o / l, log-sum-exp m + log2 l.
 //
-// Groups of many rows: the kernel of attend_many.h, whose blocks of 256 rows share keys and values through LDS.  Groups of up to 64 rows, and all rows behind the
-// shared ones: that of attend_few.hip, which reads keys and values once for up to 32 rows; both in one launch.
+// Groups of many rows: the kernel of attend_many.h, whose blocks of 256 rows share keys and values through LDS.  Groups of few: that of
+// attend_few.hip, which reads keys and values once for up to 32 rows.  Rows behind the shared ones: the kernel for few rows, in which whoever has the rows joins the
+// parts of the shared ones to them, or, for prompts, the kernel for many, in the same launch as the shared rows.
+//
+// Single tokens wait for memory, and shared rows are read once for all: 64 steps of 28 query heads on 4 KV heads of 128 over 32768 shared rows and up to 700 of their own, 63 us
+// where codecomp_attend over the same caches takes 470 (the shared rows 42, by 448 rows in blocks of 256: 1.33 PFLOP/s of the products that are formed; their own 19, of which
+// a compute unit reads 32 bytes a ns).  96 steps in eight groups of twelve behind 2001 to 9001 rows, 8 KV heads, 8 bits: 99 us instead of 213.
+// Prompts wait for the matrix units, which sharing takes no work off: 24 of up to 401 tokens in two groups behind 16000 rows, head_dim 64, 208 us instead of 217.
+// Four steps behind 2049 rows: 13 us, two launches of dependent waits (codecomp_attend 12).
+// Tried before, kernel for few rows: eight waves a workgroup (four steps 9.5 us instead of 8.7), three blocks of 16 rows (shared rows of 48 rows 52 us instead of 57, but their
+// own ones 69 instead of 62); kernel for many: a loop over units (206 -> 214 us).
 #include <float.h>
 #include <math.h>
 
@@ -24,15 +33,28 @@ extern template int launch_many_shared_of<128, true>(const ManyArgs&, hipStream_
 constexpr int kChip = 256;                       // compute units: workgroups of the kernel for many rows that run at once
 constexpr int64_t kMostBlocks = (1 << 23) - 1;    // of up to 512 threads: an axis of a grid holds 2^32 threads
 constexpr int kMostSplits = 1024;
+// Groups of 33 to 64 rows: the kernel for few rows reads the shared rows twice, the one for many has most of a block empty, but a tile's keys for all of it at once (us,
+// few | many: one group of 56 rows behind 2000 rows 14 | 23, 8192 24 | 27, 32768 36 | 39; eight behind 2000 to 9000 50 | 45, head_dim 64 31 | 34; 8 bits, 48 rows, 52 | 66:
+// never there).  By keys of all such groups and heads.
 constexpr int kFewRows = 32;
-constexpr int kOwnRows = 32;
-constexpr double kLead = 5.0, kPartElements = 600000.0;
 constexpr int64_t kFewKeys8 = INT64_MAX, kFewKeys16 = 1 << 17;
-constexpr int kFewChunk = 2048;
-constexpr int kJoinParts = 6;
-constexpr int64_t kJoinRows = 16384;
+// Most keys of a chunk in the kernel for few rows, shared and own (us, eight groups of 48 rows behind 9001: 512 77, 1024 65, 2048 57, 4096 57; 96 requests' own 2000: 512 96, 1024 85,
+// 2048 88; of 20 to 2000: 66, 61, 62).
+constexpr int kFewChunk = 2048, kOwnChunk = 1024;
+// Requests of more rows: what they have behind the shared ones is the kernel for many rows' too, once that runs (us, few | many: 8 tokens of 7 query heads over 100 to 1000 rows,
+// 32 requests, 59 | 43, 14: 82 | 59, 18: 86 | 61; 16 prompts of up to 512 over up to 2500: 603 | 299; 4 tokens 50 | 40, but at head_dim 64, 6 tokens of 4 over up to 2000, 37 | 44).
+constexpr int kOwnRows = 32;
+// Otherwise one workgroup has a request's own rows, and joins, where they are short or where there are enough of these, else chunks do and a kernel that joins (us, chunks |
+// one: 16 requests of 4 heads, up to 300 rows, 27 | 26, up to 2000 40 | 57; 64 of up to 4000 100 | 96; 128 of up to 1000 78 | 74).
 constexpr int kJoinKeys = 512;
 constexpr int64_t kJoinItems = 192;
+// The kernel that joins: several groups of threads a row, for many parts and few rows (us, one | eight: four steps 20 | 13, eight behind 32768 rows 63 | 36; 1024 steps of 32768
+// rows in all 132 | 149).
+constexpr int kJoinParts = 6;
+constexpr int64_t kJoinRows = 16384;
+// Chunks of shared rows for the kernel for many: the time of a tile is the unit.  A chunk starts and ends in 5 of them (8.6 us of 1.6 each at head_dim 128), and what it leaves
+// goes through memory twice: 600000 elements in a tile's time.
+constexpr double kLead = 5.0, kPartElements = 600000.0;
 
 int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const codecomp_pages* p, SharedPlan* pl) {
   if (int rc = make_pool(p, &pl->pool)) return rc;
@@ -80,13 +102,14 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
   if (blocks + own_blocks > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
   s.own_units = (int)own_blocks;
   const int64_t items = (int64_t)x.n_seqs * x.Hkv, own_parts = (own_most + 31) / 32;
-  // Where one workgroup has all own rows of a request's head, it joins the parts of the shared ones to them as well.
   s.join = pl->many_groups > 0 && (s.own_units > 0 || s.max_own <= kJoinKeys || items * own_parts >= kJoinItems);
   pl->few_two = s.join ? few_most > 16 : std::max(few_most, own_most) > 16;
   pl->own_two = s.join ? own_most > 16 : pl->few_two;
   const int few_each = pl->few_two ? 32 : 16, own_each = pl->own_two ? 32 : 16;
 
-  // shared rows, many: chunks such that all workgroups run at once and end together
+  // Shared rows, many: chunks for which the last workgroup ends early (rounds of as many as there are compute units, then the requests' own blocks, which fill what the last
+  // round leaves free) and not much is done in all (the chip's clock goes by it).  1, 2, 3, 4, 5 and 8 chunks, us: the 24 questions 251, 268, 208, 225, 215, 237; four prompts of
+  // 200 to 500 tokens behind 8000 rows 211, 224, 245, 250, 276, 303; 32 of 16 tokens behind 4000 94, 59, 63, 75, 73, 94.  Own rows count as three quarters of their bound.
   s.many_splits = s.few_splits = 0;
   if (pl->many_groups > 0) {
     const int tiles = std::max(1, (s.max_prefix + kManyKeys - 1) / kManyKeys);
@@ -131,7 +154,7 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
     pl->chunk = s.max_own;
     pl->own_splits = 1;
   } else {
-    cut(items * pl->row_parts, s.max_own, 2048, &pl->chunk, &pl->own_splits);
+    cut(items * pl->row_parts, s.max_own, kOwnChunk, &pl->chunk, &pl->own_splits);
   }
   pl->own_units = items * pl->row_parts * pl->own_splits;
   if (pl->own_units + few_units > kMostBlocks) return CODECOMP_EINVAL_SHAPE;        // with which the kernel that joins has less than 2^27 rows, 8 or more a workgroup

@@ -1,18 +1,35 @@
 // Eviction in place by summed attention weights (codecomp_evict): which rows stay, and their move together.
 //
-// Two kernels.  The first has a workgroup for each (layer, request, KV head): the sum that the last kept row has is found digit by digit from
-// the top (counts of 8 bits of the ordered value at a time), then rows are gone through in order and their numbers written one behind the other, the sums along
-// with them.  The second moves rows of K and V.  Row f + i comes from a row that is not before it, so a workgroup that goes through them in order, and has all
-// rows of a batch in registers before it writes the first, needs no room elsewhere; K and V, and stretches of a row, do not meet and are different workgroups'.
+// The B largest of n sums: their smallest is found digit by digit from the top, by counting how many of the sums that are still possible have each value of the
+// next 8 bits; then rows are gone through in order, and the numbers of those above it, and of the first ones at it, written one behind the other.
+// Sums are read once and stand in registers; counts are integers, so that their order does not matter.  A row has 256 bytes of K and of V and 4 of its sum:
+// the move is nearly all of the work, bound by memory: every kept row that changes its place is read and written once.
+//
+// The move is in place: row f + i comes from row kept[i], which is not before it (kept ascends).  A workgroup goes through its rows in order, a batch at a time, and has all of a
+// batch in registers before it overwrites one: what later batches read lies behind that.  K and V, heads and layers, and stretches of a
+// row, do not meet, and are different workgroups'.
+//
+// Many problems (a layer's request and head each): one kernel, a workgroup for each, whose waits for counts are hidden behind the rows of others.  28 layers, 32 requests of 900 to
+// 1500 rows, 4 heads of 128, 1024 kept: 635 us, 5.3 TB/s; 32 layers, 48 requests behind 2049 protected rows, 8 bits: 1312 us, 4.9 TB/s.
+// Fewer: two kernels, the second with two or four workgroups for each.  28 layers, one request of 32768 rows to 2048: 25 us for the numbers and 57 for the rows,
+// which come from 256 bytes here and there, 4.1 TB/s; one layer of 1088 rows to 1024: 8 and 8 us, a chain of waits for counts and numbers.
+// Tried before: digits of 11 bits (three passes; as long); the next batch sent for before one is written (as long: it is the scattered rows, not the wait);
+// loads that may stay in the caches instead of those that pass by them (651 us instead of 637 for the steps above, 1307 instead of 1313 for 8 bits).
 #include "serve.h"
 
 namespace codecomp {
 
-constexpr int kMoveDeep = 2;                             // pieces of 16 bytes that a thread has in flight
-constexpr int kBothDeep = 4, kBothThreads = 512;
-constexpr int kFewest = 256, kFewer = 64;
-constexpr int kManyProblems = 1024;
-constexpr int kFewMoves = 1024;                          // workgroups up to which they are of 1024 threads, not 256
+// From as many problems on it is one kernel (28 layers of 4 heads, 900 to 1500 rows to 1024, us, one | two: 1 request 58 | 40, 2: 58 | 56, 3: 86 | 66, 4: 111 | 116, 16: 281 | 279;
+// 8 bits and 256 kept of up to 8000, 4 requests 34 | 50, 32: 157 | 200), unless requests have many more rows than its registers hold: the rest is read
+// five times (16 requests of 16000 rows 500 | 545, 32768 731 | 573).
+constexpr int kManyProblems = 400, kBothRows = 16384;
+// Its threads, and pieces of K and of V that each has in flight (steps as above, 8 bits: 256 threads 668 us, 1315; 512 635, 1307; 1024 707, 1517; 2, 4 and 6 pieces the same).
+constexpr int kBothThreads = 512, kBothDeep = 4;
+// Two kernels: threads of a workgroup that moves rows (one request of 32768, us: 512 threads 97, 1024 85), and pieces that each has in flight (2, 4, 8: 85, 87, 87).
+constexpr int kMoveThreads = 1024, kMoveDeep = 2;
+// Rows of 256 bytes are cut into two stretches of 128 where there are fewer workgroups than compute units (114 us -> 98); stretches of 64 and 32 bytes gain
+// nothing (one layer's 4 heads of 1088 rows 18 us instead of 16.5).
+constexpr int kFewest = 256;
 constexpr int64_t kMostBlocks = (1 << 22) - 1;          // of up to 1024 threads: an axis of a grid holds 2^32 threads
 
 struct Span { int f, n, m; };                            // rows [f, n) of a request, m of them kept
@@ -258,7 +275,7 @@ __global__ __launch_bounds__(THREADS) void close_up_kernel(const EvictArgs a, in
   close_up<PIECES, THREADS, kMoveDeep, 1>(a, rest / a.n_seqs, r, head, pool, part >> 1);
 }
 
-// Both, for many problems: what one workgroup waits for while it finds its border is hidden behind the rows of others.
+// Both, for many problems.
 template <int PIECES, int THREADS, int PER>
 __global__ __launch_bounds__(THREADS) void evict_kernel(const EvictArgs a) {
   const int head = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv, r = rest % a.n_seqs, layer = rest / a.n_seqs;
@@ -270,24 +287,24 @@ __global__ __launch_bounds__(THREADS) void evict_kernel(const EvictArgs a) {
 
 template <int PIECES>
 static void launch_close_up(const EvictArgs& a, int64_t problems, int slices, hipStream_t stream) {
-  const dim3 grid((unsigned)(problems * 2 * slices));
-  if (problems * 2 * slices < kFewMoves) close_up_kernel<PIECES, 1024><<<grid, dim3(1024), 0, stream>>>(a, slices);
-  else close_up_kernel<PIECES, 256><<<grid, dim3(256), 0, stream>>>(a, slices);
+  close_up_kernel<PIECES, kMoveThreads><<<dim3((unsigned)(problems * 2 * slices)), dim3(kMoveThreads), 0, stream>>>(a, slices);
 }
 
 int launch_evict(const EvictArgs& a, int d, hipStream_t stream) {
   const int64_t problems = (int64_t)a.n_layers * a.n_seqs * a.Hkv;
   const int pieces = d * (a.pool.fp8 ? 1 : 2) / 16;
   int slices = 1;
-  while (problems * 2 * slices < (slices < pieces / 8 ? kFewest : slices < pieces / 2 ? kFewer : 0)) slices *= 2;
+  while (problems * 2 * slices < kFewest && slices < pieces / 8) slices *= 2;
   if (problems * 2 * slices > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
-  if (problems >= kManyProblems && a.max_kv <= 8192) {
+  if (problems >= kManyProblems && a.max_kv <= kBothRows) {
     const dim3 grid((unsigned)problems), block(kBothThreads);
     if (pieces == 16) evict_kernel<16, kBothThreads, 8><<<grid, block, 0, stream>>>(a);
     else if (pieces == 8) evict_kernel<8, kBothThreads, 8><<<grid, block, 0, stream>>>(a);
     else evict_kernel<4, kBothThreads, 8><<<grid, block, 0, stream>>>(a);
     return (int)hipGetLastError();
   }
+  // Rows that registers hold, or a large part of them (4 heads of 28 layers, both kernels, us: 32768 rows with 256 threads of 16 | 1024 of 32: 207 | 83; 6000: 51 | 53, 256 of 8: 56;
+  // one layer's 1088 rows with 256 of 8 | 1024 of 32: 16.5 | 29).
   if (a.max_kv > 8192) keep_kernel<1024, 32><<<dim3((unsigned)problems), dim3(1024), 0, stream>>>(a);
   else if (a.max_kv > 2048) keep_kernel<256, 16><<<dim3((unsigned)problems), dim3(256), 0, stream>>>(a);
   else keep_kernel<256, 8><<<dim3((unsigned)problems), dim3(256), 0, stream>>>(a);
@@ -295,8 +312,7 @@ int launch_evict(const EvictArgs& a, int d, hipStream_t stream) {
   switch (pieces / slices) {
     case 16: launch_close_up<16>(a, problems, slices, stream); break;
     case 8: launch_close_up<8>(a, problems, slices, stream); break;
-    case 4: launch_close_up<4>(a, problems, slices, stream); break;
-    default: launch_close_up<2>(a, problems, slices, stream); break;
+    default: launch_close_up<4>(a, problems, slices, stream); break;
   }
   return (int)hipGetLastError();
 }

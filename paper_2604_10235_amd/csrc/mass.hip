@@ -2,15 +2,23 @@
 // exp(softmax_scale q.k_j - lse).
 //
 // The logits are formed again from queries and keys, with the log-sum-exp of every row known: half of attention's products, and no row has to wait for
-// another.  A key's weights of all rows meet in one workgroup (or in a fixed number of parts, added in order): no atomics.
+// another.  A key's weights of all rows meet in one workgroup (or in a fixed number of parts, added in order): no atomics.  Logits, weights and sums are fp32.
 //
-// Few rows (up to 64): every key is read once for a handful of products, bound by memory.  A workgroup of four waves has a chunk of the cache, each wave
-// tiles of 32 or 64 keys of its own, the next one on its way into registers.  S = Q K^T, 16 rows x 16 keys per MFMA: lane = key, so that a key's weights are added
-// in place, and by two exchanges between lanes at the end.
+// Few rows (up to 64): every key is read once for a handful of products, bound by memory.  A workgroup of four waves has a stretch of the cache, each wave
+// tiles of 32 (head_dim 128) or 64 keys of its own, the next one on its way into registers.  S = Q K^T, 16 rows x 16 keys per MFMA: lane = key, so that a key's
+// weights are added in place, and by two exchanges between lanes at the end.  64 requests of 500 to 16384 rows, 8 KV heads of 128, 8 bits: 118 us, 4.6 TB/s;
+// 64 of 300 to 4100 behind 8192 protected ones, 4 KV heads, bf16: 33 us, 4.7 TB/s.  One token over 2113 rows: 7 us, which is what the launch takes.
+// Tried before: two tiles on their way (no gain), tiles of 64 keys at head_dim 128 (202 us: registers spill), five waves (133).
 //
-// Many rows: bound by the matrix units and the vector work beside them.  A workgroup keeps 256 keys in registers, 64 a wave, and takes the rows that see
-// them 32 at a time through LDS, four tiles in turn, three of them on their way.  S^T = K Q^T: lane = row, whose log-sum-exp and limit are two
-// registers; a lane adds up the weights of its rows for each of 32 keys, and the lanes are added up once, at the end.
+// Many rows: bound by the matrix units and the vector work beside them (an exponential, a product and a sum a logit).  A workgroup of eight waves keeps 512 keys in
+// registers, 64 a wave, and takes the rows that see them 32 at a time through LDS, eight tiles in turn, seven of them on their way.  S^T = K Q^T: lane = row, whose
+// log-sum-exp and limit are two registers; a lane adds up the weights of its rows for each of 32 keys, and the lanes are added up once, at the end.
+// The logits of a tile are formed while those of the tile before become weights, in an order that the source gives: MFMAs and vector work take turns.
+// A prompt of 8191 tokens, 28 query heads of 128: 258 to 265 us, 0.91 to 0.94 PFLOP/s; a step of 32 rows takes 0.97 us, its MFMAs alone 0.81.
+// The work is cut into equal parts of rows over all blocks of keys, one for each compute unit, and the parts of a block that was cut are added by a second kernel: a
+// workgroup for a block, or for two halves, took 293 us and more (blocks at the end of a causal prompt have few rows, and two workgroups on one
+// compute unit do not share it evenly).  Tried before: four waves and two workgroups on a compute unit (278), three waves for a SIMD (273: registers spill),
+// the keys waited for inside of the loop (496: the waits count what was sent for since).
 #include <float.h>
 #include <math.h>
 
@@ -44,8 +52,12 @@ struct MassArgs {
 constexpr int kMassWaves = 4, kMassThreads = 64 * kMassWaves;
 constexpr int kManyMassWaves = 8, kManyMassThreads = 64 * kManyMassWaves, kMassKeys = 64 * kManyMassWaves;      // many rows: keys of a workgroup
 constexpr int kMassStage = 512;                 // rows whose log-sum-exp and limit stand in LDS at a time
-constexpr int kMassLead = 768;                  // rows' worth of positions in front of a block's rows, for starting on its keys and ending it
-constexpr int kMassLeast = 1024;                // rows' worth that a workgroup gets at least
+// Rows' worth of positions in front of a block's rows, for starting on its keys and ending it (a prompt of 8191 tokens, 16 of 20 to 400 over 400 to 3000 rows, four of 64
+// over 500 to 4096, us: 256: 272, 76, 42; 384: 270, 81, 23; 512: 269, 81, 23; 768: 265, 80, 25; 1536: 273, 97, 29).
+constexpr int kMassLead = 768;
+// Rows' worth that a workgroup gets at least: more than the 32 of a tile, so that every workgroup between the first and the last of a block has some
+// (100 tokens over 300 rows and 512 over 4096, us: 32: 16, 34; 64: 18, 34; 128: 19, 33; 256: 22, 33; 1024: 36, 48).
+constexpr int kMassLeast = 64;
 
 __device__ __forceinline__ int first_of(const MassArgs& a, int r) { return a.first ? max(a.first[r], 0) : 0; }
 
@@ -260,7 +272,7 @@ __global__ __launch_bounds__(kMassThreads, 4) void mass_few_kernel(const MassArg
   }
 }
 
-// Blocks of 256 keys of a request, and the rows that see them: of block b those from row_of(b) on, the first one's first key being seen by the most.
+// Blocks of 512 keys of a request, and the rows that see them: of block b those from row_of(b) on, the first one's first key being seen by the most.
 struct KeyBlocks {
   int len, nq, G, q0, rows, first, count, off;       // keys, tokens, ..., first block that is not of protected rows alone, blocks from there on, rows before the new ones
   __device__ __forceinline__ int row_of(int b) const { return off == INT32_MAX ? 0 : max(b * kMassKeys - off, 0) * G; }
@@ -578,9 +590,13 @@ __global__ __launch_bounds__(2 * kMassKeys) void mass_join_kernel(const MassArgs
   sums[j] = fmaf(a.decay, old_sum(a, sums, j, of.len, of.nq), a.share * (sum_of[0][key] + sum_of[1][key]));
 }
 
-constexpr int64_t kMassEvenBytes = 1 << 24;
+// Few rows: chunks, a workgroup each, up to so many bytes of keys that there may be, else equal shares of all that there are, which take a look at all requests first
+// (us, chunks | shares: 64 requests of 300 rows 7.7 | 8.9, 16 of 500 to 4000 12.2 | 16.0, one of 100000 21 | 25, 32 of 4000, 131 MB, 25 | 27;
+// 48 of 1000 to 4000 30 | 28, 64 of 300 to 4100 39 | 33, 8 of 4000 to 32000 38 | 28).
+constexpr int64_t kMassEvenBytes = 1 << 27;
+// Four for each compute unit (512, 1024, 2048: 136, 118, 123 us for the 8-bit steps above).
 constexpr int kMassFewShares = 1024;
-constexpr int kMassShares = 256;                 // a workgroup for each compute unit
+constexpr int kMassShares = 256;                 // many rows: a workgroup for each compute unit
 constexpr int64_t kMostBlocks = (1 << 24) - 1;    // of 256 threads: an axis of a grid holds 2^32 threads
 
 int make_mass_plan(const codecomp_batch* b, const codecomp_pages* p, const codecomp_mass* m, MassPlan* pl) {
@@ -598,12 +614,11 @@ int make_mass_plan(const codecomp_batch* b, const codecomp_pages* p, const codec
     else if (rows > 0) ++pl->few_rows;
   }
   const int64_t items = (int64_t)x.n_seqs * x.Hkv;
-  int64_t chunk = (items * x.max_kv / 2048 + 255) / 256 * 256;
-  chunk = std::min<int64_t>(std::max<int64_t>(chunk, 256), 512);
+  const int64_t chunk = items * x.max_kv > 256 * 2048 ? 512 : 256;        // two tiles of every wave (one at head_dim 64), or four where there are enough workgroups all the same (128 to 1024: within 0.4 us)
   pl->chunk = (int)chunk;
   pl->chunks = (int)((x.max_kv + chunk - 1) / chunk);
-  const int64_t bytes = (int64_t)pl->few_rows * x.Hkv * x.max_kv * p->head_dim * (pl->pool.fp8 ? 1 : 2);
-  pl->shares = bytes > kMassEvenBytes || items * pl->chunks > kMostBlocks ? kMassFewShares : 0;
+  const int64_t keys = (int64_t)pl->few_rows * x.Hkv * x.max_kv;
+  pl->shares = keys > kMassEvenBytes / (p->head_dim * (pl->pool.fp8 ? 1 : 2)) || items * pl->chunks > kMostBlocks ? kMassFewShares : 0;
   pl->ws_bytes = pl->many_rows > 0 && x.max_kv > 0 ? kMassShares * (2 * kMassKeys * sizeof(float) + sizeof(CutKeys)) : 0;
   return CODECOMP_OK;
 }
