@@ -595,7 +595,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
       if (active) {
         if (__builtin_expect(partly(tile1 - 1) && not_finite != 0, 0)) {
           // from the first tile that was cleaned on: the keys before seen_by_all in it were as well
-          for (int key = max(max(seen_by_all & -kManyKeys, tile0 * kManyKeys), key_low); key < min(of.len, tile1 * kManyKeys); ++key) {
+          for (int key = max(seen_by_all & -kManyKeys, SHARED ? max(tile0 * kManyKeys, key_low) : tile0 * kManyKeys); key < min(of.len, tile1 * kManyKeys); ++key) {
             const int at = table[key >> a.pool.page_log2];
             if (at < 0 || at >= a.pool.n_pages || key >= limit) continue;
             const unsigned char* from = a.pool.v + a.layer + head * a.pool.s_head + at * a.pool.s_page + (key & in_page) * a.pool.s_tok;
