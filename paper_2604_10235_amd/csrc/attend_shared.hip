@@ -33,6 +33,9 @@ extern template int launch_many_shared_of<128, true>(const ManyArgs&, hipStream_
 constexpr int kChip = 256;                       // compute units: workgroups of the kernel for many rows that run at once
 constexpr int64_t kMostBlocks = (1 << 23) - 1;    // of up to 512 threads: an axis of a grid holds 2^32 threads
 constexpr int kMostSplits = 1024;
+// Little work, in strips of 128 keys by 32 rows: all of it in one launch of the kernel for few rows, and one that joins (us, one | the kernel for many as well: 64 steps of 7 query
+// heads on 4 KV heads behind 1000 rows, 448 strips, 22 | 28, 2048 25 | 28, 4096 30 | 30; 16 steps behind 8000, 1008 strips, 26.5 | 26, 16000 33 | 30; 226 tokens behind 47 24 | 29).
+constexpr int64_t kFewStrips = 1024;
 // Groups of 33 to 64 rows: the kernel for few rows reads the shared rows twice, the one for many has most of a block empty, but a tile's keys for all of it at once (us,
 // few | many: one group of 56 rows behind 2000 rows 14 | 23, 8192 24 | 27, 32768 36 | 39; eight behind 2000 to 9000 50 | 45, head_dim 64 31 | 34; 8 bits, 48 rows, 52 | 66:
 // never there).  By keys of all such groups and heads.
@@ -74,12 +77,18 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
   s.n_groups = g->n_groups; s.max_prefix = g->max_prefix_len; s.max_own = g->max_own_len;
   int64_t few_most = 0, blocks = 0, own_most = 0;
   pl->few_groups = pl->many_groups = 0;
-  int middle = 0;                                  // groups of more than 32 rows that either kernel can take
+  int64_t middle = 0, strips = 0;                  // groups of more than 32 rows that either kernel can take; strips of 128 keys that the one for few takes, 32 rows at a time
   for (int i = 0; i < g->n_groups; ++i) {
     const int64_t rows = (int64_t)(b->cu_q_host[g->cu_groups_host[i + 1]] - b->cu_q_host[g->cu_groups_host[i]]) * x.G;
     middle += rows > kFewRows && rows <= kFewRowsMost;
+    strips += (rows + 31) / 32 * ((s.max_prefix + 127) / 128);
   }
-  s.few_rows = (int64_t)middle * x.Hkv * s.max_prefix > (pl->pool.fp8 ? kFewKeys8 : kFewKeys16) ? kFewRows : kFewRowsMost;
+  for (int r = 0; r < x.n_seqs; ++r) {
+    const int64_t rows = (int64_t)(b->cu_q_host[r + 1] - b->cu_q_host[r]) * x.G;
+    if (rows > kOwnRows) strips += (rows + 31) / 32 * ((s.max_own + 127) / 128);
+  }
+  if (strips * x.Hkv <= kFewStrips) s.few_rows = INT32_MAX;
+  else s.few_rows = middle * x.Hkv * s.max_prefix > (pl->pool.fp8 ? kFewKeys8 : kFewKeys16) ? kFewRows : kFewRowsMost;
   for (int i = 0; i < g->n_groups; ++i) {
     const int64_t rows = (int64_t)(b->cu_q_host[g->cu_groups_host[i + 1]] - b->cu_q_host[g->cu_groups_host[i]]) * x.G;
     if (rows > s.few_rows) {

@@ -27,9 +27,9 @@ constexpr int kManyProblems = 400, kBothRows = 16384;
 constexpr int kBothThreads = 512, kBothDeep = 4;
 // Two kernels: threads of a workgroup that moves rows (one request of 32768, us: 512 threads 97, 1024 85), and pieces that each has in flight (2, 4, 8: 85, 87, 87).
 constexpr int kMoveThreads = 1024, kMoveDeep = 2;
-// Rows of 256 bytes are cut into two stretches of 128 where there are fewer workgroups than compute units (114 us -> 98); stretches of 64 and 32 bytes gain
-// nothing (one layer's 4 heads of 1088 rows 18 us instead of 16.5).
-constexpr int kFewest = 256;
+// Rows of 256 bytes are cut into two stretches of 128 where there are fewer workgroups than compute units (114 us -> 98), and down to 32 where there are very few and
+// many rows to move: fewer waits one after another (one layer's 4 heads, to 2000 rows of 5000 33 us -> 27, but to 1024 of 1088 16.5 -> 18).
+constexpr int kFewest = 256, kFewer = 64, kManyRows = 1024;
 constexpr int64_t kMostBlocks = (1 << 22) - 1;          // of up to 1024 threads: an axis of a grid holds 2^32 threads
 
 struct Span { int f, n, m; };                            // rows [f, n) of a request, m of them kept
@@ -295,6 +295,7 @@ int launch_evict(const EvictArgs& a, int d, hipStream_t stream) {
   const int pieces = d * (a.pool.fp8 ? 1 : 2) / 16;
   int slices = 1;
   while (problems * 2 * slices < kFewest && slices < pieces / 8) slices *= 2;
+  while (problems * 2 * slices < kFewer && slices < pieces / 2 && a.max_budget > kManyRows) slices *= 2;
   if (problems * 2 * slices > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
   if (problems >= kManyProblems && a.max_kv <= kBothRows) {
     const dim3 grid((unsigned)problems), block(kBothThreads);
@@ -303,16 +304,19 @@ int launch_evict(const EvictArgs& a, int d, hipStream_t stream) {
     else evict_kernel<4, kBothThreads, 8><<<grid, block, 0, stream>>>(a);
     return (int)hipGetLastError();
   }
-  // Rows that registers hold, or a large part of them (4 heads of 28 layers, both kernels, us: 32768 rows with 256 threads of 16 | 1024 of 32: 207 | 83; 6000: 51 | 53, 256 of 8: 56;
-  // one layer's 1088 rows with 256 of 8 | 1024 of 32: 16.5 | 29).
-  if (a.max_kv > 8192) keep_kernel<1024, 32><<<dim3((unsigned)problems), dim3(1024), 0, stream>>>(a);
-  else if (a.max_kv > 2048) keep_kernel<256, 16><<<dim3((unsigned)problems), dim3(256), 0, stream>>>(a);
-  else keep_kernel<256, 8><<<dim3((unsigned)problems), dim3(256), 0, stream>>>(a);
+  // As many threads and rows of each as the longest request needs: what registers do not hold is read again (4 heads, both kernels, us: 1088 rows with 256 threads of 8 | 1024 of
+  // 32: 16.5 | 29; 8000 of which 50 stay, 256 of 16 | 512 of 16 | 1024 of 16: 27 | 13.5 | 16.6; 12000, 1024 of 16 | of 32: 16.5 | 23.9; 28 layers of 32768, 256 of 16 | 1024 of 32: 207 | 83).
+  const dim3 grid((unsigned)problems);
+  if (a.max_kv > 16384) keep_kernel<1024, 32><<<grid, dim3(1024), 0, stream>>>(a);
+  else if (a.max_kv > 8192) keep_kernel<1024, 16><<<grid, dim3(1024), 0, stream>>>(a);
+  else if (a.max_kv > 2048) keep_kernel<512, 16><<<grid, dim3(512), 0, stream>>>(a);
+  else keep_kernel<256, 8><<<grid, dim3(256), 0, stream>>>(a);
   if (hipError_t e = hipGetLastError()) return (int)e;
   switch (pieces / slices) {
     case 16: launch_close_up<16>(a, problems, slices, stream); break;
     case 8: launch_close_up<8>(a, problems, slices, stream); break;
-    default: launch_close_up<4>(a, problems, slices, stream); break;
+    case 4: launch_close_up<4>(a, problems, slices, stream); break;
+    default: launch_close_up<2>(a, problems, slices, stream); break;
   }
   return (int)hipGetLastError();
 }
