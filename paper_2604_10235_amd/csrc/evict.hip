@@ -25,6 +25,11 @@ namespace codecomp {
 constexpr int kManyProblems = 400, kBothRows = 16384;
 // Its threads, and pieces of K and of V that each has in flight (steps as above, 8 bits: 256 threads 668 us, 1315; 512 635, 1307; 1024 707, 1517; 2, 4 and 6 pieces the same).
 constexpr int kBothThreads = 512, kBothDeep = 4;
+// Fewer threads where requests are short (1656 problems of up to 83 rows, us, 512 | 256 | 128 threads: 28 | 13 | 10; 28 layers, 32 requests of up to 500: 147 | 144 | 148; 8 of 900:
+// 132 | 128 | 152).
+constexpr int kShortRows = 1024, kShortThreads = 256;
+// And always where they have next to no rows (4 heads, two kernels | one: 130 rows 11.0 | 9.5, 500 12.7 | 18.6; 288 problems of up to 32 rows 13.0 | 7.6).
+constexpr int kTinyRows = 192;
 // Two kernels: threads of a workgroup that moves rows (one request of 32768, us: 512 threads 97, 1024 85), and pieces that each has in flight (2, 4, 8: 85, 87, 87).
 constexpr int kMoveThreads = 1024, kMoveDeep = 2;
 // Rows of 256 bytes are cut into two stretches of 128 where there are fewer workgroups than compute units (114 us -> 98), and down to 32 where there are very few and
@@ -290,6 +295,13 @@ static void launch_close_up(const EvictArgs& a, int64_t problems, int slices, hi
   close_up_kernel<PIECES, kMoveThreads><<<dim3((unsigned)(problems * 2 * slices)), dim3(kMoveThreads), 0, stream>>>(a, slices);
 }
 
+template <int PIECES>
+static int launch_both(const EvictArgs& a, int64_t problems, hipStream_t stream) {
+  if (a.max_kv <= kShortRows) evict_kernel<PIECES, kShortThreads, kShortRows / kShortThreads><<<dim3((unsigned)problems), dim3(kShortThreads), 0, stream>>>(a);
+  else evict_kernel<PIECES, kBothThreads, 8><<<dim3((unsigned)problems), dim3(kBothThreads), 0, stream>>>(a);
+  return (int)hipGetLastError();
+}
+
 int launch_evict(const EvictArgs& a, int d, hipStream_t stream) {
   const int64_t problems = (int64_t)a.n_layers * a.n_seqs * a.Hkv;
   const int pieces = d * (a.pool.fp8 ? 1 : 2) / 16;
@@ -297,12 +309,9 @@ int launch_evict(const EvictArgs& a, int d, hipStream_t stream) {
   while (problems * 2 * slices < kFewest && slices < pieces / 8) slices *= 2;
   while (problems * 2 * slices < kFewer && slices < pieces / 2 && a.max_budget > kManyRows) slices *= 2;
   if (problems * 2 * slices > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
-  if (problems >= kManyProblems && a.max_kv <= kBothRows) {
-    const dim3 grid((unsigned)problems), block(kBothThreads);
-    if (pieces == 16) evict_kernel<16, kBothThreads, 8><<<grid, block, 0, stream>>>(a);
-    else if (pieces == 8) evict_kernel<8, kBothThreads, 8><<<grid, block, 0, stream>>>(a);
-    else evict_kernel<4, kBothThreads, 8><<<grid, block, 0, stream>>>(a);
-    return (int)hipGetLastError();
+  if (a.max_kv <= kTinyRows || (problems >= kManyProblems && a.max_kv <= kBothRows)) {
+    if (pieces == 16) return launch_both<16>(a, problems, stream);
+    return pieces == 8 ? launch_both<8>(a, problems, stream) : launch_both<4>(a, problems, stream);
   }
   // As many threads and rows of each as the longest request needs: what registers do not hold is read again (4 heads, both kernels, us: 1088 rows with 256 threads of 8 | 1024 of
   // 32: 16.5 | 29; 8000 of which 50 stay, 256 of 16 | 512 of 16 | 1024 of 16: 27 | 13.5 | 16.6; 12000, 1024 of 16 | of 32: 16.5 | 23.9; 28 layers of 32768, 256 of 16 | 1024 of 32: 207 | 83).

@@ -756,9 +756,18 @@ def test_evict_pages_that_are_not_held():
 
 @pytest.mark.parametrize("n", [1, 2, 15])
 def test_evict_of_few_and_many_problems(n):
-    """Rows in one, two and four stretches."""
-    for layers in (1, 20):
-        check_evict(np.random.default_rng([63, n, layers]), [333] * n, [100] * n, recent=10, max_budget=100, first=[7] * n, n_kv=2, d=128, layers=layers)
+    """Rows in one stretch and in more, short requests and long ones, in one kernel and in two."""
+    for layers, rows, budget in ((1, 333, 100), (20, 333, 100), (1, 150, 100), (1, 1300, 1100), (1, 9000, 300)):
+        check_evict(np.random.default_rng([63, n, layers, rows]), [rows] * n, [budget] * n, recent=10, max_budget=budget, first=[7] * n, n_kv=2, d=128, layers=layers)
+
+
+@pytest.mark.parametrize("n, rows, budget", [(102, 190, 60), (102, 1000, 60), (102, 1100, 60), (102, 4500, 60), (3, 2048, 70), (3, 2049, 1500), (3, 8193, 80), (3, 16385, 4000)])
+@pytest.mark.parametrize("d, fp8", [(64, True), (128, False), (64, False)])
+def test_evict_around_the_sizes_that_decide(n, rows, budget, d, fp8):
+    """Requests that are as long as the bound, one that is not, and one that is empty."""
+    rng = np.random.default_rng([71, n, rows, d])
+    lens = [0, rows] + [int(x) for x in rng.integers(1, 90, n - 2)]
+    check_evict(rng, lens, [budget] * n, recent=3, max_budget=budget, first=[5] * n, n_kv=4, d=d, page=16, fp8=fp8, layers=1, values="ties")
 
 
 def test_evict_lengths_out_of_range_and_again():
