@@ -11,10 +11,12 @@
 // Tried before: two tiles on their way (no gain), tiles of 64 keys at head_dim 128 (202 us: registers spill), five waves (133).
 //
 // Many rows: bound by the matrix units and the vector work beside them (an exponential, a product and a sum a logit).  A workgroup of eight waves keeps 512 keys in
-// registers, 64 a wave, and takes the rows that see them 32 at a time through LDS, eight tiles in turn, seven of them on their way.  S^T = K Q^T: lane = row, whose
+// registers, 64 a wave, and takes the rows that see them 32 at a time through LDS, eight tiles in turn, up to six of them on their way; waves meet at every
+// second one (at each: 265 us instead of 263 below, 471 instead of 466 for 2048 tokens over 32768 8-bit rows).  S^T = K Q^T: lane = row, whose
 // log-sum-exp and limit are two registers; a lane adds up the weights of its rows for each of 32 keys, and the lanes are added up once, at the end.
 // The logits of a tile are formed while those of the tile before become weights, in an order that the source gives: MFMAs and vector work take turns.
-// A prompt of 8191 tokens, 28 query heads of 128: 258 to 265 us, 0.91 to 0.94 PFLOP/s; a step of 32 rows takes 0.97 us, its MFMAs alone 0.81.
+// A prompt of 8191 tokens, 28 query heads of 128: 258 to 264 us, 0.91 to 0.93 PFLOP/s.  A step of 32 rows takes 0.97 us, 2040 cycles, of which the vector work of a SIMD's two
+// waves takes 1670 (a logit is an exponential at a quarter of the rate, a product and a sum) and its MFMAs 1020.
 // The work is cut into equal parts of rows over all blocks of keys, one for each compute unit, and the parts of a block that was cut are added by a second kernel: a
 // workgroup for a block, or for two halves, took 293 us and more (blocks at the end of a causal prompt have few rows, and two workgroups on one
 // compute unit do not share it evenly).  Tried before: four waves and two workgroups on a compute unit (278), three waves for a SIMD (273: registers spill),
@@ -23,6 +25,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "serve.h"
 
@@ -303,7 +306,7 @@ template <int D, bool FP8>
 __global__ __launch_bounds__(kManyMassThreads, 2) void mass_many_kernel(const MassArgs a) {
   constexpr int KS = D / 16, LOADS = D * (FP8 ? 1 : 2) / 32;       // fragments of a key; 16-byte pieces of it that a lane has
   constexpr int GROUP = D / 32 * 1024, TILE = 2 * GROUP;            // bytes of 16 rows and of 32 in LDS: chunks of 1 KB, 16 rows of four 16-byte pieces, piece by piece
-  constexpr int TILES = 8, AHEAD = TILES - 1;                       // in LDS, and on their way there
+  constexpr int TILES = 8, AHEAD = TILES - 2;                       // in LDS, and on their way there
   constexpr int SENDERS = TILE / 1024;                              // waves that send for a chunk of a tile each
   constexpr int RED = 33;                                           // floats between keys where lanes are added up
   constexpr int LDS = TILES * TILE > kMassKeys * RED * 4 ? TILES * TILE : kMassKeys * RED * 4;
@@ -483,20 +486,16 @@ __global__ __launch_bounds__(kManyMassThreads, 2) void mass_many_kernel(const Ma
           }
         }
       };
-      auto step = [&](int s, f32x16 (&z)[2], f32x16 (&zp)[2]) __attribute__((always_inline)) {
+      auto step = [&](int s, f32x16 (&z)[2], f32x16 (&zp)[2], auto even) __attribute__((always_inline)) {
         const unsigned char *qt = q_lane + (s & (TILES - 1)) * TILE, *next = q_lane + ((s + 1) & (TILES - 1)) * TILE;
-        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(AHEAD - 2) : "memory");       // tile s + 1 has come, and tile s - 1 is nobody's
+        if constexpr (decltype(even)::value) asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"(AHEAD - 3) : "memory");       // tiles s + 1 and s + 2 have come, and tiles s - 2 and s - 1 are nobody's
         mask(zp);
-#pragma unroll
-        for (int g = 0; g < 2; ++g)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) z[g][i] = 0.0f;
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int f = 0; f < KS; ++f) {
           ring[(f + RING - 1) % RING] = f + RING - 1 < KS ? query_frag(qt, f + RING - 1) : query_frag(next, f + RING - 1 - KS);
 #pragma unroll
-          for (int g = 0; g < 2; ++g) z[g] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(kf[g][f]), frag(ring[f % RING]), z[g], 0, 0, 0);
+          for (int g = 0; g < 2; ++g) z[g] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(frag(kf[g][f]), frag(ring[f % RING]), f == 0 ? f32x16{} : z[g], 0, 0, 0);      // zero as an operand: no registers to clear
           weigh(zp, f);
           if (f == 0) fetch(s + AHEAD);
           __builtin_amdgcn_sched_barrier(0);
@@ -520,11 +519,11 @@ __global__ __launch_bounds__(kManyMassThreads, 2) void mass_many_kernel(const Ma
       for (int f = 0; f < RING - 1; ++f) ring[f] = query_frag(q_lane, f);
       int s = 0;
       for (; s + 1 < steps; s += 2) {
-        step(s, za, zb);
-        step(s + 1, zb, za);
+        step(s, za, zb, std::true_type{});
+        step(s + 1, zb, za, std::false_type{});
       }
       if (s < steps) {
-        step(s, za, zb);
+        step(s, za, zb, std::true_type{});
         mask(za);
 #pragma unroll
         for (int f = 0; f < KS; ++f) weigh(za, f);
