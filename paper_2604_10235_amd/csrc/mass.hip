@@ -7,7 +7,7 @@
 // Few rows (up to 64): every key is read once for a handful of products, bound by memory.  A workgroup of four waves has a stretch of the cache, each wave
 // tiles of 32 (head_dim 128) or 64 keys of its own, the next one on its way into registers.  S = Q K^T, 16 rows x 16 keys per MFMA: lane = key, so that a key's
 // weights are added in place, and by two exchanges between lanes at the end.  64 requests of 500 to 16384 rows, 8 KV heads of 128, 8 bits: 118 us, 4.6 TB/s;
-// 64 of 300 to 4100 behind 8192 protected ones, 4 KV heads, bf16: 33 us, 4.7 TB/s.  One token over 2113 rows: 7 us, which is what the launch takes.
+// 64 of 300 to 4100 behind 8192 protected ones, 4 KV heads, bf16: 38 us, 4.2 TB/s.  One token over 2113 rows: 7 us, which is what the launch takes.
 // Tried before: two tiles on their way (no gain), tiles of 64 keys at head_dim 128 (202 us: registers spill), five waves (133).
 //
 // Many rows: bound by the matrix units and the vector work beside them (an exponential, a product and a sum a logit).  A workgroup of eight waves keeps 512 keys in

@@ -996,3 +996,23 @@ def test_forked_requests_grow_and_are_evicted(fp8, n, count, wide):
             shared = c.table[0, :full]
             assert np.array_equal(k1[:, shared], k0[:, shared])
             lens.copy_(new_lens)
+
+
+def test_readme_examples_run_one_after_another():
+    """The examples of the README as they stand: compression, service from what was kept, and answers that share it."""
+    import pathlib
+    import re
+    text = (pathlib.Path(__file__).resolve().parent.parent / "README.md").read_text()
+    blocks = re.findall(r"(?:^    .*\n|^\n(?=    ))+", text[text.index("    import numpy as np, torch"):], re.M)
+    assert len(blocks) == 3
+    ns = {}
+    for i, block in enumerate(blocks):
+        exec(compile(re.sub(r"^    ", "", block, flags=re.M), f"README.md block {i}", "exec"), ns)
+    torch.cuda.synchronize()
+    n, kept, sums, rows = ns["n"], ns["kept"], ns["sums"], ns["kept_rows"]
+    assert ns["lens"].tolist() == [kept + 128 + 400 - 300] * n                                    # 300 rows of its own each, 128 of them, 100 more
+    assert bool((rows[..., -16:].cpu() == torch.arange(kept + 284, kept + 300)).all()) and bool((rows.diff(dim=-1) > 0).all()) and int(rows.min()) >= kept
+    own = sums[..., kept: kept + 228]
+    assert bool(torch.isfinite(own).all()) and bool((own > 0).all()) and bool(torch.isfinite(ns["out"].float()).all())
+    # a token gives its rows of one head a weight of less than one in all: no more than a number of them that fades comes together
+    assert float(own.sum(-1).max()) < 1 / (1 - 0.98)
