@@ -216,83 +216,87 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
   CutBlock cut = {-1, 0, 0, 0};
   int chunk_tile0 = 0, chunk_tile1 = 0, key_low = 0;               // SHARED: the tiles, and the first key of them that counts
   const int group_blocks = SHARED ? (ma.sh.many_units + 7) / 8 * 8 : 0;
-  if (SHARED && (int)blockIdx.x < group_blocks) {
+  if constexpr (SHARED) {
     // Blocks of rows of one chunk side by side, on one die: they read the same keys.
-    const int on_die = (ma.sh.many_units + 7) / 8, unit = (int)(blockIdx.x & 7) * on_die + (int)(blockIdx.x >> 3);
-    if ((int)(blockIdx.x >> 3) >= on_die || unit >= ma.sh.many_units) return;
-    // its group: 64 of them at a time are asked for their blocks
-    int group = -1, rest = unit;
-    for (int g0 = 0; group < 0 && g0 < ma.sh.n_groups; g0 += 64) {
-      const int at = min(g0 + lane, ma.sh.n_groups - 1), q0 = a.b.cu_q[ma.sh.cu_groups[at]], nq = a.b.cu_q[ma.sh.cu_groups[at + 1]] - q0;
-      const int units = g0 + lane < ma.sh.n_groups ? blocks_of(ma, 0, q0, nq).count * ma.sh.many_splits * a.b.Hkv : 0;
-      int upto = units;
+    const bool shared = (int)blockIdx.x < group_blocks;
+    const int units = shared ? ma.sh.many_units : ma.sh.own_units, on_die = (units + 7) / 8, turn = shared ? blockIdx.x : blockIdx.x - group_blocks;
+    const int unit = (turn & 7) * on_die + (turn >> 3);
+    if ((turn >> 3) >= on_die || unit >= units) return;
+    // its group or request: they are shared out over the lanes, or the threads, to count their units
+    const int count = shared ? ma.sh.n_groups : n;
+    auto blocks_at = [&](int i) __attribute__((always_inline)) {
+      const int q0 = a.b.cu_q[shared ? ma.sh.cu_groups[i] : i], q1 = a.b.cu_q[shared ? ma.sh.cu_groups[i + 1] : i + 1];
+      Blocks x = blocks_of(ma, 0, q0, q1 - q0);
+      if (!shared) x.count = (x.rows + kManyRows - 1) / kManyRows;
+      return x;
+    };
+    auto units_at = [&](int i) __attribute__((always_inline)) { return blocks_at(i).count * a.b.Hkv * (shared ? ma.sh.many_splits : 1); };
+    auto up_to = [&](int x) __attribute__((always_inline)) {       // sums over the lanes, inclusive
 #pragma unroll
       for (int off = 1; off < 64; off <<= 1) {
-        const int y = __shfl_up(upto, off);
-        if (lane >= off) upto += y;
+        const int y = __shfl_up(x, off);
+        if (lane >= off) x += y;
       }
-      const uint64_t reached = __ballot(upto > rest);
-      if (reached == 0) { rest -= __shfl(upto, 63); continue; }
-      const int owner = __builtin_ctzll(reached);
-      group = g0 + owner;
-      rest -= __shfl(upto - units, owner);
-      of = blocks_of(ma, 0, __shfl(q0, owner), __shfl(nq, owner));
-    }
-    if (group < 0) return;
-    group = uniform(group); rest = uniform(rest);
-    r = ma.sh.cu_groups[group];
-    of.len = prefix_of(ma.sh, group);
-    of = uniform(of);
-    of.causal = 0;
-    block = rest % of.count;
-    rest /= of.count;
-    g = rest % ma.sh.many_splits;                                 // number of the part
-    head = rest / ma.sh.many_splits;
-    const int tiles = (of.len + kManyKeys - 1) / kManyKeys;
-    chunk_tile0 = g * ma.sh.many_tiles;
-    chunk_tile1 = min(tiles, chunk_tile0 + ma.sh.many_tiles);
-    const int row0 = block * kManyRows, row1 = min(of.rows, row0 + kManyRows);
-    if (g == 0) no_parts<kManyThreads>(a, ma.sh.many_splits, ma.sh.splits, of.q0, head, row0, row1);
-    if (chunk_tile0 >= chunk_tile1) {
-      no_parts<kManyThreads>(a, g, g + 1, of.q0, head, row0, row1);
-      return;
-    }
-  } else if constexpr (SHARED) {
-    const int on_die = (ma.sh.own_units + 7) / 8, turn = (int)blockIdx.x - group_blocks, unit = (turn & 7) * on_die + (turn >> 3);
-    if (unit >= ma.sh.own_units) return;
-    int rest = unit;
-    r = -1;
-    for (int r0 = 0; r < 0 && r0 < n; r0 += 64) {
-      const int at = min(r0 + lane, n - 1), q0 = a.b.cu_q[at], nq = a.b.cu_q[at + 1] - q0;
-      const Blocks x = blocks_of(ma, 0, q0, nq);
-      const int units = r0 + lane < n && x.rows > 0 ? (x.rows + kManyRows - 1) / kManyRows * a.b.Hkv : 0;
-      int upto = units;
+      return x;
+    };
+    int at, rest;
+    if (count <= 64) {
+      const int units = lane < count ? units_at(lane) : 0, upto = up_to(units);
+      const uint64_t reached = __ballot(upto > unit);
+      if (reached == 0) return;
+      at = __builtin_ctzll(reached);
+      rest = uniform(unit - __shfl(upto - units, at));
+    } else {
+      const int each = (count + kManyThreads - 1) / kManyThreads, i0 = min(tid * each, count), i1 = min(i0 + each, count);
+      int counted = 0;
+      for (int i = i0; i < i1; ++i) counted += units_at(i);
+      int upto = up_to(counted);
+      if (lane == 63) wave_sum[wave] = upto;
+      if (tid == 0) found[0] = -1;
+      __syncthreads();
+      upto -= counted;
 #pragma unroll
-      for (int off = 1; off < 64; off <<= 1) {
-        const int y = __shfl_up(upto, off);
-        if (lane >= off) upto += y;
+      for (int w = 0; w < kManyWaves; ++w)
+        if (w < wave) upto += (int)wave_sum[w];
+      if (unit >= upto && unit < upto + counted) {               // one thread has it
+        int i = i0, left = unit - upto;
+        for (int u = units_at(i); left >= u; u = units_at(i)) { left -= u; ++i; }
+        found[0] = i; found[1] = left;
       }
-      const uint64_t reached = __ballot(upto > rest);
-      if (reached == 0) { rest -= __shfl(upto, 63); continue; }
-      const int owner = __builtin_ctzll(reached);
-      r = r0 + owner;
-      rest -= __shfl(upto - units, owner);
-      of = blocks_of(ma, 0, __shfl(q0, owner), __shfl(nq, owner));
+      __syncthreads();
+      at = uniform(found[0]);
+      if (at < 0) return;
+      rest = uniform(found[1]);
     }
-    if (r < 0) return;
-    r = uniform(r); rest = uniform(rest);
-    of.count = (of.rows + kManyRows - 1) / kManyRows;
-    key_low = uniform(prefix_of(ma.sh, request_of(ma.sh.cu_groups, ma.sh.n_groups, r)));
-    of.len = (int)min((int64_t)kv_len_of(a.b, r), (int64_t)key_low + ma.sh.max_own);
-    of = uniform(of);
-    block = of.count - 1 - rest % of.count;                       // those that see the most keys first
-    head = rest / of.count;
-    g = ma.sh.splits;
-    chunk_tile0 = key_low / kManyKeys;
-    chunk_tile1 = of.len > key_low ? of.tiles(block) : 0;
+    of = blocks_at(at);
+    if (shared) {
+      r = ma.sh.cu_groups[at];
+      of.len = prefix_of(ma.sh, at);
+      of = uniform(of);
+      of.causal = 0;
+      block = rest % of.count;
+      rest /= of.count;
+      g = rest % ma.sh.many_splits;                               // number of the part
+      head = rest / ma.sh.many_splits;
+      const int tiles = (of.len + kManyKeys - 1) / kManyKeys;
+      chunk_tile0 = g * ma.sh.many_tiles;
+      chunk_tile1 = min(tiles, chunk_tile0 + ma.sh.many_tiles);
+      if (g == 0) no_parts<kManyThreads>(a, ma.sh.many_splits, ma.sh.splits, of.q0, head, block * kManyRows, min(of.rows, block * kManyRows + kManyRows));
+    } else {
+      r = at;
+      key_low = prefix_of(ma.sh, request_of(ma.sh.cu_groups, ma.sh.n_groups, r));
+      of.len = (int)min((int64_t)kv_len_of(a.b, r), (int64_t)key_low + ma.sh.max_own);
+      of = uniform(of);
+      block = of.count - 1 - rest % of.count;                     // those that see the most keys first
+      head = rest / of.count;
+      g = ma.sh.splits;
+      chunk_tile0 = key_low / kManyKeys;
+      chunk_tile1 = of.len > key_low ? of.tiles(block) : 0;
+    }
+    r = uniform(r); block = uniform(block); head = uniform(head); g = uniform(g); key_low = uniform(key_low);
+    chunk_tile0 = uniform(chunk_tile0); chunk_tile1 = uniform(chunk_tile1);
     if (chunk_tile0 >= chunk_tile1) {
-      const int row0 = block * kManyRows;
-      no_parts<kManyThreads>(a, g, g + 1, of.q0, head, row0, min(of.rows, row0 + kManyRows));
+      no_parts<kManyThreads>(a, g, g + 1, of.q0, head, block * kManyRows, min(of.rows, block * kManyRows + kManyRows));
       return;
     }
   }

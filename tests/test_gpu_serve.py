@@ -270,6 +270,19 @@ def test_shared_without_tokens_and_many_groups():
     check_shared(f)
 
 
+@pytest.mark.parametrize("page, d", [(16, 64), (1, 128)])
+@pytest.mark.parametrize("n_groups, most", [(90, 3), (40, 5), (700, 2)])
+def test_shared_many_groups_and_prompts(n_groups, most, page, d):
+    """More groups and requests than a wave has lanes, and than a workgroup has threads, some of them empty or without tokens; rows that fill blocks, and that do not."""
+    rng = np.random.default_rng([52, n_groups, d])
+    members = [int(x) for x in rng.integers(0, most, n_groups)]
+    n = sum(members)
+    news = [int(x) for x in rng.choice([0, 1, 1, 2, 9, 40], n)]
+    news[n // 2] = 300
+    f = Forked(rng, members, [int(x) for x in rng.integers(0, 150, n_groups)], news, [x + int(rng.integers(0, 70)) for x in news], n_q=4, n_kv=2, d=d, page=page, loose=70000 // (1 + n_groups // 100))
+    check_shared(f)
+
+
 # requests that have their groups' tables, and no new tokens; groups of 33 to 64 rows under a loose bound (weights of 16 bits in the kernel for many rows); own rows that are joined
 # in one workgroup although there are many of them
 @pytest.mark.parametrize("members, prefixes, news, own, n_q, n_kv, d, page, bounds", [
