@@ -105,7 +105,7 @@ typedef struct codecomp_eviction {
  *   row f + i = row kept[l][r][h][i], K and V bit for bit, and kept_mass[l][r][h][f + i] = mass[l][r][h][kept[l][r][h][i]],  i < m,
  * with kept ascending, -1 from m on (DEVICE int32 [n_layers][n_seqs][n_kv_heads][max_budget], dense), and new_lens[r] = f + m (DEVICE int32 [n_seqs]).  Rows of K and V, and
  * sums, from f + m on stay as they are (codecomp_attend_mass does not read sums of new rows).  kept_mass NULL: `mass` itself; else sums of the same shape
- * elsewhere, and `mass` stays as it is.  new_lens must not be kv_lens.  A row that moves from a page that is not held becomes zeros, one that moves to such a
+ * elsewhere, and `mass` stays as it is.  new_lens must not be kv_lens, budgets or first.  A row that moves from a page that is not held becomes zeros, one that moves to such a
  * page is dropped.  mass->n_layers and n_kv_heads are the pool's, n_seqs the eviction's, width at least max_kv_len. */
 int codecomp_evict(const codecomp_mass* mass, const codecomp_eviction* eviction, const codecomp_pages* pages, int32_t* kept, int32_t* new_lens,
                    const codecomp_mass* kept_mass, void* hip_stream);

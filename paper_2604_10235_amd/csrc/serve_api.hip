@@ -95,7 +95,8 @@ int codecomp_evict(const codecomp_mass* mass, const codecomp_eviction* e, const 
   if (e->table_width < 1 || e->max_kv_len < 0 || e->max_kv_len > (int64_t)e->table_width * pages->page_size || e->max_kv_len > (1 << 30)) return CODECOMP_EINVAL_PAGES;
   if (e->max_kv_len > mass->width) return CODECOMP_EINVAL_SHAPE;
   if (e->max_budget < 1 || e->max_budget > (1 << 30) || e->recent < 0 || e->recent > e->max_budget) return CODECOMP_EINVAL_BUDGET;
-  if (misaligned4(kept) || misaligned4(new_lens) || new_lens == e->kv_lens_dev) return CODECOMP_EINVAL_SHAPE;
+  if (misaligned4(kept) || misaligned4(new_lens)) return CODECOMP_EINVAL_SHAPE;
+  if (new_lens == e->kv_lens_dev || new_lens == e->budgets_dev || new_lens == e->first_dev) return CODECOMP_EINVAL_SHAPE;       // read when it is written
   a.kv_lens = e->kv_lens_dev; a.table = e->table_dev; a.budgets = e->budgets_dev; a.first = e->first_dev;
   a.kept = kept; a.new_lens = new_lens;
   a.n_layers = pages->n_layers; a.n_seqs = e->n_seqs; a.Hkv = pages->n_kv_heads;

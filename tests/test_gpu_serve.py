@@ -211,6 +211,29 @@ def test_shared_infinities_and_nan_among_values_that_are_seen(members, news, n_q
             assert torch.equal(got[~hit], clean[~hit]) and torch.equal(got_lse, lse), (key, x)
 
 
+@pytest.mark.parametrize("members, news, n_q", [([3], [1, 4, 1], 8), ([30], [1] * 30, 8), ([3], [90, 40, 1], 3)])
+@pytest.mark.parametrize("fp8, d", [(False, 128), (True, 64)])
+@pytest.mark.parametrize("loose", [0, 70000])
+def test_shared_nan_among_keys_that_are_seen(members, news, n_q, fp8, d, loose):
+    """A NaN in one key: tokens that see it have NaN everywhere, the others keep their bits."""
+    rng = np.random.default_rng([53, members[0], d])
+    prefix = 205
+    f = Forked(rng, members, [prefix], news, [x + 37 for x in news], n_q=n_q, n_kv=1, d=d, page=16, fp8=fp8, wrong_entries=False, loose=loose)
+    clean, lse = check_shared_bits(f)
+    raw = f.cache.k.view(torch.uint8) if fp8 else f.cache.k
+    r, own = 1, f.lens[1] - news[1]
+    for owner, key in [(0, 0), (0, prefix - 1), (r, prefix), (r, own), (r, f.lens[r] - 1)]:
+        p, at = orc.place(f.cache.table, owner, key, 16, f.cache.n_pages)
+        keep = raw[0, p, 0, at].clone()
+        raw[0, p, 0, at, 3] = 0x7F if fp8 else float("nan")
+        got, got_lse = check_shared_bits(f)
+        raw[0, p, 0, at] = keep
+        hit = torch.zeros(f.T, dtype=torch.bool, device="cuda")
+        hit[slice(None) if key < prefix else slice(int(f.cu[r]) + max(0, key - own), int(f.cu[r + 1]))] = True
+        assert bool(torch.isnan(got[hit]).all()) and bool(torch.isnan(got_lse[hit]).all()), key
+        assert torch.equal(got[~hit], clean[~hit]) and torch.equal(got_lse[~hit], lse[~hit]), key
+
+
 @pytest.mark.parametrize("loose", [0, 70000])
 def test_shared_strides_scale_layers_and_another_stream(loose):
     rng = np.random.default_rng(44)

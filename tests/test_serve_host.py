@@ -160,7 +160,8 @@ def test_evict_refuses():
         assert evict(m, eviction(**bad), p) == code, bad
     assert evict(mass(width=2**31 - 1), eviction(table_width=2**31 - 1, max_kv_len=2**31 - 1), p) == -12
     assert evict(m, e, p, kept=D + 2) == -2 and evict(m, e, p, lens=D + 1) == -2
-    assert evict(m, e, p, lens=D) == -2                              # the lengths themselves
+    assert evict(m, e, p, lens=D) == -2                              # the lengths themselves, the budgets, the numbers of protected rows
+    assert evict(m, eviction(budgets_dev=D + 128), p, lens=D + 128) == -2 and evict(m, eviction(first_dev=D + 192), p, lens=D + 192) == -2
     assert evict(m, e, p, to=mass(width=65)) == -2
     assert evict(m, e, p, to=mass(stride_head=128)) == -2            # the same place with other strides
 
