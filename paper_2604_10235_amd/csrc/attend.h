@@ -35,6 +35,7 @@ struct SharedRows {
   int many_units, many_tiles, many_splits;               // of many: workgroups, tiles of a chunk, chunks
   int splits;                  // the larger one: parts of shared rows that every row has
   int own_units;               // workgroups of the kernel for many rows for what requests have behind the shared rows (one more part); 0: the kernel for few has it
+  int alone;                   // 1: everything is short, and a request's shared rows are attended to with its own ones, by the kernel for few rows: no parts
   int join;                    // 1: whoever has a request's own rows joins the parts of the shared ones to them, and writes the outputs
 };
 // What a row's parts say that had no keys: not to be read any further.

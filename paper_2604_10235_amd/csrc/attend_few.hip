@@ -90,15 +90,15 @@ __device__ __forceinline__ void join_rows(const SharedArgs& a, const float (&own
   }
 }
 
-// EVEN: the strips of all requests and heads form one sequence, cut into equal parts; else a workgroup has one chunk of a request, or (SHARED) of the rows that
-// a group shares, or of a request's rows behind them, and leaves parts of all rows.
-template <int D, bool FP8, int RB, bool EVEN, bool SHARED = false>
-__global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void attend_few_kernel(const std::conditional_t<SHARED, SharedArgs, AttendArgs> a) {
+// EVEN: the strips of all requests and heads form one sequence, cut into equal parts; else a workgroup has one chunk of a request, or (SHARED 1) of the rows that
+// a group shares, or of a request's rows behind them, and leaves parts of all rows, or (2) all rows of a request, the shared ones among them.
+template <int D, bool FP8, int RB, bool EVEN, int SHARED = 0>
+__global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void attend_few_kernel(const std::conditional_t<SHARED != 0, SharedArgs, AttendArgs> a) {
   using T = FewTile<D, FP8>;
   constexpr int KS = D / 32, DB = D / 16;
   __shared__ __attribute__((aligned(16))) unsigned char lds[kFewWaves * T::BYTES];
   __shared__ float row_m[kFewWaves][16], row_l[kFewWaves][16];
-  __shared__ __attribute__((aligned(16))) float own_o[SHARED ? 16 : 1][D], own_ml[SHARED ? 16 : 1][2];       // what the workgroup joins the shared rows' parts to
+  __shared__ __attribute__((aligned(16))) float own_o[SHARED == 1 ? 16 : 1][D], own_ml[SHARED == 1 ? 16 : 1][2];       // what the workgroup joins the shared rows' parts to
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
   int l16 = lane & 15, quarter = lane >> 4;
   int r, head, row0, key0, share = 0, strip = 0;                 // request, head, first of this workgroup's rows, first of its keys
@@ -107,9 +107,18 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void atten
   // Entries of the page table for keys tile + l16 and 16 + tile + l16, not looked at before they are needed.  Those of the first two tiles are sent for
   // before it is known how many keys there are: one wait less.
   int page[2], next_page[2];
+  const int32_t* lead_table = nullptr;                           // SHARED 2: of the group's first request, for the shared rows
+  int lead_keys = 0;
+  auto table_of = [&](int key) __attribute__((always_inline)) {
+    if constexpr (SHARED == 2) return key < lead_keys ? lead_table : table;
+    return table;
+  };
   auto look_up = [&](int (&pg)[2], int tile, int end) __attribute__((always_inline)) {
 #pragma unroll
-    for (int b = 0; b < 2; ++b) pg[b] = table[max(min(tile + 16 * b + l16, end - 1), 0) >> a.pool.page_log2];
+    for (int b = 0; b < 2; ++b) {
+      const int key = max(min(tile + 16 * b + l16, end - 1), 0);
+      pg[b] = table_of(key)[key >> a.pool.page_log2];
+    }
   };
   int64_t total = 0, shares = 0, at_strip = 0;
   CutBlock cut = {-1, 0, 0, 0};
@@ -156,6 +165,23 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void atten
     }
     __syncthreads();
     r = uniform(found[0]); strip = uniform(found[1]);
+  } else if constexpr (SHARED == 2) {
+    const int item = blockIdx.x / a.row_parts;
+    row0 = ((int)blockIdx.x - item * a.row_parts) * (16 * RB);
+    r = item / a.b.Hkv; head = item - r * a.b.Hkv;
+    shared_q0 = a.b.cu_q[r];
+    shared_nq = a.b.cu_q[r + 1] - shared_q0;
+    if (shared_nq * a.b.G <= row0) return;
+    const int g = uniform(request_of(a.sh.cu_groups, a.sh.n_groups, r));
+    lead_keys = uniform(prefix_of(a.sh, g));
+    shared_len = uniform((int)min((int64_t)kv_len_of(a.b, r), (int64_t)lead_keys + a.sh.max_own));
+    lead_table = a.b.table + (int64_t)a.sh.cu_groups[g] * a.b.table_width;
+    table = a.b.table + (int64_t)r * a.b.table_width;
+    key0 = 0;
+    key_end = shared_len;
+    causal = a.b.causal;
+    look_up(page, wave * kFewKeys, key_end);
+    look_up(next_page, (kFewWaves + wave) * kFewKeys, key_end);
   } else if constexpr (SHARED) {
     const bool group = (int)blockIdx.x < a.sh.few_units;
     const int unit = group ? blockIdx.x : blockIdx.x - a.sh.few_units, parts = group ? a.sh.few_parts : a.row_parts;
@@ -226,7 +252,7 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void atten
       look_up(next_page, key0 + (kFewWaves + wave) * kFewKeys, key1);
     } else if constexpr (SHARED) {
       key1 = causal ? min(key_end, len - nq + (min(row0 + 16 * RB, rows) - 1) / a.b.G + 1) : key_end;       // nothing behind what the last row sees
-      whole = shared_join;
+      whole = SHARED == 2 || shared_join;
     } else {
       if (rows <= row0 || rows > a.row_slots) return;
       key1 = min(len, key0 + a.chunk);
@@ -400,7 +426,7 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void atten
     if (__builtin_expect(__ballot(left_out != 0) != 0, 0)) {
       // from the first tile that was cleaned on: the keys before seen_by_all in it were as well
       for (int key = SHARED ? key0 + (max(seen_by_all - key0, 0) & -kFewKeys) : max(seen_by_all & -kFewKeys, key0); key < key1; ++key) {
-        const int at = table[key >> a.pool.page_log2];
+        const int at = table_of(key)[key >> a.pool.page_log2];
         if ((key - key0) / kFewKeys % kFewWaves != wave || at < 0 || at >= a.pool.n_pages) continue;          // another wave's
         const unsigned char* row = a.pool.v + a.layer + head * a.pool.s_head + at * a.pool.s_page + (key & in_page) * a.pool.s_tok;
 #pragma unroll
@@ -447,7 +473,7 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void atten
 #pragma unroll
           for (int i = 0; i < E; ++i) x[i] += f * o_lds[(w * 16 + n) * O_ROW + e + i];
         }
-        if (SHARED && whole) {                                     // joined below
+        if (SHARED == 1 && whole) {                                     // joined below
 #pragma unroll
           for (int i = 0; i < E; ++i) own_o[n][e + i] = x[i];
           if ((tid & 15) == 0) { own_ml[n][0] = to; own_ml[n][1] = all; }
@@ -465,7 +491,7 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void atten
           if ((tid & 15) == 0) { a.part_ml[2 * part] = to; a.part_ml[2 * part + 1] = all; }
         }
       }
-      if constexpr (SHARED) {
+      if constexpr (SHARED == 1) {
         if (shared_join) {
           __syncthreads();
           join_rows<D, 16>(a, own_o, own_ml, q0, head, row0 + rb * 16, rows, a.sh.splits);
@@ -615,8 +641,13 @@ int launch_join_own(int d, int64_t units, const SharedArgs& a, hipStream_t strea
 template <int D, bool FP8>
 static int launch_few_shared_of(bool two_blocks, int64_t units, const SharedArgs& a, hipStream_t stream) {
   const dim3 grid((unsigned)units), block(64 * kFewWaves);
-  if (two_blocks) attend_few_kernel<D, FP8, 2, false, true><<<grid, block, 0, stream>>>(a);
-  else attend_few_kernel<D, FP8, 1, false, true><<<grid, block, 0, stream>>>(a);
+  if (a.sh.alone) {
+    if (two_blocks) attend_few_kernel<D, FP8, 2, false, 2><<<grid, block, 0, stream>>>(a);
+    else attend_few_kernel<D, FP8, 1, false, 2><<<grid, block, 0, stream>>>(a);
+  } else {
+    if (two_blocks) attend_few_kernel<D, FP8, 2, false, 1><<<grid, block, 0, stream>>>(a);
+    else attend_few_kernel<D, FP8, 1, false, 1><<<grid, block, 0, stream>>>(a);
+  }
   return (int)hipGetLastError();
 }
 

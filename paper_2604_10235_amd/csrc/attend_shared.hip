@@ -6,7 +6,8 @@
 //
 // Groups of many rows: the kernel of attend_many.h, whose blocks of 256 rows share keys and values through LDS.  Groups of few: that of
 // attend_few.hip, which reads keys and values once for up to 32 rows.  Rows behind the shared ones: the kernel for few rows, in which whoever has the rows joins the
-// parts of the shared ones to them, or, for prompts, the kernel for many, in the same launch as the shared rows.
+// parts of the shared ones to them, or, for prompts, the kernel for many, in the same launch as the shared rows.  Where all is short nothing is shared: the kernel for few rows
+// takes a request's shared and own rows together.
 //
 // Single tokens wait for memory, and shared rows are read once for all: 64 steps of 28 query heads on 4 KV heads of 128 over 32768 shared rows and up to 700 of their own, 63 us
 // where codecomp_attend over the same caches takes 470 (the shared rows 42, by 448 rows in blocks of 256: 1.33 PFLOP/s of the products that are formed; their own 19, of which
@@ -33,8 +34,12 @@ extern template int launch_many_shared_of<128, true>(const ManyArgs&, hipStream_
 constexpr int kChip = 256;                       // compute units: workgroups of the kernel for many rows that run at once
 constexpr int64_t kMostBlocks = (1 << 23) - 1;    // of up to 512 threads: an axis of a grid holds 2^32 threads
 constexpr int kMostSplits = 1024;
+// Up to so many keys in all nothing is cut, shared rows are read once for every 16 or 32 rows, and there is nothing to join: one launch (us, with parts | without: 64 steps behind 16
+// rows 10.7 | 7.1, 1024 behind 300, 8 bits, 133 | 118, 226 tokens behind 47 24 | 12, 1000 requests of up to 20 tokens behind 400 426 | 384; beyond: 8 steps behind 700 11.7 | 15.7,
+// 256 behind 500 and up to 300 of their own 42 | 53, two prompts of 600 tokens 44 | 52).
+constexpr int kAloneKeys = 512;
 // Little work, in strips of 128 keys by 32 rows: all of it in one launch of the kernel for few rows, and one that joins (us, one | the kernel for many as well: 64 steps of 7 query
-// heads on 4 KV heads behind 1000 rows, 448 strips, 22 | 28, 2048 25 | 28, 4096 30 | 30; 16 steps behind 8000, 1008 strips, 26.5 | 26, 16000 33 | 30; 226 tokens behind 47 24 | 29).
+// heads on 4 KV heads behind 1000 rows, 448 strips, 22 | 28, 2048 25 | 28, 4096 30 | 30; 16 steps behind 8000, 1008 strips, 26.5 | 26, 16000 33 | 30).
 constexpr int64_t kFewStrips = 1024;
 // Groups of 33 to 64 rows: the kernel for few rows reads the shared rows twice, the one for many has most of a block empty, but a tile's keys for all of it at once (us,
 // few | many: one group of 56 rows behind 2000 rows 14 | 23, 8192 24 | 27, 32768 36 | 39; eight behind 2000 to 9000 50 | 45, head_dim 64 31 | 34; 8 bits, 48 rows, 52 | 66:
@@ -76,6 +81,18 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
   s.cu_groups = g->cu_groups_dev; s.prefix_lens = g->prefix_lens_dev;
   s.n_groups = g->n_groups; s.max_prefix = g->max_prefix_len; s.max_own = g->max_own_len;
   int64_t few_most = 0, blocks = 0, own_most = 0;
+  const int64_t items = (int64_t)x.n_seqs * x.Hkv;
+  for (int r = 0; r < x.n_seqs; ++r) own_most = std::max(own_most, (int64_t)(b->cu_q_host[r + 1] - b->cu_q_host[r]) * x.G);
+  if (s.max_prefix + (int64_t)s.max_own <= kAloneKeys) {
+    pl->own_two = own_most > 16;
+    pl->row_parts = std::max<int>(1, (int)((own_most + (pl->own_two ? 31 : 15)) / (pl->own_two ? 32 : 16)));
+    pl->own_units = items * pl->row_parts;
+    if (pl->own_units > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
+    pl->few_groups = pl->many_groups = pl->few_two = pl->chunk = pl->own_splits = 0;
+    s.alone = 1;
+    pl->ws_bytes = 0;
+    return CODECOMP_OK;
+  }
   pl->few_groups = pl->many_groups = 0;
   int64_t middle = 0, strips = 0;                  // groups of more than 32 rows that either kernel can take; strips of 128 keys that the one for few takes, 32 rows at a time
   for (int i = 0; i < g->n_groups; ++i) {
@@ -102,7 +119,6 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
   int64_t own_blocks = 0;                          // of rows, if the kernel for many rows has the own ones too
   for (int r = 0; r < x.n_seqs; ++r) {
     const int64_t rows = (int64_t)(b->cu_q_host[r + 1] - b->cu_q_host[r]) * x.G;
-    own_most = std::max(own_most, rows);
     own_blocks += (rows + kManyRows - 1) / kManyRows;
   }
   if (own_most <= kOwnRows || s.max_own == 0 || pl->many_groups == 0) own_blocks = 0;
@@ -110,7 +126,7 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
   blocks *= x.Hkv;
   if (blocks + own_blocks > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
   s.own_units = (int)own_blocks;
-  const int64_t items = (int64_t)x.n_seqs * x.Hkv, own_parts = (own_most + 31) / 32;
+  const int64_t own_parts = (own_most + 31) / 32;
   s.join = pl->many_groups > 0 && (s.own_units > 0 || s.max_own <= kJoinKeys || items * own_parts >= kJoinItems);
   pl->few_two = s.join ? few_most > 16 : std::max(few_most, own_most) > 16;
   pl->own_two = s.join ? own_most > 16 : pl->few_two;
@@ -235,6 +251,7 @@ int launch_shared(const SharedPlan& pl, const void* q, int layer, void* out, flo
   a.c = fminf(fmaxf(pl.scale * pl.pool.k_scale * kLog2e, FLT_MIN), FLT_MAX);       // a hidden logit of minus infinity times it stays one
   a.chunk = pl.chunk; a.row_parts = pl.row_parts;
   a.sh = pl.sh;
+  if (pl.sh.alone) return launch_few_shared(pl.d, pl.pool.fp8, pl.own_two, pl.own_units, a, stream);
   const int parts = pl.sh.splits + (pl.sh.join ? pl.sh.own_units > 0 : pl.own_splits);
   const int64_t rows = (int64_t)pl.batch.T * pl.batch.Hq;
   a.part_o = static_cast<float*>(workspace);

@@ -26,13 +26,14 @@ def scales(fp8):
 
 class Forked:
     """Groups of requests; the table of a group's first request holds the shared rows, the others' entries for whole shared pages are numbers of no page.  `loose`: the bound on
-    lengths that calls are told, with which there may be much work: what is little goes to one kernel whatever its rows."""
+    lengths that calls are told, under which there may be some work, or much: what is short, or little, goes to one kernel whatever its rows."""
 
     def __init__(self, rng, members, prefixes, news, owns, *, n_q, n_kv, d, page, fp8=False, layers=1, wrong_entries=True, width_more=0, loose=0):
-        self.loose, width_more = loose, max(width_more, -(-loose // page))
         self.of = [g for g, n in enumerate(members) for _ in range(n)]
         self.members, self.prefixes, self.news, self.n_q = members, prefixes, news, n_q
         self.lens = [prefixes[g] + max(o, 0) for g, o in zip(self.of, owns)]
+        self.loose = loose and max([loose] + self.lens)
+        width_more = max(width_more, -(-loose // page))
         self.cache = cu_.Cache(rng, self.lens, n_kv=n_kv, d=d, page=page, fp8=fp8, layers=layers, width_more=width_more, **scales(fp8))
         self.cu_groups = cum(members)
         if wrong_entries:
@@ -106,7 +107,7 @@ SHARED = [
 
 
 @pytest.mark.parametrize("members, prefixes, news, owns, n_q, n_kv, d, page, fp8", SHARED, ids=range(len(SHARED)))
-@pytest.mark.parametrize("loose", [0, 70000])
+@pytest.mark.parametrize("loose", [0, 1100, 70000])
 @pytest.mark.parametrize("causal", [True, False])
 def test_shared(members, prefixes, news, owns, n_q, n_kv, d, page, fp8, causal, loose):
     rng = np.random.default_rng([sum(prefixes), sum(owns), n_q, page])
@@ -127,7 +128,7 @@ def test_shared_with_loose_bounds(case, max_prefix, max_own):
 @pytest.mark.parametrize("members, news", [([3], [1, 1, 1]), ([30], [1] * 30)])
 @pytest.mark.parametrize("fp8", [False, True])
 @pytest.mark.parametrize("page", [8, 32])
-@pytest.mark.parametrize("loose", [0, 70000])
+@pytest.mark.parametrize("loose", [0, 1100, 70000])
 def test_shared_pages_that_are_not_held_and_lengths_out_of_range(members, news, fp8, page, loose):
     rng = np.random.default_rng([41, members[0], page])
     n = members[0]
@@ -154,7 +155,7 @@ def test_shared_pages_that_are_not_held_and_lengths_out_of_range(members, news, 
 
 @pytest.mark.parametrize("members, news, n_q", [([3], [1, 4, 1], 8), ([30], [1] * 30, 8), ([2], [60, 33], 4)])
 @pytest.mark.parametrize("fp8, d", [(False, 128), (True, 64)])
-@pytest.mark.parametrize("loose", [0, 70000])
+@pytest.mark.parametrize("loose", [0, 1100, 70000])
 def test_shared_garbage_in_places_that_are_not_seen(members, news, n_q, fp8, d, loose):
     """NaN in rows behind the last one of a request, in the others' copies of the page that the shared rows end in, and in pages that are nobody's."""
     rng = np.random.default_rng([42, members[0], d])
@@ -185,7 +186,7 @@ def check_shared_bits(f, causal=True):
 
 @pytest.mark.parametrize("members, news, n_q", [([3], [1, 4, 1], 8), ([30], [1] * 30, 8), ([2], [60, 33], 4), ([3], [90, 40, 1], 3)])
 @pytest.mark.parametrize("fp8, d, page", [(False, 128, 32), (True, 64, 8), (False, 64, 256)])
-@pytest.mark.parametrize("loose", [0, 70000])
+@pytest.mark.parametrize("loose", [0, 1100, 70000])
 def test_shared_infinities_and_nan_among_values_that_are_seen(members, news, n_q, fp8, d, page, loose):
     """One element of one value row: that element of every token that sees the row is infinite or NaN, everything else keeps its bits."""
     rng = np.random.default_rng([43, members[0], d])
@@ -213,7 +214,7 @@ def test_shared_infinities_and_nan_among_values_that_are_seen(members, news, n_q
 
 @pytest.mark.parametrize("members, news, n_q", [([3], [1, 4, 1], 8), ([30], [1] * 30, 8), ([3], [90, 40, 1], 3)])
 @pytest.mark.parametrize("fp8, d", [(False, 128), (True, 64)])
-@pytest.mark.parametrize("loose", [0, 70000])
+@pytest.mark.parametrize("loose", [0, 1100, 70000])
 def test_shared_nan_among_keys_that_are_seen(members, news, n_q, fp8, d, loose):
     """A NaN in one key: tokens that see it have NaN everywhere, the others keep their bits."""
     rng = np.random.default_rng([53, members[0], d])
@@ -234,7 +235,7 @@ def test_shared_nan_among_keys_that_are_seen(members, news, n_q, fp8, d, loose):
         assert torch.equal(got[~hit], clean[~hit]) and torch.equal(got_lse[~hit], lse[~hit]), key
 
 
-@pytest.mark.parametrize("loose", [0, 70000])
+@pytest.mark.parametrize("loose", [0, 1100, 70000])
 def test_shared_strides_scale_layers_and_another_stream(loose):
     rng = np.random.default_rng(44)
     f = Forked(rng, [3, 9], [100, 230], [1, 2, 1] + [1] * 9, [9] * 12, n_q=8, n_kv=2, d=64, page=16, layers=3, loose=loose)
@@ -254,7 +255,7 @@ def test_shared_strides_scale_layers_and_another_stream(loose):
 
 
 @pytest.mark.parametrize("members, n_q", [([4], 8), ([30], 8), ([2, 28], 8)])
-@pytest.mark.parametrize("loose", [0, 70000])
+@pytest.mark.parametrize("loose", [0, 1100, 70000])
 def test_shared_captured_calls_follow_lengths_and_tables(members, n_q, loose):
     rng = np.random.default_rng([45, members[0]])
     n = sum(members)
@@ -316,18 +317,18 @@ def test_shared_many_groups_and_prompts(n_groups, most, page, d):
     # own rows in the kernel for many rows: of single tokens and prompts beside one another, causal within a block and behind its end, shared rows that end inside a tile
     ([9, 2, 1], [205, 90, 0], [1, 70, 0, 3, 1, 33, 1, 9, 1, 1, 2, 150], 300, 8, 2, 64, 16, {}), ([5, 4], [1000, 63], [300, 1, 129, 2, 40, 1, 1, 1, 90], 400, 14, 2, 128, 1, {}),
     ([30], [129], [1, 9] * 15, 200, 16, 4, 128, 128, dict(max_kv=5000, max_prefix=5000, max_own=4000)), ([2, 1], [320, 64], [65, 64, 300], 1, 4, 4, 64, 64, {})])
-@pytest.mark.parametrize("loose", [0, 70000])
+@pytest.mark.parametrize("loose", [0, 1100, 70000])
 @pytest.mark.parametrize("causal", [True, False])
 def test_shared_kinds_of_groups(members, prefixes, news, own, n_q, n_kv, d, page, bounds, causal, loose):
     rng = np.random.default_rng([47, own, page])
     owns = [max(n, int(x)) for n, x in zip(news, rng.integers(0, own, sum(members)))]
     if loose:
-        bounds = {"max_own": bounds.get("max_own")}
+        bounds = {"max_own": min(bounds["max_own"], loose)} if "max_own" in bounds else {}
     more = (bounds.get("max_kv", 0)) // page
     check_shared(Forked(rng, members, prefixes, news, owns, n_q=n_q, n_kv=n_kv, d=d, page=page, width_more=more, loose=loose), causal=causal, **bounds)
 
 
-@pytest.mark.parametrize("loose", [0, 70000])
+@pytest.mark.parametrize("loose", [0, 1100, 70000])
 def test_shared_pool_with_strides_of_its_own(loose):
     rng = np.random.default_rng(48)
     f = Forked(rng, [3, 30], [140, 333], [1, 3, 2] + [1] * 30, [7] * 33, n_q=8, n_kv=2, d=64, page=16, layers=2, loose=loose)
@@ -338,7 +339,7 @@ def test_shared_pool_with_strides_of_its_own(loose):
 
 
 @pytest.mark.parametrize("members", [[3], [30], [2, 28]])
-@pytest.mark.parametrize("loose", [0, 70000])
+@pytest.mark.parametrize("loose", [0, 1100, 70000])
 def test_shared_two_graphs_and_two_streams(members, loose):
     """Graphs replayed one after the other on one workspace; calls at the same time on workspaces of their own."""
     rng = np.random.default_rng([49, members[0]])
@@ -384,7 +385,7 @@ def far_away(cache):
 
 @pytest.mark.parametrize("members", [[3], [30]])
 @pytest.mark.parametrize("fp8", [False, True])
-@pytest.mark.parametrize("loose", [0, 70000])
+@pytest.mark.parametrize("loose", [0, 1100, 70000])
 def test_shared_offsets_beyond_32_bits(members, fp8, loose):
     rng = np.random.default_rng([50, members[0]])
     n = members[0]

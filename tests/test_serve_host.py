@@ -120,6 +120,8 @@ def test_shared_refuses_pointers_layers_and_workspaces():
     assert shared(x, g, p, q=None) == -1 and shared(x, g, p, out=None) == -1
     assert shared(x, g, p, layer=2) == -12 and shared(x, g, p, layer=-1) == -12
     assert shared(x, g, p, q=D + 2) == -2 and shared(x, g, p, out=D + 8) == -2 and shared(x, g, p, lse=D + 2) == -2
+    assert b.lib().codecomp_attend_shared_workspace_bytes(ref(x), ref(g), ref(p)) == 0             # short: no parts
+    x, g = batch(table_width=64, max_kv_len=1024), groups(max_prefix_len=700)
     need = b.lib().codecomp_attend_shared_workspace_bytes(ref(x), ref(g), ref(p))
     assert need >= 3 * 28 * 130 * 4                                  # a part at least of every row
     for bad in (dict(ws=None), dict(ws=D + 16), dict(ws=D + 128), dict(size=need - 1), dict(size=0)):
