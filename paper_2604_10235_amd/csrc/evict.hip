@@ -15,6 +15,8 @@
 // which come from 256 bytes here and there, 4.1 TB/s; one layer of 1088 rows to 1024: 8 and 8 us, a chain of waits for counts and numbers.
 // Tried before: digits of 11 bits (three passes; as long); the next batch sent for before one is written (as long: it is the scattered rows, not the wait);
 // loads that may stay in the caches instead of those that pass by them (651 us instead of 637 for the steps above, 1307 instead of 1313 for 8 bits).
+#include <algorithm>
+
 #include "serve.h"
 
 namespace codecomp {
@@ -28,8 +30,9 @@ constexpr int kBothThreads = 512, kBothDeep = 4;
 // Fewer threads where requests are short (1656 problems of up to 83 rows, us, 512 | 256 | 128 threads: 28 | 13 | 10; 28 layers, 32 requests of up to 500: 147 | 144 | 148; 8 of 900:
 // 132 | 128 | 152).
 constexpr int kShortRows = 1024, kShortThreads = 256;
-// And always where they have next to no rows (4 heads, two kernels | one: 130 rows 11.0 | 9.5, 500 12.7 | 18.6; 288 problems of up to 32 rows 13.0 | 7.6).
-constexpr int kTinyRows = 192;
+// And always where few rows are kept of what registers hold (us, two kernels | one: 288 problems of up to 32 rows 13.0 | 7.6; 4 heads, 50 of 1000 rows 10.1 | 8.7, 50 of 4000 13.6 | 9.9, of
+// 8000 13.6 | 18.0; 224 heads, 64 of 2000 15.1 | 11.6, 256 26.1 | 23.9; 4 heads, 400 of 500 12.7 | 18.6).
+constexpr int kFewKept = 256, kHeldRows = 4096;
 // Two kernels: threads of a workgroup that moves rows (one request of 32768, us: 512 threads 97, 1024 85), and pieces that each has in flight (2, 4, 8: 85, 87, 87).
 constexpr int kMoveThreads = 1024, kMoveDeep = 2;
 // Rows of 256 bytes are cut into two stretches of 128 where there are fewer workgroups than compute units (114 us -> 98), and down to 32 where there are very few and
@@ -309,7 +312,7 @@ int launch_evict(const EvictArgs& a, int d, hipStream_t stream) {
   while (problems * 2 * slices < kFewest && slices < pieces / 8) slices *= 2;
   while (problems * 2 * slices < kFewer && slices < pieces / 2 && a.max_budget > kManyRows) slices *= 2;
   if (problems * 2 * slices > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
-  if (a.max_kv <= kTinyRows || (problems >= kManyProblems && a.max_kv <= kBothRows)) {
+  if ((std::min(a.max_budget, a.max_kv) <= kFewKept && a.max_kv <= kHeldRows) || (problems >= kManyProblems && a.max_kv <= kBothRows)) {
     if (pieces == 16) return launch_both<16>(a, problems, stream);
     return pieces == 8 ? launch_both<8>(a, problems, stream) : launch_both<4>(a, problems, stream);
   }

@@ -798,7 +798,7 @@ def test_evict_of_few_and_many_problems(n):
         check_evict(np.random.default_rng([63, n, layers, rows]), [rows] * n, [budget] * n, recent=10, max_budget=budget, first=[7] * n, n_kv=2, d=128, layers=layers)
 
 
-@pytest.mark.parametrize("n, rows, budget", [(102, 190, 60), (102, 1000, 60), (102, 1100, 60), (102, 4500, 60), (3, 2048, 70), (3, 2049, 1500), (3, 8193, 80), (3, 16385, 4000)])
+@pytest.mark.parametrize("n, rows, budget", [(102, 190, 60), (102, 1000, 60), (102, 1100, 60), (102, 4500, 60), (3, 2048, 70), (3, 2048, 700), (3, 2049, 1500), (3, 4097, 80), (3, 8193, 80), (3, 16385, 4000)])
 @pytest.mark.parametrize("d, fp8", [(64, True), (128, False), (64, False)])
 def test_evict_around_the_sizes_that_decide(n, rows, budget, d, fp8):
     """Requests that are as long as the bound, one that is not, and one that is empty."""
