@@ -136,7 +136,6 @@ __device__ __forceinline__ s16x4 read_columns(const unsigned char* lds) {
 }
 
 int launch_few(const AttendPlan& pl, const AttendArgs& a, hipStream_t stream);
-int launch_join_own(int d, int64_t units, const SharedArgs& a, hipStream_t stream);
 int launch_few_shared(int d, bool fp8, bool two_blocks, int64_t units, const SharedArgs& a, hipStream_t stream);
 
 }  // namespace codecomp

@@ -48,10 +48,10 @@ __device__ __forceinline__ int strips_of(const AttendArgs& a, int r) {
 }
 
 // 16 rows of a request's own keys, from row0 on, joined to the parts of the shared ones: D / 4 threads a row.  Parts come from memory (other dies wrote them):
-// LOT are sent for at a time, and the reference moves on from one lot to the next.
-template <int D, int LOT>
-__device__ __forceinline__ void join_rows(const SharedArgs& a, const float (&own_o)[16][D], const float (&own_ml)[16][2], int q0, int head, int row0, int rows, int parts) {
-  constexpr int THREADS = D / 4;
+// as many as registers hold are sent for at a time, and the reference moves on from one lot to the next.
+template <int D>
+__device__ __forceinline__ void join_rows(const SharedArgs& a, const float (&own_o)[16][D], const float (&own_ml)[16][2], int q0, int head, int row0, int rows) {
+  constexpr int THREADS = D / 4, LOT = 16;
   const int e = threadIdx.x % THREADS * 4;
   for (int n = threadIdx.x / THREADS; n < 16; n += 64 * kFewWaves / THREADS) {
     const int row = row0 + n, t = row / a.b.G, h = head * a.b.G + row - t * a.b.G;
@@ -59,14 +59,14 @@ __device__ __forceinline__ void join_rows(const SharedArgs& a, const float (&own
     const int64_t at = part_at(a, 0, q0 + t, h), step = (int64_t)a.b.T * a.b.Hq;
     float top = own_ml[n][0], all = own_ml[n][1];
     f32x4 x = *reinterpret_cast<const f32x4*>(&own_o[n][e]);
-    for (int p0 = 0; p0 < parts; p0 += LOT) {
+    for (int p0 = 0; p0 < a.sh.splits; p0 += LOT) {
       f32x4 v[LOT];
       float m[LOT], l[LOT], to = top;
 #pragma unroll
       for (int i = 0; i < LOT; ++i) {
-        const int64_t part = at + min(p0 + i, parts - 1) * step;
+        const int64_t part = at + min(p0 + i, a.sh.splits - 1) * step;
         m[i] = a.part_ml[2 * part];
-        l[i] = p0 + i < parts ? a.part_ml[2 * part + 1] : kNoPart;
+        l[i] = p0 + i < a.sh.splits ? a.part_ml[2 * part + 1] : kNoPart;
         v[i] = *reinterpret_cast<const f32x4*>(a.part_o + part * D + e);
       }
 #pragma unroll
@@ -494,7 +494,7 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void atten
       if constexpr (SHARED == 1) {
         if (shared_join) {
           __syncthreads();
-          join_rows<D, 16>(a, own_o, own_ml, q0, head, row0 + rb * 16, rows, a.sh.splits);
+          join_rows<D>(a, own_o, own_ml, q0, head, row0 + rb * 16, rows);
         }
       }
     }
@@ -615,27 +615,6 @@ static int launch_few_rows(const AttendArgs& a, hipStream_t stream) {
 int launch_few(const AttendPlan& pl, const AttendArgs& a, hipStream_t stream) {
   if (pl.d == 128) return pl.pool.fp8 ? launch_few_rows<128, true>(a, stream) : launch_few_rows<128, false>(a, stream);
   return pl.pool.fp8 ? launch_few_rows<64, true>(a, stream) : launch_few_rows<64, false>(a, stream);
-}
-
-// All parts joined, where the kernel for many rows has had requests' own keys too: 32 rows of a request and head a workgroup.
-template <int D>
-__global__ __launch_bounds__(64 * kFewWaves) void join_own_kernel(const SharedArgs a) {
-  __shared__ __attribute__((aligned(16))) float none_o[16][D], none_ml[16][2];
-  const int item = blockIdx.x / a.row_parts, row0 = (blockIdx.x - item * a.row_parts) * 32, r = item / a.b.Hkv, head = item - r * a.b.Hkv;
-  const int q0 = a.b.cu_q[r], rows = (a.b.cu_q[r + 1] - q0) * a.b.G;
-  if (rows <= row0) return;
-  for (int i = threadIdx.x; i < 16 * D; i += 64 * kFewWaves) none_o[i / D][i % D] = 0.0f;
-  if (threadIdx.x < 16) { none_ml[threadIdx.x][0] = -INFINITY; none_ml[threadIdx.x][1] = 0.0f; }
-  __syncthreads();
-#pragma unroll
-  for (int rb = 0; rb < 2; ++rb) join_rows<D, 4>(a, none_o, none_ml, q0, head, row0 + rb * 16, rows, a.sh.splits + 1);
-}
-
-int launch_join_own(int d, int64_t units, const SharedArgs& a, hipStream_t stream) {
-  const dim3 grid((unsigned)units), block(64 * kFewWaves);
-  if (d == 128) join_own_kernel<128><<<grid, block, 0, stream>>>(a);
-  else join_own_kernel<64><<<grid, block, 0, stream>>>(a);
-  return (int)hipGetLastError();
 }
 
 template <int D, bool FP8>

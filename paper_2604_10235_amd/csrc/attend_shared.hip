@@ -33,11 +33,12 @@ extern template int launch_many_shared_of<128, true>(const ManyArgs&, hipStream_
 
 constexpr int kChip = 256;                       // compute units: workgroups of the kernel for many rows that run at once
 constexpr int64_t kMostBlocks = (1 << 23) - 1;    // of up to 512 threads: an axis of a grid holds 2^32 threads
-constexpr int kMostSplits = 1024;
+constexpr int64_t kMostSplits = 1024, kMostParts = 1 << 21;       // chunks of a request's keys; of all rows together, where there are more than eight chunks: workspace
 // Up to so many keys in all nothing is cut, shared rows are read once for every 16 or 32 rows, and there is nothing to join: one launch (us, with parts | without: 64 steps behind 16
 // rows 10.7 | 7.1, 1024 behind 300, 8 bits, 133 | 118, 226 tokens behind 47 24 | 12, 1000 requests of up to 20 tokens behind 400 426 | 384; beyond: 8 steps behind 700 11.7 | 15.7,
 // 256 behind 500 and up to 300 of their own 42 | 53, two prompts of 600 tokens 44 | 52).
 constexpr int kAloneKeys = 512;
+constexpr int64_t kEmptyBlocks = 4096;
 // Little work, in strips of 128 keys by 32 rows: all of it in one launch of the kernel for few rows, and one that joins (us, one | the kernel for many as well: 64 steps of 7 query
 // heads on 4 KV heads behind 1000 rows, 448 strips, 22 | 28, 2048 25 | 28, 4096 30 | 30; 16 steps behind 8000, 1008 strips, 26.5 | 26, 16000 33 | 30).
 constexpr int64_t kFewStrips = 1024;
@@ -82,29 +83,40 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
   s.n_groups = g->n_groups; s.max_prefix = g->max_prefix_len; s.max_own = g->max_own_len;
   int64_t few_most = 0, blocks = 0, own_most = 0;
   const int64_t items = (int64_t)x.n_seqs * x.Hkv;
-  for (int r = 0; r < x.n_seqs; ++r) own_most = std::max(own_most, (int64_t)(b->cu_q_host[r + 1] - b->cu_q_host[r]) * x.G);
-  if (s.max_prefix + (int64_t)s.max_own <= kAloneKeys) {
+  int64_t own_parts = 0;                           // of 32 rows, of all requests
+  for (int r = 0; r < x.n_seqs; ++r) {
+    const int64_t rows = (int64_t)(b->cu_q_host[r + 1] - b->cu_q_host[r]) * x.G;
+    own_most = std::max(own_most, rows);
+    own_parts += (rows + 31) / 32;
+  }
+  // The kernel for few rows has workgroups for as many parts of every request, or group, as the largest one has: not where most of them would find nothing.
+  auto alike = [&](int64_t count, int64_t most, int64_t parts) { return count * ((most + 31) / 32) * x.Hkv <= 4 * parts * x.Hkv + kEmptyBlocks; };
+  if (s.max_prefix + (int64_t)s.max_own <= kAloneKeys && alike(x.n_seqs, own_most, own_parts)) {
     pl->own_two = own_most > 16;
     pl->row_parts = std::max<int>(1, (int)((own_most + (pl->own_two ? 31 : 15)) / (pl->own_two ? 32 : 16)));
     pl->own_units = items * pl->row_parts;
     if (pl->own_units > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
     pl->few_groups = pl->many_groups = pl->few_two = pl->chunk = pl->own_splits = 0;
+    pl->prompts = false;
     s.alone = 1;
     pl->ws_bytes = 0;
     return CODECOMP_OK;
   }
   pl->few_groups = pl->many_groups = 0;
   int64_t middle = 0, strips = 0;                  // groups of more than 32 rows that either kernel can take; strips of 128 keys that the one for few takes, 32 rows at a time
+  int64_t group_most = 0, group_parts = 0;
   for (int i = 0; i < g->n_groups; ++i) {
     const int64_t rows = (int64_t)(b->cu_q_host[g->cu_groups_host[i + 1]] - b->cu_q_host[g->cu_groups_host[i]]) * x.G;
     middle += rows > kFewRows && rows <= kFewRowsMost;
     strips += (rows + 31) / 32 * ((s.max_prefix + 127) / 128);
+    group_most = std::max(group_most, rows);
+    group_parts += (rows + 31) / 32;
   }
   for (int r = 0; r < x.n_seqs; ++r) {
     const int64_t rows = (int64_t)(b->cu_q_host[r + 1] - b->cu_q_host[r]) * x.G;
     if (rows > kOwnRows) strips += (rows + 31) / 32 * ((s.max_own + 127) / 128);
   }
-  if (strips * x.Hkv <= kFewStrips) s.few_rows = INT32_MAX;
+  if (strips * x.Hkv <= kFewStrips && alike(x.n_seqs, own_most, own_parts) && alike(s.n_groups, group_most, group_parts)) s.few_rows = INT32_MAX;
   else s.few_rows = middle * x.Hkv * s.max_prefix > (pl->pool.fp8 ? kFewKeys8 : kFewKeys16) ? kFewRows : kFewRowsMost;
   for (int i = 0; i < g->n_groups; ++i) {
     const int64_t rows = (int64_t)(b->cu_q_host[g->cu_groups_host[i + 1]] - b->cu_q_host[g->cu_groups_host[i]]) * x.G;
@@ -121,14 +133,14 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
     const int64_t rows = (int64_t)(b->cu_q_host[r + 1] - b->cu_q_host[r]) * x.G;
     own_blocks += (rows + kManyRows - 1) / kManyRows;
   }
-  if (own_most <= kOwnRows || s.max_own == 0 || pl->many_groups == 0) own_blocks = 0;
+  pl->prompts = pl->many_groups > 0 && own_most > kOwnRows;
+  if (!pl->prompts || s.max_own == 0) own_blocks = 0;
   own_blocks *= x.Hkv;
   blocks *= x.Hkv;
   if (blocks + own_blocks > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
   s.own_units = (int)own_blocks;
-  const int64_t own_parts = (own_most + 31) / 32;
-  s.join = pl->many_groups > 0 && (s.own_units > 0 || s.max_own <= kJoinKeys || items * own_parts >= kJoinItems);
-  pl->few_two = s.join ? few_most > 16 : std::max(few_most, own_most) > 16;
+  s.join = pl->many_groups > 0 && !pl->prompts && (s.max_own <= kJoinKeys || items * ((own_most + 31) / 32) >= kJoinItems);
+  pl->few_two = s.join || pl->prompts ? few_most > 16 : std::max(few_most, own_most) > 16;
   pl->own_two = s.join ? own_most > 16 : pl->few_two;
   const int few_each = pl->few_two ? 32 : 16, own_each = pl->own_two ? 32 : 16;
 
@@ -153,10 +165,12 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
     s.many_splits = (tiles + s.many_tiles - 1) / s.many_tiles;
     s.many_units = (int)(blocks * s.many_splits);
   }
-  auto cut = [&](int64_t items, int most, int64_t largest, int* chunk, int* splits) {
+  // Chunks of keys for `items` that have some, of `all` that there is a workgroup for.
+  const int64_t most_splits = std::min(kMostSplits, std::max<int64_t>(8, kMostParts / std::max<int64_t>(1, (int64_t)x.T * x.Hq)));
+  auto cut = [&](int64_t items, int64_t all, int most, int64_t largest, int* chunk, int* splits) {
     int64_t keys = (items * most / 512 + 127) / 128 * 128;
     keys = std::min<int64_t>(std::max<int64_t>(keys, 128), largest);
-    while ((most + keys - 1) / keys > kMostSplits || (items * ((most + keys - 1) / keys) > kMostBlocks && keys < most)) keys *= 2;
+    while ((most + keys - 1) / keys > most_splits || (all * ((most + keys - 1) / keys) > kMostBlocks / 2 && keys < most)) keys *= 2;
     *chunk = (int)std::min<int64_t>(keys, 1 << 30);
     *splits = (int)((most + keys - 1) / keys);
   };
@@ -165,7 +179,7 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
   int64_t few_units = 0;
   if (pl->few_groups > 0) {
     const int64_t units = (int64_t)s.n_groups * x.Hkv * s.few_parts;
-    cut((int64_t)pl->few_groups * x.Hkv * s.few_parts, s.max_prefix, kFewChunk, &s.few_chunk, &s.few_splits);
+    cut((int64_t)pl->few_groups * x.Hkv * s.few_parts, units, s.max_prefix, kFewChunk, &s.few_chunk, &s.few_splits);
     s.few_splits = std::max(s.few_splits, 1);
     few_units = units * s.few_splits;
     if (few_units > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
@@ -174,16 +188,19 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
   s.splits = std::max(s.many_splits, s.few_splits);
   // rows behind them
   pl->row_parts = std::max<int>(1, (int)std::min<int64_t>((own_most + own_each - 1) / own_each, INT32_MAX));
-  if (items * pl->row_parts > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
-  if (s.join) {
-    pl->chunk = s.max_own;
-    pl->own_splits = 1;
-  } else {
-    cut(items * pl->row_parts, s.max_own, kOwnChunk, &pl->chunk, &pl->own_splits);
+  pl->own_units = pl->chunk = pl->own_splits = 0;
+  if (!pl->prompts) {
+    if (items * pl->row_parts > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
+    if (s.join) {
+      pl->chunk = s.max_own;
+      pl->own_splits = 1;
+    } else {
+      cut(items * pl->row_parts, items * pl->row_parts, s.max_own, kOwnChunk, &pl->chunk, &pl->own_splits);
+    }
+    pl->own_units = items * pl->row_parts * pl->own_splits;
   }
-  pl->own_units = items * pl->row_parts * pl->own_splits;
-  if (pl->own_units + few_units > kMostBlocks) return CODECOMP_EINVAL_SHAPE;        // with which the kernel that joins has less than 2^27 rows, 8 or more a workgroup
-  pl->ws_bytes = x.T == 0 ? 0 : ((size_t)(s.splits + (s.join ? s.own_units > 0 : pl->own_splits)) * x.T * x.Hq * (p->head_dim + 2) * sizeof(float) + 255) & ~(size_t)255;
+  if (pl->own_units + few_units > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
+  pl->ws_bytes = x.T == 0 ? 0 : ((size_t)(s.splits + (s.own_units > 0 ? 1 : s.join ? 0 : pl->own_splits)) * x.T * x.Hq * (p->head_dim + 2) * sizeof(float) + 255) & ~(size_t)255;
   return CODECOMP_OK;
 }
 
@@ -194,7 +211,7 @@ __global__ __launch_bounds__(256) void join_shared_kernel(const AttendArgs a, in
   __shared__ f32x4 sums[GROUPS][ROWS][THREADS];
   __shared__ float tops[GROUPS][ROWS], alls[GROUPS][ROWS];
   const int in = threadIdx.x / THREADS, group = in % GROUPS, slot = in / GROUPS, th = threadIdx.x % THREADS, e = th * 4;
-  const int64_t rows = (int64_t)a.b.T * a.b.Hq, row = (int64_t)blockIdx.x * ROWS + slot;
+  const int64_t rows = (int64_t)a.b.T * a.b.Hq, row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * ROWS + slot;
   const bool there = row < rows;
   float top = -INFINITY, all = 0.0f;
   if (there) {
@@ -239,8 +256,8 @@ __global__ __launch_bounds__(256) void join_shared_kernel(const AttendArgs a, in
 template <int D, int GROUPS>
 static int launch_join(const AttendArgs& a, int parts, hipStream_t stream) {
   constexpr int ROWS = 256 / (D / 4) / GROUPS;
-  const int64_t rows = (int64_t)a.b.T * a.b.Hq;
-  join_shared_kernel<D, GROUPS><<<dim3((unsigned)((rows + ROWS - 1) / ROWS)), dim3(256), 0, stream>>>(a, parts);
+  const int64_t blocks = ((int64_t)a.b.T * a.b.Hq + ROWS - 1) / ROWS, width = std::min<int64_t>(blocks, 1 << 20);       // an axis of a grid holds 2^32 threads
+  join_shared_kernel<D, GROUPS><<<dim3((unsigned)width, (unsigned)((blocks + width - 1) / width)), dim3(256), 0, stream>>>(a, parts);
   return (int)hipGetLastError();
 }
 
@@ -252,7 +269,7 @@ int launch_shared(const SharedPlan& pl, const void* q, int layer, void* out, flo
   a.chunk = pl.chunk; a.row_parts = pl.row_parts;
   a.sh = pl.sh;
   if (pl.sh.alone) return launch_few_shared(pl.d, pl.pool.fp8, pl.own_two, pl.own_units, a, stream);
-  const int parts = pl.sh.splits + (pl.sh.join ? pl.sh.own_units > 0 : pl.own_splits);
+  const int parts = pl.sh.splits + (pl.sh.own_units > 0 ? 1 : pl.sh.join ? 0 : pl.own_splits);
   const int64_t rows = (int64_t)pl.batch.T * pl.batch.Hq;
   a.part_o = static_cast<float*>(workspace);
   a.part_ml = a.part_o + parts * rows * pl.d;
@@ -270,7 +287,6 @@ int launch_shared(const SharedPlan& pl, const void* q, int layer, void* out, flo
     if (pl.sh.few_units > 0)
       if (int rc = launch_few_shared(pl.d, pl.pool.fp8, pl.few_two, pl.sh.few_units, a, stream)) return rc;
     a.sh.few_units = 0;
-    if (a.sh.own_units > 0) return launch_join_own(pl.d, pl.own_units, a, stream);
     return launch_few_shared(pl.d, pl.pool.fp8, pl.own_two, pl.own_units, a, stream);
   }
   if (pl.sh.few_units + pl.own_units > 0)

@@ -20,6 +20,7 @@ struct SharedPlan {
   int d;
   float scale;
   int few_groups, many_groups; // groups of each kind (attend_shared.hip)
+  bool prompts;                // the kernel for many rows has what requests have behind the shared rows
   int few_two, own_two;        // kernel for few rows, shared and own: 32 rows a workgroup, not 16
   int row_parts, chunk, own_splits;    // rows behind the shared ones: parts of a request's rows, keys of a chunk, chunks
   int64_t own_units;

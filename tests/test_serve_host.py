@@ -184,6 +184,13 @@ def test_sizes_beyond_a_launch_are_refused():
     assert evict(mass(n_layers=15, n_seqs=65535, n_kv_heads=4096), eviction(n_seqs=65535), pool(n_kv_heads=4096, n_layers=15)) == -2
     # one prompt of very many tokens is none too many: what is behind the shared rows is joined where it is attended to
     assert b.lib().codecomp_attend_shared_validate(ref(batch([0, 1 << 20], n_q_heads=64)), ref(groups((0, 1))), ref(pool(head_dim=128))) == 0
+    # many groups without tokens beside one with some; many requests, each a group of its own, under long bounds
+    for tokens, cu in ((1000, [0] * 60000 + [1]), (1, [0] * 60000 + [1])):
+        x = batch([0, tokens], n_q_heads=64, table_width=1 << 16, max_kv_len=1 << 20)
+        for bound in (600, 1 << 20):
+            assert b.lib().codecomp_attend_shared_validate(ref(x), ref(groups(cu, max_prefix_len=bound, max_own_len=bound)), ref(pool())) == 0
+    x = batch(list(range(60001)), table_width=1 << 16, max_kv_len=1 << 20)
+    assert b.lib().codecomp_attend_shared_validate(ref(x), ref(groups(range(60001), max_prefix_len=1 << 20, max_own_len=1 << 20)), ref(pool())) == 0
     # many requests of long tables: chunks grow until a launch holds them
     x = batch(list(range(60001)), table_width=1 << 16, max_kv_len=1 << 20)
     assert b.lib().codecomp_attend_shared_workspace_bytes(ref(x), ref(groups((0, 60000), max_prefix_len=1 << 20, max_own_len=1 << 20)), ref(pool())) > 0
