@@ -35,9 +35,11 @@ constexpr int kChip = 256;                       // compute units: workgroups of
 constexpr int64_t kMostBlocks = (1 << 23) - 1;    // of up to 512 threads: an axis of a grid holds 2^32 threads
 constexpr int64_t kMostSplits = 1024, kMostParts = 1 << 21;       // chunks of a request's keys; of all rows together, where there are more than eight chunks: workspace
 // Up to so many keys in all nothing is cut, shared rows are read once for every 16 or 32 rows, and there is nothing to join: one launch (us, with parts | without: 64 steps behind 16
-// rows 10.7 | 7.1, 1024 behind 300, 8 bits, 133 | 118, 226 tokens behind 47 24 | 12, 1000 requests of up to 20 tokens behind 400 426 | 384; beyond: 8 steps behind 700 11.7 | 15.7,
-// 256 behind 500 and up to 300 of their own 42 | 53, two prompts of 600 tokens 44 | 52).
+// rows 10.7 | 7.1, 1024 in groups of 8 behind 300, 8 bits, 133 | 118, 226 tokens behind 47 24 | 12, 1000 requests of up to 20 tokens behind 400 426 | 384; beyond: 8 steps behind 700
+// 11.7 | 15.7, 256 behind 500 and up to 300 of their own 42 | 53, two prompts of 600 tokens 44 | 52).  Not where that is much work, and at least twice as much as the kernel
+// for many rows would have (1024 steps in groups of 128 behind 300 78 | 99).
 constexpr int kAloneKeys = 512;
+constexpr int64_t kAloneStrips = 8192;
 constexpr int64_t kEmptyBlocks = 4096;
 // Little work, in strips of 128 keys by 32 rows: all of it in one launch of the kernel for few rows, and one that joins (us, one | the kernel for many as well: 64 steps of 7 query
 // heads on 4 KV heads behind 1000 rows, 448 strips, 22 | 28, 2048 25 | 28, 4096 30 | 30; 16 steps behind 8000, 1008 strips, 26.5 | 26, 16000 33 | 30).
@@ -83,15 +85,27 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
   s.n_groups = g->n_groups; s.max_prefix = g->max_prefix_len; s.max_own = g->max_own_len;
   int64_t few_most = 0, blocks = 0, own_most = 0;
   const int64_t items = (int64_t)x.n_seqs * x.Hkv;
-  int64_t own_parts = 0;                           // of 32 rows, of all requests
+  int64_t own_parts = 0, group_parts = 0, group_most = 0;      // parts of 32 rows of all requests, of all groups; rows of the largest one
   for (int r = 0; r < x.n_seqs; ++r) {
     const int64_t rows = (int64_t)(b->cu_q_host[r + 1] - b->cu_q_host[r]) * x.G;
     own_most = std::max(own_most, rows);
     own_parts += (rows + 31) / 32;
   }
+  int64_t middle = 0;                              // groups of more than 32 rows that either kernel can take
+  for (int i = 0; i < g->n_groups; ++i) {
+    const int64_t rows = (int64_t)(b->cu_q_host[g->cu_groups_host[i + 1]] - b->cu_q_host[g->cu_groups_host[i]]) * x.G;
+    middle += rows > kFewRows && rows <= kFewRowsMost;
+    group_most = std::max(group_most, rows);
+    group_parts += (rows + 31) / 32;
+  }
   // The kernel for few rows has workgroups for as many parts of every request, or group, as the largest one has: not where most of them would find nothing.
   auto alike = [&](int64_t count, int64_t most, int64_t parts) { return count * ((most + 31) / 32) * x.Hkv <= 4 * parts * x.Hkv + kEmptyBlocks; };
-  if (s.max_prefix + (int64_t)s.max_own <= kAloneKeys && alike(x.n_seqs, own_most, own_parts)) {
+  // Work in strips of 128 keys by 32 rows, with the shared rows read for every request, and once for a group.
+  auto strips_of = [&](int64_t keys) { return (keys + 127) / 128; };
+  const int64_t apart = own_parts * strips_of(s.max_prefix + (int64_t)s.max_own) * x.Hkv;
+  const int64_t together = (group_parts * strips_of(s.max_prefix) + own_parts * strips_of(s.max_own)) * x.Hkv;
+  const bool pays = group_most > kFewRowsMost && apart > kAloneStrips && apart > 2 * together;
+  if (s.max_prefix + (int64_t)s.max_own <= kAloneKeys && !pays && alike(x.n_seqs, own_most, own_parts)) {
     pl->own_two = own_most > 16;
     pl->row_parts = std::max<int>(1, (int)((own_most + (pl->own_two ? 31 : 15)) / (pl->own_two ? 32 : 16)));
     pl->own_units = items * pl->row_parts;
@@ -103,18 +117,10 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
     return CODECOMP_OK;
   }
   pl->few_groups = pl->many_groups = 0;
-  int64_t middle = 0, strips = 0;                  // groups of more than 32 rows that either kernel can take; strips of 128 keys that the one for few takes, 32 rows at a time
-  int64_t group_most = 0, group_parts = 0;
-  for (int i = 0; i < g->n_groups; ++i) {
-    const int64_t rows = (int64_t)(b->cu_q_host[g->cu_groups_host[i + 1]] - b->cu_q_host[g->cu_groups_host[i]]) * x.G;
-    middle += rows > kFewRows && rows <= kFewRowsMost;
-    strips += (rows + 31) / 32 * ((s.max_prefix + 127) / 128);
-    group_most = std::max(group_most, rows);
-    group_parts += (rows + 31) / 32;
-  }
+  int64_t strips = group_parts * strips_of(s.max_prefix);        // of the shared rows, and of the own ones of requests that the kernel for many rows would take
   for (int r = 0; r < x.n_seqs; ++r) {
     const int64_t rows = (int64_t)(b->cu_q_host[r + 1] - b->cu_q_host[r]) * x.G;
-    if (rows > kOwnRows) strips += (rows + 31) / 32 * ((s.max_own + 127) / 128);
+    if (rows > kOwnRows) strips += (rows + 31) / 32 * strips_of(s.max_own);
   }
   if (strips * x.Hkv <= kFewStrips && alike(x.n_seqs, own_most, own_parts) && alike(s.n_groups, group_most, group_parts)) s.few_rows = INT32_MAX;
   else s.few_rows = middle * x.Hkv * s.max_prefix > (pl->pool.fp8 ? kFewKeys8 : kFewKeys16) ? kFewRows : kFewRowsMost;

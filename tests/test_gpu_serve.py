@@ -307,6 +307,16 @@ def test_shared_many_groups_and_prompts(n_groups, most, page, d):
     check_shared(f)
 
 
+def test_shared_very_many_steps_over_short_caches():
+    """Enough of them that sharing pays where nothing is long; and a prompt beside many of them, for whose rows most workgroups would be empty."""
+    rng = np.random.default_rng(54)
+    for members, more in ((([260] * 2), []), ([300], [1, 600])):
+        n = sum(members) + len(more)
+        news = [1] * sum(members) + more
+        f = Forked(rng, members + [1] * len(more), [200] * (len(members) + len(more)), news, [x + int(rng.integers(0, 60)) for x in news], n_q=16, n_kv=4, d=64, page=16, width_more=60)
+        check_shared(f, max_kv=1000, max_prefix=400 if not more else 200, max_own=100 if not more else 620)
+
+
 # requests that have their groups' tables, and no new tokens; groups of 33 to 64 rows under a loose bound (weights of 16 bits in the kernel for many rows); own rows that are joined
 # in one workgroup although there are many of them
 @pytest.mark.parametrize("members, prefixes, news, own, n_q, n_kv, d, page, bounds", [
