@@ -34,7 +34,7 @@ struct SharedRows {
   int few_units, few_parts, few_chunk, few_splits;       // shared rows of groups of few rows: workgroups, parts of the rows, keys of a chunk, chunks
   int many_units, many_tiles, many_splits;               // of many: workgroups, tiles of a chunk, chunks
   int splits;                  // the larger one: parts of shared rows that every row has
-  int own_units;               // workgroups of the kernel for many rows for what requests have behind the shared rows (one more part); 0: the kernel for few has it
+  int own_units, own_tiles, own_splits;                  // of many, behind the shared rows: the same, and as many more parts; 0: the kernel for few rows has those
   int alone;                   // 1: everything is short, and a request's shared rows are attended to with its own ones, by the kernel for few rows: no parts
   int join;                    // 1: whoever has a request's own rows joins the parts of the shared ones to them, and writes the outputs
 };

@@ -217,11 +217,12 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
   int chunk_tile0 = 0, chunk_tile1 = 0, key_low = 0;               // SHARED: the tiles, and the first key of them that counts
   const int group_blocks = SHARED ? (ma.sh.many_units + 7) / 8 * 8 : 0;
   if constexpr (SHARED) {
-    // Blocks of rows of one chunk side by side, on one die: they read the same keys.
+    // Blocks of rows of one chunk side by side, on one die: they read the same keys.  A request's own blocks go to the dies in turn, chunks and heads side by side, which are
+    // mostly as many as the dies are or more: requests are of very different lengths.
     const bool shared = (int)blockIdx.x < group_blocks;
     const int units = shared ? ma.sh.many_units : ma.sh.own_units, on_die = (units + 7) / 8, turn = shared ? blockIdx.x : blockIdx.x - group_blocks;
-    const int unit = (turn & 7) * on_die + (turn >> 3);
-    if ((turn >> 3) >= on_die || unit >= units) return;
+    const int unit = shared ? (turn & 7) * on_die + (turn >> 3) : turn;
+    if ((shared && (turn >> 3) >= on_die) || unit >= units) return;
     // its group or request: they are shared out over the lanes, or the threads, to count their units
     const int count = shared ? ma.sh.n_groups : n;
     auto blocks_at = [&](int i) __attribute__((always_inline)) {
@@ -230,7 +231,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
       if (!shared) x.count = (x.rows + kManyRows - 1) / kManyRows;
       return x;
     };
-    auto units_at = [&](int i) __attribute__((always_inline)) { return blocks_at(i).count * a.b.Hkv * (shared ? ma.sh.many_splits : 1); };
+    auto units_at = [&](int i) __attribute__((always_inline)) { return blocks_at(i).count * a.b.Hkv * (shared ? ma.sh.many_splits : ma.sh.own_splits); };
     auto up_to = [&](int x) __attribute__((always_inline)) {       // sums over the lanes, inclusive
 #pragma unroll
       for (int off = 1; off < 64; off <<= 1) {
@@ -287,11 +288,13 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
       key_low = prefix_of(ma.sh, request_of(ma.sh.cu_groups, ma.sh.n_groups, r));
       of.len = (int)min((int64_t)kv_len_of(a.b, r), (int64_t)key_low + ma.sh.max_own);
       of = uniform(of);
-      block = of.count - 1 - rest % of.count;                     // those that see the most keys first
-      head = rest / of.count;
-      g = ma.sh.splits;
-      chunk_tile0 = key_low / kManyKeys;
-      chunk_tile1 = of.len > key_low ? of.tiles(block) : 0;
+      head = rest % a.b.Hkv;
+      rest /= a.b.Hkv;
+      const int split = rest % ma.sh.own_splits;
+      block = of.count - 1 - rest / ma.sh.own_splits;             // those that see the most keys first
+      g = ma.sh.splits + split;
+      chunk_tile0 = key_low / kManyKeys + split * ma.sh.own_tiles;
+      chunk_tile1 = of.len > key_low ? min(of.tiles(block), chunk_tile0 + ma.sh.own_tiles) : 0;
     }
     r = uniform(r); block = uniform(block); head = uniform(head); g = uniform(g); key_low = uniform(key_low);
     chunk_tile0 = uniform(chunk_tile0); chunk_tile1 = uniform(chunk_tile1);

@@ -58,8 +58,9 @@ constexpr int kFewChunk = 2048, kOwnChunk = 1024;
 // 32 requests, 59 | 43, 14: 82 | 59, 18: 86 | 61; 16 prompts of up to 512 over up to 2500: 603 | 299; 4 tokens 50 | 40, but at head_dim 64, 6 tokens of 4 over up to 2000, 37 | 44).
 constexpr int kOwnRows = 32;
 // Otherwise one workgroup has a request's own rows, and joins, where they are short or where there are enough of these, else chunks do and a kernel that joins (us, chunks |
-// one: 16 requests of 4 heads, up to 300 rows, 27 | 26, up to 2000 40 | 57; 64 of up to 4000 100 | 96; 128 of up to 1000 78 | 74).
-constexpr int kJoinKeys = 512;
+// one: 16 requests of 4 heads, up to 300 rows, 27 | 26, up to 2000 40 | 57; 64 of up to 4000 100 | 96, of 8000 225 | 211, of up to 16000 283 | 284; 128 of up to 1000 78 | 74;
+// 200 of up to 9000 413 | 458).
+constexpr int kJoinKeys = 512, kJoinMost = 8192;
 constexpr int64_t kJoinItems = 192;
 // The kernel that joins: several groups of threads a row, for many parts and few rows (us, one | eight: four steps 20 | 13, eight behind 32768 rows 63 | 36; 1024 steps of 32768
 // rows in all 132 | 149).
@@ -145,9 +146,21 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
   if (!pl->prompts || s.max_own == 0) own_blocks = 0;
   own_blocks *= x.Hkv;
   blocks *= x.Hkv;
+  const int64_t most_splits = std::min(kMostSplits, std::max<int64_t>(8, kMostParts / std::max<int64_t>(1, (int64_t)x.T * x.Hq)));
+  double own = 0.0;                                // tiles' worth of time of a chunk of them
+  if (own_blocks > 0) {
+    // long ones in chunks of a third of what there is to do for a compute unit, at most
+    const int tiles = std::max(1, (s.max_prefix + kManyKeys - 1) / kManyKeys), own_tiles = (s.max_own + kManyKeys - 1) / kManyKeys + 1;
+    const double work = (blocks * (tiles + kLead) + own_blocks * (0.75 * own_tiles + kLead)) / kChip;
+    const int64_t chunk = std::max<int64_t>((int64_t)std::max(work / 3, 16.0), (own_tiles + most_splits - 1) / most_splits);
+    s.own_tiles = (int)std::min<int64_t>(chunk, own_tiles);
+    s.own_splits = (own_tiles + s.own_tiles - 1) / s.own_tiles;
+    own_blocks *= s.own_splits;
+    own = 0.75 * s.own_tiles + kLead;
+  }
   if (blocks + own_blocks > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
   s.own_units = (int)own_blocks;
-  s.join = pl->many_groups > 0 && !pl->prompts && (s.max_own <= kJoinKeys || items * ((own_most + 31) / 32) >= kJoinItems);
+  s.join = pl->many_groups > 0 && !pl->prompts && (s.max_own <= kJoinKeys || (s.max_own <= kJoinMost && items * ((own_most + 31) / 32) >= kJoinItems));
   pl->few_two = s.join || pl->prompts ? few_most > 16 : std::max(few_most, own_most) > 16;
   pl->own_two = s.join ? own_most > 16 : pl->few_two;
   const int few_each = pl->few_two ? 32 : 16, own_each = pl->own_two ? 32 : 16;
@@ -158,13 +171,13 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
   s.many_splits = s.few_splits = 0;
   if (pl->many_groups > 0) {
     const int tiles = std::max(1, (s.max_prefix + kManyKeys - 1) / kManyKeys);
-    const double own = 0.75 * ((s.max_own + kManyKeys - 1) / kManyKeys) + kLead, part = (double)x.T * x.Hq * p->head_dim / kPartElements;
+    const double part = (double)x.T * x.Hq * p->head_dim / kPartElements;
     int best = 1;
     double least = 0.0;
     for (int n = 1; n <= std::min(tiles, kChip) && blocks * n + own_blocks <= kMostBlocks; ++n) {
       const double each = (tiles + n - 1) / n + kLead;
       const int64_t rounds = ((blocks * n + 7) / 8 + kChip / 8 - 1) / (kChip / 8);       // of a die's compute units
-      const int64_t left = own_blocks - (rounds * kChip - blocks * n) * (int64_t)(each / own);
+      const int64_t left = own_blocks > 0 ? own_blocks - (rounds * kChip - blocks * n) * (int64_t)(each / own) : 0;
       const double end = rounds * each + (left > 0 ? (left + kChip - 1) / kChip * own : 0.0), work = (blocks * n * each + own_blocks * own) / kChip;
       const double time = end + work + n * (0.04 + part);
       if (n == 1 || time < least) { best = n; least = time; }
@@ -174,7 +187,6 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
     s.many_units = (int)(blocks * s.many_splits);
   }
   // Chunks of keys for `items` that have some, of `all` that there is a workgroup for.
-  const int64_t most_splits = std::min(kMostSplits, std::max<int64_t>(8, kMostParts / std::max<int64_t>(1, (int64_t)x.T * x.Hq)));
   auto cut = [&](int64_t items, int64_t all, int most, int64_t largest, int* chunk, int* splits) {
     int64_t keys = (items * most / 512 + 127) / 128 * 128;
     keys = std::min<int64_t>(std::max<int64_t>(keys, 128), largest);
@@ -208,7 +220,7 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
     pl->own_units = items * pl->row_parts * pl->own_splits;
   }
   if (pl->own_units + few_units > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
-  pl->ws_bytes = x.T == 0 ? 0 : ((size_t)(s.splits + (s.own_units > 0 ? 1 : s.join ? 0 : pl->own_splits)) * x.T * x.Hq * (p->head_dim + 2) * sizeof(float) + 255) & ~(size_t)255;
+  pl->ws_bytes = x.T == 0 ? 0 : ((size_t)(s.splits + (s.own_units > 0 ? s.own_splits : s.join ? 0 : pl->own_splits)) * x.T * x.Hq * (p->head_dim + 2) * sizeof(float) + 255) & ~(size_t)255;
   return CODECOMP_OK;
 }
 
@@ -277,7 +289,7 @@ int launch_shared(const SharedPlan& pl, const void* q, int layer, void* out, flo
   a.chunk = pl.chunk; a.row_parts = pl.row_parts;
   a.sh = pl.sh;
   if (pl.sh.alone) return launch_few_shared(pl.d, pl.pool.fp8, pl.own_two, pl.own_units, a, stream);
-  const int parts = pl.sh.splits + (pl.sh.own_units > 0 ? 1 : pl.sh.join ? 0 : pl.own_splits);
+  const int parts = pl.sh.splits + (pl.sh.own_units > 0 ? pl.sh.own_splits : pl.sh.join ? 0 : pl.own_splits);
   const int64_t rows = (int64_t)pl.batch.T * pl.batch.Hq;
   a.part_o = static_cast<float*>(workspace);
   a.part_ml = a.part_o + parts * rows * pl.d;
