@@ -215,14 +215,13 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
   Blocks of = uniform(request(SHARED ? 0 : r));
   CutBlock cut = {-1, 0, 0, 0};
   int chunk_tile0 = 0, chunk_tile1 = 0, key_low = 0;               // SHARED: the tiles, and the first key of them that counts
-  const int group_blocks = SHARED ? (ma.sh.many_units + 7) / 8 * 8 : 0;
+  const int group_blocks = SHARED ? ma.sh.many_units : 0;
   if constexpr (SHARED) {
-    // Blocks of rows of one chunk side by side, on one die: they read the same keys.  A request's own blocks go to the dies in turn, chunks and heads side by side, which are
-    // mostly as many as the dies are or more: requests are of very different lengths.
+    // Units go to the dies in turn, heads and chunks of a block side by side, which mostly are as many as the dies or more: then blocks of one chunk, which read the same keys, are on
+    // one die, and no die has the longest requests or groups.
     const bool shared = (int)blockIdx.x < group_blocks;
-    const int units = shared ? ma.sh.many_units : ma.sh.own_units, on_die = (units + 7) / 8, turn = shared ? blockIdx.x : blockIdx.x - group_blocks;
-    const int unit = shared ? (turn & 7) * on_die + (turn >> 3) : turn;
-    if ((shared && (turn >> 3) >= on_die) || unit >= units) return;
+    const int units = shared ? ma.sh.many_units : ma.sh.own_units, unit = shared ? blockIdx.x : blockIdx.x - group_blocks;
+    if (unit >= units) return;
     // its group or request: they are shared out over the lanes, or the threads, to count their units
     const int count = shared ? ma.sh.n_groups : n;
     auto blocks_at = [&](int i) __attribute__((always_inline)) {
@@ -275,10 +274,10 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
       of.len = prefix_of(ma.sh, at);
       of = uniform(of);
       of.causal = 0;
-      block = rest % of.count;
-      rest /= of.count;
+      head = rest % a.b.Hkv;
+      rest /= a.b.Hkv;
       g = rest % ma.sh.many_splits;                               // number of the part
-      head = rest / ma.sh.many_splits;
+      block = rest / ma.sh.many_splits;
       const int tiles = (of.len + kManyKeys - 1) / kManyKeys;
       chunk_tile0 = g * ma.sh.many_tiles;
       chunk_tile1 = min(tiles, chunk_tile0 + ma.sh.many_tiles);
@@ -666,7 +665,7 @@ int launch_many_of(const ManyArgs& m, hipStream_t stream) {
 
 template <int D, bool FP8>
 int launch_many_shared_of(const ManyArgs& m, hipStream_t stream) {
-  const dim3 grid((unsigned)((m.sh.many_units + 7) / 8 * 8 + (m.sh.own_units + 7) / 8 * 8)), block(kManyThreads);
+  const dim3 grid((unsigned)(m.sh.many_units + m.sh.own_units)), block(kManyThreads);
   if (m.a.pool.page_log2 < 4) attend_many_kernel<D, FP8, true, true><<<grid, block, 0, stream>>>(m);
   else attend_many_kernel<D, FP8, false, true><<<grid, block, 0, stream>>>(m);
   return (int)hipGetLastError();

@@ -69,6 +69,10 @@ constexpr int64_t kJoinRows = 16384;
 // Chunks of shared rows for the kernel for many: the time of a tile is the unit.  A chunk starts and ends in 5 of them (8.6 us of 1.6 each at head_dim 128), and what it leaves
 // goes through memory twice: 600000 elements in a tile's time.
 constexpr double kLead = 5.0, kPartElements = 600000.0;
+// Of the own rows of prompts: a third of what a compute unit has to do in all, and 2048 keys at least (with the tile that the shared ones end in; us, whole | in chunks: 512 tokens over
+// 60000 own rows 1080 | 447, 8 requests of up to 300 over 300 to 30000 691 | 527; with halves of the work 427, 725, before they went to the dies in turn; 100 tokens over 4000
+// with chunks of 24 | 40 tiles 47 | 65, but 48 requests of 14 over up to 2000, 8 bits, head_dim 64, 62 | 51).
+constexpr double kOwnTiles = 33.0;
 
 int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const codecomp_pages* p, SharedPlan* pl) {
   if (int rc = make_pool(p, &pl->pool)) return rc;
@@ -152,7 +156,7 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
     // long ones in chunks of a third of what there is to do for a compute unit, at most
     const int tiles = std::max(1, (s.max_prefix + kManyKeys - 1) / kManyKeys), own_tiles = (s.max_own + kManyKeys - 1) / kManyKeys + 1;
     const double work = (blocks * (tiles + kLead) + own_blocks * (0.75 * own_tiles + kLead)) / kChip;
-    const int64_t chunk = std::max<int64_t>((int64_t)std::max(work / 3, 16.0), (own_tiles + most_splits - 1) / most_splits);
+    const int64_t chunk = std::max<int64_t>((int64_t)std::max(work / 3, kOwnTiles), (own_tiles + most_splits - 1) / most_splits);
     s.own_tiles = (int)std::min<int64_t>(chunk, own_tiles);
     s.own_splits = (own_tiles + s.own_tiles - 1) / s.own_tiles;
     own_blocks *= s.own_splits;

@@ -326,7 +326,9 @@ def test_shared_very_many_steps_over_short_caches():
     ([60], [300], [1] * 60, 1500, 16, 4, 64, 64, {}), ([60], [300], [2] * 60, 700, 32, 4, 128, 16, dict(max_kv=9000, max_own=3000)),
     # own rows in the kernel for many rows: of single tokens and prompts beside one another, causal within a block and behind its end, shared rows that end inside a tile
     ([9, 2, 1], [205, 90, 0], [1, 70, 0, 3, 1, 33, 1, 9, 1, 1, 2, 150], 300, 8, 2, 64, 16, {}), ([5, 4], [1000, 63], [300, 1, 129, 2, 40, 1, 1, 1, 90], 400, 14, 2, 128, 1, {}),
-    ([30], [129], [1, 9] * 15, 200, 16, 4, 128, 128, dict(max_kv=5000, max_prefix=5000, max_own=4000)), ([2, 1], [320, 64], [65, 64, 300], 1, 4, 4, 64, 64, {})])
+    ([30], [129], [1, 9] * 15, 200, 16, 4, 128, 128, dict(max_kv=5000, max_prefix=5000, max_own=4000)), ([2, 1], [320, 64], [65, 64, 300], 1, 4, 4, 64, 64, {}),
+    # prompts with many rows of their own: in chunks, the causal end in the last ones or before them
+    ([2, 2], [150, 63], [300, 1, 70, 5], 5000, 4, 2, 64, 16, {}), ([3], [1000], [260, 40, 1], 9000, 7, 1, 128, 64, {}), ([1, 1], [0, 5], [900, 700], 3000, 2, 1, 128, 8, dict(max_kv=40000, max_own=30000))])
 @pytest.mark.parametrize("loose", [0, 1100, 70000])
 @pytest.mark.parametrize("causal", [True, False])
 def test_shared_kinds_of_groups(members, prefixes, news, own, n_q, n_kv, d, page, bounds, causal, loose):
