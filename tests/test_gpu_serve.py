@@ -892,9 +892,10 @@ def test_evict_largest_and_smallest_numbers():
         check_evict(rng, [90, 33, 90, 90] * problems, [high, low, low, high] * problems, recent=3, max_budget=30, first=[low, 5, high, 80] * problems, n_kv=1, d=64, layers=1 if problems > 1 else 3)
 
 
-def test_evict_strides_of_pool_and_sums():
+@pytest.mark.parametrize("fp8", [False, True])                          # rows of a cache line, and of half a line, whose other half is another workgroup's
+def test_evict_strides_of_pool_and_sums(fp8):
     rng = np.random.default_rng(68)
-    c, x = evict_setup(rng, [200, 150], None, layers=2)
+    c, x = evict_setup(rng, [200, 150], None, layers=2, fp8=fp8)
     table, budgets, lens = c.dev_table(), dev([64, 30]), dev([200, 150])
     kept, new_lens = torch.empty((2, 2, 2, 64), dtype=torch.int32, device="cuda"), torch.empty(2, dtype=torch.int32, device="cuda")
     e = b.make_eviction(kv_lens=lens, table=table, budgets=budgets, max_kv_len=200, max_budget=64, recent=4)
@@ -907,12 +908,31 @@ def test_evict_strides_of_pool_and_sums():
     b.codecomp_evict(b.make_mass(sums), e, b.make_pages(k, v), kept, new_lens, kept_mass=b.make_mass(to))
     assert torch.equal(sums, dense)
     b.codecomp_evict(b.make_mass(dense), e, c.pages(), dense_kept, dense_lens)
-    assert torch.equal(kept, dense_kept) and torch.equal(new_lens, dense_lens) and torch.equal(k, c.k) and torch.equal(v, c.v)
+    assert torch.equal(kept, dense_kept) and torch.equal(new_lens, dense_lens)
+    assert torch.equal(k.view(torch.uint8), c.k.view(torch.uint8)) and torch.equal(v.view(torch.uint8), c.v.view(torch.uint8))
     for r, n in enumerate(dense_lens.tolist()):
         assert torch.equal(to[:, r, :, :n], dense[:, r, :, :n])
     b.codecomp_evict(b.make_mass(sums), e, c.pages(), kept, new_lens)    # in place, strided
     assert torch.equal(kept, dense_kept) and torch.equal(sums, dense)
     assert bool((wide[..., :7] == 0).all()) and bool((wide[..., 7 + x.shape[3]:] == 0).all())
+
+
+@pytest.mark.parametrize("fp8, d", [(True, 64), (True, 128), (False, 64)])
+def test_evict_of_many_heads_side_by_side(fp8, d):
+    """Rows of all heads of a token one behind the other: lines of memory that several workgroups write to, each its own part, on whatever die."""
+    rng = np.random.default_rng([72, d])
+    c, x = evict_setup(rng, [300] * 9, None, layers=6, n_kv=8, fp8=fp8, d=d)
+    table, budgets, lens, first = c.dev_table(), dev([100] * 9), dev([300] * 9), dev([3] * 9)
+    make = lambda bound: b.make_eviction(kv_lens=lens, table=table, budgets=budgets, max_kv_len=bound, max_budget=100, recent=4, first=first)  # noqa: E731
+    dense = torch.from_numpy(x).cuda()
+    kept, new_lens = torch.empty((6, 9, 8, 100), dtype=torch.int32, device="cuda"), torch.empty(9, dtype=torch.int32, device="cuda")
+    mixed = [t.permute(1, 3, 0, 2, 4).contiguous().permute(2, 0, 3, 1, 4) for t in (c.k, c.v)]
+    b.codecomp_evict(b.make_mass(dense), make(300), b.make_pages(*mixed), kept, new_lens)
+    again = torch.from_numpy(x).cuda()
+    b.codecomp_evict(b.make_mass(again), make(300), c.pages(), torch.empty_like(kept), new_lens)
+    for t, want in zip(mixed, (c.k, c.v)):
+        assert torch.equal(t.view(torch.uint8), want.view(torch.uint8))
+    assert torch.equal(dense, again) and np.array_equal(kept.cpu().numpy(), srv.evict(x, [300] * 9, [100] * 9, recent=4, max_budget=100, first=[3] * 9)[0])
 
 
 @pytest.mark.parametrize("fp8", [False, True])
