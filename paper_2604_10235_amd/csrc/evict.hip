@@ -276,11 +276,11 @@ __global__ __launch_bounds__(THREADS) void keep_kernel(const EvictArgs a) {
 }
 
 template <int PIECES, int THREADS>
-__global__ __launch_bounds__(THREADS) void close_up_kernel(const EvictArgs a, int slices) {
-  const int part = blockIdx.x % (2 * slices), problem = blockIdx.x / (2 * slices);
+__global__ __launch_bounds__(THREADS) void close_up_kernel(const EvictArgs a, int slices, int pools) {
+  const int part = blockIdx.x % (pools * slices), problem = blockIdx.x / (pools * slices);
   const int head = problem % a.Hkv, rest = problem / a.Hkv, r = rest % a.n_seqs;
-  unsigned char* const pool[1] = {part & 1 ? a.pool.v : a.pool.k};
-  close_up<PIECES, THREADS, kMoveDeep, 1>(a, rest / a.n_seqs, r, head, pool, part >> 1);
+  unsigned char* const pool[1] = {part % pools ? a.pool.v : a.pool.k};
+  close_up<PIECES, THREADS, kMoveDeep, 1>(a, rest / a.n_seqs, r, head, pool, part / pools);
 }
 
 // Both, for many problems.
@@ -295,7 +295,8 @@ __global__ __launch_bounds__(THREADS) void evict_kernel(const EvictArgs a) {
 
 template <int PIECES>
 static void launch_close_up(const EvictArgs& a, int64_t problems, int slices, hipStream_t stream) {
-  close_up_kernel<PIECES, kMoveThreads><<<dim3((unsigned)(problems * 2 * slices)), dim3(kMoveThreads), 0, stream>>>(a, slices);
+  const int pools = a.pool.k == a.pool.v ? 1 : 2;          // a cache whose values are its keys: rows move once
+  close_up_kernel<PIECES, kMoveThreads><<<dim3((unsigned)(problems * pools * slices)), dim3(kMoveThreads), 0, stream>>>(a, slices, pools);
 }
 
 template <int PIECES>

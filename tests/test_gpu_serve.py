@@ -935,6 +935,19 @@ def test_evict_of_many_heads_side_by_side(fp8, d):
     assert torch.equal(dense, again) and np.array_equal(kept.cpu().numpy(), srv.evict(x, [300] * 9, [100] * 9, recent=4, max_budget=100, first=[3] * 9)[0])
 
 
+@pytest.mark.parametrize("n, budget", [(2, 500), (2, 40), (300, 100)])
+def test_evict_where_values_are_the_keys(n, budget):
+    rng = np.random.default_rng([73, n])
+    c, x = evict_setup(rng, [700] * n, None, layers=1)
+    sums, other = torch.from_numpy(x).cuda(), torch.from_numpy(x).cuda()
+    kept, lens = torch.empty((1, n, 2, budget), dtype=torch.int32, device="cuda"), torch.empty(n, dtype=torch.int32, device="cuda")
+    e = b.make_eviction(kv_lens=dev([700] * n), table=c.dev_table(), budgets=dev([budget] * n), max_kv_len=700, max_budget=budget, recent=4)
+    one = c.k.clone()
+    b.codecomp_evict(b.make_mass(sums), e, b.make_pages(one, one), kept, lens)
+    b.codecomp_evict(b.make_mass(other), e, c.pages(), kept, lens)
+    assert torch.equal(one, c.k) and torch.equal(sums, other)
+
+
 @pytest.mark.parametrize("fp8", [False, True])
 def test_evict_offsets_beyond_32_bits(fp8):
     rng = np.random.default_rng([69, fp8])
