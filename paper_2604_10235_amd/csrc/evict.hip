@@ -12,7 +12,7 @@
 // Many problems (a layer's request and head each): one kernel, a workgroup for each, whose waits for counts are hidden behind the rows of others.  28 layers, 32 requests of 900 to
 // 1500 rows, 4 heads of 128, 1024 kept: 635 us, 5.3 TB/s; 32 layers, 48 requests behind 2049 protected rows, 8 bits: 1312 us, 4.9 TB/s.
 // Fewer: two kernels, the second with two or four workgroups for each.  28 layers, one request of 32768 rows to 2048: 25 us for the numbers and 57 for the rows,
-// which come from 256 bytes here and there, 4.1 TB/s; one layer of 1088 rows to 1024: 8 and 8 us, a chain of waits for counts and numbers.
+// which come from 256 bytes here and there, 4.1 TB/s; one layer of 1088 rows to 1024: 8 and 5 us, a chain of waits for counts and numbers.
 // Tried before: digits of 11 bits (three passes; as long); the next batch sent for before one is written (as long: it is the scattered rows, not the wait);
 // loads that may stay in the caches instead of those that pass by them (651 us instead of 637 for the steps above, 1307 instead of 1313 for 8 bits).
 #include <algorithm>
@@ -36,8 +36,9 @@ constexpr int kFewKept = 256, kHeldRows = 4096;
 // Two kernels: threads of a workgroup that moves rows (one request of 32768, us: 512 threads 97, 1024 85), and pieces that each has in flight (2, 4, 8: 85, 87, 87).
 constexpr int kMoveThreads = 1024, kMoveDeep = 2;
 // Rows of 256 bytes are cut into two stretches of 128 where there are fewer workgroups than compute units (114 us -> 98), and down to 32 where there are very few and
-// many rows to move: fewer waits one after another (one layer's 4 heads, to 2000 rows of 5000 33 us -> 27, but to 1024 of 1088 16.5 -> 18).
-constexpr int kFewest = 256, kFewer = 64, kManyRows = 1024;
+// a batch does not move all: fewer waits one after another (4 heads, us, 128 bytes | 32: to 1024 of 1088 rows 16.4 | 12.7, to 300 of 2000 12.6 | 11.7, 8 heads to 2000 of 5000 34 | 22; up to 128
+// workgroups, 16 heads to 16000 of 30000, 226 | 155, with 256 of them 167).  Stretches of a line of memory on different dies cost most of that (155 | 320 with 32 bytes).
+constexpr int kFewest = 256, kFewer = 128, kManyRows = 256;
 constexpr int64_t kMostBlocks = (1 << 22) - 1;          // of up to 1024 threads: an axis of a grid holds 2^32 threads
 
 struct Span { int f, n, m; };                            // rows [f, n) of a request, m of them kept
@@ -277,10 +278,11 @@ __global__ __launch_bounds__(THREADS) void keep_kernel(const EvictArgs a) {
 
 template <int PIECES, int THREADS>
 __global__ __launch_bounds__(THREADS) void close_up_kernel(const EvictArgs a, int slices, int pools) {
-  const int part = blockIdx.x % (pools * slices), problem = blockIdx.x / (pools * slices);
+  // Stretches of one row on one die, mostly (workgroups go to the eight dies in turn): they are parts of the same lines of memory.
+  const int rows = gridDim.x / slices, slice = blockIdx.x / rows, part = blockIdx.x - slice * rows, problem = part / pools;
   const int head = problem % a.Hkv, rest = problem / a.Hkv, r = rest % a.n_seqs;
   unsigned char* const pool[1] = {part % pools ? a.pool.v : a.pool.k};
-  close_up<PIECES, THREADS, kMoveDeep, 1>(a, rest / a.n_seqs, r, head, pool, part / pools);
+  close_up<PIECES, THREADS, kMoveDeep, 1>(a, rest / a.n_seqs, r, head, pool, slice);
 }
 
 // Both, for many problems.
