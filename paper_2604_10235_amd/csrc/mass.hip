@@ -4,7 +4,7 @@
 // The logits are formed again from queries and keys, with the log-sum-exp of every row known: half of attention's products, and no row has to wait for
 // another.  A key's weights of all rows meet in one workgroup (or in a fixed number of parts, added in order): no atomics.  Logits, weights and sums are fp32.
 //
-// Few rows (up to 64): every key is read once for a handful of products, bound by memory.  A workgroup of four waves has a stretch of the cache, each wave
+// Few rows (up to 64; up to 16 beside requests of more): every key is read once for a handful of products, bound by memory.  A workgroup of four waves has a stretch of the cache, each wave
 // tiles of 32 (head_dim 128) or 64 keys of its own, the next one on its way into registers.  S = Q K^T, 16 rows x 16 keys per MFMA: lane = key, so that a key's
 // weights are added in place, and by two exchanges between lanes at the end.  64 requests of 500 to 16384 rows, 8 KV heads of 128, 8 bits: 118 us, 4.6 TB/s;
 // 64 of 300 to 4100 behind 8192 protected ones, 4 KV heads, bf16: 38 us, 4.2 TB/s.  One token over 2113 rows: 7 us, which is what the launch takes.
@@ -50,6 +50,7 @@ struct MassArgs {
   int64_t layer;               // byte offset of the layer in the pool
   float c, decay, share;       // softmax_scale * k_scale * log2(e); 1 / G
   int chunk, shares, few_shares;
+  int few_most;                // rows of a request up to which the kernel for few has it
 };
 
 constexpr int kMassWaves = 4, kMassThreads = 64 * kMassWaves;
@@ -78,7 +79,7 @@ __device__ __forceinline__ float old_sum(const MassArgs& a, const float* sums, i
 template <int STRIP>
 __device__ __forceinline__ int mass_strips(const MassArgs& a, int r) {
   const int nq = a.b.cu_q[r + 1] - a.b.cu_q[r], len = kv_len_of(a.b, r), from = first_of(a, r);
-  return nq <= 0 || nq > kFewRowsMost || nq * a.b.G > kFewRowsMost || from >= len ? 0 : (len + STRIP - 1) / STRIP - from / STRIP;
+  return nq <= 0 || nq > a.few_most || nq * a.b.G > a.few_most || from >= len ? 0 : (len + STRIP - 1) / STRIP - from / STRIP;
 }
 
 // EVEN: the strips of all requests and heads form one sequence, cut into equal parts; else a workgroup has one chunk of a request.
@@ -160,7 +161,7 @@ __global__ __launch_bounds__(kMassThreads, 4) void mass_few_kernel(const MassArg
       look_up(page, (int64_t)key0 + wave * KEYS, key1);
       look_up(next_page, (int64_t)key0 + (kMassWaves + wave) * KEYS, key1);
     } else {
-      if (nq <= 0 || nq > kFewRowsMost || rows > kFewRowsMost) return;
+      if (nq <= 0 || nq > a.few_most || rows > a.few_most) return;
       key1 = (int)min((int64_t)len, (int64_t)key0 + a.chunk);
       if (key0 >= key1 || key1 <= from) return;
     }
@@ -298,7 +299,7 @@ __device__ __forceinline__ KeyBlocks blocks_of(const MassArgs& a, int r) {
   x.rows = x.nq * x.G;
   x.off = a.b.causal ? x.len - x.nq : INT32_MAX;
   x.first = first_of(a, r) / kMassKeys;
-  x.count = x.rows <= kFewRowsMost || first_of(a, r) >= x.len ? 0 : (x.len + kMassKeys - 1) / kMassKeys - x.first;
+  x.count = x.rows <= a.few_most || first_of(a, r) >= x.len ? 0 : (x.len + kMassKeys - 1) / kMassKeys - x.first;
   return x;
 }
 
@@ -595,6 +596,11 @@ __global__ __launch_bounds__(2 * kMassKeys) void mass_join_kernel(const MassArgs
 constexpr int64_t kMassEvenBytes = 1 << 27;
 // Four for each compute unit (512, 1024, 2048: 136, 118, 123 us for the 8-bit steps above).
 constexpr int kMassFewShares = 1024;
+// Where some request has more than 64 rows, and the kernel for many runs, it has all of more than 16, and what is left as well if that is no more than 64 blocks of keys: a
+// launch less (us, split at 64 | so: 9 requests of 5 to 15 tokens of 7 query heads over 526 to 3688 rows 31 | 19, 16 of up to 20 over 100 to 2000 31 | 20, two over 13 to 15
+// rows 19 | 14, 40 of up to 20 over 100 to 2000 41 | 32, 64 of up to 12 over 500 to 8000 128 | 129; 30 steps beside a prompt, 240 blocks, 25 | 25, with all together 34).
+constexpr int kMassSteps = 16;
+constexpr int64_t kMassTogether = 64;
 constexpr int kMassShares = 256;                 // many rows: a workgroup for each compute unit
 constexpr int64_t kMostBlocks = (1 << 24) - 1;    // of 256 threads: an axis of a grid holds 2^32 threads
 
@@ -606,12 +612,18 @@ int make_mass_plan(const codecomp_batch* b, const codecomp_pages* p, const codec
   if (m->n_layers != p->n_layers || m->n_seqs != b->n_seqs || m->n_kv_heads != p->n_kv_heads || m->width < b->max_kv_len) return CODECOMP_EINVAL_SHAPE;
   pl->d = p->head_dim;
   pl->scale = b->softmax_scale > 0.0f ? b->softmax_scale : 1.0f / sqrtf((float)p->head_dim);
-  pl->few_rows = pl->many_rows = 0;
-  for (int r = 0; r < x.n_seqs; ++r) {
-    const int64_t rows = (int64_t)(b->cu_q_host[r + 1] - b->cu_q_host[r]) * x.G;
-    if (rows > kFewRowsMost) ++pl->many_rows;
-    else if (rows > 0) ++pl->few_rows;
-  }
+  auto count = [&](int few_most) {
+    pl->few_most = few_most;
+    pl->few_rows = pl->many_rows = 0;
+    for (int r = 0; r < x.n_seqs; ++r) {
+      const int64_t rows = (int64_t)(b->cu_q_host[r + 1] - b->cu_q_host[r]) * x.G;
+      if (rows > few_most) ++pl->many_rows;
+      else if (rows > 0) ++pl->few_rows;
+    }
+  };
+  count(kFewRowsMost);
+  if (pl->many_rows > 0) count(kMassSteps);
+  if (pl->many_rows > 0 && pl->few_rows > 0 && (int64_t)pl->few_rows * x.Hkv * ((x.max_kv + kMassKeys - 1) / kMassKeys) <= kMassTogether) count(0);
   const int64_t items = (int64_t)x.n_seqs * x.Hkv;
   const int64_t chunk = items * x.max_kv > 256 * 2048 ? 512 : 256;        // two tiles of every wave (one at head_dim 64), or four where there are enough workgroups all the same (128 to 1024: within 0.4 us)
   pl->chunk = (int)chunk;
@@ -655,6 +667,7 @@ int launch_mass(const MassPlan& pl, const void* q, const float* lse, int layer, 
   a.c = fminf(fmaxf(pl.scale * pl.pool.k_scale * kLog2e, FLT_MIN), FLT_MAX);
   a.decay = decay; a.share = 1.0f / pl.batch.G;
   a.cuts = reinterpret_cast<CutKeys*>(a.part + 2 * kMassShares * kMassKeys);
+  a.few_most = pl.few_most;
   a.chunk = pl.chunk; a.shares = kMassShares; a.few_shares = pl.shares;
   if (pl.d == 128) return pl.pool.fp8 ? launch_mass_of<128, true>(pl, a, stream) : launch_mass_of<128, false>(pl, a, stream);
   return pl.pool.fp8 ? launch_mass_of<64, true>(pl, a, stream) : launch_mass_of<64, false>(pl, a, stream);

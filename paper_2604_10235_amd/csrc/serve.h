@@ -37,6 +37,7 @@ struct MassPlan {
   int d;
   float scale;
   int few_rows, many_rows;     // requests of each kind (mass.hip)
+  int few_most;                // rows of a request up to which it is of the first kind
   int chunk, chunks;           // few rows: keys of a workgroup, and workgroups for a request and head,
   int shares;                  // or (not 0) equal parts of the keys of all requests and heads
   size_t ws_bytes;
