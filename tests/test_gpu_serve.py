@@ -488,6 +488,15 @@ def test_mass(lens, news, n_q, n_kv, d, page, fp8, causal):
     check_mass(rng, lens, news, n_q, n_kv=n_kv, d=d, page=page, fp8=fp8, causal=causal)
 
 
+@pytest.mark.parametrize("max_kv", [900, 70000])
+@pytest.mark.parametrize("news", [[16, 17, 64, 65, 1, 0], [16, 17, 64, 33, 1, 0], [16, 15, 1, 65, 0, 1]])
+@pytest.mark.parametrize("d, page, fp8", [(128, 16, False), (64, 4, True)])
+def test_mass_of_rows_around_the_numbers_that_decide(max_kv, news, d, page, fp8):
+    """One query head: rows are tokens.  With a loose bound on lengths there may be much work for either kernel."""
+    rng = np.random.default_rng([74, sum(news), d])
+    check_mass(rng, [100, 600, 64, 900, 513, 77], news, 2, n_kv=2, d=d, page=page, fp8=fp8, first=[5, 0, 0, 512, 1, 0], decay=0.9, max_kv=max_kv, width=max_kv, width_more=70000 // page)
+
+
 @pytest.mark.parametrize("lens, news, n_q, d", [([300, 77, 900], [1, 1, 3], 4, 128), ([300, 77, 900], [90, 40, 1], 4, 64), ([300, 77, 900], [2, 77, 100], 14, 128)])
 @pytest.mark.parametrize("first", [[0, 77, 130], [299, 0, 511], [300, 1000, -7], [31, 32, 256]])
 @pytest.mark.parametrize("decay", [0.0, 0.75])
