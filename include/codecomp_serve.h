@@ -50,8 +50,8 @@ size_t codecomp_attend_shared_workspace_bytes(const codecomp_batch* batch, const
  * codecomp_attend would let it see (j < kv_lens[r]; causal: j <= kv_lens[r] - cu_q[r + 1] + t).  The shared rows are to lie before the new
  * tokens of every request, prefix_lens[g] <= kv_lens[r] - (cu_q[r + 1] - cu_q[r]), and then the result is that of codecomp_attend but for roundings.
  * What stands in rows that a token does not see has no part in its result; an infinity or NaN in what it sees counts as for codecomp_attend.
- * Logits, sums and outputs are fp32.  Weights enter the second product rounded to bf16, or as two bf16, 16 bits together: those of the shared rows where
- * the group has up to 64 rows (new tokens of its requests * query heads per KV head), those of the other rows where the request has.
+ * Logits, sums and outputs are fp32.  Weights enter the second product rounded to bf16, or as two bf16, 16 bits together, for requests of up to 64 rows (new
+ * tokens * query heads per KV head), as in codecomp_attend, whatever is in the group and the batch with them.
  * workspace: >= codecomp_attend_shared_workspace_bytes(), 256-byte aligned, contents on entry do not matter; calls that may run at the same
  * time need workspaces of their own. */
 int codecomp_attend_shared(const void* q, const codecomp_batch* batch, const codecomp_groups* groups, const codecomp_pages* pages, int32_t layer, void* out,

@@ -33,6 +33,7 @@ struct SharedRows {
   int few_rows;                // rows of a group up to which the kernel for few rows has its shared rows
   int few_units, few_parts, few_chunk, few_splits;       // shared rows of groups of few rows: workgroups, parts of the rows, keys of a chunk, chunks
   int many_units, many_tiles, many_splits;               // of many: workgroups, tiles of a chunk, chunks
+  int fine;                    // of many, weights of the shared rows as two bf16: 0 never, 1 always, 2 in waves with rows of a request of up to kFewRowsMost
   int splits;                  // the larger one: parts of shared rows that every row has
   int own_units, own_tiles, own_splits;                  // of many, behind the shared rows: the same, and as many more parts; 0: the kernel for few rows has those
   int alone;                   // 1: everything is short, and a request's shared rows are attended to with its own ones, by the kernel for few rows: no parts

@@ -13,6 +13,8 @@
 // vector instructions for half the products: 480 to 505 us, 0.93 to 0.97 PFLOP/s.  8-bit caches: 785 to 815 and 500 to 516 us, the codes are widened on the way to LDS.
 // Weights are rounded to bf16 for the second product, which puts a bf16 output 1.3 to 1.45 times as far from the exact one as rounding alone; as two bf16, which
 // requests of up to 64 rows have (they wait for memory), these chunks would take 1124 us instead of 783, and 712 instead of 494.
+// In groups of requests (SHARED), whose rows may fill blocks, it goes by the request all the same, for each wave: what is served beside a token has no part in how exact
+// its result is (64 steps over 32768 shared rows 72 us instead of 60, 24 questions, three of them short, 219 instead of 207, and 234 were it for each block).
 // The 50 to 75 scalar registers that do not fit are kept in lanes of vector registers and come back between parts: none in a step's instructions.
 // Tried before: waves with 512 registers (the compiler keeps the accumulators in the half that vector instructions do not reach, and copies them); the page
 // table looked up key by key (790 us; as one load per 1024 keys 760).
@@ -216,6 +218,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
   CutBlock cut = {-1, 0, 0, 0};
   int chunk_tile0 = 0, chunk_tile1 = 0, key_low = 0;               // SHARED: the tiles, and the first key of them that counts
   const int group_blocks = SHARED ? ma.sh.many_units : 0;
+  bool short_rows = false;                                        // SHARED: the wave has rows of a request of up to kFewRowsMost
   if constexpr (SHARED) {
     // Units go to the dies in turn, heads and chunks of a block side by side, which mostly are as many as the dies or more: then blocks of one chunk, which read the same keys, are on
     // one die, and no die has the longest requests or groups.
@@ -300,6 +303,18 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
     if (chunk_tile0 >= chunk_tile1) {
       no_parts<kManyThreads>(a, g, g + 1, of.q0, head, block * kManyRows, min(of.rows, block * kManyRows + kManyRows));
       return;
+    }
+    short_rows = shared ? ma.sh.fine == 1 : of.rows <= kFewRowsMost;
+    if (shared && ma.sh.fine == 2) {
+      if (tid == 0) found[3] = 0;                                 // the waves of which it is true
+      __syncthreads();
+      for (int i = r + tid; i < ma.sh.cu_groups[at + 1]; i += kManyThreads) {
+        const int first = (a.b.cu_q[i] - of.q0) * of.G - block * kManyRows, last = (a.b.cu_q[i + 1] - of.q0) * of.G - block * kManyRows - 1;        // its rows in the block
+        if (first <= last && last - first < kFewRowsMost && last >= 0 && first < kManyRows)
+          atomicOr(&found[3], (2 << (min(last, kManyRows - 1) >> 5)) - (1 << (max(first, 0) >> 5)));
+      }
+      __syncthreads();
+      short_rows = uniform(found[3] >> wave) & 1;
     }
   }
 
@@ -428,6 +443,11 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[db][i] = 0.0f;
       f32x16 za, zb;                                               // logits of the first and of the second 32 keys of a tile
+      auto begin = [&]() __attribute__((always_inline)) {
+        __syncthreads();                                           // the segment before is through with LDS
+        if (tid == 0) not_finite = 0;
+      };
+      if constexpr (SHARED) begin();                               // by all waves together: which loop they take is each one's
       // The tiles, with weights rounded to bf16, or (FINE) as two bf16, the rounded one and the rest: what requests of as many rows as the other kernel takes
       // have there, they have here as well, whatever is in the batch with them.
       auto walk = [&](auto two) __attribute__((always_inline)) {
@@ -523,8 +543,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
         };
 
         // ---- before the first tile
-        __syncthreads();                                             // the segment before is through with LDS
-        if (tid == 0) not_finite = 0;
+        if constexpr (!SHARED) begin();
 #pragma unroll
         for (int j = 0; j < (ROWWISE ? 5 : 3); ++j) fetch_entries((ROWWISE ? tile0 : tile0 >> 4) + j);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -596,7 +615,7 @@ __global__ __launch_bounds__(kManyThreads, 2) void attend_many_kernel(const Many
           }
         }
       };
-      if (__builtin_expect(of.rows > kFewRowsMost, 1)) walk(std::false_type{});
+      if (__builtin_expect(SHARED ? !short_rows : of.rows > kFewRowsMost, 1)) walk(std::false_type{});
       else walk(std::true_type{});
       if (active) {
         if (__builtin_expect(partly(tile1 - 1) && not_finite != 0, 0)) {

@@ -9,10 +9,10 @@
 // parts of the shared ones to them, or, for prompts, the kernel for many, in the same launch as the shared rows.  Where all is short nothing is shared: the kernel for few rows
 // takes a request's shared and own rows together.
 //
-// Single tokens wait for memory, and shared rows are read once for all: 64 steps of 28 query heads on 4 KV heads of 128 over 32768 shared rows and up to 700 of their own, 63 us
-// where codecomp_attend over the same caches takes 470 (the shared rows 42, by 448 rows in blocks of 256: 1.33 PFLOP/s of the products that are formed; their own 19, of which
+// Single tokens wait for memory, and shared rows are read once for all: 64 steps of 28 query heads on 4 KV heads of 128 over 32768 shared rows and up to 700 of their own, 72 us
+// where codecomp_attend over the same caches takes 470 (the shared rows 53, by 448 rows in blocks of 256, whose weights are two bf16: half as many products again; their own 19, of which
 // a compute unit reads 32 bytes a ns).  96 steps in eight groups of twelve behind 2001 to 9001 rows, 8 KV heads, 8 bits: 99 us instead of 213.
-// Prompts wait for the matrix units, which sharing takes no work off: 24 of up to 401 tokens in two groups behind 16000 rows, head_dim 64, 208 us instead of 220.
+// Prompts wait for the matrix units, which sharing takes no work off: 24 of up to 401 tokens in two groups behind 16000 rows, head_dim 64, 219 us, as long as codecomp_attend.
 // Four steps behind 2049 rows: 13 us, two launches of dependent waits (codecomp_attend 12).
 // Tried before, kernel for few rows: eight waves a workgroup (four steps 9.5 us instead of 8.7), three blocks of 16 rows (shared rows of 48 rows 52 us instead of 57, but their
 // own ones 69 instead of 62); kernel for many: a loop over units (206 -> 214 us).
@@ -37,15 +37,16 @@ constexpr int64_t kMostSplits = 1024, kMostParts = 1 << 21;       // chunks of a
 // Up to so many keys in all nothing is cut, shared rows are read once for every 16 or 32 rows, and there is nothing to join: one launch (us, with parts | without: 64 steps behind 16
 // rows 10.7 | 7.1, 1024 in groups of 8 behind 300, 8 bits, 133 | 118, 226 tokens behind 47 24 | 12, 1000 requests of up to 20 tokens behind 400 426 | 384; beyond: 8 steps behind 700
 // 11.7 | 15.7, 256 behind 500 and up to 300 of their own 42 | 53, two prompts of 600 tokens 44 | 52).  Not where that is much work, and at least twice as much as the kernel
-// for many rows would have (1024 steps in groups of 128 behind 300 78 | 99).
+// for many rows would have (1024 steps in groups of 128 behind 300 80 | 96).
 constexpr int kAloneKeys = 512;
 constexpr int64_t kAloneStrips = 8192;
 // Empty workgroups that are let pass, beside four for each that is not (a prompt of 400 tokens among steps over 50 rows, us, with the kernel for many rows | mostly empty: 50 steps
 // 41 | 45, 200 68 | 123, 700 145 | 382).
 constexpr int64_t kEmptyBlocks = 4096;
 // Little work, in strips of 128 keys by 32 rows: all of it in one launch of the kernel for few rows, and one that joins (us, one | the kernel for many as well: 64 steps of 7 query
-// heads on 4 KV heads behind 1000 rows, 448 strips, 22 | 28, 2048 25 | 28, 4096 30 | 30; 16 steps behind 8000, 1008 strips, 26.5 | 26, 16000 33 | 30).
-constexpr int64_t kFewStrips = 1024;
+// heads on 4 KV heads behind 2048 rows, 896 strips, 29 | 33, 4096 34.6 | 37.1, 8192 46 | 41; 16 steps behind 16000, 2000 strips, 34.3 | 35.5, 32000 46 | 42; 64 steps behind 4096, 8 KV
+// heads, 8 bits, 2048 strips, 31 | 38; behind 16000, head_dim 64, 2000 strips, 23 | 29).  Less where a request has more than 64 rows, whose weights the kernel for many rounds.
+constexpr int64_t kFewStrips = 2048, kFewStripsRounded = 1024;
 // Groups of 33 to 64 rows: the kernel for few rows reads the shared rows twice, the one for many has most of a block empty, but a tile's keys for all of it at once (us,
 // few | many: one group of 56 rows behind 2000 rows 14 | 23, 8192 24 | 27, 32768 36 | 39; eight behind 2000 to 9000 50 | 45, head_dim 64 31 | 34; 8 bits, 48 rows, 52 | 66:
 // never there).  By keys of all such groups and heads.
@@ -129,18 +130,25 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
     const int64_t rows = (int64_t)(b->cu_q_host[r + 1] - b->cu_q_host[r]) * x.G;
     if (rows > kOwnRows) strips += (rows + 31) / 32 * strips_of(s.max_own);
   }
-  if (strips * x.Hkv <= kFewStrips && alike(x.n_seqs, own_most, own_parts) && alike(s.n_groups, group_most, group_parts)) s.few_rows = INT32_MAX;
+  if (strips * x.Hkv <= (own_most > kFewRowsMost ? kFewStripsRounded : kFewStrips) && alike(x.n_seqs, own_most, own_parts) && alike(s.n_groups, group_most, group_parts)) s.few_rows = INT32_MAX;
   else s.few_rows = middle * x.Hkv * s.max_prefix > (pl->pool.fp8 ? kFewKeys8 : kFewKeys16) ? kFewRows : kFewRowsMost;
+  bool fine = false, rounded = false;              // in groups of many rows: requests of up to 64 rows, of more
   for (int i = 0; i < g->n_groups; ++i) {
     const int64_t rows = (int64_t)(b->cu_q_host[g->cu_groups_host[i + 1]] - b->cu_q_host[g->cu_groups_host[i]]) * x.G;
     if (rows > s.few_rows) {
       ++pl->many_groups;
       blocks += (rows + kManyRows - 1) / kManyRows;
+      for (int r = g->cu_groups_host[i]; r < g->cu_groups_host[i + 1]; ++r) {
+        const int64_t own = (int64_t)(b->cu_q_host[r + 1] - b->cu_q_host[r]) * x.G;
+        if (own > kFewRowsMost) rounded = true;
+        else if (own > 0) fine = true;
+      }
     } else if (rows > 0) {
       ++pl->few_groups;
       few_most = std::max(few_most, rows);
     }
   }
+  s.fine = !fine ? 0 : rounded ? 2 : 1;
   int64_t own_blocks = 0;                          // of rows, if the kernel for many rows has the own ones too
   for (int r = 0; r < x.n_seqs; ++r) {
     const int64_t rows = (int64_t)(b->cu_q_host[r + 1] - b->cu_q_host[r]) * x.G;
@@ -170,8 +178,8 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
   const int few_each = pl->few_two ? 32 : 16, own_each = pl->own_two ? 32 : 16;
 
   // Shared rows, many: chunks for which the last workgroup ends early (rounds of as many as there are compute units, then the requests' own blocks, which fill what the last
-  // round leaves free) and not much is done in all (the chip's clock goes by it).  1, 2, 3, 4, 5 and 8 chunks, us: the 24 questions 251, 268, 208, 225, 215, 237; four prompts of
-  // 200 to 500 tokens behind 8000 rows 211, 224, 245, 250, 276, 303; 32 of 16 tokens behind 4000 94, 59, 63, 75, 73, 94.  Own rows count as three quarters of their bound.
+  // round leaves free) and not much is done in all (the chip's clock goes by it).  1, 2, 3, 4, 5 and 8 chunks, us: the 24 questions 308, 273, 219, 227, 225, 242; four prompts of
+  // 200 to 500 tokens behind 8000 rows 211, 228, 245, 249, 263, 296; 32 of 16 tokens behind 4000 92, 58, 52, 63, 70, 82; 24, 32 and 43: 64 steps behind 32768 rows 75, 72, 96.  Own rows count as three quarters of their bound.
   s.many_splits = s.few_splits = 0;
   if (pl->many_groups > 0) {
     const int tiles = std::max(1, (s.max_prefix + kManyKeys - 1) / kManyKeys);

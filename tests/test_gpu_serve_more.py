@@ -1,0 +1,40 @@
+"""codecomp_attend_shared: how exact the weights of a request are, whatever stands beside it in its group and in the batch."""
+import numpy as np
+import pytest
+import torch
+
+from tests import cache_util as cu_
+from tests.test_gpu_serve import Forked, shared_workspace
+
+pytestmark = pytest.mark.gpu
+
+
+def check_weights(f, causal, max_prefix=None, max_own=None):
+    """Tokens of requests of up to 64 rows against the tolerance of weights of 16 bits, the others' of 8; all rows, shared and own."""
+    from paper_2604_10235_amd import binding as b
+    batch, pages, groups = f.batch(causal=causal), f.cache.pages(), f.groups(max_prefix, max_own)
+    ws, guard = shared_workspace(batch, groups, pages)
+    out, lse = torch.full_like(f.q, 7.0), torch.full((f.T, f.n_q), 7.0, device="cuda")
+    b.codecomp_attend_shared(f.q, batch, groups, pages, 0, out, ws, lse=lse)
+    want = f.want(0, causal)
+    short = np.array([n * f.n_q // f.cache.k.shape[2] <= 64 for n in f.news for _ in range(n)])
+    for these, bits in ((short, 16), (~short, 8)):
+        if these.any():
+            at = torch.from_numpy(these).cuda()
+            cu_.assert_attended(out[at], lse[at], tuple(x[these] for x in want), f.cache.d, bits)
+    assert bool((guard == 0xA5).all())
+    return short
+
+
+# groups of more than 64 rows in all, of single tokens and of some, alone and beside prompts, which begin and end inside of blocks of 256 rows; several groups, some of one request,
+# of none, or of prompts alone
+@pytest.mark.parametrize("members, prefixes, news, n_q, n_kv", [
+    ([30], [700], [1] * 30, 8, 2), ([70], [333], [1, 2, 0] * 23 + [4], 28, 4), ([11], [900], [16] * 11, 8, 2), ([9], [600], [1, 90, 1, 1, 17, 16, 0, 300, 2], 8, 2),
+    ([5, 0, 40, 2], [500, 9, 640, 130], [100, 1, 70, 1, 1] + [1] * 40 + [80, 120], 14, 2), ([3], [1030], [64, 65, 64], 2, 2),
+    ([600], [90], [1] * 300 + [100, 0] + [1] * 298, 4, 2)])
+@pytest.mark.parametrize("fp8, d, page", [(False, 128, 16), (True, 128, 8), (False, 64, 4), (True, 64, 64)])
+@pytest.mark.parametrize("causal, loose", [(True, 0), (True, 70000), (False, 70000)])
+def test_weights_of_short_requests_in_large_groups(members, prefixes, news, n_q, n_kv, fp8, d, page, causal, loose):
+    rng = np.random.default_rng([81, sum(news), d, page])
+    f = Forked(rng, members, prefixes, news, [n + int(rng.integers(0, 90)) for n in news], n_q=n_q, n_kv=n_kv, d=d, page=page, fp8=fp8, loose=loose)
+    assert check_weights(f, causal).any()
