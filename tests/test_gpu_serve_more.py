@@ -38,3 +38,13 @@ def test_weights_of_short_requests_in_large_groups(members, prefixes, news, n_q,
     rng = np.random.default_rng([81, sum(news), d, page])
     f = Forked(rng, members, prefixes, news, [n + int(rng.integers(0, 90)) for n in news], n_q=n_q, n_kv=n_kv, d=d, page=page, fp8=fp8, loose=loose)
     assert check_weights(f, causal).any()
+
+
+# no shared rows, by a bound that lets there be many: all weights are those of own rows
+@pytest.mark.parametrize("members, news, own", [([30], [1] * 30, 400), ([12], [1, 16, 2, 300, 1, 9, 0, 1, 40, 16, 17, 3], 700), ([2, 9], [70, 1] + [8] * 9, 1500)])
+@pytest.mark.parametrize("fp8, d, page", [(False, 128, 16), (True, 64, 8), (False, 64, 128)])
+@pytest.mark.parametrize("causal, loose, max_own", [(True, 70000, None), (True, 70000, 20000), (False, 9000, None)])
+def test_weights_of_own_rows_in_large_groups(members, news, own, fp8, d, page, causal, loose, max_own):
+    rng = np.random.default_rng([82, sum(news), d, page])
+    f = Forked(rng, members, [0] * len(members), news, [n + int(rng.integers(0, own)) for n in news], n_q=8, n_kv=2, d=d, page=page, fp8=fp8, loose=loose)
+    assert check_weights(f, causal, max_own=max_own and min(max_own, loose)).any()
