@@ -34,8 +34,10 @@ struct SharedRows {
   int few_units, few_parts, few_chunk, few_splits;       // shared rows of groups of few rows: workgroups, parts of the rows, keys of a chunk, chunks
   int many_units, many_tiles, many_splits;               // of many: workgroups, tiles of a chunk, chunks
   int fine;                    // of many, weights of the shared rows as two bf16: 0 never, 1 always, 2 in waves with rows of a request of up to kFewRowsMost
-  int splits;                  // the larger one: parts of shared rows that every row has
-  int own_units, own_tiles, own_splits;                  // of many, behind the shared rows: the same, and as many more parts; 0: the kernel for few rows has those
+  int many_tokens, few_tokens; // tokens of groups of each kind; a row has a part for each chunk of its kind's
+  int32_t* place;              // where there are both: of a token among those of its kind, few: ~place (written by the kernel for many rows, which does not need them)
+  int64_t own_base;            // tokens' parts of shared rows, all together; behind them those of the rows behind, chunk by chunk of all tokens
+  int own_units, own_tiles, own_splits;                  // of many, behind the shared rows: the same, and their parts; 0: the kernel for few rows has those
   int alone;                   // 1: everything is short, and a request's shared rows are attended to with its own ones, by the kernel for few rows: no parts
   int join;                    // 1: whoever has a request's own rows joins the parts of the shared ones to them, and writes the outputs
 };
@@ -56,23 +58,27 @@ struct AttendArgs {
   int shares;                  // few rows: equal parts that all keys are cut into; 0: chunks
   CutBlock* cuts;              // [shares]
 };
-// Part p of row t * Hq + h is part_o[(p * T * Hq + row)].
 struct SharedArgs : AttendArgs {
   SharedRows sh;
 };
 
 __device__ __forceinline__ int prefix_of(const SharedRows& sh, int g) { return min(max(sh.prefix_lens[g], 0), sh.max_prefix); }
-// The place of part p of a row among all parts.
-__device__ __forceinline__ int64_t part_at(const AttendArgs& a, int p, int token, int head) { return ((int64_t)p * a.b.T + token) * a.b.Hq + head; }
-// Parts first .. last - 1 of rows row0 .. row1 - 1 of a KV head, which has tokens from q0 on: nothing in them.
+// Parts lie chunk by chunk, all rows of a kind of groups, [chunk][token][head]: part p of a group's token and a head is row_part(first + p * step, token, head).
+struct GroupParts { int64_t first, step; int count; };
+__device__ __forceinline__ GroupParts parts_of_group(const SharedRows& sh, int token) {
+  if (!sh.place) return {0, sh.many_tokens + sh.few_tokens, max(sh.many_splits, sh.few_splits)};
+  const int at = sh.place[token];
+  if (at >= 0) return {at - token, sh.many_tokens, sh.many_splits};
+  return {(int64_t)sh.many_splits * sh.many_tokens + ~at - token, sh.few_tokens, sh.few_splits};
+}
+__device__ __forceinline__ int64_t row_part(const AttendArgs& a, int64_t base, int token, int head) { return (base + token) * a.b.Hq + head; }
+// A part of rows row0 .. row1 - 1 of a KV head, which has tokens from q0 on: nothing in it.
 template <int THREADS>
-__device__ __forceinline__ void no_parts(const AttendArgs& a, int first, int last, int q0, int head, int row0, int row1) {
+__device__ __forceinline__ void no_part(const AttendArgs& a, int64_t base, int q0, int head, int row0, int row1) {
   for (int row = row0 + threadIdx.x; row < row1; row += THREADS) {
     const int t = row / a.b.G, h = head * a.b.G + row - t * a.b.G;
-    for (int p = first; p < last; ++p) {
-      const int64_t part = part_at(a, p, q0 + t, h);
-      a.part_ml[2 * part] = -INFINITY; a.part_ml[2 * part + 1] = kNoPart;
-    }
+    const int64_t part = row_part(a, base, q0 + t, h);
+    a.part_ml[2 * part] = -INFINITY; a.part_ml[2 * part + 1] = kNoPart;
   }
 }
 

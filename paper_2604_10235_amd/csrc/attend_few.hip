@@ -53,20 +53,21 @@ template <int D>
 __device__ __forceinline__ void join_rows(const SharedArgs& a, const float (&own_o)[16][D], const float (&own_ml)[16][2], int q0, int head, int row0, int rows) {
   constexpr int THREADS = D / 4, LOT = 16;
   const int e = threadIdx.x % THREADS * 4;
+  const GroupParts parts = parts_of_group(a.sh, q0);
   for (int n = threadIdx.x / THREADS; n < 16; n += 64 * kFewWaves / THREADS) {
     const int row = row0 + n, t = row / a.b.G, h = head * a.b.G + row - t * a.b.G;
     if (row >= rows) return;
-    const int64_t at = part_at(a, 0, q0 + t, h), step = (int64_t)a.b.T * a.b.Hq;
+    const int64_t at = row_part(a, parts.first, q0 + t, h), step = parts.step * a.b.Hq;
     float top = own_ml[n][0], all = own_ml[n][1];
     f32x4 x = *reinterpret_cast<const f32x4*>(&own_o[n][e]);
-    for (int p0 = 0; p0 < a.sh.splits; p0 += LOT) {
+    for (int p0 = 0; p0 < parts.count; p0 += LOT) {
       f32x4 v[LOT];
       float m[LOT], l[LOT], to = top;
 #pragma unroll
       for (int i = 0; i < LOT; ++i) {
-        const int64_t part = at + min(p0 + i, a.sh.splits - 1) * step;
+        const int64_t part = at + min(p0 + i, parts.count - 1) * step;
         m[i] = a.part_ml[2 * part];
-        l[i] = p0 + i < a.sh.splits ? a.part_ml[2 * part + 1] : kNoPart;
+        l[i] = p0 + i < parts.count ? a.part_ml[2 * part + 1] : kNoPart;
         v[i] = *reinterpret_cast<const f32x4*>(a.part_o + part * D + e);
       }
 #pragma unroll
@@ -86,7 +87,7 @@ __device__ __forceinline__ void join_rows(const SharedArgs& a, const float (&own
     }
     const float inv = all == 0.0f ? 0.0f : a.pool.v_scale / all;
     *reinterpret_cast<u32x2*>(a.out + (q0 + t) * a.b.o_st + h * a.b.o_sh + e) = u32x2{pack2(x.x * inv, x.y * inv), pack2(x.z * inv, x.w * inv)};
-    if (a.lse && e == 0) a.lse[at] = all == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(all)) * kLn2;
+    if (a.lse && e == 0) a.lse[(int64_t)(q0 + t) * a.b.Hq + h] = all == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(all)) * kLn2;
   }
 }
 
@@ -122,7 +123,17 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void atten
   };
   int64_t total = 0, shares = 0, at_strip = 0;
   CutBlock cut = {-1, 0, 0, 0};
-  int shared_q0 = 0, shared_nq = 0, shared_len = 0, shared_part = 0, key_end = 0;        // SHARED: tokens of the group or request, keys up to which there are some, number of the part
+  int shared_q0 = 0, shared_nq = 0, shared_len = 0, key_end = 0;        // SHARED: tokens of the group or request, keys up to which there are some
+  int shared_part = 0;                                           // SHARED 1: number of its part
+  bool shared_own = false;                                       // SHARED 1: of rows behind the shared ones
+  auto part_base = [&]() __attribute__((always_inline)) {
+    if constexpr (SHARED == 1) {
+      if (shared_own) return a.sh.own_base + (int64_t)shared_part * a.b.T;
+      const GroupParts parts = parts_of_group(a.sh, shared_q0);
+      return parts.first + shared_part * parts.step;
+    }
+    return (int64_t)0;
+  };
   int causal = SHARED ? 0 : a.b.causal;
   bool shared_join = false;                                       // these are a request's own rows, and the parts of the shared ones are joined to them
   if constexpr (EVEN) {
@@ -199,7 +210,6 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void atten
       key0 = split * a.sh.few_chunk;
       key_end = key0 + a.sh.few_chunk;
       shared_part = split;
-      if (split == 0) no_parts<64 * kFewWaves>(a, a.sh.few_splits, a.sh.splits, shared_q0, head, row0, min(shared_nq * a.b.G, row0 + 16 * RB));
     } else {
       shared_q0 = a.b.cu_q[r];
       shared_nq = a.b.cu_q[r + 1] - shared_q0;
@@ -208,12 +218,13 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void atten
       shared_len = uniform((int)min((int64_t)kv_len_of(a.b, r), (int64_t)before + a.sh.max_own));
       key0 = (int)min(before + (int64_t)split * a.chunk, (int64_t)INT32_MAX);
       key_end = (int)min((int64_t)key0 + a.chunk, (int64_t)INT32_MAX);
-      shared_part = a.sh.splits + split;
+      shared_part = split;
+      shared_own = true;
       causal = a.b.causal;
       shared_join = a.sh.join != 0;
     }
     if (key0 >= shared_len && (group || !a.sh.join)) {
-      no_parts<64 * kFewWaves>(a, shared_part, shared_part + 1, shared_q0, head, row0, min(shared_nq * a.b.G, row0 + 16 * RB));
+      no_part<64 * kFewWaves>(a, part_base(), shared_q0, head, row0, min(shared_nq * a.b.G, row0 + 16 * RB));
       return;
     }
     table = a.b.table + (int64_t)r * a.b.table_width;
@@ -270,7 +281,7 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void atten
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
         qf[rb][ks] = *reinterpret_cast<const u32x4*>(p + T::q_element(ks, quarter));
-        if (row >= rows) qf[rb][ks] = u32x4{0, 0, 0, 0};
+        if (!SHARED && row >= rows) qf[rb][ks] = u32x4{0, 0, 0, 0};
       }
       limit[rb] = causal ? min(len, len - nq + t + 1) : len;
     }
@@ -309,6 +320,14 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void atten
     unsigned left_out = 0;
     int tile = key0 + wave * kFewKeys;
     if (tile < key1) send_for(tile, page);
+    if constexpr (SHARED != 0) {                                   // rows that are not there; the queries are waited for behind the keys
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int rb = 0; rb < RB; ++rb)
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+          if (row0 + rb * 16 + l16 >= rows) qf[rb][ks] = u32x4{0, 0, 0, 0};
+    }
     for (; tile < key1; tile += kFewWaves * kFewKeys) {
       bool there[2];
 #pragma unroll
@@ -485,7 +504,9 @@ __global__ __launch_bounds__(64 * kFewWaves, RB == 2 || EVEN ? 2 : 3) void atten
           for (int i = 0; i < E; i += 2) *reinterpret_cast<unsigned*>(out + i) = pack2(x[i] * inv, x[i + 1] * inv);
           if (a.lse && (tid & 15) == 0) a.lse[(int64_t)(q0 + t) * a.b.Hq + h] = all == 0.0f ? -INFINITY : (to + __builtin_amdgcn_logf(all)) * kLn2;
         } else {
-          const int64_t part = SHARED ? part_at(a, shared_part, q0 + row / a.b.G, head * a.b.G + row % a.b.G) : part0 + row;
+          int64_t part;
+          if constexpr (SHARED) part = row_part(a, part_base(), q0 + row / a.b.G, head * a.b.G + row % a.b.G);
+          else part = part0 + row;
 #pragma unroll
           for (int i = 0; i < E; i += 4) *reinterpret_cast<f32x4*>(a.part_o + part * D + e + i) = f32x4{x[i], x[i + 1], x[i + 2], x[i + 3]};
           if ((tid & 15) == 0) { a.part_ml[2 * part] = to; a.part_ml[2 * part + 1] = all; }

@@ -125,6 +125,7 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
     return CODECOMP_OK;
   }
   pl->few_groups = pl->many_groups = 0;
+  s.many_tokens = s.few_tokens = 0;
   int64_t strips = group_parts * strips_of(s.max_prefix);        // of the shared rows, and of the own ones of requests that the kernel for many rows would take
   for (int r = 0; r < x.n_seqs; ++r) {
     const int64_t rows = (int64_t)(b->cu_q_host[r + 1] - b->cu_q_host[r]) * x.G;
@@ -137,6 +138,7 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
     const int64_t rows = (int64_t)(b->cu_q_host[g->cu_groups_host[i + 1]] - b->cu_q_host[g->cu_groups_host[i]]) * x.G;
     if (rows > s.few_rows) {
       ++pl->many_groups;
+      s.many_tokens += (int)(rows / x.G);
       blocks += (rows + kManyRows - 1) / kManyRows;
       for (int r = g->cu_groups_host[i]; r < g->cu_groups_host[i + 1]; ++r) {
         const int64_t own = (int64_t)(b->cu_q_host[r + 1] - b->cu_q_host[r]) * x.G;
@@ -145,6 +147,7 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
       }
     } else if (rows > 0) {
       ++pl->few_groups;
+      s.few_tokens += (int)(rows / x.G);
       few_most = std::max(few_most, rows);
     }
   }
@@ -158,7 +161,8 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
   if (!pl->prompts || s.max_own == 0) own_blocks = 0;
   own_blocks *= x.Hkv;
   blocks *= x.Hkv;
-  const int64_t most_splits = std::min(kMostSplits, std::max<int64_t>(8, kMostParts / std::max<int64_t>(1, (int64_t)x.T * x.Hq)));
+  auto most_of = [&](int64_t tokens) { return std::min(kMostSplits, std::max<int64_t>(8, kMostParts / std::max<int64_t>(1, tokens * x.Hq))); };
+  const int64_t most_splits = most_of(x.T);
   double own = 0.0;                                // tiles' worth of time of a chunk of them
   if (own_blocks > 0) {
     // long ones in chunks of a third of what there is to do for a compute unit, at most
@@ -170,7 +174,8 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
     own_blocks *= s.own_splits;
     own = 0.75 * s.own_tiles + kLead;
   }
-  if (blocks + own_blocks > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
+  const int64_t most_units = kMostBlocks - (pl->few_groups > 0 ? kPlacers : 0);
+  if (blocks + own_blocks > most_units) return CODECOMP_EINVAL_SHAPE;
   s.own_units = (int)own_blocks;
   s.join = pl->many_groups > 0 && !pl->prompts && (s.max_own <= kJoinKeys || (s.max_own <= kJoinMost && items * ((own_most + 31) / 32) >= kJoinItems));
   pl->few_two = s.join || pl->prompts ? few_most > 16 : std::max(few_most, own_most) > 16;
@@ -183,10 +188,10 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
   s.many_splits = s.few_splits = 0;
   if (pl->many_groups > 0) {
     const int tiles = std::max(1, (s.max_prefix + kManyKeys - 1) / kManyKeys);
-    const double part = (double)x.T * x.Hq * p->head_dim / kPartElements;
+    const double part = (double)s.many_tokens * x.Hq * p->head_dim / kPartElements;
     int best = 1;
     double least = 0.0;
-    for (int n = 1; n <= std::min(tiles, kChip) && blocks * n + own_blocks <= kMostBlocks; ++n) {
+    for (int n = 1; n <= std::min(tiles, kChip) && blocks * n + own_blocks <= most_units; ++n) {
       const double each = (tiles + n - 1) / n + kLead;
       const int64_t rounds = ((blocks * n + 7) / 8 + kChip / 8 - 1) / (kChip / 8);       // of a die's compute units
       const int64_t left = own_blocks > 0 ? own_blocks - (rounds * kChip - blocks * n) * (int64_t)(each / own) : 0;
@@ -199,7 +204,7 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
     s.many_units = (int)(blocks * s.many_splits);
   }
   // Chunks of keys for `items` that have some, of `all` that there is a workgroup for.
-  auto cut = [&](int64_t items, int64_t all, int most, int64_t largest, int* chunk, int* splits) {
+  auto cut = [&](int64_t items, int64_t all, int most, int64_t largest, int64_t most_splits, int* chunk, int* splits) {
     int64_t keys = (items * most / 512 + 127) / 128 * 128;
     keys = std::min<int64_t>(std::max<int64_t>(keys, 128), largest);
     while ((most + keys - 1) / keys > most_splits || (all * ((most + keys - 1) / keys) > kMostBlocks / 2 && keys < most)) keys *= 2;
@@ -211,13 +216,12 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
   int64_t few_units = 0;
   if (pl->few_groups > 0) {
     const int64_t units = (int64_t)s.n_groups * x.Hkv * s.few_parts;
-    cut((int64_t)pl->few_groups * x.Hkv * s.few_parts, units, s.max_prefix, kFewChunk, &s.few_chunk, &s.few_splits);
+    cut((int64_t)pl->few_groups * x.Hkv * s.few_parts, units, s.max_prefix, kFewChunk, most_of(s.few_tokens), &s.few_chunk, &s.few_splits);
     s.few_splits = std::max(s.few_splits, 1);
     few_units = units * s.few_splits;
     if (few_units > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
   }
   s.few_units = (int)few_units;
-  s.splits = std::max(s.many_splits, s.few_splits);
   // rows behind them
   pl->row_parts = std::max<int>(1, (int)std::min<int64_t>((own_most + own_each - 1) / own_each, INT32_MAX));
   pl->own_units = pl->chunk = pl->own_splits = 0;
@@ -227,28 +231,41 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
       pl->chunk = s.max_own;
       pl->own_splits = 1;
     } else {
-      cut(items * pl->row_parts, items * pl->row_parts, s.max_own, kOwnChunk, &pl->chunk, &pl->own_splits);
+      cut(items * pl->row_parts, items * pl->row_parts, s.max_own, kOwnChunk, most_splits, &pl->chunk, &pl->own_splits);
     }
     pl->own_units = items * pl->row_parts * pl->own_splits;
   }
   if (pl->own_units + few_units > kMostBlocks) return CODECOMP_EINVAL_SHAPE;
-  pl->ws_bytes = x.T == 0 ? 0 : ((size_t)(s.splits + (s.own_units > 0 ? s.own_splits : s.join ? 0 : pl->own_splits)) * x.T * x.Hq * (p->head_dim + 2) * sizeof(float) + 255) & ~(size_t)255;
+  // parts, and where there are groups of both kinds, places of tokens
+  pl->own_parts = s.own_units > 0 ? s.own_splits : s.join ? 0 : pl->own_splits;
+  s.own_base = (int64_t)s.many_splits * s.many_tokens + (int64_t)s.few_splits * s.few_tokens;
+  pl->parts = (s.own_base + (int64_t)pl->own_parts * x.T) * x.Hq;
+  pl->both = s.many_tokens > 0 && s.few_tokens > 0;
+  pl->ws_bytes = x.T == 0 ? 0 : ((size_t)pl->parts * (p->head_dim + 2) * sizeof(float) + (pl->both ? x.T * sizeof(int32_t) : 0) + 255) & ~(size_t)255;
   return CODECOMP_OK;
 }
 
 // A row's parts, those of the shared rows first: GROUPS times D / 4 threads a row, the parts shared out over the groups and these added up in order.
-template <int D, int GROUPS>
-__global__ __launch_bounds__(256) void join_shared_kernel(const AttendArgs a, int parts) {
+// BOTH: there are groups of few rows and of many; else all rows have as many parts, one behind the other.
+template <int D, int GROUPS, bool BOTH>
+__global__ __launch_bounds__(256) void join_shared_kernel(const SharedArgs a, int own_parts) {
   constexpr int THREADS = D / 4, ROWS = 256 / THREADS / GROUPS;
   __shared__ f32x4 sums[GROUPS][ROWS][THREADS];
   __shared__ float tops[GROUPS][ROWS], alls[GROUPS][ROWS];
   const int in = threadIdx.x / THREADS, group = in % GROUPS, slot = in / GROUPS, th = threadIdx.x % THREADS, e = th * 4;
   const int64_t rows = (int64_t)a.b.T * a.b.Hq, row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * ROWS + slot;
   const bool there = row < rows;
+  GroupParts shared = {0, 0, max(a.sh.many_splits, a.sh.few_splits)};
+  if (BOTH && there) shared = parts_of_group(a.sh, (int)(row / a.b.Hq));
+  const int parts = shared.count + own_parts;
+  auto place = [&](int p) __attribute__((always_inline)) {
+    if constexpr (BOTH) return (p < shared.count ? shared.first + p * shared.step : a.sh.own_base + (int64_t)(p - shared.count) * a.b.T) * a.b.Hq + row;
+    return p * rows + row;
+  };
   float top = -INFINITY, all = 0.0f;
   if (there) {
 #pragma unroll 8
-    for (int p = group; p < parts; p += GROUPS) top = fmaxf(top, a.part_ml[2 * (p * rows + row)]);
+    for (int p = group; p < parts; p += GROUPS) top = fmaxf(top, a.part_ml[2 * place(p)]);
   }
   if constexpr (GROUPS > 1) {
     if (th == 0) tops[group][slot] = top;
@@ -260,7 +277,7 @@ __global__ __launch_bounds__(256) void join_shared_kernel(const AttendArgs a, in
   if (there) {
 #pragma unroll 4
     for (int p = group; p < parts; p += GROUPS) {
-      const int64_t part = p * rows + row;
+      const int64_t part = place(p);
       const float m = a.part_ml[2 * part], l = a.part_ml[2 * part + 1];
       const f32x4 v = *reinterpret_cast<const f32x4*>(a.part_o + part * D + e);
       if (l == kNoPart) continue;
@@ -286,10 +303,12 @@ __global__ __launch_bounds__(256) void join_shared_kernel(const AttendArgs a, in
 }
 
 template <int D, int GROUPS>
-static int launch_join(const AttendArgs& a, int parts, hipStream_t stream) {
+static int launch_join(const SharedArgs& a, int own_parts, hipStream_t stream) {
   constexpr int ROWS = 256 / (D / 4) / GROUPS;
   const int64_t blocks = ((int64_t)a.b.T * a.b.Hq + ROWS - 1) / ROWS, width = std::min<int64_t>(blocks, 1 << 20);       // an axis of a grid holds 2^32 threads
-  join_shared_kernel<D, GROUPS><<<dim3((unsigned)width, (unsigned)((blocks + width - 1) / width)), dim3(256), 0, stream>>>(a, parts);
+  const dim3 grid((unsigned)width, (unsigned)((blocks + width - 1) / width));
+  if (a.sh.place) join_shared_kernel<D, GROUPS, true><<<grid, dim3(256), 0, stream>>>(a, own_parts);
+  else join_shared_kernel<D, GROUPS, false><<<grid, dim3(256), 0, stream>>>(a, own_parts);
   return (int)hipGetLastError();
 }
 
@@ -301,10 +320,10 @@ int launch_shared(const SharedPlan& pl, const void* q, int layer, void* out, flo
   a.chunk = pl.chunk; a.row_parts = pl.row_parts;
   a.sh = pl.sh;
   if (pl.sh.alone) return launch_few_shared(pl.d, pl.pool.fp8, pl.own_two, pl.own_units, a, stream);
-  const int parts = pl.sh.splits + (pl.sh.own_units > 0 ? pl.sh.own_splits : pl.sh.join ? 0 : pl.own_splits);
   const int64_t rows = (int64_t)pl.batch.T * pl.batch.Hq;
   a.part_o = static_cast<float*>(workspace);
-  a.part_ml = a.part_o + parts * rows * pl.d;
+  a.part_ml = a.part_o + pl.parts * pl.d;
+  if (pl.both) a.sh.place = reinterpret_cast<int32_t*>(a.part_ml + 2 * pl.parts);
   if (pl.many_groups > 0) {
     ManyArgs m = {};
     m.a = a;
@@ -323,9 +342,9 @@ int launch_shared(const SharedPlan& pl, const void* q, int layer, void* out, flo
   }
   if (pl.sh.few_units + pl.own_units > 0)
     if (int rc = launch_few_shared(pl.d, pl.pool.fp8, pl.few_two, pl.sh.few_units + pl.own_units, a, stream)) return rc;
-  const bool many = parts >= kJoinParts && rows <= kJoinRows;
-  if (pl.d == 128) return many ? launch_join<128, 8>(a, parts, stream) : launch_join<128, 1>(a, parts, stream);
-  return many ? launch_join<64, 16>(a, parts, stream) : launch_join<64, 1>(a, parts, stream);
+  const bool many = std::max(pl.sh.many_splits, pl.sh.few_splits) + pl.own_parts >= kJoinParts && rows <= kJoinRows;
+  if (pl.d == 128) return many ? launch_join<128, 8>(a, pl.own_parts, stream) : launch_join<128, 1>(a, pl.own_parts, stream);
+  return many ? launch_join<64, 16>(a, pl.own_parts, stream) : launch_join<64, 1>(a, pl.own_parts, stream);
 }
 
 }  // namespace codecomp

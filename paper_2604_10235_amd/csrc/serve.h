@@ -24,6 +24,9 @@ struct SharedPlan {
   int few_two, own_two;        // kernel for few rows, shared and own: 32 rows a workgroup, not 16
   int row_parts, chunk, own_splits;    // rows behind the shared ones: parts of a request's rows, keys of a chunk, chunks
   int64_t own_units;
+  int own_parts;               // parts of a row behind the shared ones
+  int64_t parts;               // of all rows
+  bool both;                   // groups of either kind
   size_t ws_bytes;
 };
 int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const codecomp_pages* p, SharedPlan* plan);

@@ -249,3 +249,22 @@ def test_binding_refuses_tensors_that_do_not_fit():
         return
     with pytest.raises(ValueError):           # everything there, but on the CPU
         b.codecomp_evict(m, e, p, i32(1, 2, 2, 8), i32(2))
+
+
+@pytest.mark.parametrize("news, members, prefix, own", [
+    ([1] * 64 + [1], [64, 1], 32768, 700), ([1] * 200 + [1], [200, 1], 32768, 700), ([512, 1], [1, 1], 32768, 700), ([4096] * 16 + [1], [16, 1], 8192, 4096),
+    ([1] + [600] * 4, [1, 2, 2], 20000, 3000), ([1] * 1000 + [90], [4] * 250 + [1], 9000, 300)])
+def test_workspace_of_both_kinds_of_groups_is_that_of_each(news, members, prefix, own):
+    """A group of few rows has as many chunks of its shared rows as it needs, and one of many; neither number is every row's.  Own rows and places of tokens come on top."""
+    cu, cg = np.concatenate([[0], np.cumsum(news)]), np.concatenate([[0], np.cumsum(members)])
+
+    def need(these):
+        """Bytes where only some of the groups have tokens."""
+        host = np.concatenate([[0], np.cumsum([n if these[int(np.searchsorted(cg, r, side="right")) - 1] else 0 for r, n in enumerate(news)])])
+        x = batch(host, table_width=(prefix + own) // 16 + 1, max_kv_len=prefix + own)
+        return b.lib().codecomp_attend_shared_workspace_bytes(ref(x), ref(groups(cg, max_prefix_len=prefix, max_own_len=own)), ref(pool()))
+
+    rows = [7 * int(cu[cg[g + 1]] - cu[cg[g]]) for g in range(len(members))]
+    both, many, few = need([True] * len(members)), need([n > 64 for n in rows]), need([n <= 64 for n in rows])
+    assert many > 0 and few > 0
+    assert both <= 1.25 * (many + few) + 4 * int(cu[-1]) + (1 << 20), (both, many, few)
