@@ -12,8 +12,8 @@
 // Single tokens wait for memory, and shared rows are read once for all: 64 steps of 28 query heads on 4 KV heads of 128 over 32768 shared rows and up to 700 of their own, 72 us
 // where codecomp_attend over the same caches takes 470 (the shared rows 53, by 448 rows in blocks of 256, whose weights are two bf16: half as many products again; their own 19, of which
 // a compute unit reads 32 bytes a ns).  96 steps in eight groups of twelve behind 2001 to 9001 rows, 8 KV heads, 8 bits: 99 us instead of 213.
-// Prompts wait for the matrix units, which sharing takes no work off: 24 of up to 401 tokens in two groups behind 16000 rows, head_dim 64, 219 us, as long as codecomp_attend.
-// Four steps behind 2049 rows: 13 us, two launches of dependent waits (codecomp_attend 12).
+// Prompts wait for the matrix units, which sharing takes no work off: 24 of up to 401 tokens in two groups behind 16000 rows, head_dim 64, 215 us instead of 220.
+// Four steps behind 2049 rows: 12 us, two launches of dependent waits, as in codecomp_attend.
 // Tried before, kernel for few rows: eight waves a workgroup (four steps 9.5 us instead of 8.7), three blocks of 16 rows (shared rows of 48 rows 52 us instead of 57, but their
 // own ones 69 instead of 62); kernel for many: a loop over units (206 -> 214 us).
 #include <float.h>
@@ -63,9 +63,9 @@ constexpr int kOwnRows = 32;
 // 200 of up to 9000 413 | 458).
 constexpr int kJoinKeys = 512, kJoinMost = 8192;
 constexpr int64_t kJoinItems = 192;
-// The kernel that joins: several groups of threads a row, for many parts and few rows (us, one | eight: four steps 20 | 13, eight behind 32768 rows 63 | 36; 1024 steps of 32768
-// rows in all 132 | 149).
-constexpr int kJoinParts = 6;
+// The kernel that joins: several groups of threads a row, for many parts and few rows (us, one | eight: four steps of 18 parts 14.3 | 12.3, one behind 32768 rows 39 | 23, eight 41 |
+// 33, 64 of 10 parts 23 | 23, 96 of 7 parts 99 | 101; 32 requests of 16 tokens, 14336 rows of 4 parts, 51 | 58).
+constexpr int kJoinParts = 8;
 constexpr int64_t kJoinRows = 16384;
 // Chunks of shared rows for the kernel for many: the time of a tile is the unit.  A chunk starts and ends in 5 of them (8.6 us of 1.6 each at head_dim 128), and what it leaves
 // goes through memory twice: 600000 elements in a tile's time.
@@ -262,33 +262,50 @@ __global__ __launch_bounds__(256) void join_shared_kernel(const SharedArgs a, in
     if constexpr (BOTH) return (p < shared.count ? shared.first + p * shared.step : a.sh.own_base + (int64_t)(p - shared.count) * a.b.T) * a.b.Hq + row;
     return p * rows + row;
   };
+  // Parts come from memory (other dies wrote them): a lot is sent for before one of it is looked at, and the reference moves on from lot to lot.
+  constexpr int LOT = 4;
   float top = -INFINITY, all = 0.0f;
+  f32x4 x = {0, 0, 0, 0};
   if (there) {
-#pragma unroll 8
-    for (int p = group; p < parts; p += GROUPS) top = fmaxf(top, a.part_ml[2 * place(p)]);
+    for (int p0 = group; p0 < parts; p0 += LOT * GROUPS) {
+      float2 ml[LOT];
+      f32x4 v[LOT];
+      float to = top;
+#pragma unroll
+      for (int i = 0; i < LOT; ++i) {
+        const int64_t part = place(min(p0 + i * GROUPS, parts - 1));
+        ml[i] = *reinterpret_cast<const float2*>(a.part_ml + 2 * part);
+        v[i] = *reinterpret_cast<const f32x4*>(a.part_o + part * D + e);
+      }
+#pragma unroll
+      for (int i = 0; i < LOT; ++i) {
+        if (p0 + i * GROUPS >= parts) ml[i] = float2{-INFINITY, kNoPart};
+        to = fmaxf(to, ml[i].x);
+      }
+      const float old = to == top ? 1.0f : __builtin_amdgcn_exp2f(top - to);
+      top = to;
+      x *= old;
+      all *= old;
+#pragma unroll
+      for (int i = 0; i < LOT; ++i) {
+        const float f = ml[i].x == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml[i].x - to);       // times zeros, or an infinity or NaN that it saw
+        const bool some = ml[i].y != kNoPart;
+        all += some ? f * ml[i].y : 0.0f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] += some ? f * v[i][k] : 0.0f;
+      }
+    }
   }
   if constexpr (GROUPS > 1) {
     if (th == 0) tops[group][slot] = top;
     __syncthreads();
+    float to = top;
 #pragma unroll
-    for (int g = 0; g < GROUPS; ++g) top = fmaxf(top, tops[g][slot]);
-  }
-  f32x4 x = {0, 0, 0, 0};
-  if (there) {
-#pragma unroll 4
-    for (int p = group; p < parts; p += GROUPS) {
-      const int64_t part = place(p);
-      const float m = a.part_ml[2 * part], l = a.part_ml[2 * part + 1];
-      const f32x4 v = *reinterpret_cast<const f32x4*>(a.part_o + part * D + e);
-      if (l == kNoPart) continue;
-      const float f = m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m - top);       // times zeros, or an infinity or NaN that it saw
-      all += l * f;
-      x += v * f;
-    }
-  }
-  if constexpr (GROUPS > 1) {
-    sums[group][slot][th] = x;
-    if (th == 0) alls[group][slot] = all;
+    for (int g = 0; g < GROUPS; ++g) to = fmaxf(to, tops[g][slot]);
+    const float f = to == top ? 1.0f : __builtin_amdgcn_exp2f(top - to);
+    top = to;
+    sums[group][slot][th] = x * f;
+    if (th == 0) alls[group][slot] = all * f;
     __syncthreads();
     if (group > 0) return;
     x = sums[0][slot][th]; all = alls[0][slot];
