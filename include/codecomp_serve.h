@@ -76,11 +76,13 @@ size_t codecomp_attend_mass_workspace_bytes(const codecomp_batch* batch, const c
  * over its new tokens t that see row j (as in codecomp_attend) and the G query heads h of the KV head: the attention mass u(j) of
  * codecomp_score, mean over the heads.  lse is what codecomp_attend or codecomp_attend_shared has left for the same batch (or any other f32 [T][n_q_heads], dense, e.g. one
  * joined over several caches); a token and head whose lse is -inf gives no weight.  Old rows are those before the new tokens
- * (j < kv_lens[r] - (cu_q[r + 1] - cu_q[r])) when causal, and all rows otherwise; sums of rows that are not old are not read: they need no clearing.  decay
- * in [0, 1]; 0 reads no sums.  Rows of pages that are not held get no weight; rows outside of first[r] .. kv_lens[r] - 1, and all of a request
- * without new tokens, stay as they are.  first: DEVICE int32 [n_seqs] (below 0 counts as 0), NULL = 0.
+ * (j < kv_lens[r] - (cu_q[r + 1] - cu_q[r])) when causal, and all rows otherwise; sums of rows that are not old are not read: they need no clearing when causal.  Without
+ * the mask no row is known to be new: the caller clears the sums of rows that it appends, also where evicted ones stood.  decay in [0, 1]; 0 reads no sums.
+ * Rows of pages that are not held get no weight; rows outside of first[r] .. kv_lens[r] - 1, and all of a request without new tokens, stay as they are.
+ * first: DEVICE int32 [n_seqs] (below 0 counts as 0), NULL = 0.
  * The batch's max_kv_len is at most the width, its n_seqs that of the sums.  Weights and sums are fp32; every sum has a fixed order.
- * An infinity or NaN in a key or query makes the sums of the rows that it meets NaN or infinite, and no others.
+ * What an infinity or NaN in a key, a query or lse makes of a weight - NaN, infinite, or zero where z - lse is minus infinity - the sum of that row becomes; no other
+ * sum changes.
  * workspace: >= codecomp_attend_mass_workspace_bytes(), 256-byte aligned, contents on entry do not matter; NULL when that is 0. */
 int codecomp_attend_mass(const void* q, const float* lse, const codecomp_batch* batch, const codecomp_pages* pages, int32_t layer, const int32_t* first,
                          float decay, const codecomp_mass* mass, void* workspace, size_t workspace_bytes, void* hip_stream);
@@ -104,7 +106,7 @@ typedef struct codecomp_eviction {
  * of the largest sums (equal ones: the lower row; ordered as IEEE floats, -0 == +0, NaN below everything else) - and move together:
  *   row f + i = row kept[l][r][h][i], K and V bit for bit, and kept_mass[l][r][h][f + i] = mass[l][r][h][kept[l][r][h][i]],  i < m,
  * with kept ascending, -1 from m on (DEVICE int32 [n_layers][n_seqs][n_kv_heads][max_budget], dense), and new_lens[r] = f + m (DEVICE int32 [n_seqs]).  Rows of K and V, and
- * sums, from f + m on stay as they are (codecomp_attend_mass does not read sums of new rows).  kept_mass NULL: `mass` itself; else sums of the same shape
+ * sums, from f + m on stay as they are (of causal batches codecomp_attend_mass does not read them; before others, clear the sums of the rows that come there).  kept_mass NULL: `mass` itself; else sums of the same shape
  * elsewhere, and `mass` stays as it is.  new_lens must not be kv_lens, budgets or first.  A row that moves from a page that is not held becomes zeros, one that moves to such a
  * page is dropped.  mass->n_layers and n_kv_heads are the pool's, n_seqs the eviction's, width at least max_kv_len. */
 int codecomp_evict(const codecomp_mass* mass, const codecomp_eviction* eviction, const codecomp_pages* pages, int32_t* kept, int32_t* new_lens,
