@@ -35,32 +35,33 @@ constexpr int kChip = 256;                       // compute units: workgroups of
 constexpr int64_t kMostBlocks = (1 << 23) - 1;    // of up to 512 threads: an axis of a grid holds 2^32 threads
 constexpr int64_t kMostSplits = 1024, kMostParts = 1 << 21;       // chunks of a request's keys; of all rows together, where there are more than eight chunks: workspace
 // Up to so many keys in all nothing is cut, shared rows are read once for every 16 or 32 rows, and there is nothing to join: one launch (us, with parts | without: 64 steps behind 16
-// rows 10.7 | 7.1, 1024 in groups of 8 behind 300, 8 bits, 133 | 118, 226 tokens behind 47 24 | 12, 1000 requests of up to 20 tokens behind 400 426 | 384; beyond: 8 steps behind 700
-// 11.7 | 15.7, 256 behind 500 and up to 300 of their own 42 | 53, two prompts of 600 tokens 44 | 52).  Not where that is much work, and at least twice as much as the kernel
-// for many rows would have (1024 steps in groups of 128 behind 300 80 | 96).
+// rows 12.0 | 7.3, 1024 in groups of 8 behind 300, 8 bits, 128 | 116, 226 tokens behind 47 23 | 12, 1000 requests of up to 20 tokens behind 400, head_dim 64, 195 | 129; beyond: 8
+// steps behind 700 12.8 | 14.6, 256 behind 500 and up to 300 of their own 41 | 51, two prompts of 600 tokens behind 600 50 | 79).  Not where that is much work, and at least twice as
+// much as the kernel for many rows would have (1024 steps in groups of 128 behind 300 82 | 96).
 constexpr int kAloneKeys = 512;
 constexpr int64_t kAloneStrips = 8192;
-// Empty workgroups that are let pass, beside four for each that is not (a prompt of 400 tokens among steps over 50 rows, us, with the kernel for many rows | mostly empty: 50 steps
-// 41 | 45, 200 68 | 123, 700 145 | 382).
+// Empty workgroups that are let pass, beside four for each that is not (a prompt of 400 tokens among steps over 50 rows, 30 of them shared, us, with the kernel for many rows | mostly
+// empty: 50 steps 33 | 40, 200 46 | 121, 700 127 | 390).
 constexpr int64_t kEmptyBlocks = 4096;
 // Little work, in strips of 128 keys by 32 rows: all of it in one launch of the kernel for few rows, and one that joins (us, one | the kernel for many as well: 64 steps of 7 query
 // heads on 4 KV heads behind 2048 rows, 896 strips, 29 | 33, 4096 34.6 | 37.1, 8192 46 | 41; 16 steps behind 16000, 2000 strips, 34.3 | 35.5, 32000 46 | 42; 64 steps behind 4096, 8 KV
 // heads, 8 bits, 2048 strips, 31 | 38; behind 16000, head_dim 64, 2000 strips, 23 | 29).  Less where a request has more than 64 rows, whose weights the kernel for many rounds.
 constexpr int64_t kFewStrips = 2048, kFewStripsRounded = 1024;
 // Groups of 33 to 64 rows: the kernel for few rows reads the shared rows twice, the one for many has most of a block empty, but a tile's keys for all of it at once (us,
-// few | many: one group of 56 rows behind 2000 rows 14 | 23, 8192 24 | 27, 32768 36 | 39; eight behind 2000 to 9000 50 | 45, head_dim 64 31 | 34; 8 bits, 48 rows, 52 | 66:
-// never there).  By keys of all such groups and heads.
+// few | many: one group of 56 rows behind 2000 rows 13 | 23, 8192 21 | 28, 32768 33 | 39; eight behind 2000 to 9000 51 | 45, of 64 rows at head_dim 64 31 | 36; 8 bits, 48 rows, 99 |
+// 118: never there).  By keys of all such groups and heads.
 constexpr int kFewRows = 32;
 constexpr int64_t kFewKeys8 = INT64_MAX, kFewKeys16 = 1 << 17;
 // Most keys of a chunk in the kernel for few rows, shared and own (us, eight groups of 48 rows behind 9001: 512 77, 1024 65, 2048 57, 4096 57; 96 requests' own 2000: 512 96, 1024 85,
 // 2048 88; of 20 to 2000: 66, 61, 62).
 constexpr int kFewChunk = 2048, kOwnChunk = 1024;
-// Requests of more rows: what they have behind the shared ones is the kernel for many rows' too, once that runs (us, few | many: 8 tokens of 7 query heads over 100 to 1000 rows,
-// 32 requests, 59 | 43, 14: 82 | 59, 18: 86 | 61; 16 prompts of up to 512 over up to 2500: 603 | 299; 4 tokens 50 | 40, but at head_dim 64, 6 tokens of 4 over up to 2000, 37 | 44).
+// Requests of more rows: what they have behind the shared ones is the kernel for many rows' too, once that runs (us, few | many: 8 tokens of 7 query heads over 100 to 1000 rows
+// behind 2000, 32 requests, 59 | 47, 14: 71 | 42, 18: 73 | 43; 16 prompts of up to 512 over up to 2500: 856 | 281; 4 tokens 51 | 45, but at head_dim 64, 6 tokens of 4 over up to 2000,
+// 38 | 56).
 constexpr int kOwnRows = 32;
 // Otherwise one workgroup has a request's own rows, and joins, where they are short or where there are enough of these, else chunks do and a kernel that joins (us, chunks |
-// one: 16 requests of 4 heads, up to 300 rows, 27 | 26, up to 2000 40 | 57; 64 of up to 4000 100 | 96, of 8000 225 | 211, of up to 16000 283 | 284; 128 of up to 1000 78 | 74;
-// 200 of up to 9000 413 | 458).
+// one: 16 requests of 4 heads, up to 300 rows, 25 | 26, up to 2000 39 | 58; 64 of up to 4000 94 | 100, of 8000 227 | 215, of up to 16000 230 | 276; 128 of up to 1000 88 | 85;
+// 200 of up to 9000 432 | 446).
 constexpr int kJoinKeys = 512, kJoinMost = 8192;
 constexpr int64_t kJoinItems = 192;
 // The kernel that joins: several groups of threads a row, for many parts and few rows (us, one | eight: four steps of 18 parts 14.3 | 12.3, one behind 32768 rows 39 | 23, eight 41 |
@@ -71,8 +72,8 @@ constexpr int64_t kJoinRows = 16384;
 // goes through memory twice: 600000 elements in a tile's time.
 constexpr double kLead = 5.0, kPartElements = 600000.0;
 // Of the own rows of prompts: a third of what a compute unit has to do in all, and 2048 keys at least (with the tile that the shared ones end in; us, whole | in chunks: 512 tokens over
-// 60000 own rows 1080 | 447, 8 requests of up to 300 over 300 to 30000 691 | 527; with halves of the work 427, 725, before they went to the dies in turn; 100 tokens over 4000
-// with chunks of 24 | 40 tiles 47 | 65, but 48 requests of 14 over up to 2000, 8 bits, head_dim 64, 62 | 51).
+// 60000 own rows 1097 | 455, 8 requests of up to 300 over 300 to 30000 592 | 562; with halves of the work 427, 725, before they went to the dies in turn; 100 tokens over 4000
+// with chunks of 24 | 33 | 40 tiles 46 | 57 | 64, but 48 requests of 14 over up to 2000, 8 bits, head_dim 64, with 24 | 40 62 | 51).
 constexpr double kOwnTiles = 33.0;
 
 int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const codecomp_pages* p, SharedPlan* pl) {
