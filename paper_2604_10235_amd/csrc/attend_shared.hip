@@ -9,9 +9,9 @@
 // parts of the shared ones to them, or, for prompts, the kernel for many, in the same launch as the shared rows.  Where all is short nothing is shared: the kernel for few rows
 // takes a request's shared and own rows together.
 //
-// Single tokens wait for memory, and shared rows are read once for all: 64 steps of 28 query heads on 4 KV heads of 128 over 32768 shared rows and up to 700 of their own, 72 us
-// where codecomp_attend over the same caches takes 470 (the shared rows 53, by 448 rows in blocks of 256, whose weights are two bf16: half as many products again; their own 19, of which
-// a compute unit reads 32 bytes a ns).  96 steps in eight groups of twelve behind 2001 to 9001 rows, 8 KV heads, 8 bits: 99 us instead of 213.
+// Single tokens wait for memory, and shared rows are read once for all: 64 steps of 28 query heads on 4 KV heads of 128 over 32768 shared rows and up to 700 of their own, 73 us
+// where codecomp_attend over the same caches takes 470 (the shared rows 54, by 448 rows in blocks of 256, whose weights are two bf16: half as many products again; their own 20, of which
+// a compute unit reads 32 bytes a ns).  96 steps in eight groups of twelve behind 2001 to 9001 rows, 8 KV heads, 8 bits: 99 us instead of 219.
 // Prompts wait for the matrix units, which sharing takes no work off: 24 of up to 401 tokens in two groups behind 16000 rows, head_dim 64, 215 us instead of 220.
 // Four steps behind 2049 rows: 12 us, two launches of dependent waits, as in codecomp_attend.
 // Tried before, kernel for few rows: eight waves a workgroup (four steps 9.5 us instead of 8.7), three blocks of 16 rows (shared rows of 48 rows 52 us instead of 57, but their
