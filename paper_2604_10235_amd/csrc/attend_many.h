@@ -14,7 +14,7 @@
 // Weights are rounded to bf16 for the second product, which puts a bf16 output 1.3 to 1.45 times as far from the exact one as rounding alone; as two bf16, which
 // requests of up to 64 rows have (they wait for memory), these chunks would take 1124 us instead of 783, and 712 instead of 494.
 // In groups of requests (SHARED), whose rows may fill blocks, it goes by the request all the same, for each wave: what is served beside a token has no part in how exact
-// its result is (64 steps over 32768 shared rows 72 us instead of 60, 24 questions, three of them short, 219 instead of 207, and 234 were it for each block).
+// its result is (64 steps over 32768 shared rows 74 us instead of 63, 24 questions, three of them short, 223 instead of 210, and 16 more were it for each block).
 // The 50 to 75 scalar registers that do not fit are kept in lanes of vector registers and come back between parts: none in a step's instructions.
 // Tried before: waves with 512 registers (the compiler keeps the accumulators in the half that vector instructions do not reach, and copies them); the page
 // table looked up key by key (790 us; as one load per 1024 keys 760).

@@ -12,7 +12,7 @@
 // Single tokens wait for memory, and shared rows are read once for all: 64 steps of 28 query heads on 4 KV heads of 128 over 32768 shared rows and up to 700 of their own, 73 us
 // where codecomp_attend over the same caches takes 470 (the shared rows 54, by 448 rows in blocks of 256, whose weights are two bf16: half as many products again; their own 20, of which
 // a compute unit reads 32 bytes a ns).  96 steps in eight groups of twelve behind 2001 to 9001 rows, 8 KV heads, 8 bits: 99 us instead of 219.
-// Prompts wait for the matrix units, which sharing takes no work off: 24 of up to 401 tokens in two groups behind 16000 rows, head_dim 64, 215 us instead of 220.
+// Prompts wait for the matrix units, which sharing takes no work off: 24 of up to 401 tokens in two groups behind 16000 rows, head_dim 64, 215 to 223 us, codecomp_attend 220.
 // Four steps behind 2049 rows: 12 us, two launches of dependent waits, as in codecomp_attend.
 // Tried before, kernel for few rows: eight waves a workgroup (four steps 9.5 us instead of 8.7), three blocks of 16 rows (shared rows of 48 rows 52 us instead of 57, but their
 // own ones 69 instead of 62); kernel for many: a loop over units (206 -> 214 us).
@@ -184,8 +184,8 @@ int make_shared_plan(const codecomp_batch* b, const codecomp_groups* g, const co
   const int few_each = pl->few_two ? 32 : 16, own_each = pl->own_two ? 32 : 16;
 
   // Shared rows, many: chunks for which the last workgroup ends early (rounds of as many as there are compute units, then the requests' own blocks, which fill what the last
-  // round leaves free) and not much is done in all (the chip's clock goes by it).  1, 2, 3, 4, 5 and 8 chunks, us: the 24 questions 308, 273, 219, 227, 225, 242; four prompts of
-  // 200 to 500 tokens behind 8000 rows 211, 228, 245, 249, 263, 296; 32 of 16 tokens behind 4000 92, 58, 52, 63, 70, 82; 24, 32 and 43: 64 steps behind 32768 rows 75, 72, 96.  Own rows count as three quarters of their bound.
+  // round leaves free) and not much is done in all (the chip's clock goes by it).  1, 2, 3, 4, 5 and 8 chunks, us: the 24 questions 307, 273, 223, 228, 228, 245; four prompts of
+  // 200 to 500 tokens behind 8000 rows 217, 234, 253, 256, 268, 304; 32 of 16 tokens behind 4000 92, 58, 53, 65, 65, 79; 24, 32 and 43: 64 steps behind 32768 rows 77, 74, 97.  Own rows count as three quarters of their bound.
   s.many_splits = s.few_splits = 0;
   if (pl->many_groups > 0) {
     const int tiles = std::max(1, (s.max_prefix + kManyKeys - 1) / kManyKeys);
